@@ -367,6 +367,62 @@ int dr_regress_shard_grads(const dr_conv_desc* desc, int B, int batch, int H, in
                            const void* w_bf16, const float* b, void* y, void* dz, float* dw, float* db, float* loss,
                            void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- layer normalisation ---------------------------------------------------------------
+ * Each pixel (row) of C channels is normalised by its own mean and variance:
+ *   y = (x - mean) * rstd * gamma + beta,   rstd = 1 / sqrt(var + eps),   var = sum (x - mean)^2 / C.
+ *  x: npix rows of C channels, row r at x + r*ldx elements (ldx = 0: dense, C); the same for y.  x (and dx) are
+ *  bfloat16, or float32 with DR_LN_X_F32; y (and dy) bfloat16, or float32 with DR_LN_Y_F32.  gamma, beta: float32 [C],
+ *  or NULL (1 and 0).  mean, rstd: float32 [npix], or NULL where no backward pass follows.  y may be x itself (same
+ *  type and ldx = ldy).  Sums are float32: the mean first, then the squared distances from it.  Any C; rows need
+ *  only their type's alignment, and 16-byte aligned rows of a multiple of 8 channels take 16-byte accesses.
+ *  A row that holds a NaN or an infinity gives a row of NaN and touches no other row.
+ * Errors: INVALID_ARG (nulls, C <= 0, ld < C, eps < 0, unknown flags), ALIGNMENT.                                    */
+#define DR_LN_X_F32 0x1u
+#define DR_LN_Y_F32 0x2u
+int dr_layernorm(size_t npix, int C, const void* x, int ldx, const float* gamma, const float* beta, float eps, void* y,
+                 int ldy, float* mean, float* rstd, unsigned flags, void* stream);
+/* The gradients, from the statistics the forward pass wrote.  With t = dy * gamma and xhat = (x - mean) * rstd,
+ *   dx = rstd * (t - mean_c(t) - xhat * mean_c(t * xhat)),   dgamma = sum_rows dy * xhat,   dbeta = sum_rows dy.
+ *  dx may be dy or x itself (same type and ld).  dgamma, dbeta: float32 [C], overwritten, or NULL; both NULL: no
+ *  workspace is needed.  Sums over the rows are taken in a fixed order: the same result on every run.
+ *  workspace: dr_layernorm_bwd_workspace_bytes(npix, C) bytes, 256-byte aligned, contents irrelevant.
+ *  npix = 0 writes zeros to dgamma and dbeta.
+ * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE.                                                                         */
+int dr_layernorm_bwd_workspace_bytes(size_t npix, int C, size_t* bytes);
+int dr_layernorm_bwd(size_t npix, int C, const void* dy, int lddy, const void* x, int ldx, const float* gamma,
+                     const float* mean, const float* rstd, void* dx, int lddx, float* dgamma, float* dbeta,
+                     void* workspace, size_t workspace_bytes, unsigned flags, void* stream);
+
+/* ---- orthogonalised updates -------------------------------------------------------------
+ * For each of `batch` dense matrices U [rows][cols], by Newton-Schulz products,
+ *   X = U / (|U|_F + eps);   `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X;   O = X
+ * (on the transpose where rows > cols), which moves every singular value of U towards 1 and keeps its singular vectors.
+ *  coef: NULL (a, b, c = 3.4445, -4.7750, 2.0315 in every step), or 3 * steps host floats, read before the call returns.
+ *  steps <= DR_NS_MAX_STEPS, rows and cols <= DR_NS_MAX_DIM, batch <= 65535.
+ *  The products take operands of 11 significant bits (the term a X and the diagonals of A and of b A + c A A: 22 or
+ *  more) and sum in float32: the relative error of O is below 1e-3, under half of its rounding to bfloat16.
+ *  The values of A and of the polynomial must stay below 65504: with coefficients that let X grow past that, O is not finite.
+ *  An all-zero U gives zeros (eps > 0); a matrix with a NaN or an infinity gives NaN and touches no other matrix.
+ * dr_orthogonalise: g bfloat16, or float32 with DR_NS_G_F32; o bfloat16; both [batch][rows][cols].
+ *  workspace: dr_orthogonalise_workspace_bytes bytes, 256-byte aligned, contents irrelevant; calls that may overlap on
+ *  the GPU need their own.
+ * Errors: INVALID_ARG, UNSUPPORTED (the limits above), ALIGNMENT, WORKSPACE, CUDA.                                   */
+#define DR_NS_G_F32     0x1u
+#define DR_NS_MAX_STEPS 16
+#define DR_NS_MAX_DIM   65536
+int dr_orthogonalise_workspace_bytes(int batch, int rows, int cols, size_t* bytes);
+int dr_orthogonalise(int batch, int rows, int cols, const void* g, int steps, const float* coef, float eps, void* o,
+                     void* workspace, size_t workspace_bytes, unsigned flags, void* stream);
+/* One step of an optimiser that applies orthogonalised momentum, the counterpart of dr_sgd_update for filter banks
+ * (w is [Cout][k*k*Cin]) and other matrices:
+ *   v <- momentum * v + g;   U = nesterov ? g + momentum * v : v;   O as above;
+ *   w <- w - lr * (sqrt(max(1, rows/cols)) * O + decay * w).
+ *  w, v, g: float32 [batch][rows][cols], w and v updated in place; w_bf16: NULL, or bfloat16 of the same extents, the
+ *  updated w rounded to nearest even.  Workspace and errors as dr_orthogonalise.                                     */
+int dr_muon_update(int batch, int rows, int cols, float* w, float* v, const float* g, float lr, float momentum,
+                   float decay, int nesterov, int steps, const float* coef, float eps, void* w_bf16, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
 /* Kernels of this library launched by this process so far. */
 long long dr_launch_count(void);
 /* Tensor maps (TMA descriptors) the library has had the driver encode so far.  Maps are remembered by the arguments

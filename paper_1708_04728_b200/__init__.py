@@ -32,6 +32,7 @@ DR_PATH_AUTO, DR_PATH_SIMT, DR_PATH_UMMA_GATHER, DR_PATH_UMMA_TMA, DR_PATH_UMMA_
 DR_PATH_UMMA_SPLITK = 8
 DR_PATH_UMMA_QLIN = 9
 DR_CONV_WS_COUNTER_BYTES = 1024
+DR_LN_X_F32, DR_LN_Y_F32, DR_NS_G_F32, DR_NS_MAX_STEPS, DR_NS_MAX_DIM = 0x1, 0x2, 0x1, 16, 65536
 PATH_NAMES = {0: "auto", 1: "simt", 2: "umma_gather", 3: "umma_tma", 4: "umma_patch", 5: "umma_stem", 6: "retired", 7: "umma_stem_d",
               8: "umma_splitk", 9: "umma_qlin", -1: "-"}
 
@@ -82,6 +83,12 @@ _SIGS = {
     "dr_sgd_update": (_I, [_Z, _P, _P, _P, _F, _F, _F, _P, _P]),
     "dr_regress_step_workspace_bytes": (_I, [C.POINTER(dr_conv_desc), _I, _I, _I, C.POINTER(_Z)]),
     "dr_regress_step": (_I, [C.POINTER(dr_conv_desc), _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _F, _F, _F, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "dr_layernorm": (_I, [_Z, _I, _P, _I, _P, _P, _F, _P, _I, _P, _P, C.c_uint, _P]),
+    "dr_layernorm_bwd_workspace_bytes": (_I, [_Z, _I, C.POINTER(_Z)]),
+    "dr_layernorm_bwd": (_I, [_Z, _I, _P, _I, _P, _I, _P, _P, _P, _P, _I, _P, _P, _P, _Z, C.c_uint, _P]),
+    "dr_orthogonalise_workspace_bytes": (_I, [_I, _I, _I, C.POINTER(_Z)]),
+    "dr_orthogonalise": (_I, [_I, _I, _I, _P, _I, C.POINTER(_F), _F, _P, _P, _Z, C.c_uint, _P]),
+    "dr_muon_update": (_I, [_I, _I, _I, _P, _P, _P, _F, _F, _F, _I, _I, C.POINTER(_F), _F, _P, _P, _Z, _P]),
     "dr_conv_workspace_bytes": (_I, [C.POINTER(dr_conv_desc), _I, _I, _I, C.POINTER(_Z)]),
     "dr_conv_slim_ws": (_I, [C.POINTER(dr_conv_desc), _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "dr_inception_workspace_bytes": (_I, [C.POINTER(dr_inception_desc), _I, _I, _I, C.POINTER(_Z)]),
@@ -226,6 +233,48 @@ def dr_regress_grad_shard(B, batch, H, W, Cc, y, yt, relu, dz, db, loss, workspa
 def dr_regress_shard_grads(desc, B, batch, H, W, x, yt, w_bf16, b, y, dz, dw, db, loss, workspace, workspace_bytes, stream=None):
     _check(_lib.dr_regress_shard_grads(C.byref(desc), B, batch, H, W, _ptr(x), _ptr(yt), _ptr(w_bf16), _ptr(b), _ptr(y), _ptr(dz), _ptr(dw),
                                        _ptr(db), _ptr(loss), _ptr(workspace), workspace_bytes, _stream(stream)), "dr_regress_shard_grads")
+
+
+def dr_layernorm(npix, Cc, x, ldx, gamma, beta, eps, y, ldy, mean=None, rstd=None, flags=0, stream=None):
+    _check(_lib.dr_layernorm(npix, Cc, _ptr(x), ldx, _ptr(gamma), _ptr(beta), eps, _ptr(y), ldy, _ptr(mean), _ptr(rstd), flags,
+                             _stream(stream)), "dr_layernorm")
+
+
+def dr_layernorm_bwd_workspace_bytes(npix, Cc) -> int:
+    n = _Z(0)
+    _check(_lib.dr_layernorm_bwd_workspace_bytes(npix, Cc, C.byref(n)), "dr_layernorm_bwd_workspace_bytes")
+    return n.value
+
+
+def dr_layernorm_bwd(npix, Cc, dy, lddy, x, ldx, gamma, mean, rstd, dx, lddx, dgamma, dbeta, workspace, workspace_bytes, flags=0, stream=None):
+    _check(_lib.dr_layernorm_bwd(npix, Cc, _ptr(dy), lddy, _ptr(x), ldx, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx), lddx, _ptr(dgamma),
+                                 _ptr(dbeta), _ptr(workspace), workspace_bytes, flags, _stream(stream)), "dr_layernorm_bwd")
+
+
+def dr_orthogonalise_workspace_bytes(batch, rows, cols) -> int:
+    n = _Z(0)
+    _check(_lib.dr_orthogonalise_workspace_bytes(batch, rows, cols, C.byref(n)), "dr_orthogonalise_workspace_bytes")
+    return n.value
+
+
+def _coef(coef, steps):
+    """3 * steps host floats (a, b, c of each step), or None for the library's own."""
+    if coef is None:
+        return None
+    flat = [float(c) for c in coef]
+    if len(flat) != 3 * steps:
+        raise ValueError(f"coef holds {len(flat)} values: 3 for each of {steps} steps are wanted")
+    return (_F * len(flat))(*flat)
+
+
+def dr_orthogonalise(batch, rows, cols, g, steps, coef, eps, o, workspace, workspace_bytes, flags=0, stream=None):
+    _check(_lib.dr_orthogonalise(batch, rows, cols, _ptr(g), steps, _coef(coef, steps), eps, _ptr(o), _ptr(workspace), workspace_bytes, flags,
+                                 _stream(stream)), "dr_orthogonalise")
+
+
+def dr_muon_update(batch, rows, cols, w, v, g, lr, momentum, decay, nesterov, steps, coef, eps, w_bf16, workspace, workspace_bytes, stream=None):
+    _check(_lib.dr_muon_update(batch, rows, cols, _ptr(w), _ptr(v), _ptr(g), lr, momentum, decay, int(nesterov), steps, _coef(coef, steps), eps,
+                               _ptr(w_bf16), _ptr(workspace), workspace_bytes, _stream(stream)), "dr_muon_update")
 
 
 def dr_conv_workspace_bytes(desc, B, H, W) -> int:
