@@ -158,6 +158,44 @@ def test_channel_slices_are_kept_apart(dr, M, C, pad, off):
         assert bool((t[:, :off] == 7).all()) and bool((t[:, off + C:] == 7).all()), "written outside the slice"
 
 
+@pytest.mark.parametrize("xf32,yf32", [(False, False), (True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("M,C,ldx,ldy,offx,offy", [(50, 40, 41, 40, 0, 0), (9000, 65, 72, 67, 3, 2), (700, 200, 203, 201, 1, 0), (300, 600, 601, 603, 0, 2),
+                                                   (500, 2000, 2003, 2000, 1, 0), (40, 4096, 4096, 4096, 0, 1), (20, 5001, 5003, 5001, 0, 0),
+                                                   (9001, 61, 61, 61, 5, 5), (6000, 333, 341, 349, 2, 10), (2500, 1030, 1033, 1033, 7, 7)])
+def test_rows_at_any_offset(dr, M, C, ldx, ldy, offx, offy, xf32, yf32):
+    """Rows whose offset from a 16-byte boundary differs between the tensors, or changes from row to row, over several rounds."""
+    import torch
+    flags = dr.DR_LN_X_F32 * xf32 | dr.DR_LN_Y_F32 * yf32
+    xa, dya = rows(f"ao{C}", M, C), S.round_bf16(S.normal(0, f"aod{C}", (M, C)))
+    g, b = 1 + 0.2 * S.normal(0, f"g{C}", (C,)), 0.3 * S.normal(0, f"b{C}", (C,))
+
+    def strided(a, ld, off, f32):
+        t = torch.full((off + M * ld,), 9.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+        v = t[off:].view(M, ld)[:, :C]
+        if a is not None:
+            v.copy_(dev(a, f32))
+        return t, v
+
+    (_, x), (_, dy), (yt, y), (dxt, dx) = strided(xa, ldx, offx, xf32), strided(dya, ldy, offy, yf32), strided(None, ldy, offy, yf32), strided(None, ldx, offx, xf32)
+    mean, rstd = empty((M,), True), empty((M,), True)
+    dr.dr_layernorm(M, C, x, ldx, dev(g, True), dev(b, True), 1e-5, y, ldy, mean, rstd, flags)
+    check_forward((host(y), host(mean), host(rstd)), xa, g.astype(np.float64), b.astype(np.float64), 1e-5, yf32)
+    dg, db = empty((C,), True), empty((C,), True)
+    ws = torch.empty(dr.dr_layernorm_bwd_workspace_bytes(M, C), dtype=torch.uint8, device="cuda")
+    dr.dr_layernorm_bwd(M, C, dy, ldy, x, ldx, dev(g, True), mean, rstd, dx, ldx, dg, db, ws, ws.numel(), flags)
+    m64, r64 = host(mean), host(rstd)
+    rdx, rdg, rdb = backward(dya.astype(np.float64), xa.astype(np.float64), g.astype(np.float64), m64, r64)
+    h = np.abs((xa - m64[:, None]) * r64[:, None])
+    t = np.abs(dya * g)
+    parts = r64[:, None] * (t + t.mean(1, keepdims=True) + h * (t * h).mean(1, keepdims=True))
+    assert np.all(np.abs(host(dx) - rdx) <= SUM * parts + (U32 if xf32 else U16) * np.abs(rdx))
+    assert np.all(np.abs(host(dg) - rdg) <= 544 * U32 * (np.abs(dya) * h).sum(0) + 1e-30)
+    assert np.all(np.abs(host(db) - rdb) <= 544 * U32 * np.abs(dya).sum(0) + 1e-30)
+    for whole, view, off, ld in ((yt, y, offy, ldy), (dxt, dx, offx, ldx)):
+        view.fill_(9.0)
+        assert bool((whole == 9).all()), "written outside the rows"
+
+
 @pytest.mark.parametrize("C", [64, 100, 777, 1024, 4096])
 def test_no_weights_no_statistics_in_place(dr, C):
     import torch
