@@ -1,131 +1,694 @@
 // Orthogonalising an update by Newton-Schulz products, and the optimiser step that uses it:
 //   X_0 = U / (|U|_F + eps),   A = X X^T,   X <- a X + (b A + c A A) X   (`steps` times),   O = X
 //   v <- momentum v + g;  U = g + momentum v (Nesterov) or v;  w <- w - lr (sqrt(max(1, rows / cols)) O + decay w)
-// X has n = min(rows, cols) rows: a taller U is worked on as its transpose.
+// X has n = min(rows, cols) rows and m columns: a taller U is worked on as its transpose.
 //
-// First form: everything in float32 on CUDA cores, a 64 x 64 tile of a product per block.
+// Arithmetic.  The products run on the tensor cores with float16 operands (11 significant bits) and float32 sums.  What keeps the
+// result close to the formula is what is NOT rounded to 11 bits:
+//  - X is carried as a pair of float16, X = (hi + lo) / 4096 (22 bits); the products read hi, the term a X reads both.
+//  - A is split into its diagonal and the rest, A = D + E, D in float32:
+//      A A = E E + D E + E D + D D,  so only E, small where X is nearly orthogonal, is rounded (and only for E E);
+//    likewise the polynomial b A + c A A = diag + F:  X <- (a + diag) X + F X with a row factor in float32.
+//    With the whole of A in float16 the relative error of O is 2e-3 .. 4e-3 (random matrices); with the split 2e-4 .. 1e-3.
+//  - Products symmetric by construction (A, E E) are computed for the lower triangle and mirrored, so they stay symmetric.
+// bfloat16 operands would cost 2e-3 .. 6e-3 even so: more than the rounding of O to bfloat16 itself.
+//
+// Execution.  One persistent kernel runs all products of a matrix: a group of G CTAs (one per SM) works through the phases
+// A -> F -> X of every step and meets at a barrier between them; a batch is spread over the groups.  Inside a phase a CTA is a
+// pipeline: one warp loads 64-deep operand slices by TMA, one issues tcgen05.mma into one of two accumulators in tensor
+// memory, eight drain the other one.  A group of up to 16 CTAs is a thread-block cluster and uses its barrier; a larger one is
+// launched cooperatively and counts arrivals in global memory.
+#include <algorithm>
 #include <cmath>
+#include <cuda_fp16.h>
 
-#include "common.cuh"
+#include "conv_common.cuh"
+#include "umma_ptx.cuh"
 
 namespace dr {
+using namespace ptx;
 
-constexpr int NS_NORM_BLOCKS = 128;
+constexpr int NS_THREADS = 320;             // warp 0: TMA, warp 1: MMA, warps 2 - 9: drain
+constexpr int NS_STAGES = 8;                // at most
+constexpr int NS_SMEM = 196608;             // operand ring
+constexpr int NS_BOX = 64 * 128;            // one TMA box: 64 rows of 64 float16
+constexpr float NS_SCALE = 4096.f;          // X is stored times this: entries of every size stay in float16's normal range
+constexpr int NS_NORM_BLOCKS = 256;         // partial sums of squares at most
 
 struct NsInput {
-    int rows, cols, tall, n, m;
-    const void* g;              // gradient (bf16 or f32), or the optimiser's float32 gradient
+    int rows, cols, tall;
+    const void* g;              // gradient (bfloat16 or float32), or the optimiser's float32 gradient
     int g_f32;
     float *v, *w;               // optimiser state, nullptr for the product alone
     float momentum;
     int nesterov;
     float eps;
+    float lr_scale, keep;       // w <- keep w - lr_scale O
+    __nv_bfloat16* out;         // O, or the bfloat16 copy of w (may be nullptr then)
 };
 
+struct NsParams {
+    NsInput in;
+    int batch, steps;
+    int n, m, ldx, lda;         // X: n x m, row stride ldx; A, E, F: n x n, row stride lda
+    int G, groups, cluster;
+    int nt_a, nt_s, nt_x;       // tile columns of the three products (rows: 128)
+    int tiles_a, tiles_s, tiles_x;
+    int splits;                 // ranges of the long axis in A = X X^T
+    int terms;                  // 1: hi hi;  3: hi hi + hi lo + lo hi
+    int stages, stage_bytes;
+    float coef[3 * DR_NS_MAX_STEPS];
+    // per group
+    __half *hi[2], *lo, *E, *F, *Elo, *Flo;
+    float *A, *d, *rs, *part;
+    double* norm;               // [groups][n_norm] where the kernel sums itself, [batch][n_norm] where ns_begin_kernel did
+    int n_norm;
+    unsigned* arrived;          // [groups]
+    int* status;
+};
+
+struct NsShared {
+    uint64_t full[NS_STAGES], empty[NS_STAGES], tfull[2], tempty[2];
+    uint32_t tmem_base;
+    int abort;
+    double red[10];
+};
+
+struct __align__(32) Half16 { uint32_t u[8]; };
+struct __align__(32) Float8 { float f[8]; };
+__device__ __forceinline__ Half16 ld16h(const __half* p) {
+    Half16 v;
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(v.u[0]), "=r"(v.u[1]), "=r"(v.u[2]), "=r"(v.u[3]), "=r"(v.u[4]), "=r"(v.u[5]), "=r"(v.u[6]), "=r"(v.u[7]) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st16h(__half* p, const Half16& v) {
+    asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(v.u[0]), "r"(v.u[1]), "r"(v.u[2]), "r"(v.u[3]), "r"(v.u[4]), "r"(v.u[5]), "r"(v.u[6]), "r"(v.u[7]), "l"(p) : "memory");
+}
+__device__ __forceinline__ void ld8f(const float* p, float* f) {
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void st8f(float* p, const float* f) {
+    asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]), "l"(p) : "memory");
+}
+__device__ __forceinline__ float2 half2_at(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// ------------------------------------------------------------------------------------------------ input and output
 __device__ __forceinline__ float ns_value(const NsInput& in, size_t i) {
     const float g = in.g_f32 ? ((const float*)in.g)[i] : __bfloat162float(((const __nv_bfloat16*)in.g)[i]);
     if (!in.v) return g;
-    return in.nesterov ? fmaf(in.momentum, in.v[i], g) : in.v[i];
+    const float v = in.v[i];
+    return in.nesterov ? fmaf(in.momentum, v, g) : v;
 }
 
-__global__ void __launch_bounds__(256) ns_momentum_kernel(const NsInput in, size_t n) {
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256)
-        in.v[i] = fmaf(in.momentum, in.v[i], ((const float*)in.g)[i]);
-}
-
-__device__ double ns_block_sum(double s) {
-    __shared__ double red[256];
-    red[threadIdx.x] = s;
-    __syncthreads();
-    for (int o = 128; o; o >>= 1) {
-        if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-        __syncthreads();
-    }
-    return red[0];
-}
-
-// sum of squares of matrix blockIdx.y, one partial per block
-__global__ void __launch_bounds__(256) ns_norm_kernel(const NsInput in, double* partial) {
-    const size_t per = (size_t)in.rows * in.cols;
+// v <- momentum v + g and this thread's part of the sum of squares of U (in float64: no size of U overflows or vanishes)
+__device__ __forceinline__ double ns_momentum(const NsInput& in, size_t base, size_t per, size_t first, size_t stride) {
     double s = 0.;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < per; i += (size_t)NS_NORM_BLOCKS * 256) {
-        const double u = ns_value(in, blockIdx.y * per + i);
-        s += u * u;
+    for (size_t i = first; i < per; i += stride) {
+        if (in.v) in.v[base + i] = fmaf(in.momentum, in.v[base + i], ((const float*)in.g)[base + i]);
+        const double u = ns_value(in, base + i);
+        s = fma(u, u, s);
     }
-    s = ns_block_sum(s);
-    if (threadIdx.x == 0) partial[(size_t)blockIdx.y * NS_NORM_BLOCKS + blockIdx.x] = s;
+    return s;
 }
 
-__global__ void __launch_bounds__(256) ns_scale_kernel(const NsInput in, const double* partial, float* X) {
-    const double s = ns_block_sum(threadIdx.x < NS_NORM_BLOCKS ? partial[(size_t)blockIdx.y * NS_NORM_BLOCKS + threadIdx.x] : 0.);
-    const float inv = (float)(1. / (sqrt(s) + (double)in.eps));
+__device__ __forceinline__ double ns_warp_sum(double s) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+}
+
+__global__ void __launch_bounds__(256) ns_begin_kernel(const NsInput in, double* norm, unsigned* arrived, int groups) {
+    __shared__ double red[8];
     const size_t per = (size_t)in.rows * in.cols;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < per; i += (size_t)gridDim.x * 256) {
-        const size_t r = i / in.cols, c = i - r * in.cols;
-        X[blockIdx.y * per + (in.tall ? c * in.rows + r : i)] = ns_value(in, blockIdx.y * per + i) * inv;
+    if (blockIdx.y == 0 && blockIdx.x == 0)
+        for (int i = threadIdx.x; i < groups; i += 256) arrived[i] = 0;
+    const double s = ns_warp_sum(ns_momentum(in, blockIdx.y * per, per, (size_t)blockIdx.x * 256 + threadIdx.x, (size_t)gridDim.x * 256));
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double t = 0.;
+        for (int i = 0; i < 8; ++i) t += red[i];
+        norm[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = t;
     }
 }
 
-// out[i][j] = alpha * add[i][j] + beta * sum_k P[i][k] * (TRANS ? Q[j][k] : Q[k][j])
-template <bool TRANS>
-__global__ void __launch_bounds__(256) ns_product_kernel(int I, int J, int K, const float* P, const float* Q, float alpha, const float* add, float beta, float* out) {
-    __shared__ float sp[16][65], sq[16][65];
-    P += (size_t)blockIdx.z * I * K;
-    Q += (size_t)blockIdx.z * J * K;
-    const size_t o = (size_t)blockIdx.z * I * J;
-    const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, ti = threadIdx.x >> 4, tj = threadIdx.x & 15;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < K; k0 += 16) {
-        for (int e = threadIdx.x; e < 1024; e += 256) {
-            const int i = e >> 4, k = e & 15;
-            sp[k][i] = i0 + i < I && k0 + k < K ? P[(size_t)(i0 + i) * K + k0 + k] : 0.f;
-            if (TRANS) sq[k][i] = j0 + i < J && k0 + k < K ? Q[(size_t)(j0 + i) * K + k0 + k] : 0.f;
-            const int kk = e >> 6, j = e & 63;
-            if (!TRANS) sq[kk][j] = j0 + j < J && k0 + kk < K ? Q[(size_t)(k0 + kk) * J + j0 + j] : 0.f;
-        }
-        __syncthreads();
-        for (int k = 0; k < 16; ++k)
-            for (int a = 0; a < 4; ++a)
-                for (int b = 0; b < 4; ++b) acc[a][b] = fmaf(sp[k][ti + 16 * a], sq[k][tj + 16 * b], acc[a][b]);
-        __syncthreads();
+// ------------------------------------------------------------------------------------------------ the products' tiles
+// Tiles of 128 rows x nt columns that reach the lower triangle, row by row.
+__host__ __device__ __forceinline__ int ns_tri_row(int i, int n, int nt) { return min((n + nt - 1) / nt, (i * 128 + 127) / nt + 1); }
+__device__ __forceinline__ void ns_tri_tile(int t, int n, int nt, int& i, int& j) {
+    i = 0;
+    for (int c; t >= (c = ns_tri_row(i, n, nt)); ++i) t -= c;
+    j = t;
+}
+
+enum { NS_A, NS_S, NS_X };
+struct NsItem { int i, j, k0, k1, split, tile; };
+template <int PHASE>
+__device__ __forceinline__ NsItem ns_item(const NsParams& p, int item) {
+    NsItem it;
+    it.split = 0;
+    const int kb = ((PHASE == NS_A ? p.m : p.n) + 63) / 64;
+    it.k0 = 0;
+    it.k1 = kb;
+    it.tile = item;
+    if (PHASE == NS_A) {
+        it.split = item / p.tiles_a;
+        it.tile = item - it.split * p.tiles_a;
+        it.k0 = (int)((long long)kb * it.split / p.splits);
+        it.k1 = (int)((long long)kb * (it.split + 1) / p.splits);
     }
-    for (int a = 0; a < 4; ++a)
-        for (int b = 0; b < 4; ++b) {
-            const int i = i0 + ti + 16 * a, j = j0 + tj + 16 * b;
-            if (i < I && j < J) {
-                const size_t e = o + (size_t)i * J + j;
-                out[e] = beta * acc[a][b] + (add ? alpha * add[e] : 0.f);
+    if (PHASE == NS_X) {
+        const int ni = (p.n + 127) / 128;
+        it.j = item / ni;
+        it.i = item - it.j * ni;
+    } else {
+        ns_tri_tile(it.tile, p.n, PHASE == NS_A ? p.nt_a : p.nt_s, it.i, it.j);
+    }
+    return it;
+}
+
+// the first `count` of CN float16 values of a row (a whole number of 16-byte pieces in all but the diagonal's tiles)
+template <int CN>
+__device__ __forceinline__ void ns_row_store(__half* p, const uint32_t* h, int count) {
+    if (count == CN) {
+#pragma unroll
+        for (int c = 0; c < CN / 2; c += 4) *reinterpret_cast<uint4*>(p + 2 * c) = make_uint4(h[c], h[c + 1], h[c + 2], h[c + 3]);
+    } else {
+#pragma unroll
+        for (int c = 0; c < CN; ++c)
+            if (c < count) p[c] = __ushort_as_half((unsigned short)(h[c / 2] >> (16 * (c & 1))));
+    }
+}
+
+// What the drain of A leaves for (row i, columns c0 .. c0 + CN - 1), of which those up to the diagonal count.
+template <int CN>
+__device__ __forceinline__ void ns_emit_a(const NsParams& p, size_t mat, float* dvec, int i, int c0, float* v) {
+    if (c0 > i) return;
+    float* A = p.A + mat;
+#pragma unroll
+    for (int c = 0; c < CN; c += 8) st8f(A + (size_t)i * p.lda + c0 + c, v + c);
+    if (i < c0 + CN) {
+#pragma unroll
+        for (int c = 0; c < CN; ++c)
+            if (c0 + c == i) {
+                dvec[i] = v[c];
+                v[c] = 0.f;
+            }
+    }
+    uint32_t h[CN / 2];
+#pragma unroll
+    for (int c = 0; c < CN; c += 2) h[c / 2] = pack_half(v[c], v[c + 1]);
+    float l[CN];
+#pragma unroll
+    for (int c = 0; c < CN; c += 2) {
+        const float2 f = half2_at(h[c / 2]);
+        l[c] = v[c] - f.x;
+        l[c + 1] = v[c + 1] - f.y;
+    }
+    const int last = min(CN, i - c0 + 1);
+    ns_row_store<CN>(p.E + mat + (size_t)i * p.lda + c0, h, last);
+#pragma unroll
+    for (int c = 0; c < CN; ++c)
+        if (c < last) {
+            const __half e = __ushort_as_half((unsigned short)(h[c / 2] >> (16 * (c & 1)))), el = __float2half_rn(l[c]);
+            p.E[mat + (size_t)(c0 + c) * p.lda + i] = e;
+            if (p.terms == 3) {
+                p.Elo[mat + (size_t)i * p.lda + c0 + c] = el;
+                p.Elo[mat + (size_t)(c0 + c) * p.lda + i] = el;
             }
         }
 }
 
-__global__ void __launch_bounds__(256) ns_finish_kernel(const NsInput in, const float* X, float lr_scale, float keep, __nv_bfloat16* out) {
-    const size_t per = (size_t)in.rows * in.cols;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < per; i += (size_t)gridDim.x * 256) {
-        const size_t r = i / in.cols, c = i - r * in.cols, e = blockIdx.y * per + i;
-        const float x = X[blockIdx.y * per + (in.tall ? c * in.rows + r : i)];
-        if (in.w) {
-            const float wn = fmaf(-lr_scale, x, keep * in.w[e]);
-            in.w[e] = wn;
-            if (out) out[e] = __float2bfloat16_rn(wn);
-        } else {
-            out[e] = __float2bfloat16_rn(x);
+// (row i, columns c0 ..) of E E -> the polynomial b A + c A A: F off the diagonal, a + its diagonal as the row's factor
+template <int CN>
+__device__ __forceinline__ void ns_emit_f(const NsParams& p, size_t mat, const float* dvec, float* rs, float a, float b, float cc, int i, int c0, float* v) {
+    if (c0 > i) return;
+    float e[CN];
+#pragma unroll
+    for (int c = 0; c < CN; c += 8) ld8f(p.A + mat + (size_t)i * p.lda + c0 + c, e + c);
+    const float di = dvec[i];
+    const int last = min(CN, i - c0 + 1);
+    uint32_t h[CN / 2];
+#pragma unroll
+    for (int c = 0; c < CN; ++c) {
+        if (c0 + c < i) v[c] = fmaf(b, e[c], cc * fmaf(di + dvec[c0 + c], e[c], v[c]));
+        else if (c0 + c == i) {
+            rs[i] = a + fmaf(b, di, cc * fmaf(di, di, v[c]));
+            v[c] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CN; c += 2) h[c / 2] = pack_half(v[c], v[c + 1]);
+    ns_row_store<CN>(p.F + mat + (size_t)i * p.lda + c0, h, last);
+#pragma unroll
+    for (int c = 0; c < CN; ++c)
+        if (c < last) {
+            const __half fh = __ushort_as_half((unsigned short)(h[c / 2] >> (16 * (c & 1))));
+            p.F[mat + (size_t)(c0 + c) * p.lda + i] = fh;
+            if (p.terms == 3) {
+                const __half fl = __float2half_rn(v[c] - __half2float(fh));
+                p.Flo[mat + (size_t)i * p.lda + c0 + c] = fl;
+                p.Flo[mat + (size_t)(c0 + c) * p.lda + i] = fl;
+            }
+        }
+}
+
+struct NsMaps { CUtensorMap hi[2], lo, E, F, Elo, Flo; };
+
+// Where the roles of a CTA stand in their rings; kept from phase to phase.
+struct NsPipe {
+    int stage = 0;
+    uint32_t phase = 0;
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    __device__ __forceinline__ void next_stage(int stages) { if (++stage == stages) { stage = 0; phase ^= 1; } }
+    __device__ __forceinline__ void next_acc() { if (++acc == 2) { acc = 0; acc_phase ^= 1; } }
+};
+
+template <int PHASE>
+__device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps, NsShared& sh, uint32_t smem, uint32_t tmem, NsPipe& pipe, int group, int rank, int src, const float* coef) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int nt = PHASE == NS_A ? p.nt_a : PHASE == NS_S ? p.nt_s : p.nt_x;
+    const int items = PHASE == NS_A ? p.tiles_a * p.splits : PHASE == NS_S ? p.tiles_s : p.tiles_x;
+    volatile int* abort_flag = &sh.abort;
+    if (warp == 0) {
+        if (lane == 0) {
+            const CUtensorMap *ah, *al, *bh, *bl;
+            if (PHASE == NS_A) { ah = bh = &maps.hi[src]; al = bl = &maps.lo; }
+            else if (PHASE == NS_S) { ah = bh = &maps.E; al = bl = &maps.Elo; }
+            else { ah = &maps.F; al = &maps.Flo; bh = &maps.hi[src]; bl = &maps.lo; }
+            const uint32_t bytes = (uint32_t)(2 + nt / 64) * NS_BOX;
+            for (int item = rank; item < items; item += p.G) {
+                const NsItem it = ns_item<PHASE>(p, item);
+                for (int term = 0; term < p.terms; ++term) {
+                    const CUtensorMap* am = term == 2 ? al : ah;
+                    const CUtensorMap* bm = term == 1 ? bl : bh;
+                    for (int kb = it.k0; kb < it.k1; ++kb) {
+                        uint64_t* full = &sh.full[pipe.stage];
+                        if (!mbar_wait(&sh.empty[pipe.stage], pipe.phase ^ 1, abort_flag)) {
+                            if (!*abort_flag) report_timeout(p.status, 71, item);
+                            *abort_flag = 1;
+                            goto out;
+                        }
+                        mbar_arrive_expect_tx(full, bytes);
+                        const uint32_t dst = smem + pipe.stage * p.stage_bytes;
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) tma_load_3d_u32<false>(dst + r * NS_BOX, am, smem_u32(full), kb * 64, it.i * 128 + 64 * r, group, 1);
+                        for (int r = 0; r < nt / 64; ++r) {
+                            if (PHASE == NS_X) tma_load_3d_u32<false>(dst + (2 + r) * NS_BOX, bm, smem_u32(full), it.j * nt + 64 * r, kb * 64, group, 1);
+                            else tma_load_3d_u32<false>(dst + (2 + r) * NS_BOX, bm, smem_u32(full), kb * 64, it.j * nt + 64 * r, group, 1);
+                        }
+                        pipe.next_stage(p.stages);
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            // D float32, A and B float16; B of the X product lies with the contraction index as its rows
+            const uint32_t idesc = (1u << 4) | ((uint32_t)(nt >> 3) << 17) | (8u << 24) | (PHASE == NS_X ? 1u << 16 : 0u);
+            for (int item = rank; item < items; item += p.G) {
+                const NsItem it = ns_item<PHASE>(p, item);
+                if (!mbar_wait(&sh.tempty[pipe.acc], pipe.acc_phase ^ 1, abort_flag)) {
+                    if (!*abort_flag) report_timeout(p.status, 72, item);
+                    *abort_flag = 1;
+                    goto out;
+                }
+                tc_fence_after();
+                const uint32_t acc = tmem + pipe.acc * 256;
+                uint32_t accumulate = 0;
+                for (int k = (it.k1 - it.k0) * p.terms; k > 0; --k) {
+                    if (!mbar_wait(&sh.full[pipe.stage], pipe.phase, abort_flag)) {
+                        if (!*abort_flag) report_timeout(p.status, 73, item);
+                        *abort_flag = 1;
+                        goto out;
+                    }
+                    tc_fence_after();
+                    const uint32_t a = smem + pipe.stage * p.stage_bytes, b = a + 2 * NS_BOX;
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks) {
+                        const uint32_t bd = PHASE == NS_X ? (((b & 0x3FFFFu) >> 4) | ((NS_BOX >> 4) << 16)) + ks * 128 : sdesc_lo(b) + ks * 2;
+                        umma_bf16_lo<false>(acc, sdesc_lo(a) + ks * 2, bd, idesc, accumulate, 1u);
+                        accumulate = 1;
+                    }
+                    umma_commit(&sh.empty[pipe.stage]);
+                    pipe.next_stage(p.stages);
+                }
+                umma_commit(&sh.tfull[pipe.acc]);
+                pipe.next_acc();
+            }
+        }
+    } else {
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        const size_t mat = (size_t)group * p.n * p.lda, xm = (size_t)group * p.n * p.ldx;
+        float* dvec = p.d + (size_t)group * p.n;
+        float* rs = p.rs + (size_t)group * p.n;
+        for (int item = rank; item < items; item += p.G) {
+            const NsItem it = ns_item<PHASE>(p, item);
+            const int row = it.i * 128 + q * 32 + lane;
+            float factor = 0.f;
+            if (PHASE == NS_X && row < p.n) factor = rs[row];
+            const bool ok = __all_sync(0xffffffffu, mbar_wait(&sh.tfull[pipe.acc], pipe.acc_phase, abort_flag));
+            if (!ok) {
+                if (!*abort_flag) report_timeout(p.status, 74, item);
+                *abort_flag = 1;
+                goto out;
+            }
+            tc_fence_after();
+            const uint32_t acc = tmem + pipe.acc * 256 + ((uint32_t)(q * 32) << 16);
+            for (int c = half * 16; c < nt; c += 32) {
+                uint32_t raw[16];
+                float v[16];
+                tmem_ld_x16(acc + c, raw);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(raw[e]);
+                const int col = it.j * nt + c;
+                if (PHASE == NS_A && p.splits > 1) {
+                    float* out = p.part + (((size_t)group * p.splits + it.split) * p.tiles_a + it.tile) * nt * 128 + (size_t)c * 128 + q * 32 + lane;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) out[e * 128] = v[e];
+                } else if (row < p.n) {
+                    if (PHASE == NS_A) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] *= 1.f / (NS_SCALE * NS_SCALE);
+                        ns_emit_a<16>(p, mat, dvec, row, col, v);
+                    } else if (PHASE == NS_S) {
+                        ns_emit_f<16>(p, mat, dvec, rs, coef[0], coef[1], coef[2], row, col, v);
+                    } else if (col < p.ldx) {
+                        const size_t at = xm + (size_t)row * p.ldx + col;
+                        Half16 h = ld16h(p.hi[src] + at), l = ld16h(p.lo + at);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float2 fh = half2_at(h.u[e]), fl = half2_at(l.u[e]);
+                            const float x0 = fmaf(factor, fh.x + fl.x, v[2 * e]), x1 = fmaf(factor, fh.y + fl.y, v[2 * e + 1]);
+                            h.u[e] = pack_half(x0, x1);
+                            const float2 r = half2_at(h.u[e]);
+                            l.u[e] = pack_half(x0 - r.x, x1 - r.y);
+                        }
+                        st16h(p.hi[src ^ 1] + at, h);
+                        st16h(p.lo + at, l);
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.tempty[pipe.acc]);
+            pipe.next_acc();
+        }
+    }
+out:                                            // also after a wait that ran out: the whole warp goes on to the next barrier
+    __syncwarp();
+}
+
+// All threads of the group's CTAs meet; what they wrote to global memory is visible to the others' loads, TMA included.
+__device__ __forceinline__ void ns_group_sync(const NsParams& p, NsShared& sh, int group, unsigned& epoch) {
+    asm volatile("fence.proxy.async;" ::: "memory");
+    if (p.G == 1) {
+        __syncthreads();
+    } else if (p.cluster) {
+        cluster_sync_all();
+    } else {
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            unsigned* c = p.arrived + group;
+            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(c) : "memory");
+            const unsigned target = ++epoch * (unsigned)p.G;
+            const long long t0 = clock64();
+            for (;;) {
+                unsigned seen;
+                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(c) : "memory");
+                if (seen >= target || sh.abort) break;
+                if (clock64() - t0 > WAIT_LIMIT_CYCLES) {
+                    report_timeout(p.status, 75, (int)epoch);
+                    sh.abort = 1;
+                    break;
+                }
+            }
+        }
+        __syncthreads();
+        __threadfence();
+    }
+    asm volatile("fence.proxy.async;" ::: "memory");
+}
+
+// X_0 from U, transposed where U is tall (through a 64 x 64 tile in shared memory)
+__device__ __forceinline__ void ns_load_x(const NsParams& p, float* tile, int group, int rank, size_t base, float inv) {
+    const NsInput& in = p.in;
+    __half* hi = p.hi[0] + (size_t)group * p.n * p.ldx;
+    __half* lo = p.lo + (size_t)group * p.n * p.ldx;
+    auto put = [&](size_t at, float u) {
+        const float x = u * inv;
+        const __half h = __float2half_rn(x);
+        hi[at] = h;
+        lo[at] = __float2half_rn(x - __half2float(h));
+    };
+    if (!in.tall) {
+        const size_t per = (size_t)in.rows * in.cols;
+        for (size_t i = (size_t)rank * NS_THREADS + threadIdx.x; i < per; i += (size_t)p.G * NS_THREADS) {
+            const size_t r = i / in.cols;
+            put(r * p.ldx + (i - r * in.cols), ns_value(in, base + i));
+        }
+    } else {
+        const int tr = (in.rows + 63) / 64, tc = (in.cols + 63) / 64;
+        for (int t = rank; t < tr * tc; t += p.G) {
+            const int r0 = t / tc * 64, c0 = t % tc * 64;
+            __syncthreads();
+            for (int e = threadIdx.x; e < 4096; e += NS_THREADS) {
+                const int r = r0 + (e >> 6), c = c0 + (e & 63);
+                if (r < in.rows && c < in.cols) tile[(e >> 6) * 65 + (e & 63)] = ns_value(in, base + (size_t)r * in.cols + c);
+            }
+            __syncthreads();
+            for (int e = threadIdx.x; e < 4096; e += NS_THREADS) {
+                const int c = c0 + (e >> 6), r = r0 + (e & 63);
+                if (r < in.rows && c < in.cols) put((size_t)c * p.ldx + r, tile[(e & 63) * 65 + (e >> 6)]);
+            }
         }
     }
 }
 
-struct NsWorkspace { size_t partial, x0, x1, a, b, total; };
-static NsWorkspace ns_workspace(int batch, int rows, int cols) {
-    const size_t n = rows < cols ? rows : cols, x = (size_t)batch * rows * cols * sizeof(float), a = (size_t)batch * n * n * sizeof(float);
-    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
-    NsWorkspace w;
-    w.partial = 0;
-    w.x0 = up((size_t)batch * NS_NORM_BLOCKS * sizeof(double));
-    w.x1 = w.x0 + up(x);
-    w.a = w.x1 + up(x);
-    w.b = w.a + up(a);
-    w.total = w.b + up(a);
-    return w;
+__device__ __forceinline__ void ns_store_o(const NsParams& p, float* tile, int group, int rank, size_t base, int src) {
+    const NsInput& in = p.in;
+    const __half* hi = p.hi[src] + (size_t)group * p.n * p.ldx;
+    const __half* lo = p.lo + (size_t)group * p.n * p.ldx;
+    auto get = [&](size_t at) { return (__half2float(hi[at]) + __half2float(lo[at])) * (1.f / NS_SCALE); };
+    auto put = [&](size_t at, float o) {
+        if (in.w) {
+            o = fmaf(-in.lr_scale, o, in.keep * in.w[at]);
+            in.w[at] = o;
+        }
+        if (in.out) in.out[at] = __float2bfloat16_rn(o);
+    };
+    if (!in.tall) {
+        const size_t per = (size_t)in.rows * in.cols;
+        for (size_t i = (size_t)rank * NS_THREADS + threadIdx.x; i < per; i += (size_t)p.G * NS_THREADS) {
+            const size_t r = i / in.cols;
+            put(base + i, get(r * p.ldx + (i - r * in.cols)));
+        }
+    } else {
+        const int tr = (in.rows + 63) / 64, tc = (in.cols + 63) / 64;
+        for (int t = rank; t < tr * tc; t += p.G) {
+            const int r0 = t / tc * 64, c0 = t % tc * 64;
+            __syncthreads();
+            for (int e = threadIdx.x; e < 4096; e += NS_THREADS) {
+                const int c = c0 + (e >> 6), r = r0 + (e & 63);
+                if (r < in.rows && c < in.cols) tile[(e & 63) * 65 + (e >> 6)] = get((size_t)c * p.ldx + r);
+            }
+            __syncthreads();
+            for (int e = threadIdx.x; e < 4096; e += NS_THREADS) {
+                const int r = r0 + (e >> 6), c = c0 + (e & 63);
+                if (r < in.rows && c < in.cols) put(base + (size_t)r * in.cols + c, tile[(e >> 6) * 65 + (e & 63)]);
+            }
+        }
+    }
+}
+
+__global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsParams p) {
+    extern __shared__ uint8_t ns_smem_raw[];
+    __shared__ NsShared sh;
+    const uint32_t smem = (smem_u32(ns_smem_raw) + 1023u) & ~1023u;
+    float* tile = reinterpret_cast<float*>(ns_smem_raw + (smem - smem_u32(ns_smem_raw)));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = blockIdx.x / p.G, rank = blockIdx.x - group * p.G;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < NS_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 8); }
+        sh.abort = 0;
+        fence_barrier_init();
+    }
+    if (warp == 1) { tmem_alloc(&sh.tmem_base, 512); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem_base;
+    NsPipe pipe;
+    unsigned epoch = 0;
+    const size_t per = (size_t)p.in.rows * p.in.cols;
+
+    for (int b = group; b < p.batch; b += p.groups) {
+        const size_t base = (size_t)b * per;
+        const double* norm = p.norm + (size_t)b * p.n_norm;
+        if (p.G == 1 || p.cluster) {            // no kernel in front has summed the squares: the group does
+            double s = ns_warp_sum(ns_momentum(p.in, base, per, (size_t)rank * NS_THREADS + threadIdx.x, (size_t)p.G * NS_THREADS));
+            if (lane == 0) sh.red[warp] = s;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                s = 0.;
+                for (int i = 0; i < NS_THREADS / 32; ++i) s += sh.red[i];
+                p.norm[(size_t)group * p.n_norm + rank] = s;
+            }
+            norm = p.norm + (size_t)group * p.n_norm;
+            ns_group_sync(p, sh, group, epoch);
+        }
+        double s = 0.;
+        for (int i = lane; i < p.n_norm; i += 32) s += norm[i];
+        const float inv = (float)((double)NS_SCALE / (sqrt(ns_warp_sum(s)) + (double)p.in.eps));
+        ns_load_x(p, tile, group, rank, base, inv);
+        ns_group_sync(p, sh, group, epoch);
+        int src = 0;
+        for (int k = 0; k < p.steps; ++k, src ^= 1) {
+            ns_product<NS_A>(p, maps, sh, smem, tmem, pipe, group, rank, src, nullptr);
+            ns_group_sync(p, sh, group, epoch);
+            if (p.splits > 1) {
+                // the ranges' parts of A in order: a warp takes 32 rows x 8 columns
+                const int nt = p.nt_a, units = p.tiles_a * nt / 2;
+                for (int u = rank * (NS_THREADS / 32) + warp; u < units; u += p.G * (NS_THREADS / 32)) {
+                    const int t = u / (nt / 2), rem = u - t * (nt / 2);
+                    int i, j;
+                    ns_tri_tile(t, p.n, nt, i, j);
+                    const int row = i * 128 + (rem & 3) * 32 + lane, c = (rem >> 2) * 8;
+                    const float* in = p.part + ((size_t)group * p.splits * p.tiles_a + t) * nt * 128 + (size_t)c * 128 + (rem & 3) * 32 + lane;
+                    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    for (int q = 0; q < p.splits; ++q)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] += in[(size_t)q * p.tiles_a * nt * 128 + e * 128];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] *= 1.f / (NS_SCALE * NS_SCALE);
+                    if (row < p.n) ns_emit_a<8>(p, (size_t)group * p.n * p.lda, p.d + (size_t)group * p.n, row, j * nt + c, v);
+                }
+                ns_group_sync(p, sh, group, epoch);
+            }
+            ns_product<NS_S>(p, maps, sh, smem, tmem, pipe, group, rank, src, p.coef + 3 * k);
+            ns_group_sync(p, sh, group, epoch);
+            ns_product<NS_X>(p, maps, sh, smem, tmem, pipe, group, rank, src, nullptr);
+            ns_group_sync(p, sh, group, epoch);
+        }
+        ns_store_o(p, tile, group, rank, base, src);
+        ns_group_sync(p, sh, group, epoch);     // the buffers are free for the group's next matrix
+    }
+    if (sh.abort) {                             // copies and products in flight end within microseconds; then the CTA may go
+        const long long t0 = clock64();
+        while (clock64() - t0 < 4000000) {}
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+static bool ns_attributes() {
+    static PerDeviceFlag attr_set;
+    if (attr_set.get()) return true;
+    if (cudaFuncSetAttribute(ns_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM + 1024) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return false;
+    }
+    attr_set.set();
+    return true;
+}
+
+struct NsPlan {
+    NsParams p;
+    size_t hi0, hi1, lo, E, F, Elo, Flo, A, d, rs, part, norm, arrived, total;
+    int norm_blocks;
+};
+
+static int ns_tri_tiles(int n, int nt) {
+    int t = 0;
+    for (int i = 0; i < (n + 127) / 128; ++i) t += ns_tri_row(i, n, nt);
+    return t;
+}
+
+// The largest cluster (a power of two, at most 16) the device can hold with the kernel's shared memory.
+static int ns_max_cluster() {
+    static std::atomic<int> known[64];
+    std::atomic<int>& slot = known[PerDeviceFlag::dev()];
+    int c = slot.load(std::memory_order_relaxed);
+    if (c) return c;
+    for (c = 16; c > 8; c /= 2) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.gridDim = dim3(c); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM + 1024; cfg.attrs = attr; cfg.numAttrs = 1;
+        int n = 0;
+        if (ns_attributes() && cudaOccupancyMaxActiveClusters(&n, ns_kernel, &cfg) == cudaSuccess && n > 0) break;
+        (void)cudaGetLastError();
+    }
+    slot.store(c, std::memory_order_relaxed);
+    return c;
+}
+
+static NsPlan ns_plan(int batch, int rows, int cols) {
+    NsPlan l = {};
+    NsParams& p = l.p;
+    const int sms = num_sms();
+    p.batch = batch;
+    p.in.rows = rows; p.in.cols = cols; p.in.tall = rows > cols;
+    p.n = std::min(rows, cols); p.m = std::max(rows, cols);
+    p.ldx = (p.m + 63) / 64 * 64; p.lda = (p.n + 63) / 64 * 64;
+    p.terms = p.n <= tunable("DR_NS_FINE", 128) ? 3 : 1;
+    const int ni = (p.n + 127) / 128;
+    auto tiles_x = [&](int nt) { return ni * ((p.m + nt - 1) / nt); };
+    // CTAs per matrix: what the widest phase can use with its narrowest tiles, at most all SMs
+    const int batch1 = batch < 1 ? 1 : batch;
+    int g = std::min(std::max(tiles_x(64), 1), sms);
+    g = std::min(g, std::max(1, sms / batch1));
+    const int max_cluster = tunable("DR_NS_CLUSTER", ns_max_cluster());
+    if (g <= max_cluster) {
+        int q = 1;
+        while (q * 2 <= g) q *= 2;
+        g = q;
+        p.cluster = g > 1;
+    }
+    p.G = g;
+    p.groups = std::min(batch1, std::max(1, sms / g));
+    // the widest tiles that still give every CTA of the group one
+    auto widest = [&](auto tiles) { return tiles(256) >= g ? 256 : tiles(128) >= g ? 128 : 64; };
+    p.nt_x = widest(tiles_x);
+    p.nt_s = widest([&](int nt) { return ns_tri_tiles(p.n, nt); });
+    p.nt_a = ns_tri_tiles(p.n, 256) >= g ? 256 : 128;
+    p.tiles_x = tiles_x(p.nt_x); p.tiles_s = ns_tri_tiles(p.n, p.nt_s); p.tiles_a = ns_tri_tiles(p.n, p.nt_a);
+    const int kb = (p.m + 63) / 64;
+    p.splits = std::max(1, std::min(g / p.tiles_a, kb / 4));
+    p.stage_bytes = (2 + std::max(p.nt_x, std::max(p.nt_s, p.nt_a)) / 64) * NS_BOX;
+    p.stages = std::min(NS_STAGES, NS_SMEM / p.stage_bytes);
+    l.norm_blocks = (int)std::min<size_t>(NS_NORM_BLOCKS, ((size_t)rows * cols + 2047) / 2048);
+    p.n_norm = p.cluster || g == 1 ? g : l.norm_blocks;
+    size_t at = 0;
+    auto take = [&](size_t& where, size_t bytes) { where = at; at += (bytes + 255) / 256 * 256; };
+    const size_t x = (size_t)p.groups * p.n * p.ldx * 2, a = (size_t)p.groups * p.n * p.lda * 2;
+    take(l.hi0, x); take(l.hi1, x); take(l.lo, x);
+    take(l.E, a); take(l.F, a); take(l.Elo, p.terms == 3 ? a : 0); take(l.Flo, p.terms == 3 ? a : 0); take(l.A, 2 * a);
+    take(l.d, (size_t)p.groups * p.n * 4); take(l.rs, (size_t)p.groups * p.n * 4);
+    take(l.part, p.splits > 1 ? (size_t)p.groups * p.splits * p.tiles_a * p.nt_a * 128 * 4 : 0);
+    take(l.norm, (size_t)(p.cluster || g == 1 ? p.groups : batch1) * p.n_norm * 8);
+    take(l.arrived, (size_t)p.groups * 4);
+    l.total = at;
+    return l;
+}
+
+static int ns_map(CUtensorMap* map, const void* ptr, int cols, int rows, int ld, int groups) {
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)groups};
+    const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)rows * ld * 2};
+    const cuuint32_t box[3] = {64, 64, 1};
+    return tmap_tiled(map, 3, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 static int ns_check(int batch, int rows, int cols, int steps, const float* coef, float eps) {
@@ -137,28 +700,51 @@ static int ns_check(int batch, int rows, int cols, int steps, const float* coef,
     return DR_OK;
 }
 
-static int ns_run(int batch, const NsInput& in, int steps, const float* coef, float lr_scale, float keep, __nv_bfloat16* out, char* ws, cudaStream_t s) {
-    const NsWorkspace l = ns_workspace(batch, in.rows, in.cols);
-    const size_t per = (size_t)in.rows * in.cols;
-    const unsigned eb = (unsigned)std::min<size_t>((per + 255) / 256, (size_t)num_sms() * 8);
-    double* partial = (double*)(ws + l.partial);
-    float *X = (float*)(ws + l.x0), *Y = (float*)(ws + l.x1), *A = (float*)(ws + l.a), *B = (float*)(ws + l.b);
-    if (in.v) {
-        ns_momentum_kernel<<<(unsigned)num_sms() * 8, 256, 0, s>>>(in, per * batch);
+static int ns_run(NsPlan& l, const NsInput& in, int steps, const float* coef, char* ws, cudaStream_t s) {
+    NsParams& p = l.p;
+    p.in = in;
+    p.in.tall = p.in.rows > p.in.cols;
+    p.steps = steps;
+    const float usual[3] = {3.4445f, -4.7750f, 2.0315f};
+    for (int i = 0; i < 3 * steps; ++i) p.coef[i] = coef ? coef[i] : usual[i % 3];
+    p.hi[0] = (__half*)(ws + l.hi0); p.hi[1] = (__half*)(ws + l.hi1); p.lo = (__half*)(ws + l.lo);
+    p.E = (__half*)(ws + l.E); p.F = (__half*)(ws + l.F); p.Elo = (__half*)(ws + l.Elo); p.Flo = (__half*)(ws + l.Flo);
+    p.A = (float*)(ws + l.A); p.d = (float*)(ws + l.d); p.rs = (float*)(ws + l.rs); p.part = (float*)(ws + l.part);
+    p.norm = (double*)(ws + l.norm); p.arrived = (unsigned*)(ws + l.arrived);
+    p.status = dev_status_ptr();
+    alignas(64) NsMaps maps;
+    int st = ns_map(&maps.hi[0], p.hi[0], p.m, p.n, p.ldx, p.groups);
+    if (st == DR_OK) st = ns_map(&maps.hi[1], p.hi[1], p.m, p.n, p.ldx, p.groups);
+    if (st == DR_OK) st = ns_map(&maps.lo, p.lo, p.m, p.n, p.ldx, p.groups);
+    if (st == DR_OK) st = ns_map(&maps.E, p.E, p.n, p.n, p.lda, p.groups);
+    if (st == DR_OK) st = ns_map(&maps.F, p.F, p.n, p.n, p.lda, p.groups);
+    if (st == DR_OK) st = p.terms == 3 ? ns_map(&maps.Elo, p.Elo, p.n, p.n, p.lda, p.groups) : DR_OK;
+    if (st == DR_OK) st = p.terms == 3 ? ns_map(&maps.Flo, p.Flo, p.n, p.n, p.lda, p.groups) : DR_OK;
+    if (st != DR_OK) return st;
+    if (p.terms == 1) maps.Elo = maps.E, maps.Flo = maps.F;
+    if (!ns_attributes()) return DR_ERR_CUDA;
+    const bool counted = !(p.cluster || p.G == 1);
+    if (counted) {
+        ns_begin_kernel<<<dim3((unsigned)p.n_norm, (unsigned)p.batch), 256, 0, s>>>(p.in, p.norm, p.arrived, p.groups);
         count_launch();
+        st = launch_status();
+        if (st != DR_OK) return st;
     }
-    ns_norm_kernel<<<dim3(NS_NORM_BLOCKS, batch), 256, 0, s>>>(in, partial);
-    ns_scale_kernel<<<dim3(eb, batch), 256, 0, s>>>(in, partial, X);
-    const unsigned tn = (in.n + 63) / 64, tm = (in.m + 63) / 64;
-    for (int k = 0; k < steps; ++k) {
-        const float a = coef ? coef[3 * k] : 3.4445f, b = coef ? coef[3 * k + 1] : -4.7750f, c = coef ? coef[3 * k + 2] : 2.0315f;
-        ns_product_kernel<true><<<dim3(tn, tn, batch), 256, 0, s>>>(in.n, in.n, in.m, X, X, 0.f, nullptr, 1.f, A);
-        ns_product_kernel<false><<<dim3(tn, tn, batch), 256, 0, s>>>(in.n, in.n, in.n, A, A, b, A, c, B);
-        ns_product_kernel<false><<<dim3(tm, tn, batch), 256, 0, s>>>(in.n, in.m, in.n, B, X, a, X, 1.f, Y);
-        std::swap(X, Y);
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    cfg.gridDim = dim3((unsigned)(p.groups * p.G)); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM + 1024; cfg.stream = s;
+    cfg.attrs = attr;
+    if (counted) {
+        attr[0].id = cudaLaunchAttributeCooperative;
+        attr[0].val.cooperative = 1;
+        cfg.numAttrs = 1;
+    } else if (p.cluster) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = p.G; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.numAttrs = 1;
     }
-    ns_finish_kernel<<<dim3(eb, batch), 256, 0, s>>>(in, X, lr_scale, keep, out);
-    count_launch(3 + 3 * steps);
+    if (cudaLaunchKernelEx(&cfg, ns_kernel, maps, p) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+    count_launch();
     return launch_status();
 }
 
@@ -170,7 +756,7 @@ extern "C" int dr_orthogonalise_workspace_bytes(int batch, int rows, int cols, s
     if (!bytes) return DR_ERR_INVALID_ARG;
     const int st = ns_check(batch, rows, cols, 1, nullptr, 0.f);
     if (st != DR_OK) return st;
-    *bytes = ns_workspace(batch, rows, cols).total;
+    *bytes = ns_plan(batch, rows, cols).total;
     return DR_OK;
 }
 
@@ -181,12 +767,12 @@ extern "C" int dr_orthogonalise(int batch, int rows, int cols, const void* g, in
     if (!g || !o || !workspace || (flags & ~(unsigned)DR_NS_G_F32)) return DR_ERR_INVALID_ARG;
     const bool f32 = flags & DR_NS_G_F32;
     if (((uintptr_t)g & (f32 ? 3u : 1u)) || ((uintptr_t)o & 1u) || ((uintptr_t)workspace & 255)) return DR_ERR_ALIGNMENT;
-    if (workspace_bytes < ns_workspace(batch, rows, cols).total) return DR_ERR_WORKSPACE;
+    NsPlan l = ns_plan(batch, rows, cols);
+    if (workspace_bytes < l.total) return DR_ERR_WORKSPACE;
     if (batch == 0) return DR_OK;
     NsInput in = {};
-    in.rows = rows; in.cols = cols; in.tall = rows > cols; in.n = in.tall ? cols : rows; in.m = in.tall ? rows : cols;
-    in.g = g; in.g_f32 = f32; in.eps = eps;
-    return ns_run(batch, in, steps, coef, 0.f, 0.f, (__nv_bfloat16*)o, (char*)workspace, (cudaStream_t)stream);
+    in.rows = rows; in.cols = cols; in.g = g; in.g_f32 = f32; in.eps = eps; in.out = (__nv_bfloat16*)o;
+    return ns_run(l, in, steps, coef, (char*)workspace, (cudaStream_t)stream);
 }
 
 extern "C" int dr_muon_update(int batch, int rows, int cols, float* w, float* v, const float* g, float lr, float momentum, float decay, int nesterov,
@@ -195,11 +781,13 @@ extern "C" int dr_muon_update(int batch, int rows, int cols, float* w, float* v,
     if (st != DR_OK) return st;
     if (!w || !v || !g || !workspace) return DR_ERR_INVALID_ARG;
     if (((uintptr_t)w & 3u) || ((uintptr_t)v & 3u) || ((uintptr_t)g & 3u) || ((uintptr_t)w_bf16 & 1u) || ((uintptr_t)workspace & 255)) return DR_ERR_ALIGNMENT;
-    if (workspace_bytes < ns_workspace(batch, rows, cols).total) return DR_ERR_WORKSPACE;
+    NsPlan l = ns_plan(batch, rows, cols);
+    if (workspace_bytes < l.total) return DR_ERR_WORKSPACE;
     if (batch == 0) return DR_OK;
     NsInput in = {};
-    in.rows = rows; in.cols = cols; in.tall = rows > cols; in.n = in.tall ? cols : rows; in.m = in.tall ? rows : cols;
-    in.g = g; in.g_f32 = 1; in.eps = eps; in.v = v; in.w = w; in.momentum = momentum; in.nesterov = nesterov != 0;
-    const float scale = rows > cols ? sqrtf((float)rows / (float)cols) : 1.f;
-    return ns_run(batch, in, steps, coef, lr * scale, 1.f - lr * decay, (__nv_bfloat16*)w_bf16, (char*)workspace, (cudaStream_t)stream);
+    in.rows = rows; in.cols = cols; in.g = g; in.g_f32 = 1; in.eps = eps; in.v = v; in.w = w; in.momentum = momentum; in.nesterov = nesterov != 0;
+    in.lr_scale = lr * (rows > cols ? sqrtf((float)rows / (float)cols) : 1.f);
+    in.keep = 1.f - lr * decay;
+    in.out = (__nv_bfloat16*)w_bf16;
+    return ns_run(l, in, steps, coef, (char*)workspace, (cudaStream_t)stream);
 }
