@@ -45,6 +45,7 @@ struct NsInput {
     float eps;
     float lr_scale, keep;       // w <- keep w - lr_scale O
     __nv_bfloat16* out;         // O, or the bfloat16 copy of w (may be nullptr then)
+    int vec;                    // rows of a multiple of 8 elements at 16-byte aligned addresses: 16-byte accesses
 };
 
 struct NsParams {
@@ -54,6 +55,7 @@ struct NsParams {
     int G, groups, cluster;
     int nt_a, nt_s, nt_x;       // tile columns of the three products (rows: 128)
     int tiles_a, tiles_s, tiles_x;
+    int full_a, full_s;         // whether all tiles of A and of E E are computed, not those of the lower triangle alone
     int splits;                 // ranges of the long axis in A = X X^T
     int terms;                  // 1: hi hi;  3: hi hi + hi lo + lo hi
     int stages, stage_bytes;
@@ -97,22 +99,74 @@ __device__ __forceinline__ uint32_t pack_half(float a, float b) {
 }
 
 // ------------------------------------------------------------------------------------------------ input and output
-__device__ __forceinline__ float ns_value(const NsInput& in, size_t i) {
-    const float g = in.g_f32 ? ((const float*)in.g)[i] : __bfloat162float(((const __nv_bfloat16*)in.g)[i]);
-    if (!in.v) return g;
-    const float v = in.v[i];
-    return in.nesterov ? fmaf(in.momentum, v, g) : v;
+// CN consecutive values of U: from the gradient, or from the updated momentum and, with Nesterov, the gradient
+template <int CN, typename T> __device__ __forceinline__ void ns_read(const T* p, float* f);
+template <> __device__ __forceinline__ void ns_read<1, float>(const float* p, float* f) { f[0] = *p; }
+template <> __device__ __forceinline__ void ns_read<1, __nv_bfloat16>(const __nv_bfloat16* p, float* f) { f[0] = __bfloat162float(*p); }
+template <> __device__ __forceinline__ void ns_read<8, float>(const float* p, float* f) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+template <> __device__ __forceinline__ void ns_read<8, __nv_bfloat16>(const __nv_bfloat16* p, float* f) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    f[0] = bf16_lo(a.x); f[1] = bf16_hi(a.x); f[2] = bf16_lo(a.y); f[3] = bf16_hi(a.y);
+    f[4] = bf16_lo(a.z); f[5] = bf16_hi(a.z); f[6] = bf16_lo(a.w); f[7] = bf16_hi(a.w);
+}
+template <int CN> __device__ __forceinline__ void ns_write(float* p, const float* f) {
+    if (CN == 8) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1 % CN], f[2 % CN], f[3 % CN]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(f[4 % CN], f[5 % CN], f[6 % CN], f[7 % CN]);
+    } else {
+        *p = f[0];
+    }
+}
+template <int CN> __device__ __forceinline__ void ns_write(__nv_bfloat16* p, const float* f) {
+    if (CN == 8) *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1 % CN]), pack_bf16(f[2 % CN], f[3 % CN]), pack_bf16(f[4 % CN], f[5 % CN]), pack_bf16(f[6 % CN], f[7 % CN]));
+    else *p = __float2bfloat16_rn(f[0]);
+}
+template <int CN>
+__device__ __forceinline__ void ns_value(const NsInput& in, size_t i, float* u) {
+    if (in.v) {
+        ns_read<CN>(in.v + i, u);
+        if (in.nesterov) {
+            float g[CN];
+            ns_read<CN>((const float*)in.g + i, g);
+#pragma unroll
+            for (int c = 0; c < CN; ++c) u[c] = fmaf(in.momentum, u[c], g[c]);
+        }
+    } else if (in.g_f32) {
+        ns_read<CN>((const float*)in.g + i, u);
+    } else {
+        ns_read<CN>((const __nv_bfloat16*)in.g + i, u);
+    }
 }
 
 // v <- momentum v + g and this thread's part of the sum of squares of U (in float64: no size of U overflows or vanishes)
-__device__ __forceinline__ double ns_momentum(const NsInput& in, size_t base, size_t per, size_t first, size_t stride) {
+template <int CN>
+__device__ __forceinline__ double ns_momentum_part(const NsInput& in, size_t base, size_t count, size_t first, size_t stride) {
     double s = 0.;
-    for (size_t i = first; i < per; i += stride) {
-        if (in.v) in.v[base + i] = fmaf(in.momentum, in.v[base + i], ((const float*)in.g)[base + i]);
-        const double u = ns_value(in, base + i);
-        s = fma(u, u, s);
+    for (size_t i = first; i < count; i += stride) {
+        float u[CN], g[CN];
+        if (in.v) {
+            ns_read<CN>(in.v + base + i * CN, u);
+            ns_read<CN>((const float*)in.g + base + i * CN, g);
+#pragma unroll
+            for (int c = 0; c < CN; ++c) u[c] = fmaf(in.momentum, u[c], g[c]);
+            ns_write<CN>(in.v + base + i * CN, u);
+            if (in.nesterov) {
+#pragma unroll
+                for (int c = 0; c < CN; ++c) u[c] = fmaf(in.momentum, u[c], g[c]);
+            }
+        } else {
+            ns_value<CN>(in, base + i * CN, u);
+        }
+#pragma unroll
+        for (int c = 0; c < CN; ++c) s = fma((double)u[c], (double)u[c], s);
     }
     return s;
+}
+__device__ __forceinline__ double ns_momentum(const NsInput& in, size_t base, size_t per, size_t first, size_t stride) {
+    return in.vec ? ns_momentum_part<8>(in, base, per / 8, first, stride) : ns_momentum_part<1>(in, base, per, first, stride);
 }
 
 __device__ __forceinline__ double ns_warp_sum(double s) {
@@ -165,6 +219,10 @@ __device__ __forceinline__ NsItem ns_item(const NsParams& p, int item) {
         const int ni = (p.n + 127) / 128;
         it.j = item / ni;
         it.i = item - it.j * ni;
+    } else if (PHASE == NS_A ? p.full_a : p.full_s) {
+        const int ni = (p.n + 127) / 128;
+        it.j = it.tile / ni;
+        it.i = it.tile - it.j * ni;
     } else {
         ns_tri_tile(it.tile, p.n, PHASE == NS_A ? p.nt_a : p.nt_s, it.i, it.j);
     }
@@ -172,6 +230,22 @@ __device__ __forceinline__ NsItem ns_item(const NsParams& p, int item) {
 }
 
 // the first `count` of CN float16 values of a row (a whole number of 16-byte pieces in all but the diagonal's tiles)
+template <int CN>
+__device__ __forceinline__ void ns_mirror(__half* p, int ld, int i, int c0, const uint32_t* h, int count) {
+#pragma unroll
+    for (int c = 0; c < CN; ++c)
+        if (c < count) p[(size_t)(c0 + c) * ld + i] = __ushort_as_half((unsigned short)(h[c / 2] >> (16 * (c & 1))));
+}
+// v as float16 h and what that leaves out as float16 l
+template <int CN>
+__device__ __forceinline__ void ns_split(const float* v, uint32_t* h, uint32_t* l) {
+#pragma unroll
+    for (int c = 0; c < CN; c += 2) {
+        h[c / 2] = pack_half(v[c], v[c + 1]);
+        const float2 f = half2_at(h[c / 2]);
+        l[c / 2] = pack_half(v[c] - f.x, v[c + 1] - f.y);
+    }
+}
 template <int CN>
 __device__ __forceinline__ void ns_row_store(__half* p, const uint32_t* h, int count) {
     if (count == CN) {
@@ -184,14 +258,22 @@ __device__ __forceinline__ void ns_row_store(__half* p, const uint32_t* h, int c
     }
 }
 
-// What the drain of A leaves for (row i, columns c0 .. c0 + CN - 1), of which those up to the diagonal count.
+// What the drain of A leaves for (row i, columns c0 .. c0 + CN - 1): A in float32, its diagonal, and the rest as float16.  `full`: every
+// tile of the matrix is drained; otherwise those that reach the lower triangle, whose entries are mirrored.
 template <int CN>
-__device__ __forceinline__ void ns_emit_a(const NsParams& p, size_t mat, float* dvec, int i, int c0, float* v) {
-    if (c0 > i) return;
+__device__ __forceinline__ void ns_emit_a(const NsParams& p, size_t mat, float* dvec, bool full, int i, int c0, float* v) {
+    if (!full && c0 > i) return;
     float* A = p.A + mat;
+    const int last = full ? CN : min(CN, i - c0 + 1);
+    if (last == CN) {
 #pragma unroll
-    for (int c = 0; c < CN; c += 8) st8f(A + (size_t)i * p.lda + c0 + c, v + c);
-    if (i < c0 + CN) {
+        for (int c = 0; c < CN; c += 8) st8f(A + (size_t)i * p.lda + c0 + c, v + c);
+    } else {
+#pragma unroll
+        for (int c = 0; c < CN; ++c)
+            if (c < last) A[(size_t)i * p.lda + c0 + c] = v[c];
+    }
+    if (i >= c0 && i < c0 + CN) {
 #pragma unroll
         for (int c = 0; c < CN; ++c)
             if (c0 + c == i) {
@@ -199,62 +281,42 @@ __device__ __forceinline__ void ns_emit_a(const NsParams& p, size_t mat, float* 
                 v[c] = 0.f;
             }
     }
-    uint32_t h[CN / 2];
-#pragma unroll
-    for (int c = 0; c < CN; c += 2) h[c / 2] = pack_half(v[c], v[c + 1]);
-    float l[CN];
-#pragma unroll
-    for (int c = 0; c < CN; c += 2) {
-        const float2 f = half2_at(h[c / 2]);
-        l[c] = v[c] - f.x;
-        l[c + 1] = v[c + 1] - f.y;
-    }
-    const int last = min(CN, i - c0 + 1);
+    uint32_t h[CN / 2], l[CN / 2];
+    ns_split<CN>(v, h, l);
     ns_row_store<CN>(p.E + mat + (size_t)i * p.lda + c0, h, last);
+    if (p.terms == 3) ns_row_store<CN>(p.Elo + mat + (size_t)i * p.lda + c0, l, last);
+    if (!full) {
+        ns_mirror<CN>(p.E + mat, p.lda, i, c0, h, last);
+        if (p.terms == 3) ns_mirror<CN>(p.Elo + mat, p.lda, i, c0, l, last);
+        if (p.full_s) {
 #pragma unroll
-    for (int c = 0; c < CN; ++c)
-        if (c < last) {
-            const __half e = __ushort_as_half((unsigned short)(h[c / 2] >> (16 * (c & 1)))), el = __float2half_rn(l[c]);
-            p.E[mat + (size_t)(c0 + c) * p.lda + i] = e;
-            if (p.terms == 3) {
-                p.Elo[mat + (size_t)i * p.lda + c0 + c] = el;
-                p.Elo[mat + (size_t)(c0 + c) * p.lda + i] = el;
-            }
+            for (int c = 0; c < CN; ++c)
+                if (c0 + c < i) A[(size_t)(c0 + c) * p.lda + i] = v[c];
         }
+    }
 }
 
-// (row i, columns c0 ..) of E E -> the polynomial b A + c A A: F off the diagonal, a + its diagonal as the row's factor
+// (row i, columns c0 ..) of E E -> the polynomial b A + c A A: F off the diagonal, a + its diagonal as the row's factor.
+// e: A's row, dj: A's diagonal at the columns
 template <int CN>
-__device__ __forceinline__ void ns_emit_f(const NsParams& p, size_t mat, const float* dvec, float* rs, float a, float b, float cc, int i, int c0, float* v) {
-    if (c0 > i) return;
-    float e[CN];
-#pragma unroll
-    for (int c = 0; c < CN; c += 8) ld8f(p.A + mat + (size_t)i * p.lda + c0 + c, e + c);
-    const float di = dvec[i];
-    const int last = min(CN, i - c0 + 1);
-    uint32_t h[CN / 2];
+__device__ __forceinline__ void ns_emit_f(const NsParams& p, size_t mat, float* rs, const float* coef, bool full, int i, int c0, float di, const float* dj, const float* e, float* v) {
+    if (!full && c0 > i) return;
+    const float a = coef[0], b = coef[1], cc = coef[2];
 #pragma unroll
     for (int c = 0; c < CN; ++c) {
-        if (c0 + c < i) v[c] = fmaf(b, e[c], cc * fmaf(di + dvec[c0 + c], e[c], v[c]));
-        else if (c0 + c == i) {
-            rs[i] = a + fmaf(b, di, cc * fmaf(di, di, v[c]));
-            v[c] = 0.f;
-        }
+        const float f = fmaf(b, e[c], cc * fmaf(di + dj[c], e[c], v[c]));
+        if (c0 + c == i) rs[i] = a + fmaf(b, di, cc * fmaf(di, di, v[c]));
+        v[c] = c0 + c == i ? 0.f : f;
     }
-#pragma unroll
-    for (int c = 0; c < CN; c += 2) h[c / 2] = pack_half(v[c], v[c + 1]);
+    uint32_t h[CN / 2], l[CN / 2];
+    ns_split<CN>(v, h, l);
+    const int last = full ? CN : min(CN, i - c0 + 1);
     ns_row_store<CN>(p.F + mat + (size_t)i * p.lda + c0, h, last);
-#pragma unroll
-    for (int c = 0; c < CN; ++c)
-        if (c < last) {
-            const __half fh = __ushort_as_half((unsigned short)(h[c / 2] >> (16 * (c & 1))));
-            p.F[mat + (size_t)(c0 + c) * p.lda + i] = fh;
-            if (p.terms == 3) {
-                const __half fl = __float2half_rn(v[c] - __half2float(fh));
-                p.Flo[mat + (size_t)i * p.lda + c0 + c] = fl;
-                p.Flo[mat + (size_t)(c0 + c) * p.lda + i] = fl;
-            }
-        }
+    if (p.terms == 3) ns_row_store<CN>(p.Flo + mat + (size_t)i * p.lda + c0, l, last);
+    if (!full) {
+        ns_mirror<CN>(p.F + mat, p.lda, i, c0, h, last);
+        if (p.terms == 3) ns_mirror<CN>(p.Flo + mat, p.lda, i, c0, l, last);
+    }
 }
 
 struct NsMaps { CUtensorMap hi[2], lo, E, F, Elo, Flo; };
@@ -345,13 +407,37 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
     } else {
         const int q = warp & 3, half = (warp - 2) >> 2;
         const size_t mat = (size_t)group * p.n * p.lda, xm = (size_t)group * p.n * p.ldx;
-        float* dvec = p.d + (size_t)group * p.n;
-        float* rs = p.rs + (size_t)group * p.n;
+        float* dvec = p.d + (size_t)group * p.lda;
+        float* rs = p.rs + (size_t)group * p.lda;
         for (int item = rank; item < items; item += p.G) {
             const NsItem it = ns_item<PHASE>(p, item);
             const int row = it.i * 128 + q * 32 + lane;
-            float factor = 0.f;
+            // Chunks of 16 columns, two at a time: columns half * 16 + 0 .. 15 and + 32 .. 47 of every 64.  What a chunk needs from memory is
+            // requested a pair ahead, the first pair before the product is waited for.
+            float factor = 0.f, dj_next = 0.f;
+            Half16 h[2], l[2];
+            alignas(32) float e[2][16];
+            auto request = [&](int pair, int k) {
+                const int col = it.j * nt + pair * 64 + half * 16 + 32 * k;
+                if (PHASE == NS_X && row < p.n && col < p.ldx) {
+                    const size_t at = xm + (size_t)row * p.ldx + col;
+                    h[k] = ld16h(p.hi[src] + at);
+                    l[k] = ld16h(p.lo + at);
+                }
+                if (PHASE == NS_S && row < p.n && col < p.lda) {
+                    ld8f(p.A + mat + (size_t)row * p.lda + col, e[k]);
+                    ld8f(p.A + mat + (size_t)row * p.lda + col + 8, e[k] + 8);
+                }
+            };
+            auto request_d = [&](int pair) {
+                const int col = it.j * nt + pair * 64 + half * 16 + (lane & 15) + 2 * (lane & 16);
+                if (PHASE == NS_S) dj_next = col < p.lda ? dvec[col] : 0.f;
+            };
             if (PHASE == NS_X && row < p.n) factor = rs[row];
+            if (PHASE == NS_S && row < p.n) factor = dvec[row];
+            request(0, 0);
+            request(0, 1);
+            request_d(0);
             const bool ok = __all_sync(0xffffffffu, mbar_wait(&sh.tfull[pipe.acc], pipe.acc_phase, abort_flag));
             if (!ok) {
                 if (!*abort_flag) report_timeout(p.status, 74, item);
@@ -360,39 +446,48 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             }
             tc_fence_after();
             const uint32_t acc = tmem + pipe.acc * 256 + ((uint32_t)(q * 32) << 16);
-            for (int c = half * 16; c < nt; c += 32) {
-                uint32_t raw[16];
-                float v[16];
-                tmem_ld_x16(acc + c, raw);
-                tmem_ld_wait();
+            for (int pair = 0; pair < nt / 64; ++pair) {
+                const float dj_all = dj_next;
+                if (pair + 1 < nt / 64) request_d(pair + 1);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(raw[e]);
-                const int col = it.j * nt + c;
-                if (PHASE == NS_A && p.splits > 1) {
-                    float* out = p.part + (((size_t)group * p.splits + it.split) * p.tiles_a + it.tile) * nt * 128 + (size_t)c * 128 + q * 32 + lane;
+                for (int k = 0; k < 2; ++k) {
+                    const int c = pair * 64 + half * 16 + 32 * k, col = it.j * nt + c;
+                    uint32_t raw[16];
+                    alignas(32) float v[16];
+                    tmem_ld_x16(acc + c, raw);
+                    float dj[16];
+                    if (PHASE == NS_S) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) out[e * 128] = v[e];
-                } else if (row < p.n) {
-                    if (PHASE == NS_A) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) v[e] *= 1.f / (NS_SCALE * NS_SCALE);
-                        ns_emit_a<16>(p, mat, dvec, row, col, v);
-                    } else if (PHASE == NS_S) {
-                        ns_emit_f<16>(p, mat, dvec, rs, coef[0], coef[1], coef[2], row, col, v);
-                    } else if (col < p.ldx) {
-                        const size_t at = xm + (size_t)row * p.ldx + col;
-                        Half16 h = ld16h(p.hi[src] + at), l = ld16h(p.lo + at);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float2 fh = half2_at(h.u[e]), fl = half2_at(l.u[e]);
-                            const float x0 = fmaf(factor, fh.x + fl.x, v[2 * e]), x1 = fmaf(factor, fh.y + fl.y, v[2 * e + 1]);
-                            h.u[e] = pack_half(x0, x1);
-                            const float2 r = half2_at(h.u[e]);
-                            l.u[e] = pack_half(x0 - r.x, x1 - r.y);
-                        }
-                        st16h(p.hi[src ^ 1] + at, h);
-                        st16h(p.lo + at, l);
+                        for (int t = 0; t < 16; ++t) dj[t] = __shfl_sync(0xffffffffu, dj_all, t + 16 * k);
                     }
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int t = 0; t < 16; ++t) v[t] = __uint_as_float(raw[t]);
+                    if (PHASE == NS_A && p.splits > 1) {
+                        float* out = p.part + (((size_t)group * p.splits + it.split) * p.tiles_a + it.tile) * nt * 128 + (size_t)c * 128 + q * 32 + lane;
+#pragma unroll
+                        for (int t = 0; t < 16; ++t) out[t * 128] = v[t];
+                    } else if (row < p.n) {
+                        if (PHASE == NS_A && col < p.lda) {
+#pragma unroll
+                            for (int t = 0; t < 16; ++t) v[t] *= 1.f / (NS_SCALE * NS_SCALE);
+                            ns_emit_a<16>(p, mat, dvec, p.full_a, row, col, v);
+                        } else if (PHASE == NS_S && col < p.lda) {
+                            ns_emit_f<16>(p, mat, rs, coef, p.full_s, row, col, factor, dj, e[k], v);
+                        } else if (PHASE == NS_X && col < p.ldx) {
+                            const size_t at = xm + (size_t)row * p.ldx + col;
+#pragma unroll
+                            for (int t = 0; t < 8; ++t) {
+                                const float2 fh = half2_at(h[k].u[t]), fl = half2_at(l[k].u[t]);
+                                v[2 * t] = fmaf(factor, fh.x + fl.x, v[2 * t]);
+                                v[2 * t + 1] = fmaf(factor, fh.y + fl.y, v[2 * t + 1]);
+                            }
+                            ns_split<16>(v, h[k].u, l[k].u);
+                            st16h(p.hi[src ^ 1] + at, h[k]);
+                            st16h(p.lo + at, l[k]);
+                        }
+                    }
+                    if (pair + 1 < nt / 64) request(pair + 1, k);
                 }
             }
             tc_fence_before();
@@ -437,74 +532,142 @@ __device__ __forceinline__ void ns_group_sync(const NsParams& p, NsShared& sh, i
     asm volatile("fence.proxy.async;" ::: "memory");
 }
 
-// X_0 from U, transposed where U is tall (through a 64 x 64 tile in shared memory)
-__device__ __forceinline__ void ns_load_x(const NsParams& p, float* tile, int group, int rank, size_t base, float inv) {
-    const NsInput& in = p.in;
-    __half* hi = p.hi[0] + (size_t)group * p.n * p.ldx;
-    __half* lo = p.lo + (size_t)group * p.n * p.ldx;
-    auto put = [&](size_t at, float u) {
-        const float x = u * inv;
-        const __half h = __float2half_rn(x);
-        hi[at] = h;
-        lo[at] = __float2half_rn(x - __half2float(h));
-    };
-    if (!in.tall) {
-        const size_t per = (size_t)in.rows * in.cols;
-        for (size_t i = (size_t)rank * NS_THREADS + threadIdx.x; i < per; i += (size_t)p.G * NS_THREADS) {
-            const size_t r = i / in.cols;
-            put(r * p.ldx + (i - r * in.cols), ns_value(in, base + i));
-        }
+// 8 (or 1) values of X_0 from U
+template <int CN>
+__device__ __forceinline__ void ns_put_x(__half* hi, __half* lo, float inv, float* u) {
+#pragma unroll
+    for (int c = 0; c < CN; ++c) u[c] *= inv;
+    if (CN == 8) {
+        uint32_t h[4], l[4];
+        ns_split<8>(u, h, l);
+        *reinterpret_cast<uint4*>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
     } else {
-        const int tr = (in.rows + 63) / 64, tc = (in.cols + 63) / 64;
-        for (int t = rank; t < tr * tc; t += p.G) {
-            const int r0 = t / tc * 64, c0 = t % tc * 64;
-            __syncthreads();
-            for (int e = threadIdx.x; e < 4096; e += NS_THREADS) {
-                const int r = r0 + (e >> 6), c = c0 + (e & 63);
-                if (r < in.rows && c < in.cols) tile[(e >> 6) * 65 + (e & 63)] = ns_value(in, base + (size_t)r * in.cols + c);
-            }
-            __syncthreads();
-            for (int e = threadIdx.x; e < 4096; e += NS_THREADS) {
-                const int c = c0 + (e >> 6), r = r0 + (e & 63);
-                if (r < in.rows && c < in.cols) put((size_t)c * p.ldx + r, tile[(e & 63) * 65 + (e >> 6)]);
-            }
-        }
+        *hi = __float2half_rn(u[0]);
+        *lo = __float2half_rn(u[0] - __half2float(*hi));
+    }
+}
+// 8 (or 1) values of the result: O, or the update of w
+template <int CN>
+__device__ __forceinline__ void ns_put_o(const NsInput& in, size_t at, float* o) {
+    if (in.w) {
+        float w[CN];
+        ns_read<CN>(in.w + at, w);
+#pragma unroll
+        for (int c = 0; c < CN; ++c) o[c] = fmaf(-in.lr_scale, o[c], in.keep * w[c]);
+        ns_write<CN>(in.w + at, o);
+    }
+    if (in.out) ns_write<CN>(in.out + at, o);
+}
+__device__ __forceinline__ void ns_get_x8(const __half* hi, const __half* lo, float* x) {
+    const uint4 h = *reinterpret_cast<const uint4*>(hi), l = *reinterpret_cast<const uint4*>(lo);
+    const uint32_t hu[4] = {h.x, h.y, h.z, h.w}, lu[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const float2 a = half2_at(hu[c]), b = half2_at(lu[c]);
+        x[2 * c] = (a.x + b.x) * (1.f / NS_SCALE);
+        x[2 * c + 1] = (a.y + b.y) * (1.f / NS_SCALE);
     }
 }
 
-__device__ __forceinline__ void ns_store_o(const NsParams& p, float* tile, int group, int rank, size_t base, int src) {
+// X_0 from U (LOAD) or the result from X.  Rows lie alike in both unless U is tall: a warp takes up to 1024 columns of a row.
+// A tall U is transposed through a 64 x 64 tile in shared memory.
+template <bool LOAD>
+__device__ __forceinline__ void ns_convert(const NsParams& p, float* tile, int group, int rank, size_t base, int src, float inv) {
     const NsInput& in = p.in;
-    const __half* hi = p.hi[src] + (size_t)group * p.n * p.ldx;
-    const __half* lo = p.lo + (size_t)group * p.n * p.ldx;
-    auto get = [&](size_t at) { return (__half2float(hi[at]) + __half2float(lo[at])) * (1.f / NS_SCALE); };
-    auto put = [&](size_t at, float o) {
-        if (in.w) {
-            o = fmaf(-in.lr_scale, o, in.keep * in.w[at]);
-            in.w[at] = o;
-        }
-        if (in.out) in.out[at] = __float2bfloat16_rn(o);
-    };
+    __half* hi = p.hi[src] + (size_t)group * p.n * p.ldx;
+    __half* lo = p.lo + (size_t)group * p.n * p.ldx;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (!in.tall) {
-        const size_t per = (size_t)in.rows * in.cols;
-        for (size_t i = (size_t)rank * NS_THREADS + threadIdx.x; i < per; i += (size_t)p.G * NS_THREADS) {
-            const size_t r = i / in.cols;
-            put(base + i, get(r * p.ldx + (i - r * in.cols)));
-        }
-    } else {
-        const int tr = (in.rows + 63) / 64, tc = (in.cols + 63) / 64;
-        for (int t = rank; t < tr * tc; t += p.G) {
-            const int r0 = t / tc * 64, c0 = t % tc * 64;
-            __syncthreads();
-            for (int e = threadIdx.x; e < 4096; e += NS_THREADS) {
-                const int c = c0 + (e >> 6), r = r0 + (e & 63);
-                if (r < in.rows && c < in.cols) tile[(e & 63) * 65 + (e >> 6)] = get((size_t)c * p.ldx + r);
+        const int segs = (in.cols + 1023) / 1024, units = in.rows * segs;
+        for (int u = rank * (NS_THREADS / 32) + warp; u < units; u += p.G * (NS_THREADS / 32)) {
+            const int r = u / segs, c0 = (u - r * segs) * 1024, c1 = min(in.cols, c0 + 1024);
+            const size_t x = (size_t)r * p.ldx, o = base + (size_t)r * in.cols;
+            if (in.vec) {
+#pragma unroll 4
+                for (int c = c0 + lane * 8; c < c1; c += 256) {
+                    float f[8];
+                    if (LOAD) {
+                        ns_value<8>(in, o + c, f);
+                        ns_put_x<8>(hi + x + c, lo + x + c, inv, f);
+                    } else {
+                        ns_get_x8(hi + x + c, lo + x + c, f);
+                        ns_put_o<8>(in, o + c, f);
+                    }
+                }
+            } else {
+#pragma unroll 4
+                for (int c = c0 + lane; c < c1; c += 32) {
+                    float f[1];
+                    if (LOAD) {
+                        ns_value<1>(in, o + c, f);
+                        ns_put_x<1>(hi + x + c, lo + x + c, inv, f);
+                    } else {
+                        f[0] = (__half2float(hi[x + c]) + __half2float(lo[x + c])) * (1.f / NS_SCALE);
+                        ns_put_o<1>(in, o + c, f);
+                    }
+                }
             }
-            __syncthreads();
-            for (int e = threadIdx.x; e < 4096; e += NS_THREADS) {
-                const int r = r0 + (e >> 6), c = c0 + (e & 63);
-                if (r < in.rows && c < in.cols) put(base + (size_t)r * in.cols + c, tile[(e >> 6) * 65 + (e & 63)]);
-            }
         }
+        return;
+    }
+    const int tr = (in.rows + 63) / 64, tc = (in.cols + 63) / 64;
+    for (int t = rank; t < tr * tc; t += p.G) {
+        const int r0 = t / tc * 64, c0 = (t - t / tc * tc) * 64;
+        // tile[row of U][column of U]
+        auto user = [&]() {
+            if (in.vec) {
+                for (int e = threadIdx.x; e < 512; e += NS_THREADS) {
+                    const int r = e >> 3, c = (e & 7) * 8;
+                    if (r0 + r >= in.rows || c0 + c >= in.cols) continue;
+                    const size_t o = base + (size_t)(r0 + r) * in.cols + c0 + c;
+                    float f[8];
+                    if (LOAD) ns_value<8>(in, o, f);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (LOAD) tile[r * 65 + c + k] = f[k];
+                        else f[k] = tile[r * 65 + c + k];
+                    }
+                    if (!LOAD) ns_put_o<8>(in, o, f);
+                }
+            } else {
+                for (int e = threadIdx.x; e < 4096; e += NS_THREADS) {
+                    const int r = e >> 6, c = e & 63;
+                    if (r0 + r >= in.rows || c0 + c >= in.cols) continue;
+                    const size_t o = base + (size_t)(r0 + r) * in.cols + c0 + c;
+                    float f[1];
+                    if (LOAD) {
+                        ns_value<1>(in, o, f);
+                        tile[r * 65 + c] = f[0];
+                    } else {
+                        f[0] = tile[r * 65 + c];
+                        ns_put_o<1>(in, o, f);
+                    }
+                }
+            }
+        };
+        // X's rows are padded to 64 columns: whole vectors there
+        auto inner = [&]() {
+            for (int e = threadIdx.x; e < 512; e += NS_THREADS) {
+                const int c = e & 63, r = (e >> 6) * 8;
+                if (c0 + c >= in.cols) continue;
+                const size_t x = (size_t)(c0 + c) * p.ldx + r0 + r;
+                float f[8];
+                if (!LOAD) ns_get_x8(hi + x, lo + x, f);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (LOAD) f[k] = r0 + r + k < in.rows ? tile[(r + k) * 65 + c] : 0.f;
+                    else tile[(r + k) * 65 + c] = f[k];
+                }
+                if (LOAD) ns_put_x<8>(hi + x, lo + x, inv, f);
+            }
+        };
+        __syncthreads();
+        if (LOAD) user();
+        else inner();
+        __syncthreads();
+        if (LOAD) inner();
+        else user();
     }
 }
 
@@ -548,7 +711,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
         double s = 0.;
         for (int i = lane; i < p.n_norm; i += 32) s += norm[i];
         const float inv = (float)((double)NS_SCALE / (sqrt(ns_warp_sum(s)) + (double)p.in.eps));
-        ns_load_x(p, tile, group, rank, base, inv);
+        ns_convert<true>(p, tile, group, rank, base, 0, inv);
         ns_group_sync(p, sh, group, epoch);
         int src = 0;
         for (int k = 0; k < p.steps; ++k, src ^= 1) {
@@ -563,13 +726,13 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
                     ns_tri_tile(t, p.n, nt, i, j);
                     const int row = i * 128 + (rem & 3) * 32 + lane, c = (rem >> 2) * 8;
                     const float* in = p.part + ((size_t)group * p.splits * p.tiles_a + t) * nt * 128 + (size_t)c * 128 + (rem & 3) * 32 + lane;
-                    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    alignas(32) float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                     for (int q = 0; q < p.splits; ++q)
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[e] += in[(size_t)q * p.tiles_a * nt * 128 + e * 128];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] *= 1.f / (NS_SCALE * NS_SCALE);
-                    if (row < p.n) ns_emit_a<8>(p, (size_t)group * p.n * p.lda, p.d + (size_t)group * p.n, row, j * nt + c, v);
+                    if (row < p.n) ns_emit_a<8>(p, (size_t)group * p.n * p.lda, p.d + (size_t)group * p.lda, false, row, j * nt + c, v);
                 }
                 ns_group_sync(p, sh, group, epoch);
             }
@@ -578,7 +741,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
             ns_product<NS_X>(p, maps, sh, smem, tmem, pipe, group, rank, src, nullptr);
             ns_group_sync(p, sh, group, epoch);
         }
-        ns_store_o(p, tile, group, rank, base, src);
+        ns_convert<false>(p, tile, group, rank, base, src, 0.f);
         ns_group_sync(p, sh, group, epoch);     // the buffers are free for the group's next matrix
     }
     if (sh.abort) {                             // copies and products in flight end within microseconds; then the CTA may go
@@ -660,13 +823,19 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     p.G = g;
     p.groups = std::min(batch1, std::max(1, sms / g));
     // the widest tiles that still give every CTA of the group one
-    auto widest = [&](auto tiles) { return tiles(256) >= g ? 256 : tiles(128) >= g ? 128 : 64; };
-    p.nt_x = widest(tiles_x);
-    p.nt_s = widest([&](int nt) { return ns_tri_tiles(p.n, nt); });
-    p.nt_a = ns_tri_tiles(p.n, 256) >= g ? 256 : 128;
-    p.tiles_x = tiles_x(p.nt_x); p.tiles_s = ns_tri_tiles(p.n, p.nt_s); p.tiles_a = ns_tri_tiles(p.n, p.nt_a);
+    p.nt_x = tiles_x(256) >= g ? 256 : tiles_x(128) >= g ? 128 : 64;
+    p.tiles_x = tiles_x(p.nt_x);
     const int kb = (p.m + 63) / 64;
-    p.splits = std::max(1, std::min(g / p.tiles_a, kb / 4));
+    auto all = [&](int nt) { return ni * ((p.n + nt - 1) / nt); };
+    // E E: all tiles of 64 columns where the group has a CTA for each (no mirrored stores); otherwise the lower triangle
+    p.full_s = all(64) <= g;
+    p.nt_s = p.full_s ? 64 : ns_tri_tiles(p.n, 256) >= g ? 256 : 128;
+    p.tiles_s = p.full_s ? all(64) : ns_tri_tiles(p.n, p.nt_s);
+    // A: likewise where the long axis is short; a long one is split over the CTAs, whose parts meet after another barrier
+    p.full_a = all(64) <= g && kb <= tunable("DR_NS_FULL_KB", 48);
+    p.nt_a = p.full_a ? 64 : ns_tri_tiles(p.n, 256) >= g ? 256 : 128;
+    p.tiles_a = p.full_a ? all(64) : ns_tri_tiles(p.n, p.nt_a);
+    p.splits = p.full_a ? 1 : std::max(1, std::min(g / p.tiles_a, kb / 4));
     p.stage_bytes = (2 + std::max(p.nt_x, std::max(p.nt_s, p.nt_a)) / 64) * NS_BOX;
     p.stages = std::min(NS_STAGES, NS_SMEM / p.stage_bytes);
     l.norm_blocks = (int)std::min<size_t>(NS_NORM_BLOCKS, ((size_t)rows * cols + 2047) / 2048);
@@ -676,7 +845,7 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     const size_t x = (size_t)p.groups * p.n * p.ldx * 2, a = (size_t)p.groups * p.n * p.lda * 2;
     take(l.hi0, x); take(l.hi1, x); take(l.lo, x);
     take(l.E, a); take(l.F, a); take(l.Elo, p.terms == 3 ? a : 0); take(l.Flo, p.terms == 3 ? a : 0); take(l.A, 2 * a);
-    take(l.d, (size_t)p.groups * p.n * 4); take(l.rs, (size_t)p.groups * p.n * 4);
+    take(l.d, (size_t)p.groups * p.lda * 4); take(l.rs, (size_t)p.groups * p.lda * 4);
     take(l.part, p.splits > 1 ? (size_t)p.groups * p.splits * p.tiles_a * p.nt_a * 128 * 4 : 0);
     take(l.norm, (size_t)(p.cluster || g == 1 ? p.groups : batch1) * p.n_norm * 8);
     take(l.arrived, (size_t)p.groups * 4);
@@ -705,6 +874,7 @@ static int ns_run(NsPlan& l, const NsInput& in, int steps, const float* coef, ch
     p.in = in;
     p.in.tall = p.in.rows > p.in.cols;
     p.steps = steps;
+    p.in.vec = (p.in.cols & 7) == 0 && aligned16(in.g) && aligned16(in.v) && aligned16(in.w) && aligned16(in.out);
     const float usual[3] = {3.4445f, -4.7750f, 2.0315f};
     for (int i = 0; i < 3 * steps; ++i) p.coef[i] = coef ? coef[i] : usual[i % 3];
     p.hi[0] = (__half*)(ws + l.hi0); p.hi[1] = (__half*)(ws + l.hi1); p.lo = (__half*)(ws + l.lo);
