@@ -15,11 +15,12 @@
 //
 // Execution.  One persistent kernel runs all products of a matrix: a group of G CTAs (one per SM) works through the phases
 // A -> F -> X of every step and meets at a barrier between them; a batch is spread over the groups.  Inside a phase a CTA is a
-// pipeline: one warp loads 64-deep operand slices by TMA, one issues tcgen05.mma into one of two accumulators in tensor
+// pipeline: one warp loads 128-deep operand slices by TMA, one issues tcgen05.mma into one of two accumulators in tensor
 // memory, eight drain the other one.  A group of up to 16 CTAs is a thread-block cluster and uses its barrier; a larger one is
 // launched cooperatively and counts arrivals in global memory.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 #include <cuda_fp16.h>
 
 #include "conv_common.cuh"
@@ -31,7 +32,10 @@ using namespace ptx;
 constexpr int NS_THREADS = 320;             // warp 0: TMA, warp 1: MMA, warps 2 - 9: drain
 constexpr int NS_STAGES = 8;                // at most
 constexpr int NS_SMEM = 196608;             // operand ring
-constexpr int NS_BOX = 64 * 128;            // one TMA box: 64 rows of 64 float16
+constexpr int NS_CHUNK = 128 * 128;          // 128 rows x 64 float16
+// 64-column chunks a stage is deep in the contraction: 2, since the issuing threads take 400 cycles to hand a stage over; 1 where two
+// CTAs share tiles of 256 x 256, whose MMAs take longer than that and want more stages of the same bytes (1.24 against 1.35 ms at 4096 x 4096)
+__host__ __device__ constexpr int ns_depth(bool pair) { return pair ? 1 : 2; }
 constexpr float NS_SCALE = 4096.f;          // X is stored times this: entries of every size stay in float16's normal range
 constexpr int NS_NORM_BLOCKS = 256;         // partial sums of squares at most
 
@@ -52,8 +56,9 @@ struct NsParams {
     NsInput in;
     int batch, steps;
     int n, m, ldx, lda;         // X: n x m, row stride ldx; A, E, F: n x n, row stride lda
-    int G, groups, cluster;
-    int nt_a, nt_s, nt_x;       // tile columns of the three products (rows: 128)
+    int G, groups, cluster, pair;
+    int tr;                     // tile rows: 128, or 256 where two CTAs share a tile
+    int nt_a, nt_s, nt_x;       // tile columns of the three products
     int tiles_a, tiles_s, tiles_x;
     int full_a, full_s;         // whether all tiles of A and of E E are computed, not those of the lower triangle alone
     int splits;                 // ranges of the long axis in A = X X^T
@@ -75,6 +80,12 @@ struct NsShared {
     int abort;
     double red[10];
 };
+
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
+    asm volatile("{\n.reg .pred P;\nelect.sync _|P, 0xffffffff;\nselp.u32 %0, 1, 0, P;\n}" : "=r"(e));
+    return e != 0;
+}
 
 struct __align__(32) Half16 { uint32_t u[8]; };
 struct __align__(32) Float8 { float f[8]; };
@@ -191,21 +202,21 @@ __global__ void __launch_bounds__(256) ns_begin_kernel(const NsInput in, double*
 }
 
 // ------------------------------------------------------------------------------------------------ the products' tiles
-// Tiles of 128 rows x nt columns that reach the lower triangle, row by row.
-__host__ __device__ __forceinline__ int ns_tri_row(int i, int n, int nt) { return min((n + nt - 1) / nt, (i * 128 + 127) / nt + 1); }
-__device__ __forceinline__ void ns_tri_tile(int t, int n, int nt, int& i, int& j) {
+// Tiles of tr rows x nt columns that reach the lower triangle, row by row.
+__host__ __device__ __forceinline__ int ns_tri_row(int i, int n, int tr, int nt) { return min((n + nt - 1) / nt, (i * tr + tr - 1) / nt + 1); }
+__device__ __forceinline__ void ns_tri_tile(int t, int n, int tr, int nt, int& i, int& j) {
     i = 0;
-    for (int c; t >= (c = ns_tri_row(i, n, nt)); ++i) t -= c;
+    for (int c; t >= (c = ns_tri_row(i, n, tr, nt)); ++i) t -= c;
     j = t;
 }
 
 enum { NS_A, NS_S, NS_X };
 struct NsItem { int i, j, k0, k1, split, tile; };
-template <int PHASE>
+template <int PHASE, bool PAIR>
 __device__ __forceinline__ NsItem ns_item(const NsParams& p, int item) {
     NsItem it;
     it.split = 0;
-    const int kb = ((PHASE == NS_A ? p.m : p.n) + 63) / 64;
+    const int kb = ((PHASE == NS_A ? p.m : p.n) + 64 * ns_depth(PAIR) - 1) / (64 * ns_depth(PAIR));
     it.k0 = 0;
     it.k1 = kb;
     it.tile = item;
@@ -216,15 +227,15 @@ __device__ __forceinline__ NsItem ns_item(const NsParams& p, int item) {
         it.k1 = (int)((long long)kb * (it.split + 1) / p.splits);
     }
     if (PHASE == NS_X) {
-        const int ni = (p.n + 127) / 128;
+        const int ni = (p.n + p.tr - 1) / p.tr;
         it.j = item / ni;
         it.i = item - it.j * ni;
     } else if (PHASE == NS_A ? p.full_a : p.full_s) {
-        const int ni = (p.n + 127) / 128;
+        const int ni = (p.n + p.tr - 1) / p.tr;
         it.j = it.tile / ni;
         it.i = it.tile - it.j * ni;
     } else {
-        ns_tri_tile(it.tile, p.n, PHASE == NS_A ? p.nt_a : p.nt_s, it.i, it.j);
+        ns_tri_tile(it.tile, p.n, p.tr, PHASE == NS_A ? p.nt_a : p.nt_s, it.i, it.j);
     }
     return it;
 }
@@ -319,7 +330,9 @@ __device__ __forceinline__ void ns_emit_f(const NsParams& p, size_t mat, float* 
     }
 }
 
-struct NsMaps { CUtensorMap hi[2], lo, E, F, Elo, Flo; };
+// All operands are seen as [group][64-column chunk][row][64].  The first operand's boxes are 128 rows x 2 chunks (pairs: 1); so are the
+// second's (b_*), except for tiles of 64 columns and in the X product of pairs (64 rows x 2 chunks).
+struct NsMaps { CUtensorMap hi[2], lo, E, F, Elo, Flo, ba_hi[2], ba_lo, bs_hi, bs_lo, bx_hi[2], bx_lo; };
 
 // Where the roles of a CTA stand in their rings; kept from phase to phase.
 struct NsPipe {
@@ -331,76 +344,90 @@ struct NsPipe {
     __device__ __forceinline__ void next_acc() { if (++acc == 2) { acc = 0; acc_phase ^= 1; } }
 };
 
-template <int PHASE>
+template <int PHASE, bool PAIR>
 __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps, NsShared& sh, uint32_t smem, uint32_t tmem, NsPipe& pipe, int group, int rank, int src, const float* coef) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int nt = PHASE == NS_A ? p.nt_a : PHASE == NS_S ? p.nt_s : p.nt_x;
     const int items = PHASE == NS_A ? p.tiles_a * p.splits : PHASE == NS_S ? p.tiles_s : p.tiles_x;
+    const int first = PAIR ? rank >> 1 : rank, step = PAIR ? p.G >> 1 : p.G, side = PAIR ? rank & 1 : 0;
+    const uint32_t full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]), tfull0 = smem_u32(&sh.tfull[0]), tempty0 = smem_u32(&sh.tempty[0]);
+    constexpr int D = ns_depth(PAIR);
     volatile int* abort_flag = &sh.abort;
+    // The issuing threads: one elected lane of a warp whose number the compiler knows to be uniform, so that addresses and
+    // descriptors stay in uniform registers.  With a plain lane test a hand-over of a stage cost 800 cycles, this way 400;
+    // and a stage is two TMA boxes and up to eight MMAs for the same reason.
     if (warp == 0) {
-        if (lane == 0) {
+        if (elect_one()) {
             const CUtensorMap *ah, *al, *bh, *bl;
-            if (PHASE == NS_A) { ah = bh = &maps.hi[src]; al = bl = &maps.lo; }
-            else if (PHASE == NS_S) { ah = bh = &maps.E; al = bl = &maps.Elo; }
-            else { ah = &maps.F; al = &maps.Flo; bh = &maps.hi[src]; bl = &maps.lo; }
-            const uint32_t bytes = (uint32_t)(2 + nt / 64) * NS_BOX;
-            for (int item = rank; item < items; item += p.G) {
-                const NsItem it = ns_item<PHASE>(p, item);
-                for (int term = 0; term < p.terms; ++term) {
+            if (PHASE == NS_A) { ah = &maps.hi[src]; al = &maps.lo; bh = &maps.ba_hi[src]; bl = &maps.ba_lo; }
+            else if (PHASE == NS_S) { ah = &maps.E; al = &maps.Elo; bh = &maps.bs_hi; bl = &maps.bs_lo; }
+            else { ah = &maps.F; al = &maps.Flo; bh = &maps.bx_hi[src]; bl = &maps.bx_lo; }
+            const uint32_t bytes = PAIR ? 4u * NS_CHUNK : (uint32_t)(2 * NS_CHUNK + nt * 256);
+            bool ok = true;
+            fence_proxy_async_all();                            // what the barrier made visible to this thread, to its TMA loads
+            uint32_t ready = mbar_test_u32(empty0 + 8 * pipe.stage, pipe.phase ^ 1);
+            for (int item = first; item < items && ok; item += step) {
+                const NsItem it = ns_item<PHASE, PAIR>(p, item);
+                const int ar = it.i * p.tr + side * 128, bc = it.j * nt + side * (nt / 2);
+                for (int term = 0; term < p.terms && ok; ++term) {
                     const CUtensorMap* am = term == 2 ? al : ah;
                     const CUtensorMap* bm = term == 1 ? bl : bh;
                     for (int kb = it.k0; kb < it.k1; ++kb) {
-                        uint64_t* full = &sh.full[pipe.stage];
-                        if (!mbar_wait(&sh.empty[pipe.stage], pipe.phase ^ 1, abort_flag)) {
+                        if (!ready && !mbar_wait_slow_u32(empty0 + 8 * pipe.stage, pipe.phase ^ 1, abort_flag)) {
                             if (!*abort_flag) report_timeout(p.status, 71, item);
                             *abort_flag = 1;
-                            goto out;
+                            ok = false;
+                            break;
                         }
-                        mbar_arrive_expect_tx(full, bytes);
+                        const uint32_t full = PAIR ? (full0 + 8 * pipe.stage) & PEER_BIT_MASK : full0 + 8 * pipe.stage;
                         const uint32_t dst = smem + pipe.stage * p.stage_bytes;
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) tma_load_3d_u32<false>(dst + r * NS_BOX, am, smem_u32(full), kb * 64, it.i * 128 + 64 * r, group, 1);
-                        for (int r = 0; r < nt / 64; ++r) {
-                            if (PHASE == NS_X) tma_load_3d_u32<false>(dst + (2 + r) * NS_BOX, bm, smem_u32(full), it.j * nt + 64 * r, kb * 64, group, 1);
-                            else tma_load_3d_u32<false>(dst + (2 + r) * NS_BOX, bm, smem_u32(full), kb * 64, it.j * nt + 64 * r, group, 1);
-                        }
+                        if (side == 0) mbar_expect_tx_u32(full, bytes);
+                        tma_load_4d_u32<PAIR>(dst, am, full, 0, ar, D * kb, group, 1u);
+                        if (PHASE == NS_X) tma_load_4d_u32<PAIR>(dst + D * NS_CHUNK, bm, full, 0, D * 64 * kb, bc >> 6, group, 1u);
+                        else tma_load_4d_u32<PAIR>(dst + D * NS_CHUNK, bm, full, 0, bc, D * kb, group, 1u);
                         pipe.next_stage(p.stages);
+                        ready = mbar_test_u32(empty0 + 8 * pipe.stage, pipe.phase ^ 1);
                     }
                 }
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (side == 0 && elect_one()) {
             // D float32, A and B float16; B of the X product lies with the contraction index as its rows
-            const uint32_t idesc = (1u << 4) | ((uint32_t)(nt >> 3) << 17) | (8u << 24) | (PHASE == NS_X ? 1u << 16 : 0u);
-            for (int item = rank; item < items; item += p.G) {
-                const NsItem it = ns_item<PHASE>(p, item);
-                if (!mbar_wait(&sh.tempty[pipe.acc], pipe.acc_phase ^ 1, abort_flag)) {
+            const uint32_t idesc = (1u << 4) | ((uint32_t)(nt >> 3) << 17) | ((PAIR ? 16u : 8u) << 24) | (PHASE == NS_X ? 1u << 16 : 0u);
+            const uint32_t b_chunk = (uint32_t)(PAIR ? 128 : nt) * 128u >> 4;       // 64 deep in K: a chunk of B's rows
+            bool ok = true;
+            uint32_t ready = mbar_test_u32(full0 + 8 * pipe.stage, pipe.phase);
+            for (int item = first; item < items && ok; item += step) {
+                const NsItem it = ns_item<PHASE, PAIR>(p, item);
+                if (!mbar_wait_u32(tempty0 + 8 * pipe.acc, pipe.acc_phase ^ 1, abort_flag)) {
                     if (!*abort_flag) report_timeout(p.status, 72, item);
                     *abort_flag = 1;
-                    goto out;
+                    break;
                 }
                 tc_fence_after();
                 const uint32_t acc = tmem + pipe.acc * 256;
                 uint32_t accumulate = 0;
                 for (int k = (it.k1 - it.k0) * p.terms; k > 0; --k) {
-                    if (!mbar_wait(&sh.full[pipe.stage], pipe.phase, abort_flag)) {
+                    if (!ready && !mbar_wait_slow_u32(full0 + 8 * pipe.stage, pipe.phase, abort_flag)) {
                         if (!*abort_flag) report_timeout(p.status, 73, item);
                         *abort_flag = 1;
-                        goto out;
+                        ok = false;
+                        break;
                     }
                     tc_fence_after();
-                    const uint32_t a = smem + pipe.stage * p.stage_bytes, b = a + 2 * NS_BOX;
+                    const uint32_t a = smem + pipe.stage * p.stage_bytes, b = a + D * NS_CHUNK, empty = empty0 + 8 * pipe.stage;
+                    const uint32_t ad = sdesc_lo(a), bd = PHASE == NS_X ? (((b & 0x3FFFFu) >> 4) | ((D * 512u) << 16)) : sdesc_lo(b);
+                    pipe.next_stage(p.stages);
+                    ready = mbar_test_u32(full0 + 8 * pipe.stage, pipe.phase);
 #pragma unroll
-                    for (int ks = 0; ks < 4; ++ks) {
-                        const uint32_t bd = PHASE == NS_X ? (((b & 0x3FFFFu) >> 4) | ((NS_BOX >> 4) << 16)) + ks * 128 : sdesc_lo(b) + ks * 2;
-                        umma_bf16_lo<false>(acc, sdesc_lo(a) + ks * 2, bd, idesc, accumulate, 1u);
+                    for (int ks = 0; ks < 4 * D; ++ks) {
+                        umma_bf16_lo<PAIR>(acc, ad + (ks >> 2) * 1024 + (ks & 3) * 2, bd + (PHASE == NS_X ? ks * 128 : (ks >> 2) * b_chunk + (ks & 3) * 2), idesc, accumulate, 1u);
                         accumulate = 1;
                     }
-                    umma_commit(&sh.empty[pipe.stage]);
-                    pipe.next_stage(p.stages);
+                    umma_commit_u32<PAIR>(empty);
                 }
-                umma_commit(&sh.tfull[pipe.acc]);
+                umma_commit_u32<PAIR>(tfull0 + 8 * pipe.acc);
                 pipe.next_acc();
             }
         }
@@ -409,9 +436,9 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
         const size_t mat = (size_t)group * p.n * p.lda, xm = (size_t)group * p.n * p.ldx;
         float* dvec = p.d + (size_t)group * p.lda;
         float* rs = p.rs + (size_t)group * p.lda;
-        for (int item = rank; item < items; item += p.G) {
-            const NsItem it = ns_item<PHASE>(p, item);
-            const int row = it.i * 128 + q * 32 + lane;
+        for (int item = first; item < items; item += step) {
+            const NsItem it = ns_item<PHASE, PAIR>(p, item);
+            const int row = it.i * p.tr + side * 128 + q * 32 + lane;
             // Chunks of 16 columns, two at a time: columns half * 16 + 0 .. 15 and + 32 .. 47 of every 64.  What a chunk needs from memory is
             // requested a pair ahead, the first pair before the product is waited for.
             float factor = 0.f, dj_next = 0.f;
@@ -438,7 +465,7 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             request(0, 0);
             request(0, 1);
             request_d(0);
-            const bool ok = __all_sync(0xffffffffu, mbar_wait(&sh.tfull[pipe.acc], pipe.acc_phase, abort_flag));
+            const bool ok = __all_sync(0xffffffffu, mbar_wait_u32(tfull0 + 8 * pipe.acc, pipe.acc_phase, abort_flag));
             if (!ok) {
                 if (!*abort_flag) report_timeout(p.status, 74, item);
                 *abort_flag = 1;
@@ -492,7 +519,11 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.tempty[pipe.acc]);
+            if (PAIR) {
+                if (lane == 0) mbar_arrive_leader(&sh.tempty[pipe.acc]);
+            } else {
+                if (lane == 0) mbar_arrive(&sh.tempty[pipe.acc]);
+            }
             pipe.next_acc();
         }
     }
@@ -502,13 +533,12 @@ out:                                            // also after a wait that ran ou
 
 // All threads of the group's CTAs meet; what they wrote to global memory is visible to the others' loads, TMA included.
 __device__ __forceinline__ void ns_group_sync(const NsParams& p, NsShared& sh, int group, unsigned& epoch) {
-    asm volatile("fence.proxy.async;" ::: "memory");
+    asm volatile("fence.proxy.async;" ::: "memory");     // this thread's stores, before the other proxy's loads that follow the barrier
     if (p.G == 1) {
         __syncthreads();
     } else if (p.cluster) {
         cluster_sync_all();
     } else {
-        __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) {
             unsigned* c = p.arrived + group;
@@ -527,9 +557,7 @@ __device__ __forceinline__ void ns_group_sync(const NsParams& p, NsShared& sh, i
             }
         }
         __syncthreads();
-        __threadfence();
     }
-    asm volatile("fence.proxy.async;" ::: "memory");
 }
 
 // 8 (or 1) values of X_0 from U
@@ -583,6 +611,8 @@ __device__ __forceinline__ void ns_convert(const NsParams& p, float* tile, int g
         for (int u = rank * (NS_THREADS / 32) + warp; u < units; u += p.G * (NS_THREADS / 32)) {
             const int r = u / segs, c0 = (u - r * segs) * 1024, c1 = min(in.cols, c0 + 1024);
             const size_t x = (size_t)r * p.ldx, o = base + (size_t)r * in.cols;
+            if (LOAD && c1 == in.cols)          // to a whole chunk of columns
+                for (int c = c1 + lane; c < p.ldx; c += 32) hi[x + c] = lo[x + c] = __float2half_rn(0.f);
             if (in.vec) {
 #pragma unroll 4
                 for (int c = c0 + lane * 8; c < c1; c += 256) {
@@ -671,6 +701,7 @@ __device__ __forceinline__ void ns_convert(const NsParams& p, float* tile, int g
     }
 }
 
+template <bool PAIR>
 __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsParams p) {
     extern __shared__ uint8_t ns_smem_raw[];
     __shared__ NsShared sh;
@@ -680,17 +711,30 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     const int group = blockIdx.x / p.G, rank = blockIdx.x - group * p.G;
     if (threadIdx.x == 0) {
         for (int i = 0; i < NS_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 8); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], PAIR ? 16 : 8); }
         sh.abort = 0;
         fence_barrier_init();
     }
-    if (warp == 1) { tmem_alloc(&sh.tmem_base, 512); tmem_relinquish(); }
+    if (warp == 1) {
+        if (PAIR) { tmem_alloc_pair(&sh.tmem_base, 512); tmem_relinquish_pair(); }
+        else { tmem_alloc(&sh.tmem_base, 512); tmem_relinquish(); }
+    }
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cluster_sync_all();               // both CTAs' barriers exist before any remote arrive
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
     NsPipe pipe;
     unsigned epoch = 0;
+    // the columns that pad A, E and F to whole chunks take part in the products: zero (X's are zeroed where it is loaded)
+    for (int i = rank * NS_THREADS + threadIdx.x; i < p.n * (p.lda - p.n); i += p.G * NS_THREADS) {
+        const int r = i / (p.lda - p.n);
+        const size_t at = ((size_t)group * p.n + r) * p.lda + p.n + (i - r * (p.lda - p.n));
+        p.E[at] = p.F[at] = __float2half_rn(0.f);
+        if (p.terms == 3) p.Elo[at] = p.Flo[at] = __float2half_rn(0.f);
+        p.A[at] = 0.f;
+        if (r == 0) p.d[(size_t)group * p.lda + p.n + i] = 0.f;
+    }
     const size_t per = (size_t)p.in.rows * p.in.cols;
 
     for (int b = group; b < p.batch; b += p.groups) {
@@ -715,7 +759,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
         ns_group_sync(p, sh, group, epoch);
         int src = 0;
         for (int k = 0; k < p.steps; ++k, src ^= 1) {
-            ns_product<NS_A>(p, maps, sh, smem, tmem, pipe, group, rank, src, nullptr);
+            ns_product<NS_A, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, nullptr);
             ns_group_sync(p, sh, group, epoch);
             if (p.splits > 1) {
                 // the ranges' parts of A in order: a warp takes 32 rows x 8 columns
@@ -723,7 +767,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
                 for (int u = rank * (NS_THREADS / 32) + warp; u < units; u += p.G * (NS_THREADS / 32)) {
                     const int t = u / (nt / 2), rem = u - t * (nt / 2);
                     int i, j;
-                    ns_tri_tile(t, p.n, nt, i, j);
+                    ns_tri_tile(t, p.n, 128, nt, i, j);
                     const int row = i * 128 + (rem & 3) * 32 + lane, c = (rem >> 2) * 8;
                     const float* in = p.part + ((size_t)group * p.splits * p.tiles_a + t) * nt * 128 + (size_t)c * 128 + (rem & 3) * 32 + lane;
                     alignas(32) float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -736,9 +780,9 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
                 }
                 ns_group_sync(p, sh, group, epoch);
             }
-            ns_product<NS_S>(p, maps, sh, smem, tmem, pipe, group, rank, src, p.coef + 3 * k);
+            ns_product<NS_S, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, p.coef + 3 * k);
             ns_group_sync(p, sh, group, epoch);
-            ns_product<NS_X>(p, maps, sh, smem, tmem, pipe, group, rank, src, nullptr);
+            ns_product<NS_X, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, nullptr);
             ns_group_sync(p, sh, group, epoch);
         }
         ns_convert<false>(p, tile, group, rank, base, src, 0.f);
@@ -750,15 +794,20 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) tmem_dealloc(tmem, 512);
+    if (PAIR) cluster_sync_all();               // neither CTA leaves while the other may still signal it
+    if (warp == 1) {
+        if (PAIR) tmem_dealloc_pair(tmem, 512);
+        else tmem_dealloc(tmem, 512);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ host side
 static bool ns_attributes() {
     static PerDeviceFlag attr_set;
     if (attr_set.get()) return true;
-    if (cudaFuncSetAttribute(ns_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM + 1024) != cudaSuccess ||
-        cudaFuncSetAttribute(ns_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+    if (cudaFuncSetAttribute(ns_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM + 1024) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM + 1024) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
         (void)cudaGetLastError();
         return false;
     }
@@ -772,9 +821,9 @@ struct NsPlan {
     int norm_blocks;
 };
 
-static int ns_tri_tiles(int n, int nt) {
+static int ns_tri_tiles(int n, int tr, int nt) {
     int t = 0;
-    for (int i = 0; i < (n + 127) / 128; ++i) t += ns_tri_row(i, n, nt);
+    for (int i = 0; i < (n + tr - 1) / tr; ++i) t += ns_tri_row(i, n, tr, nt);
     return t;
 }
 
@@ -791,7 +840,7 @@ static int ns_max_cluster() {
         attr[0].val.clusterDim.x = c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         cfg.gridDim = dim3(c); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM + 1024; cfg.attrs = attr; cfg.numAttrs = 1;
         int n = 0;
-        if (ns_attributes() && cudaOccupancyMaxActiveClusters(&n, ns_kernel, &cfg) == cudaSuccess && n > 0) break;
+        if (ns_attributes() && cudaOccupancyMaxActiveClusters(&n, ns_kernel<false>, &cfg) == cudaSuccess && n > 0) break;
         (void)cudaGetLastError();
     }
     slot.store(c, std::memory_order_relaxed);
@@ -822,21 +871,35 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     }
     p.G = g;
     p.groups = std::min(batch1, std::max(1, sms / g));
-    // the widest tiles that still give every CTA of the group one
-    p.nt_x = tiles_x(256) >= g ? 256 : tiles_x(128) >= g ? 128 : 64;
-    p.tiles_x = tiles_x(p.nt_x);
-    const int kb = (p.m + 63) / 64;
-    auto all = [&](int nt) { return ni * ((p.n + nt - 1) / nt); };
-    // E E: all tiles of 64 columns where the group has a CTA for each (no mirrored stores); otherwise the lower triangle
-    p.full_s = all(64) <= g;
-    p.nt_s = p.full_s ? 64 : ns_tri_tiles(p.n, 256) >= g ? 256 : 128;
-    p.tiles_s = p.full_s ? all(64) : ns_tri_tiles(p.n, p.nt_s);
-    // A: likewise where the long axis is short; a long one is split over the CTAs, whose parts meet after another barrier
-    p.full_a = all(64) <= g && kb <= tunable("DR_NS_FULL_KB", 48);
-    p.nt_a = p.full_a ? 64 : ns_tri_tiles(p.n, 256) >= g ? 256 : 128;
-    p.tiles_a = p.full_a ? all(64) : ns_tri_tiles(p.n, p.nt_a);
-    p.splits = p.full_a ? 1 : std::max(1, std::min(g / p.tiles_a, kb / 4));
-    p.stage_bytes = (2 + std::max(p.nt_x, std::max(p.nt_s, p.nt_a)) / 64) * NS_BOX;
+    const int kb = (p.m + 127) / 128, kn = (p.n + 127) / 128;       // stages of 128 along either axis
+    p.pair = g == sms && sms % 2 == 0 && p.n >= tunable("DR_NS_PAIR", 1024);
+    p.tr = p.pair ? 256 : 128;
+    if (p.pair) {
+        p.nt_x = p.nt_s = p.nt_a = 256;
+        p.tiles_x = ((p.n + 255) / 256) * ((p.m + 255) / 256);
+        p.tiles_s = p.tiles_a = ns_tri_tiles(p.n, 256, 256);
+        p.splits = 1;
+    } else {
+        // Cycles of a phase: rounds of tiles over the group's CTAs, each of `k` stages at the issuing thread's pace (as slow for 64
+        // columns as for 128) and a tile's fill and drain.
+        auto cost = [&](int tiles, int k, int nt) { return (long long)((tiles + g - 1) / g) * (k * 850 + (nt == 64 ? 3000 : 4500)); };
+        auto all = [&](int nt) { return ni * ((p.n + nt - 1) / nt); };
+        const int tri = ns_tri_tiles(p.n, 128, 128);
+        p.nt_x = cost(tiles_x(64), kn, 64) < cost(tiles_x(128), kn, 128) ? 64 : 128;
+        p.tiles_x = tiles_x(p.nt_x);
+        // E E: all tiles where the group has a CTA for each (no mirrored stores), otherwise the lower triangle
+        p.full_s = all(128) <= g;
+        p.nt_s = all(64) <= g ? 64 : 128;
+        p.tiles_s = p.full_s ? all(p.nt_s) : tri;
+        // A: likewise; or the lower triangle with the long axis split over the CTAs, whose parts meet after another barrier
+        const int s = std::max(1, std::min(g / tri, kb / 2));
+        const long long split = cost(tri * s, (kb + s - 1) / s, 128) + (s > 1 ? tunable("DR_NS_SPLITCOST", 11000) : 0), full64 = cost(all(64), kb, 64), full128 = cost(all(128), kb, 128);
+        p.full_a = std::min(full64, full128) <= split;
+        p.nt_a = p.full_a && full64 <= full128 ? 64 : 128;
+        p.tiles_a = p.full_a ? all(p.nt_a) : tri;
+        p.splits = p.full_a ? 1 : s;
+    }
+    p.stage_bytes = p.pair ? 2 * NS_CHUNK : 2 * NS_CHUNK + std::max(p.nt_x, std::max(p.nt_s, p.nt_a)) * 256;
     p.stages = std::min(NS_STAGES, NS_SMEM / p.stage_bytes);
     l.norm_blocks = (int)std::min<size_t>(NS_NORM_BLOCKS, ((size_t)rows * cols + 2047) / 2048);
     p.n_norm = p.cluster || g == 1 ? g : l.norm_blocks;
@@ -853,11 +916,11 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     return l;
 }
 
-static int ns_map(CUtensorMap* map, const void* ptr, int cols, int rows, int ld, int groups) {
-    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)groups};
-    const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)rows * ld * 2};
-    const cuuint32_t box[3] = {64, 64, 1};
-    return tmap_tiled(map, 3, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+static int ns_map(CUtensorMap* map, const void* ptr, int rows, int ld, int groups, int box_rows, int box_chunks) {
+    const cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)(ld / 64), (cuuint64_t)groups};
+    const cuuint64_t strides[3] = {(cuuint64_t)ld * 2, 128, (cuuint64_t)rows * ld * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_chunks, 1};
+    return tmap_tiled(map, 4, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 static int ns_check(int batch, int rows, int cols, int steps, const float* coef, float eps) {
@@ -883,15 +946,31 @@ static int ns_run(NsPlan& l, const NsInput& in, int steps, const float* coef, ch
     p.norm = (double*)(ws + l.norm); p.arrived = (unsigned*)(ws + l.arrived);
     p.status = dev_status_ptr();
     alignas(64) NsMaps maps;
-    int st = ns_map(&maps.hi[0], p.hi[0], p.m, p.n, p.ldx, p.groups);
-    if (st == DR_OK) st = ns_map(&maps.hi[1], p.hi[1], p.m, p.n, p.ldx, p.groups);
-    if (st == DR_OK) st = ns_map(&maps.lo, p.lo, p.m, p.n, p.ldx, p.groups);
-    if (st == DR_OK) st = ns_map(&maps.E, p.E, p.n, p.n, p.lda, p.groups);
-    if (st == DR_OK) st = ns_map(&maps.F, p.F, p.n, p.n, p.lda, p.groups);
-    if (st == DR_OK) st = p.terms == 3 ? ns_map(&maps.Elo, p.Elo, p.n, p.n, p.lda, p.groups) : DR_OK;
-    if (st == DR_OK) st = p.terms == 3 ? ns_map(&maps.Flo, p.Flo, p.n, p.n, p.lda, p.groups) : DR_OK;
+    int st = DR_OK;
+    auto put = [&](CUtensorMap& m, const void* ptr, int ld, int box_rows, int box_chunks) {
+        if (st == DR_OK) st = ns_map(&m, ptr, p.n, ld, p.groups, box_rows, box_chunks);
+    };
+    auto same = [](CUtensorMap& m, const CUtensorMap& o) { std::memcpy(&m, &o, sizeof(m)); };
+    const bool lows = p.terms == 3;
+    for (int k = 0; k < 2; ++k) {
+        put(maps.hi[k], p.hi[k], p.ldx, 128, ns_depth(p.pair));
+        if (p.nt_a == 64) put(maps.ba_hi[k], p.hi[k], p.ldx, 64, 2); else same(maps.ba_hi[k], maps.hi[k]);
+        if (p.nt_x == 64) put(maps.bx_hi[k], p.hi[k], p.ldx, 128, 1); else if (p.pair) put(maps.bx_hi[k], p.hi[k], p.ldx, 64, 2); else same(maps.bx_hi[k], maps.hi[k]);
+    }
+    put(maps.E, p.E, p.lda, 128, ns_depth(p.pair));
+    put(maps.F, p.F, p.lda, 128, ns_depth(p.pair));
+    if (p.nt_s == 64) put(maps.bs_hi, p.E, p.lda, 64, 2); else same(maps.bs_hi, maps.E);
+    if (lows) {
+        put(maps.lo, p.lo, p.ldx, 128, 2);
+        put(maps.Elo, p.Elo, p.lda, 128, 2);
+        put(maps.Flo, p.Flo, p.lda, 128, 2);
+        if (p.nt_a == 64) put(maps.ba_lo, p.lo, p.ldx, 64, 2); else same(maps.ba_lo, maps.lo);
+        if (p.nt_x == 64) put(maps.bx_lo, p.lo, p.ldx, 128, 1); else same(maps.bx_lo, maps.lo);
+        if (p.nt_s == 64) put(maps.bs_lo, p.Elo, p.lda, 64, 2); else same(maps.bs_lo, maps.Elo);
+    } else {                                    // not read
+        for (CUtensorMap* m : {&maps.lo, &maps.Elo, &maps.Flo, &maps.ba_lo, &maps.bx_lo, &maps.bs_lo}) same(*m, maps.E);
+    }
     if (st != DR_OK) return st;
-    if (p.terms == 1) maps.Elo = maps.E, maps.Flo = maps.F;
     if (!ns_attributes()) return DR_ERR_CUDA;
     const bool counted = !(p.cluster || p.G == 1);
     if (counted) {
@@ -901,19 +980,21 @@ static int ns_run(NsPlan& l, const NsInput& in, int steps, const float* coef, ch
         if (st != DR_OK) return st;
     }
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     cfg.gridDim = dim3((unsigned)(p.groups * p.G)); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM + 1024; cfg.stream = s;
     cfg.attrs = attr;
     if (counted) {
         attr[0].id = cudaLaunchAttributeCooperative;
         attr[0].val.cooperative = 1;
-        cfg.numAttrs = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = p.pair ? 2 : 1;
     } else if (p.cluster) {
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim.x = p.G; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         cfg.numAttrs = 1;
     }
-    if (cudaLaunchKernelEx(&cfg, ns_kernel, maps, p) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+    if ((p.pair ? cudaLaunchKernelEx(&cfg, ns_kernel<true>, maps, p) : cudaLaunchKernelEx(&cfg, ns_kernel<false>, maps, p)) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
     count_launch();
     return launch_status();
 }
