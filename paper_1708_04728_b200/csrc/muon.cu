@@ -21,36 +21,19 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <cuda_fp16.h>
 
-#include "conv_common.cuh"
-#include "umma_ptx.cuh"
+#include "muon_common.cuh"
 
 namespace dr {
-using namespace ptx;
 
 constexpr int NS_THREADS = 320;             // warp 0: TMA, warp 1: MMA, warps 2 - 9: drain
 constexpr int NS_STAGES = 8;                // at most
-constexpr int NS_SMEM = 196608;             // operand ring
+constexpr int NS_SMEM = 196608;             // operand ring; also keeps every SM to one CTA, which owns all its tensor memory
 constexpr int NS_CHUNK = 128 * 128;          // 128 rows x 64 float16
 // 64-column chunks a stage is deep in the contraction: 2, since the issuing threads take 400 cycles to hand a stage over; 1 where two
 // CTAs share tiles of 256 x 256, whose MMAs take longer than that and want more stages of the same bytes (1.24 against 1.35 ms at 4096 x 4096)
 __host__ __device__ constexpr int ns_depth(bool pair) { return pair ? 1 : 2; }
-constexpr float NS_SCALE = 4096.f;          // X is stored times this: entries of every size stay in float16's normal range
 constexpr int NS_NORM_BLOCKS = 256;         // partial sums of squares at most
-
-struct NsInput {
-    int rows, cols, tall;
-    const void* g;              // gradient (bfloat16 or float32), or the optimiser's float32 gradient
-    int g_f32;
-    float *v, *w;               // optimiser state, nullptr for the product alone
-    float momentum;
-    int nesterov;
-    float eps;
-    float lr_scale, keep;       // w <- keep w - lr_scale O
-    __nv_bfloat16* out;         // O, or the bfloat16 copy of w (may be nullptr then)
-    int vec;                    // rows of a multiple of 8 elements at 16-byte aligned addresses: 16-byte accesses
-};
 
 struct NsParams {
     NsInput in;
@@ -81,111 +64,7 @@ struct NsShared {
     double red[10];
 };
 
-__device__ __forceinline__ bool elect_one() {
-    uint32_t e;
-    asm volatile("{\n.reg .pred P;\nelect.sync _|P, 0xffffffff;\nselp.u32 %0, 1, 0, P;\n}" : "=r"(e));
-    return e != 0;
-}
-
-struct __align__(32) Half16 { uint32_t u[8]; };
-struct __align__(32) Float8 { float f[8]; };
-__device__ __forceinline__ Half16 ld16h(const __half* p) {
-    Half16 v;
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(v.u[0]), "=r"(v.u[1]), "=r"(v.u[2]), "=r"(v.u[3]), "=r"(v.u[4]), "=r"(v.u[5]), "=r"(v.u[6]), "=r"(v.u[7]) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ void st16h(__half* p, const Half16& v) {
-    asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(v.u[0]), "r"(v.u[1]), "r"(v.u[2]), "r"(v.u[3]), "r"(v.u[4]), "r"(v.u[5]), "r"(v.u[6]), "r"(v.u[7]), "l"(p) : "memory");
-}
-__device__ __forceinline__ void ld8f(const float* p, float* f) {
-    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]) : "l"(p) : "memory");
-}
-__device__ __forceinline__ void st8f(float* p, const float* f) {
-    asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]), "l"(p) : "memory");
-}
-__device__ __forceinline__ float2 half2_at(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
-__device__ __forceinline__ uint32_t pack_half(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // ------------------------------------------------------------------------------------------------ input and output
-// CN consecutive values of U: from the gradient, or from the updated momentum and, with Nesterov, the gradient
-template <int CN, typename T> __device__ __forceinline__ void ns_read(const T* p, float* f);
-template <> __device__ __forceinline__ void ns_read<1, float>(const float* p, float* f) { f[0] = *p; }
-template <> __device__ __forceinline__ void ns_read<1, __nv_bfloat16>(const __nv_bfloat16* p, float* f) { f[0] = __bfloat162float(*p); }
-template <> __device__ __forceinline__ void ns_read<8, float>(const float* p, float* f) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-template <> __device__ __forceinline__ void ns_read<8, __nv_bfloat16>(const __nv_bfloat16* p, float* f) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    f[0] = bf16_lo(a.x); f[1] = bf16_hi(a.x); f[2] = bf16_lo(a.y); f[3] = bf16_hi(a.y);
-    f[4] = bf16_lo(a.z); f[5] = bf16_hi(a.z); f[6] = bf16_lo(a.w); f[7] = bf16_hi(a.w);
-}
-template <int CN> __device__ __forceinline__ void ns_write(float* p, const float* f) {
-    if (CN == 8) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1 % CN], f[2 % CN], f[3 % CN]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(f[4 % CN], f[5 % CN], f[6 % CN], f[7 % CN]);
-    } else {
-        *p = f[0];
-    }
-}
-template <int CN> __device__ __forceinline__ void ns_write(__nv_bfloat16* p, const float* f) {
-    if (CN == 8) *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1 % CN]), pack_bf16(f[2 % CN], f[3 % CN]), pack_bf16(f[4 % CN], f[5 % CN]), pack_bf16(f[6 % CN], f[7 % CN]));
-    else *p = __float2bfloat16_rn(f[0]);
-}
-template <int CN>
-__device__ __forceinline__ void ns_value(const NsInput& in, size_t i, float* u) {
-    if (in.v) {
-        ns_read<CN>(in.v + i, u);
-        if (in.nesterov) {
-            float g[CN];
-            ns_read<CN>((const float*)in.g + i, g);
-#pragma unroll
-            for (int c = 0; c < CN; ++c) u[c] = fmaf(in.momentum, u[c], g[c]);
-        }
-    } else if (in.g_f32) {
-        ns_read<CN>((const float*)in.g + i, u);
-    } else {
-        ns_read<CN>((const __nv_bfloat16*)in.g + i, u);
-    }
-}
-
-// v <- momentum v + g and this thread's part of the sum of squares of U (in float64: no size of U overflows or vanishes)
-template <int CN>
-__device__ __forceinline__ double ns_momentum_part(const NsInput& in, size_t base, size_t count, size_t first, size_t stride) {
-    double s = 0.;
-    for (size_t i = first; i < count; i += stride) {
-        float u[CN], g[CN];
-        if (in.v) {
-            ns_read<CN>(in.v + base + i * CN, u);
-            ns_read<CN>((const float*)in.g + base + i * CN, g);
-#pragma unroll
-            for (int c = 0; c < CN; ++c) u[c] = fmaf(in.momentum, u[c], g[c]);
-            ns_write<CN>(in.v + base + i * CN, u);
-            if (in.nesterov) {
-#pragma unroll
-                for (int c = 0; c < CN; ++c) u[c] = fmaf(in.momentum, u[c], g[c]);
-            }
-        } else {
-            ns_value<CN>(in, base + i * CN, u);
-        }
-#pragma unroll
-        for (int c = 0; c < CN; ++c) s = fma((double)u[c], (double)u[c], s);
-    }
-    return s;
-}
-__device__ __forceinline__ double ns_momentum(const NsInput& in, size_t base, size_t per, size_t first, size_t stride) {
-    return in.vec ? ns_momentum_part<8>(in, base, per / 8, first, stride) : ns_momentum_part<1>(in, base, per, first, stride);
-}
-
-__device__ __forceinline__ double ns_warp_sum(double s) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    return s;
-}
-
 __global__ void __launch_bounds__(256) ns_begin_kernel(const NsInput in, double* norm, unsigned* arrived, int groups) {
     __shared__ double red[8];
     const size_t per = (size_t)in.rows * in.cols;
@@ -246,16 +125,6 @@ __device__ __forceinline__ void ns_mirror(__half* p, int ld, int i, int c0, cons
 #pragma unroll
     for (int c = 0; c < CN; ++c)
         if (c < count) p[(size_t)(c0 + c) * ld + i] = __ushort_as_half((unsigned short)(h[c / 2] >> (16 * (c & 1))));
-}
-// v as float16 h and what that leaves out as float16 l
-template <int CN>
-__device__ __forceinline__ void ns_split(const float* v, uint32_t* h, uint32_t* l) {
-#pragma unroll
-    for (int c = 0; c < CN; c += 2) {
-        h[c / 2] = pack_half(v[c], v[c + 1]);
-        const float2 f = half2_at(h[c / 2]);
-        l[c / 2] = pack_half(v[c] - f.x, v[c + 1] - f.y);
-    }
 }
 template <int CN>
 __device__ __forceinline__ void ns_row_store(__half* p, const uint32_t* h, int count) {
@@ -574,18 +443,6 @@ __device__ __forceinline__ void ns_put_x(__half* hi, __half* lo, float inv, floa
         *hi = __float2half_rn(u[0]);
         *lo = __float2half_rn(u[0] - __half2float(*hi));
     }
-}
-// 8 (or 1) values of the result: O, or the update of w
-template <int CN>
-__device__ __forceinline__ void ns_put_o(const NsInput& in, size_t at, float* o) {
-    if (in.w) {
-        float w[CN];
-        ns_read<CN>(in.w + at, w);
-#pragma unroll
-        for (int c = 0; c < CN; ++c) o[c] = fmaf(-in.lr_scale, o[c], in.keep * w[c]);
-        ns_write<CN>(in.w + at, o);
-    }
-    if (in.out) ns_write<CN>(in.out + at, o);
 }
 __device__ __forceinline__ void ns_get_x8(const __half* hi, const __half* lo, float* x) {
     const uint4 h = *reinterpret_cast<const uint4*>(hi), l = *reinterpret_cast<const uint4*>(lo);
@@ -920,7 +777,7 @@ static int ns_map(CUtensorMap* map, const void* ptr, int rows, int ld, int group
     const cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)(ld / 64), (cuuint64_t)groups};
     const cuuint64_t strides[3] = {(cuuint64_t)ld * 2, 128, (cuuint64_t)rows * ld * 2};
     const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_chunks, 1};
-    return tmap_tiled(map, 4, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
+    return tmap_tiled(map, 4, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 static int ns_check(int batch, int rows, int cols, int steps, const float* coef, float eps) {
@@ -932,14 +789,24 @@ static int ns_check(int batch, int rows, int cols, int steps, const float* coef,
     return DR_OK;
 }
 
-static int ns_run(NsPlan& l, const NsInput& in, int steps, const float* coef, char* ws, cudaStream_t s) {
+static int ns_run(int batch, NsInput in, int steps, const float* coef, char* ws, size_t ws_bytes, cudaStream_t s) {
+    in.tall = in.rows > in.cols;
+    in.vec = (in.cols & 7) == 0 && aligned16(in.g) && aligned16(in.v) && aligned16(in.w) && aligned16(in.out);
+    float own[3 * DR_NS_MAX_STEPS];
+    const float usual[3] = {3.4445f, -4.7750f, 2.0315f};
+    for (int i = 0; i < 3 * steps; ++i) own[i] = coef ? coef[i] : usual[i % 3];
+    const NsSmallPlan small = ns_small_plan(batch, in.rows, in.cols);
+    if (small.ctas) {
+        if (ws_bytes < small.bytes) return DR_ERR_WORKSPACE;
+        return batch == 0 ? DR_OK : ns_small_run(small, batch, in, steps, own, ws, s);
+    }
+    NsPlan l = ns_plan(batch, in.rows, in.cols);
+    if (ws_bytes < l.total) return DR_ERR_WORKSPACE;
+    if (batch == 0) return DR_OK;
     NsParams& p = l.p;
     p.in = in;
-    p.in.tall = p.in.rows > p.in.cols;
     p.steps = steps;
-    p.in.vec = (p.in.cols & 7) == 0 && aligned16(in.g) && aligned16(in.v) && aligned16(in.w) && aligned16(in.out);
-    const float usual[3] = {3.4445f, -4.7750f, 2.0315f};
-    for (int i = 0; i < 3 * steps; ++i) p.coef[i] = coef ? coef[i] : usual[i % 3];
+    for (int i = 0; i < 3 * steps; ++i) p.coef[i] = own[i];
     p.hi[0] = (__half*)(ws + l.hi0); p.hi[1] = (__half*)(ws + l.hi1); p.lo = (__half*)(ws + l.lo);
     p.E = (__half*)(ws + l.E); p.F = (__half*)(ws + l.F); p.Elo = (__half*)(ws + l.Elo); p.Flo = (__half*)(ws + l.Flo);
     p.A = (float*)(ws + l.A); p.d = (float*)(ws + l.d); p.rs = (float*)(ws + l.rs); p.part = (float*)(ws + l.part);
@@ -1007,7 +874,8 @@ extern "C" int dr_orthogonalise_workspace_bytes(int batch, int rows, int cols, s
     if (!bytes) return DR_ERR_INVALID_ARG;
     const int st = ns_check(batch, rows, cols, 1, nullptr, 0.f);
     if (st != DR_OK) return st;
-    *bytes = ns_plan(batch, rows, cols).total;
+    const NsSmallPlan small = ns_small_plan(batch, rows, cols);
+    *bytes = small.ctas ? small.bytes : ns_plan(batch, rows, cols).total;
     return DR_OK;
 }
 
@@ -1018,12 +886,9 @@ extern "C" int dr_orthogonalise(int batch, int rows, int cols, const void* g, in
     if (!g || !o || !workspace || (flags & ~(unsigned)DR_NS_G_F32)) return DR_ERR_INVALID_ARG;
     const bool f32 = flags & DR_NS_G_F32;
     if (((uintptr_t)g & (f32 ? 3u : 1u)) || ((uintptr_t)o & 1u) || ((uintptr_t)workspace & 255)) return DR_ERR_ALIGNMENT;
-    NsPlan l = ns_plan(batch, rows, cols);
-    if (workspace_bytes < l.total) return DR_ERR_WORKSPACE;
-    if (batch == 0) return DR_OK;
     NsInput in = {};
     in.rows = rows; in.cols = cols; in.g = g; in.g_f32 = f32; in.eps = eps; in.out = (__nv_bfloat16*)o;
-    return ns_run(l, in, steps, coef, (char*)workspace, (cudaStream_t)stream);
+    return ns_run(batch, in, steps, coef, (char*)workspace, workspace_bytes, (cudaStream_t)stream);
 }
 
 extern "C" int dr_muon_update(int batch, int rows, int cols, float* w, float* v, const float* g, float lr, float momentum, float decay, int nesterov,
@@ -1032,13 +897,10 @@ extern "C" int dr_muon_update(int batch, int rows, int cols, float* w, float* v,
     if (st != DR_OK) return st;
     if (!w || !v || !g || !workspace) return DR_ERR_INVALID_ARG;
     if (((uintptr_t)w & 3u) || ((uintptr_t)v & 3u) || ((uintptr_t)g & 3u) || ((uintptr_t)w_bf16 & 1u) || ((uintptr_t)workspace & 255)) return DR_ERR_ALIGNMENT;
-    NsPlan l = ns_plan(batch, rows, cols);
-    if (workspace_bytes < l.total) return DR_ERR_WORKSPACE;
-    if (batch == 0) return DR_OK;
     NsInput in = {};
     in.rows = rows; in.cols = cols; in.g = g; in.g_f32 = 1; in.eps = eps; in.v = v; in.w = w; in.momentum = momentum; in.nesterov = nesterov != 0;
     in.lr_scale = lr * (rows > cols ? sqrtf((float)rows / (float)cols) : 1.f);
     in.keep = 1.f - lr * decay;
     in.out = (__nv_bfloat16*)w_bf16;
-    return ns_run(l, in, steps, coef, (char*)workspace, (cudaStream_t)stream);
+    return ns_run(batch, in, steps, coef, (char*)workspace, workspace_bytes, (cudaStream_t)stream);
 }
