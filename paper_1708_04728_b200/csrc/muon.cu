@@ -153,13 +153,14 @@ __device__ __forceinline__ void ns_emit_a(const NsParams& p, size_t mat, float* 
         for (int c = 0; c < CN; ++c)
             if (c < last) A[(size_t)i * p.lda + c0 + c] = v[c];
     }
-    if (i >= c0 && i < c0 + CN) {
+    if (c0 < (i | 31) + 1 && c0 + CN > (i & ~31)) {      // one of the warp's 32 rows meets its diagonal here: selects, and one store
+        float d = 0.f;
 #pragma unroll
-        for (int c = 0; c < CN; ++c)
-            if (c0 + c == i) {
-                dvec[i] = v[c];
-                v[c] = 0.f;
-            }
+        for (int c = 0; c < CN; ++c) {
+            d = c0 + c == i ? v[c] : d;
+            v[c] = c0 + c == i ? 0.f : v[c];
+        }
+        if (i >= c0 && i < c0 + CN) dvec[i] = d;
     }
     uint32_t h[CN / 2], l[CN / 2];
     ns_split<CN>(v, h, l);
@@ -182,12 +183,13 @@ template <int CN>
 __device__ __forceinline__ void ns_emit_f(const NsParams& p, size_t mat, float* rs, const float* coef, bool full, int i, int c0, float di, const float* dj, const float* e, float* v) {
     if (!full && c0 > i) return;
     const float a = coef[0], b = coef[1], cc = coef[2];
+    float sq = 0.f;
 #pragma unroll
     for (int c = 0; c < CN; ++c) {
-        const float f = fmaf(b, e[c], cc * fmaf(di + dj[c], e[c], v[c]));
-        if (c0 + c == i) rs[i] = a + fmaf(b, di, cc * fmaf(di, di, v[c]));
-        v[c] = c0 + c == i ? 0.f : f;
+        sq = c0 + c == i ? v[c] : sq;
+        v[c] = c0 + c == i ? 0.f : fmaf(b, e[c], cc * fmaf(di + dj[c], e[c], v[c]));
     }
+    if (i >= c0 && i < c0 + CN) rs[i] = a + fmaf(b, di, cc * fmaf(di, di, sq));
     uint32_t h[CN / 2], l[CN / 2];
     ns_split<CN>(v, h, l);
     const int last = full ? CN : min(CN, i - c0 + 1);

@@ -151,7 +151,7 @@ __device__ __forceinline__ void ns_put_o(const NsInput& in, size_t at, float* o)
     if (in.out) ns_write<CN>(in.out + at, o);
 }
 // The kernel for matrices of at most 128 rows that a cluster holds in shared memory (muon_small.cu); 0 CTAs: not for this shape.
-struct NsSmallPlan { int ctas, groups, chunks, terms; size_t bytes; };
+struct NsSmallPlan { int ctas, groups, chunks, terms; size_t part, sums, diag, bytes; };
 NsSmallPlan ns_small_plan(int batch, int rows, int cols);
 int ns_small_run(const NsSmallPlan& plan, int batch, const NsInput& in, int steps, const float* coef, void* workspace, cudaStream_t stream);
 

@@ -3,9 +3,11 @@
 // What bounds such a matrix is not its arithmetic but 15 dependent products, so nothing leaves the SM that does not have to.  A CTA
 // keeps a slab of X's columns in shared memory for all steps, as float16 pairs in the layout that serves both as rows of X (A = X X^T,
 // contraction along the slab) and as the second operand of F X.  Per step
-//   A    each CTA multiplies its slab by its own transpose; the parts are summed through global memory, every CTA the columns it
-//        owns, and E (A without its diagonal) and the diagonal go to all CTAs' shared memory: two cluster barriers,
-//   F    every CTA computes E E and the polynomial for itself: one 128 x 128 product is cheaper than another exchange,
+//   A    each CTA multiplies its slab by its own transpose and leaves its part in global memory (L2); after a cluster barrier it sums the
+//        columns it owns over all parts, in the CTAs' order, and after another one takes everyone's: 64 KB read twice at n = 128.
+//        (Every CTA summing all parts for itself saves a barrier but took 7.5 us of a step with 8 CTAs; sending the sums to the
+//        others' shared memory took longer than the round trip through L2.)
+//   F    every CTA computes E E (E: A without its diagonal) and the polynomial for itself,
 //   X    every CTA updates its slab in place.
 // Products and element-wise terms as in the kernel for larger matrices (muon.cu); with few rows rounding errors average less, so
 // matrices of up to 64 rows multiply hi hi + hi lo + lo hi: the tensor cores idle here either way.
@@ -17,12 +19,12 @@
 
 namespace dr {
 
-constexpr int NSS_THREADS = 256;
+constexpr int NSS_THREADS = 512;           // 16 warps: four share the 32 accumulator rows that each of them can read
 constexpr int NSS_CHUNK = 128 * 128;        // 64 columns of 128 rows
-constexpr int NSS_MAX_CHUNKS = 4;           // of a CTA's slab: 64 KB hi, 64 KB lo
-// Always asked for in full: one CTA per SM.  A second one there would wait for the first one's tensor memory, and the first, at a
-// cluster barrier, for the second.
-constexpr int NSS_SMEM = 2 * NSS_MAX_CHUNKS * NSS_CHUNK + 4 * NSS_CHUNK + 1024;
+// Shared memory, in chunks: X (hi, lo) as wide as the slab, E (hi, lo) as wide as n.  Always asked for in full: one CTA per SM.  A second one
+// there would wait for the first one's tensor memory, and the first, at a cluster barrier, for the second.
+constexpr int NSS_CHUNKS = 12;
+constexpr int NSS_SMEM = NSS_CHUNKS * NSS_CHUNK + 1024;
 static_assert(NSS_SMEM > 114 * 1024, "two CTAs must not fit an SM");
 
 struct NsSmall {
@@ -30,6 +32,8 @@ struct NsSmall {
     int batch, steps, n, m, G, groups, chunks, terms;
     float coef[3 * DR_NS_MAX_STEPS];
     float* part;                // [group][CTA][column][128 rows]: parts of A
+    uint4* sums;                // [group][row][8-column unit][hi, lo]: E
+    float* diag;                // [group][128]
     int* status;
 };
 
@@ -37,8 +41,9 @@ struct NsSmallShared {
     uint64_t done;
     uint32_t tmem_base;
     int abort;
-    double red[8], norm[16];
-    float d[128], rs[128];
+    double red[NSS_THREADS / 32], norm[16];
+    alignas(16) float d[128];
+    float rs[128];
 };
 
 // byte offset of 8 columns (one 16-byte unit) of a row inside [chunk][128 rows][128 bytes], 128-byte swizzle
@@ -50,30 +55,123 @@ __device__ __forceinline__ void nss_ld(const uint8_t* base, int row, int unit, u
 __device__ __forceinline__ void nss_st(uint8_t* base, int row, int unit, const uint32_t* u) {
     *reinterpret_cast<uint4*>(base + nss_at(row, unit)) = make_uint4(u[0], u[1], u[2], u[3]);
 }
-__device__ __forceinline__ void nss_st_remote(uint32_t addr, int cta, const uint32_t* u) {
-    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mapa_shared(addr, cta)), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
-}
 
-// 8 values of U at (row i, columns c .. c + 7) of X (zero past m); `at` is the first one's place in the user's matrix
-__device__ __forceinline__ void nss_value(const NsSmall& p, size_t base, int i, int c, float* u) {
-    const NsInput& in = p.in;
-    if (!in.tall && in.vec && c < p.m) {
-        ns_value<8>(in, base + (size_t)i * in.cols + c, u);
-        return;
+// A CTA's slab in the user's memory, 8 columns at a time (16-byte accesses) or, where rows are not aligned or U is tall, element by element:
+// a warp takes one of the user's rows after the other (tall: one of X's columns), so that no index needs a division.
+struct NssPlace { int i, c; size_t at; bool ok; };           // row and column in the slab, place in the user's matrix
+template <int CN>
+struct NssWalk {
+    int rows, len, r, x, per;
+    __device__ __forceinline__ NssWalk(const NsSmall& p) {
+        per = p.chunks * 64 / CN;
+        rows = CN == 1 ? (p.in.tall ? per : p.n) : 1;
+        len = CN == 1 ? (p.in.tall ? p.n : per) : p.n * per;
+        r = CN == 1 ? threadIdx.x >> 5 : 0;
+        x = CN == 1 ? threadIdx.x & 31 : threadIdx.x;
+        if (CN == 8 && x >= len) r = rows;
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        u[k] = 0.f;
-        if (c + k < p.m) ns_value<1>(in, base + (in.tall ? (size_t)(c + k) * in.cols + i : (size_t)i * in.cols + c + k), u + k);
+    static constexpr int U = CN == 1 ? 8 : 2, STEP = CN == 1 ? 32 : NSS_THREADS;        // places whose loads go out together
+    __device__ __forceinline__ bool more() const { return r < rows; }
+    __device__ __forceinline__ void next() {
+        x += U * STEP;
+        if (CN == 8) {
+            if (x >= len) r = rows;
+        } else if (x - (int)(threadIdx.x & 31) >= len) {
+            r += NSS_THREADS / 32;
+            x = threadIdx.x & 31;
+        }
     }
-}
-__device__ __forceinline__ double nss_momentum(const NsSmall& p, size_t base, int i, int c) {
+    __device__ __forceinline__ bool get(const NsSmall& p, int k, int c0, NssPlace& t) const {
+        const int y = x + k * STEP;
+        if (CN == 8) { t.i = y / per; t.c = (y - t.i * per) * CN; }
+        else { t.i = p.in.tall ? y : r; t.c = p.in.tall ? r : y; }
+        t.at = CN == 1 && p.in.tall ? (size_t)(c0 + t.c) * p.in.cols + t.i : (size_t)t.i * p.in.cols + c0 + t.c;
+        t.ok = y < len && c0 + t.c < p.m;
+        return y < len;
+    }
+};
+// v <- momentum v + g; U waits in the place of X, 16 bytes of a unit of 8 columns where its hi half goes and 16 where the lo half goes.
+// Returns this thread's part of the sum of squares, in float64: no size of U overflows or vanishes.
+template <int CN>
+__device__ __forceinline__ double nss_load(const NsSmall& p, uint8_t* X, int xlo, int c0, size_t base) {
+    constexpr int U = NssWalk<CN>::U;
     const NsInput& in = p.in;
-    if (!in.tall && in.vec && c < p.m) return ns_momentum_part<8>(in, base + (size_t)i * in.cols + c, 1, 0, 1);
     double s = 0.;
-    for (int k = 0; k < 8; ++k)
-        if (c + k < p.m) s += ns_momentum_part<1>(in, base + (in.tall ? (size_t)(c + k) * in.cols + i : (size_t)i * in.cols + c + k), 1, 0, 1);
+#pragma unroll 1
+    for (NssWalk<CN> walk(p); walk.more(); walk.next()) {
+        alignas(16) float f[U][CN], v[U][CN];
+        NssPlace t[U];
+        bool mine[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            mine[k] = walk.get(p, k, c0, t[k]);
+#pragma unroll
+            for (int e = 0; e < CN; ++e) f[k][e] = v[k][e] = 0.f;
+            if (!t[k].ok) continue;
+            if (in.g_f32) ns_read<CN>((const float*)in.g + base + t[k].at, f[k]);
+            else ns_read<CN>((const __nv_bfloat16*)in.g + base + t[k].at, f[k]);
+            if (in.v) ns_read<CN>(in.v + base + t[k].at, v[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (in.v) {
+#pragma unroll
+                for (int e = 0; e < CN; ++e) v[k][e] = fmaf(in.momentum, v[k][e], f[k][e]);
+                if (t[k].ok) ns_write<CN>(in.v + base + t[k].at, v[k]);
+#pragma unroll
+                for (int e = 0; e < CN; ++e) f[k][e] = in.nesterov ? fmaf(in.momentum, v[k][e], f[k][e]) : v[k][e];
+            }
+#pragma unroll
+            for (int e = 0; e < CN; ++e) s = fma((double)f[k][e], (double)f[k][e], s);
+            if (!mine[k]) continue;
+            uint8_t* to = X + nss_at(t[k].i, t[k].c >> 3);
+            if (CN == 8) {
+                *reinterpret_cast<float4*>(to) = make_float4(f[k][0], f[k][1 % CN], f[k][2 % CN], f[k][3 % CN]);
+                *reinterpret_cast<float4*>(to + xlo) = make_float4(f[k][4 % CN], f[k][5 % CN], f[k][6 % CN], f[k][7 % CN]);
+            } else {
+                *reinterpret_cast<float*>(to + (t[k].c & 4 ? xlo : 0) + (t[k].c & 3) * 4) = f[k][0];
+            }
+        }
+    }
     return s;
+}
+template <int CN>
+__device__ __forceinline__ void nss_store(const NsSmall& p, const uint8_t* X, int xlo, int c0, size_t base) {
+    constexpr int U = NssWalk<CN>::U;
+    const NsInput& in = p.in;
+#pragma unroll 1
+    for (NssWalk<CN> walk(p); walk.more(); walk.next()) {
+        float f[U][CN], w[U][CN];
+        NssPlace t[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            walk.get(p, k, c0, t[k]);
+            if (!t[k].ok) continue;
+            if (in.w) ns_read<CN>(in.w + base + t[k].at, w[k]);
+            const uint8_t* from = X + nss_at(t[k].i, t[k].c >> 3) + (CN == 1 ? (t[k].c & 7) * 2 : 0);
+            if (CN == 8) {
+                const uint4 h = *reinterpret_cast<const uint4*>(from), l = *reinterpret_cast<const uint4*>(from + xlo);
+                const uint32_t hu[4] = {h.x, h.y, h.z, h.w}, lu[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+                for (int e = 0; e < CN; ++e) {
+                    const float2 fh = half2_at(hu[e / 2]), fl = half2_at(lu[e / 2]);
+                    f[k][e] = (e & 1 ? fh.y + fl.y : fh.x + fl.x) * (1.f / NS_SCALE);
+                }
+            } else {
+                f[k][0] = (__half2float(*reinterpret_cast<const __half*>(from)) + __half2float(*reinterpret_cast<const __half*>(from + xlo))) * (1.f / NS_SCALE);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (!t[k].ok) continue;
+            if (in.w) {
+#pragma unroll
+                for (int e = 0; e < CN; ++e) f[k][e] = fmaf(-in.lr_scale, f[k][e], in.keep * w[k][e]);
+                ns_write<CN>(in.w + base + t[k].at, f[k]);
+            }
+            if (in.out) ns_write<CN>(in.out + base + t[k].at, f[k]);
+        }
+    }
 }
 
 __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_constant__ NsSmall p) {
@@ -130,6 +228,7 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
     // D += P Q^T over `kchunks` chunks of 64, both operands with the contraction along their rows
     auto product = [&](uint32_t d, uint32_t pa, uint32_t qa, int kchunks, int N, uint32_t accumulate) {
         const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | (8u << 24);
+#pragma unroll 1
         for (int k = 0; k < kchunks; ++k, pa += NSS_CHUNK, qa += NSS_CHUNK)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
@@ -140,12 +239,8 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
 
     for (int b = group; b < p.batch; b += p.groups) {
         const size_t base = (size_t)b * p.n * p.m;
-        // v, and the sum of the squares of U: tall matrices are read along their rows, which are X's columns
-        double s = 0.;
-        for (int u = threadIdx.x; u < p.n * units; u += NSS_THREADS) {
-            const int i = p.in.tall ? u % p.n : u / units, c = (p.in.tall ? u / p.n : u % units) * 8 + c0;
-            if (c < p.m) s += nss_momentum(p, base, i, c);
-        }
+        const bool wide = p.in.vec && !p.in.tall;
+        double s = wide ? nss_load<8>(p, X, xlo, c0, base) : nss_load<1>(p, X, xlo, c0, base);
         s = ns_warp_sum(s);
         if (lane == 0) sh.red[warp] = s;
         __syncthreads();
@@ -159,13 +254,18 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
         s = 0.;
         for (int i = 0; i < p.G; ++i) s += sh.norm[i];
         const float inv = (float)((double)NS_SCALE / (sqrt(s) + (double)p.in.eps));
+#pragma unroll 1
         for (int u = threadIdx.x; u < p.n * units; u += NSS_THREADS) {
-            const int i = p.in.tall ? u % p.n : u / units, w = p.in.tall ? u / p.n : u % units;
-            alignas(8) float f[8];
+            const int i = u / units, w = u - i * units;
             uint32_t h[4], l[4];
-            nss_value(p, base, i, c0 + w * 8, f);
+            float f[8];
+            nss_ld(X, i, w, h);
+            nss_ld(X + xlo, i, w, l);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] *= inv;
+            for (int k = 0; k < 4; ++k) {
+                f[k] = __uint_as_float(h[k]) * inv;
+                f[4 + k] = __uint_as_float(l[k]) * inv;
+            }
             ns_split<8>(f, h, l);
             nss_st(X, i, w, h);
             nss_st(X + xlo, i, w, l);
@@ -173,169 +273,148 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
         for (int step = 0; step < p.steps; ++step) {
             const float ca = p.coef[3 * step], cb = p.coef[3 * step + 1], cc = p.coef[3 * step + 2];
             run([&]() {
-                product(acc_a, smem, smem, p.chunks, kc * 64, 0);
-                if (p.terms == 3) {
-                    product(acc_a, smem, smem + xlo, p.chunks, kc * 64, 1);
-                    product(acc_a, smem + xlo, smem, p.chunks, kc * 64, 1);
-                }
+#pragma unroll 1
+                for (int t = 0; t < p.terms; ++t) product(acc_a, smem + (t == 2 ? xlo : 0), smem + (t == 1 ? xlo : 0), p.chunks, kc * 64, t > 0);
             });
-            float* part = p.part + ((size_t)group * p.G + rank) * p.n * 128;
-            for (int c = half * 16; c < p.n; c += 32) {
-                uint32_t raw[16];
-                __syncwarp();
-                tmem_ld_x16(acc_a + c + ((uint32_t)(q * 32) << 16), raw);
-                tmem_ld_wait();
-                float v[16];
+            float* const part = p.part + (size_t)group * p.G * p.n * 128;
+            if (q * 32 < p.n)
+                for (int c = half * 16; c < p.n; c += 64) {
+                    uint32_t raw[16];
+                    __syncwarp();
+                    tmem_ld_x16(acc_a + c + ((uint32_t)(q * 32) << 16), raw);
+                    tmem_ld_wait();
+                    float v[16];
 #pragma unroll
-                for (int t = 0; t < 16; ++t) v[t] = __uint_as_float(raw[t]) * (1.f / (NS_SCALE * NS_SCALE));
-                if (row >= p.n) continue;
-                if (p.G > 1) {
+                    for (int t = 0; t < 16; ++t) v[t] = __uint_as_float(raw[t]) * (1.f / (NS_SCALE * NS_SCALE));
+                    if (p.G > 1) {
 #pragma unroll
-                    for (int t = 0; t < 16; ++t)
-                        if (c + t < p.n) part[(size_t)(c + t) * 128 + row] = v[t];
-                } else {
+                        for (int t = 0; t < 16; ++t)
+                            if (c + t < p.n) part[(size_t)rank * p.n * 128 + (c + t) * 128 + row] = v[t];
+                    } else if (row < p.n) {
+                        float d = 0.f;
 #pragma unroll
-                    for (int t = 0; t < 16; ++t)
-                        if (c + t == row) {
-                            sh.d[row] = v[t];
-                            v[t] = 0.f;
+                        for (int t = 0; t < 16; ++t) {
+                            d = c + t == row ? v[t] : d;
+                            v[t] = c + t == row ? 0.f : v[t];
                         }
-                    uint32_t h[8], l[8];
-                    ns_split<16>(v, h, l);
+                        if (row >= c && row < c + 16) sh.d[row] = d;
+                        uint32_t h[8], l[8];
+                        ns_split<16>(v, h, l);
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        nss_st(E, row, c / 8 + w, h + 4 * w);
-                        nss_st(E + elo, row, c / 8 + w, l + 4 * w);
+                        for (int w = 0; w < 2; ++w) {
+                            nss_st(E, row, c / 8 + w, h + 4 * w);
+                            nss_st(E + elo, row, c / 8 + w, l + 4 * w);
+                        }
                     }
                 }
-            }
             if (p.G > 1) {
                 cluster_sync_all();
-                // this CTA's columns j of A (rows j, A being symmetric): 8 entries a thread, summed in the CTAs' order, to everyone
                 const int j0 = p.n * rank / p.G, j1 = p.n * (rank + 1) / p.G, n8 = (p.n + 7) / 8;
-                const float* in = p.part + (size_t)group * p.G * p.n * 128;
+                uint4* const sums = p.sums + (size_t)group * p.n * n8 * 2;
+                float* const diag = p.diag + (size_t)group * 128;
+#pragma unroll 1
                 for (int u = threadIdx.x; u < (j1 - j0) * n8; u += NSS_THREADS) {
-                    const int j = j0 + u / n8, w = u % n8;
-                    alignas(32) float v[8];
-                    float t[8];
-                    ld8f(in + (size_t)j * 128 + w * 8, v);
-#pragma unroll 4
-                    for (int r = 1; r < p.G; ++r) {
-                        ld8f(in + ((size_t)r * p.n + j) * 128 + w * 8, t);
+                    const int jj = u / n8, j = j0 + jj, w = u - jj * n8;
+                    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, t[8];
+                    const float* from = part + j * 128 + w * 8;
+#pragma unroll 8
+                    for (int r = 0; r < p.G; ++r, from += p.n * 128) {
+                        ld8f(from, t);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) v[k] += t[k];
                     }
+                    float d = 0.f;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        if (w * 8 + k == j)
-                            for (int r = 0; r < p.G; ++r) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_shared(smem_u32(&sh.d[j]), r)), "f"(v[k]) : "memory");
-                        if (w * 8 + k == j || w * 8 + k >= p.n) v[k] = 0.f;
+                        d = w * 8 + k == j ? v[k] : d;
+                        v[k] = w * 8 + k == j || w * 8 + k >= p.n ? 0.f : v[k];
                     }
+                    if ((j >> 3) == w) diag[j] = d;
                     uint32_t h[4], l[4];
                     ns_split<8>(v, h, l);
-                    const uint32_t at = smem + e_at + nss_at(j, w);
-                    for (int r = 0; r < p.G; ++r) {
-                        nss_st_remote(at, r, h);
-                        nss_st_remote(at + elo, r, l);
-                    }
+                    sums[(j * n8 + w) * 2] = make_uint4(h[0], h[1], h[2], h[3]);
+                    sums[(j * n8 + w) * 2 + 1] = make_uint4(l[0], l[1], l[2], l[3]);
                 }
-                asm volatile("fence.proxy.async;" ::: "memory");
                 cluster_sync_all();
+                if (threadIdx.x < p.n) sh.d[threadIdx.x] = diag[threadIdx.x];
+#pragma unroll 4
+                for (int u = threadIdx.x; u < p.n * n8 * 2; u += NSS_THREADS) {
+                    const int j = u / (n8 * 2), w = u - j * (n8 * 2);
+                    *reinterpret_cast<uint4*>(E + (w & 1 ? elo : 0) + nss_at(j, w >> 1)) = sums[u];
+                }
             }
+            // E E, then F X; either product updates pairs in shared memory in place: E -> F = (b + c (d_i + d_j)) E + c E E, X -> r X + F X.
+            // One code for both: a step's instructions are fetched once per step, and the fetch shows.
             const uint32_t ea = smem + e_at;
-            run([&]() {
-                product(acc_a, ea, ea, kc, kc * 64, 0);
-                if (p.terms == 3) {
-                    product(acc_a, ea, ea + elo, kc, kc * 64, 1);
-                    product(acc_a, ea + elo, ea, kc, kc * 64, 1);
-                }
-            });
-            const float di = sh.d[row];
-            for (int c = half * 16; c < p.n; c += 32) {
-                uint32_t raw[16], h[8], l[8];
-                __syncwarp();
-                tmem_ld_x16(acc_a + c + ((uint32_t)(q * 32) << 16), raw);
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    nss_ld(E, row, c / 8 + w, h + 4 * w);
-                    nss_ld(E + elo, row, c / 8 + w, l + 4 * w);
-                }
-                tmem_ld_wait();
-                float v[16];
-#pragma unroll
-                for (int t = 0; t < 16; ++t) {
-                    const float2 fh = half2_at(h[t / 2]), fl = half2_at(l[t / 2]);
-                    const float e = t & 1 ? fh.y + fl.y : fh.x + fl.x, sq = __uint_as_float(raw[t]);
-                    if (c + t == row && row < p.n) sh.rs[row] = ca + fmaf(cb, di, cc * fmaf(di, di, sq));
-                    v[t] = c + t == row || c + t >= p.n ? 0.f : fmaf(cb, e, cc * fmaf(di + sh.d[c + t], e, sq));
-                }
-                if (row >= p.n) continue;
-                ns_split<16>(v, h, l);
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    nss_st(E, row, c / 8 + w, h + 4 * w);
-                    nss_st(E + elo, row, c / 8 + w, l + 4 * w);
-                }
-            }
-            run([&]() {
-                // X lies with the contraction index (its rows) across: 16 rows a step, 64 columns a chunk
-                const uint32_t idesc = (1u << 4) | ((uint32_t)(p.chunks * 8) << 17) | (8u << 24) | (1u << 16);
-                uint32_t accumulate = 0;
-                for (int t = 0; t < p.terms; ++t) {
-                    const uint32_t fa = ea + (t == 2 ? elo : 0), xa = smem + (t == 1 ? xlo : 0);
-                    for (int k = 0; k < 4 * kc; ++k) {
-                        umma_bf16_lo<false>(acc_x, sdesc_lo(fa + (k >> 2) * NSS_CHUNK) + 2 * (k & 3), (((xa & 0x3FFFFu) >> 4) | ((NSS_CHUNK >> 4) << 16)) + k * 128, idesc, accumulate, 1u);
-                        accumulate = 1;
+#pragma unroll 1
+            for (int pass = 0; pass < 2; ++pass) {
+                const bool is_x = pass;
+                run([&]() {
+                    const uint32_t idesc = (1u << 4) | ((uint32_t)(is_x ? p.chunks * 8 : kc * 8) << 17) | (8u << 24) | (is_x ? 1u << 16 : 0u);
+                    const uint32_t d = is_x ? acc_x : acc_a, qh = is_x ? smem : ea, ql = is_x ? smem + xlo : ea + elo;
+                    uint32_t accumulate = 0;
+#pragma unroll 1
+                    for (int t = 0; t < p.terms; ++t) {
+                        const uint32_t fa = ea + (t == 2 ? elo : 0), xa = t == 1 ? ql : qh;
+#pragma unroll 1
+                        for (int k = 0; k < 4 * kc; ++k) {
+                            // X lies with the contraction index (its rows) across: 16 rows a step, 64 columns a chunk
+                            const uint32_t bd = is_x ? (((xa & 0x3FFFFu) >> 4) | ((NSS_CHUNK >> 4) << 16)) + k * 128 : sdesc_lo(xa + (k >> 2) * NSS_CHUNK) + 2 * (k & 3);
+                            umma_bf16_lo<false>(d, sdesc_lo(fa + (k >> 2) * NSS_CHUNK) + 2 * (k & 3), bd, idesc, accumulate, 1u);
+                            accumulate = 1;
+                        }
                     }
-                }
-            });
-            const float factor = sh.rs[row];
-            for (int c = half * 16; c < p.chunks * 64; c += 32) {
-                uint32_t raw[16], h[8], l[8];
-                __syncwarp();
-                tmem_ld_x16(acc_x + c + ((uint32_t)(q * 32) << 16), raw);
+                });
+                if (q * 32 >= p.n) continue;
+                const float di = sh.d[row], factor = is_x ? sh.rs[row] : fmaf(cc, di, cb), fd = is_x ? 0.f : cc, beta = is_x ? 1.f : cc;
+                uint8_t* const at = is_x ? X : E;
+                const int lo = is_x ? xlo : elo, width = is_x ? p.chunks * 64 : p.n;
+                const uint32_t acc = (is_x ? acc_x : acc_a) + ((uint32_t)(q * 32) << 16);
+#pragma unroll 1
+                for (int c = half * 16; c < width; c += 64) {
+                    uint32_t raw[16], h[8], l[8];
+                    __syncwarp();
+                    tmem_ld_x16(acc + c, raw);
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    nss_ld(X, row, c / 8 + w, h + 4 * w);
-                    nss_ld(X + xlo, row, c / 8 + w, l + 4 * w);
-                }
-                tmem_ld_wait();
-                if (row >= p.n) continue;
-                float v[16];
+                    for (int w = 0; w < 2; ++w) {
+                        nss_ld(at, row, c / 8 + w, h + 4 * w);
+                        nss_ld(at + lo, row, c / 8 + w, l + 4 * w);
+                    }
+                    float dj[16], v[16];
 #pragma unroll
-                for (int t = 0; t < 16; ++t) {
-                    const float2 fh = half2_at(h[t / 2]), fl = half2_at(l[t / 2]);
-                    v[t] = fmaf(factor, t & 1 ? fh.y + fl.y : fh.x + fl.x, __uint_as_float(raw[t]));
-                }
-                ns_split<16>(v, h, l);
+                    for (int t = 0; t < 16; t += 4) {
+                        const float4 x = *reinterpret_cast<const float4*>(&sh.d[(c & 127) + t]);
+                        dj[t] = x.x; dj[t + 1] = x.y; dj[t + 2] = x.z; dj[t + 3] = x.w;
+                    }
+                    tmem_ld_wait();
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    nss_st(X, row, c / 8 + w, h + 4 * w);
-                    nss_st(X + xlo, row, c / 8 + w, l + 4 * w);
+                    for (int t = 0; t < 16; ++t) {
+                        const float2 fh = half2_at(h[t / 2]), fl = half2_at(l[t / 2]);
+                        v[t] = fmaf(is_x ? factor : fmaf(fd, dj[t], factor), t & 1 ? fh.y + fl.y : fh.x + fl.x, beta * __uint_as_float(raw[t]));
+                    }
+                    if (!is_x) {                // selects, one store: sixteen branches of one lane each took 1.3 us
+                        float sq = 0.f;
+#pragma unroll
+                        for (int t = 0; t < 16; ++t) {
+                            sq = c + t == row ? __uint_as_float(raw[t]) : sq;
+                            v[t] = c + t == row || c + t >= p.n ? 0.f : v[t];
+                        }
+                        if (row >= c && row < c + 16 && row < p.n) sh.rs[row] = ca + fmaf(cb, di, cc * fmaf(di, di, sq));
+                    }
+                    if (row < p.n) {
+                        ns_split<16>(v, h, l);
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            nss_st(at, row, c / 8 + w, h + 4 * w);
+                            nss_st(at + lo, row, c / 8 + w, l + 4 * w);
+                        }
+                    }
                 }
             }
         }
         __syncthreads();
-        for (int u = threadIdx.x; u < p.n * units; u += NSS_THREADS) {
-            const int i = p.in.tall ? u % p.n : u / units, w = p.in.tall ? u / p.n : u % units, c = c0 + w * 8;
-            uint32_t h[4], l[4];
-            float f[8];
-            nss_ld(X, i, w, h);
-            nss_ld(X + xlo, i, w, l);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float2 fh = half2_at(h[k]), fl = half2_at(l[k]);
-                f[2 * k] = (fh.x + fl.x) * (1.f / NS_SCALE);
-                f[2 * k + 1] = (fh.y + fl.y) * (1.f / NS_SCALE);
-            }
-            if (!p.in.tall && p.in.vec && c < p.m) {
-                ns_put_o<8>(p.in, base + (size_t)i * p.in.cols + c, f);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (c + k < p.m) ns_put_o<1>(p.in, base + (p.in.tall ? (size_t)(c + k) * p.in.cols + i : (size_t)i * p.in.cols + c + k), f + k);
-            }
-        }
+        if (wide) nss_store<8>(p, X, xlo, c0, base);
+        else nss_store<1>(p, X, xlo, c0, base);
         __syncthreads();                        // X is read before the next matrix takes its place
     }
     if (sh.abort) {                             // products in flight end within microseconds; then the CTA may go
@@ -384,20 +463,24 @@ NsSmallPlan ns_small_plan(int batch, int rows, int cols) {
     NsSmallPlan l = {};
     const int n = std::min(rows, cols), m = std::max(rows, cols), all = (m + 63) / 64;
     if (n > 128) return l;
-    // As many CTAs as there are chunks of 64 columns (the slab's products and element-wise work get shorter, the exchange hardly
-    // longer), fewer where a batch fills the device without.
-    const int want = std::max(1, batch);
-    for (int g = 16; g >= 1; g /= 2) {
+    // One CTA where it holds X: no exchange.  Otherwise a chunk of 64 columns each, more where a batch would not fit the device
+    // (128 x 864: 60 us with 16 CTAs, 64 with 8, 76 with 4).
+    for (int g = 1; g <= 16; g *= 2) {
         const int chunks = (all + g - 1) / g, clusters = nss_clusters(g);
-        if ((g > all && g > 1) || clusters < 1) continue;
-        if (chunks > NSS_MAX_CHUNKS) break;
+        if (chunks > 4 || 2 * chunks + 2 * ((n + 63) / 64) > NSS_CHUNKS || clusters < 1) continue;
+        if (l.ctas && clusters < std::max(1, batch)) break;
         l.ctas = g;
         l.chunks = chunks;
-        l.groups = std::min(want, clusters);
-        if (clusters >= want) break;
+        l.groups = std::min(std::max(1, batch), clusters);
+        if (g == 1 || chunks == 1) break;
     }
     l.terms = n <= 64 ? 3 : 1;
-    l.bytes = l.ctas > 1 ? (size_t)l.groups * l.ctas * n * 128 * sizeof(float) : 256;
+    size_t at = 0;
+    auto take = [&](size_t& where, size_t bytes) { where = at; at += (bytes + 255) / 256 * 256; };
+    take(l.part, l.ctas > 1 ? (size_t)l.groups * l.ctas * n * 128 * sizeof(float) : 0);
+    take(l.sums, l.ctas > 1 ? (size_t)l.groups * n * ((n + 7) / 8) * 2 * sizeof(uint4) : 0);
+    take(l.diag, (size_t)l.groups * 128 * sizeof(float));
+    l.bytes = at;
     return l;
 }
 
@@ -407,7 +490,9 @@ int ns_small_run(const NsSmallPlan& plan, int batch, const NsInput& in, int step
     p.batch = batch; p.steps = steps; p.n = std::min(in.rows, in.cols); p.m = std::max(in.rows, in.cols);
     p.G = plan.ctas; p.groups = plan.groups; p.chunks = plan.chunks; p.terms = plan.terms;
     for (int i = 0; i < 3 * steps; ++i) p.coef[i] = coef[i];
-    p.part = (float*)workspace;
+    p.part = (float*)((char*)workspace + plan.part);
+    p.sums = (uint4*)((char*)workspace + plan.sums);
+    p.diag = (float*)((char*)workspace + plan.diag);
     p.status = dev_status_ptr();
     if (!nss_attributes()) return DR_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
