@@ -15,8 +15,8 @@
 //
 // Execution.  One persistent kernel runs all products of a matrix: a group of G CTAs (one per SM) works through the phases
 // A -> F -> X of every step and meets at a barrier between them; a batch is spread over the groups.  Inside a phase a CTA is a
-// pipeline: one warp loads 128-deep operand slices by TMA, one issues tcgen05.mma into one of two accumulators in tensor
-// memory, eight drain the other one.  A group of up to 16 CTAs is a thread-block cluster and uses its barrier; a larger one is
+// pipeline: one warp loads 128-deep operand slices by TMA, two issue tcgen05.mma into one of two sets of accumulators in
+// tensor memory, eight drain the other one.  A group of up to 16 CTAs is a thread-block cluster and uses its barrier; a larger one is
 // launched cooperatively and counts arrivals in global memory.
 #include <algorithm>
 #include <cmath>
@@ -26,7 +26,7 @@
 
 namespace dr {
 
-constexpr int NS_THREADS = 320;             // warp 0: TMA, warp 1: MMA, warps 2 - 9: drain
+constexpr int NS_THREADS = 384;             // warp 0: TMA, warps 1 and 2: MMA, warps 4 - 11: drain, two for each quarter of the accumulator's rows
 constexpr int NS_STAGES = 8;                // at most
 constexpr int NS_SMEM = 196608;             // operand ring; also keeps every SM to one CTA, which owns all its tensor memory
 constexpr int NS_CHUNK = 128 * 128;          // 128 rows x 64 float16
@@ -61,7 +61,7 @@ struct NsShared {
     uint64_t full[NS_STAGES], empty[NS_STAGES], tfull[2], tempty[2];
     uint32_t tmem_base;
     int abort;
-    double red[10];
+    double red[NS_THREADS / 32];
 };
 
 // ------------------------------------------------------------------------------------------------ input and output
@@ -95,15 +95,15 @@ template <int PHASE, bool PAIR>
 __device__ __forceinline__ NsItem ns_item(const NsParams& p, int item) {
     NsItem it;
     it.split = 0;
-    const int kb = ((PHASE == NS_A ? p.m : p.n) + 64 * ns_depth(PAIR) - 1) / (64 * ns_depth(PAIR));
+    const int kb = ((PHASE == NS_A ? p.m : p.n) + 64 * ns_depth(PAIR) - 1) / (64 * ns_depth(PAIR));      // at most 1024; splits at most 148
     it.k0 = 0;
     it.k1 = kb;
     it.tile = item;
-    if (PHASE == NS_A) {
+    if (PHASE == NS_A && p.splits > 1) {
         it.split = item / p.tiles_a;
         it.tile = item - it.split * p.tiles_a;
-        it.k0 = (int)((long long)kb * it.split / p.splits);
-        it.k1 = (int)((long long)kb * (it.split + 1) / p.splits);
+        it.k0 = kb * it.split / p.splits;
+        it.k1 = kb * (it.split + 1) / p.splits;
     }
     if (PHASE == NS_X) {
         const int ni = (p.n + p.tr - 1) / p.tr;
@@ -235,7 +235,6 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             else { ah = &maps.F; al = &maps.Flo; bh = &maps.bx_hi[src]; bl = &maps.bx_lo; }
             const uint32_t bytes = PAIR ? 4u * NS_CHUNK : (uint32_t)(2 * NS_CHUNK + nt * 256);
             bool ok = true;
-            fence_proxy_async_all();                            // what the barrier made visible to this thread, to its TMA loads
             uint32_t ready = mbar_test_u32(empty0 + 8 * pipe.stage, pipe.phase ^ 1);
             for (int item = first; item < items && ok; item += step) {
                 const NsItem it = ns_item<PHASE, PAIR>(p, item);
@@ -262,13 +261,15 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
                 }
             }
         }
-    } else if (warp == 1) {
-        if (side == 0 && elect_one()) {
+    } else if (warp <= 2) {
+        // Two issuing warps (pairs of CTAs: one), each on every second stage into an accumulator of its own, which the drain adds: while one
+        // hands a stage over, the other's MMAs run.
+        const int which = warp - 1;
+        if (side == 0 && (!PAIR || which == 0) && elect_one()) {
             // D float32, A and B float16; B of the X product lies with the contraction index as its rows
             const uint32_t idesc = (1u << 4) | ((uint32_t)(nt >> 3) << 17) | ((PAIR ? 16u : 8u) << 24) | (PHASE == NS_X ? 1u << 16 : 0u);
             const uint32_t b_chunk = (uint32_t)(PAIR ? 128 : nt) * 128u >> 4;       // 64 deep in K: a chunk of B's rows
             bool ok = true;
-            uint32_t ready = mbar_test_u32(full0 + 8 * pipe.stage, pipe.phase);
             for (int item = first; item < items && ok; item += step) {
                 const NsItem it = ns_item<PHASE, PAIR>(p, item);
                 if (!mbar_wait_u32(tempty0 + 8 * pipe.acc, pipe.acc_phase ^ 1, abort_flag)) {
@@ -277,65 +278,66 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
                     break;
                 }
                 tc_fence_after();
-                const uint32_t acc = tmem + pipe.acc * 256;
+                const uint32_t acc = tmem + pipe.acc * 256 + (PAIR ? 0 : which * 128);
                 uint32_t accumulate = 0;
-                for (int k = (it.k1 - it.k0) * p.terms; k > 0; --k) {
-                    if (!ready && !mbar_wait_slow_u32(full0 + 8 * pipe.stage, pipe.phase, abort_flag)) {
+                const int count = (it.k1 - it.k0) * p.terms;
+                for (int k = 0; k < count; ++k) {
+                    if (!PAIR && (k & 1) != which) {
+                        pipe.next_stage(p.stages);
+                        continue;
+                    }
+                    if (!mbar_wait_u32(full0 + 8 * pipe.stage, pipe.phase, abort_flag)) {
                         if (!*abort_flag) report_timeout(p.status, 73, item);
                         *abort_flag = 1;
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t a = smem + pipe.stage * p.stage_bytes, b = a + D * NS_CHUNK, empty = empty0 + 8 * pipe.stage;
+                    const uint32_t a = smem + pipe.stage * p.stage_bytes, b = a + D * NS_CHUNK;
                     const uint32_t ad = sdesc_lo(a), bd = PHASE == NS_X ? (((b & 0x3FFFFu) >> 4) | ((D * 512u) << 16)) : sdesc_lo(b);
-                    pipe.next_stage(p.stages);
-                    ready = mbar_test_u32(full0 + 8 * pipe.stage, pipe.phase);
 #pragma unroll
                     for (int ks = 0; ks < 4 * D; ++ks) {
                         umma_bf16_lo<PAIR>(acc, ad + (ks >> 2) * 1024 + (ks & 3) * 2, bd + (PHASE == NS_X ? ks * 128 : (ks >> 2) * b_chunk + (ks & 3) * 2), idesc, accumulate, 1u);
                         accumulate = 1;
                     }
-                    umma_commit_u32<PAIR>(empty);
+                    umma_commit_u32<PAIR>(empty0 + 8 * pipe.stage);
+                    pipe.next_stage(p.stages);
                 }
                 umma_commit_u32<PAIR>(tfull0 + 8 * pipe.acc);
                 pipe.next_acc();
             }
         }
-    } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;
+    } else if (warp >= 4) {
+        const int q = warp & 3, part = (warp - 4) >> 2;
         const size_t mat = (size_t)group * p.n * p.lda, xm = (size_t)group * p.n * p.ldx;
         float* dvec = p.d + (size_t)group * p.lda;
         float* rs = p.rs + (size_t)group * p.lda;
         for (int item = first; item < items; item += step) {
             const NsItem it = ns_item<PHASE, PAIR>(p, item);
             const int row = it.i * p.tr + side * 128 + q * 32 + lane;
-            // Chunks of 16 columns, two at a time: columns half * 16 + 0 .. 15 and + 32 .. 47 of every 64.  What a chunk needs from memory is
-            // requested a pair ahead, the first pair before the product is waited for.
+            // Chunks of 16 columns: columns part * 16 .. + 15 of every 32.  What a chunk needs from memory is requested a chunk ahead, the first
+            // one's before the product is waited for.
             float factor = 0.f, dj_next = 0.f;
-            Half16 h[2], l[2];
-            alignas(32) float e[2][16];
-            auto request = [&](int pair, int k) {
-                const int col = it.j * nt + pair * 64 + half * 16 + 32 * k;
+            Half16 hn, ln;
+            alignas(32) float en[16];
+            auto request = [&](int c) {
+                const int col = it.j * nt + c;
                 if (PHASE == NS_X && row < p.n && col < p.ldx) {
                     const size_t at = xm + (size_t)row * p.ldx + col;
-                    h[k] = ld16h(p.hi[src] + at);
-                    l[k] = ld16h(p.lo + at);
+                    hn = ld16h(p.hi[src] + at);
+                    ln = ld16h(p.lo + at);
                 }
-                if (PHASE == NS_S && row < p.n && col < p.lda) {
-                    ld8f(p.A + mat + (size_t)row * p.lda + col, e[k]);
-                    ld8f(p.A + mat + (size_t)row * p.lda + col + 8, e[k] + 8);
+                if (PHASE == NS_S && col < p.lda) {
+                    dj_next = dvec[col + (lane & 15)];
+                    if (row < p.n) {
+                        ld8f(p.A + mat + (size_t)row * p.lda + col, en);
+                        ld8f(p.A + mat + (size_t)row * p.lda + col + 8, en + 8);
+                    }
                 }
-            };
-            auto request_d = [&](int pair) {
-                const int col = it.j * nt + pair * 64 + half * 16 + (lane & 15) + 2 * (lane & 16);
-                if (PHASE == NS_S) dj_next = col < p.lda ? dvec[col] : 0.f;
             };
             if (PHASE == NS_X && row < p.n) factor = rs[row];
             if (PHASE == NS_S && row < p.n) factor = dvec[row];
-            request(0, 0);
-            request(0, 1);
-            request_d(0);
+            request(part * 16);
             const bool ok = __all_sync(0xffffffffu, mbar_wait_u32(tfull0 + 8 * pipe.acc, pipe.acc_phase, abort_flag));
             if (!ok) {
                 if (!*abort_flag) report_timeout(p.status, 74, item);
@@ -344,48 +346,52 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             }
             tc_fence_after();
             const uint32_t acc = tmem + pipe.acc * 256 + ((uint32_t)(q * 32) << 16);
-            for (int pair = 0; pair < nt / 64; ++pair) {
-                const float dj_all = dj_next;
-                if (pair + 1 < nt / 64) request_d(pair + 1);
+            const bool two = (it.k1 - it.k0) * p.terms > 1;         // both issuers had a stage
+#pragma unroll 1
+            for (int c = part * 16; c < nt; c += 32) {
+                const int col = it.j * nt + c;
+                uint32_t raw[16], raw2[16];
+                alignas(32) float v[16];
+                __syncwarp();
+                tmem_ld_x16(acc + c, raw);
+                if (!PAIR && two) tmem_ld_x16(acc + 128 + c, raw2);
+                float dj[16], e[16];
+                Half16 h, l;
+                if (PHASE == NS_X) { h = hn; l = ln; }
+                if (PHASE == NS_S) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int c = pair * 64 + half * 16 + 32 * k, col = it.j * nt + c;
-                    uint32_t raw[16];
-                    alignas(32) float v[16];
-                    tmem_ld_x16(acc + c, raw);
-                    float dj[16];
-                    if (PHASE == NS_S) {
-#pragma unroll
-                        for (int t = 0; t < 16; ++t) dj[t] = __shfl_sync(0xffffffffu, dj_all, t + 16 * k);
+                    for (int t = 0; t < 16; ++t) {
+                        e[t] = en[t];
+                        dj[t] = __shfl_sync(0xffffffffu, dj_next, t);
                     }
-                    tmem_ld_wait();
+                }
+                if (PHASE != NS_A && c + 32 < nt) request(c + 32);
+                tmem_ld_wait();
 #pragma unroll
-                    for (int t = 0; t < 16; ++t) v[t] = __uint_as_float(raw[t]);
-                    if (PHASE == NS_A && p.splits > 1) {
-                        float* out = p.part + (((size_t)group * p.splits + it.split) * p.tiles_a + it.tile) * nt * 128 + (size_t)c * 128 + q * 32 + lane;
+                for (int t = 0; t < 16; ++t) v[t] = !PAIR && two ? __uint_as_float(raw[t]) + __uint_as_float(raw2[t]) : __uint_as_float(raw[t]);
+                if (PHASE == NS_A && p.splits > 1) {
+                    float* out = p.part + (((size_t)group * p.splits + it.split) * p.tiles_a + it.tile) * nt * 128 + (size_t)c * 128 + q * 32 + lane;
 #pragma unroll
-                        for (int t = 0; t < 16; ++t) out[t * 128] = v[t];
-                    } else if (row < p.n) {
-                        if (PHASE == NS_A && col < p.lda) {
+                    for (int t = 0; t < 16; ++t) out[t * 128] = v[t];
+                } else if (row < p.n) {
+                    if (PHASE == NS_A && col < p.lda) {
 #pragma unroll
-                            for (int t = 0; t < 16; ++t) v[t] *= 1.f / (NS_SCALE * NS_SCALE);
-                            ns_emit_a<16>(p, mat, dvec, p.full_a, row, col, v);
-                        } else if (PHASE == NS_S && col < p.lda) {
-                            ns_emit_f<16>(p, mat, rs, coef, p.full_s, row, col, factor, dj, e[k], v);
-                        } else if (PHASE == NS_X && col < p.ldx) {
-                            const size_t at = xm + (size_t)row * p.ldx + col;
+                        for (int t = 0; t < 16; ++t) v[t] *= 1.f / (NS_SCALE * NS_SCALE);
+                        ns_emit_a<16>(p, mat, dvec, p.full_a, row, col, v);
+                    } else if (PHASE == NS_S && col < p.lda) {
+                        ns_emit_f<16>(p, mat, rs, coef, p.full_s, row, col, factor, dj, e, v);
+                    } else if (PHASE == NS_X && col < p.ldx) {
+                        const size_t at = xm + (size_t)row * p.ldx + col;
 #pragma unroll
-                            for (int t = 0; t < 8; ++t) {
-                                const float2 fh = half2_at(h[k].u[t]), fl = half2_at(l[k].u[t]);
-                                v[2 * t] = fmaf(factor, fh.x + fl.x, v[2 * t]);
-                                v[2 * t + 1] = fmaf(factor, fh.y + fl.y, v[2 * t + 1]);
-                            }
-                            ns_split<16>(v, h[k].u, l[k].u);
-                            st16h(p.hi[src ^ 1] + at, h[k]);
-                            st16h(p.lo + at, l[k]);
+                        for (int t = 0; t < 8; ++t) {
+                            const float2 fh = half2_at(h.u[t]), fl = half2_at(l.u[t]);
+                            v[2 * t] = fmaf(factor, fh.x + fl.x, v[2 * t]);
+                            v[2 * t + 1] = fmaf(factor, fh.y + fl.y, v[2 * t + 1]);
                         }
+                        ns_split<16>(v, h.u, l.u);
+                        st16h(p.hi[src ^ 1] + at, h);
+                        st16h(p.lo + at, l);
                     }
-                    if (pair + 1 < nt / 64) request(pair + 1, k);
                 }
             }
             tc_fence_before();
@@ -570,7 +576,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     const int group = blockIdx.x / p.G, rank = blockIdx.x - group * p.G;
     if (threadIdx.x == 0) {
         for (int i = 0; i < NS_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], PAIR ? 16 : 8); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], PAIR ? 1 : 2); mbar_init(&sh.tempty[i], PAIR ? 16 : 8); }
         sh.abort = 0;
         fence_barrier_init();
     }
@@ -752,7 +758,7 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
         p.tiles_s = p.full_s ? all(p.nt_s) : tri;
         // A: likewise; or the lower triangle with the long axis split over the CTAs, whose parts meet after another barrier
         const int s = std::max(1, std::min(g / tri, kb / 2));
-        const long long split = cost(tri * s, (kb + s - 1) / s, 128) + (s > 1 ? tunable("DR_NS_SPLITCOST", 11000) : 0), full64 = cost(all(64), kb, 64), full128 = cost(all(128), kb, 128);
+        const long long split = cost(tri * s, (kb + s - 1) / s, 128) + (s > 1 ? 12000 : 0), full64 = cost(all(64), kb, 64), full128 = cost(all(128), kb, 128);
         p.full_a = std::min(full64, full128) <= split;
         p.nt_a = p.full_a && full64 <= full128 ? 64 : 128;
         p.tiles_a = p.full_a ? all(p.nt_a) : tri;
