@@ -45,12 +45,15 @@ struct NsParams {
     int tiles_a, tiles_s, tiles_x;
     int full_a, full_s;         // whether all tiles of A and of E E are computed, not those of the lower triangle alone
     int splits;                 // ranges of the long axis in A = X X^T
+    int merge;                  // whether X takes two steps at a time
     int terms;                  // 1: hi hi;  3: hi hi + hi lo + lo hi
     int stages, stage_bytes;
     float coef[3 * DR_NS_MAX_STEPS];
     // per group
-    __half *hi[2], *lo, *E, *F, *Elo, *Flo;
-    float *A, *d, *rs, *part;
+    __half *hi[2], *lo;
+    // three n x n matrices: off-diagonal entries as float16 (and what that leaves out, with terms == 3), in float32, the diagonal
+    __half *H[3], *L[2];
+    float *W[3], *D[3], *part;
     double* norm;               // [groups][n_norm] where the kernel sums itself, [batch][n_norm] where ns_begin_kernel did
     int n_norm;
     unsigned* arrived;          // [groups]
@@ -143,7 +146,7 @@ __device__ __forceinline__ void ns_row_store(__half* p, const uint32_t* h, int c
 template <int CN>
 __device__ __forceinline__ void ns_emit_a(const NsParams& p, size_t mat, float* dvec, bool full, int i, int c0, float* v) {
     if (!full && c0 > i) return;
-    float* A = p.A + mat;
+    float* A = p.W[0] + mat;
     const int last = full ? CN : min(CN, i - c0 + 1);
     if (last == CN) {
 #pragma unroll
@@ -164,11 +167,11 @@ __device__ __forceinline__ void ns_emit_a(const NsParams& p, size_t mat, float* 
     }
     uint32_t h[CN / 2], l[CN / 2];
     ns_split<CN>(v, h, l);
-    ns_row_store<CN>(p.E + mat + (size_t)i * p.lda + c0, h, last);
-    if (p.terms == 3) ns_row_store<CN>(p.Elo + mat + (size_t)i * p.lda + c0, l, last);
+    ns_row_store<CN>(p.H[0] + mat + (size_t)i * p.lda + c0, h, last);
+    if (p.terms == 3) ns_row_store<CN>(p.L[0] + mat + (size_t)i * p.lda + c0, l, last);
     if (!full) {
-        ns_mirror<CN>(p.E + mat, p.lda, i, c0, h, last);
-        if (p.terms == 3) ns_mirror<CN>(p.Elo + mat, p.lda, i, c0, l, last);
+        ns_mirror<CN>(p.H[0] + mat, p.lda, i, c0, h, last);
+        if (p.terms == 3) ns_mirror<CN>(p.L[0] + mat, p.lda, i, c0, l, last);
         if (p.full_s) {
 #pragma unroll
             for (int c = 0; c < CN; ++c)
@@ -177,33 +180,56 @@ __device__ __forceinline__ void ns_emit_a(const NsParams& p, size_t mat, float* 
     }
 }
 
-// (row i, columns c0 ..) of E E -> the polynomial b A + c A A: F off the diagonal, a + its diagonal as the row's factor.
-// e: A's row, dj: A's diagonal at the columns
+// A product of two of the n x n matrices, U V with U = diag(du) + Eu and V = diag(dv) + Ev: the tensor cores give Eu Ev (v), the rest is added
+// here, du_i Ev_ij + Eu_ij dv_j and du_i dv_i.  `poly`: U = V = A, and the result is a + b A + c A A.  eu, ev: row i of U and V in
+// float32, dj: V's diagonal at the columns.  `full` as above.
+struct NsTriple { int u, v, to, poly, keep; };              // keep: the result is a factor of a later product, kept in float32 too
 template <int CN>
-__device__ __forceinline__ void ns_emit_f(const NsParams& p, size_t mat, float* rs, const float* coef, bool full, int i, int c0, float di, const float* dj, const float* e, float* v) {
+__device__ __forceinline__ void ns_emit_n(const NsParams& p, const NsTriple& t, size_t mat, float* dvec, const float* coef, bool full, int i, int c0, float du, float dv, const float* dj,
+                                          const float* eu, const float* ev, float* v) {
     if (!full && c0 > i) return;
-    const float a = coef[0], b = coef[1], cc = coef[2];
-    float sq = 0.f;
+    float diag = 0.f;
 #pragma unroll
     for (int c = 0; c < CN; ++c) {
-        sq = c0 + c == i ? v[c] : sq;
-        v[c] = c0 + c == i ? 0.f : fmaf(b, e[c], cc * fmaf(di + dj[c], e[c], v[c]));
+        diag = c0 + c == i ? v[c] : diag;
+        float f = fmaf(du, ev[c], fmaf(eu[c], dj[c], v[c]));
+        if (t.poly) f = fmaf(coef[1], eu[c], coef[2] * f);
+        v[c] = c0 + c == i ? 0.f : f;
     }
-    if (i >= c0 && i < c0 + CN) rs[i] = a + fmaf(b, di, cc * fmaf(di, di, sq));
+    if (i >= c0 && i < c0 + CN) {
+        diag = fmaf(du, dv, diag);
+        dvec[i] = t.poly ? coef[0] + fmaf(coef[1], du, coef[2] * diag) : diag;
+    }
     uint32_t h[CN / 2], l[CN / 2];
     ns_split<CN>(v, h, l);
     const int last = full ? CN : min(CN, i - c0 + 1);
-    ns_row_store<CN>(p.F + mat + (size_t)i * p.lda + c0, h, last);
-    if (p.terms == 3) ns_row_store<CN>(p.Flo + mat + (size_t)i * p.lda + c0, l, last);
-    if (!full) {
-        ns_mirror<CN>(p.F + mat, p.lda, i, c0, h, last);
-        if (p.terms == 3) ns_mirror<CN>(p.Flo + mat, p.lda, i, c0, l, last);
+    ns_row_store<CN>(p.H[t.to] + mat + (size_t)i * p.lda + c0, h, last);
+    if (!full) ns_mirror<CN>(p.H[t.to] + mat, p.lda, i, c0, h, last);
+    if (p.terms == 3) {
+        ns_row_store<CN>(p.L[t.to] + mat + (size_t)i * p.lda + c0, l, last);
+        if (!full) ns_mirror<CN>(p.L[t.to] + mat, p.lda, i, c0, l, last);
+    }
+    if (t.keep) {
+        float* w = p.W[t.to] + mat + (size_t)i * p.lda + c0;
+        if (last == CN) {
+#pragma unroll
+            for (int c = 0; c < CN; c += 8) st8f(w + c, v + c);
+        } else {
+#pragma unroll
+            for (int c = 0; c < CN; ++c)
+                if (c < last) w[c] = v[c];
+        }
     }
 }
 
-// All operands are seen as [group][64-column chunk][row][64].  The first operand's boxes are 128 rows x 2 chunks (pairs: 1); so are the
-// second's (b_*), except for tiles of 64 columns and in the X product of pairs (64 rows x 2 chunks).
-struct NsMaps { CUtensorMap hi[2], lo, E, F, Elo, Flo, ba_hi[2], ba_lo, bs_hi, bs_lo, bx_hi[2], bx_lo; };
+// All operands are seen as [group][64-column chunk][row][64].  The first operand's boxes are 128 rows x a stage's depth in chunks.  The second's
+// (b_*): 128 rows or, for the narrower tiles, 64; in the X product a stage's depth in rows x 2 chunks or 1.
+struct NsMaps { CUtensorMap hi[2], lo, H[3], L[2], ba_hi[2], ba_lo, bs[3], bs_lo, bx_hi[2], bx_lo; };
+
+template <int CN> __device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t* r) {
+    if constexpr (CN == 8) tmem_ld_x8(addr, r);
+    else tmem_ld_x16(addr, r);
+}
 
 // Where the roles of a CTA stand in their rings; kept from phase to phase.
 struct NsPipe {
@@ -216,7 +242,7 @@ struct NsPipe {
 };
 
 template <int PHASE, bool PAIR>
-__device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps, NsShared& sh, uint32_t smem, uint32_t tmem, NsPipe& pipe, int group, int rank, int src, const float* coef) {
+__device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps, NsShared& sh, uint32_t smem, uint32_t tmem, NsPipe& pipe, int group, int rank, int src, const NsTriple triple, const float* coef) {
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int nt = PHASE == NS_A ? p.nt_a : PHASE == NS_S ? p.nt_s : p.nt_x;
     const int items = PHASE == NS_A ? p.tiles_a * p.splits : PHASE == NS_S ? p.tiles_s : p.tiles_x;
@@ -231,9 +257,9 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
         if (elect_one()) {
             const CUtensorMap *ah, *al, *bh, *bl;
             if (PHASE == NS_A) { ah = &maps.hi[src]; al = &maps.lo; bh = &maps.ba_hi[src]; bl = &maps.ba_lo; }
-            else if (PHASE == NS_S) { ah = &maps.E; al = &maps.Elo; bh = &maps.bs_hi; bl = &maps.bs_lo; }
-            else { ah = &maps.F; al = &maps.Flo; bh = &maps.bx_hi[src]; bl = &maps.bx_lo; }
-            const uint32_t bytes = PAIR ? 4u * NS_CHUNK : (uint32_t)(2 * NS_CHUNK + nt * 256);
+            else if (PHASE == NS_S) { ah = &maps.H[triple.u]; al = &maps.L[0]; bh = &maps.bs[triple.v]; bl = &maps.bs_lo; }
+            else { ah = &maps.H[triple.u]; al = &maps.L[1]; bh = &maps.bx_hi[src]; bl = &maps.bx_lo; }
+            const uint32_t bytes = PAIR ? (uint32_t)(2 * NS_CHUNK + nt * 128) : (uint32_t)(2 * NS_CHUNK + nt * 256);      // of a stage, pairs: of both CTAs
             bool ok = true;
             uint32_t ready = mbar_test_u32(empty0 + 8 * pipe.stage, pipe.phase ^ 1);
             for (int item = first; item < items && ok; item += step) {
@@ -268,7 +294,7 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
         if (side == 0 && (!PAIR || which == 0) && elect_one()) {
             // D float32, A and B float16; B of the X product lies with the contraction index as its rows
             const uint32_t idesc = (1u << 4) | ((uint32_t)(nt >> 3) << 17) | ((PAIR ? 16u : 8u) << 24) | (PHASE == NS_X ? 1u << 16 : 0u);
-            const uint32_t b_chunk = (uint32_t)(PAIR ? 128 : nt) * 128u >> 4;       // 64 deep in K: a chunk of B's rows
+            const uint32_t b_chunk = (uint32_t)nt * 128u >> 4;      // 64 deep in K: a chunk of B's rows
             bool ok = true;
             for (int item = first; item < items && ok; item += step) {
                 const NsItem it = ns_item<PHASE, PAIR>(p, item);
@@ -281,27 +307,29 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
                 const uint32_t acc = tmem + pipe.acc * 256 + (PAIR ? 0 : which * 128);
                 uint32_t accumulate = 0;
                 const int count = (it.k1 - it.k0) * p.terms;
+                uint32_t ready = 0;
                 for (int k = 0; k < count; ++k) {
                     if (!PAIR && (k & 1) != which) {
                         pipe.next_stage(p.stages);
                         continue;
                     }
-                    if (!mbar_wait_u32(full0 + 8 * pipe.stage, pipe.phase, abort_flag)) {
+                    if (!ready && !mbar_wait_u32(full0 + 8 * pipe.stage, pipe.phase, abort_flag)) {
                         if (!*abort_flag) report_timeout(p.status, 73, item);
                         *abort_flag = 1;
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t a = smem + pipe.stage * p.stage_bytes, b = a + D * NS_CHUNK;
+                    const uint32_t a = smem + pipe.stage * p.stage_bytes, b = a + D * NS_CHUNK, empty = empty0 + 8 * pipe.stage;
+                    pipe.next_stage(p.stages);
+                    if (PAIR) ready = mbar_test_u32(full0 + 8 * pipe.stage, pipe.phase);    // asked before the MMAs, known after them
                     const uint32_t ad = sdesc_lo(a), bd = PHASE == NS_X ? (((b & 0x3FFFFu) >> 4) | ((D * 512u) << 16)) : sdesc_lo(b);
 #pragma unroll
                     for (int ks = 0; ks < 4 * D; ++ks) {
                         umma_bf16_lo<PAIR>(acc, ad + (ks >> 2) * 1024 + (ks & 3) * 2, bd + (PHASE == NS_X ? ks * 128 : (ks >> 2) * b_chunk + (ks & 3) * 2), idesc, accumulate, 1u);
                         accumulate = 1;
                     }
-                    umma_commit_u32<PAIR>(empty0 + 8 * pipe.stage);
-                    pipe.next_stage(p.stages);
+                    umma_commit_u32<PAIR>(empty);
                 }
                 umma_commit_u32<PAIR>(tfull0 + 8 * pipe.acc);
                 pipe.next_acc();
@@ -310,16 +338,16 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
     } else if (warp >= 4) {
         const int q = warp & 3, part = (warp - 4) >> 2;
         const size_t mat = (size_t)group * p.n * p.lda, xm = (size_t)group * p.n * p.ldx;
-        float* dvec = p.d + (size_t)group * p.lda;
-        float* rs = p.rs + (size_t)group * p.lda;
+        const size_t dg = (size_t)group * p.lda;
         for (int item = first; item < items; item += step) {
             const NsItem it = ns_item<PHASE, PAIR>(p, item);
             const int row = it.i * p.tr + side * 128 + q * 32 + lane;
-            // Chunks of 16 columns: columns part * 16 .. + 15 of every 32.  What a chunk needs from memory is requested a chunk ahead, the first
-            // one's before the product is waited for.
-            float factor = 0.f, dj_next = 0.f;
+            // Chunks of 16 columns (8 in the n x n products, which need more of each), alternating between the two warps of a quarter.  What a
+            // chunk needs from memory is requested a chunk ahead, the first one's before the product is waited for.
+            constexpr int CN = PHASE == NS_S ? 8 : 16;
+            float factor = 0.f, dv = 0.f, dj_next = 0.f;    // NS_X: the row's factor; NS_S: the row's diagonal entries in U and V
             Half16 hn, ln;
-            alignas(32) float en[16];
+            alignas(32) float un[8], vn[8];
             auto request = [&](int c) {
                 const int col = it.j * nt + c;
                 if (PHASE == NS_X && row < p.n && col < p.ldx) {
@@ -328,16 +356,16 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
                     ln = ld16h(p.lo + at);
                 }
                 if (PHASE == NS_S && col < p.lda) {
-                    dj_next = dvec[col + (lane & 15)];
+                    dj_next = p.D[triple.v][dg + col + (lane & 7)];
                     if (row < p.n) {
-                        ld8f(p.A + mat + (size_t)row * p.lda + col, en);
-                        ld8f(p.A + mat + (size_t)row * p.lda + col + 8, en + 8);
+                        ld8f(p.W[triple.u] + mat + (size_t)row * p.lda + col, un);
+                        if (!triple.poly) ld8f(p.W[triple.v] + mat + (size_t)row * p.lda + col, vn);
                     }
                 }
             };
-            if (PHASE == NS_X && row < p.n) factor = rs[row];
-            if (PHASE == NS_S && row < p.n) factor = dvec[row];
-            request(part * 16);
+            if (PHASE != NS_A && row < p.n) factor = p.D[triple.u][dg + row];
+            if (PHASE == NS_S && row < p.n) dv = p.D[triple.v][dg + row];
+            request(part * CN);
             const bool ok = __all_sync(0xffffffffu, mbar_wait_u32(tfull0 + 8 * pipe.acc, pipe.acc_phase, abort_flag));
             if (!ok) {
                 if (!*abort_flag) report_timeout(p.status, 74, item);
@@ -348,39 +376,42 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             const uint32_t acc = tmem + pipe.acc * 256 + ((uint32_t)(q * 32) << 16);
             const bool two = (it.k1 - it.k0) * p.terms > 1;         // both issuers had a stage
 #pragma unroll 1
-            for (int c = part * 16; c < nt; c += 32) {
+            for (int c = part * CN; c < nt; c += 2 * CN) {
                 const int col = it.j * nt + c;
-                uint32_t raw[16], raw2[16];
-                alignas(32) float v[16];
+                uint32_t raw[CN], raw2[CN];
+                alignas(32) float v[CN];
                 __syncwarp();
-                tmem_ld_x16(acc + c, raw);
-                if (!PAIR && two) tmem_ld_x16(acc + 128 + c, raw2);
-                float dj[16], e[16];
+                tmem_ld<CN>(acc + c, raw);
+                if (!PAIR && two) tmem_ld<CN>(acc + 128 + c, raw2);
+                float dj[8], eu[8], ev[8];
                 Half16 h, l;
                 if (PHASE == NS_X) { h = hn; l = ln; }
                 if (PHASE == NS_S) {
 #pragma unroll
-                    for (int t = 0; t < 16; ++t) {
-                        e[t] = en[t];
+                    for (int t = 0; t < 8; ++t) {
+                        eu[t] = un[t];
+                        ev[t] = triple.poly ? un[t] : vn[t];
                         dj[t] = __shfl_sync(0xffffffffu, dj_next, t);
                     }
                 }
-                if (PHASE != NS_A && c + 32 < nt) request(c + 32);
+                if (PHASE != NS_A && c + 2 * CN < nt) request(c + 2 * CN);
                 tmem_ld_wait();
 #pragma unroll
-                for (int t = 0; t < 16; ++t) v[t] = !PAIR && two ? __uint_as_float(raw[t]) + __uint_as_float(raw2[t]) : __uint_as_float(raw[t]);
+                for (int t = 0; t < CN; ++t) v[t] = !PAIR && two ? __uint_as_float(raw[t]) + __uint_as_float(raw2[t]) : __uint_as_float(raw[t]);
                 if (PHASE == NS_A && p.splits > 1) {
                     float* out = p.part + (((size_t)group * p.splits + it.split) * p.tiles_a + it.tile) * nt * 128 + (size_t)c * 128 + q * 32 + lane;
 #pragma unroll
-                    for (int t = 0; t < 16; ++t) out[t * 128] = v[t];
+                    for (int t = 0; t < CN; ++t) out[t * 128] = v[t];
                 } else if (row < p.n) {
-                    if (PHASE == NS_A && col < p.lda) {
+                    if constexpr (PHASE == NS_A) {
+                        if (col < p.lda) {
 #pragma unroll
-                        for (int t = 0; t < 16; ++t) v[t] *= 1.f / (NS_SCALE * NS_SCALE);
-                        ns_emit_a<16>(p, mat, dvec, p.full_a, row, col, v);
-                    } else if (PHASE == NS_S && col < p.lda) {
-                        ns_emit_f<16>(p, mat, rs, coef, p.full_s, row, col, factor, dj, e, v);
-                    } else if (PHASE == NS_X && col < p.ldx) {
+                            for (int t = 0; t < CN; ++t) v[t] *= 1.f / (NS_SCALE * NS_SCALE);
+                            ns_emit_a<CN>(p, mat, p.D[0] + dg, p.full_a, row, col, v);
+                        }
+                    } else if constexpr (PHASE == NS_S) {
+                        if (col < p.lda) ns_emit_n<CN>(p, triple, mat, p.D[triple.to] + dg, coef, p.full_s, row, col, factor, dv, dj, eu, ev, v);
+                    } else if (col < p.ldx) {
                         const size_t at = xm + (size_t)row * p.ldx + col;
 #pragma unroll
                         for (int t = 0; t < 8; ++t) {
@@ -591,14 +622,16 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     const uint32_t tmem = sh.tmem_base;
     NsPipe pipe;
     unsigned epoch = 0;
-    // the columns that pad A, E and F to whole chunks take part in the products: zero (X's are zeroed where it is loaded)
+    // the columns that pad the n x n matrices to whole chunks take part in the products: zero (X's are zeroed where it is loaded)
     for (int i = rank * NS_THREADS + threadIdx.x; i < p.n * (p.lda - p.n); i += p.G * NS_THREADS) {
         const int r = i / (p.lda - p.n);
         const size_t at = ((size_t)group * p.n + r) * p.lda + p.n + (i - r * (p.lda - p.n));
-        p.E[at] = p.F[at] = __float2half_rn(0.f);
-        if (p.terms == 3) p.Elo[at] = p.Flo[at] = __float2half_rn(0.f);
-        p.A[at] = 0.f;
-        if (r == 0) p.d[(size_t)group * p.lda + p.n + i] = 0.f;
+        for (int k = 0; k < (p.merge ? 3 : 2); ++k) {
+            p.H[k][at] = __float2half_rn(0.f);
+            if (k == 0 || p.merge) p.W[k][at] = 0.f;
+            if (p.terms == 3) p.L[k][at] = __float2half_rn(0.f);
+            if (r == 0) p.D[k][(size_t)group * p.lda + p.n + i] = 0.f;
+        }
     }
     const size_t per = (size_t)p.in.rows * p.in.cols;
 
@@ -623,8 +656,9 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
         ns_convert<true>(p, tile, group, rank, base, 0, inv);
         ns_group_sync(p, sh, group, epoch);
         int src = 0;
-        for (int k = 0; k < p.steps; ++k, src ^= 1) {
-            ns_product<NS_A, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, nullptr);
+        for (int k = 0; k < p.steps; src ^= 1) {
+            const bool two = p.merge && k + 1 < p.steps;
+            ns_product<NS_A, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, NsTriple{}, nullptr);
             ns_group_sync(p, sh, group, epoch);
             if (p.splits > 1) {
                 // the ranges' parts of A in order: a warp takes 32 rows x 8 columns
@@ -641,14 +675,21 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
                         for (int e = 0; e < 8; ++e) v[e] += in[(size_t)q * p.tiles_a * nt * 128 + e * 128];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] *= 1.f / (NS_SCALE * NS_SCALE);
-                    if (row < p.n) ns_emit_a<8>(p, (size_t)group * p.n * p.lda, p.d + (size_t)group * p.lda, false, row, j * nt + c, v);
+                    if (row < p.n) ns_emit_a<8>(p, (size_t)group * p.n * p.lda, p.D[0] + (size_t)group * p.lda, false, row, j * nt + c, v);
                 }
                 ns_group_sync(p, sh, group, epoch);
             }
-            ns_product<NS_S, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, p.coef + 3 * k);
+            // A in 0.  One step: Q(A) in 1, X <- Q X.  Two: all factors are polynomials of A and commute, so the second step's A is Q A Q:
+            // Q(A) in 1, Q A in 2, A' = (Q A) Q in 0, Q'(A') in 2, Q' Q in 0, X <- (Q' Q) X.
+#pragma unroll 1
+            for (int j = 0; j < (two ? 5 : 1); ++j) {
+                const NsTriple t = j == 0 ? NsTriple{0, 0, 1, 1, two} : j == 1 ? NsTriple{1, 0, 2, 0, 1} : j == 2 ? NsTriple{2, 1, 0, 0, 1} : j == 3 ? NsTriple{0, 0, 2, 1, 1} : NsTriple{2, 1, 0, 0, 0};
+                ns_product<NS_S, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, t, p.coef + 3 * (k + (j == 3)));
+                ns_group_sync(p, sh, group, epoch);
+            }
+            ns_product<NS_X, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, NsTriple{two ? 0 : 1, 0, 0, 0, 0}, nullptr);
             ns_group_sync(p, sh, group, epoch);
-            ns_product<NS_X, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, nullptr);
-            ns_group_sync(p, sh, group, epoch);
+            k += two ? 2 : 1;
         }
         ns_convert<false>(p, tile, group, rank, base, src, 0.f);
         ns_group_sync(p, sh, group, epoch);     // the buffers are free for the group's next matrix
@@ -682,7 +723,7 @@ static bool ns_attributes() {
 
 struct NsPlan {
     NsParams p;
-    size_t hi0, hi1, lo, E, F, Elo, Flo, A, d, rs, part, norm, arrived, total;
+    size_t hi0, hi1, lo, H[3], L[2], W[3], D[3], part, norm, arrived, total;
     int norm_blocks;
 };
 
@@ -720,15 +761,13 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     p.in.rows = rows; p.in.cols = cols; p.in.tall = rows > cols;
     p.n = std::min(rows, cols); p.m = std::max(rows, cols);
     p.ldx = (p.m + 63) / 64 * 64; p.lda = (p.n + 63) / 64 * 64;
-    p.terms = p.n <= tunable("DR_NS_FINE", 128) ? 3 : 1;
-    const int ni = (p.n + 127) / 128;
-    auto tiles_x = [&](int nt) { return ni * ((p.m + nt - 1) / nt); };
+    p.terms = p.n <= 64 ? 3 : 1;
     // CTAs per matrix: what the widest phase can use with its narrowest tiles, at most all SMs
     const int batch1 = batch < 1 ? 1 : batch;
-    int g = std::min(std::max(tiles_x(64), 1), sms);
-    g = std::min(g, std::max(1, sms / batch1));
-    const int max_cluster = tunable("DR_NS_CLUSTER", ns_max_cluster());
-    if (g <= max_cluster) {
+    const int rows128 = (p.n + 127) / 128, rows256 = (p.n + 255) / 256;
+    auto across = [](int width, int nt) { return (width + nt - 1) / nt; };
+    int g = std::min({std::max(rows128 * across(p.m, 64), 1), sms, std::max(1, sms / batch1)});
+    if (g <= ns_max_cluster()) {
         int q = 1;
         while (q * 2 <= g) q *= 2;
         g = q;
@@ -736,44 +775,65 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     }
     p.G = g;
     p.groups = std::min(batch1, std::max(1, sms / g));
-    const int kb = (p.m + 127) / 128, kn = (p.n + 127) / 128;       // stages of 128 along either axis
-    p.pair = g == sms && sms % 2 == 0 && p.n >= tunable("DR_NS_PAIR", 1024);
-    p.tr = p.pair ? 256 : 128;
-    if (p.pair) {
-        p.nt_x = p.nt_s = p.nt_a = 256;
-        p.tiles_x = ((p.n + 255) / 256) * ((p.m + 255) / 256);
-        p.tiles_s = p.tiles_a = ns_tri_tiles(p.n, 256, 256);
-        p.splits = 1;
-    } else {
-        // Cycles of a phase: rounds of tiles over the group's CTAs, each of `k` stages at the issuing thread's pace (as slow for 64
-        // columns as for 128) and a tile's fill and drain.
-        auto cost = [&](int tiles, int k, int nt) { return (long long)((tiles + g - 1) / g) * (k * 850 + (nt == 64 ? 3000 : 4500)); };
-        auto all = [&](int nt) { return ni * ((p.n + nt - 1) / nt); };
-        const int tri = ns_tri_tiles(p.n, 128, 128);
-        p.nt_x = cost(tiles_x(64), kn, 64) < cost(tiles_x(128), kn, 128) ? 64 : 128;
-        p.tiles_x = tiles_x(p.nt_x);
-        // E E: all tiles where the group has a CTA for each (no mirrored stores), otherwise the lower triangle
-        p.full_s = all(128) <= g;
-        p.nt_s = all(64) <= g ? 64 : 128;
-        p.tiles_s = p.full_s ? all(p.nt_s) : tri;
-        // A: likewise; or the lower triangle with the long axis split over the CTAs, whose parts meet after another barrier
-        const int s = std::max(1, std::min(g / tri, kb / 2));
-        const long long split = cost(tri * s, (kb + s - 1) / s, 128) + (s > 1 ? 12000 : 0), full64 = cost(all(64), kb, 64), full128 = cost(all(128), kb, 128);
-        p.full_a = std::min(full64, full128) <= split;
-        p.nt_a = p.full_a && full64 <= full128 ? 64 : 128;
-        p.tiles_a = p.full_a ? all(p.nt_a) : tri;
-        p.splits = p.full_a ? 1 : s;
+    // Cycles of a phase, fitted on 15 shapes: its start, rounds of tiles over the group's CTAs, and the last tile's drain.  A round takes the longer of
+    // its slices and the drain of the tile before it; a 64-deep slice the longest of its MMAs, the issuing threads' hand-over (one of
+    // two threads, or a pair's only one) and its operands' way out of L2 (7000 bytes a cycle for all SMs).
+    auto cost = [&](int tiles, int chunks, int nt, bool pair) {
+        const int units = pair ? g / 2 : g, rounds = (tiles + units - 1) / units, busy = std::min(tiles, units) * (pair ? 2 : 1);
+        const long long bytes = NS_CHUNK + (pair ? nt / 2 : nt) * 128, drain = 60 * nt;
+        const long long slice = std::max<long long>({pair ? 700 : 330, 2 * std::max(nt, 128), p.groups * busy * bytes / 7000});
+        return 2500 + rounds * std::max(chunks * slice, drain) + drain;
+    };
+    constexpr long long BARRIER = 2500, SPLIT = 10000;          // a barrier; what splitting A adds: parts written, barrier, parts summed
+    const int cm = (p.m + 63) / 64, cn = (p.n + 63) / 64;
+    struct Choice { long long a, s, x; int nt_a, nt_s, nt_x, tiles_a, tiles_s, tiles_x, full_a, full_s, splits; };
+    auto choose = [&](bool pair) {
+        Choice c = {};
+        const int rows = pair ? rows256 : rows128, tr = pair ? 256 : 128, wide = pair ? 256 : 128, narrow = wide / 2;
+        c.x = c.s = c.a = -1;
+        for (int nt : {wide, narrow}) {
+            const int all_x = rows * across(p.m, nt), all_n = rows * across(p.n, nt), tri = ns_tri_tiles(p.n, tr, nt);
+            auto take = [](long long& best, long long now) { const bool better = best < 0 || now < best; if (better) best = now; return better; };
+            if (take(c.x, cost(all_x, cn, nt, pair))) { c.nt_x = nt; c.tiles_x = all_x; }
+            // all tiles of a symmetric product where the group has a CTA for each (no mirrored stores), otherwise those of the lower triangle
+            const bool full = !pair && all_n <= g;
+            if ((full || nt == wide || pair) && take(c.s, cost(full ? all_n : tri, cn, nt, pair))) { c.nt_s = nt; c.full_s = full; c.tiles_s = full ? all_n : tri; }
+            if (full && take(c.a, cost(all_n, cm, nt, pair))) { c.nt_a = nt; c.full_a = 1; c.tiles_a = all_n; c.splits = 1; }
+            if (nt == wide || pair) {
+                // or the lower triangle with the long axis split over the CTAs, whose parts meet after another barrier
+                const int s = pair ? 1 : std::max(1, std::min(g / tri, cm / 4));
+                if (take(c.a, cost(tri * s, (cm + s - 1) / s, nt, pair) + (s > 1 ? SPLIT : 0))) { c.nt_a = nt; c.full_a = 0; c.tiles_a = tri; c.splits = s; }
+            }
+        }
+        return c;
+    };
+    Choice c = choose(false);
+    if (g == sms && sms % 2 == 0 && p.n > 128) {
+        const Choice two = choose(true);
+        if (two.a + two.s + two.x < c.a + c.s + c.x) { c = two; p.pair = 1; }
     }
-    p.stage_bytes = p.pair ? 2 * NS_CHUNK : 2 * NS_CHUNK + std::max(p.nt_x, std::max(p.nt_s, p.nt_a)) * 256;
+    p.tr = p.pair ? 256 : 128;
+    p.nt_a = c.nt_a; p.nt_s = c.nt_s; p.nt_x = c.nt_x;
+    p.tiles_a = c.tiles_a; p.tiles_s = c.tiles_s; p.tiles_x = c.tiles_x;
+    p.full_a = c.full_a; p.full_s = c.full_s; p.splits = c.splits;
+    p.stage_bytes = ns_depth(p.pair) * (NS_CHUNK + std::max(p.nt_x, std::max(p.nt_s, p.nt_a)) * (p.pair ? 64 : 128));
     p.stages = std::min(NS_STAGES, NS_SMEM / p.stage_bytes);
+    // Two steps of X at a time save one A and one X product of every two and cost three more n x n products, and a barrier each (512 x 13200:
+    // 270 -> 256 us, 4096 x 9216: 2.42 -> 2.12 ms, but 512 x 2048: 134 -> 150 us).  Rounding errors of A' are of A's size, not of its
+    // small entries': fine for one such step (1.5 times the error of O on spectra over four decades), not for a chain of them.
+    p.merge = p.terms == 1 && 5 * (c.a + c.x + 2 * BARRIER) > 7 * 3 * (c.s + BARRIER);
     l.norm_blocks = (int)std::min<size_t>(NS_NORM_BLOCKS, ((size_t)rows * cols + 2047) / 2048);
     p.n_norm = p.cluster || g == 1 ? g : l.norm_blocks;
     size_t at = 0;
     auto take = [&](size_t& where, size_t bytes) { where = at; at += (bytes + 255) / 256 * 256; };
     const size_t x = (size_t)p.groups * p.n * p.ldx * 2, a = (size_t)p.groups * p.n * p.lda * 2;
     take(l.hi0, x); take(l.hi1, x); take(l.lo, x);
-    take(l.E, a); take(l.F, a); take(l.Elo, p.terms == 3 ? a : 0); take(l.Flo, p.terms == 3 ? a : 0); take(l.A, 2 * a);
-    take(l.d, (size_t)p.groups * p.lda * 4); take(l.rs, (size_t)p.groups * p.lda * 4);
+    for (int k = 0; k < 3; ++k) {
+        take(l.H[k], k < 2 || p.merge ? a : 0);
+        take(l.W[k], k == 0 || p.merge ? 2 * a : 0);
+        take(l.D[k], (size_t)p.groups * p.lda * 4);
+        if (k < 2) take(l.L[k], p.terms == 3 ? a : 0);
+    }
     take(l.part, p.splits > 1 ? (size_t)p.groups * p.splits * p.tiles_a * p.nt_a * 128 * 4 : 0);
     take(l.norm, (size_t)(p.cluster || g == 1 ? p.groups : batch1) * p.n_norm * 8);
     take(l.arrived, (size_t)p.groups * 4);
@@ -816,8 +876,11 @@ static int ns_run(int batch, NsInput in, int steps, const float* coef, char* ws,
     p.steps = steps;
     for (int i = 0; i < 3 * steps; ++i) p.coef[i] = own[i];
     p.hi[0] = (__half*)(ws + l.hi0); p.hi[1] = (__half*)(ws + l.hi1); p.lo = (__half*)(ws + l.lo);
-    p.E = (__half*)(ws + l.E); p.F = (__half*)(ws + l.F); p.Elo = (__half*)(ws + l.Elo); p.Flo = (__half*)(ws + l.Flo);
-    p.A = (float*)(ws + l.A); p.d = (float*)(ws + l.d); p.rs = (float*)(ws + l.rs); p.part = (float*)(ws + l.part);
+    for (int k = 0; k < 3; ++k) {
+        p.H[k] = (__half*)(ws + l.H[k]); p.W[k] = (float*)(ws + l.W[k]); p.D[k] = (float*)(ws + l.D[k]);
+        if (k < 2) p.L[k] = (__half*)(ws + l.L[k]);
+    }
+    p.part = (float*)(ws + l.part);
     p.norm = (double*)(ws + l.norm); p.arrived = (unsigned*)(ws + l.arrived);
     p.status = dev_status_ptr();
     alignas(64) NsMaps maps;
@@ -827,23 +890,30 @@ static int ns_run(int batch, NsInput in, int steps, const float* coef, char* ws,
     };
     auto same = [](CUtensorMap& m, const CUtensorMap& o) { std::memcpy(&m, &o, sizeof(m)); };
     const bool lows = p.terms == 3;
+    const int depth = ns_depth(p.pair), narrow = p.pair ? 128 : 64;
     for (int k = 0; k < 2; ++k) {
-        put(maps.hi[k], p.hi[k], p.ldx, 128, ns_depth(p.pair));
-        if (p.nt_a == 64) put(maps.ba_hi[k], p.hi[k], p.ldx, 64, 2); else same(maps.ba_hi[k], maps.hi[k]);
-        if (p.nt_x == 64) put(maps.bx_hi[k], p.hi[k], p.ldx, 128, 1); else if (p.pair) put(maps.bx_hi[k], p.hi[k], p.ldx, 64, 2); else same(maps.bx_hi[k], maps.hi[k]);
+        put(maps.hi[k], p.hi[k], p.ldx, 128, depth);
+        if (p.nt_a == narrow) put(maps.ba_hi[k], p.hi[k], p.ldx, 64, depth); else same(maps.ba_hi[k], maps.hi[k]);
+        put(maps.bx_hi[k], p.hi[k], p.ldx, 64 * depth, p.nt_x == narrow ? 1 : 2);
     }
-    put(maps.E, p.E, p.lda, 128, ns_depth(p.pair));
-    put(maps.F, p.F, p.lda, 128, ns_depth(p.pair));
-    if (p.nt_s == 64) put(maps.bs_hi, p.E, p.lda, 64, 2); else same(maps.bs_hi, maps.E);
+    for (int k = 0; k < 3; ++k) {
+        if (k == 2 && !p.merge) {               // not read
+            same(maps.H[2], maps.H[0]);
+            same(maps.bs[2], maps.bs[0]);
+            break;
+        }
+        put(maps.H[k], p.H[k], p.lda, 128, depth);
+        if (p.nt_s == narrow) put(maps.bs[k], p.H[k], p.lda, 64, depth); else same(maps.bs[k], maps.H[k]);
+    }
     if (lows) {
         put(maps.lo, p.lo, p.ldx, 128, 2);
-        put(maps.Elo, p.Elo, p.lda, 128, 2);
-        put(maps.Flo, p.Flo, p.lda, 128, 2);
+        put(maps.L[0], p.L[0], p.lda, 128, 2);
+        put(maps.L[1], p.L[1], p.lda, 128, 2);
         if (p.nt_a == 64) put(maps.ba_lo, p.lo, p.ldx, 64, 2); else same(maps.ba_lo, maps.lo);
         if (p.nt_x == 64) put(maps.bx_lo, p.lo, p.ldx, 128, 1); else same(maps.bx_lo, maps.lo);
-        if (p.nt_s == 64) put(maps.bs_lo, p.Elo, p.lda, 64, 2); else same(maps.bs_lo, maps.Elo);
+        if (p.nt_s == 64) put(maps.bs_lo, p.L[0], p.lda, 64, 2); else same(maps.bs_lo, maps.L[0]);
     } else {                                    // not read
-        for (CUtensorMap* m : {&maps.lo, &maps.Elo, &maps.Flo, &maps.ba_lo, &maps.bx_lo, &maps.bs_lo}) same(*m, maps.E);
+        for (CUtensorMap* m : {&maps.lo, &maps.L[0], &maps.L[1], &maps.ba_lo, &maps.bx_lo, &maps.bs_lo}) same(*m, maps.H[0]);
     }
     if (st != DR_OK) return st;
     if (!ns_attributes()) return DR_ERR_CUDA;

@@ -86,7 +86,7 @@ def test_orthogonalise(dr, b, r, c, f32):
     assert torch.equal(o, again), "not the same on a second run"
 
 
-@pytest.mark.parametrize("r,c", [(1000, 2048), (2048, 1500), (1536, 1536)])
+@pytest.mark.parametrize("r,c", [(1000, 2048), (2048, 1500), (1536, 1536), (1100, 2305), (4100, 1040)])
 def test_orthogonalise_large(dr, r, c):
     """Sizes at which every processor has several tiles."""
     g = gradient(f"nsl{r}.{c}", (1, r, c))
@@ -94,9 +94,10 @@ def test_orthogonalise_large(dr, r, c):
     close(o.double().cpu().numpy()[0], polynomial(gd[0]))
 
 
-@pytest.mark.parametrize("steps", [1, 2, 3, 7])
-def test_steps_and_coefficients(dr, steps):
-    g = gradient(f"st{steps}", (1, 80, 208))
+@pytest.mark.parametrize("r,c", [(80, 208), (160, 200), (400, 140), (136, 1000)])
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 7])
+def test_steps_and_coefficients(dr, steps, r, c):
+    g = gradient(f"st{steps}", (1, r, c))
     coef = []
     for k in range(steps):
         coef += [3.0 - 0.2 * k, -3.2 + 0.1 * k, 1.2 - 0.05 * k]
