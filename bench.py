@@ -355,8 +355,18 @@ def run_finetune(args):
         torch.cuda.current_stream().wait_stream(gstream)
         wgrad = lambda: dr.dr_conv_wgrad(d, B, hw, hw, x, dz, dw, ws, wg_need)
         fwd = lambda: dr.dr_conv_slim_ws(d, B, hw, hw, x, shadow, b, None, y, None, None, 0)
+        # the alternatives next to the step: the orthogonalised update of the filters, and a layer norm over the output's channels
+        npix, ld = B * ho * ho, k * k * cin
+        mu_ws = torch.empty(dr.dr_orthogonalise_workspace_bytes(1, cout, ld), dtype=torch.uint8, device="cuda")
+        muon = lambda: dr.dr_muon_update(1, cout, ld, w, vw, dw, 1e-6, 0.9, 1e-4, True, 5, None, 1e-7, shadow, mu_ws, mu_ws.numel())
+        gamma, beta = torch.ones(cout, device="cuda"), torch.zeros(cout, device="cuda")
+        mean, rstd = torch.empty(npix, device="cuda"), torch.empty(npix, device="cuda")
+        ln_ws = torch.empty(dr.dr_layernorm_bwd_workspace_bytes(npix, cout), dtype=torch.uint8, device="cuda")
+        norm = lambda: dr.dr_layernorm(npix, cout, y, 0, gamma, beta, 1e-5, dz, 0, mean, rstd)
+        norm_bwd = lambda: dr.dr_layernorm_bwd(npix, cout, yt, 0, y, 0, gamma, mean, rstd, dz, 0, db, db, ln_ws, ln_ws.numel())
         t = {}
-        for what, fn in (("step", step), ("step_graph", graph.replay), ("wgrad", wgrad), ("forward", fwd)):
+        for what, fn in (("step", step), ("step_graph", graph.replay), ("wgrad", wgrad), ("forward", fwd), ("muon", muon), ("layernorm", norm),
+                         ("layernorm_bwd", norm_bwd)):
             ts = []
             for i in range(args.warmup + min(args.steps, 20)):
                 flush.zero_()
@@ -387,6 +397,7 @@ def run_finetune(args):
                         ts.append(a.elapsed_time(e) * 1e3)
                 lib[what] = statistics.median(ts)
         rows.append({"layer": name, "step_us": t["step"], "step_graph_us": t["step_graph"], "forward_us": t["forward"], "wgrad_us": t["wgrad"],
+                     "muon_update_us": t["muon"], "layernorm_us": t["layernorm"], "layernorm_bwd_us": t["layernorm_bwd"],
                      "images_per_s": B / t["step"] * 1e6, "wgrad_tflops": flops / t["wgrad"] * 1e-6,
                      "wgrad_frac": flops / t["wgrad"] * 1e-6 / pk["bf16_tflops"], "forward_tflops": flops / t["forward"] * 1e-6,
                      "loss": float(loss), **lib})
