@@ -60,7 +60,10 @@ struct NsParams {
     int* status;
 };
 
+enum { NS_A, NS_S, NS_X };
+struct NsItem { int i, j, k0, k1, split, tile; };
 struct NsShared {
+    NsItem first[3];            // the CTA's first tile of each phase: found once, its divisions took 0.3 us of every phase
     uint64_t full[NS_STAGES], empty[NS_STAGES], tfull[2], tempty[2];
     uint32_t tmem_base;
     int abort;
@@ -92,8 +95,6 @@ __device__ __forceinline__ void ns_tri_tile(int t, int n, int tr, int nt, int& i
     j = t;
 }
 
-enum { NS_A, NS_S, NS_X };
-struct NsItem { int i, j, k0, k1, split, tile; };
 template <int PHASE, bool PAIR>
 __device__ __forceinline__ NsItem ns_item(const NsParams& p, int item) {
     NsItem it;
@@ -263,7 +264,7 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             bool ok = true;
             uint32_t ready = mbar_test_u32(empty0 + 8 * pipe.stage, pipe.phase ^ 1);
             for (int item = first; item < items && ok; item += step) {
-                const NsItem it = ns_item<PHASE, PAIR>(p, item);
+                const NsItem it = item == first ? sh.first[PHASE] : ns_item<PHASE, PAIR>(p, item);
                 const int ar = it.i * p.tr + side * 128, bc = it.j * nt + side * (nt / 2);
                 for (int term = 0; term < p.terms && ok; ++term) {
                     const CUtensorMap* am = term == 2 ? al : ah;
@@ -297,7 +298,7 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             const uint32_t b_chunk = (uint32_t)nt * 128u >> 4;      // 64 deep in K: a chunk of B's rows
             bool ok = true;
             for (int item = first; item < items && ok; item += step) {
-                const NsItem it = ns_item<PHASE, PAIR>(p, item);
+                const NsItem it = item == first ? sh.first[PHASE] : ns_item<PHASE, PAIR>(p, item);
                 if (!mbar_wait_u32(tempty0 + 8 * pipe.acc, pipe.acc_phase ^ 1, abort_flag)) {
                     if (!*abort_flag) report_timeout(p.status, 72, item);
                     *abort_flag = 1;
@@ -340,7 +341,7 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
         const size_t mat = (size_t)group * p.n * p.lda, xm = (size_t)group * p.n * p.ldx;
         const size_t dg = (size_t)group * p.lda;
         for (int item = first; item < items; item += step) {
-            const NsItem it = ns_item<PHASE, PAIR>(p, item);
+            const NsItem it = item == first ? sh.first[PHASE] : ns_item<PHASE, PAIR>(p, item);
             const int row = it.i * p.tr + side * 128 + q * 32 + lane;
             // Chunks of 16 columns (8 in the n x n products, which need more of each), alternating between the two warps of a quarter.  What a
             // chunk needs from memory is requested a chunk ahead, the first one's before the product is waited for.
@@ -620,6 +621,12 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     if (PAIR) cluster_sync_all();               // both CTAs' barriers exist before any remote arrive
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
+    if (threadIdx.x == 0) {
+        const int unit = PAIR ? rank >> 1 : rank;
+        if (unit < p.tiles_a * p.splits) sh.first[NS_A] = ns_item<NS_A, PAIR>(p, unit);
+        if (unit < p.tiles_s) sh.first[NS_S] = ns_item<NS_S, PAIR>(p, unit);
+        if (unit < p.tiles_x) sh.first[NS_X] = ns_item<NS_X, PAIR>(p, unit);
+    }
     NsPipe pipe;
     unsigned epoch = 0;
     // the columns that pad the n x n matrices to whole chunks take part in the products: zero (X's are zeroed where it is loaded)
@@ -670,6 +677,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
                     const int row = i * 128 + (rem & 3) * 32 + lane, c = (rem >> 2) * 8;
                     const float* in = p.part + ((size_t)group * p.splits * p.tiles_a + t) * nt * 128 + (size_t)c * 128 + (rem & 3) * 32 + lane;
                     alignas(32) float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
                     for (int q = 0; q < p.splits; ++q)
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[e] += in[(size_t)q * p.tiles_a * nt * 128 + e * 128];
