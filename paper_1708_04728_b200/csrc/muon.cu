@@ -598,6 +598,12 @@ __device__ __forceinline__ void ns_convert(const NsParams& p, float* tile, int g
     }
 }
 
+__device__ __forceinline__ uint32_t cluster_ctas() {
+    uint32_t n;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+    return n;
+}
+
 template <bool PAIR>
 __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsParams p) {
     extern __shared__ uint8_t ns_smem_raw[];
@@ -606,6 +612,11 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     float* tile = reinterpret_cast<float*>(ns_smem_raw + (smem - smem_u32(ns_smem_raw)));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = blockIdx.x / p.G, rank = blockIdx.x - group * p.G;
+    // A launch that lost its cluster size (a profiler that replays a cooperative launch, say) must not reach an instruction for CTA pairs.
+    if (PAIR && cluster_ctas() != 2) {
+        if (threadIdx.x == 0) report_timeout(p.status, 77, 0);
+        return;
+    }
     if (threadIdx.x == 0) {
         for (int i = 0; i < NS_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], PAIR ? 1 : 2); mbar_init(&sh.tempty[i], PAIR ? 16 : 8); }
