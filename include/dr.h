@@ -400,8 +400,11 @@ int dr_layernorm_bwd(size_t npix, int C, const void* dy, int lddy, const void* x
  *  coef: NULL (a, b, c = 3.4445, -4.7750, 2.0315 in every step), or 3 * steps host floats, read before the call returns.
  *  steps <= DR_NS_MAX_STEPS, rows and cols <= DR_NS_MAX_DIM, batch <= 65535.
  *  The products take operands of 11 significant bits (the term a X and the diagonals of A and of b A + c A A: 22 or
- *  more) and sum in float32: the relative error of O is below 1e-3, under half of its rounding to bfloat16.
- *  The values of A and of the polynomial must stay below 65504: with coefficients that let X grow past that, O is not finite.
+ *  more; all of them where min(rows, cols) <= 64) and sum in float32.  Relative error of O (Frobenius, before it is
+ *  rounded to bfloat16): 1e-4 .. 1e-3 for random matrices, up to 4e-3 where the singular values of U spread over many
+ *  decades or its rank is low; below 1e-4 where min(rows, cols) <= 64.
+ *  X is kept in float16 times 4096, A and the polynomial in float16: with coefficients that let a singular value of X reach
+ *  16, or an entry of the others 65504, O is not finite.
  *  An all-zero U gives zeros (eps > 0); a matrix with a NaN or an infinity gives NaN and touches no other matrix.
  * dr_orthogonalise: g bfloat16, or float32 with DR_NS_G_F32; o bfloat16; both [batch][rows][cols].
  *  workspace: dr_orthogonalise_workspace_bytes bytes, 256-byte aligned, contents irrelevant; calls that may overlap on

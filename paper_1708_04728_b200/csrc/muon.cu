@@ -9,7 +9,8 @@
 //  - A is split into its diagonal and the rest, A = D + E, D in float32:
 //      A A = E E + D E + E D + D D,  so only E, small where X is nearly orthogonal, is rounded (and only for E E);
 //    likewise the polynomial b A + c A A = diag + F:  X <- (a + diag) X + F X with a row factor in float32.
-//    With the whole of A in float16 the relative error of O is 2e-3 .. 4e-3 (random matrices); with the split 2e-4 .. 1e-3.
+//    With the whole of A in float16 the relative error of O is 2e-3 .. 4e-3 (random matrices); with the split 1e-4 .. 6e-4, and
+//    1.3e-3 (512 rows) .. 2.2e-3 (96 rows) at most for spectra over up to six decades and matrices of rank 4.
 //  - Products symmetric by construction (A, E E) are computed for the lower triangle and mirrored, so they stay symmetric.
 // bfloat16 operands would cost 2e-3 .. 6e-3 even so: more than the rounding of O to bfloat16 itself.
 //
@@ -18,6 +19,14 @@
 // pipeline: one warp loads 128-deep operand slices by TMA, two issue tcgen05.mma into one of two sets of accumulators in
 // tensor memory, eight drain the other one.  A group of up to 16 CTAs is a thread-block cluster and uses its barrier; a larger one is
 // launched cooperatively and counts arrivals in global memory.
+//
+// Measured on a B200, five steps; flops of the formula with A and A A by their lower triangles, against 1650 TFLOP/s of a bfloat16 product:
+//   4096 x 9216   2.07 .. 2.4 ms (the clock falls with the power drawn), 0.78 .. 0.67 of that rate; the plain form in float32 takes
+//                 62.7 ms.  Bound by the tensor pipe and by whole rounds of tiles.
+//   2048 x 2048   337 us, 0.31: 64 tiles of 256 x 256 for 74 pairs, drains of 8 us behind MMAs of 10.
+//   1000 x 2048   174 us, 512 x 13200 with the optimiser's step 256 us, 512 x 2048 132 us, 6 x 256 x 2304 168 us, 192 x 576 101 us: 15 dependent
+//                 phases of 6 to 20 us each.  A phase is a barrier 1.3 .. 1.9 us, 0.5 .. 1 to its first MMA's operands, 0.8 of TMA latency, the MMAs, and
+//                 a drain of 1.3 .. 3; where all SMs load operands, the way out of L2 (12 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -28,7 +37,7 @@ namespace dr {
 
 constexpr int NS_THREADS = 384;             // warp 0: TMA, warps 1 and 2: MMA, warps 4 - 11: drain, two for each quarter of the accumulator's rows
 constexpr int NS_STAGES = 8;                // at most
-constexpr int NS_SMEM = 196608;             // operand ring; also keeps every SM to one CTA, which owns all its tensor memory
+constexpr int NS_SMEM = NS_SMEM_ALL - 1024; // operand ring
 constexpr int NS_CHUNK = 128 * 128;          // 128 rows x 64 float16
 // 64-column chunks a stage is deep in the contraction: 2, since the issuing threads take 400 cycles to hand a stage over; 1 where two
 // CTAs share tiles of 256 x 256, whose MMAs take longer than that and want more stages of the same bytes (1.24 against 1.35 ms at 4096 x 4096)
@@ -730,8 +739,8 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
 static bool ns_attributes() {
     static PerDeviceFlag attr_set;
     if (attr_set.get()) return true;
-    if (cudaFuncSetAttribute(ns_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM + 1024) != cudaSuccess ||
-        cudaFuncSetAttribute(ns_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM + 1024) != cudaSuccess ||
+    if (cudaFuncSetAttribute(ns_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
         cudaFuncSetAttribute(ns_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
         (void)cudaGetLastError();
         return false;
@@ -763,7 +772,7 @@ static int ns_max_cluster() {
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim.x = c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        cfg.gridDim = dim3(c); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM + 1024; cfg.attrs = attr; cfg.numAttrs = 1;
+        cfg.gridDim = dim3(c); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM_ALL; cfg.attrs = attr; cfg.numAttrs = 1;
         int n = 0;
         if (ns_attributes() && cudaOccupancyMaxActiveClusters(&n, ns_kernel<false>, &cfg) == cudaSuccess && n > 0) break;
         (void)cudaGetLastError();
@@ -945,7 +954,7 @@ static int ns_run(int batch, NsInput in, int steps, const float* coef, char* ws,
     }
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
-    cfg.gridDim = dim3((unsigned)(p.groups * p.G)); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM + 1024; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)(p.groups * p.G)); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM_ALL; cfg.stream = s;
     cfg.attrs = attr;
     if (counted) {
         attr[0].id = cudaLaunchAttributeCooperative;

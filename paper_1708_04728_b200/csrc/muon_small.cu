@@ -10,7 +10,11 @@
 //   F    every CTA computes E E (E: A without its diagonal) and the polynomial for itself,
 //   X    every CTA updates its slab in place.
 // Products and element-wise terms as in the kernel for larger matrices (muon.cu); with few rows rounding errors average less, so
-// matrices of up to 64 rows multiply hi hi + hi lo + lo hi: the tensor cores idle here either way.
+// matrices of up to 64 rows multiply hi hi + hi lo + lo hi: the tensor cores idle here either way (relative error of O 1e-6 .. 3e-5).
+//
+// Measured on a B200, five steps: 64 x 147 47 us (49 us with the optimiser's momentum and update; 3 products of 0.6 us, two roundings to pairs
+// and three block barriers a step), 128 x 864 60 us, 27 x 96 x 800 with the optimiser 76 .. 98 us.  At 128 x 864 the tensor pipe is busy 5 % of the
+// time and 41 % of the issue slots are taken: a step of 11 us is a chain of element-wise passes over E and X between MMAs of under a microsecond.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -21,11 +25,8 @@ namespace dr {
 
 constexpr int NSS_THREADS = 512;           // 16 warps: four share the 32 accumulator rows that each of them can read
 constexpr int NSS_CHUNK = 128 * 128;        // 64 columns of 128 rows
-// Shared memory, in chunks: X (hi, lo) as wide as the slab, E (hi, lo) as wide as n.  Always asked for in full: one CTA per SM.  A second one
-// there would wait for the first one's tensor memory, and the first, at a cluster barrier, for the second.
-constexpr int NSS_CHUNKS = 12;
-constexpr int NSS_SMEM = NSS_CHUNKS * NSS_CHUNK + 1024;
-static_assert(NSS_SMEM > 114 * 1024, "two CTAs must not fit an SM");
+constexpr int NSS_CHUNKS = 12;             // of shared memory: X (hi, lo) as wide as the slab, E (hi, lo) as wide as n
+static_assert(NSS_CHUNKS * NSS_CHUNK + 1024 <= NS_SMEM_ALL, "");
 
 struct NsSmall {
     NsInput in;
@@ -429,7 +430,7 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
 static bool nss_attributes() {
     static PerDeviceFlag attr_set;
     if (attr_set.get()) return true;
-    if (cudaFuncSetAttribute(ns_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NSS_SMEM) != cudaSuccess ||
+    if (cudaFuncSetAttribute(ns_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
         cudaFuncSetAttribute(ns_small_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
         (void)cudaGetLastError();
         return false;
@@ -450,7 +451,7 @@ static int nss_clusters(int ctas) {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(NSS_THREADS); cfg.dynamicSmemBytes = NSS_SMEM; cfg.attrs = attr; cfg.numAttrs = 1;
+    cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(NSS_THREADS); cfg.dynamicSmemBytes = NS_SMEM_ALL; cfg.attrs = attr; cfg.numAttrs = 1;
     if (!nss_attributes() || cudaOccupancyMaxActiveClusters(&n, ns_small_kernel, &cfg) != cudaSuccess || n < 0) {
         (void)cudaGetLastError();
         n = num_sms() / ctas;                   // no device to ask
@@ -500,7 +501,7 @@ int ns_small_run(const NsSmallPlan& plan, int batch, const NsInput& in, int step
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = p.G; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)(p.groups * p.G)); cfg.blockDim = dim3(NSS_THREADS); cfg.stream = stream;
-    cfg.dynamicSmemBytes = NSS_SMEM;
+    cfg.dynamicSmemBytes = NS_SMEM_ALL;
     cfg.attrs = attr; cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, ns_small_kernel, p) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
     count_launch();
