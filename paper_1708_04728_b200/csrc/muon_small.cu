@@ -56,6 +56,11 @@ __device__ __forceinline__ void nss_ld(const uint8_t* base, int row, int unit, u
 __device__ __forceinline__ void nss_st(uint8_t* base, int row, int unit, const uint32_t* u) {
     *reinterpret_cast<uint4*>(base + nss_at(row, unit)) = make_uint4(u[0], u[1], u[2], u[3]);
 }
+// and the same again 64 rows on
+__device__ __forceinline__ void nss_st_rows(uint8_t* base, int row, int unit, const uint32_t* u, bool twice) {
+    nss_st(base, row, unit, u);
+    if (twice) nss_st(base + 64 * 128, row, unit, u);
+}
 
 // A CTA's slab in the user's memory, 8 columns at a time (16-byte accesses) or, where rows are not aligned or U is tall, element by element:
 // a warp takes one of the user's rows after the other (tall: one of X's columns), so that no index needs a division.
@@ -184,7 +189,13 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
     const int kc = (p.n + 63) / 64, elo = kc * NSS_CHUNK;              // chunks of an n x n operand
     uint8_t* const E = X + e_at;                                       // E, later F: hi, then lo
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const int q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+    // A warp reads 32 of the accumulators' 128 rows, and warps whose rows are the same modulo 128 share a quarter of the SM.  Matrices of up to 64
+    // rows fill only half of that, so theirs are held twice, as rows 0 .. 63 and 64 .. 127 of the first operands: all warps have rows, and
+    // half as many columns of them (64 x 147: 47 -> 41 us).
+    const bool twice = p.n <= 64;
+    const int q = warp & 3, row = (twice ? q & 1 : q) * 32 + lane;
+    const int first = ((warp >> 2) + (twice ? q >> 1 << 2 : 0)) * 8, stride = twice ? 64 : 32;      // a warp's columns: 8 from here, 8 a stride on
+    const bool has_rows = row - lane < p.n;
     const int group = blockIdx.x / p.G, rank = blockIdx.x - group * p.G;
     const int c0 = rank * p.chunks * 64, units = p.chunks * 8;         // the slab: first column, 8-column units
     volatile int* abort_flag = &sh.abort;
@@ -268,8 +279,8 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
                 f[4 + k] = __uint_as_float(l[k]) * inv;
             }
             ns_split<8>(f, h, l);
-            nss_st(X, i, w, h);
-            nss_st(X + xlo, i, w, l);
+            nss_st_rows(X, i, w, h, twice);
+            nss_st_rows(X + xlo, i, w, l, twice);
         }
         for (int step = 0; step < p.steps; ++step) {
             const float ca = p.coef[3 * step], cb = p.coef[3 * step + 1], cc = p.coef[3 * step + 2];
@@ -278,34 +289,32 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
                 for (int t = 0; t < p.terms; ++t) product(acc_a, smem + (t == 2 ? xlo : 0), smem + (t == 1 ? xlo : 0), p.chunks, kc * 64, t > 0);
             });
             float* const part = p.part + (size_t)group * p.G * p.n * 128;
-            if (q * 32 < p.n)
-                for (int c = half * 16; c < p.n; c += 64) {
-                    uint32_t raw[16];
+            if (has_rows)
+#pragma unroll 1
+                for (int c = first; c < p.n; c += stride) {
+                    uint32_t raw[8];
                     __syncwarp();
-                    tmem_ld_x16(acc_a + c + ((uint32_t)(q * 32) << 16), raw);
+                    tmem_ld_x8(acc_a + c + ((uint32_t)(q * 32) << 16), raw);
                     tmem_ld_wait();
-                    float v[16];
+                    float v[8];
 #pragma unroll
-                    for (int t = 0; t < 16; ++t) v[t] = __uint_as_float(raw[t]) * (1.f / (NS_SCALE * NS_SCALE));
+                    for (int t = 0; t < 8; ++t) v[t] = __uint_as_float(raw[t]) * (1.f / (NS_SCALE * NS_SCALE));
                     if (p.G > 1) {
 #pragma unroll
-                        for (int t = 0; t < 16; ++t)
+                        for (int t = 0; t < 8; ++t)
                             if (c + t < p.n) part[(size_t)rank * p.n * 128 + (c + t) * 128 + row] = v[t];
                     } else if (row < p.n) {
                         float d = 0.f;
 #pragma unroll
-                        for (int t = 0; t < 16; ++t) {
+                        for (int t = 0; t < 8; ++t) {
                             d = c + t == row ? v[t] : d;
                             v[t] = c + t == row ? 0.f : v[t];
                         }
-                        if (row >= c && row < c + 16) sh.d[row] = d;
-                        uint32_t h[8], l[8];
-                        ns_split<16>(v, h, l);
-#pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            nss_st(E, row, c / 8 + w, h + 4 * w);
-                            nss_st(E + elo, row, c / 8 + w, l + 4 * w);
-                        }
+                        if (row >= c && row < c + 8) sh.d[row] = d;
+                        uint32_t h[4], l[4];
+                        ns_split<8>(v, h, l);
+                        nss_st_rows(E, row, c / 8, h, twice);
+                        nss_st_rows(E + elo, row, c / 8, l, twice);
                     }
                 }
             if (p.G > 1) {
@@ -341,7 +350,10 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
 #pragma unroll 4
                 for (int u = threadIdx.x; u < p.n * n8 * 2; u += NSS_THREADS) {
                     const int j = u / (n8 * 2), w = u - j * (n8 * 2);
-                    *reinterpret_cast<uint4*>(E + (w & 1 ? elo : 0) + nss_at(j, w >> 1)) = sums[u];
+                    const uint4 v = sums[u];
+                    uint8_t* const to = E + (w & 1 ? elo : 0) + nss_at(j, w >> 1);
+                    *reinterpret_cast<uint4*>(to) = v;
+                    if (twice) *reinterpret_cast<uint4*>(to + 64 * 128) = v;
                 }
             }
             // E E, then F X; either product updates pairs in shared memory in place: E -> F = (b + c (d_i + d_j)) E + c E E, X -> r X + F X.
@@ -366,49 +378,43 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
                         }
                     }
                 });
-                if (q * 32 >= p.n) continue;
+                if (!has_rows) continue;
                 const float di = sh.d[row], factor = is_x ? sh.rs[row] : fmaf(cc, di, cb), fd = is_x ? 0.f : cc, beta = is_x ? 1.f : cc;
                 uint8_t* const at = is_x ? X : E;
                 const int lo = is_x ? xlo : elo, width = is_x ? p.chunks * 64 : p.n;
                 const uint32_t acc = (is_x ? acc_x : acc_a) + ((uint32_t)(q * 32) << 16);
 #pragma unroll 1
-                for (int c = half * 16; c < width; c += 64) {
-                    uint32_t raw[16], h[8], l[8];
+                for (int c = first; c < width; c += stride) {
+                    uint32_t raw[8], h[4], l[4];
                     __syncwarp();
-                    tmem_ld_x16(acc + c, raw);
+                    tmem_ld_x8(acc + c, raw);
+                    nss_ld(at, row, c / 8, h);
+                    nss_ld(at + lo, row, c / 8, l);
+                    float dj[8], v[8];
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        nss_ld(at, row, c / 8 + w, h + 4 * w);
-                        nss_ld(at + lo, row, c / 8 + w, l + 4 * w);
-                    }
-                    float dj[16], v[16];
-#pragma unroll
-                    for (int t = 0; t < 16; t += 4) {
+                    for (int t = 0; t < 8; t += 4) {
                         const float4 x = *reinterpret_cast<const float4*>(&sh.d[(c & 127) + t]);
                         dj[t] = x.x; dj[t + 1] = x.y; dj[t + 2] = x.z; dj[t + 3] = x.w;
                     }
                     tmem_ld_wait();
 #pragma unroll
-                    for (int t = 0; t < 16; ++t) {
+                    for (int t = 0; t < 8; ++t) {
                         const float2 fh = half2_at(h[t / 2]), fl = half2_at(l[t / 2]);
                         v[t] = fmaf(is_x ? factor : fmaf(fd, dj[t], factor), t & 1 ? fh.y + fl.y : fh.x + fl.x, beta * __uint_as_float(raw[t]));
                     }
-                    if (!is_x) {                // selects, one store: sixteen branches of one lane each took 1.3 us
+                    if (!is_x) {                // selects, one store: branches of one lane each took 1.3 us a step
                         float sq = 0.f;
 #pragma unroll
-                        for (int t = 0; t < 16; ++t) {
+                        for (int t = 0; t < 8; ++t) {
                             sq = c + t == row ? __uint_as_float(raw[t]) : sq;
                             v[t] = c + t == row || c + t >= p.n ? 0.f : v[t];
                         }
-                        if (row >= c && row < c + 16 && row < p.n) sh.rs[row] = ca + fmaf(cb, di, cc * fmaf(di, di, sq));
+                        if (row >= c && row < c + 8 && row < p.n) sh.rs[row] = ca + fmaf(cb, di, cc * fmaf(di, di, sq));
                     }
                     if (row < p.n) {
-                        ns_split<16>(v, h, l);
-#pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            nss_st(at, row, c / 8 + w, h + 4 * w);
-                            nss_st(at + lo, row, c / 8 + w, l + 4 * w);
-                        }
+                        ns_split<8>(v, h, l);
+                        nss_st_rows(at, row, c / 8, h, twice);
+                        nss_st_rows(at + lo, row, c / 8, l, twice);
                     }
                 }
             }
