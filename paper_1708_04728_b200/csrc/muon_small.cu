@@ -17,7 +17,7 @@
 // time and 41 % of the issue slots are taken: a step of 11 us is a chain of element-wise passes over E and X between MMAs of under a microsecond.
 #include <algorithm>
 #include <cmath>
-#include <mutex>
+#include <initializer_list>
 
 #include "muon_common.cuh"
 
@@ -62,38 +62,35 @@ __device__ __forceinline__ void nss_st_rows(uint8_t* base, int row, int unit, co
     if (twice) nss_st(base + 64 * 128, row, unit, u);
 }
 
-// A CTA's slab in the user's memory, 8 columns at a time (16-byte accesses) or, where rows are not aligned or U is tall, element by element:
-// a warp takes one of the user's rows after the other (tall: one of X's columns), so that no index needs a division.
-struct NssPlace { int i, c; size_t at; bool ok; };           // row and column in the slab, place in the user's matrix
+// A CTA's slab in the user's memory, element by element (CN = 1) or, where rows are aligned and U is not tall, 8 columns at a time in 16-byte
+// accesses.  Elements are taken as they lie in memory, across the ends of rows, so that every thread's rounds are full: row by row to
+// the warps, the input of 64 x 147 took 6 us; like this 64 x 147 takes 39 instead of 43 us and 128 x 865 62 instead of 72.
+struct NssPlace { int i, c, at; bool ok; };              // row and column in the slab, place in the user's matrix
 template <int CN>
 struct NssWalk {
-    int rows, len, r, x, per;
-    __device__ __forceinline__ NssWalk(const NsSmall& p) {
-        per = p.chunks * 64 / CN;
-        rows = CN == 1 ? (p.in.tall ? per : p.n) : 1;
-        len = CN == 1 ? (p.in.tall ? p.n : per) : p.n * per;
-        r = CN == 1 ? threadIdx.x >> 5 : 0;
-        x = CN == 1 ? threadIdx.x & 31 : threadIdx.x;
-        if (CN == 8 && x >= len) r = rows;
+    static constexpr int U = CN == 1 ? 10 : 2;              // places whose loads go out together
+    int x, end, inner, start, skip;
+    float inv;
+    __device__ __forceinline__ NssWalk(const NsSmall& p, int c0) {
+        const int width = max(min(p.m - c0, p.chunks * 64), 0);
+        inner = CN == 8 ? p.chunks * 8 : p.in.tall ? p.n : width;
+        x = threadIdx.x;
+        end = CN == 8 ? p.n * inner : p.n * width;
+        inv = 1.f / (float)inner;
+        start = p.in.tall ? c0 * p.n : c0;
+        skip = (p.in.tall ? p.n : p.in.cols) - inner;       // from one of the user's rows to the next (CN = 1)
     }
-    static constexpr int U = CN == 1 ? 8 : 2, STEP = CN == 1 ? 32 : NSS_THREADS;        // places whose loads go out together
-    __device__ __forceinline__ bool more() const { return r < rows; }
-    __device__ __forceinline__ void next() {
-        x += U * STEP;
-        if (CN == 8) {
-            if (x >= len) r = rows;
-        } else if (x - (int)(threadIdx.x & 31) >= len) {
-            r += NSS_THREADS / 32;
-            x = threadIdx.x & 31;
-        }
-    }
+    __device__ __forceinline__ bool more() const { return x < end; }
+    __device__ __forceinline__ void next() { x += U * NSS_THREADS; }
     __device__ __forceinline__ bool get(const NsSmall& p, int k, int c0, NssPlace& t) const {
-        const int y = x + k * STEP;
-        if (CN == 8) { t.i = y / per; t.c = (y - t.i * per) * CN; }
-        else { t.i = p.in.tall ? y : r; t.c = p.in.tall ? r : y; }
-        t.at = CN == 1 && p.in.tall ? (size_t)(c0 + t.c) * p.in.cols + t.i : (size_t)t.i * p.in.cols + c0 + t.c;
-        t.ok = y < len && c0 + t.c < p.m;
-        return y < len;
+        const int e = x + k * NSS_THREADS;
+        // at most 32768 elements, rows of at most 256: the quotient is 0.5 / 256 or more from a whole number, its rounding error below 2^-15
+        const int r = (int)(((float)e + 0.5f) * inv), y = e - r * inner;
+        t.i = CN == 1 && p.in.tall ? y : r;
+        t.c = CN == 1 && p.in.tall ? r : y * CN;
+        t.at = start + (CN == 1 ? e + r * skip : t.i * p.in.cols + t.c);
+        t.ok = e < end && c0 + t.c < p.m;
+        return e < end;
     }
 };
 // v <- momentum v + g; U waits in the place of X, 16 bytes of a unit of 8 columns where its hi half goes and 16 where the lo half goes.
@@ -104,7 +101,7 @@ __device__ __forceinline__ double nss_load(const NsSmall& p, uint8_t* X, int xlo
     const NsInput& in = p.in;
     double s = 0.;
 #pragma unroll 1
-    for (NssWalk<CN> walk(p); walk.more(); walk.next()) {
+    for (NssWalk<CN> walk(p, c0); walk.more(); walk.next()) {
         alignas(16) float f[U][CN], v[U][CN];
         NssPlace t[U];
         bool mine[U];
@@ -146,7 +143,7 @@ __device__ __forceinline__ void nss_store(const NsSmall& p, const uint8_t* X, in
     constexpr int U = NssWalk<CN>::U;
     const NsInput& in = p.in;
 #pragma unroll 1
-    for (NssWalk<CN> walk(p); walk.more(); walk.next()) {
+    for (NssWalk<CN> walk(p, c0); walk.more(); walk.next()) {
         float f[U][CN], w[U][CN];
         NssPlace t[U];
 #pragma unroll
@@ -180,6 +177,8 @@ __device__ __forceinline__ void nss_store(const NsSmall& p, const uint8_t* X, in
     }
 }
 
+// CN: how U is read and the result written, as in NssWalk (a kernel each: the registers of one for both cost every shape 2 to 4 us).
+template <int CN>
 __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_constant__ NsSmall p) {
     extern __shared__ uint8_t nss_raw[];
     __shared__ NsSmallShared sh;
@@ -251,8 +250,17 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
 
     for (int b = group; b < p.batch; b += p.groups) {
         const size_t base = (size_t)b * p.n * p.m;
-        const bool wide = p.in.vec && !p.in.tall;
-        double s = wide ? nss_load<8>(p, X, xlo, c0, base) : nss_load<1>(p, X, xlo, c0, base);
+        if (CN == 1 && b != group) {   // columns past m: zero again, whatever the matrix before left there
+            for (int i = threadIdx.x; i < p.n * units; i += NSS_THREADS) {
+                const int r = i / units, w = i - r * units;
+                const uint32_t zero[4] = {0, 0, 0, 0};
+                if (c0 + w * 8 + 8 <= p.m) continue;
+                nss_st(X, r, w, zero);
+                nss_st(X + xlo, r, w, zero);
+            }
+            __syncthreads();
+        }
+        double s = nss_load<CN>(p, X, xlo, c0, base);
         s = ns_warp_sum(s);
         if (lane == 0) sh.red[warp] = s;
         __syncthreads();
@@ -420,8 +428,7 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
             }
         }
         __syncthreads();
-        if (wide) nss_store<8>(p, X, xlo, c0, base);
-        else nss_store<1>(p, X, xlo, c0, base);
+        nss_store<CN>(p, X, xlo, c0, base);
         __syncthreads();                        // X is read before the next matrix takes its place
     }
     if (sh.abort) {                             // products in flight end within microseconds; then the CTA may go
@@ -433,14 +440,16 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
     if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
+typedef void (*NssKernel)(const NsSmall);
 static bool nss_attributes() {
     static PerDeviceFlag attr_set;
     if (attr_set.get()) return true;
-    if (cudaFuncSetAttribute(ns_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
-        cudaFuncSetAttribute(ns_small_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return false;
-    }
+    for (NssKernel k : {ns_small_kernel<8>, ns_small_kernel<1>})
+        if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
+            cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return false;
+        }
     attr_set.set();
     return true;
 }
@@ -458,7 +467,7 @@ static int nss_clusters(int ctas) {
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(NSS_THREADS); cfg.dynamicSmemBytes = NS_SMEM_ALL; cfg.attrs = attr; cfg.numAttrs = 1;
-    if (!nss_attributes() || cudaOccupancyMaxActiveClusters(&n, ns_small_kernel, &cfg) != cudaSuccess || n < 0) {
+    if (!nss_attributes() || cudaOccupancyMaxActiveClusters(&n, ns_small_kernel<8>, &cfg) != cudaSuccess || n < 0) {
         (void)cudaGetLastError();
         n = num_sms() / ctas;                   // no device to ask
     }
@@ -509,7 +518,8 @@ int ns_small_run(const NsSmallPlan& plan, int batch, const NsInput& in, int step
     cfg.gridDim = dim3((unsigned)(p.groups * p.G)); cfg.blockDim = dim3(NSS_THREADS); cfg.stream = stream;
     cfg.dynamicSmemBytes = NS_SMEM_ALL;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, ns_small_kernel, p) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+    const NssKernel kernel = in.vec && !in.tall ? ns_small_kernel<8> : ns_small_kernel<1>;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
     count_launch();
     return launch_status();
 }
