@@ -18,13 +18,14 @@
 // A -> F -> X of every step and meets at a barrier between them; a batch is spread over the groups.  Inside a phase a CTA is a
 // pipeline: one warp loads 128-deep operand slices by TMA, two issue tcgen05.mma into one of two sets of accumulators in
 // tensor memory, eight drain the other one.  A group of up to 16 CTAs is a thread-block cluster and uses its barrier; a larger one is
-// launched cooperatively and counts arrivals in global memory.
+// launched cooperatively and counts arrivals in global memory.  Where A has few tiles, its long axis is divided: over the CTAs of a
+// cluster that exchange their parts through each other's shared memory, or over all CTAs with a phase more to sum the parts.
 //
 // Measured on a B200, five steps; flops of the formula with A and A A by their lower triangles, against 1650 TFLOP/s of a bfloat16 product:
 //   4096 x 9216   2.07 .. 2.4 ms (the clock falls with the power drawn), 0.78 .. 0.67 of that rate; the plain form in float32 takes
 //                 62.7 ms.  Bound by the tensor pipe and by whole rounds of tiles.
 //   2048 x 2048   337 us, 0.31: 64 tiles of 256 x 256 for 74 pairs, drains of 8 us behind MMAs of 10.
-//   1000 x 2048   174 us, 512 x 13200 with the optimiser's step 256 us, 512 x 2048 132 us, 6 x 256 x 2304 168 us, 192 x 576 101 us: 15 dependent
+//   1000 x 2048   174 us, 512 x 13200 with the optimiser's step 256 us, 512 x 2048 120 us, 6 x 256 x 2304 161 us, 192 x 576 101 us: 15 dependent
 //                 phases of 6 to 20 us each.  A phase is a barrier 1.3 .. 1.9 us, 0.5 .. 1 to its first MMA's operands, 0.8 of TMA latency, the MMAs, and
 //                 a drain of 1.3 .. 3; where all SMs load operands, the way out of L2 (12 TB/s).
 #include <algorithm>
@@ -53,7 +54,8 @@ struct NsParams {
     int nt_a, nt_s, nt_x;       // tile columns of the three products
     int tiles_a, tiles_s, tiles_x;
     int full_a, full_s;         // whether all tiles of A and of E E are computed, not those of the lower triangle alone
-    int splits;                 // ranges of the long axis in A = X X^T
+    int splits;                 // ranges of the long axis in A = X X^T whose parts meet in global memory, in a phase of its own
+    int share;                  // or CTAs of a cluster that share a tile of it, a range each, and exchange parts through their shared memory
     int merge;                  // whether X takes two steps at a time
     int terms;                  // 1: hi hi;  3: hi hi + hi lo + lo hi
     int stages, stage_bytes;
@@ -70,6 +72,9 @@ struct NsParams {
 };
 
 enum { NS_A, NS_S, NS_X };
+// Kernels: each CTA for itself, CTAs of a cluster that share A's tiles along the long axis, pairs of CTAs that share all tiles.  One kernel for the
+// first two cost either 2 us in registers.
+enum { NS_ALONE, NS_SHARE, NS_PAIR };
 struct NsItem { int i, j, k0, k1, split, tile; };
 struct NsShared {
     NsItem first[3];            // the CTA's first tile of each phase: found once, its divisions took 0.3 us of every phase
@@ -112,6 +117,12 @@ __device__ __forceinline__ NsItem ns_item(const NsParams& p, int item) {
     it.k0 = 0;
     it.k1 = kb;
     it.tile = item;
+    if (PHASE == NS_A && p.share > 1) {
+        it.tile = item / p.share;
+        it.split = item - it.tile * p.share;
+        it.k0 = kb * it.split / p.share;
+        it.k1 = kb * (it.split + 1) / p.share;
+    }
     if (PHASE == NS_A && p.splits > 1) {
         it.split = item / p.tiles_a;
         it.tile = item - it.split * p.tiles_a;
@@ -251,11 +262,12 @@ struct NsPipe {
     __device__ __forceinline__ void next_acc() { if (++acc == 2) { acc = 0; acc_phase ^= 1; } }
 };
 
-template <int PHASE, bool PAIR>
+template <int PHASE, int KIND>
 __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps, NsShared& sh, uint32_t smem, uint32_t tmem, NsPipe& pipe, int group, int rank, int src, const NsTriple triple, const float* coef) {
+    constexpr bool PAIR = KIND == NS_PAIR, SHARE = KIND == NS_SHARE;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int nt = PHASE == NS_A ? p.nt_a : PHASE == NS_S ? p.nt_s : p.nt_x;
-    const int items = PHASE == NS_A ? p.tiles_a * p.splits : PHASE == NS_S ? p.tiles_s : p.tiles_x;
+    const int items = PHASE == NS_A ? p.tiles_a * p.splits * p.share : PHASE == NS_S ? p.tiles_s : p.tiles_x;
     const int first = PAIR ? rank >> 1 : rank, step = PAIR ? p.G >> 1 : p.G, side = PAIR ? rank & 1 : 0;
     const uint32_t full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]), tfull0 = smem_u32(&sh.tfull[0]), tempty0 = smem_u32(&sh.tempty[0]);
     constexpr int D = ns_depth(PAIR);
@@ -408,7 +420,12 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
                 tmem_ld_wait();
 #pragma unroll
                 for (int t = 0; t < CN; ++t) v[t] = !PAIR && two ? __uint_as_float(raw[t]) + __uint_as_float(raw2[t]) : __uint_as_float(raw[t]);
-                if (PHASE == NS_A && p.splits > 1) {
+                if (PHASE == NS_A && SHARE) {
+                    const int cs = nt / p.share, owner = c / cs;
+                    const uint32_t to = mapa_shared(smem + NS_SMEM - nt * 512, (p.cluster ? rank - it.split : 0) + owner) + (uint32_t)((it.split * cs + c - owner * cs) * 128 + q * 32 + lane) * 4;
+#pragma unroll
+                    for (int t = 0; t < CN; ++t) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + t * 512), "f"(v[t]) : "memory");
+                } else if (PHASE == NS_A && !SHARE && p.splits > 1) {
                     float* out = p.part + (((size_t)group * p.splits + it.split) * p.tiles_a + it.tile) * nt * 128 + (size_t)c * 128 + q * 32 + lane;
 #pragma unroll
                     for (int t = 0; t < CN; ++t) out[t * 128] = v[t];
@@ -613,8 +630,9 @@ __device__ __forceinline__ uint32_t cluster_ctas() {
     return n;
 }
 
-template <bool PAIR>
+template <int KIND>
 __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsParams p) {
+    constexpr bool PAIR = KIND == NS_PAIR, SHARE = KIND == NS_SHARE;
     extern __shared__ uint8_t ns_smem_raw[];
     __shared__ NsShared sh;
     const uint32_t smem = (smem_u32(ns_smem_raw) + 1023u) & ~1023u;
@@ -643,7 +661,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     const uint32_t tmem = sh.tmem_base;
     if (threadIdx.x == 0) {
         const int unit = PAIR ? rank >> 1 : rank;
-        if (unit < p.tiles_a * p.splits) sh.first[NS_A] = ns_item<NS_A, PAIR>(p, unit);
+        if (unit < p.tiles_a * p.splits * p.share) sh.first[NS_A] = ns_item<NS_A, PAIR>(p, unit);
         if (unit < p.tiles_s) sh.first[NS_S] = ns_item<NS_S, PAIR>(p, unit);
         if (unit < p.tiles_x) sh.first[NS_X] = ns_item<NS_X, PAIR>(p, unit);
     }
@@ -685,37 +703,52 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
         int src = 0;
         for (int k = 0; k < p.steps; src ^= 1) {
             const bool two = p.merge && k + 1 < p.steps;
-            ns_product<NS_A, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, NsTriple{}, nullptr);
-            ns_group_sync(p, sh, group, epoch);
-            if (p.splits > 1) {
-                // the ranges' parts of A in order: a warp takes 32 rows x 8 columns
-                const int nt = p.nt_a, units = p.tiles_a * nt / 2;
-                for (int u = rank * (NS_THREADS / 32) + warp; u < units; u += p.G * (NS_THREADS / 32)) {
-                    const int t = u / (nt / 2), rem = u - t * (nt / 2);
-                    int i, j;
-                    ns_tri_tile(t, p.n, 128, nt, i, j);
-                    const int row = i * 128 + (rem & 3) * 32 + lane, c = (rem >> 2) * 8;
-                    const float* in = p.part + ((size_t)group * p.splits * p.tiles_a + t) * nt * 128 + (size_t)c * 128 + (rem & 3) * 32 + lane;
+            ns_product<NS_A, KIND>(p, maps, sh, smem, tmem, pipe, group, rank, src, NsTriple{}, nullptr);
+            if (SHARE || (!PAIR && p.splits > 1)) {
+                // The ranges' parts of A in order: a warp takes 32 rows x 8 columns, of those its CTA owns (share: their parts lie in its shared
+                // memory) or of all.
+                constexpr bool own = SHARE;
+                if (own) cluster_sync_all();
+                else ns_group_sync(p, sh, group, epoch);
+                const int nt = p.nt_a, width = own ? nt / p.share : nt, parts = own ? p.share : p.splits;
+                const int units = own ? (rank < p.tiles_a * p.share ? width / 2 : 0) : p.tiles_a * nt / 2;
+                const size_t apart = own ? width * 128 : (size_t)p.tiles_a * nt * 128;
+                for (int u = own ? warp : rank * (NS_THREADS / 32) + warp; u < units; u += own ? NS_THREADS / 32 : p.G * (NS_THREADS / 32)) {
+                    const int t = u / (width / 2), rem = u - t * (width / 2), r = (rem & 3) * 32 + lane, c = (rem >> 2) * 8;
+                    int i, j, col;
+                    const float* in;
+                    if (own) {
+                        i = sh.first[NS_A].i;
+                        j = sh.first[NS_A].j;
+                        col = j * nt + sh.first[NS_A].split * width + c;
+                        in = tile + (NS_SMEM - nt * 512) / 4;
+                    } else {
+                        ns_tri_tile(t, p.n, 128, nt, i, j);
+                        col = j * nt + c;
+                        in = p.part + ((size_t)group * p.splits * p.tiles_a + t) * nt * 128;
+                    }
+                    const int row = i * 128 + r;
+                    in += (size_t)c * 128 + r;
                     alignas(32) float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-                    for (int q = 0; q < p.splits; ++q)
+                    for (int q = 0; q < parts; ++q, in += apart)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += in[(size_t)q * p.tiles_a * nt * 128 + e * 128];
+                        for (int e = 0; e < 8; ++e) v[e] += in[e * 128];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] *= 1.f / (NS_SCALE * NS_SCALE);
-                    if (row < p.n) ns_emit_a<8>(p, (size_t)group * p.n * p.lda, p.D[0] + (size_t)group * p.lda, false, row, j * nt + c, v);
+                    if (row < p.n && col < p.lda) ns_emit_a<8>(p, (size_t)group * p.n * p.lda, p.D[0] + (size_t)group * p.lda, p.full_a, row, col, v);
                 }
-                ns_group_sync(p, sh, group, epoch);
             }
+            ns_group_sync(p, sh, group, epoch);
             // A in 0.  One step: Q(A) in 1, X <- Q X.  Two: all factors are polynomials of A and commute, so the second step's A is Q A Q:
             // Q(A) in 1, Q A in 2, A' = (Q A) Q in 0, Q'(A') in 2, Q' Q in 0, X <- (Q' Q) X.
 #pragma unroll 1
             for (int j = 0; j < (two ? 5 : 1); ++j) {
                 const NsTriple t = j == 0 ? NsTriple{0, 0, 1, 1, two} : j == 1 ? NsTriple{1, 0, 2, 0, 1} : j == 2 ? NsTriple{2, 1, 0, 0, 1} : j == 3 ? NsTriple{0, 0, 2, 1, 1} : NsTriple{2, 1, 0, 0, 0};
-                ns_product<NS_S, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, t, p.coef + 3 * (k + (j == 3)));
+                ns_product<NS_S, KIND>(p, maps, sh, smem, tmem, pipe, group, rank, src, t, p.coef + 3 * (k + (j == 3)));
                 ns_group_sync(p, sh, group, epoch);
             }
-            ns_product<NS_X, PAIR>(p, maps, sh, smem, tmem, pipe, group, rank, src, NsTriple{two ? 0 : 1, 0, 0, 0, 0}, nullptr);
+            ns_product<NS_X, KIND>(p, maps, sh, smem, tmem, pipe, group, rank, src, NsTriple{two ? 0 : 1, 0, 0, 0, 0}, nullptr);
             ns_group_sync(p, sh, group, epoch);
             k += two ? 2 : 1;
         }
@@ -739,9 +772,11 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
 static bool ns_attributes() {
     static PerDeviceFlag attr_set;
     if (attr_set.get()) return true;
-    if (cudaFuncSetAttribute(ns_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
-        cudaFuncSetAttribute(ns_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
-        cudaFuncSetAttribute(ns_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+    if (cudaFuncSetAttribute(ns_kernel<NS_ALONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_kernel<NS_SHARE>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_kernel<NS_PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM_ALL) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_kernel<NS_ALONE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_kernel<NS_SHARE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
         (void)cudaGetLastError();
         return false;
     }
@@ -774,11 +809,30 @@ static int ns_max_cluster() {
         attr[0].val.clusterDim.x = c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         cfg.gridDim = dim3(c); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM_ALL; cfg.attrs = attr; cfg.numAttrs = 1;
         int n = 0;
-        if (ns_attributes() && cudaOccupancyMaxActiveClusters(&n, ns_kernel<false>, &cfg) == cudaSuccess && n > 0) break;
+        if (ns_attributes() && cudaOccupancyMaxActiveClusters(&n, ns_kernel<NS_ALONE>, &cfg) == cudaSuccess && n > 0) break;
         (void)cudaGetLastError();
     }
     slot.store(c, std::memory_order_relaxed);
     return c;
+}
+
+// Clusters of 2 or 4 CTAs the device holds at a time.
+static int ns_clusters(int ctas) {
+    static std::atomic<int> known[64][2];
+    std::atomic<int>& slot = known[PerDeviceFlag::dev()][ctas > 2];
+    int n = slot.load(std::memory_order_relaxed);
+    if (n) return n - 1;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM_ALL; cfg.attrs = attr; cfg.numAttrs = 1;
+    if (!ns_attributes() || cudaOccupancyMaxActiveClusters(&n, ns_kernel<NS_SHARE>, &cfg) != cudaSuccess || n < 0) {
+        (void)cudaGetLastError();
+        n = 0;
+    }
+    slot.store(n + 1, std::memory_order_relaxed);
+    return n;
 }
 
 static NsPlan ns_plan(int batch, int rows, int cols) {
@@ -814,7 +868,7 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     };
     constexpr long long BARRIER = 2500, SPLIT = 10000;          // a barrier; what splitting A adds: parts written, barrier, parts summed
     const int cm = (p.m + 63) / 64, cn = (p.n + 63) / 64;
-    struct Choice { long long a, s, x; int nt_a, nt_s, nt_x, tiles_a, tiles_s, tiles_x, full_a, full_s, splits; };
+    struct Choice { long long a, s, x; int nt_a, nt_s, nt_x, tiles_a, tiles_s, tiles_x, full_a, full_s, splits, share; };
     auto choose = [&](bool pair) {
         Choice c = {};
         const int rows = pair ? rows256 : rows128, tr = pair ? 256 : 128, wide = pair ? 256 : 128, narrow = wide / 2;
@@ -826,11 +880,18 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
             // all tiles of a symmetric product where the group has a CTA for each (no mirrored stores), otherwise those of the lower triangle
             const bool full = !pair && all_n <= g;
             if ((full || nt == wide || pair) && take(c.s, cost(full ? all_n : tri, cn, nt, pair))) { c.nt_s = nt; c.full_s = full; c.tiles_s = full ? all_n : tri; }
-            if (full && take(c.a, cost(all_n, cm, nt, pair))) { c.nt_a = nt; c.full_a = 1; c.tiles_a = all_n; c.splits = 1; }
+            if (full && take(c.a, cost(all_n, cm, nt, pair))) { c.nt_a = nt; c.full_a = 1; c.tiles_a = all_n; c.splits = c.share = 1; }
+            // Few tiles: a cluster's CTAs share each, a range of the long axis a CTA (one SM's operands arrive at 70 bytes a cycle, whatever the
+            // others do: 512 x 2048 129.5 -> 119.5 us, 256 x 2304 123 -> 107 us, but 1000 x 2048, which fills the SMs, 174 -> 191 us).  A CTA drains
+            // its share of the columns; the exchange is a cluster barrier and the columns' way.
+            for (int k = 2; !pair && k <= 4; k *= 2) {
+                if (!full || all_n * k > g || g % k || cm < 2 * k || (!p.cluster && ns_clusters(k) * k < p.groups * g)) continue;
+                if (take(c.a, cost(all_n * k, (cm + k - 1) / k, nt, false) - 60 * nt * (k - 1) / k + 1500 + 32 * nt)) { c.nt_a = nt; c.full_a = 1; c.tiles_a = all_n; c.splits = 1; c.share = k; }
+            }
             if (nt == wide || pair) {
                 // or the lower triangle with the long axis split over the CTAs, whose parts meet after another barrier
                 const int s = pair ? 1 : std::max(1, std::min(g / tri, cm / 4));
-                if (take(c.a, cost(tri * s, (cm + s - 1) / s, nt, pair) + (s > 1 ? SPLIT : 0))) { c.nt_a = nt; c.full_a = 0; c.tiles_a = tri; c.splits = s; }
+                if (take(c.a, cost(tri * s, (cm + s - 1) / s, nt, pair) + (s > 1 ? SPLIT : 0))) { c.nt_a = nt; c.full_a = 0; c.tiles_a = tri; c.splits = s; c.share = 1; }
             }
         }
         return c;
@@ -843,9 +904,9 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     p.tr = p.pair ? 256 : 128;
     p.nt_a = c.nt_a; p.nt_s = c.nt_s; p.nt_x = c.nt_x;
     p.tiles_a = c.tiles_a; p.tiles_s = c.tiles_s; p.tiles_x = c.tiles_x;
-    p.full_a = c.full_a; p.full_s = c.full_s; p.splits = c.splits;
+    p.full_a = c.full_a; p.full_s = c.full_s; p.splits = c.splits; p.share = c.share;
     p.stage_bytes = ns_depth(p.pair) * (NS_CHUNK + std::max(p.nt_x, std::max(p.nt_s, p.nt_a)) * (p.pair ? 64 : 128));
-    p.stages = std::min(NS_STAGES, NS_SMEM / p.stage_bytes);
+    p.stages = std::min(NS_STAGES, (NS_SMEM - (p.share > 1 ? p.nt_a * 512 : 0)) / p.stage_bytes);
     // Two steps of X at a time save one A and one X product of every two and cost three more n x n products, and a barrier each (512 x 13200:
     // 270 -> 256 us, 4096 x 9216: 2.42 -> 2.12 ms, but 512 x 2048: 134 -> 150 us).  Rounding errors of A' are of A's size, not of its
     // small entries': fine for one such step (1.5 times the error of O on spectra over four decades), not for a chain of them.
@@ -960,14 +1021,14 @@ static int ns_run(int batch, NsInput in, int steps, const float* coef, char* ws,
         attr[0].id = cudaLaunchAttributeCooperative;
         attr[0].val.cooperative = 1;
         attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-        cfg.numAttrs = p.pair ? 2 : 1;
+        attr[1].val.clusterDim.x = p.pair ? 2 : p.share; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = p.pair || p.share > 1 ? 2 : 1;
     } else if (p.cluster) {
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim.x = p.G; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         cfg.numAttrs = 1;
     }
-    if ((p.pair ? cudaLaunchKernelEx(&cfg, ns_kernel<true>, maps, p) : cudaLaunchKernelEx(&cfg, ns_kernel<false>, maps, p)) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, p.pair ? ns_kernel<NS_PAIR> : p.share > 1 ? ns_kernel<NS_SHARE> : ns_kernel<NS_ALONE>, maps, p) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
     count_launch();
     return launch_status();
 }

@@ -94,6 +94,19 @@ def test_orthogonalise_large(dr, r, c):
     close(o.double().cpu().numpy()[0], polynomial(gd[0]))
 
 
+@pytest.mark.parametrize("b,r,c", [(1, 256, 2304), (6, 256, 2304), (1, 2304, 250), (2, 200, 6000), (1, 130, 9000), (1, 512, 2048), (1, 320, 4200), (14, 256, 1152), (1, 136, 5001)])
+def test_few_long_rows(dr, b, r, c):
+    """Sizes at which several processors share a tile of X X^T along the long axis."""
+    import torch
+    g = gradient(f"fl{b}.{r}.{c}", (b, r, c))
+    o, gd = orthogonalise(dr, g, True)
+    got = o.double().cpu().numpy()
+    for i in range(b):
+        close(got[i], polynomial(gd[i]), f"matrix {i}")
+    again, _ = orthogonalise(dr, g, True)
+    assert torch.equal(o, again), "not the same on a second run"
+
+
 @pytest.mark.parametrize("r,c", [(80, 208), (160, 200), (400, 140), (136, 1000)])
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 7])
 def test_steps_and_coefficients(dr, steps, r, c):
