@@ -565,12 +565,23 @@ static LnChoice ln_pick() {
 
 // The narrowest team whose registers hold the row, 16 channels a thread: fewer threads per row mean fewer steps in its
 // sums and fewer registers spent on half-empty vectors.  PHASED: at least 2 E threads, one for each channel outside the vectors.
+// Forward, rows a little too long for a team get 24 channels a thread instead of a team of twice the size that is mostly empty (bfloat16,
+// 154000 rows of 333, phased: 58 -> 42 us; 46000 of 1104: 54 -> 42 us; 24000 of 2100: 84 -> 46 us; 1536, three quarters full: 41 -> 37 us;
+// with float32 vectors of 4, 333: 64 -> 55 us, but 1400: 50 -> 53 us, so only up to a third more).  The backward pass would not fit its registers.
 template <bool BWD, typename TI, typename TO, int MODE>
 static LnChoice ln_pick_vec(int C) {
     constexpr int E = sizeof(TI) + sizeof(TO) == 4 ? 8 : 4, V = 16 / E, W = MODE == LN_PHASED ? 2 * E : 8;
     if (C <= 8 * W) return ln_pick<BWD, TI, TO, E, V / 2, W, MODE>();
     if (C <= 128) return ln_pick<BWD, TI, TO, E, V, W, MODE>();
     if (C <= 256) return ln_pick<BWD, TI, TO, E, V, 16, MODE>();
+    if constexpr (!BWD) {
+        auto more = [&](int full) { return C > full && C <= full + (E == 8 ? full / 2 : full / 3); };
+        if (more(256)) return ln_pick<BWD, TI, TO, E, 3 * V / 2, 16, MODE>();
+        if (more(512)) return ln_pick<BWD, TI, TO, E, 3 * V / 2, 32, MODE>();
+        if (more(1024)) return ln_pick<BWD, TI, TO, E, 3 * V / 2, 64, MODE>();
+        if (more(2048)) return ln_pick<BWD, TI, TO, E, 3 * V / 2, 128, MODE>();
+        if (more(4096)) return ln_pick<BWD, TI, TO, E, 3 * V / 2, 256, MODE>();
+    }
     if (C <= 512) return ln_pick<BWD, TI, TO, E, V, 32, MODE>();
     if (C <= 1024) return ln_pick<BWD, TI, TO, E, V, 64, MODE>();
     if (C <= 2048) return ln_pick<BWD, TI, TO, E, V, 128, MODE>();

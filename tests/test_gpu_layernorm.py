@@ -196,6 +196,25 @@ def test_rows_at_any_offset(dr, M, C, ldx, ldy, offx, offy, xf32, yf32):
         assert bool((whole == 9).all()), "written outside the rows"
 
 
+@pytest.mark.parametrize("xf32,yf32", [(False, False), (True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("C", [257, 264, 341, 384, 385, 520, 683, 768, 1030, 1365, 1536, 2056, 2730, 3001, 3080, 4104, 5461, 6144, 6150])
+def test_rows_a_little_longer_than_a_team(dr, C, xf32, yf32):
+    """Channel counts on both sides of every change of a thread's share, of dense rows and of rows inside wider ones."""
+    import torch
+    M = 203
+    x = rows(f"t{C}", M, C)
+    g, b = 1 + 0.2 * S.normal(0, f"g{C}", (C,)), 0.3 * S.normal(0, f"b{C}", (C,))
+    for pad in (0, 16):
+        xt, yt = empty((M, C + pad), xf32), empty((M, C + pad), yf32)
+        xt[:, pad // 2:pad // 2 + C] = dev(x, xf32)
+        yt.fill_(7.0)
+        mean, rstd = empty((M,), True), empty((M,), True)
+        dr.dr_layernorm(M, C, xt[:, pad // 2:], C + pad, dev(g, True), dev(b, True), 1e-5, yt[:, pad // 2:], C + pad, mean, rstd,
+                        dr.DR_LN_X_F32 * xf32 | dr.DR_LN_Y_F32 * yf32)
+        check_forward((host(yt[:, pad // 2:pad // 2 + C]), host(mean), host(rstd)), x, g.astype(np.float64), b.astype(np.float64), 1e-5, yf32)
+        assert bool((yt[:, :pad // 2] == 7).all()) and bool((yt[:, pad // 2 + C:] == 7).all())
+
+
 @pytest.mark.parametrize("C", [64, 100, 777, 1024, 4096])
 def test_no_weights_no_statistics_in_place(dr, C):
     import torch
