@@ -796,30 +796,12 @@ static int ns_tri_tiles(int n, int tr, int nt) {
     return t;
 }
 
-// The largest cluster (a power of two, at most 16) the device can hold with the kernel's shared memory.
-static int ns_max_cluster() {
-    static std::atomic<int> known[64];
-    std::atomic<int>& slot = known[PerDeviceFlag::dev()];
-    int c = slot.load(std::memory_order_relaxed);
-    if (c) return c;
-    for (c = 16; c > 8; c /= 2) {
-        cudaLaunchConfig_t cfg = {};
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        cfg.gridDim = dim3(c); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM_ALL; cfg.attrs = attr; cfg.numAttrs = 1;
-        int n = 0;
-        if (ns_attributes() && cudaOccupancyMaxActiveClusters(&n, ns_kernel<NS_ALONE>, &cfg) == cudaSuccess && n > 0) break;
-        (void)cudaGetLastError();
-    }
-    slot.store(c, std::memory_order_relaxed);
-    return c;
-}
-
-// Clusters of 2 or 4 CTAs the device holds at a time.
+// Clusters of 2, 4, 8 or 16 CTAs the device holds at a time, with all of an SM's shared memory to a CTA.
 static int ns_clusters(int ctas) {
-    static std::atomic<int> known[64][2];
-    std::atomic<int>& slot = known[PerDeviceFlag::dev()][ctas > 2];
+    static std::atomic<int> known[64][4];
+    int k = 0;
+    while ((2 << k) < ctas) ++k;
+    std::atomic<int>& slot = known[PerDeviceFlag::dev()][k];
     int n = slot.load(std::memory_order_relaxed);
     if (n) return n - 1;
     cudaLaunchConfig_t cfg = {};
@@ -849,11 +831,14 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     const int rows128 = (p.n + 127) / 128, rows256 = (p.n + 255) / 256;
     auto across = [](int width, int nt) { return (width + nt - 1) / nt; };
     int g = std::min({std::max(rows128 * across(p.m, 64), 1), sms, std::max(1, sms / batch1)});
-    if (g <= ns_max_cluster()) {
-        int q = 1;
-        while (q * 2 <= g) q *= 2;
+    // As a cluster (of a power of two) where the device holds one for every matrix at a time: as nine clusters of 16 that take turns, 9 x 144 x
+    // 816 took 211 us, as nine groups of a cooperative launch 120.  And where that leaves few CTAs unused: 20 x 144 x 816 in clusters of 4
+    // took 202 us, in groups of 7 140; 12 x 160 x 160 with 8 and 12 125 and 99 us.
+    int q = 1;
+    while (q * 2 <= g) q *= 2;
+    if (q > 1 && g <= 16 && 4 * q >= 3 * g && ns_clusters(q) >= std::min(batch1, sms / q)) {
         g = q;
-        p.cluster = g > 1;
+        p.cluster = 1;
     }
     p.G = g;
     p.groups = std::min(batch1, std::max(1, sms / g));

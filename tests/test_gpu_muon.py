@@ -107,6 +107,16 @@ def test_few_long_rows(dr, b, r, c):
     assert torch.equal(o, again), "not the same on a second run"
 
 
+@pytest.mark.parametrize("b,r,c", [(9, 144, 816), (20, 144, 300), (12, 160, 160), (37, 144, 270), (40, 260, 131), (160, 129, 130)])
+def test_many_matrices(dr, b, r, c):
+    """Batches whose matrices get groups of processors of every kind, side by side and in turns."""
+    g = gradient(f"mm{b}.{r}.{c}", (b, r, c))
+    o, gd = orthogonalise(dr, g, True)
+    got = o.double().cpu().numpy()
+    for i in range(b):
+        close(got[i], polynomial(gd[i]), f"matrix {i}")
+
+
 @pytest.mark.parametrize("r,c", [(80, 208), (160, 200), (400, 140), (136, 1000)])
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 7])
 def test_steps_and_coefficients(dr, steps, r, c):
