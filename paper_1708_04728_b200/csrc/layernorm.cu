@@ -11,7 +11,7 @@
 // Measured on a B200 against a copy of 1 Gi elements at 6530 GB/s.  200704 rows x 256 channels, bfloat16: forward 38 us
 // (5.4 TB/s, 0.83 of that copy; a copy of these 206 MB takes 35 us), backward 56 us (5.5 TB/s, 0.84); with loads straight into
 // registers, one row ahead, they took 90 and 241 us.  12544 x 2048, float32 x and dx: backward 48 us (5.4 TB/s, 0.82).
-// 50176 x 333 between rows of 1024 (no row but every eighth aligned): forward 21 us (3.1 TB/s), bound by instruction issue:
+// 50176 x 333 inside rows of 501 (no row but every eighth aligned): forward 16 us (4.1 TB/s), bound by instruction issue:
 // the channels outside the vectors cost a load, a store and the selects of a whole vector.  49 x 1024: 5.3 and 8.3 us, the
 // launches (a kernel that does nothing takes 2 us between its neighbours; the backward pass has two).
 #include <algorithm>
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(TW > 256 ? TW : 256) ln_forward_kernel(const L
 // dx, and the block's sums of dy * xhat and of dy: every thread adds up its own channels over its rows in registers, the
 // teams of a block are joined in shared memory in order, and the block writes one row of partial sums.  One block of 512
 // threads per SM: the sums take 32 registers of a thread, and fewer, wider blocks leave fewer rows of partial sums to join
-// (148 x 2 C floats).  Joined by the last block of the same launch over a cluster, 49 x 1024 took 8.0 us instead of 8.2, but
+// (148 x 2 C floats).  As one cluster that joins its own sums, 49 x 1024 took 8.0 us instead of 8.2, but
 // 196 x 512 and more rows took longer; the join stays a launch of its own.
 template <typename TI, typename TO, int E, int V, int TW, int MODE>
 __global__ void __launch_bounds__(LN_BWD_THREADS, 1) ln_backward_kernel(const LnParams p) {

@@ -25,7 +25,7 @@
 //   4096 x 9216   2.07 .. 2.4 ms (the clock falls with the power drawn), 0.78 .. 0.67 of that rate; the plain form in float32 takes
 //                 62.7 ms.  Bound by the tensor pipe and by whole rounds of tiles.
 //   2048 x 2048   337 us, 0.31: 64 tiles of 256 x 256 for 74 pairs, drains of 8 us behind MMAs of 10.
-//   1000 x 2048   174 us, 512 x 13200 with the optimiser's step 256 us, 512 x 2048 120 us, 6 x 256 x 2304 161 us, 192 x 576 101 us: 15 dependent
+//   1000 x 2048   175 us, 512 x 13200 with the optimiser's step 253 us, 512 x 2048 120 us, 6 x 256 x 2304 161 us, 192 x 576 101 us: 15 dependent
 //                 phases of 6 to 20 us each.  A phase is a barrier 1.3 .. 1.9 us, 0.5 .. 1 to its first MMA's operands, 0.8 of TMA latency, the MMAs, and
 //                 a drain of 1.3 .. 3; where all SMs load operands, the way out of L2 (12 TB/s).
 #include <algorithm>

@@ -12,9 +12,9 @@
 // Products and element-wise terms as in the kernel for larger matrices (muon.cu); with few rows rounding errors average less, so
 // matrices of up to 64 rows multiply hi hi + hi lo + lo hi: the tensor cores idle here either way (relative error of O 1e-6 .. 3e-5).
 //
-// Measured on a B200, five steps: 64 x 147 47 us (49 us with the optimiser's momentum and update; 3 products of 0.6 us, two roundings to pairs
-// and three block barriers a step), 128 x 864 60 us, 27 x 96 x 800 with the optimiser 76 .. 98 us.  At 128 x 864 the tensor pipe is busy 5 % of the
-// time and 41 % of the issue slots are taken: a step of 11 us is a chain of element-wise passes over E and X between MMAs of under a microsecond.
+// Measured on a B200, five steps: 64 x 147 37 us (39 us with the optimiser's momentum and update), 128 x 864 58 us, 27 x 96 x 800 with the
+// optimiser 72 us.  At 128 x 864 the tensor pipe is busy 5 % of the time and 41 % of the issue slots are taken: a step is a chain of
+// element-wise passes over E and X (0.3 .. 0.9 us each) between three products of 0.7 .. 1.2 us from the barrier in front to the last MMA.
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     // A warp reads 32 of the accumulators' 128 rows, and warps whose rows are the same modulo 128 share a quarter of the SM.  Matrices of up to 64
     // rows fill only half of that, so theirs are held twice, as rows 0 .. 63 and 64 .. 127 of the first operands: all warps have rows, and
-    // half as many columns of them (64 x 147: 47 -> 41 us).
+    // half as many columns of them (64 x 147: 47 -> 41 us, then).
     const bool twice = p.n <= 64;
     const int q = warp & 3, row = (twice ? q & 1 : q) * 32 + lane;
     const int first = ((warp >> 2) + (twice ? q >> 1 << 2 : 0)) * 8, stride = twice ? 64 : 32;      // a warp's columns: 8 from here, 8 a stride on
@@ -480,7 +480,7 @@ NsSmallPlan ns_small_plan(int batch, int rows, int cols) {
     const int n = std::min(rows, cols), m = std::max(rows, cols), all = (m + 63) / 64;
     if (n > 128) return l;
     // One CTA where it holds X: no exchange.  Otherwise a chunk of 64 columns each, more where a batch would not fit the device
-    // (128 x 864: 60 us with 16 CTAs, 64 with 8, 76 with 4).
+    // (128 x 864, at an earlier stage: 60 us with 16 CTAs, 64 with 8, 76 with 4).
     for (int g = 1; g <= 16; g *= 2) {
         const int chunks = (all + g - 1) / g, clusters = nss_clusters(g);
         if (chunks > 4 || 2 * chunks + 2 * ((n + 63) / 64) > NSS_CHUNKS || clusters < 1) continue;
