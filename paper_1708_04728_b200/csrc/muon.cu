@@ -639,8 +639,9 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     float* tile = reinterpret_cast<float*>(ns_smem_raw + (smem - smem_u32(ns_smem_raw)));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = blockIdx.x / p.G, rank = blockIdx.x - group * p.G;
-    // A launch that lost its cluster size (a profiler that replays a cooperative launch, say) must not reach an instruction for CTA pairs.
-    if (PAIR && cluster_ctas() != 2) {
+    // A launch that lost its cluster size (a profiler that replays a cooperative launch, say) must not reach an instruction for CTA pairs or
+    // a neighbour's shared memory.
+    if ((PAIR && cluster_ctas() != 2) || (SHARE && (int)cluster_ctas() != (p.cluster ? p.G : p.share))) {
         if (threadIdx.x == 0) report_timeout(p.status, 77, 0);
         return;
     }
