@@ -78,7 +78,7 @@ enum { NS_ALONE, NS_SHARE, NS_PAIR };
 struct NsItem { int i, j, k0, k1, split, tile; };
 struct NsShared {
     NsItem first[3];            // the CTA's first tile of each phase: found once, its divisions took 0.3 us of every phase
-    uint64_t full[NS_STAGES], empty[NS_STAGES], tfull[2], tempty[2];
+    uint64_t full[2 * NS_STAGES], empty[NS_STAGES], tfull[2], tempty[2];    // full: of each issuing warp
     uint32_t tmem_base;
     int abort;
     double red[NS_THREADS / 32];
@@ -258,6 +258,7 @@ struct NsPipe {
     uint32_t phase = 0;
     int acc = 0;
     uint32_t acc_phase = 0;
+    uint32_t mine = 0;          // an issuing warp: a bit for each stage, the parity of its own next fill
     __device__ __forceinline__ void next_stage(int stages) { if (++stage == stages) { stage = 0; phase ^= 1; } }
     __device__ __forceinline__ void next_acc() { if (++acc == 2) { acc = 0; acc_phase ^= 1; } }
 };
@@ -287,6 +288,7 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             for (int item = first; item < items && ok; item += step) {
                 const NsItem it = item == first ? sh.first[PHASE] : ns_item<PHASE, PAIR>(p, item);
                 const int ar = it.i * p.tr + side * 128, bc = it.j * nt + side * (nt / 2);
+                uint32_t which = 0;                     // the warp that takes the slice
                 for (int term = 0; term < p.terms && ok; ++term) {
                     const CUtensorMap* am = term == 2 ? al : ah;
                     const CUtensorMap* bm = term == 1 ? bl : bh;
@@ -297,7 +299,8 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
                             ok = false;
                             break;
                         }
-                        const uint32_t full = PAIR ? (full0 + 8 * pipe.stage) & PEER_BIT_MASK : full0 + 8 * pipe.stage;
+                        const uint32_t full = PAIR ? (full0 + 8 * pipe.stage) & PEER_BIT_MASK : full0 + which + 8 * pipe.stage;
+                        if (!PAIR) which ^= 8 * NS_STAGES;
                         const uint32_t dst = smem + pipe.stage * p.stage_bytes;
                         if (side == 0) mbar_expect_tx_u32(full, bytes);
                         tma_load_4d_u32<PAIR>(dst, am, full, 0, ar, D * kb, group, 1u);
@@ -310,8 +313,10 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
             }
         }
     } else if (warp <= 2) {
-        // Two issuing warps (pairs of CTAs: one), each on every second stage into an accumulator of its own, which the drain adds: while one
-        // hands a stage over, the other's MMAs run.
+        // Two issuing warps (pairs of CTAs: one), each on every second slice into an accumulator of its own, which the drain adds: while one
+        // hands a stage over, the other's MMAs run.  A warp sees only its own fills, and slices may land out of order, so each warp has a full
+        // barrier of its own for every stage: on a common one, whose phases the other's fills complete too, the parity of a fill two phases ahead
+        // is that of the one before it, and a wait for a slice could pass while the stage's last one was still on its way.
         const int which = warp - 1;
         if (side == 0 && (!PAIR || which == 0) && elect_one()) {
             // D float32, A and B float16; B of the X product lies with the contraction index as its rows
@@ -335,7 +340,7 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
                         pipe.next_stage(p.stages);
                         continue;
                     }
-                    if (!ready && !mbar_wait_u32(full0 + 8 * pipe.stage, pipe.phase, abort_flag)) {
+                    if (!ready && !mbar_wait_u32(full0 + 8 * (pipe.stage + which * NS_STAGES), PAIR ? pipe.phase : (pipe.mine >> pipe.stage) & 1u, abort_flag)) {
                         if (!*abort_flag) report_timeout(p.status, 73, item);
                         *abort_flag = 1;
                         ok = false;
@@ -343,6 +348,7 @@ __device__ __forceinline__ void ns_product(const NsParams& p, const NsMaps& maps
                     }
                     tc_fence_after();
                     const uint32_t a = smem + pipe.stage * p.stage_bytes, b = a + D * NS_CHUNK, empty = empty0 + 8 * pipe.stage;
+                    if (!PAIR) pipe.mine ^= 1u << pipe.stage;
                     pipe.next_stage(p.stages);
                     if (PAIR) ready = mbar_test_u32(full0 + 8 * pipe.stage, pipe.phase);    // asked before the MMAs, known after them
                     const uint32_t ad = sdesc_lo(a), bd = PHASE == NS_X ? (((b & 0x3FFFFu) >> 4) | ((D * 512u) << 16)) : sdesc_lo(b);
@@ -646,7 +652,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
         return;
     }
     if (threadIdx.x == 0) {
-        for (int i = 0; i < NS_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < NS_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.full[NS_STAGES + i], 1); mbar_init(&sh.empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], PAIR ? 1 : 2); mbar_init(&sh.tempty[i], PAIR ? 16 : 8); }
         sh.abort = 0;
         fence_barrier_init();
