@@ -299,6 +299,10 @@ int dr_device_status(int info[4]);
  * (1 .. 2e9), on a barrier nothing arrives on, and then leaves the same record a convolution kernel would.
  * dr_device_status() afterwards returns DR_ERR_DEVICE_TIMEOUT with info[1] = 99; the context stays usable. */
 int dr_selftest_wait_timeout(long long limit_cycles, void* stream);
+/* Self-test of the orthogonalised update's guard against a launch that lost its thread-block cluster: launches one of its kernels
+ * (kind 0: in shared memory, 1: each CTA for itself, 2: shared tiles) without the cluster its arguments name.  The kernel returns at once;
+ * dr_device_status() afterwards returns DR_ERR_DEVICE_TIMEOUT with info[1] = 77.                       */
+int dr_selftest_lost_cluster(int kind, void* stream);
 /* ---- layer-wise regression of a slim layer (Section 3.1, Eq. (w_b) and Lemma 1) -------------------------
  * The slim layer f~(W, b; X) = ReLU(conv(X; W) + b) is re-learned from pairs (X, Y_CNN) of the input and the
  * output feature map of the layer group it replaces, by SGD on L = 1/(2B) * sum_i ||Y_CNN^i - f~(W, b; X^i)||_F^2

@@ -119,6 +119,7 @@ _SIGS = {
     "dr_last_conv_path": (_I, []),
     "dr_device_status": (_I, [C.POINTER(_I)]),
     "dr_selftest_wait_timeout": (_I, [C.c_longlong, _P]),
+    "dr_selftest_lost_cluster": (_I, [_I, _P]),
     "dr_launch_count": (C.c_longlong, []),
     "dr_tensor_map_encodes": (C.c_longlong, []),
     "dr_conv_plan": (_I, [C.POINTER(dr_conv_desc), _I, _I, _I, _Z, C.POINTER(_I)]),
@@ -376,6 +377,10 @@ def dr_device_status():
 
 def dr_selftest_wait_timeout(limit_cycles: int, stream=None):
     _check(_lib.dr_selftest_wait_timeout(limit_cycles, _stream(stream)), "dr_selftest_wait_timeout")
+
+
+def dr_selftest_lost_cluster(kind: int, stream=None):
+    _check(_lib.dr_selftest_lost_cluster(kind, _stream(stream)), "dr_selftest_lost_cluster")
 
 
 def dr_launch_count() -> int:

@@ -35,6 +35,19 @@ __device__ __forceinline__ bool elect_one() {
     return e != 0;
 }
 
+__device__ __forceinline__ int cluster_ctas() {
+    uint32_t n;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+    return (int)n;
+}
+// A launch that lost its cluster size (a profiler that replays a cooperative launch, say) must not reach an instruction for clusters or CTA
+// pairs, nor a neighbour's shared memory: the kernels ask this first, and return.
+__device__ __forceinline__ bool cluster_lost(int ctas, int* status) {
+    if (cluster_ctas() == ctas) return false;
+    if (threadIdx.x == 0) report_timeout(status, 77, ctas);
+    return true;
+}
+
 struct __align__(32) Half16 { uint32_t u[8]; };
 struct __align__(32) Float8 { float f[8]; };
 __device__ __forceinline__ Half16 ld16h(const __half* p) {
@@ -159,6 +172,7 @@ __device__ __forceinline__ void ns_put_o(const NsInput& in, size_t at, float* o)
 // The kernel for matrices of at most 128 rows that a cluster holds in shared memory (muon_small.cu); 0 CTAs: not for this shape.
 struct NsSmallPlan { int ctas, groups, chunks, terms; size_t part, sums, diag, bytes; };
 NsSmallPlan ns_small_plan(int batch, int rows, int cols);
+int ns_small_lost_cluster(cudaStream_t stream);         // self-test, see dr_selftest_lost_cluster
 int ns_small_run(const NsSmallPlan& plan, int batch, const NsInput& in, int steps, const float* coef, void* workspace, cudaStream_t stream);
 
 }  // namespace dr

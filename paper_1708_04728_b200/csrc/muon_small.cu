@@ -182,6 +182,7 @@ template <int CN>
 __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_constant__ NsSmall p) {
     extern __shared__ uint8_t nss_raw[];
     __shared__ NsSmallShared sh;
+    if (cluster_lost(p.G, p.status)) return;
     const uint32_t smem = (smem_u32(nss_raw) + 1023u) & ~1023u;
     uint8_t* const X = nss_raw + (smem - smem_u32(nss_raw));           // hi chunks, then lo chunks
     const int xlo = p.chunks * NSS_CHUNK, e_at = 2 * xlo;
@@ -452,6 +453,16 @@ static bool nss_attributes() {
         }
     attr_set.set();
     return true;
+}
+
+int ns_small_lost_cluster(cudaStream_t stream) {
+    NsSmall p = {};
+    p.G = 2;
+    p.status = dev_status_ptr();
+    if (!nss_attributes()) return DR_ERR_CUDA;
+    ns_small_kernel<8><<<2, NSS_THREADS, NS_SMEM_ALL, stream>>>(p);
+    count_launch();
+    return launch_status();
 }
 
 // Clusters of `ctas` CTAs the device holds at a time.

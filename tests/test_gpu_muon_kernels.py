@@ -64,3 +64,15 @@ def test_operands_from_memory(dr, b, r, c, steps):
         assert error(o[i], u[i], steps) <= (FEW_ROWS if min(r, c) <= 64 else RANDOM)
     for _ in range(3):
         assert torch.equal(update(dr, u, steps), o), "not the same on a second run"
+
+
+@pytest.mark.parametrize("kind", [0, 1, 2])
+def test_a_launch_without_its_cluster_returns(dr, kind):
+    """The kernels compare the cluster they find with the one their arguments name before the first instruction that needs it."""
+    assert dr.dr_device_status()[0] == 0
+    dr.dr_selftest_lost_cluster(kind)
+    st, info = dr.dr_device_status()
+    assert st == dr.DR_ERR_DEVICE_TIMEOUT and info[1] == 77
+    assert dr.dr_device_status()[0] == 0
+    u = gaussian(kind, 1, 40, 72)
+    assert error(update(dr, u)[0], u[0]) <= FEW_ROWS
