@@ -418,6 +418,15 @@ int dr_layernorm_bwd(size_t npix, int C, const void* dy, int lddy, const void* x
 #define DR_NS_MAX_STEPS 16
 #define DR_NS_MAX_DIM   65536
 int dr_orthogonalise_workspace_bytes(int batch, int rows, int cols, size_t* bytes);
+/* How the matrices would be worked on (no launch): plan[0] the kernel (DR_NS_KERNEL_*), plan[1] CTAs of a matrix, plan[2] matrices at a
+ * time, plan[3] 1 if X takes two steps at a time, plan[4] parts of the long axis in X X^T that meet in the workspace, plan[5] parts
+ * that meet within a cluster, plan[6] terms of a product (1: the high halves, 3: high and low), plan[7] 1 if a matrix's CTAs are one
+ * thread-block cluster.  The answer belongs to the current device.  Errors: INVALID_ARG, UNSUPPORTED.                    */
+#define DR_NS_KERNEL_SMALL 0   /* X stays in the shared memory of a cluster (at most 128 rows or columns)     */
+#define DR_NS_KERNEL_ALONE 1   /* each CTA has tiles of its own                                                */
+#define DR_NS_KERNEL_SHARE 2   /* CTAs of a cluster share a tile of X X^T along the long axis                  */
+#define DR_NS_KERNEL_PAIR  3   /* two CTAs share every tile (cta_group::2)                                     */
+int dr_orthogonalise_plan(int batch, int rows, int cols, int plan[8]);
 int dr_orthogonalise(int batch, int rows, int cols, const void* g, int steps, const float* coef, float eps, void* o,
                      void* workspace, size_t workspace_bytes, unsigned flags, void* stream);
 /* One step of an optimiser that applies orthogonalised momentum, the counterpart of dr_sgd_update for filter banks

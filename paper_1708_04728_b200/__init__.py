@@ -32,6 +32,7 @@ DR_PATH_AUTO, DR_PATH_SIMT, DR_PATH_UMMA_GATHER, DR_PATH_UMMA_TMA, DR_PATH_UMMA_
 DR_PATH_UMMA_SPLITK = 8
 DR_PATH_UMMA_QLIN = 9
 DR_CONV_WS_COUNTER_BYTES = 1024
+NS_KERNELS = ("small", "alone", "share", "pair")
 DR_LN_X_F32, DR_LN_Y_F32, DR_NS_G_F32, DR_NS_MAX_STEPS, DR_NS_MAX_DIM = 0x1, 0x2, 0x1, 16, 65536
 PATH_NAMES = {0: "auto", 1: "simt", 2: "umma_gather", 3: "umma_tma", 4: "umma_patch", 5: "umma_stem", 6: "retired", 7: "umma_stem_d",
               8: "umma_splitk", 9: "umma_qlin", -1: "-"}
@@ -87,6 +88,7 @@ _SIGS = {
     "dr_layernorm_bwd_workspace_bytes": (_I, [_Z, _I, C.POINTER(_Z)]),
     "dr_layernorm_bwd": (_I, [_Z, _I, _P, _I, _P, _I, _P, _P, _P, _P, _I, _P, _P, _P, _Z, C.c_uint, _P]),
     "dr_orthogonalise_workspace_bytes": (_I, [_I, _I, _I, C.POINTER(_Z)]),
+    "dr_orthogonalise_plan": (_I, [_I, _I, _I, C.POINTER(_I)]),
     "dr_orthogonalise": (_I, [_I, _I, _I, _P, _I, C.POINTER(_F), _F, _P, _P, _Z, C.c_uint, _P]),
     "dr_muon_update": (_I, [_I, _I, _I, _P, _P, _P, _F, _F, _F, _I, _I, C.POINTER(_F), _F, _P, _P, _Z, _P]),
     "dr_conv_workspace_bytes": (_I, [C.POINTER(dr_conv_desc), _I, _I, _I, C.POINTER(_Z)]),
@@ -270,6 +272,14 @@ def dr_orthogonalise_workspace_bytes(batch, rows, cols) -> int:
     n = _Z(0)
     _check(_lib.dr_orthogonalise_workspace_bytes(batch, rows, cols, C.byref(n)), "dr_orthogonalise_workspace_bytes")
     return n.value
+
+
+def dr_orthogonalise_plan(batch, rows, cols) -> dict:
+    """How the library would work on the matrices: kernel, CTAs of a matrix, matrices at a time, two steps at a time, parts, terms."""
+    plan = (_I * 8)()
+    _check(_lib.dr_orthogonalise_plan(batch, rows, cols, plan), "dr_orthogonalise_plan")
+    return {"kernel": NS_KERNELS[plan[0]], "ctas": plan[1], "groups": plan[2], "two_steps": plan[3], "splits": plan[4], "share": plan[5],
+            "terms": plan[6], "cluster": plan[7]}
 
 
 def _coef(coef, steps):

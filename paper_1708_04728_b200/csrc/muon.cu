@@ -792,12 +792,12 @@ static int ns_tri_tiles(int n, int tr, int nt) {
     return t;
 }
 
-// Clusters of 2, 4, 8 or 16 CTAs the device holds at a time, with all of an SM's shared memory to a CTA.
-static int ns_clusters(int ctas) {
-    static std::atomic<int> known[64][4];
+// Clusters of 2, 4, 8 or 16 CTAs the device holds at a time, with all of an SM's shared memory to a CTA; `pair`: of the kernel for CTA pairs.
+static int ns_clusters(int ctas, bool pair = false) {
+    static std::atomic<int> known[64][5];
     int k = 0;
     while ((2 << k) < ctas) ++k;
-    std::atomic<int>& slot = known[PerDeviceFlag::dev()][k];
+    std::atomic<int>& slot = known[PerDeviceFlag::dev()][pair ? 4 : k];
     int n = slot.load(std::memory_order_relaxed);
     if (n) return n - 1;
     cudaLaunchConfig_t cfg = {};
@@ -805,7 +805,7 @@ static int ns_clusters(int ctas) {
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(NS_THREADS); cfg.dynamicSmemBytes = NS_SMEM_ALL; cfg.attrs = attr; cfg.numAttrs = 1;
-    if (!ns_attributes() || cudaOccupancyMaxActiveClusters(&n, ns_kernel<NS_SHARE>, &cfg) != cudaSuccess || n < 0) {
+    if (!ns_attributes() || cudaOccupancyMaxActiveClusters(&n, pair ? ns_kernel<NS_PAIR> : ns_kernel<NS_SHARE>, &cfg) != cudaSuccess || n < 0) {
         (void)cudaGetLastError();
         n = 0;
     }
@@ -878,7 +878,8 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
         return c;
     };
     Choice c = choose(false);
-    if (g == sms && sms % 2 == 0 && p.n > 128) {
+    // Pairs meet at grid barriers: only where the device holds all of them at a time.
+    if (g == sms && sms % 2 == 0 && p.n > 128 && 2 * ns_clusters(2, true) >= sms) {
         const Choice two = choose(true);
         if (two.a + two.s + two.x < c.a + c.s + c.x) { c = two; p.pair = 1; }
     }
@@ -1045,6 +1046,22 @@ extern "C" int dr_orthogonalise_workspace_bytes(int batch, int rows, int cols, s
     if (st != DR_OK) return st;
     const NsSmallPlan small = ns_small_plan(batch, rows, cols);
     *bytes = small.ctas ? small.bytes : ns_plan(batch, rows, cols).total;
+    return DR_OK;
+}
+
+extern "C" int dr_orthogonalise_plan(int batch, int rows, int cols, int plan[8]) {
+    if (!plan) return DR_ERR_INVALID_ARG;
+    const int st = ns_check(batch, rows, cols, 1, nullptr, 0.f);
+    if (st != DR_OK) return st;
+    const NsSmallPlan small = ns_small_plan(batch, rows, cols);
+    for (int i = 0; i < 8; ++i) plan[i] = 0;
+    if (small.ctas) {
+        plan[0] = DR_NS_KERNEL_SMALL; plan[1] = small.ctas; plan[2] = small.groups; plan[4] = plan[5] = 1; plan[6] = small.terms; plan[7] = small.ctas > 1;
+        return DR_OK;
+    }
+    const NsParams p = ns_plan(batch, rows, cols).p;
+    plan[0] = p.pair ? DR_NS_KERNEL_PAIR : p.share > 1 ? DR_NS_KERNEL_SHARE : DR_NS_KERNEL_ALONE;
+    plan[1] = p.G; plan[2] = p.groups; plan[3] = p.merge; plan[4] = p.splits; plan[5] = p.share; plan[6] = p.terms; plan[7] = p.cluster;
     return DR_OK;
 }
 

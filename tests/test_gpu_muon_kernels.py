@@ -76,3 +76,12 @@ def test_a_launch_without_its_cluster_returns(dr, kind):
     assert dr.dr_device_status()[0] == 0
     u = gaussian(kind, 1, 40, 72)
     assert error(update(dr, u)[0], u[0]) <= FEW_ROWS
+
+
+@pytest.mark.parametrize("shape,kernel,two_steps", [
+    ((1, 2048, 2048), "pair", 0), ((1, 2049, 2300), "pair", 0), ((1, 2000, 16000), "pair", 1), ((1, 13200, 512), "alone", 1),
+    ((40, 130, 4200), "alone", 1), ((200, 100, 4200), "alone", 1), ((1, 512, 2048), "share", 0), ((1, 1000, 2048), "alone", 0)])
+def test_every_kernel_has_its_shapes(dr, shape, kernel, two_steps):
+    """The shapes by which the tests below reach each kernel: a change of the plan's rules must not leave one untested."""
+    plan = dr.dr_orthogonalise_plan(*shape)
+    assert plan["kernel"] == kernel and plan["two_steps"] == two_steps, plan
