@@ -404,9 +404,10 @@ int dr_layernorm_bwd(size_t npix, int C, const void* dy, int lddy, const void* x
  *  coef: NULL (a, b, c = 3.4445, -4.7750, 2.0315 in every step), or 3 * steps host floats, read before the call returns.
  *  steps <= DR_NS_MAX_STEPS, rows and cols <= DR_NS_MAX_DIM, batch <= 65535.
  *  The products take operands of 11 significant bits (the term a X and the diagonals of A and of b A + c A A: 22 or
- *  more; all of them where min(rows, cols) <= 64) and sum in float32.  Relative error of O (Frobenius, before it is
- *  rounded to bfloat16): 1e-4 .. 1e-3 for random matrices, up to 4e-3 where the singular values of U spread over many
- *  decades or its rank is low; below 1e-4 where min(rows, cols) <= 64.
+ *  more; all of them where min(rows, cols) <= 64) and sum in float32.  Relative error of O after five steps (Frobenius,
+ *  before it is rounded to bfloat16): 1e-4 .. 1e-3 for matrices of normal values, up to 4e-3 where the singular values of U
+ *  spread over many decades or its rank is low, up to 1e-2 where U is a single direction (rounding errors then add up instead
+ *  of averaging: 8e-3 with 65 rows, 2e-3 with 256, 1e-3 with 512); below 1e-4 where min(rows, cols) <= 64.
  *  X is kept in float16 times 4096, A and the polynomial in float16: with coefficients that let a singular value of X reach
  *  16, or an entry of the others 65504, O is not finite.
  *  An all-zero U gives zeros (eps > 0); a matrix with a NaN or an infinity gives NaN and touches no other matrix.

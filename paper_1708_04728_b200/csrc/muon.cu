@@ -9,8 +9,9 @@
 //  - A is split into its diagonal and the rest, A = D + E, D in float32:
 //      A A = E E + D E + E D + D D,  so only E, small where X is nearly orthogonal, is rounded (and only for E E);
 //    likewise the polynomial b A + c A A = diag + F:  X <- (a + diag) X + F X with a row factor in float32.
-//    With the whole of A in float16 the relative error of O is 2e-3 .. 4e-3 (random matrices); with the split 1e-4 .. 6e-4, and
-//    1.3e-3 (512 rows) .. 2.2e-3 (96 rows) at most for spectra over up to six decades and matrices of rank 4.
+//    With the whole of A in float16 the relative error of O is 2e-3 .. 4e-3 (random matrices); with the split 1e-4 .. 9e-4, at most
+//    1.3e-3 (512 rows) .. 2.3e-3 (130 rows, two steps at a time) for spectra over up to six decades, 1.2e-3 (512) .. 3.8e-3 (65 rows) for
+//    ranks of 2 .. 16, and 1e-3 (512) .. 8e-3 (65 rows) for a single direction, where rounding errors do not average.
 //  - Products symmetric by construction (A, E E) are computed for the lower triangle and mirrored, so they stay symmetric.
 // bfloat16 operands would cost 2e-3 .. 6e-3 even so: more than the rounding of O to bfloat16 itself.
 //

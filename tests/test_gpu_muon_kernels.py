@@ -7,8 +7,8 @@ import pytest
 pytestmark = pytest.mark.gpu
 
 COEF = (3.4445, -4.7750, 2.0315)
-# What include/dr.h states for the relative error of O (Frobenius): random matrices, wide spectra or low rank, at most 64 rows.
-RANDOM, SPREAD, FEW_ROWS = 1e-3, 4e-3, 1e-4
+# What include/dr.h states for the relative error of O (Frobenius): normal values, wide spectra or low rank, one direction, at most 64 rows.
+RANDOM, SPREAD, SINGLE, FEW_ROWS = 1e-3, 4e-3, 1e-2, 1e-4
 
 
 @pytest.fixture(scope="module")
@@ -85,3 +85,91 @@ def test_every_kernel_has_its_shapes(dr, shape, kernel, two_steps):
     """The shapes by which the tests below reach each kernel: a change of the plan's rules must not leave one untested."""
     plan = dr.dr_orthogonalise_plan(*shape)
     assert plan["kernel"] == kernel and plan["two_steps"] == two_steps, plan
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("own_coef", [False, True])
+@pytest.mark.parametrize("b,r,c", [(1, 2048, 2048), (1, 2049, 2300), (1, 2000, 16000), (1, 13200, 512), (1, 520, 13207), (40, 130, 4200), (1, 512, 2048)])
+def test_steps_of_the_large_kernels(dr, b, r, c, own_coef, steps):
+    """CTA pairs, two steps at a time (with a single one behind them where the number is odd), both, shared tiles; coefficients per step."""
+    import torch
+    u = gaussian(r + c + steps, b, r, c)
+    coef = [x for k in range(steps) for x in (3.0 - 0.2 * k, -3.2 + 0.1 * k, 1.2 - 0.05 * k)] if own_coef else None
+    o = update(dr, u, steps, coef)
+    for i in {0, b - 1}:
+        assert error(o[i], u[i], steps, coef) <= RANDOM
+    assert torch.equal(update(dr, u, steps, coef), o), "not the same on a second run"
+
+
+@pytest.mark.parametrize("b,r,c", [(1, 1, 300), (1, 300, 1), (2, 2, 50), (1, 64, 147), (3, 33, 200), (150, 16, 24), (1, 576, 64), (1, 60, 4200), (1, 65, 70), (27, 96, 800),
+                                   (1, 100, 4096), (1, 128, 864), (1, 100, 4200), (1, 129, 130), (160, 129, 130), (9, 144, 816), (1, 192, 576), (6, 256, 2304), (1, 2304, 250),
+                                   (1, 512, 2049), (1, 1000, 2048), (1, 4100, 1040)])
+def test_every_kernel_in_float32(dr, b, r, c):
+    u = gaussian(b + r + c, b, r, c)
+    o = update(dr, u)
+    for i in {0, b // 2, b - 1}:
+        assert error(o[i], u[i]) <= (FEW_ROWS if min(r, c) <= 64 else RANDOM)
+
+
+@pytest.mark.parametrize("r,c", [(40, 72), (64, 576), (60, 4200), (65, 300), (96, 800), (100, 4200), (130, 1000), (200, 1000), (512, 2048), (512, 13200), (2048, 2048), (2000, 16000)])
+def test_spectra_and_ranks(dr, r, c):
+    """Singular values over two, four and six decades; ranks 16, 4 and 1."""
+    import torch
+    k = min(r, c)
+    p, q = (torch.linalg.qr(gaussian(s + k, s, k).double())[0] for s in (r, c))
+    for decades in (2, 4, 6):
+        u = (p * torch.logspace(0, -decades, k, device="cuda", dtype=torch.float64) @ q.T).float()[None]
+        assert error(update(dr, u)[0], u[0]) <= (FEW_ROWS if k <= 64 else SPREAD), f"{decades} decades"
+    for rank in (16, 4, 1):
+        u = (gaussian(rank, 1, r, rank) @ gaussian(rank + 1, 1, rank, c))
+        assert error(update(dr, u)[0], u[0]) <= (FEW_ROWS if k <= 64 else SINGLE if rank == 1 else SPREAD), f"rank {rank}"
+
+
+@pytest.mark.parametrize("b,r,c", [(160, 129, 130), (300, 40, 72), (300, 72, 41), (200, 100, 300), (40, 128, 1021), (30, 256, 200), (3, 300, 520), (2, 2048, 2048)])
+def test_nan_and_infinity_stay_in_their_matrix(dr, b, r, c):
+    """Groups of processors that take matrices in turns, on the buffers of the one before, and matrices side by side: what is clean comes out
+    with the same bits, whatever its neighbours held."""
+    import torch
+    u = gaussian(b + r, b, r, c)
+    clean = update(dr, u)
+    spoilt = {0: float("nan"), 1: float("inf"), b // 2: float("-inf")} if b > 3 else {0: float("nan")}
+    for i, x in spoilt.items():
+        u[i, (7 * i) % r, (11 * i + c - 1) % c] = x
+    o = update(dr, u)
+    for i in range(b):
+        if i in spoilt:
+            assert bool(torch.isnan(o[i]).all()), f"matrix {i}"
+        else:
+            assert torch.equal(o[i], clean[i]), f"matrix {i}"
+
+
+@pytest.mark.parametrize("b,r,c", [(1, 1000, 2048), (1, 512, 2048), (1, 2048, 2048), (1, 512, 13200), (9, 144, 816), (200, 100, 300)])
+def test_captured_graph_and_late_input(dr, b, r, c):
+    """Launches with and without the kernel in front, replayed from a graph; and on a stream whose input comes late."""
+    import torch
+    u = gaussian(b + c, b, r, c)
+    ref, o = (torch.zeros((b, r, c), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ws = torch.empty(dr.dr_orthogonalise_workspace_bytes(b, r, c), dtype=torch.uint8, device="cuda")
+    call = lambda x, out, stream=None: dr.dr_orthogonalise(b, r, c, x, 5, None, 1e-7, out, ws, ws.numel(), dr.DR_NS_G_F32, stream)
+    call(u, ref)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(u, o)
+    for _ in range(3):
+        o.zero_()
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, ref)
+    side, late, big = torch.cuda.Stream(), torch.zeros_like(u), torch.randn(4096, 4096, device="cuda")
+    o.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(4):
+            big = big @ big * 1e-4
+        late.copy_(u)
+    call(late, o, side)
+    side.synchronize()
+    assert torch.equal(o, ref)
+    assert dr.dr_device_status()[0] == 0
