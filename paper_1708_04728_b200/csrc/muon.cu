@@ -504,9 +504,9 @@ __device__ __forceinline__ void ns_group_sync(const NsParams& p, NsShared& sh, i
 
 // 8 (or 1) values of X_0 from U
 template <int CN>
-__device__ __forceinline__ void ns_put_x(__half* hi, __half* lo, float inv, float* u) {
+__device__ __forceinline__ void ns_put_x(__half* hi, __half* lo, NsFactor by, float* u) {
 #pragma unroll
-    for (int c = 0; c < CN; ++c) u[c] *= inv;
+    for (int c = 0; c < CN; ++c) u[c] = u[c] * by.first * by.second;
     if (CN == 8) {
         uint32_t h[4], l[4];
         ns_split<8>(u, h, l);
@@ -531,7 +531,7 @@ __device__ __forceinline__ void ns_get_x8(const __half* hi, const __half* lo, fl
 // X_0 from U (LOAD) or the result from X.  Rows lie alike in both unless U is tall: a warp takes up to 1024 columns of a row.
 // A tall U is transposed through a 64 x 64 tile in shared memory.
 template <bool LOAD>
-__device__ __forceinline__ void ns_convert(const NsParams& p, float* tile, int group, int rank, size_t base, int src, float inv) {
+__device__ __forceinline__ void ns_convert(const NsParams& p, float* tile, int group, int rank, size_t base, int src, NsFactor by) {
     const NsInput& in = p.in;
     __half* hi = p.hi[src] + (size_t)group * p.n * p.ldx;
     __half* lo = p.lo + (size_t)group * p.n * p.ldx;
@@ -549,7 +549,7 @@ __device__ __forceinline__ void ns_convert(const NsParams& p, float* tile, int g
                     float f[8];
                     if (LOAD) {
                         ns_value<8>(in, o + c, f);
-                        ns_put_x<8>(hi + x + c, lo + x + c, inv, f);
+                        ns_put_x<8>(hi + x + c, lo + x + c, by, f);
                     } else {
                         ns_get_x8(hi + x + c, lo + x + c, f);
                         ns_put_o<8>(in, o + c, f);
@@ -561,7 +561,7 @@ __device__ __forceinline__ void ns_convert(const NsParams& p, float* tile, int g
                     float f[1];
                     if (LOAD) {
                         ns_value<1>(in, o + c, f);
-                        ns_put_x<1>(hi + x + c, lo + x + c, inv, f);
+                        ns_put_x<1>(hi + x + c, lo + x + c, by, f);
                     } else {
                         f[0] = (__half2float(hi[x + c]) + __half2float(lo[x + c])) * (1.f / NS_SCALE);
                         ns_put_o<1>(in, o + c, f);
@@ -619,7 +619,7 @@ __device__ __forceinline__ void ns_convert(const NsParams& p, float* tile, int g
                     if (LOAD) f[k] = r0 + r + k < in.rows ? tile[(r + k) * 65 + c] : 0.f;
                     else tile[(r + k) * 65 + c] = f[k];
                 }
-                if (LOAD) ns_put_x<8>(hi + x, lo + x, inv, f);
+                if (LOAD) ns_put_x<8>(hi + x, lo + x, by, f);
             }
         };
         __syncthreads();
@@ -694,8 +694,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
         }
         double s = 0.;
         for (int i = lane; i < p.n_norm; i += 32) s += norm[i];
-        const float inv = (float)((double)NS_SCALE / (sqrt(ns_warp_sum(s)) + (double)p.in.eps));
-        ns_convert<true>(p, tile, group, rank, base, 0, inv);
+        ns_convert<true>(p, tile, group, rank, base, 0, ns_factor(ns_warp_sum(s), p.in.eps));
         ns_group_sync(p, sh, group, epoch);
         int src = 0;
         for (int k = 0; k < p.steps; src ^= 1) {
@@ -749,7 +748,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
             ns_group_sync(p, sh, group, epoch);
             k += two ? 2 : 1;
         }
-        ns_convert<false>(p, tile, group, rank, base, src, 0.f);
+        ns_convert<false>(p, tile, group, rank, base, src, NsFactor{});
         ns_group_sync(p, sh, group, epoch);     // the buffers are free for the group's next matrix
     }
     if (sh.abort) {                             // copies and products in flight end within microseconds; then the CTA may go

@@ -157,6 +157,15 @@ __device__ __forceinline__ double ns_warp_sum(double s) {
     return s;
 }
 
+// X_0 = U / (|U|_F + eps), times NS_SCALE: u * first * second.  The quotient alone leaves float32's normal range where the norm is below 1.2e-35 or
+// above 3.4e41; a power of two in front (exact, but for entries 2^-110 times the norm) keeps both factors inside it for every size of U.
+struct NsFactor { float first, second; };
+__device__ __forceinline__ NsFactor ns_factor(double squares, float eps) {
+    const double d = sqrt(squares) + (double)eps;
+    const double first = d < 0x1p-64 ? 0x1p100 : d > 0x1p64 ? 0x1p-80 : 1.;
+    return {(float)first, (float)((double)NS_SCALE / (d * first))};
+}
+
 // 8 (or 1) values of the result: O, or the update of w
 template <int CN>
 __device__ __forceinline__ void ns_put_o(const NsInput& in, size_t at, float* o) {

@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
         meet();
         s = 0.;
         for (int i = 0; i < p.G; ++i) s += sh.norm[i];
-        const float inv = (float)((double)NS_SCALE / (sqrt(s) + (double)p.in.eps));
+        const NsFactor by = ns_factor(s, p.in.eps);
 #pragma unroll 1
         for (int u = threadIdx.x; u < p.n * units; u += NSS_THREADS) {
             const int i = u / units, w = u - i * units;
@@ -284,8 +284,8 @@ __global__ void __launch_bounds__(NSS_THREADS, 1) ns_small_kernel(const __grid_c
             nss_ld(X + xlo, i, w, l);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                f[k] = __uint_as_float(h[k]) * inv;
-                f[4 + k] = __uint_as_float(l[k]) * inv;
+                f[k] = __uint_as_float(h[k]) * by.first * by.second;
+                f[4 + k] = __uint_as_float(l[k]) * by.first * by.second;
             }
             ns_split<8>(f, h, l);
             nss_st_rows(X, i, w, h, twice);

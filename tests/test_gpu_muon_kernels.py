@@ -173,3 +173,15 @@ def test_captured_graph_and_late_input(dr, b, r, c):
     side.synchronize()
     assert torch.equal(o, ref)
     assert dr.dr_device_status()[0] == 0
+
+
+@pytest.mark.parametrize("r,c", [(40, 72), (96, 224), (33, 65), (160, 352), (300, 171), (4200, 60)])
+def test_any_size_of_the_gradient(dr, r, c):
+    """Norms from the smallest numbers float32 holds to the largest, without eps; all zeros with the smallest eps."""
+    import torch
+    for scale in (1e-43, 1e-39, 1e-36, 1e-20, 1e20, 1e37):
+        u = (gaussian(r, 1, r, c).double() * scale).float()
+        assert bool(torch.isfinite(u).all()) and float(u.abs().max()) > 0
+        assert error(update(dr, u, 5, None, 0.0)[0], u[0], 5, None, 0.0) <= (FEW_ROWS if min(r, c) <= 64 else RANDOM), scale
+    for eps in (1e-30, 1e-36, 1e-40, 1e-45):
+        assert bool((update(dr, torch.zeros((1, r, c), device="cuda"), 5, None, eps) == 0).all()), eps
