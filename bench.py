@@ -362,8 +362,9 @@ def run_finetune(args):
         gamma, beta = torch.ones(cout, device="cuda"), torch.zeros(cout, device="cuda")
         mean, rstd = torch.empty(npix, device="cuda"), torch.empty(npix, device="cuda")
         ln_ws = torch.empty(dr.dr_layernorm_bwd_workspace_bytes(npix, cout), dtype=torch.uint8, device="cuda")
-        norm = lambda: dr.dr_layernorm(npix, cout, y, 0, gamma, beta, 1e-5, dz, 0, mean, rstd)
-        norm_bwd = lambda: dr.dr_layernorm_bwd(npix, cout, yt, 0, y, 0, gamma, mean, rstd, dz, 0, db, db, ln_ws, ln_ws.numel())
+        dgamma, dbeta, normed = torch.empty_like(gamma), torch.empty_like(beta), torch.empty_like(yt)      # its own: the step's buffers stay as they are
+        norm = lambda: dr.dr_layernorm(npix, cout, y, 0, gamma, beta, 1e-5, normed, 0, mean, rstd)
+        norm_bwd = lambda: dr.dr_layernorm_bwd(npix, cout, yt, 0, y, 0, gamma, mean, rstd, normed, 0, dgamma, dbeta, ln_ws, ln_ws.numel())
         t = {}
         for what, fn in (("step", step), ("step_graph", graph.replay), ("wgrad", wgrad), ("forward", fwd), ("muon", muon), ("layernorm", norm),
                          ("layernorm_bwd", norm_bwd)):

@@ -387,7 +387,7 @@ int dr_layernorm(size_t npix, int C, const void* x, int ldx, const float* gamma,
                  int ldy, float* mean, float* rstd, unsigned flags, void* stream);
 /* The gradients, from the statistics the forward pass wrote.  With t = dy * gamma and xhat = (x - mean) * rstd,
  *   dx = rstd * (t - mean_c(t) - xhat * mean_c(t * xhat)),   dgamma = sum_rows dy * xhat,   dbeta = sum_rows dy.
- *  dx may be dy or x itself (same type and ld).  dgamma, dbeta: float32 [C], overwritten, or NULL; both NULL: no
+ *  dx may be dy or x itself (same type and ld).  dgamma, dbeta: float32 [C] each, overwritten, or NULL; both NULL: no
  *  workspace is needed.  Sums over the rows are taken in a fixed order: the same result on every run.
  *  workspace: dr_layernorm_bwd_workspace_bytes(npix, C) bytes, 256-byte aligned, contents irrelevant.
  *  npix = 0 writes zeros to dgamma and dbeta.

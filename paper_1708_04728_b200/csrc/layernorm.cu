@@ -720,6 +720,7 @@ extern "C" int dr_layernorm_bwd(size_t npix, int C, const void* dy, int lddy, co
     size_t need = 0;
     dr_layernorm_bwd_workspace_bytes(npix, C, &need);
     if (sums && workspace_bytes < need) return DR_ERR_WORKSPACE;
+    if (sums && dgamma == dbeta) return DR_ERR_INVALID_ARG;         // two writers of one buffer
     cudaStream_t s = (cudaStream_t)stream;
     if (npix == 0) {            // an empty sum
         if (dgamma && cudaMemsetAsync(dgamma, 0, (size_t)C * sizeof(float), s) != cudaSuccess) return DR_ERR_CUDA;
