@@ -378,7 +378,9 @@ int dr_regress_shard_grads(const dr_conv_desc* desc, int B, int batch, int H, in
  *  bfloat16, or float32 with DR_LN_X_F32; y (and dy) bfloat16, or float32 with DR_LN_Y_F32.  gamma, beta: float32 [C],
  *  or NULL (1 and 0).  mean, rstd: float32 [npix], or NULL where no backward pass follows.  y may be x itself (same
  *  type and ldx = ldy).  Sums are float32: the mean first, then the squared distances from it.  Any C; rows need
- *  only their type's alignment, and 16-byte aligned rows of a multiple of 8 channels take 16-byte accesses.
+ *  only their type's alignment.  Accesses of 16 bytes (of the wider type) are taken up to C = 8192 where in any one row all
+ *  tensors are the same number of elements off a multiple of 8 (4 where one of them is float32); other rows go element by
+ *  element.
  *  A row that holds a NaN or an infinity gives a row of NaN and touches no other row.
  * Errors: INVALID_ARG (nulls, C <= 0, ld < C, eps < 0, unknown flags), ALIGNMENT.                                    */
 #define DR_LN_X_F32 0x1u

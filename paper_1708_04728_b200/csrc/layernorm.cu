@@ -38,7 +38,8 @@ struct LnParams {
     float *dgamma, *dbeta;
 };
 
-// How a row lies in memory.  ALIGNED: every row of every tensor starts on a 16-byte boundary and C is a multiple of 8.
+// How a row lies in memory, in vectors of 8 elements where all tensors are bfloat16 and of 4 where one is float32 (16 bytes of the widest
+// type).  ALIGNED: every row of every tensor is a whole number of vectors from a vector's boundary on.
 // PHASED: rows start anywhere, but all tensors are off the boundary by the same number of elements in any one row, and a
 // team takes rows a multiple of 8 apart, so that its offset never changes: whole vectors from the first boundary on, and
 // the few channels in front of it and behind the last vector one to a thread.  SINGLE: neither; single elements.
@@ -615,13 +616,16 @@ static bool ln_aligned(const void* p, bool f32) { return ((uintptr_t)p & (f32 ? 
 // the mode of a call whose tensors have these addresses and row strides (in elements of 4 or 2 bytes)
 struct LnRowsAt { const void* p; int ld; bool f32; };
 static int ln_mode(int C, std::initializer_list<LnRowsAt> ts) {
-    bool aligned = (C & 7) == 0, phased = true;
+    unsigned mask = 7;                          // elements of a vector, less one
+    for (const LnRowsAt& t : ts)
+        if (t.f32) mask = 3;
+    bool aligned = (C & mask) == 0, phased = true;
     const LnRowsAt& a = *ts.begin();
     const uintptr_t first = (uintptr_t)a.p / (a.f32 ? 4 : 2);
     for (const LnRowsAt& t : ts) {
         const uintptr_t at = (uintptr_t)t.p / (t.f32 ? 4 : 2);
-        aligned = aligned && (at & 7) == 0 && (t.ld & 7) == 0;
-        phased = phased && ((at - first) & 7) == 0 && ((t.ld - a.ld) & 7) == 0;
+        aligned = aligned && (at & mask) == 0 && (t.ld & mask) == 0;
+        phased = phased && ((at - first) & mask) == 0 && ((t.ld - a.ld) & mask) == 0;
     }
     return aligned ? LN_ALIGNED : phased ? LN_PHASED : LN_SINGLE;
 }
