@@ -412,7 +412,13 @@ __global__ void __launch_bounds__(LN_BWD_THREADS, 1) ln_backward_kernel(const Ln
             nmean = more ? ma[(it + 1) * t.step] : 0.f;
             nrstd = more ? ra[(it + 1) * t.step] : 0.f;
         }
-        // channels past the row have dy = 0, and so no part in any sum
+        // Channels past the row have x = dy = 0, and so no part in any sum, unless mean * rstd passes float32's range: then x = mean there.
+        // (46000 x 1101 98 -> 100 us by this test, 122 by a select for each vector, 125 by leaving the empty vectors out; 154000 x 333 77 -> 77, 76, 100.)
+        if (!(fabsf(mean * rstd) < INFINITY)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < V * E ? !at.in(i / E) : i > V * E || !at.single) h[i] = mean;
+        }
         float2 s1 = f2(0.f), s2 = s1;
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {

@@ -49,3 +49,31 @@ def test_float32_rows_four_elements_apart(dr, M, C, whole, xf32, yf32):
     for r in results[1:]:
         for name, a, e in zip(("y", "mean", "rstd", "dx", "dgamma", "dbeta"), r, results[0]):
             assert torch.equal(a, e), name
+
+
+@pytest.mark.parametrize("yf32", [True, False])
+@pytest.mark.parametrize("C,pad", [(3, 0), (20, 0), (100, 0), (333, 0), (333, 1), (513, 0), (1000, 0), (1030, 3), (3001, 2), (6000, 0), (8191, 0), (9000, 0)])
+def test_backward_of_a_constant_row_far_from_zero(dr, C, pad, yf32):
+    """x = mean throughout and 1/sqrt(eps) = 1e6: xhat is zero, though mean / sqrt(eps) passes float32's range; dx is that of the centred gradient."""
+    import torch
+    M, eps = 5, 1e-12
+    x = S.normal(0, f"cr{C}", (M, C)).astype("float32")
+    x[1], x[3] = 1e33, -2e33
+    dyt = dev(S.normal(0, f"crd{C}", (M, C)), yf32)
+    g = dev(1 + 0.2 * S.normal(0, f"crg{C}", (C,)), True)
+    x64 = torch.from_numpy(x).cuda().double()
+    mean = x64.mean(1).float()
+    mean[1], mean[3] = 1e33, -2e33
+    rstd = (1 / (((x64 - mean.double()[:, None]) ** 2).mean(1) + eps).sqrt()).float()
+    xv, dx = at(dev(x, True), 0, C + pad), torch.empty((M, C), device="cuda")
+    dg, db = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    ws = torch.empty(dr.dr_layernorm_bwd_workspace_bytes(M, C), dtype=torch.uint8, device="cuda")
+    dr.dr_layernorm_bwd(M, C, dyt, 0, xv, C + pad, g, mean, rstd, dx, 0, dg, db, ws, ws.numel(), dr.DR_LN_X_F32 | dr.DR_LN_Y_F32 * yf32)
+    h = (xv.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    t = dyt.double() * g.double()
+    ref = rstd.double()[:, None] * (t - t.mean(1, keepdim=True) - h * (t * h).mean(1, keepdim=True))
+    # 64 rounding errors of 2^-24 on the sizes of the summands, as everywhere for these sums
+    tol = 64 * 2.0 ** -24 * rstd.double()[:, None] * (t.abs() + t.abs().mean(1, keepdim=True) + h.abs() * (t * h).abs().mean(1, keepdim=True))
+    assert bool(((dx.double() - ref).abs() <= tol).all())
+    assert bool(((dg.double() - (dyt.double() * h).sum(0)).abs() <= 64 * 2.0 ** -24 * (dyt.double() * h).abs().sum(0)).all())
+    assert bool(((db.double() - dyt.double().sum(0)).abs() <= 64 * 2.0 ** -24 * dyt.double().abs().sum(0)).all())
