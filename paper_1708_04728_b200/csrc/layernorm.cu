@@ -475,22 +475,23 @@ __global__ void __launch_bounds__(LN_BWD_THREADS, 1) ln_backward_kernel(const Ln
 template <typename TI, typename TO>
 __global__ void __launch_bounds__(512) ln_forward_long_kernel(const LnParams p) {
     __shared__ float2 slots[2][16];
+    const unsigned C = p.C;                     // positions past C, and the backward pass' second half of sums, pass 31 bits
     int buf = 0;
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     for (size_t r = blockIdx.x; r < p.M; r += gridDim.x) {
         float s[1] = {0.f};
-        for (int c = threadIdx.x; c < p.C; c += 512) s[0] += ln_value(((const TI*)p.x)[r * p.ldx + c]);
+        for (unsigned c = threadIdx.x; c < C; c += 512) s[0] += ln_value(((const TI*)p.x)[r * p.ldx + c]);
         ln_team_sum<512>(s, slots, buf);
         const float mean = s[0] * p.inv_c;
         s[0] = 0.f;
-        for (int c = threadIdx.x; c < p.C; c += 512) {
+        for (unsigned c = threadIdx.x; c < C; c += 512) {
             const float d = ln_value(((const TI*)p.x)[r * p.ldx + c]) - mean;
             s[0] = fmaf(d, d, s[0]);
         }
         ln_team_sum<512>(s, slots, buf);
         const float rstd = rsqrtf(fmaf(s[0], p.inv_c, p.eps));
-        for (int c = threadIdx.x; c < p.C; c += 512) {
+        for (unsigned c = threadIdx.x; c < C; c += 512) {
             const float v = fmaf((ln_value(((const TI*)p.x)[r * p.ldx + c]) - mean) * rstd, p.gamma ? p.gamma[c] : 1.f, p.beta ? p.beta[c] : 0.f);
             ln_store1((TO*)p.y + r * p.ldy + c, v);
         }
@@ -504,29 +505,31 @@ __global__ void __launch_bounds__(512) ln_forward_long_kernel(const LnParams p) 
 template <typename TI, typename TO>
 __global__ void __launch_bounds__(512) ln_backward_long_kernel(const LnParams p) {
     __shared__ float2 slots[2][16];
+    const unsigned C = p.C;                     // positions past C, and the backward pass' second half of sums, pass 31 bits
     int buf = 0;
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    float* sg = p.partials ? p.partials + (size_t)blockIdx.x * 2 * p.C : nullptr;
+    float* sg = p.partials ? p.partials + (size_t)blockIdx.x * 2 * C : nullptr;
+    float* sb = sg ? sg + C : nullptr;
     if (sg)
-        for (int c = threadIdx.x; c < p.C; c += 512) sg[c] = sg[p.C + c] = 0.f;
+        for (unsigned c = threadIdx.x; c < C; c += 512) sg[c] = sb[c] = 0.f;
     for (size_t r = blockIdx.x; r < p.M; r += gridDim.x) {
         const float mean = p.mean_in[r], rstd = p.rstd_in[r];
         float s[2] = {0.f, 0.f};
-        for (int c = threadIdx.x; c < p.C; c += 512) {
+        for (unsigned c = threadIdx.x; c < C; c += 512) {
             const float d = ln_value(((const TO*)p.dy)[r * p.ldy + c]), h = (ln_value(((const TI*)p.x)[r * p.ldx + c]) - mean) * rstd;
             const float t = d * (p.gamma ? p.gamma[c] : 1.f);
             s[0] += t;
             s[1] = fmaf(t, h, s[1]);
             if (sg) {
                 sg[c] = fmaf(d, h, sg[c]);
-                sg[p.C + c] += d;
+                sb[c] += d;
             }
         }
         ln_team_sum<512>(s, slots, buf);
         s[0] *= p.inv_c;
         s[1] *= p.inv_c;
-        for (int c = threadIdx.x; c < p.C; c += 512) {
+        for (unsigned c = threadIdx.x; c < C; c += 512) {
             const float t = ln_value(((const TO*)p.dy)[r * p.ldy + c]) * (p.gamma ? p.gamma[c] : 1.f), h = (ln_value(((const TI*)p.x)[r * p.ldx + c]) - mean) * rstd;
             const float v = rstd * (t - fmaf(h, s[1], s[0]));
             ln_store1((TI*)p.dx + r * p.lddx + c, v);
@@ -539,19 +542,20 @@ __global__ void __launch_bounds__(512) ln_join_kernel(const LnParams p) {
     __shared__ float red[16][32];
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    const int i = blockIdx.x * 32 + (threadIdx.x & 31), q = threadIdx.x >> 5;
+    const size_t C = p.C, i = (size_t)blockIdx.x * 32 + (threadIdx.x & 31);
+    const int q = threadIdx.x >> 5;
     float s = 0.f;
-    if (i < 2 * p.C) {
+    if (i < 2 * C) {
 #pragma unroll 10
-        for (int k = q; k < p.n_part; k += 16) s += p.partials[(size_t)k * 2 * p.C + i];
+        for (int k = q; k < p.n_part; k += 16) s += p.partials[k * 2 * C + i];
     }
     red[q][threadIdx.x & 31] = s;
     __syncthreads();
-    if (q == 0 && i < 2 * p.C) {
+    if (q == 0 && i < 2 * C) {
 #pragma unroll
         for (int k = 1; k < 16; ++k) s += red[k][threadIdx.x];
-        float* out = i < p.C ? p.dgamma : p.dbeta;
-        if (out) out[i < p.C ? i : i - p.C] = s;
+        float* out = i < C ? p.dgamma : p.dbeta;
+        if (out) out[i < C ? i : i - C] = s;
     }
 }
 

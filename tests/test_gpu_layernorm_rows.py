@@ -77,3 +77,28 @@ def test_backward_of_a_constant_row_far_from_zero(dr, C, pad, yf32):
     assert bool(((dx.double() - ref).abs() <= tol).all())
     assert bool(((dg.double() - (dyt.double() * h).sum(0)).abs() <= 64 * 2.0 ** -24 * (dyt.double() * h).abs().sum(0)).all())
     assert bool(((db.double() - dyt.double().sum(0)).abs() <= 64 * 2.0 ** -24 * dyt.double().abs().sum(0)).all())
+
+
+def test_one_row_of_the_most_channels(dr):
+    """Two to the 31st less one: positions in the row and the stride behind them pass 31 bits."""
+    import torch
+    C = 2 ** 31 - 1
+    x = torch.tensor([1.0, -1.0], dtype=torch.bfloat16, device="cuda").repeat(2 ** 30)[:C]
+    y, mean, rstd = torch.empty_like(x), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    dr.dr_layernorm(1, C, x, 0, None, None, 0.0, y, 0, mean, rstd)
+    # mean 1 / C, variance 1; a thread's sums are whole numbers below 2^24, their join is rounded as every mean here: 64 errors of 2^-24 of mean |x|
+    assert torch.equal(y, x)
+    assert abs(float(mean) - 1 / C) <= 64 * 2.0 ** -24 and abs(float(rstd) - 1) <= 64 * 2.0 ** -24
+
+
+def test_weight_gradients_of_a_row_of_2_to_the_30_channels(dr):
+    import torch
+    C = 2 ** 30
+    pattern = lambda *v: torch.tensor(v, dtype=torch.bfloat16, device="cuda").repeat(C // 4)
+    x, dy = pattern(1.0, -1.0, 1.0, -1.0), pattern(1.0, 2.0, 3.0, 4.0)
+    dx, dg, db = torch.empty_like(x), torch.full((C,), float("nan"), device="cuda"), torch.full((C,), float("nan"), device="cuda")
+    ws = torch.empty(dr.dr_layernorm_bwd_workspace_bytes(1, C), dtype=torch.uint8, device="cuda")
+    dr.dr_layernorm_bwd(1, C, dy, 0, x, 0, None, torch.zeros(1, device="cuda"), torch.ones(1, device="cuda"), dx, 0, dg, db, ws, ws.numel())
+    # mean of dy 2.5, of dy xhat -0.5: dx = dy - 2.5 + 0.5 x
+    assert torch.equal(dx, pattern(-1.0, -1.0, 1.0, 1.0))
+    assert torch.equal(db, dy.float()) and torch.equal(dg, dy.float() * x.float())
