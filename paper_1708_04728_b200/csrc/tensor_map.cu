@@ -68,11 +68,14 @@ bool lookup(const Key& k, CUtensorMap* out) {
     return true;
 }
 void remember(const Key& k, const CUtensorMap* m) {
-    std::lock_guard<std::mutex> lock(g_mu);
-    if (g_memo.size() >= MAX_ENTRIES) g_memo.clear();
     Map64 v;
     std::memcpy(&v.m, m, sizeof(CUtensorMap));
-    g_memo.emplace(k, v);
+    try {
+        std::lock_guard<std::mutex> lock(g_mu);
+        if (g_memo.size() >= MAX_ENTRIES) g_memo.clear();
+        g_memo.emplace(k, v);
+    } catch (...) {             // no memory for the table: encoded again next time, nothing may leave a C entry
+    }
 }
 }  // namespace
 
@@ -121,12 +124,17 @@ long long tmap_driver_encodes() { return g_driver_encodes.load(std::memory_order
 
 // Integer tunable from the environment (for A/B timing); the environment is read once per name.
 int tunable(const char* name, int dflt) {
-    std::lock_guard<std::mutex> lock(g_mu);
-    auto it = g_tunables.find(name);
-    if (it != g_tunables.end()) return it->second == INT32_MIN ? dflt : it->second;
-    const char* v = getenv(name);
-    g_tunables.emplace(name, v ? atoi(v) : INT32_MIN);
-    return v ? atoi(v) : dflt;
+    try {
+        std::lock_guard<std::mutex> lock(g_mu);
+        auto it = g_tunables.find(name);
+        if (it != g_tunables.end()) return it->second == INT32_MIN ? dflt : it->second;
+        const char* v = getenv(name);
+        g_tunables.emplace(name, v ? atoi(v) : INT32_MIN);
+        return v ? atoi(v) : dflt;
+    } catch (...) {             // no memory for the table
+        const char* v = getenv(name);
+        return v ? atoi(v) : dflt;
+    }
 }
 
 }  // namespace dr
