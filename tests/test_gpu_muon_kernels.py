@@ -185,3 +185,13 @@ def test_any_size_of_the_gradient(dr, r, c):
         assert error(update(dr, u, 5, None, 0.0)[0], u[0], 5, None, 0.0) <= (FEW_ROWS if min(r, c) <= 64 else RANDOM), scale
     for eps in (1e-30, 1e-36, 1e-40, 1e-45):
         assert bool((update(dr, torch.zeros((1, r, c), device="cuda"), 5, None, eps) == 0).all()), eps
+
+
+@pytest.mark.parametrize("b,r,c", [(150, 4, 4096), (150, 4, 65536), (150, 65536, 3), (75, 7, 40000), (1, 4, 65536), (1, 60, 65536), (3, 65536, 66)])
+def test_the_longest_rows(dr, b, r, c):
+    """Float32 sums along the longest side the calls take, by one processor and by many."""
+    u = gaussian(b + r + c, b, r, c)
+    o = update(dr, u)
+    few = min(r, c) <= 64 and (b == 1 or max(r, c) <= 4096)
+    for i in {0, b - 1}:
+        assert error(o[i], u[i]) <= (FEW_ROWS if few else RANDOM)
