@@ -409,15 +409,17 @@ int dr_layernorm_bwd(size_t npix, int C, const void* dy, int lddy, const void* x
  *  more; all of them where min(rows, cols) <= 64) and sum in float32.  Relative error of O after five steps (Frobenius,
  *  before it is rounded to bfloat16): 1e-4 .. 1e-3 for matrices of normal values, up to 4e-3 where the singular values of U
  *  spread over many decades or its rank is low, up to 1e-2 where U is a single direction (rounding errors then add up instead
- *  of averaging: 8e-3 with 65 rows, 2e-3 with 256, 1e-3 with 512).  Where min(rows, cols) <= 64: below 1e-4 for a single matrix and up to a long side of
- *  4096, below 1e-3 for any (a batch of 150 and more leaves one CTA to a matrix, and its float32 sums err with their length: 1.2e-4
- *  at 12000, 8.4e-4 at 65536).
+ *  of averaging: 8e-3 with 65 rows, 2e-3 with 256, 1e-3 with 512).  Where min(rows, cols) <= 64: below 1e-4 for a single
+ *  matrix and up to a long side of 4096, below 1e-3 for any (a batch of 150 and more leaves one CTA to a matrix, and its
+ *  float32 sums err with their length: 1.2e-4 at 12000, 8.4e-4 at 65536).
  *  X is kept in float16 times 4096, A and the polynomial in float16: with coefficients that let a singular value of X reach
  *  16, or an entry of the others 65504, O is not finite.
  *  An all-zero U gives zeros (eps > 0); a matrix with a NaN or an infinity gives NaN and touches no other matrix.
  * dr_orthogonalise: g bfloat16, or float32 with DR_NS_G_F32; o bfloat16; both [batch][rows][cols].
  *  workspace: dr_orthogonalise_workspace_bytes bytes, 256-byte aligned, contents irrelevant; calls that may overlap on
- *  the GPU need their own.
+ *  the GPU need their own.  With n = min(rows, cols), m = max, M and N their multiples of 64, about 6 n M + 8 n N bytes for each
+ *  matrix worked on at a time (dr_orthogonalise_plan), 18 n N instead of 8 where X takes two steps at a time (4096 x 9216: 529 MB),
+ *  and the parts of X X^T where the plan splits it; where X stays in shared memory 4 n n, and 512 n for each CTA of a matrix.
  * Errors: INVALID_ARG, UNSUPPORTED (the limits above), ALIGNMENT, WORKSPACE, CUDA.                                   */
 #define DR_NS_G_F32     0x1u
 #define DR_NS_MAX_STEPS 16

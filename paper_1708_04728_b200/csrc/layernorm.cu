@@ -9,11 +9,13 @@
 // registers, and have the next rows' loads in flight while they work on this one.
 //
 // Measured on a B200 against a copy of 1 Gi elements at 6530 GB/s.  200704 rows x 256 channels, bfloat16: forward 38 us
-// (5.4 TB/s, 0.83 of that copy; a copy of these 206 MB takes 35 us), backward 56 us (5.5 TB/s, 0.84); with loads straight into
+// (5.4 TB/s, 0.83 of that copy; a copy of these 206 MB takes 35 us), backward 57 us (5.4 TB/s, 0.83); with loads straight into
 // registers, one row ahead, they took 90 and 241 us.  12544 x 2048, float32 x and dx: backward 48 us (5.4 TB/s, 0.82).
-// 50176 x 333 inside rows of 501 (no row but every eighth aligned): forward 16 us (4.1 TB/s), bound by instruction issue:
-// the channels outside the vectors cost a load, a store and the selects of a whole vector.  49 x 1024: 5.3 and 8.3 us, the
-// launches (a kernel that does nothing takes 2 us between its neighbours; the backward pass has two).
+// 50176 x 333 inside rows of 501 (no row but every eighth aligned): forward 16 us (4.1 TB/s), backward 35 us.  Neither memory
+// (29 % in the forward pass) nor the issue slots (47 %) are full: latency, with 114 registers a thread and so 16 warps on an
+// SM.  Of the 207 kernels here 32 of the backward pass spill 4 .. 36 bytes at 128 registers, all phased ones of 16 channels a
+// thread among them, and one of the forward pass 4.  49 x 1024: 5.5 and 8.3 us, the launches (a kernel that does nothing
+// takes 2 us between its neighbours; the backward pass has two).
 #include <algorithm>
 #include <initializer_list>
 #include <map>
@@ -47,7 +49,7 @@ enum { LN_ALIGNED, LN_PHASED, LN_SINGLE };
 
 constexpr int LN_BWD_THREADS = 512;
 constexpr size_t LN_SMEM_MAX = 216 * 1024;
-// Rows a thread has on their way besides the one it works on (ALIGNED: copied to shared memory by cp.async, each thread
+// Rows a thread has on their way besides the one it works on (ALIGNED and PHASED: copied to shared memory by cp.async, each thread
 // its own vectors, so that no barrier is needed): 24 KB or more in flight per SM at all times.
 __host__ __device__ constexpr int ln_ring(int bytes_per_row) { return bytes_per_row <= 96 ? 4 : 3; }
 

@@ -12,21 +12,24 @@
 //    With the whole of A in float16 the relative error of O is 2e-3 .. 4e-3 (random matrices); with the split 1e-4 .. 9e-4, at most
 //    1.3e-3 (512 rows) .. 2.3e-3 (130 rows, two steps at a time) for spectra over up to six decades, 1.2e-3 (512) .. 3.8e-3 (65 rows) for
 //    ranks of 2 .. 16, and 1e-3 (512) .. 8e-3 (65 rows) for a single direction, where rounding errors do not average.
-//  - Products symmetric by construction (A, E E) are computed for the lower triangle and mirrored, so they stay symmetric.
+//  - A and E E are symmetric.  Where a group has a CTA for every tile, all are computed; otherwise those that reach the lower triangle, and
+//    mirrored.  (Products of two different polynomials, two steps at a time, are symmetric up to rounding in the first case.)
 // bfloat16 operands would cost 2e-3 .. 6e-3 even so: more than the rounding of O to bfloat16 itself.
 //
 // Execution.  One persistent kernel runs all products of a matrix: a group of G CTAs (one per SM) works through the phases
 // A -> F -> X of every step and meets at a barrier between them; a batch is spread over the groups.  Inside a phase a CTA is a
 // pipeline: one warp loads 128-deep operand slices by TMA, two issue tcgen05.mma into one of two sets of accumulators in
-// tensor memory, eight drain the other one.  A group of up to 16 CTAs is a thread-block cluster and uses its barrier; a larger one is
-// launched cooperatively and counts arrivals in global memory.  Where A has few tiles, its long axis is divided: over the CTAs of a
+// tensor memory, eight drain the other one.  A group of up to 16 CTAs is a thread-block cluster and uses its barrier, where the device holds
+// a cluster for every matrix and a power of two of CTAs leaves at most a quarter of them unused; others are launched cooperatively and
+// count arrivals in global memory.  Where A has few tiles, its long axis is divided: over the CTAs of a
 // cluster that exchange their parts through each other's shared memory, or over all CTAs with a phase more to sum the parts.
 //
-// Measured on a B200, five steps; flops of the formula with A and A A by their lower triangles, against 1650 TFLOP/s of a bfloat16 product:
-//   4096 x 9216   2.07 .. 2.4 ms (the clock falls with the power drawn), 0.78 .. 0.67 of that rate; the plain form in float32 takes
-//                 62.7 ms.  Bound by the tensor pipe and by whole rounds of tiles.
-//   2048 x 2048   337 us, 0.31: 64 tiles of 256 x 256 for 74 pairs, drains of 8 us behind MMAs of 10.
-//   1000 x 2048   175 us, 512 x 13200 with the optimiser's step 253 us, 512 x 2048 120 us, 6 x 256 x 2304 161 us, 192 x 576 101 us: 15 dependent
+// Measured on a B200, five steps; flops executed, with A and A A by their lower triangles, against 1650 TFLOP/s of a bfloat16 product:
+//   4096 x 9216   2.07 .. 2.48 ms (the clock falls with the power drawn), 0.63 .. 0.52 of that rate (2147 GFLOP, two steps of X at a time; the
+//                 formula's 2663 would be 0.78 .. 0.65); the plain form in float32 takes 62.7 ms.  A pair's slice is 512 cycles of MMAs against
+//                 700 of hand-over by its only issuing thread and as many for its operands out of L2; then whole rounds of tiles.
+//   2048 x 2048   336 us, 0.31: 64 tiles of 256 x 256 for 74 pairs, drains of 8 us behind MMAs of 10.
+//   1000 x 2048   176 us, 512 x 13200 with the optimiser's step 254 us, 512 x 2048 119 us, 6 x 256 x 2304 156 us (with the step 170), 192 x 576 101 us: 15 dependent
 //                 phases of 6 to 20 us each.  A phase is a barrier 1.3 .. 1.9 us, 0.5 .. 1 to its first MMA's operands, 0.8 of TMA latency, the MMAs, and
 //                 a drain of 1.3 .. 3; where all SMs load operands, the way out of L2 (12 TB/s).
 #include <algorithm>
@@ -838,7 +841,7 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     }
     p.G = g;
     p.groups = std::min(batch1, std::max(1, sms / g));
-    // Cycles of a phase, fitted on 15 shapes: its start, rounds of tiles over the group's CTAs, and the last tile's drain.  A round takes the longer of
+    // Cycles of a phase, by a model that ranks the choices below: its start, rounds of tiles over the group's CTAs, and the last tile's drain.  A round takes the longer of
     // its slices and the drain of the tile before it; a 64-deep slice the longest of its MMAs, the issuing threads' hand-over (one of
     // two threads, or a pair's only one) and its operands' way out of L2 (7000 bytes a cycle for all SMs).
     auto cost = [&](int tiles, int chunks, int nt, bool pair) {
@@ -889,9 +892,13 @@ static NsPlan ns_plan(int batch, int rows, int cols) {
     p.full_a = c.full_a; p.full_s = c.full_s; p.splits = c.splits; p.share = c.share;
     p.stage_bytes = ns_depth(p.pair) * (NS_CHUNK + std::max(p.nt_x, std::max(p.nt_s, p.nt_a)) * (p.pair ? 64 : 128));
     p.stages = std::min(NS_STAGES, (NS_SMEM - (p.share > 1 ? p.nt_a * 512 : 0)) / p.stage_bytes);
-    // Two steps of X at a time save one A and one X product of every two and cost three more n x n products, and a barrier each (512 x 13200:
-    // 270 -> 256 us, 4096 x 9216: 2.42 -> 2.12 ms, but 512 x 2048: 134 -> 150 us).  Rounding errors of A' are of A's size, not of its
-    // small entries': fine for one such step (1.5 times the error of O on spectra over four decades), not for a chain of them.
+    // Two steps of X at a time save one A and one X product of every two and cost three more n x n products, and a barrier each.  Taken where
+    // the model's saving is 7/5 of its cost, since it errs (saving over cost, one and two steps at a time, five steps in all):
+    //   512 x 2048 0.68 119 142 us, 1000 x 2048 0.95 176 193, 4096 x 4096 0.94 1497 1642, 512 x 4608 1.04 166 172, 2048 x 4608 1.22 504 496,
+    //   300 x 9000 1.33 168 173, 1024 x 4608 1.45 243 238, 512 x 8192 1.47 201 201, 512 x 13200 1.74 250 233, 4096 x 9216 1.82 2664 2379,
+    //   2048 x 8192 2.02 819 691, 640 x 20800 2.75 398 340, 40 x 130 x 4200 3.72 805 627.
+    // Rounding errors of A' are of A's size, not of its small entries': fine for one such step (up to twice the error of O on spectra over
+    // several decades: 1.3e-3 at 512 x 13200 against 7e-4 at 512 x 2048), not for a chain of them.
     p.merge = p.terms == 1 && 5 * (c.a + c.x + 2 * BARRIER) > 7 * 3 * (c.s + BARRIER);
     l.norm_blocks = (int)std::min<size_t>(NS_NORM_BLOCKS, ((size_t)rows * cols + 2047) / 2048);
     p.n_norm = p.cluster || g == 1 ? g : l.norm_blocks;

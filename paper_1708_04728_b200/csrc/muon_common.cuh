@@ -8,11 +8,14 @@
 namespace dr {
 using namespace ptx;
 
-constexpr float NS_SCALE = 4096.f;          // X is stored times this: entries of every size stay in float16's normal range
+// X is stored times this: entries from 1.5e-8 on are in float16's normal range, their low halves from 6e-5 on; smaller ones have fewer bits, and an
+// absolute error of at most 7e-12.
+constexpr float NS_SCALE = 4096.f;
 
-// Shared memory every CTA asks for, whether it needs it or not: what is left of its SM's is less than any kernel that uses tensor memory asks
-// for.  CTAs here wait for one another at cluster and grid barriers, so none of them may have to wait for tensor memory that another
-// CTA on its SM holds (and that one perhaps for a CTA of its own).  All 227 KB cost cache: 4096 x 9216 2.34 ms against 2.07, 192 x 576 105
+// Shared memory every CTA asks for, whether it needs it or not.  CTAs here wait for one another at cluster and grid barriers, so none of them may
+// have to wait for tensor memory that another CTA on its SM holds (and that one perhaps for a CTA of its own).  Today's registers (384
+// threads of 168, 512 of 128) leave no room for another CTA anyway; with this, no kernel that uses tensor memory fits beside one of these
+// whatever registers a compiler gives.  All 227 KB cost cache: 4096 x 9216 2.34 ms against 2.07, 192 x 576 105
 // against 102 us.
 constexpr int NS_SMEM_ALL = 193 * 1024;
 

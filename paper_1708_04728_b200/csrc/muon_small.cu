@@ -10,7 +10,7 @@
 //   F    every CTA computes E E (E: A without its diagonal) and the polynomial for itself,
 //   X    every CTA updates its slab in place.
 // Products and element-wise terms as in the kernel for larger matrices (muon.cu); with few rows rounding errors average less, so
-// matrices of up to 64 rows multiply hi hi + hi lo + lo hi: the tensor cores idle here either way (relative error of O 1e-6 .. 3e-5).
+// matrices of up to 64 rows multiply hi hi + hi lo + lo hi: the tensor cores idle here either way (relative error of O 1e-6 .. 3e-5, 7e-5 for a single direction).
 //
 // Measured on a B200, five steps: 64 x 147 37 us (39 us with the optimiser's momentum and update), 128 x 864 58 us, 27 x 96 x 800 with the
 // optimiser 72 us.  At 128 x 864 the tensor pipe is busy 5 % of the time and 41 % of the issue slots are taken: a step is a chain of
