@@ -107,6 +107,11 @@ def teacher(batch, size, cin, cout, k=3, seed=1):
     return x, t.forward(x).clone()
 
 
+def filter_rate(lr, update):
+    """The filters' learning rate: the one that was asked for, zero included, or the update's default."""
+    return lr if lr is not None else 0.4 if update == "muon" else 0.0005
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=40)
@@ -118,7 +123,7 @@ def main():
     ap.add_argument("--lr", type=float, default=None, help="of the filters; default 0.4 (muon), 0.0005 (sgd)")
     a = ap.parse_args()
     x, target = teacher(a.batch, a.size, a.cin, a.cout)
-    layer = Refit(a.batch, a.size, a.cin, a.cout, update=a.update, lr=a.lr or (0.4 if a.update == "muon" else 0.0005))
+    layer = Refit(a.batch, a.size, a.cin, a.cout, update=a.update, lr=filter_rate(a.lr, a.update))
     for i in range(a.steps):
         layer.step(x, target)
         if i % 5 == 0 or i == a.steps - 1:
