@@ -195,3 +195,40 @@ def test_the_longest_rows(dr, b, r, c):
     few = min(r, c) <= 64 and (b == 1 or max(r, c) <= 4096)
     for i in {0, b - 1}:
         assert error(o[i], u[i]) <= (FEW_ROWS if few else RANDOM)
+
+
+@pytest.mark.parametrize("shapes", [[(1, 2048, 2048), (1, 64, 147)], [(1, 1000, 2048), (9, 144, 816)], [(1, 512, 2048), (200, 100, 300)], [(1, 512, 13200), (27, 96, 800)]])
+def test_beside_convolutions(dr, shapes):
+    """Updates on two streams while a third runs convolutions: all of them want tensor memory, and some have to run on all processors at a time."""
+    import torch
+    us = [gaussian(sum(s), *s) for s in shapes]
+    wss = [torch.empty(dr.dr_orthogonalise_workspace_bytes(*s), dtype=torch.uint8, device="cuda") for s in shapes]
+    d = dr.dr_conv_desc(k=3, stride=1, pad=1, Cin=192, Cout=256, flags=dr.DR_BIAS | dr.DR_RELU)
+    x, w, b = gaussian(1, 64, 28, 28, 192).to(torch.bfloat16), gaussian(2, 256, 3, 3, 192).to(torch.bfloat16) * 0.02, gaussian(3, 256)
+    outs = lambda n: [[torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in shapes] for _ in range(n)]
+    ys = [torch.zeros((64, 28, 28, 256), dtype=torch.bfloat16, device="cuda") for _ in range(7)]
+
+    def updates(i, o, stream=None):
+        dr.dr_orthogonalise(*shapes[i], us[i], 5, None, 1e-7, o[i], wss[i], wss[i].numel(), dr.DR_NS_G_F32, stream)
+
+    def conv(y, stream=None):
+        dr.dr_conv_slim_ws(d, 64, 28, 28, x, w, b, None, y, None, None, 0, stream)
+
+    ref, = outs(1)
+    for i in range(2):
+        updates(i, ref)
+    conv(ys[-1])
+    got, streams = outs(6), [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for k in range(6):
+        for _ in range(4):
+            conv(ys[k], streams[2])
+        for i in range(2):
+            updates(i, got[k], streams[i])
+        for _ in range(4):
+            conv(ys[k], streams[2])
+    st, info = dr.dr_device_status()
+    assert st == 0, info
+    for o in got:
+        assert all(torch.equal(a, e) for a, e in zip(o, ref))
+    assert all(torch.equal(y, ys[-1]) for y in ys)
