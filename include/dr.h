@@ -410,7 +410,7 @@ int dr_layernorm_bwd(size_t npix, int C, const void* dy, int lddy, const void* x
  *  before it is rounded to bfloat16): 1e-4 .. 1e-3 for matrices of normal values, up to 4e-3 where the singular values of U
  *  spread over many decades or its rank is low, up to 1e-2 where U is a single direction (rounding errors then add up instead
  *  of averaging: 8e-3 with 65 rows, 2e-3 with 256, 1e-3 with 512).  Where min(rows, cols) <= 64: below 1e-4 for a single
- *  matrix and up to a long side of 4096, below 1e-3 for any (a batch of 150 and more leaves one CTA to a matrix, and its
+ *  matrix and up to a long side of 4096, below 1e-3 for any (a batch of 75 and more leaves one CTA to a matrix, and its
  *  float32 sums err with their length: 1.2e-4 at 12000, 8.4e-4 at 65536).
  *  X is kept in float16 times 4096, A and the polynomial in float16: with coefficients that let a singular value of X reach
  *  16, or an entry of the others 65504, O is not finite.
