@@ -446,6 +446,70 @@ int dr_muon_update(int batch, int rows, int cols, float* w, float* v, const floa
                    float decay, int nesterov, int steps, const float* coef, float eps, void* w_bf16, void* workspace,
                    size_t workspace_bytes, void* stream);
 
+/* ---- dropout ----------------------------------------------------------------------------
+ *   y = residual + keep * x / (1 - p)
+ * element by element, with a mask that is drawn and never stored; the gradient of x is the same call on the gradient of y (without
+ * the residual, whose own gradient is that of y).  The mask is a function of (seed, offset, *step) and the element's number alone: element e = row * C + channel
+ * takes 16 bits of Philox4x32-10 under the key `seed` at the counter (e / 8, offset + *step) - word (e mod 8) / 2, low half first - and is
+ * dropped where they are below round(p * 65536).  p is thereby taken to the nearest multiple of 1/65536, and 1 / (1 - p) is that
+ * probability's.  A dropped element gives 0 (or the residual) whatever x holds there.
+ *  rows of C channels, row r at ld* elements (0: dense, C) from the one before.  x: bfloat16, or float32 with DR_DROP_X_F32; y and residual (NULL: none):
+ *  bfloat16, or float32 with DR_DROP_Y_F32.  y may be x or residual itself (same type and ld).  Any C; pointers need only
+ *  their type's alignment; 16-byte accesses are taken where the rows' places allow them.
+ *  0 <= p <= 1 (1 drops everything).  step: NULL, or a counter in device memory read when the kernel runs, so that a captured call draws
+ *  another mask whenever the counter has moved.
+ * Errors: INVALID_ARG (nulls, C <= 0, ld < C, p outside [0, 1], unknown flags), ALIGNMENT.                            */
+#define DR_DROP_X_F32 0x1u
+#define DR_DROP_Y_F32 0x2u
+int dr_dropout(size_t rows, int C, const void* x, int ldx, const void* residual, int ldr, void* y, int ldy, double p,
+               unsigned long long seed, unsigned long long offset, const unsigned long long* step, unsigned flags,
+               void* stream);
+
+/* ---- low-rank adapters beside a shared layer ------------------------------------------------
+ * Many variants of one 1 x 1 (or fully connected) slim layer run in one call: all rows (pixels, or pooled images) share the filters W, and
+ * each request adds the low-rank product of its own variant a:
+ *   t = D(x) A_a^T,    y = act(x W^T + bias + scale[a] * t B_a^T),
+ * D the dropout of dr_dropout (drop_p = 0: none) over the M x Cin elements of x, act ReLU with DR_RELU.
+ *  Request s covers the rows row_start[s] <= m < row_start[s+1] and uses variant adapter[s]; any other number than 0 .. adapters-1 (say
+ *  -1) is the shared layer alone.  row_start: `segments` + 1 non-decreasing int32 in DEVICE memory (offsets that decrease put rows into some
+ *  request, and nothing is read or written out of range); adapter: int32 [segments] in device memory.  Both are read when the kernels run: a captured
+ *  call serves other requests when they have changed.  Requests may be empty and share variants.  Rows of no request (in front of
+ *  row_start[0], from row_start[segments] on) are left as they were in y, t and dx, and count in no gradient.
+ *  x: [M][Cin] bfloat16, row pitch ldx elements (0: Cin); w: [Cout][Cin] bfloat16; bias: float32 [Cout] (with DR_BIAS); a: [adapters][rank][Cin]
+ *  and b: [adapters][Cout][rank] bfloat16; scale: float32 [adapters], or NULL (1); y: [M][Cout], pitch ldy (0: Cout), bfloat16, or
+ *  float32 with DR_OUT_F32; t: NULL, or float32 [M][rank], what a backward pass needs of the forward pass (0 in rows without a variant).
+ *  x, w, a, b: 16-byte aligned; y: its type's alignment; any Cin, Cout, rank and pitches.  Where Cin or ldx is no multiple of 8 the call lays out
+ *  aligned copies in the workspace first.  y may not overlap an input.
+ *  Products are of bfloat16 values and sum in float32; t and u enter the second product as the sum of two bfloat16 values (16 to 17 bits).
+ *  step: NULL or a counter in device memory, as in dr_dropout.  workspace: dr_adapter_workspace_bytes bytes, 256-byte aligned, contents
+ *  irrelevant; calls that may overlap on the GPU need their own.
+ * Errors: INVALID_ARG, UNSUPPORTED (the limits below), ALIGNMENT, WORKSPACE, CUDA.                                    */
+#define DR_ADAPTER_MAX_RANK     256
+#define DR_ADAPTER_MAX_CHANNELS 65536
+#define DR_ADAPTER_MAX_ADAPTERS 4096
+#define DR_ADAPTER_MAX_ROWS     (1 << 30)
+typedef struct dr_adapter_desc {
+    int Cin, Cout, rank, adapters;
+    unsigned flags;                        /* DR_BIAS | DR_RELU | DR_OUT_F32; the backward pass does not look at them */
+    float drop_p;                          /* dropout of the adapters' input                                          */
+    unsigned long long drop_seed, drop_offset;
+} dr_adapter_desc;
+int dr_adapter_workspace_bytes(const dr_adapter_desc* desc, int M, int ldx, size_t* bytes);
+int dr_adapter(const dr_adapter_desc* desc, int M, const void* x, int ldx, const void* w, const float* bias, const void* a,
+               const void* b, const float* scale, int segments, const int* row_start, const int* adapter, void* y, int ldy,
+               float* t, const unsigned long long* step, void* workspace, size_t workspace_bytes, void* stream);
+/* The gradients, for dy the gradient of what act is applied to (dr_regress_grad's dZ):
+ *   u = scale[a] * dy B_a,   dx = dy W + D(u A_a),   da_a = sum_rows u^T D(x),   db_a = scale[a] * sum_rows dy^T t.
+ *  dy: [M][Cout] bfloat16, pitch lddy, 16-byte aligned; dx: [M][Cin] bfloat16, pitch lddx, or NULL; da: float32
+ *  [adapters][rank][Cin], db: float32 [adapters][Cout][rank], overwritten (zeros for a variant without rows), or NULL.  x is read for da, t for db.  Sums over rows are
+ *  taken in a fixed order: the same result on every run.  W itself and the bias take no gradient here (dr_conv_wgrad, dr_regress_grad).
+ *  dx may not overlap an input.  With M = 0 or without segments da and db are zeros.  Workspace and errors as dr_adapter.                                  */
+int dr_adapter_bwd_workspace_bytes(const dr_adapter_desc* desc, int M, int ldx, int lddy, size_t* bytes);
+int dr_adapter_bwd(const dr_adapter_desc* desc, int M, const void* dy, int lddy, const void* x, int ldx, const void* w,
+                   const void* a, const void* b, const float* scale, int segments, const int* row_start, const int* adapter,
+                   const float* t, void* dx, int lddx, float* da, float* db, const unsigned long long* step, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
 /* Kernels of this library launched by this process so far. */
 long long dr_launch_count(void);
 /* Tensor maps (TMA descriptors) the library has had the driver encode so far.  Maps are remembered by the arguments

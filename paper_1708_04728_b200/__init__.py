@@ -33,6 +33,8 @@ DR_PATH_UMMA_SPLITK = 8
 DR_PATH_UMMA_QLIN = 9
 DR_CONV_WS_COUNTER_BYTES = 1024
 NS_KERNELS = ("small", "alone", "share", "pair")
+DR_DROP_X_F32, DR_DROP_Y_F32 = 0x1, 0x2
+DR_ADAPTER_MAX_RANK, DR_ADAPTER_MAX_CHANNELS, DR_ADAPTER_MAX_ADAPTERS, DR_ADAPTER_MAX_ROWS = 256, 65536, 4096, 1 << 30
 DR_LN_X_F32, DR_LN_Y_F32, DR_NS_G_F32, DR_NS_MAX_STEPS, DR_NS_MAX_DIM = 0x1, 0x2, 0x1, 16, 65536
 PATH_NAMES = {0: "auto", 1: "simt", 2: "umma_gather", 3: "umma_tma", 4: "umma_patch", 5: "umma_stem", 6: "retired", 7: "umma_stem_d",
               8: "umma_splitk", 9: "umma_qlin", -1: "-"}
@@ -47,6 +49,11 @@ class dr_conv_desc(C.Structure):
 
 class dr_inception_desc(C.Structure):
     _fields_ = [("Cin", C.c_int), ("c3r", C.c_int), ("c3", C.c_int), ("cm", C.c_int), ("pool_after", C.c_int)]
+
+
+class dr_adapter_desc(C.Structure):
+    _fields_ = [("Cin", C.c_int), ("Cout", C.c_int), ("rank", C.c_int), ("adapters", C.c_int), ("flags", C.c_uint), ("drop_p", C.c_float),
+                ("drop_seed", C.c_ulonglong), ("drop_offset", C.c_ulonglong)]
 
 
 class dr_param_spec(C.Structure):
@@ -91,6 +98,11 @@ _SIGS = {
     "dr_orthogonalise_plan": (_I, [_I, _I, _I, C.POINTER(_I)]),
     "dr_orthogonalise": (_I, [_I, _I, _I, _P, _I, C.POINTER(_F), _F, _P, _P, _Z, C.c_uint, _P]),
     "dr_muon_update": (_I, [_I, _I, _I, _P, _P, _P, _F, _F, _F, _I, _I, C.POINTER(_F), _F, _P, _P, _Z, _P]),
+    "dr_dropout": (_I, [_Z, _I, _P, _I, _P, _I, _P, _I, C.c_double, C.c_ulonglong, C.c_ulonglong, _P, C.c_uint, _P]),
+    "dr_adapter_workspace_bytes": (_I, [C.POINTER(dr_adapter_desc), _I, _I, C.POINTER(_Z)]),
+    "dr_adapter": (_I, [C.POINTER(dr_adapter_desc), _I, _P, _I, _P, _P, _P, _P, _P, _I, _P, _P, _P, _I, _P, _P, _P, _Z, _P]),
+    "dr_adapter_bwd_workspace_bytes": (_I, [C.POINTER(dr_adapter_desc), _I, _I, _I, C.POINTER(_Z)]),
+    "dr_adapter_bwd": (_I, [C.POINTER(dr_adapter_desc), _I, _P, _I, _P, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _Z, _P]),
     "dr_conv_workspace_bytes": (_I, [C.POINTER(dr_conv_desc), _I, _I, _I, C.POINTER(_Z)]),
     "dr_conv_slim_ws": (_I, [C.POINTER(dr_conv_desc), _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "dr_inception_workspace_bytes": (_I, [C.POINTER(dr_inception_desc), _I, _I, _I, C.POINTER(_Z)]),
@@ -300,6 +312,34 @@ def dr_orthogonalise(batch, rows, cols, g, steps, coef, eps, o, workspace, works
 def dr_muon_update(batch, rows, cols, w, v, g, lr, momentum, decay, nesterov, steps, coef, eps, w_bf16, workspace, workspace_bytes, stream=None):
     _check(_lib.dr_muon_update(batch, rows, cols, _ptr(w), _ptr(v), _ptr(g), lr, momentum, decay, int(nesterov), steps, _coef(coef, steps), eps,
                                _ptr(w_bf16), _ptr(workspace), workspace_bytes, _stream(stream)), "dr_muon_update")
+
+
+def dr_dropout(rows, Cc, x, ldx, residual, ldr, y, ldy, p, seed, offset, step=None, flags=0, stream=None):
+    _check(_lib.dr_dropout(rows, Cc, _ptr(x), ldx, _ptr(residual), ldr, _ptr(y), ldy, p, seed, offset, _ptr(step), flags, _stream(stream)), "dr_dropout")
+
+
+def dr_adapter_workspace_bytes(desc, M, ldx=0) -> int:
+    n = _Z(0)
+    _check(_lib.dr_adapter_workspace_bytes(C.byref(desc), M, ldx, C.byref(n)), "dr_adapter_workspace_bytes")
+    return n.value
+
+
+def dr_adapter(desc, M, x, ldx, w, bias, a, b, scale, segments, row_start, adapter, y, ldy, t, step, workspace, workspace_bytes, stream=None):
+    _check(_lib.dr_adapter(C.byref(desc), M, _ptr(x), ldx, _ptr(w), _ptr(bias), _ptr(a), _ptr(b), _ptr(scale), segments, _ptr(row_start), _ptr(adapter),
+                           _ptr(y), ldy, _ptr(t), _ptr(step), _ptr(workspace), workspace_bytes, _stream(stream)), "dr_adapter")
+
+
+def dr_adapter_bwd_workspace_bytes(desc, M, ldx=0, lddy=0) -> int:
+    n = _Z(0)
+    _check(_lib.dr_adapter_bwd_workspace_bytes(C.byref(desc), M, ldx, lddy, C.byref(n)), "dr_adapter_bwd_workspace_bytes")
+    return n.value
+
+
+def dr_adapter_bwd(desc, M, dy, lddy, x, ldx, w, a, b, scale, segments, row_start, adapter, t, dx, lddx, da, db, step, workspace, workspace_bytes,
+                   stream=None):
+    _check(_lib.dr_adapter_bwd(C.byref(desc), M, _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), _ptr(a), _ptr(b), _ptr(scale), segments, _ptr(row_start),
+                               _ptr(adapter), _ptr(t), _ptr(dx), lddx, _ptr(da), _ptr(db), _ptr(step), _ptr(workspace), workspace_bytes,
+                               _stream(stream)), "dr_adapter_bwd")
 
 
 def dr_conv_workspace_bytes(desc, B, H, W) -> int:
