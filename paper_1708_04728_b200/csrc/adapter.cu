@@ -1,110 +1,10 @@
 // A 1 x 1 (or fully connected) layer with the low-rank adapters of many requests beside its shared filters, forward and backward:
 //   t = D(x) A_a^T,  y = act(x W^T + bias + scale_a t B_a^T);     u = scale_a dy B_a,  dx = dy W + D(u A_a),  dA_a = sum u^T D(x),
 //   dB_a = scale_a sum dy^T t,     a the adapter of the request that a row belongs to, D the dropout of dropout.cuh.
-#include <climits>
-
-#include "common.cuh"
-#include "dropout.cuh"
+// Arguments, workspaces and the order of the kernels: adapter_down.cu (t and u), adapter_product.cu (y and dx), adapter_grad.cu (dA and dB).
+#include "adapter.cuh"
 
 namespace dr {
-
-constexpr int ROW_SHARED = -1;      // a row of a request without an adapter
-constexpr int ROW_NONE = -2;        // a row of no request: left as it was
-
-struct AdRows {
-    int M, segments, adapters;
-    const int *row_start, *adapter;
-};
-
-// The adapter of row m.  Whatever the offsets hold, the search stays inside them; an adapter out of range is none.
-__device__ __forceinline__ int adapter_of_row(const AdRows& r, int m) {
-    int lo = 0, hi = r.segments + 1;            // number of offsets <= m
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (r.row_start[mid] <= m) lo = mid + 1;
-        else hi = mid;
-    }
-    if (lo == 0 || lo > r.segments) return ROW_NONE;
-    const int a = r.adapter[lo - 1];
-    return a >= 0 && a < r.adapters ? a : ROW_SHARED;
-}
-
-__global__ void adapter_rows_kernel(const AdRows r, int* __restrict__ row_id) {
-    const int m = blockIdx.x * blockDim.x + threadIdx.x;
-    if (m < r.M) row_id[m] = r.segments > 0 ? adapter_of_row(r, m) : ROW_NONE;
-}
-
-// out[m][r] = factor * sum_k D(z)[m][k] f_a[r][k], f_a rows of K (fr = K, fk = 1) or columns (fr = 1, fk = R)
-__global__ void adapter_down_kernel(int M, int K, int R, const __nv_bfloat16* __restrict__ z, int ldz, const __nv_bfloat16* __restrict__ f, int fr, int fk,
-                                    const float* __restrict__ scale, const DropKey key, const int* __restrict__ row_id, float* __restrict__ out, float* __restrict__ keep) {
-    const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= (size_t)M * R) return;
-    const int m = (int)(i / R), r = (int)(i - (size_t)m * R), a = row_id[m];
-    float s = 0.f;
-    if (a >= 0) {
-        const unsigned long long off = drop_offset(key);
-        const __nv_bfloat16* w = f + (size_t)a * R * K + (size_t)r * fr;
-        for (int k = 0; k < K; ++k) {
-            const bool kept = key.thr == 0 || drop_keep_at(key, off, (unsigned long long)m * K + k);
-            if (kept) s = fmaf(__bfloat162float(z[(size_t)m * ldz + k]), __bfloat162float(w[(size_t)k * fk]), s);
-        }
-        s *= key.thr ? key.scale : 1.f;
-        if (scale) s *= scale[a];
-    }
-    out[i] = s;
-    if (keep && a != ROW_NONE) keep[i] = s;
-}
-
-__global__ void adapter_forward_kernel(int M, int K, int N, int R, const __nv_bfloat16* __restrict__ x, int ldx, const __nv_bfloat16* __restrict__ w,
-                                       const float* __restrict__ bias, const __nv_bfloat16* __restrict__ b, const float* __restrict__ scale,
-                                       const int* __restrict__ row_id, const float* __restrict__ t, unsigned flags, void* __restrict__ y, int ldy) {
-    const int n = blockIdx.x * blockDim.x + threadIdx.x, m = blockIdx.y + blockIdx.z * 32768;
-    if (n >= N || m >= M || row_id[m] == ROW_NONE) return;
-    float s = 0.f, l = 0.f;
-    for (int k = 0; k < K; ++k) s = fmaf(__bfloat162float(x[(size_t)m * ldx + k]), __bfloat162float(w[(size_t)n * K + k]), s);
-    const int a = row_id[m];
-    if (a >= 0) {
-        for (int r = 0; r < R; ++r) l = fmaf(t[(size_t)m * R + r], __bfloat162float(b[((size_t)a * N + n) * R + r]), l);
-        s = fmaf(scale ? scale[a] : 1.f, l, s);
-    }
-    if (flags & DR_BIAS) s += bias[n];
-    if (flags & DR_RELU) s = s < 0.f ? 0.f : s;         // NaN stays NaN
-    if (flags & DR_OUT_F32) ((float*)y)[(size_t)m * ldy + n] = s;
-    else ((__nv_bfloat16*)y)[(size_t)m * ldy + n] = __float2bfloat16_rn(s);
-}
-
-__global__ void adapter_dx_kernel(int M, int K, int N, int R, const __nv_bfloat16* __restrict__ dy, int lddy, const __nv_bfloat16* __restrict__ w,
-                                  const __nv_bfloat16* __restrict__ f, const int* __restrict__ row_id, const float* __restrict__ u, const DropKey key,
-                                  __nv_bfloat16* __restrict__ dx, int lddx) {
-    const int k = blockIdx.x * blockDim.x + threadIdx.x, m = blockIdx.y + blockIdx.z * 32768;
-    if (k >= K || m >= M || row_id[m] == ROW_NONE) return;
-    float s = 0.f, l = 0.f;
-    for (int n = 0; n < N; ++n) s = fmaf(__bfloat162float(dy[(size_t)m * lddy + n]), __bfloat162float(w[(size_t)n * K + k]), s);
-    const int a = row_id[m];
-    if (a >= 0) {
-        for (int r = 0; r < R; ++r) l = fmaf(u[(size_t)m * R + r], __bfloat162float(f[((size_t)a * R + r) * K + k]), l);
-        if (key.thr == 0) s += l;
-        else if (drop_keep_at(key, drop_offset(key), (unsigned long long)m * K + k)) s = fmaf(key.scale, l, s);
-    }
-    dx[(size_t)m * lddx + k] = __float2bfloat16_rn(s);
-}
-
-// out[a][r][c] (rc) or out[a][c][r]: sum over the rows of adapter a of factor * p[m][r] * D(z)[m][c]
-__global__ void adapter_grad_kernel(int M, int C, int R, int adapters, const __nv_bfloat16* __restrict__ z, int ldz, const float* __restrict__ p,
-                                    const float* __restrict__ scale, const int* __restrict__ row_id, const DropKey key, int rc, float* __restrict__ out) {
-    const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= (size_t)adapters * R * C) return;
-    const int a = (int)(i / ((size_t)R * C));
-    const int rest = (int)(i - (size_t)a * R * C);
-    const int r = rc ? rest / C : rest % R, c = rc ? rest % C : rest / R;
-    const unsigned long long off = drop_offset(key);
-    float s = 0.f;
-    for (int m = 0; m < M; ++m)
-        if (row_id[m] == a && (key.thr == 0 || drop_keep_at(key, off, (unsigned long long)m * C + c)))
-            s = fmaf(p[(size_t)m * R + r], __bfloat162float(z[(size_t)m * ldz + c]), s);
-    if (key.thr) s *= key.scale;
-    out[i] = scale ? s * scale[a] : s;
-}
 
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -121,6 +21,75 @@ static int ld_check(int* ld, int C) {
     return *ld < C ? DR_ERR_INVALID_ARG : DR_OK;
 }
 
+// Places in the workspace.  Rows that are not on 16-byte boundaries are laid out there first: 16-byte loads and TMA want them so.
+struct Places {
+    size_t bytes = 0;
+    size_t take(size_t n) { const size_t at = bytes; bytes += up256(n); return at; }
+};
+static int up8(int n) { return (n + 7) & ~7; }
+
+struct ForwardPlan {
+    DownPlan down;
+    int Kp, Rp;
+    bool copy_x, copy_k;        // x; w and a
+    size_t t, x, w, a, bytes;
+};
+static ForwardPlan forward_plan(const dr_adapter_desc* d, int M, int ldx, int segments) {
+    ForwardPlan f;
+    f.down = adapter_down_plan(M, d->Cin, d->rank, d->adapters, segments);
+    f.Kp = up8(d->Cin);
+    f.Rp = up8(d->rank);
+    f.copy_k = d->Cin & 7;
+    f.copy_x = f.copy_k || (ldx & 7);
+    Places at;
+    f.t = at.take((size_t)f.down.ks * M * f.Rp * 4);
+    f.x = at.take(f.copy_x ? (size_t)M * f.Kp * 2 : 0);
+    f.w = at.take(f.copy_k ? (size_t)d->Cout * f.Kp * 2 : 0);
+    f.a = at.take(f.copy_k ? (size_t)d->adapters * d->rank * f.Kp * 2 : 0);
+    f.bytes = at.bytes;
+    return f;
+}
+
+struct BackwardPlan {
+    DownPlan down;
+    GradPlan grad;
+    int Kp, Np, Rp;
+    bool copy_x, copy_k, copy_dy;
+    size_t u, x, w, a, dy, bt, g, bytes;
+};
+static BackwardPlan backward_plan(const dr_adapter_desc* d, int M, int ldx, int lddy, int segments) {
+    BackwardPlan f;
+    f.down = adapter_down_plan(M, d->Cout, d->rank, d->adapters, segments);
+    const int C[2] = {d->Cin, d->Cout};
+    f.grad = adapter_grad_plan(M, d->rank, d->adapters, C);
+    f.Kp = up8(d->Cin);
+    f.Np = up8(d->Cout);
+    f.Rp = up8(d->rank);
+    f.copy_k = d->Cin & 7;
+    f.copy_x = f.copy_k || (ldx & 7);
+    f.copy_dy = (d->Cout & 7) || (lddy & 7);
+    Places at;
+    f.u = at.take((size_t)f.down.ks * M * f.Rp * 4);
+    f.x = at.take(f.copy_x ? (size_t)M * f.Kp * 2 : 0);
+    f.w = at.take(f.copy_k ? (size_t)d->Cout * f.Kp * 2 : 0);
+    f.a = at.take(f.copy_k ? (size_t)d->adapters * d->rank * f.Kp * 2 : 0);
+    f.dy = at.take(f.copy_dy ? (size_t)M * f.Np * 2 : 0);
+    f.bt = at.take((size_t)d->adapters * d->rank * f.Np * 2);
+    f.g = at.take(f.grad.bytes);
+    f.bytes = at.bytes;
+    return f;
+}
+// the tensor itself, or its aligned copy
+static int place(bool copy, size_t rows, int cols, int colsp, const void* src, size_t ld, char* ws, size_t at, const __nv_bfloat16** p, size_t* ldp, cudaStream_t s) {
+    *p = (const __nv_bfloat16*)src;
+    *ldp = ld;
+    if (!copy) return DR_OK;
+    __nv_bfloat16* dst = (__nv_bfloat16*)(ws + at);
+    *p = dst;
+    *ldp = colsp;
+    return adapter_align_run(rows, cols, (const __nv_bfloat16*)src, ld, dst, colsp, s);
+}
+
 }  // namespace dr
 
 using namespace dr;
@@ -129,7 +98,7 @@ extern "C" int dr_adapter_workspace_bytes(const dr_adapter_desc* d, int M, int l
     const int rc = desc_check(d, M);
     if (rc != DR_OK) return rc;
     if (!bytes || ld_check(&ldx, d->Cin) != DR_OK) return DR_ERR_INVALID_ARG;
-    *bytes = up256((size_t)M * 4) + up256((size_t)M * d->rank * 4);
+    *bytes = forward_plan(d, M, ldx, 1).bytes;
     return DR_OK;
 }
 
@@ -137,7 +106,7 @@ extern "C" int dr_adapter_bwd_workspace_bytes(const dr_adapter_desc* d, int M, i
     const int rc = desc_check(d, M);
     if (rc != DR_OK) return rc;
     if (!bytes || ld_check(&ldx, d->Cin) != DR_OK || ld_check(&lddy, d->Cout) != DR_OK) return DR_ERR_INVALID_ARG;
-    *bytes = up256((size_t)M * 4) + up256((size_t)M * d->rank * 4);
+    *bytes = backward_plan(d, M, ldx, lddy, 1).bytes;
     return DR_OK;
 }
 
@@ -153,22 +122,23 @@ extern "C" int dr_adapter(const dr_adapter_desc* d, int M, const void* x, int ld
         ((uintptr_t)scale & 3) || ((uintptr_t)row_start & 3) || ((uintptr_t)adapter & 3) || ((uintptr_t)t & 3) || ((uintptr_t)step & 7) ||
         ((uintptr_t)workspace & 255))
         return DR_ERR_ALIGNMENT;
-    size_t need = 0;
-    rc = dr_adapter_workspace_bytes(d, M, ldx, &need);
-    if (rc != DR_OK) return rc;
-    if (workspace_bytes < need) return DR_ERR_WORKSPACE;
+    const ForwardPlan f = forward_plan(d, M, ldx, segments);
+    if (workspace_bytes < f.bytes) return DR_ERR_WORKSPACE;
     const cudaStream_t s = (cudaStream_t)stream;
+    char* const ws = (char*)workspace;
     const int K = d->Cin, N = d->Cout, R = d->rank;
-    int* row_id = (int*)workspace;
-    float* tw = (float*)((char*)workspace + up256((size_t)M * 4));
     const AdRows rows = {M, segments, d->adapters, row_start, adapter};
-    const DropKey key = drop_key(d->drop_p, d->drop_seed, d->drop_offset, step);
-    adapter_rows_kernel<<<(M + 255) / 256, 256, 0, s>>>(rows, row_id);
-    adapter_down_kernel<<<(unsigned)(((size_t)M * R + 255) / 256), 256, 0, s>>>(M, K, R, (const __nv_bfloat16*)x, ldx, (const __nv_bfloat16*)a, K, 1, nullptr, key, row_id, tw, t);
-    adapter_forward_kernel<<<dim3((N + 127) / 128, M < 32768 ? M : 32768, (M + 32767) / 32768), 128, 0, s>>>(
-        M, K, N, R, (const __nv_bfloat16*)x, ldx, (const __nv_bfloat16*)w, bias, (const __nv_bfloat16*)b, scale, row_id, tw, d->flags, y, ldy);
-    count_launch(3);
-    return launch_status();
+    const DropKey key = drop_key(d->drop_p, d->drop_seed, d->drop_offset, step), none = drop_key(0., 0, 0, nullptr);
+    const __nv_bfloat16 *xp, *wp, *ap;
+    size_t ldxp, ldwp, ldap;
+    if ((rc = place(f.copy_x, M, K, f.Kp, x, ldx, ws, f.x, &xp, &ldxp, s)) != DR_OK) return rc;
+    if ((rc = place(f.copy_k, N, K, f.Kp, w, K, ws, f.w, &wp, &ldwp, s)) != DR_OK) return rc;
+    if ((rc = place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, ws, f.a, &ap, &ldap, s)) != DR_OK) return rc;
+    float* const tw = (float*)(ws + f.t);
+    rc = adapter_down_run(f.down, rows, K, R, f.Rp, xp, ldxp, ap, ldap, key, key.thr ? key.scale : 1.f, tw, s);
+    if (rc != DR_OK) return rc;
+    ProductArgs g = {rows, K, N, R, f.Rp, f.down.ks, xp, wp, (const __nv_bfloat16*)b, ldxp, ldwp, 0, tw, scale, bias, 1.f, t, d->flags, y, (size_t)ldy, false, none};
+    return adapter_product_run(g, true, s);
 }
 
 extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, int lddy, const void* x, int ldx, const void* w, const void* a, const void* b,
@@ -189,29 +159,36 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     if (!aligned16(dy) || !aligned16(x) || !aligned16(w) || !aligned16(a) || !aligned16(b) || ((uintptr_t)dx & 1) || ((uintptr_t)scale & 3) ||
         ((uintptr_t)row_start & 3) || ((uintptr_t)adapter & 3) || ((uintptr_t)t & 3) || ((uintptr_t)step & 7) || ((uintptr_t)workspace & 255))
         return DR_ERR_ALIGNMENT;
-    size_t need = 0;
-    rc = dr_adapter_bwd_workspace_bytes(d, M, ldx, lddy, &need);
-    if (rc != DR_OK) return rc;
-    if (workspace_bytes < need) return DR_ERR_WORKSPACE;
-    int* row_id = (int*)workspace;
-    float* u = (float*)((char*)workspace + up256((size_t)M * 4));
+    const BackwardPlan f = backward_plan(d, M, ldx, lddy, segments);
+    if (workspace_bytes < f.bytes) return DR_ERR_WORKSPACE;
+    if (!dx && !da && !db) return DR_OK;
+    char* const ws = (char*)workspace;
     const AdRows rows = {M, segments, d->adapters, row_start, adapter};
     const DropKey key = drop_key(d->drop_p, d->drop_seed, d->drop_offset, step), none = drop_key(0., 0, 0, nullptr);
-    adapter_rows_kernel<<<(M + 255) / 256, 256, 0, s>>>(rows, row_id);
-    adapter_down_kernel<<<(unsigned)(((size_t)M * R + 255) / 256), 256, 0, s>>>(M, N, R, (const __nv_bfloat16*)dy, lddy, (const __nv_bfloat16*)b, 1, R, scale, none, row_id, u, nullptr);
-    count_launch(2);
+    const float kept = key.thr ? key.scale : 1.f;
+    const __nv_bfloat16 *dyp, *xp = nullptr, *wp = nullptr, *ap = nullptr;
+    size_t lddyp, ldxp = 0, ldwp = 0, ldap = 0;
+    if ((rc = place(f.copy_dy, M, N, f.Np, dy, lddy, ws, f.dy, &dyp, &lddyp, s)) != DR_OK) return rc;
+    if (da && (rc = place(f.copy_x, M, K, f.Kp, x, ldx, ws, f.x, &xp, &ldxp, s)) != DR_OK) return rc;
+    if (dx && (rc = place(f.copy_k, N, K, f.Kp, w, K, ws, f.w, &wp, &ldwp, s)) != DR_OK) return rc;
+    if (dx && (rc = place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, ws, f.a, &ap, &ldap, s)) != DR_OK) return rc;
+    float* const u = (float*)(ws + f.u);
+    if (da || db) {
+        rc = adapter_sort_run(rows, (int*)(ws + f.g + f.grad.perm), (int*)(ws + f.g + f.grad.start), s);
+        if (rc != DR_OK) return rc;
+    }
+    if (dx || da) {
+        __nv_bfloat16* const bt = (__nv_bfloat16*)(ws + f.bt);
+        if ((rc = adapter_transpose_run(d->adapters, N, R, (const __nv_bfloat16*)b, bt, f.Np, s)) != DR_OK) return rc;
+        if ((rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, u, s)) != DR_OK) return rc;
+    }
     if (dx) {
-        adapter_dx_kernel<<<dim3((K + 127) / 128, M < 32768 ? M : 32768, (M + 32767) / 32768), 128, 0, s>>>(
-            M, K, N, R, (const __nv_bfloat16*)dy, lddy, (const __nv_bfloat16*)w, (const __nv_bfloat16*)a, row_id, u, key, (__nv_bfloat16*)dx, lddx);
-        count_launch();
+        const ProductArgs g = {rows, N, K, R, f.Rp, f.down.ks, dyp, wp, ap, lddyp, ldwp, ldap, u, scale, nullptr, kept, nullptr, 0, dx, (size_t)lddx, true, key};
+        if ((rc = adapter_product_run(g, true, s)) != DR_OK) return rc;
     }
-    if (da) {
-        adapter_grad_kernel<<<(unsigned)(((size_t)d->adapters * R * K + 255) / 256), 256, 0, s>>>(M, K, R, d->adapters, (const __nv_bfloat16*)x, ldx, u, nullptr, row_id, key, 1, da);
-        count_launch();
+    if (da || db) {
+        const GradJob jobs[2] = {{K, xp, ldxp, u, f.down.ks, f.Rp, scale, kept, key, da, 0}, {N, dyp, lddyp, t, 1, R, scale, 1.f, none, db, 1}};
+        if ((rc = adapter_grad_run(f.grad, rows, R, jobs, ws + f.g, s)) != DR_OK) return rc;
     }
-    if (db) {
-        adapter_grad_kernel<<<(unsigned)(((size_t)d->adapters * R * N + 255) / 256), 256, 0, s>>>(M, N, R, d->adapters, (const __nv_bfloat16*)dy, lddy, t, scale, row_id, none, 0, db);
-        count_launch();
-    }
-    return launch_status();
+    return DR_OK;
 }

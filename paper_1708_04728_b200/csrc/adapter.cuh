@@ -1,0 +1,132 @@
+// What the kernels of the low-rank adapters share: which request a row belongs to, masks of neighbouring elements, launch parameters.
+#pragma once
+#include <cuda.h>
+
+#include "common.cuh"
+#include "dropout.cuh"
+
+namespace dr {
+
+constexpr int ROW_SHARED = -1;      // a row of a request without an adapter
+constexpr int ROW_NONE = -2;        // a row of no request: left as it was
+
+struct AdRows {
+    int M, segments, adapters;
+    const int *row_start, *adapter;
+};
+
+// Number of offsets row_start[lo .. hi) that are <= m, plus lo, by binary search.  Whatever the offsets hold, the search stays inside them.
+__device__ __forceinline__ int offsets_upto(const AdRows& r, int m, int lo, int hi) {
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (__ldg(r.row_start + mid) <= m) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+__device__ __forceinline__ int adapter_of_count(const AdRows& r, int count) {     // count: offsets <= the row
+    if (count <= 0 || count > r.segments) return ROW_NONE;
+    const int a = __ldg(r.adapter + count - 1);
+    return a >= 0 && a < r.adapters ? a : ROW_SHARED;           // an adapter out of range is none
+}
+// The adapter of row m0 + lane, by a whole warp: 32 offsets are probed at a time (two dependent loads for a thousand requests instead of ten), for
+// the first and the last of the rows; rows between two requests search between these alone.
+__device__ __forceinline__ int adapter_of_warp_row(const AdRows& r, int m0, int lane) {
+    const int last = m0 + 31;
+    int lo[2] = {0, 0}, n[2] = {r.segments + 1, r.segments + 1};
+    while (n[0] > 0 || n[1] > 0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (n[k] <= 0) continue;
+            const int step = (n[k] + 31) >> 5;                  // lane probes the last offset of its piece
+            const int at = min(lane * step + step - 1, n[k] - 1);
+            const bool le = lane * step < n[k] && __ldg(r.row_start + lo[k] + at) <= (k ? last : m0);
+            const unsigned below = __ballot_sync(0xffffffffu, le);
+            const int pieces = __popc(below & ~(below + 1));    // the pieces in front of the first one that reaches beyond the row
+            const int skip = min(pieces * step, n[k]);
+            lo[k] += skip;
+            n[k] = skip == n[k] ? 0 : min(step - 1, n[k] - skip - 1);   // the probed offset of the next piece is above the row
+        }
+    }
+    const int m = m0 + lane;
+    if (m >= r.M) return ROW_NONE;
+    return adapter_of_count(r, lo[0] >= lo[1] ? lo[0] : offsets_upto(r, m, lo[0], lo[1]));
+}
+
+// Which of 8 consecutive elements, the first with number e, are kept: bit i for element e + i.
+__device__ __forceinline__ uint32_t drop_bits8(const DropKey& k, unsigned long long off, unsigned long long counter) {
+    const uint4 w = drop_words(k, off, counter);
+    uint32_t b = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b |= drop_keep(w, i, k.thr) ? 1u << i : 0u;
+    return b;
+}
+__device__ __forceinline__ uint32_t drop_bits8_at(const DropKey& k, unsigned long long off, unsigned long long e) {
+    uint32_t b = drop_bits8(k, off, e >> 3);
+    const int sh = (int)(e & 7);
+    if (sh) b = (b | drop_bits8(k, off, (e >> 3) + 1) << 8) >> sh;
+    return b & 0xFFu;
+}
+// 8 bfloat16 values, those whose bit is clear set to zero
+__device__ __forceinline__ uint4 drop_apply8(uint4 v, uint32_t bits) {
+    auto two = [](uint32_t u, uint32_t b) { return u & ((b & 1 ? 0xFFFFu : 0u) | (b & 2 ? 0xFFFF0000u : 0u)); };
+    return make_uint4(two(v.x, bits), two(v.y, bits >> 2), two(v.z, bits >> 4), two(v.w, bits >> 6));
+}
+
+// A float32 value as the sum of two bfloat16 values (16 to 17 significant bits): high in the low half of the word pair order of the caller.
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+    hi = pack_bf16(a, b);
+    // an infinity (or what rounds to one) has no remainder: inf - inf would be NaN
+    const float ra = a - bf16_lo(hi), rb = b - bf16_hi(hi);
+    lo = pack_bf16(fabsf(bf16_lo(hi)) <= 3.0e38f ? ra : 0.f, fabsf(bf16_hi(hi)) <= 3.0e38f ? rb : 0.f);
+}
+
+// ---- launches (adapter_down.cu, adapter_product.cu, adapter_grad.cu) -------------------------------------------------------
+// out[ks][m][r] = factor * sum over a range of L of D(z)[m][l] f_a[r][l]; f [adapters * R][ldf], 16-byte aligned rows, zeros behind L
+struct DownPlan { int mt, warps_k, rows_cta, ks, zsplit, rt, rchunks; };
+DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments);
+int adapter_down_run(const DownPlan& plan, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
+                     const DropKey& key, float factor, float* out, cudaStream_t s);
+
+// out[m][c] = act(sum_l z[m][l] w + bias[c] + D(scale_a factor t[m] f_a)):   forward w [C][ldw] (rows of l), f [adapters][C][R];
+// transposed w [L][ldw] (rows of c), f [adapters][R][ldf]
+struct ProductArgs {
+    AdRows rows;
+    int L, C, R, Rp, ks;
+    const __nv_bfloat16 *z, *w, *f;
+    size_t ldz, ldw, ldf;
+    const float *t, *scale, *bias;
+    float factor;
+    float* keep;                // forward: t as the caller keeps it
+    unsigned flags;
+    void* out;
+    size_t ldo;
+    bool transposed;
+    DropKey key;                // thr 0: D is the identity (the forward pass')
+};
+int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s);
+
+// g_a[r][c] = sum over the rows of adapter a of P[m][r] D(z)[m][c]
+struct GradJob {
+    int C;
+    const __nv_bfloat16* z;
+    size_t ldz;
+    const float* p;             // [ks][M][ldp]
+    int ks, ldp;
+    const float* scale;         // scale_a on P, or nullptr
+    float factor;
+    DropKey key;
+    float* out;                 // [adapters][R][C], or [adapters][C][R] where swap
+    int swap;
+};
+struct GradPlan { int splits, rt, rchunks; size_t perm, start, part[2], bytes; };
+GradPlan adapter_grad_plan(int M, int R, int adapters, const int C[2]);
+int adapter_sort_run(const AdRows& rows, int* perm, int* start, cudaStream_t s);
+int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const GradJob jobs[2], char* ws, cudaStream_t s);
+
+// rows of `cols` elements, `ld` apart, as rows of ldd >= cols with zeros behind them
+int adapter_align_run(size_t rows, int cols, const __nv_bfloat16* src, size_t ld, __nv_bfloat16* dst, size_t ldd, cudaStream_t s);
+// [batch][rows][cols] -> [batch][cols][ldd], zeros behind rows
+int adapter_transpose_run(int batch, int rows, int cols, const __nv_bfloat16* src, __nv_bfloat16* dst, size_t ldd, cudaStream_t s);
+
+}  // namespace dr
