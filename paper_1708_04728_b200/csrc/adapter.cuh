@@ -73,28 +73,35 @@ __device__ __forceinline__ uint4 drop_apply8(uint4 v, uint32_t bits) {
     return make_uint4(two(v.x, bits), two(v.y, bits >> 2), two(v.z, bits >> 4), two(v.w, bits >> 6));
 }
 
-// A float32 value as the sum of two bfloat16 values (16 to 17 significant bits): high in the low half of the word pair order of the caller.
+// Two float32 values as sums of two bfloat16 values each (16 to 17 significant bits), or of three (all 24): packed in pairs.
 __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
     hi = pack_bf16(a, b);
     // an infinity (or what rounds to one) has no remainder: inf - inf would be NaN
     const float ra = a - bf16_lo(hi), rb = b - bf16_hi(hi);
-    lo = pack_bf16(fabsf(bf16_lo(hi)) <= 3.0e38f ? ra : 0.f, fabsf(bf16_hi(hi)) <= 3.0e38f ? rb : 0.f);
+    lo = pack_bf16(fabsf(bf16_lo(hi)) <= 3.4e38f ? ra : 0.f, fabsf(bf16_hi(hi)) <= 3.4e38f ? rb : 0.f);
+}
+__device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+    hi = pack_bf16(a, b);
+    const float ra = fabsf(bf16_lo(hi)) <= 3.4e38f ? a - bf16_lo(hi) : 0.f, rb = fabsf(bf16_hi(hi)) <= 3.4e38f ? b - bf16_hi(hi) : 0.f;
+    mid = pack_bf16(ra, rb);
+    lo = pack_bf16(ra - bf16_lo(mid), rb - bf16_hi(mid));
 }
 
 // ---- launches (adapter_down.cu, adapter_product.cu, adapter_grad.cu) -------------------------------------------------------
-// out[ks][m][r] = factor * sum over a range of L of D(z)[m][l] f_a[r][l]; f [adapters * R][ldf], 16-byte aligned rows, zeros behind L
+// out[m][r] = factor * sum_l D(z)[m][l] f_a[r][l] in rows of Rp, and each row's adapter; f [adapters * R][ldf], 16-byte aligned rows, zeros behind L
 struct DownPlan { int mt, warps_k, rows_cta, ks, zsplit, rt, rchunks; };
 DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments);
 int adapter_down_run(const DownPlan& plan, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
-                     const DropKey& key, float factor, float* out, cudaStream_t s);
+                     const DropKey& key, float factor, float* out, int* row_id, cudaStream_t s);
 
 // out[m][c] = act(sum_l z[m][l] w + bias[c] + D(scale_a factor t[m] f_a)):   forward w [C][ldw] (rows of l), f [adapters][C][R];
 // transposed w [L][ldw] (rows of c), f [adapters][R][ldf]
 struct ProductArgs {
     AdRows rows;
-    int L, C, R, Rp, ks;
+    int L, C, R, Rp;
     const __nv_bfloat16 *z, *w, *f;
     size_t ldz, ldw, ldf;
+    const int* row_id;
     const float *t, *scale, *bias;
     float factor;
     float* keep;                // forward: t as the caller keeps it
@@ -111,8 +118,8 @@ struct GradJob {
     int C;
     const __nv_bfloat16* z;
     size_t ldz;
-    const float* p;             // [ks][M][ldp]
-    int ks, ldp;
+    const float* p;             // [M][ldp]
+    int ldp;
     const float* scale;         // scale_a on P, or nullptr
     float factor;
     DropKey key;

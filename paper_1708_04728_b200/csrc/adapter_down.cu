@@ -4,11 +4,12 @@
 // registers; no shared memory, and the dropout's mask is drawn where the values are.  A warp whose rows belong to several adapters does
 // the product once for each and keeps the rows that are that adapter's.
 //
-// Few rows: the warps of a CTA share 16 rows and split l, further CTAs take ranges of l (their sums meet in whoever reads the result, in
-// order) and adapters of their own.
+// Few rows: the warps of a CTA share 16 rows and split l, a cluster of CTAs takes ranges of l (their sums meet in distributed shared memory, in
+// order), and further clusters take adapters of their own.
 #include <algorithm>
 
 #include "adapter.cuh"
+#include "umma_ptx.cuh"
 
 namespace dr {
 
@@ -21,6 +22,7 @@ struct DownParams {
     DropKey key;
     float factor;
     float* out;
+    int* row_id;
 };
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -33,6 +35,7 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 template <int MT, int RT, bool DROP, bool JOIN>
 __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
     __shared__ float join[JOIN ? 8 : 1][JOIN ? 16 : 1][JOIN ? RT * 8 + 1 : 1];
+    __shared__ float range[JOIN ? 16 * RT * 8 : 1];              // this range's sums, read by the cluster
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int m0 = ((int)blockIdx.x * (JOIN ? 1 : 8) + (JOIN ? 0 : warp)) * MT * 16;
@@ -41,6 +44,7 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
     if (m0 >= p.rows.M) return;                                  // JOIN: the whole CTA
     int id = adapter_of_warp_row(p.rows, m0, lane);
     if (lane >= MT * 16) id = ROW_NONE;
+    else if (p.row_id && blockIdx.y == 0 && blockIdx.z == 0 && (!JOIN || warp == 0) && m0 + lane < p.rows.M) p.row_id[m0 + lane] = id;
     const unsigned long long off = DROP ? drop_offset(p.key) : 0ull;
     const bool whole = (p.L & 7) == 0;
 
@@ -111,14 +115,28 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
                 __syncthreads();
                 for (int i = threadIdx.x; i < 16 * RT * 8; i += 256) {
                     const int row = i / (RT * 8), r = i - row * (RT * 8);
-                    if ((mine >> (16 * t + row) & 1) && r0 + r < p.Rp) {
-                        float s = join[0][row][r];
+                    float s = join[0][row][r];
 #pragma unroll
-                        for (int w = 1; w < 8; ++w) s += join[w][row][r];
-                        p.out[((size_t)ks * p.rows.M + m0 + 16 * t + row) * p.Rp + r0 + r] = s * p.factor;
-                    }
+                    for (int w = 1; w < 8; ++w) s += join[w][row][r];
+                    if (p.ks > 1) range[i] = s;
+                    else if ((mine >> (16 * t + row) & 1) && r0 + r < p.Rp) p.out[(size_t)(m0 + 16 * t + row) * p.Rp + r0 + r] = s * p.factor;
                 }
-                __syncthreads();
+                if (p.ks > 1) {
+                    ptx::cluster_sync_all();
+                    for (int i = 256 * ks + threadIdx.x; i < 16 * RT * 8; i += 256 * p.ks) {
+                        const int row = i / (RT * 8), r = i - row * (RT * 8);
+                        float s = 0.f;
+                        for (int k = 0; k < p.ks; ++k) {
+                            float v;
+                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ptx::mapa_shared(ptx::smem_u32(range + i), (uint32_t)k)) : "memory");
+                            s += v;
+                        }
+                        if ((mine >> (16 * t + row) & 1) && r0 + r < p.Rp) p.out[(size_t)(m0 + 16 * t + row) * p.Rp + r0 + r] = s * p.factor;
+                    }
+                    ptx::cluster_sync_all();                     // the sums are read: they may be overwritten, the CTA may leave
+                } else {
+                    __syncthreads();
+                }
             }
         } else {
 #pragma unroll
@@ -129,7 +147,7 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
                     for (int h = 0; h < 2; ++h) {
                         const int row = 16 * t + 8 * h + g, c = r0 + 8 * r + 2 * q;
                         if ((mine >> row & 1) && c < p.Rp)
-                            *reinterpret_cast<float2*>(p.out + ((size_t)ks * p.rows.M + m0 + row) * p.Rp + c) = make_float2(acc[t][r][2 * h] * p.factor, acc[t][r][2 * h + 1] * p.factor);
+                            *reinterpret_cast<float2*>(p.out + (size_t)(m0 + row) * p.Rp + c) = make_float2(acc[t][r][2 * h] * p.factor, acc[t][r][2 * h + 1] * p.factor);
                     }
         }
     }
@@ -149,7 +167,7 @@ DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments) {
     d.warps_k = 8; d.rows_cta = 16 * d.mt;
     const int tiles = (M + d.rows_cta - 1) / d.rows_cta;
     if (tiles < sms) {
-        d.ks = std::max(1, std::min((L + 511) / 512, 2 * sms / tiles));
+        d.ks = std::max(1, std::min(std::min(8, (L + 511) / 512), 2 * sms / tiles));     // 8: the largest cluster every device holds
         const int distinct = std::min(std::min(16, M), std::min(adapters, segments));
         d.zsplit = std::max(1, std::min(distinct, 4 * sms / (tiles * d.ks)));
     }
@@ -157,32 +175,38 @@ DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments) {
 }
 
 template <int MT, int RT, bool JOIN>
-static void down_launch(const DownPlan& d, const DownParams& p, cudaStream_t s) {
-    const dim3 grid((unsigned)((p.rows.M + d.rows_cta - 1) / d.rows_cta), (unsigned)d.ks, (unsigned)(d.zsplit * d.rchunks));
-    if (p.key.thr) adapter_down_kernel<MT, RT, true, JOIN><<<grid, 256, 0, s>>>(p);
-    else adapter_down_kernel<MT, RT, false, JOIN><<<grid, 256, 0, s>>>(p);
+static int down_launch(const DownPlan& d, const DownParams& p, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((p.rows.M + d.rows_cta - 1) / d.rows_cta), (unsigned)d.ks, (unsigned)(d.zsplit * d.rchunks));
+    cfg.blockDim = dim3(256);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = (unsigned)d.ks; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = d.ks > 1 ? 1 : 0;
+    const cudaError_t e = p.key.thr ? cudaLaunchKernelEx(&cfg, adapter_down_kernel<MT, RT, true, JOIN>, p) : cudaLaunchKernelEx(&cfg, adapter_down_kernel<MT, RT, false, JOIN>, p);
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+    count_launch();
+    return DR_OK;
 }
 template <int RT>
-static void down_launch_rt(const DownPlan& d, const DownParams& p, cudaStream_t s) {
-    if (d.warps_k == 1) down_launch<2, RT, false>(d, p, s);
-    else if (d.mt == 2) down_launch<2, RT, true>(d, p, s);
-    else down_launch<1, RT, true>(d, p, s);
+static int down_launch_rt(const DownPlan& d, const DownParams& p, cudaStream_t s) {
+    if (d.warps_k == 1) return down_launch<2, RT, false>(d, p, s);
+    return d.mt == 2 ? down_launch<2, RT, true>(d, p, s) : down_launch<1, RT, true>(d, p, s);
 }
 
 int adapter_down_run(const DownPlan& d, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
-                     const DropKey& key, float factor, float* out, cudaStream_t s) {
+                     const DropKey& key, float factor, float* out, int* row_id, cudaStream_t s) {
     DownParams p;
     p.rows = rows;
     p.L = L; p.L8 = (L + 7) / 8 * 8; p.R = R; p.Rp = Rp; p.ks = d.ks; p.zsplit = d.zsplit;
     p.l_range = (((L + d.ks - 1) / d.ks) + 63) / 64 * 64;
     p.z = z; p.f = f; p.ldz = ldz; p.ldf = ldf;
-    p.key = key; p.factor = factor; p.out = out;
-    if (d.rt == 1) down_launch_rt<1>(d, p, s);
-    else if (d.rt == 2) down_launch_rt<2>(d, p, s);
-    else if (d.rt == 4) down_launch_rt<4>(d, p, s);
-    else down_launch_rt<8>(d, p, s);
-    count_launch();
-    return launch_status();
+    p.key = key; p.factor = factor; p.out = out; p.row_id = row_id;
+    if (d.rt == 1) return down_launch_rt<1>(d, p, s);
+    if (d.rt == 2) return down_launch_rt<2>(d, p, s);
+    return d.rt == 4 ? down_launch_rt<4>(d, p, s) : down_launch_rt<8>(d, p, s);
 }
 
 // ---- layouts ------------------------------------------------------------------------------------------------------

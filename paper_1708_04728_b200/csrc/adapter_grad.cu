@@ -79,7 +79,7 @@ struct GradParams {
     const int *perm, *start;
     int blocks0;                // column blocks of the first job
     struct Job {
-        int C, ks, ldp, swap;
+        int C, ldp, swap;
         const __nv_bfloat16* z;
         size_t ldz;
         const float *p, *scale;
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(256) adapter_grad_kernel(const GradParams p) {
                         const int r = r0 + 16 * t + 8 * h + g;
                         float s = 0.f;
                         if (row[k] >= 0 && r < p.R)
-                            for (int n = 0; n < j.ks; ++n) s += __ldg(j.p + ((size_t)n * p.M + row[k]) * j.ldp + r);
+                            s = __ldg(j.p + (size_t)row[k] * j.ldp + r);
                         x[h][k] = s * w;
                     }
                 split2(x[0][0], x[0][1], ph[t][0], pl[t][0]);
@@ -255,7 +255,7 @@ int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const Grad
     int blocks[2], most = 0;
     for (int k = 0; k < 2; ++k) {
         const GradJob& g = jobs[k];
-        p.job[k] = {g.C, g.ks, g.ldp, g.swap, g.z, g.ldz, g.p, g.scale, g.factor, g.key, (float*)(ws + plan.part[k]), g.out};
+        p.job[k] = {g.C, g.ldp, g.swap, g.z, g.ldz, g.p, g.scale, g.factor, g.key, (float*)(ws + plan.part[k]), g.out};
         blocks[k] = g.out ? (g.C + 63) / 64 : 0;
         if (g.out) most = std::max(most, g.C);
     }

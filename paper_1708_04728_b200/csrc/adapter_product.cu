@@ -4,7 +4,8 @@
 // A tile of 128 rows (256 by a pair of CTAs) may hold rows of many adapters.  Behind the blocks of 64 l it takes further
 // blocks for the adapters in use among its rows, each with `rank` columns of its own: a row has its T in its adapter's columns and zeros in
 // the others', so the same MMAs serve any mixture of requests, and the work grows with the adapters' bytes, which have to be read anyway.  T
-// enters as the sum of two bfloat16 values (columns twice, high and low), because a single one would cost the adapter's part 2^-9.
+// enters as the sum of two bfloat16 values (its columns twice, high and low), because a single one would cost the adapter's part 2^-9; of three
+// where the result is float32.
 // Where a mask lies between the adapter's product and the sum (the gradient of the input behind a dropout), that product has an accumulator of its own
 // and the drain draws the mask again.
 //
@@ -25,16 +26,19 @@ constexpr int AP_THREADS = 384;
 constexpr int AP_MAX_STAGES = 16;
 constexpr int AP_SMEM = 200 * 1024;
 constexpr int AP_TILE = 128;
-constexpr int AP_EXT = 32;              // columns of T in a further block: high and low fill its 64
+constexpr int AP_CACHE = 32 * 1024;     // T of a tile of few rows
 
 struct ApParams {
     AdRows rows;
-    int L, C, R, Rp, ks;
+    int L, C, R, Rp;
+    int terms, width;           // bfloat16 values to a T, columns of T in a further block of 64: 2 and 32, 3 and 16
     int nt;                     // columns of a tile
     int tiles_c, tiles;
     int kblocks, kpb, main_stages, stages;
     uint32_t a_bytes, b_bytes, stage_bytes;     // of a block of 64 l: z rows, w of this CTA; of a stage
     uint32_t acc_cols, tmem_cols;
+    const int* row_id;          // nullptr: found here, ahead of the kernel in front (few rows)
+    int cache;                  // bytes of T kept in shared memory, or 0
     const float *t, *scale, *bias;
     const __nv_bfloat16* f;
     size_t ldf;
@@ -93,13 +97,27 @@ __device__ __forceinline__ bool finite_only(uint4& v) {
     }
     return any;
 }
-__device__ __forceinline__ float ap_t(const ApParams& p, int m, int r) {
-    float s = 0.f;
-    for (int k = 0; k < p.ks; ++k) s += __ldcg(p.t + ((size_t)k * p.rows.M + m) * p.Rp + r);
-    return s;
+// stages that hold the further blocks of `ext` columns
+__device__ __forceinline__ int further_stages(const ApParams& p, int ext) {
+    const int blocks = (ext + p.width - 1) / p.width;
+    return (blocks + p.kpb - 1) / p.kpb;
+}
+// eight T as bfloat16 values
+template <int TERMS>
+__device__ __forceinline__ void split8(const float* v, float c, uint4* o) {
+    uint32_t u[3][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (TERMS == 2) split2(v[2 * i] * c, v[2 * i + 1] * c, u[0][i], u[1][i]);
+        else split3(v[2 * i] * c, v[2 * i + 1] * c, u[0][i], u[1][i], u[2][i]);
+    }
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) o[k] = make_uint4(u[k][0], u[k][1], u[k][2], u[k][3]);
 }
 
-template <bool PAIR, bool ROWS, bool DUAL>
+// PAIR: tiles of 256 rows by two CTAs.  ROWS: w and f have the contraction index as their rows.  DUAL: an accumulator of its own for the adapters.
+// TERMS: bfloat16 values to a T.
+template <bool PAIR, bool ROWS, bool DUAL, int TERMS>
 __global__ void __launch_bounds__(AP_THREADS, 1)
 adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_w, const ApParams p) {
     extern __shared__ uint8_t ap_raw[];
@@ -111,8 +129,10 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
     const int tile_m = PAIR ? 2 * AP_TILE : AP_TILE;
     const int cols = PAIR ? p.nt >> 1 : p.nt;                  // columns of w that this CTA loads
     volatile int* abort_flag = &sh.abort;
-    // after the ring, 4 KB for each draining warp
+    constexpr int WIDTH = TERMS == 2 ? 32 : 16;
+    // after the ring, 4 KB for each draining warp, and T of a tile of few rows
     const uint32_t stage_out = ring + (uint32_t)p.stages * p.stage_bytes + (p.a_bytes < 16384u ? 16384u - p.a_bytes : 0u);
+    float* const cache = reinterpret_cast<float*>(ap_raw + (stage_out + 4 * 4096u - smem_u32(ap_raw)));
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) { mbar_init(&sh.full[i], PAIR ? 2 : 1); mbar_init(&sh.empty[i], 1); }
@@ -173,7 +193,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 if (!ok) break;
                 const int ib = it & 1;
                 if (!mbar_wait(&sh.ifull[ib], (it >> 1) & 1, abort_flag)) { give_up(82, tile); break; }
-                const int further = (sh.ext[ib] + AP_EXT - 1) / AP_EXT;
+                const int further = further_stages(p, sh.ext[ib]);
                 mbar_arrive(&sh.iempty[ib]);
                 // The parity of a barrier tells two neighbouring phases apart and no more: who waits for a stage must know that the use before the
                 // last one is over.  The builders know it once this tile's loads are all issued; this thread, for the next tile, where
@@ -222,15 +242,17 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 const int ext = sh.ext[ib];
                 const uint32_t de = d + (DUAL ? p.acc_cols : 0u);
                 if (DUAL) accum = 0;
-                for (int c = 0; c < ext; c += AP_EXT) {
+                for (int c = 0; c < ext; c += WIDTH * p.kpb) {
                     if (!mbar_wait_u32(full0 + 8 * s, ph, abort_flag)) { give_up(86, tile); ok = false; break; }
                     tc_fence_after();
-                    const int n16 = min(AP_EXT, ext - c) >> 3;            // w columns, high and low: 2 w / 16 steps
-                    const uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + (uint32_t)p.kpb * p.a_bytes;
-                    const uint32_t al = sdesc_lo(a), bl = ROWS ? sdesc_rows_lo(b, 8192) : sdesc_lo(b);
-                    for (int k = 0; k < n16; ++k) {
-                        umma_bf16_lo<PAIR>(de, al + 2 * k, bl + b_step * k, idesc, accum, 1u);
-                        accum = 1;
+                    uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + (uint32_t)p.kpb * p.a_bytes;
+                    for (int e = c; e < min(ext, c + WIDTH * p.kpb); e += WIDTH, a += p.a_bytes, b += p.b_bytes) {
+                        const int n16 = (TERMS * min(WIDTH, ext - e) + 15) >> 4;
+                        const uint32_t al = sdesc_lo(a), bl = ROWS ? sdesc_rows_lo(b, 8192) : sdesc_lo(b);
+                        for (int k = 0; k < n16; ++k) {
+                            umma_bf16_lo<PAIR>(de, al + 2 * k, bl + b_step * k, idesc, accum, 1u);
+                            accum = 1;
+                        }
                     }
                     umma_commit_u32<PAIR>(empty0 + 8 * s);
                     if (++s == p.stages) { s = 0; ph ^= 1; }
@@ -247,17 +269,22 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
         int s = 0, it = 0;
         uint32_t ph = 0;
         bool ok = true, waited = false;
+        if (p.row_id) { grid_dependency_wait(); waited = true; }               // the rows' adapters, and t, are the kernel's in front
         for (int tile = unit; tile < p.tiles && ok; tile += units, ++it) {
             const int ib = it & 1;
             const int mt = tile / p.tiles_c, ct = tile - mt * p.tiles_c;
             sh.bits[bt] = 0;
-            const bool free_now = mbar_wait(&sh.iempty[ib], ((it >> 1) & 1) ^ 1, abort_flag);
-            if (!free_now) give_up(87, tile);
-            if (builders_any(!free_now)) break;
             int id[PAIR ? 2 : 1];
 #pragma unroll
             for (int h = 0; h < (PAIR ? 2 : 1); ++h) {
-                id[h] = adapter_of_warp_row(p.rows, mt * tile_m + h * AP_TILE + (bt & ~31), lane);
+                const int m = mt * tile_m + h * AP_TILE + bt;
+                id[h] = !p.row_id ? adapter_of_warp_row(p.rows, m - lane, lane) : m < p.rows.M ? __ldcg(p.row_id + m) : ROW_NONE;
+            }
+            const bool free_now = mbar_wait(&sh.iempty[ib], ((it >> 1) & 1) ^ 1, abort_flag);
+            if (!free_now) give_up(87, tile);
+            if (builders_any(!free_now)) break;
+#pragma unroll
+            for (int h = 0; h < (PAIR ? 2 : 1); ++h) {
                 const unsigned same = __match_any_sync(0xffffffffu, id[h]);
                 if (id[h] >= 0 && __ffs(same) - 1 == lane) atomicOr(&sh.bits[id[h] >> 5], 1u << (id[h] & 31));
             }
@@ -290,47 +317,24 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
             while (s >= p.stages) { s -= p.stages; ph ^= 1; }
 
             const int m = mt * tile_m + (int)rank * AP_TILE + bt, c0 = ct * p.nt + (int)rank * cols;
-            if (!waited) { grid_dependency_wait(); waited = true; }            // t is the kernel's in front
-            const float scale = own >= 0 && p.scale ? __ldg(p.scale + own) : 1.f;
-            if (p.keep && ct == 0 && own == ROW_SHARED)
-                for (int r = 0; r < p.R; ++r) p.keep[(size_t)m * p.R + r] = 0.f;
-            for (int e0 = 0; e0 < ext; e0 += AP_EXT) {
-                const int w = min(AP_EXT, ext - e0), wc = w >> 3;
-                uint4 hi[4], lo[4], fv[8];
-                // T of this thread's row
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    hi[j] = lo[j] = make_uint4(0, 0, 0, 0);
-                    const int r = e0 + 8 * j - slot * p.Rp;
-                    if (slot >= 0 && r >= 0 && r < p.Rp && j < wc) {
-                        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                        for (int k = 0; k < p.ks; ++k) {
-                            const float4* src = reinterpret_cast<const float4*>(p.t + ((size_t)k * p.rows.M + m) * p.Rp + r);
-                            const float4 x = __ldcg(src), y = __ldcg(src + 1);
-                            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-                        }
-                        if (p.keep && ct == 0) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) if (r + i < p.R) p.keep[(size_t)m * p.R + r + i] = v[i];
-                        }
-                        const float c = scale * p.factor;
-                        split2(v[0] * c, v[1] * c, hi[j].x, lo[j].x);
-                        split2(v[2] * c, v[3] * c, hi[j].y, lo[j].y);
-                        split2(v[4] * c, v[5] * c, hi[j].z, lo[j].z);
-                        split2(v[6] * c, v[7] * c, hi[j].w, lo[j].w);
-                    }
-                }
-                // f of the adapters in use
+            const float scale = (own >= 0 && p.scale ? __ldg(p.scale + own) : 1.f) * p.factor;
+            float* const keep = p.keep && ct == 0 && own != ROW_NONE ? p.keep + (size_t)m * p.R : nullptr;
+            if (keep && own == ROW_SHARED)
+                for (int r = 0; r < p.R; ++r) keep[r] = 0.f;
+            // a thread's pieces of f: of sub-block j its rows row0 + k * step, 16 bytes at cj
+            const int cpr = ROWS ? cols >> 3 : 4;                              // 16-byte pieces of a row of a block
+            const int cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
+            const int each = ((ROWS ? WIDTH : cols) + step - 1) / step;        // pieces of a sub-block: kpb * each <= 8
+            for (int e0 = 0; e0 < ext; e0 += WIDTH * p.kpb) {
+                uint4 fv[8], tv[4][TERMS];
                 bool odd = false;
-                const int cpr = ROWS ? cols >> 3 : 4;                          // 16-byte pieces of a row of the block
-                const int cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
-                const int nrows = ROWS ? w : cols;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     fv[i] = make_uint4(0, 0, 0, 0);
-                    const int row = row0 + i * step;
-                    if (row < nrows && (ROWS || cj < wc)) {
-                        const int e = e0 + (ROWS ? row : 8 * cj), d = e / p.Rp, r = e - d * p.Rp;
+                    const int j = p.kpb == 1 ? 0 : i / each, row = row0 + (i - j * each) * step;
+                    const int eb = e0 + j * WIDTH, w = min(WIDTH, ext - eb);
+                    if (j < p.kpb && w > 0 && row < (ROWS ? w : cols) && (ROWS || 8 * cj < w)) {
+                        const int e = eb + (ROWS ? row : 8 * cj), d = e / p.Rp, r = e - d * p.Rp;
                         const int a = sh.list[ib][d];
                         if (ROWS) {
                             const int c = c0 + 8 * cj;
@@ -342,13 +346,43 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                             } else {
                                 unsigned short h[8];
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) h[k] = r + k < p.R ? __ldg(reinterpret_cast<const unsigned short*>(src) + k) : (unsigned short)0;
+                                for (int q = 0; q < 8; ++q) h[q] = r + q < p.R ? __ldg(reinterpret_cast<const unsigned short*>(src) + q) : (unsigned short)0;
                                 fv[i] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
                             }
                         }
-                        odd |= finite_only(fv[i]);
                     }
                 }
+                if (e0 == 0) {
+                    if (!waited) { grid_dependency_wait(); waited = true; }
+                    if (p.cache && slot >= 0) {
+                        for (int r = 0; r < p.Rp; r += 4) *reinterpret_cast<float4*>(cache + (size_t)bt * p.Rp + r) = __ldcg(reinterpret_cast<const float4*>(p.t + (size_t)m * p.Rp + r));
+                        if (keep) for (int r = 0; r < p.R; ++r) keep[r] = cache[(size_t)bt * p.Rp + r];
+                    }
+                }
+                // T of this thread's row in sub-block `eb`
+                auto load_t = [&](int eb) {
+                    const int w = min(WIDTH, ext - eb);
+#pragma unroll
+                    for (int j = 0; j < WIDTH / 8; ++j) {
+#pragma unroll
+                        for (int k = 0; k < TERMS; ++k) tv[j][k] = make_uint4(0, 0, 0, 0);
+                        const int r = eb + 8 * j - slot * p.Rp;
+                        if (slot >= 0 && r >= 0 && r < p.Rp && 8 * j < w) {
+                            float v[8];
+                            const float4* src = reinterpret_cast<const float4*>((p.cache ? cache + (size_t)bt * p.Rp : p.t + (size_t)m * p.Rp) + r);
+                            const float4 x = p.cache ? src[0] : __ldcg(src), y = p.cache ? src[1] : __ldcg(src + 1);
+                            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+                            if (keep && !p.cache) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) if (r + i < p.R) keep[r + i] = v[i];
+                            }
+                            split8<TERMS>(v, scale, tv[j]);
+                        }
+                    }
+                };
+                load_t(e0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) odd |= finite_only(fv[i]);
                 if (odd) {
                     // Both CTAs of a pair drain all columns: each is told.  The number only grows, so that a CTA that runs ahead hides nothing
                     // from one behind; a number ahead of a tile's costs that tile a search for entries it does not have.
@@ -363,26 +397,35 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                                                                    mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag));
                 if (!slot_free) give_up(88, tile);
                 if (slot_free) {
-                    const uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + (uint32_t)p.kpb * p.a_bytes;
-                    if ((uint32_t)bt * 128u < p.a_bytes) {
+                    const uint32_t a0 = ring + (uint32_t)s * p.stage_bytes, b0 = a0 + (uint32_t)p.kpb * p.a_bytes;
+                    for (int j = 0; j < p.kpb && e0 + j * WIDTH < ext; ++j) {
+                        if (j > 0) load_t(e0 + j * WIDTH);
+                        const int w = min(WIDTH, ext - e0 - j * WIDTH), wc = w >> 3;
+                        const uint32_t a = a0 + (uint32_t)j * p.a_bytes;
+                        if ((uint32_t)bt * 128u < p.a_bytes) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (j < wc) {
-                                st_shared16(a + bt * 128 + ((j ^ (bt & 7)) << 4), hi[j]);
-                                st_shared16(a + bt * 128 + (((j + wc) ^ (bt & 7)) << 4), lo[j]);
-                            }
+                            for (int i = 0; i < WIDTH / 8; ++i)
+                                if (i < wc) {
+#pragma unroll
+                                    for (int k = 0; k < TERMS; ++k) st_shared16(a + bt * 128 + (((i + k * wc) ^ (bt & 7)) << 4), tv[i][k]);
+                                }
+                            if (TERMS == 3 && wc == 1) st_shared16(a + bt * 128 + ((3 ^ (bt & 7)) << 4), make_uint4(0, 0, 0, 0));     // 24 columns: two steps of 16
+                        }
                     }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int row = row0 + i * step;
-                        if (row < nrows && (ROWS || cj < wc)) {
+                        const int j = p.kpb == 1 ? 0 : i / each, row = row0 + (i - j * each) * step;
+                        const int w = min(WIDTH, ext - e0 - j * WIDTH), wc = w >> 3;
+                        if (j < p.kpb && w > 0 && row < (ROWS ? w : cols) && (ROWS || cj < wc)) {
+                            const uint32_t b = b0 + (uint32_t)j * p.b_bytes;
                             if (ROWS) {
                                 const uint32_t g = b + (uint32_t)(cj >> 3) * 8192u;
-                                st_shared16(g + row * 128 + (((cj & 7) ^ (row & 7)) << 4), fv[i]);
-                                st_shared16(g + (row + w) * 128 + (((cj & 7) ^ ((row + w) & 7)) << 4), fv[i]);
+#pragma unroll
+                                for (int k = 0; k < TERMS; ++k) st_shared16(g + (row + k * w) * 128 + (((cj & 7) ^ ((row + k * w) & 7)) << 4), fv[i]);
                             } else {
-                                st_shared16(b + row * 128 + ((cj ^ (row & 7)) << 4), fv[i]);
-                                st_shared16(b + row * 128 + (((cj + wc) ^ (row & 7)) << 4), fv[i]);
+#pragma unroll
+                                for (int k = 0; k < TERMS; ++k) st_shared16(b + row * 128 + (((cj + k * wc) ^ (row & 7)) << 4), fv[i]);
+                                if (TERMS == 3 && wc == 1) st_shared16(b + row * 128 + ((3 ^ (row & 7)) << 4), make_uint4(0, 0, 0, 0));
                             }
                         }
                     }
@@ -443,7 +486,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                     const float w = (p.scale ? p.scale[a] : 1.f) * p.factor;
 #pragma unroll 1
                     for (int r = 0; r < p.R; ++r) {
-                        const float tv = ap_t(p, m, r) * w;
+                        const float tv = __ldcg(p.t + (size_t)m * p.Rp + r) * w;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
                             if (n0 + c + i >= p.C) continue;
@@ -546,10 +589,10 @@ static int ap_map(CUtensorMap* map, const void* ptr, size_t rows, size_t inner, 
     return tmap_tiled(map, 2, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
-template <bool PAIR, bool ROWS, bool DUAL>
+template <bool PAIR, bool ROWS, bool DUAL, int TERMS>
 static int ap_launch(const CUtensorMap& mz, const CUtensorMap& mw, const ApParams& p, bool overlap, size_t smem, cudaStream_t s) {
     static PerDeviceFlag ready;
-    auto* k = adapter_product_kernel<PAIR, ROWS, DUAL>;
+    auto* k = adapter_product_kernel<PAIR, ROWS, DUAL, TERMS>;
     if (!ready.get()) {
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 8192 - 1024) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
         ready.set();
@@ -582,7 +625,7 @@ static int ap_launch(const CUtensorMap& mz, const CUtensorMap& mw, const ApParam
 int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
     ApParams p = {};
     p.rows = a.rows;
-    p.L = a.L; p.C = a.C; p.R = a.R; p.Rp = a.Rp; p.ks = a.ks;
+    p.L = a.L; p.C = a.C; p.R = a.R; p.Rp = a.Rp;
     p.t = a.t; p.scale = a.scale; p.bias = a.bias; p.f = a.f; p.ldf = a.ldf; p.factor = a.factor; p.keep = a.keep;
     p.f_vec = !a.transposed && (a.R & 7) == 0;
     p.flags = a.flags; p.out = a.out; p.ldo = a.ldo; p.key = a.key;
@@ -619,25 +662,31 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
     const uint32_t block = p.a_bytes + p.b_bytes;
     p.kpb = block <= 8192 ? 4 : block <= 16384 ? 2 : 1;
     p.kpb = std::min(p.kpb, p.kblocks);
+    p.terms = (a.flags & DR_OUT_F32) ? 3 : 2;
+    p.width = p.terms == 2 ? 32 : 16;
+    p.row_id = M > AP_TILE ? a.row_id : nullptr;
+    p.cache = p.kpb > 1 ? (M * a.Rp * 4 + 1023) / 1024 * 1024 : 0;
+    if (p.cache > AP_CACHE) { p.cache = 0; p.kpb = 1; }
     p.main_stages = (p.kblocks + p.kpb - 1) / p.kpb;
     p.stage_bytes = (uint32_t)p.kpb * block;
     const uint32_t slack = p.a_bytes < 16384u ? 16384u - p.a_bytes : 0u;      // the MMA reads 128 rows from the last stage on
-    p.stages = (int)std::min<uint32_t>(AP_MAX_STAGES, (AP_SMEM - slack) / p.stage_bytes);
+    p.stages = (int)std::min<uint32_t>(AP_MAX_STAGES, (AP_SMEM - p.cache - slack) / p.stage_bytes);
     p.acc_cols = 32;
     while ((int)p.acc_cols < nt) p.acc_cols *= 2;
     p.tmem_cols = p.acc_cols * (dual ? 4 : 2);
-    const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes + slack + 4 * 4096;
+    const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes + slack + 4 * 4096 + p.cache;
     alignas(64) CUtensorMap mz, mw;
     int rc = ap_map(&mz, a.z, M, a.L, a.ldz, 64, a_rows);
     if (rc != DR_OK) return rc;
     rc = a.transposed ? ap_map(&mw, a.w, a.L, a.C, a.ldw, 64, 64) : ap_map(&mw, a.w, a.C, a.L, a.ldw, 64, cols);
     if (rc != DR_OK) return rc;
-    if (pair) {
-        if (!a.transposed) return ap_launch<true, false, false>(mz, mw, p, overlap, smem, s);
-        return dual ? ap_launch<true, true, true>(mz, mw, p, overlap, smem, s) : ap_launch<true, true, false>(mz, mw, p, overlap, smem, s);
+    const bool f32 = p.terms == 3;
+    if (a.transposed) {
+        if (pair) return dual ? ap_launch<true, true, true, 2>(mz, mw, p, overlap, smem, s) : ap_launch<true, true, false, 2>(mz, mw, p, overlap, smem, s);
+        return dual ? ap_launch<false, true, true, 2>(mz, mw, p, overlap, smem, s) : ap_launch<false, true, false, 2>(mz, mw, p, overlap, smem, s);
     }
-    if (!a.transposed) return ap_launch<false, false, false>(mz, mw, p, overlap, smem, s);
-    return dual ? ap_launch<false, true, true>(mz, mw, p, overlap, smem, s) : ap_launch<false, true, false>(mz, mw, p, overlap, smem, s);
+    if (pair) return f32 ? ap_launch<true, false, false, 3>(mz, mw, p, overlap, smem, s) : ap_launch<true, false, false, 2>(mz, mw, p, overlap, smem, s);
+    return f32 ? ap_launch<false, false, false, 3>(mz, mw, p, overlap, smem, s) : ap_launch<false, false, false, 2>(mz, mw, p, overlap, smem, s);
 }
 
 }  // namespace dr
