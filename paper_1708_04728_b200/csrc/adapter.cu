@@ -138,9 +138,9 @@ extern "C" int dr_adapter(const dr_adapter_desc* d, int M, const void* x, int ld
     if ((rc = place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, ws, f.a, &ap, &ldap, s)) != DR_OK) return rc;
     float* const tw = (float*)(ws + f.t);
     int* const ids = (int*)(ws + f.ids);
-    rc = adapter_down_run(f.down, rows, K, R, f.Rp, xp, ldxp, ap, ldap, key, key.thr ? key.scale : 1.f, tw, ids, s);
+    rc = adapter_down_run(f.down, rows, K, R, f.Rp, xp, ldxp, ap, ldap, key, key.thr ? key.scale : 1.f, tw, t, ids, s);
     if (rc != DR_OK) return rc;
-    const ProductArgs g = {rows, K, N, R, f.Rp, xp, wp, (const __nv_bfloat16*)b, ldxp, ldwp, 0, ids, tw, scale, bias, 1.f, t, d->flags, y, (size_t)ldy, false, none};
+    const ProductArgs g = {rows, K, N, R, f.Rp, xp, wp, (const __nv_bfloat16*)b, ldxp, ldwp, 0, ids, tw, scale, bias, 1.f, d->flags, y, (size_t)ldy, false, none};
     return adapter_product_run(g, true, s);
 }
 
@@ -184,10 +184,10 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     if (dx || da) {
         __nv_bfloat16* const bt = (__nv_bfloat16*)(ws + f.bt);
         if ((rc = adapter_transpose_run(d->adapters, N, R, (const __nv_bfloat16*)b, bt, f.Np, s)) != DR_OK) return rc;
-        if ((rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, u, ids, s)) != DR_OK) return rc;
+        if ((rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, u, nullptr, ids, s)) != DR_OK) return rc;
     }
     if (dx) {
-        const ProductArgs g = {rows, N, K, R, f.Rp, dyp, wp, ap, lddyp, ldwp, ldap, ids, u, scale, nullptr, kept, nullptr, 0, dx, (size_t)lddx, true, key};
+        const ProductArgs g = {rows, N, K, R, f.Rp, dyp, wp, ap, lddyp, ldwp, ldap, ids, u, scale, nullptr, kept, 0, dx, (size_t)lddx, true, key};
         if ((rc = adapter_product_run(g, true, s)) != DR_OK) return rc;
     }
     if (da || db) {

@@ -88,11 +88,12 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t&
 }
 
 // ---- launches (adapter_down.cu, adapter_product.cu, adapter_grad.cu) -------------------------------------------------------
-// out[m][r] = factor * sum_l D(z)[m][l] f_a[r][l] in rows of Rp, and each row's adapter; f [adapters * R][ldf], 16-byte aligned rows, zeros behind L
+// out[m][r] = factor * sum_l D(z)[m][l] f_a[r][l] in rows of Rp, the same in rows of R in keep (may be nullptr; zeros where a row has no adapter, nothing
+// where it has no request), and each row's adapter; f [adapters * R][ldf], 16-byte aligned rows, zeros behind L
 struct DownPlan { int mt, warps_k, rows_cta, ks, zsplit, rt, rchunks; };
 DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments);
 int adapter_down_run(const DownPlan& plan, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
-                     const DropKey& key, float factor, float* out, int* row_id, cudaStream_t s);
+                     const DropKey& key, float factor, float* out, float* keep, int* row_id, cudaStream_t s);
 
 // out[m][c] = act(sum_l z[m][l] w + bias[c] + D(scale_a factor t[m] f_a)):   forward w [C][ldw] (rows of l), f [adapters][C][R];
 // transposed w [L][ldw] (rows of c), f [adapters][R][ldf]
@@ -104,7 +105,6 @@ struct ProductArgs {
     const int* row_id;
     const float *t, *scale, *bias;
     float factor;
-    float* keep;                // forward: t as the caller keeps it
     unsigned flags;
     void* out;
     size_t ldo;

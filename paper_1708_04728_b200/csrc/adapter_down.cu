@@ -21,7 +21,7 @@ struct DownParams {
     size_t ldz, ldf;
     DropKey key;
     float factor;
-    float* out;
+    float *out, *keep;
     int* row_id;
 };
 
@@ -54,6 +54,12 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) zr[t][h] = p.z + (size_t)min(m0 + 16 * t + 8 * h + g, p.rows.M - 1) * p.ldz;
 
+    auto put = [&](int row, int r, float v) {                    // row of this warp's, column of all
+        p.out[(size_t)(m0 + row) * p.Rp + r] = v;
+        if (p.keep && r < p.R) p.keep[(size_t)(m0 + row) * p.R + r] = v;
+    };
+    if (p.keep && id == ROW_SHARED && blockIdx.y == 0 && zi == 0 && (!JOIN || warp == 0))
+        for (int r = r0; r < min(p.R, r0 + RT * 8); ++r) p.keep[(size_t)(m0 + lane) * p.R + r] = 0.f;
     int number = 0;
     for (unsigned rest = __ballot_sync(0xffffffffu, id >= 0); rest;) {
         const int a = __shfl_sync(0xffffffffu, id, __ffs(rest) - 1);
@@ -119,7 +125,7 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
 #pragma unroll
                     for (int w = 1; w < 8; ++w) s += join[w][row][r];
                     if (p.ks > 1) range[i] = s;
-                    else if ((mine >> (16 * t + row) & 1) && r0 + r < p.Rp) p.out[(size_t)(m0 + 16 * t + row) * p.Rp + r0 + r] = s * p.factor;
+                    else if ((mine >> (16 * t + row) & 1) && r0 + r < p.Rp) put(16 * t + row, r0 + r, s * p.factor);
                 }
                 if (p.ks > 1) {
                     ptx::cluster_sync_all();
@@ -131,7 +137,7 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
                             asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ptx::mapa_shared(ptx::smem_u32(range + i), (uint32_t)k)) : "memory");
                             s += v;
                         }
-                        if ((mine >> (16 * t + row) & 1) && r0 + r < p.Rp) p.out[(size_t)(m0 + 16 * t + row) * p.Rp + r0 + r] = s * p.factor;
+                        if ((mine >> (16 * t + row) & 1) && r0 + r < p.Rp) put(16 * t + row, r0 + r, s * p.factor);
                     }
                     ptx::cluster_sync_all();                     // the sums are read: they may be overwritten, the CTA may leave
                 } else {
@@ -146,8 +152,15 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int row = 16 * t + 8 * h + g, c = r0 + 8 * r + 2 * q;
-                        if ((mine >> row & 1) && c < p.Rp)
-                            *reinterpret_cast<float2*>(p.out + (size_t)(m0 + row) * p.Rp + c) = make_float2(acc[t][r][2 * h] * p.factor, acc[t][r][2 * h + 1] * p.factor);
+                        if ((mine >> row & 1) && c < p.Rp) {
+                            const float2 v = make_float2(acc[t][r][2 * h] * p.factor, acc[t][r][2 * h + 1] * p.factor);
+                            *reinterpret_cast<float2*>(p.out + (size_t)(m0 + row) * p.Rp + c) = v;
+                            if (p.keep) {
+                                float* to = p.keep + (size_t)(m0 + row) * p.R + c;
+                                if (c < p.R) to[0] = v.x;
+                                if (c + 1 < p.R) to[1] = v.y;
+                            }
+                        }
                     }
         }
     }
@@ -197,13 +210,13 @@ static int down_launch_rt(const DownPlan& d, const DownParams& p, cudaStream_t s
 }
 
 int adapter_down_run(const DownPlan& d, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
-                     const DropKey& key, float factor, float* out, int* row_id, cudaStream_t s) {
+                     const DropKey& key, float factor, float* out, float* keep, int* row_id, cudaStream_t s) {
     DownParams p;
     p.rows = rows;
     p.L = L; p.L8 = (L + 7) / 8 * 8; p.R = R; p.Rp = Rp; p.ks = d.ks; p.zsplit = d.zsplit;
     p.l_range = (((L + d.ks - 1) / d.ks) + 63) / 64 * 64;
     p.z = z; p.f = f; p.ldz = ldz; p.ldf = ldf;
-    p.key = key; p.factor = factor; p.out = out; p.row_id = row_id;
+    p.key = key; p.factor = factor; p.out = out; p.keep = keep; p.row_id = row_id;
     if (d.rt == 1) return down_launch_rt<1>(d, p, s);
     if (d.rt == 2) return down_launch_rt<2>(d, p, s);
     return d.rt == 4 ? down_launch_rt<4>(d, p, s) : down_launch_rt<8>(d, p, s);

@@ -29,7 +29,6 @@ constexpr int AP_MAX_STAGES = 16;
 constexpr int AP_SMEM = 184 * 1024;     // the ring's; with 32 KB of the drain's and the barriers' all of an SM's
 constexpr int AP_SMEM_MOST = 217 * 1024;
 constexpr int AP_TILE = 128;
-constexpr int AP_CACHE = 32 * 1024;     // T of a tile of few rows
 
 struct ApParams {
     AdRows rows;
@@ -37,17 +36,16 @@ struct ApParams {
     uint32_t rp_magic;          // 2^32 / Rp, rounded up: columns / Rp by a multiplication
     int nt;                     // columns of a tile
     int tiles_c, tiles;
-    int kblocks, main_stages, stages;
+    int kblocks, stages;
     uint32_t a_bytes, b_bytes, stage_bytes;     // of a block of 64 l: z rows, w of this CTA; of a stage
     uint32_t acc_cols, tmem_cols;
-    const int* row_id;          // nullptr: found here, ahead of the kernel in front (few rows)
-    int cache;                  // bytes of T kept in shared memory, or 0
+    int split;                  // few rows: CTAs of a cluster that share a tile's l
+    const int* row_id;
     const float *t, *scale, *bias;
     const __nv_bfloat16* f;
     size_t ldf;
     int f_vec;
     float factor;
-    float* keep;
     unsigned flags;
     void* out;
     size_t ldo;
@@ -56,6 +54,12 @@ struct ApParams {
     int* status;
 };
 
+struct ApFind {
+    int lowest[4], highest[4];
+    uint32_t bits[128];
+    int before[128];
+    int sums[4];
+};
 struct ApShared {
     uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], tfull[2], tempty[2], ifull[2], iempty[2], loads[2], built[2];
     uint32_t tmem;
@@ -64,9 +68,7 @@ struct ApShared {
     int odd[2];                 // number (from 1) of the latest tile that met an f that is not finite
     int slot[2][AP_TILE];       // place of the row's adapter in list, ROW_SHARED or ROW_NONE
     uint16_t list[2][2 * AP_TILE];
-    uint32_t bits[128];
-    int before[128];
-    int sums[4];
+    ApFind find;
     alignas(16) float bias[2][512];
 };
 
@@ -113,17 +115,159 @@ __device__ __forceinline__ void split8(const float* v, float c, uint4* o) {
     for (int k = 0; k < TERMS; ++k) o[k] = make_uint4(u[k][0], u[k][1], u[k][2], u[k][3]);
 }
 
-// What one kernel is compiled for.  KPB: blocks of 64 l to a stage.  PAIR: tiles of 256 rows by two CTAs.  WIDE (pairs): two accumulators of 256
+// What one kernel is compiled for.  PAIR: tiles of 256 rows by two CTAs.  WIDE (pairs): two accumulators of 256
 // columns share the rows' blocks, each with an issuing warp of its own.  ROWS: w and f have the contraction index as their rows.  DUAL: an
 // accumulator of its own for the adapters.  TERMS: bfloat16 values to a T.
-template <int KPB_, bool PAIR_, bool WIDE_, bool ROWS_, bool DUAL_, int TERMS_>
+template <bool PAIR_, bool WIDE_, bool ROWS_, bool DUAL_, int TERMS_>
 struct ApKind {
-    static constexpr int KPB = KPB_, TERMS = TERMS_;
+    static constexpr int TERMS = TERMS_;
     static constexpr bool PAIR = PAIR_, WIDE = WIDE_, ROWS = ROWS_, DUAL = DUAL_;
     static constexpr int WIDTH = TERMS == 2 ? 32 : 16;         // columns of T in a further block of 64
-    static constexpr int STAGE_WIDTH = WIDTH * KPB;
-    static constexpr int EACH = 8 / KPB;                        // 16-byte pieces of a block's f that a thread brings
+    static constexpr int EACH = 8;                              // 16-byte pieces of a block's f that a thread brings, at most
 };
+
+// ---- the builders' steps (128 threads, bt their number) --------------------------------------------------------------------
+// The adapters in use among the rows whose adapters id[] are (N of them a thread): their list in ascending order, this thread's places in it (or id
+// itself where that is none), and how many there are.
+template <int N>
+__device__ __forceinline__ int ap_find(ApFind& f, uint16_t* list, const int (&id)[N], int (&slot)[N], int bt) {
+    const int lane = bt & 31, w = bt >> 5;
+    int lo = 0x7fffffff, hi = -1;
+#pragma unroll
+    for (int h = 0; h < N; ++h) {
+        lo = min(lo, id[h] >= 0 ? id[h] : 0x7fffffff);
+        hi = max(hi, id[h]);
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) { f.lowest[w] = lo; f.highest[w] = hi; }
+    f.bits[bt] = 0;
+    builders_sync();
+    lo = min(min(f.lowest[0], f.lowest[1]), min(f.lowest[2], f.lowest[3]));
+    hi = max(max(f.highest[0], f.highest[1]), max(f.highest[2], f.highest[3]));
+    if (hi < 0 || lo == hi) {                       // none, or one: most tiles
+        if (bt == 0) list[0] = (uint16_t)max(hi, 0);
+#pragma unroll
+        for (int h = 0; h < N; ++h) slot[h] = id[h] >= 0 ? 0 : id[h];
+        return hi < 0 ? 0 : 1;
+    }
+#pragma unroll
+    for (int h = 0; h < N; ++h)
+        if (id[h] >= 0) atomicOr(&f.bits[id[h] >> 5], 1u << (id[h] & 31));
+    builders_sync();
+    const uint32_t word = f.bits[bt];
+    const int n = __popc(word);
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) f.sums[w] = incl;
+    builders_sync();
+    int at = incl - n;
+    for (int k = 0; k < w; ++k) at += f.sums[k];
+    f.before[bt] = at;
+    for (uint32_t x = word; x; x &= x - 1) list[at++] = (uint16_t)(bt * 32 + __ffs(x) - 1);
+    builders_sync();
+#pragma unroll
+    for (int h = 0; h < N; ++h) slot[h] = id[h] >= 0 ? f.before[id[h] >> 5] + __popc(f.bits[id[h] >> 5] & ((1u << (id[h] & 31)) - 1u)) : id[h];
+    return f.sums[0] + f.sums[1] + f.sums[2] + f.sums[3];
+}
+
+// This thread's pieces of f in the block of `eb`: rows row0 + i * step of the block (ROWS: contraction rows, else columns of the output), 16 bytes at cj;
+// column(i): the output column that place i of the CTA's is.  Returns whether one was not finite (those are made zero).
+template <class Kind, class Column>
+__device__ __forceinline__ void ap_load_f(const ApParams& p, const uint16_t* list, int eb, int w, int cols, int row0, int step, int cj, Column column, uint4 (&fv)[Kind::EACH]) {
+    const int ef = eb + 8 * cj, df = (int)__umulhi((uint32_t)ef, p.rp_magic), rf = ef - df * p.Rp;
+    const bool mine = Kind::ROWS || 8 * cj < w;
+    const int c_rows = Kind::ROWS ? column(8 * cj) : 0;
+    const __nv_bfloat16* fa = p.f + (Kind::ROWS ? (size_t)c_rows : mine ? (size_t)list[df] * p.C * p.R + rf : 0);
+#pragma unroll
+    for (int i = 0; i < Kind::EACH; ++i) {
+        fv[i] = make_uint4(0, 0, 0, 0);
+        const int row = row0 + i * step;
+        if (Kind::ROWS) {
+            if (row < w && c_rows < p.C) {
+                const int e = eb + row, d = (int)__umulhi((uint32_t)e, p.rp_magic), r = e - d * p.Rp;
+                if (r < p.R) fv[i] = __ldg(reinterpret_cast<const uint4*>(fa + ((size_t)list[d] * p.R + r) * p.ldf));
+            }
+        } else {
+            const int c = column(row);
+            if (mine && row < cols && c < p.C) {
+                const __nv_bfloat16* src = fa + (size_t)c * p.R;
+                if (p.f_vec) {
+                    fv[i] = __ldg(reinterpret_cast<const uint4*>(src));
+                } else {
+                    unsigned short h[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) h[q] = rf + q < p.R ? __ldg(reinterpret_cast<const unsigned short*>(src) + q) : (unsigned short)0;
+                    fv[i] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+                }
+            }
+        }
+    }
+}
+// T of this thread's row in the block of `eb`: eight columns at a time, high and low values
+template <class Kind, bool SHARED>
+__device__ __forceinline__ void ap_load_t(const float* trow, int slot, int Rp, int eb, int w, float scale, uint4 (&tv)[Kind::WIDTH / 8][Kind::TERMS]) {
+#pragma unroll
+    for (int j = 0; j < Kind::WIDTH / 8; ++j) {
+#pragma unroll
+        for (int k = 0; k < Kind::TERMS; ++k) tv[j][k] = make_uint4(0, 0, 0, 0);
+        const int r = eb + 8 * j - slot * Rp;
+        if (slot >= 0 && (unsigned)r < (unsigned)Rp && 8 * j < w) {
+            const float4* src = reinterpret_cast<const float4*>(trow + r);
+            const float4 x = SHARED ? src[0] : __ldcg(src), y = SHARED ? src[1] : __ldcg(src + 1);
+            const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+            split8<Kind::TERMS>(v, scale, tv[j]);
+        }
+    }
+}
+// both into the stage: z's part at a (rows of 128 bytes), w's at b
+template <class Kind>
+__device__ __forceinline__ void ap_store_block(uint32_t a, uint32_t b, int bt, bool row_there, int w, int cols, int row0, int step, int cj, const uint4 (&fv)[Kind::EACH],
+                                               const uint4 (&tv)[Kind::WIDTH / 8][Kind::TERMS]) {
+    const int wc = w >> 3;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    if (row_there) {
+        const uint32_t at = a + bt * 128, x = (uint32_t)(bt & 7);
+#pragma unroll
+        for (int i = 0; i < Kind::WIDTH / 8; ++i)
+            if (i < wc) {
+#pragma unroll
+                for (int k = 0; k < Kind::TERMS; ++k) st_shared16(at + (((uint32_t)(i + k * wc) ^ x) << 4), tv[i][k]);
+            }
+        if (Kind::TERMS == 3 && wc == 1) st_shared16(at + ((3u ^ x) << 4), zero);              // 24 columns: two steps of 16
+    }
+#pragma unroll
+    for (int i = 0; i < Kind::EACH; ++i) {
+        const int row = row0 + i * step;
+        if (Kind::ROWS) {
+            if (row < w) {
+                const uint32_t g = b + (uint32_t)(cj >> 3) * 8192u;
+#pragma unroll
+                for (int k = 0; k < Kind::TERMS; ++k) st_shared16(g + (row + k * w) * 128 + (((cj & 7) ^ ((row + k * w) & 7)) << 4), fv[i]);
+            }
+        } else if (row < cols && cj < wc) {
+            const uint32_t at = b + row * 128, x = (uint32_t)(row & 7);
+#pragma unroll
+            for (int k = 0; k < Kind::TERMS; ++k) st_shared16(at + (((uint32_t)(cj + k * wc) ^ x) << 4), fv[i]);
+            if (Kind::TERMS == 3 && wc == 1) st_shared16(at + ((3u ^ x) << 4), zero);
+        }
+    }
+}
+// what entries of f that are not finite add to out[m][c]: an infinity, NaN, or 0
+template <bool ROWS>
+__device__ __noinline__ float ap_odd(const ApParams& p, int a, int m, int c) {
+    const float w = (p.scale ? p.scale[a] : 1.f) * p.factor;
+    float s = 0.f;
+    for (int r = 0; r < p.R; ++r) {
+        const float fr = __bfloat162float(ROWS ? p.f[((size_t)a * p.R + r) * p.ldf + c] : p.f[((size_t)a * p.C + c) * p.R + r]);
+        if (!(fabsf(fr) <= 3.4e38f)) s = fmaf(__ldcg(p.t + (size_t)m * p.Rp + r) * w, fr, s);
+    }
+    return s;
+}
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -137,9 +281,10 @@ __device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
 
 template <class Kind>
 __global__ void __launch_bounds__(AP_THREADS, 1)
-adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_w, const ApParams p) {
+adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_out,
+                       const __grid_constant__ ApParams p) {
     constexpr bool PAIR = Kind::PAIR, WIDE = Kind::WIDE, ROWS = Kind::ROWS, DUAL = Kind::DUAL;
-    constexpr int KPB = Kind::KPB, TERMS = Kind::TERMS, WIDTH = Kind::WIDTH;
+    constexpr int TERMS = Kind::TERMS, WIDTH = Kind::WIDTH;
     extern __shared__ uint8_t ap_raw[];
     __shared__ ApShared sh;
     const uint32_t ring = (smem_u32(ap_raw) + 1023u) & ~1023u;
@@ -151,10 +296,8 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
     // column of the output that place i of them is: a wide tile's halves are 256 columns apart, 128 of each in either CTA
     auto column = [&](int i) { return WIDE ? (i >> 7) * 256 + (int)rank * 128 + (i & 127) : (int)rank * cols + i; };
     volatile int* abort_flag = &sh.abort;
-    // after the ring, 4 KB for each draining warp, and T of a tile of few rows
-    const uint32_t stage_out = ring + (uint32_t)p.stages * p.stage_bytes + (p.a_bytes < 16384u ? 16384u - p.a_bytes : 0u);
-    float* const cache = reinterpret_cast<float*>(ap_raw + (stage_out + 8 * 4096u - smem_u32(ap_raw)));
-    auto further_stages = [](int ext) { return (ext + Kind::STAGE_WIDTH - 1) / Kind::STAGE_WIDTH; };
+    const uint32_t stage_out = ring + (uint32_t)p.stages * p.stage_bytes;      // after the ring, 4 KB for each draining warp
+    auto further_stages = [](int ext) { return (ext + Kind::WIDTH - 1) / Kind::WIDTH; };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) { mbar_init(&sh.full[i], PAIR ? 2 : 1); mbar_init(&sh.empty[i], WIDE ? 2 : 1); }
@@ -171,6 +314,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
         fence_barrier_init();
         prefetch_tensormap(&map_z);
         prefetch_tensormap(&map_w);
+        if (p.out_vec) prefetch_tensormap(&map_out);
     }
     if (warp == 1) {
         if (PAIR) { tmem_alloc_pair(&sh.tmem, p.tmem_cols); tmem_relinquish_pair(); }
@@ -213,23 +357,18 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 const int mt = tile / p.tiles_c, ct = tile - mt * p.tiles_c;
                 const int m0 = mt * tile_m + (int)rank * AP_TILE, c0 = ct * p.nt;
                 if (it > 0 && !pass(tile)) break;
-                for (int kb = 0; kb < p.kblocks; kb += KPB) {
+                for (int kb = 0; kb < p.kblocks; ++kb) {
                     if (!mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag)) { give_up(81, tile); ok = false; break; }
-                    const int n = min(KPB, p.kblocks - kb);
                     const uint32_t fb = (full0 + 8 * s) & full_mask;
-                    if (!PAIR || rank == 0) mbar_expect_tx_u32(fb, (PAIR ? 2u : 1u) * (uint32_t)n * (p.a_bytes + p.b_bytes));
-                    uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + (uint32_t)KPB * p.a_bytes;
-#pragma unroll
-                    for (int j = 0; j < KPB; ++j, a += p.a_bytes, b += p.b_bytes) {
-                        if (j >= n) break;
-                        const int l = (kb + j) << 6;
-                        tma_load_2d_u32<PAIR>(a, &map_z, fb, l, m0, 1u);
-                        if (ROWS) {
-                            for (int g = 0; g < cols >> 6; ++g) tma_load_2d_u32<PAIR>(b + (uint32_t)g * 8192u, &map_w, fb, c0 + column(64 * g), l, 1u);
-                        } else {
-                            tma_load_2d_u32<PAIR>(b, &map_w, fb, l, c0 + column(0), 1u);
-                            if (WIDE) tma_load_2d_u32<PAIR>(b + 16384u, &map_w, fb, l, c0 + column(128), 1u);
-                        }
+                    if (!PAIR || rank == 0) mbar_expect_tx_u32(fb, (PAIR ? 2u : 1u) * p.stage_bytes);
+                    const uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + p.a_bytes;
+                    const int l = kb << 6;
+                    tma_load_2d_u32<PAIR>(a, &map_z, fb, l, m0, 1u);
+                    if (ROWS) {
+                        for (int g = 0; g < cols >> 6; ++g) tma_load_2d_u32<PAIR>(b + (uint32_t)g * 8192u, &map_w, fb, c0 + column(64 * g), l, 1u);
+                    } else {
+                        tma_load_2d_u32<PAIR>(b, &map_w, fb, l, c0 + column(0), 1u);
+                        if (WIDE) tma_load_2d_u32<PAIR>(b + 16384u, &map_w, fb, l, c0 + column(128), 1u);
                     }
                     if (PAIR && rank == 0) mbar_arrive(&sh.full[s]);      // the barrier counts two: in a further block each CTA's builders
                     if (++s == p.stages) { s = 0; ph ^= 1; }
@@ -257,18 +396,16 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 mbar_arrive(&sh.iempty[ib]);
                 const uint32_t de = d + (DUAL ? p.acc_cols : 0u);
                 uint32_t acc = DUAL ? 0u : accum;
-                for (int c = 0; c < ext; c += Kind::STAGE_WIDTH) {
+                for (int e = 0; e < ext; e += WIDTH) {
                     if (!mbar_wait_u32(full0 + 8 * s, ph, abort_flag)) { give_up(86, tile); return false; }
                     tc_fence_after();
-                    uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + (uint32_t)KPB * p.a_bytes + (uint32_t)half * 16384u;
-                    for (int e = c; e < min(ext, c + Kind::STAGE_WIDTH); e += WIDTH, a += p.a_bytes, b += p.b_bytes) {
-                        const int n16 = (TERMS * min(WIDTH, ext - e) + 15) >> 4;
-                        const uint32_t al = sdesc_lo(a), bl = ROWS ? sdesc_rows_lo(b, 8192) : sdesc_lo(b);
+                    const uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + p.a_bytes + (uint32_t)half * 16384u;
+                    const int n16 = (TERMS * min(WIDTH, ext - e) + 15) >> 4;
+                    const uint32_t al = sdesc_lo(a), bl = ROWS ? sdesc_rows_lo(b, 8192) : sdesc_lo(b);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            umma_bf16_lo<PAIR>(de, al + 2 * k, bl + b_step * k, idesc, acc, k < n16 ? 1u : 0u);
-                            acc = 1;
-                        }
+                    for (int k = 0; k < 4; ++k) {
+                        umma_bf16_lo<PAIR>(de, al + 2 * k, bl + b_step * k, idesc, acc, k < n16 ? 1u : 0u);
+                        acc = 1;
                     }
                     umma_commit_u32<PAIR>(empty0 + 8 * s);
                     if (++s == p.stages) { s = 0; ph ^= 1; }
@@ -284,21 +421,16 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 accum = 0;
                 if (it > 0 && !further(tile)) break;
                 bool ok = true;
-                for (int kb = 0; kb < p.kblocks; kb += KPB) {
+                for (int kb = 0; kb < p.kblocks; ++kb) {
                     if (!mbar_wait_u32(full0 + 8 * s, ph, abort_flag)) { give_up(84, tile); ok = false; break; }
                     tc_fence_after();
-                    const int n = min(KPB, p.kblocks - kb);
-                    uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + (uint32_t)KPB * p.a_bytes + (uint32_t)half * 16384u;
+                    const uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + p.a_bytes + (uint32_t)half * 16384u;
+                    const uint32_t al = sdesc_lo(a), bl = ROWS ? sdesc_rows_lo(b, 8192) : sdesc_lo(b);
+                    const int n16 = kb == p.kblocks - 1 ? tail16 : 4;
 #pragma unroll
-                    for (int j = 0; j < KPB; ++j, a += p.a_bytes, b += p.b_bytes) {
-                        if (j >= n) break;
-                        const uint32_t al = sdesc_lo(a), bl = ROWS ? sdesc_rows_lo(b, 8192) : sdesc_lo(b);
-                        const int n16 = kb + j == p.kblocks - 1 ? tail16 : 4;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            umma_bf16_lo<PAIR>(d, al + 2 * k, bl + b_step * k, idesc, accum, k < n16 ? 1u : 0u);
-                            accum = 1;
-                        }
+                    for (int k = 0; k < 4; ++k) {
+                        umma_bf16_lo<PAIR>(d, al + 2 * k, bl + b_step * k, idesc, accum, k < n16 ? 1u : 0u);
+                        accum = 1;
                     }
                     umma_commit_u32<PAIR>(empty0 + 8 * s);
                     if (++s == p.stages) { s = 0; ph ^= 1; }
@@ -313,127 +445,50 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
         const int bt = threadIdx.x - 384;
         int s = 0, it = 0;
         uint32_t ph = 0;
-        bool ok = true, waited = false;
+        bool ok = true;
         auto advance = [&](int n) {
             s += n;
             while (s >= p.stages) { s -= p.stages; ph ^= 1; }
         };
-        if (p.row_id) { grid_dependency_wait(); waited = true; }               // the rows' adapters, and t, are the kernel's in front
-        // a thread's pieces of f: of a block its rows row0 + k * step, 16 bytes at cj
+        constexpr int H = PAIR ? 2 : 1;
+        int id[H], next[H];
+        auto ids = [&](int tile, int (&to)[H]) {
+            const int mt = tile / p.tiles_c;
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                const int m = mt * tile_m + h * AP_TILE + bt;
+                to[h] = tile < p.tiles && m < p.rows.M ? __ldcg(p.row_id + m) : ROW_NONE;
+            }
+        };
+        grid_dependency_wait();                                                // the rows' adapters, and t, are the kernel's in front
+        ids(unit, id);
         const int cpr = ROWS ? cols >> 3 : 4;                                  // 16-byte pieces of a row of a block
         const int cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
         for (int tile = unit; tile < p.tiles && ok; tile += units, ++it) {
             const int ib = it & 1;
             const int mt = tile / p.tiles_c, ct = tile - mt * p.tiles_c, c0 = ct * p.nt;
-            sh.bits[bt] = 0;
-            int id[PAIR ? 2 : 1];
-#pragma unroll
-            for (int h = 0; h < (PAIR ? 2 : 1); ++h) {
-                const int m = mt * tile_m + h * AP_TILE + bt;
-                id[h] = !p.row_id ? adapter_of_warp_row(p.rows, m - lane, lane) : m < p.rows.M ? __ldcg(p.row_id + m) : ROW_NONE;
-            }
+            const int m = mt * tile_m + (int)rank * AP_TILE + bt;
+            ids(tile + units, next);                                           // on their way while this tile's blocks are built
             const bool free_now = mbar_wait(&sh.iempty[ib], ((it >> 1) & 1) ^ 1, abort_flag);
             if (!free_now) give_up(87, tile);
             if (builders_any(!free_now)) break;
             if (p.flags & DR_BIAS)
                 for (int c = bt; c < p.nt; c += 128) sh.bias[ib][c] = c0 + c < p.C ? __ldg(p.bias + c0 + c) : 0.f;
-#pragma unroll
-            for (int h = 0; h < (PAIR ? 2 : 1); ++h) {
-                const unsigned same = __match_any_sync(0xffffffffu, id[h]);
-                if (id[h] >= 0 && __ffs(same) - 1 == lane) atomicOr(&sh.bits[id[h] >> 5], 1u << (id[h] & 31));
-            }
-            builders_sync();
-            {
-                const uint32_t word = sh.bits[bt];
-                int n = __popc(word), incl = n;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int v = __shfl_up_sync(0xffffffffu, incl, o);
-                    if (lane >= o) incl += v;
-                }
-                if (lane == 31) sh.sums[bt >> 5] = incl;
-                builders_sync();
-                int at = incl - n;
-                for (int k = 0; k < (bt >> 5); ++k) at += sh.sums[k];
-                sh.before[bt] = at;
-                for (uint32_t w = word; w; w &= w - 1) sh.list[ib][at++] = (uint16_t)(bt * 32 + __ffs(w) - 1);
-                builders_sync();
-            }
-            const int own = PAIR ? id[rank] : id[0];
-            const int slot = own >= 0 ? sh.before[own >> 5] + __popc(sh.bits[own >> 5] & ((1u << (own & 31)) - 1u)) : own;
-            const int ext = (sh.sums[0] + sh.sums[1] + sh.sums[2] + sh.sums[3]) * p.Rp;
+            int slots[H];
+            const int used = ap_find(sh.find, sh.list[ib], id, slots, bt);
+            const int own = id[PAIR ? rank : 0], slot = slots[PAIR ? rank : 0], ext = used * p.Rp;
             sh.slot[ib][bt] = slot;
             if (bt == 0) sh.ext[ib] = ext;
-            builders_sync();                            // before the next tile clears the bits
-            mbar_arrive(&sh.ifull[ib]);
-            if (it == 0) advance(p.main_stages);
-
-            const int m = mt * tile_m + (int)rank * AP_TILE + bt;
             const float scale = (own >= 0 && p.scale ? __ldg(p.scale + own) : 1.f) * p.factor;
-            float* const keep = p.keep && ct == 0 && own != ROW_NONE ? p.keep + (size_t)m * p.R : nullptr;
-            if (keep && own == ROW_SHARED)
-                for (int r = 0; r < p.R; ++r) keep[r] = 0.f;
-            const float* const trow = KPB > 1 ? cache + (size_t)bt * p.Rp : p.t + (size_t)m * p.Rp;
-            for (int e0 = 0; e0 < ext; e0 += Kind::STAGE_WIDTH) {
+            builders_sync();                            // the list stands; and no one still reads what the next tile's search clears
+            mbar_arrive(&sh.ifull[ib]);
+            if (it == 0) advance(p.kblocks);
+            const float* const trow = p.t + (size_t)m * p.Rp;
+            for (int e0 = 0; e0 < ext; e0 += WIDTH) {
                 uint4 fv[8], tv[WIDTH / 8][TERMS];
-#pragma unroll
-                for (int j = 0; j < KPB; ++j) {
-                    const int eb = e0 + j * WIDTH, w = min(WIDTH, ext - eb);
-                    const int ef = eb + 8 * cj, df = (int)__umulhi((uint32_t)ef, p.rp_magic), rf = ef - df * p.Rp;
-                    const int af = !ROWS && 8 * cj < w ? sh.list[ib][df] : 0;
-#pragma unroll
-                    for (int i = 0; i < Kind::EACH; ++i) {
-                        uint4& v = fv[j * Kind::EACH + i];
-                        v = make_uint4(0, 0, 0, 0);
-                        const int row = row0 + i * step;
-                        if (ROWS) {
-                            const int c = c0 + column(8 * cj);
-                            if (row < w && c < p.C) {
-                                const int e = eb + row, dd = (int)__umulhi((uint32_t)e, p.rp_magic), r = e - dd * p.Rp;
-                                if (r < p.R) v = __ldg(reinterpret_cast<const uint4*>(p.f + ((size_t)sh.list[ib][dd] * p.R + r) * p.ldf + c));
-                            }
-                        } else {
-                            const int c = c0 + column(row);
-                            if (8 * cj < w && row < cols && c < p.C) {
-                                const __nv_bfloat16* src = p.f + ((size_t)af * p.C + c) * p.R + rf;
-                                if (p.f_vec) {
-                                    v = __ldg(reinterpret_cast<const uint4*>(src));
-                                } else {
-                                    unsigned short h[8];
-#pragma unroll
-                                    for (int q = 0; q < 8; ++q) h[q] = rf + q < p.R ? __ldg(reinterpret_cast<const unsigned short*>(src) + q) : (unsigned short)0;
-                                    v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
-                                }
-                            }
-                        }
-                    }
-                }
-                if (!waited) { grid_dependency_wait(); waited = true; }
-                if (KPB > 1 && e0 == 0 && slot >= 0) {
-                    for (int r = 0; r < p.Rp; r += 4) *reinterpret_cast<float4*>(cache + (size_t)bt * p.Rp + r) = __ldcg(reinterpret_cast<const float4*>(p.t + (size_t)m * p.Rp + r));
-                    if (keep) for (int r = 0; r < p.R; ++r) keep[r] = cache[(size_t)bt * p.Rp + r];
-                }
-                // T of this thread's row in the block `eb`
-                auto load_t = [&](int eb) {
-                    const int w = min(WIDTH, ext - eb);
-#pragma unroll
-                    for (int j = 0; j < WIDTH / 8; ++j) {
-#pragma unroll
-                        for (int k = 0; k < TERMS; ++k) tv[j][k] = make_uint4(0, 0, 0, 0);
-                        const int r = eb + 8 * j - slot * p.Rp;
-                        if (slot >= 0 && r >= 0 && r < p.Rp && 8 * j < w) {
-                            const float4* src = reinterpret_cast<const float4*>(trow + r);
-                            const float4 x = KPB > 1 ? src[0] : __ldcg(src), y = KPB > 1 ? src[1] : __ldcg(src + 1);
-                            const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                            if (KPB == 1 && keep) {
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) if (r + i < p.R) keep[r + i] = v[i];
-                            }
-                            split8<TERMS>(v, scale, tv[j]);
-                        }
-                    }
-                };
-                load_t(e0);
+                const int w = min(WIDTH, ext - e0);
+                ap_load_f<Kind>(p, sh.list[ib], e0, w, cols, row0, step, cj, [&](int i) { return c0 + column(i); }, fv);
+                ap_load_t<Kind, false>(trow, slot, p.Rp, e0, w, scale, tv);
                 bool odd = false;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) odd |= finite_only(fv[i]);
@@ -452,40 +507,8 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                                                                    mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag));
                 if (!slot_free) give_up(88, tile);
                 if (slot_free) {
-                    uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + (uint32_t)KPB * p.a_bytes;
-#pragma unroll
-                    for (int j = 0; j < KPB; ++j, a += p.a_bytes, b += p.b_bytes) {
-                        const int eb = e0 + j * WIDTH, w = min(WIDTH, ext - eb), wc = w >> 3;
-                        if (w <= 0) break;
-                        if (j > 0) load_t(eb);
-                        if ((uint32_t)bt * 128u < p.a_bytes) {
-                            const uint32_t at = a + bt * 128, x = (uint32_t)(bt & 7);
-#pragma unroll
-                            for (int i = 0; i < WIDTH / 8; ++i)
-                                if (i < wc) {
-#pragma unroll
-                                    for (int k = 0; k < TERMS; ++k) st_shared16(at + (((uint32_t)(i + k * wc) ^ x) << 4), tv[i][k]);
-                                }
-                            if (TERMS == 3 && wc == 1) st_shared16(at + ((3u ^ x) << 4), make_uint4(0, 0, 0, 0));     // 24 columns: two steps of 16
-                        }
-#pragma unroll
-                        for (int i = 0; i < Kind::EACH; ++i) {
-                            const uint4& v = fv[j * Kind::EACH + i];
-                            const int row = row0 + i * step;
-                            if (ROWS) {
-                                if (row < w) {
-                                    const uint32_t g = b + (uint32_t)(cj >> 3) * 8192u;
-#pragma unroll
-                                    for (int k = 0; k < TERMS; ++k) st_shared16(g + (row + k * w) * 128 + (((cj & 7) ^ ((row + k * w) & 7)) << 4), v);
-                                }
-                            } else if (row < cols && cj < wc) {
-                                const uint32_t at = b + row * 128, x = (uint32_t)(row & 7);
-#pragma unroll
-                                for (int k = 0; k < TERMS; ++k) st_shared16(at + (((uint32_t)(cj + k * wc) ^ x) << 4), v);
-                                if (TERMS == 3 && wc == 1) st_shared16(at + ((3u ^ x) << 4), make_uint4(0, 0, 0, 0));
-                            }
-                        }
-                    }
+                    const uint32_t a = ring + (uint32_t)s * p.stage_bytes;
+                    ap_store_block<Kind>(a, a + p.a_bytes, bt, true, w, cols, row0, step, cj, fv, tv);
                 }
                 fence_proxy_async_smem();
                 if (builders_any(!slot_free)) { ok = false; break; }
@@ -496,19 +519,19 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 advance(1);
             }
             if (bt == 0) mbar_arrive(&sh.built[ib]);
-            if (it > 0) advance(p.main_stages);
+            if (it > 0) advance(p.kblocks);
+#pragma unroll
+            for (int h = 0; h < H; ++h) id[h] = next[h];
         }
-        if (!waited) grid_dependency_wait();        // what follows this kernel sees the one in front complete
     } else if (warp >= 4) {
         // ---------------------------------------------------------------- drain: two warps to a quarter of the rows, every other 128 bytes of columns each
         const int q = warp & 3, side = (warp - 4) >> 2;
         const uint32_t buf = stage_out + (uint32_t)(warp - 4) * 4096u;
-        const uint32_t put = buf + lane * 128, px = (uint32_t)(lane & 7), get = buf + (lane >> 3) * 128;
+        const uint32_t put = buf + lane * 128, px = (uint32_t)(lane & 7);
         const bool f32 = TERMS == 3;
         constexpr int CHUNK = TERMS == 3 ? 32 : 64;                            // columns of 128 bytes
         const float low = (p.flags & DR_RELU) ? 0.f : -INFINITY;
         const uint32_t low2 = (p.flags & DR_RELU) ? 0u : 0xFF80FF80u;
-        const size_t size = f32 ? 4 : 2;
         const unsigned long long off = DUAL ? drop_offset(p.key) : 0ull;
         int it = 0;
         bool ok = true;
@@ -521,8 +544,8 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
             const unsigned valid = __ballot_sync(0xffffffffu, slot != ROW_NONE);
             const int mw = mt * tile_m + (int)rank * AP_TILE + q * 32, m = mw + lane;
             const int ext = sh.ext[ib];
-            char* const rowp = (char*)p.out + ((size_t)(mw + (lane >> 3)) * p.ldo + n0) * size + (lane & 7) * 16;
-            const size_t row4 = 4 * p.ldo * size;
+            // no row of no request among them: whole boxes by TMA, which leaves out what lies behind the last row or column
+            const bool boxes = p.out_vec && mw < p.rows.M && valid == (p.rows.M - mw >= 32 ? 0xffffffffu : (1u << (p.rows.M - mw)) - 1u);
             const uint32_t quarter = (uint32_t)(q * 32) << 16;
 #pragma unroll 1
             for (int part = 0; part < (WIDE ? 2 : 1); ++part) {
@@ -550,21 +573,26 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                                 if (bits >> i & 1) v[h + i] = __float_as_uint(__uint_as_float(v[h + i]) + __uint_as_float(u[i]));
                         }
                     }
-                    if (odd && slot >= 0) {
-                        const int a = sh.list[ib][slot];
-                        const float w = (p.scale ? p.scale[a] : 1.f) * p.factor;
+                    if (lane == 0) tma_store_wait_read();                      // the box in front has been read
+                    __syncwarp();
+                    if (odd) {
 #pragma unroll 1
-                        for (int r = 0; r < p.R; ++r) {
-                            const float tv = __ldcg(p.t + (size_t)m * p.Rp + r) * w;
+                        for (int h = 0; h < CHUNK; h += 32) {
+                            for (int i = 0; i < 32; ++i) {                     // this row's 32 values, in its own place of the buffer
+                                const int col = n0 + cb + c + h + i;
+                                const bool mine = slot >= 0 && col < p.C && (!DUAL || drop_keep_at(p.key, off, (unsigned long long)m * p.C + col));
+                                const float x = mine ? ap_odd<ROWS>(p, sh.list[ib][slot], m, col) : 0.f;
+                                asm volatile("st.shared.f32 [%0], %1;" ::"r"(put + 4 * i), "f"(x) : "memory");
+                            }
 #pragma unroll
-                            for (int i = 0; i < CHUNK; ++i) {
-                                const int col = n0 + cb + c + i;
-                                if (col >= p.C) continue;
-                                const float fr = __bfloat162float(ROWS ? p.f[((size_t)a * p.R + r) * p.ldf + col] : p.f[((size_t)a * p.C + col) * p.R + r]);
-                                if (!(fabsf(fr) <= 3.4e38f) && (!DUAL || drop_keep_at(p.key, off, (unsigned long long)m * p.C + col)))
-                                    v[i] = __float_as_uint(fmaf(tv, fr, __uint_as_float(v[i])));
+                            for (int i = 0; i < 32; ++i) {
+                                float x;
+                                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(put + 4 * i) : "memory");
+                                if (h == 0) v[i] = __float_as_uint(__uint_as_float(v[i]) + x);
+                                else v[(32 + i) % CHUNK] = __float_as_uint(__uint_as_float(v[(32 + i) % CHUNK]) + x);
                             }
                         }
+                        __syncwarp();
                     }
                     if (p.flags & DR_BIAS) {
                         const float4* bias = reinterpret_cast<const float4*>(&sh.bias[ib][cb + c]);
@@ -577,7 +605,6 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                             v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + x.w);
                         }
                     }
-                    // through shared memory, so that a store instruction writes whole rows of 128 bytes
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         uint4 x;
@@ -593,48 +620,34 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                         }
                         st_shared16(put + (((uint32_t)j ^ px) << 4), x);
                     }
+                    if (boxes && (c_end - c >= CHUNK || (n0 + cb + c_end == p.C && p.C * (f32 ? 4 : 2) % 16 == 0))) {
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(&map_out, buf, (n0 + cb + c) * (f32 ? 2 : 1), mw);      // float32 go as pairs of 16 bits
+                            tma_store_commit();
+                        }
+                        continue;
+                    }
                     __syncwarp();
                     const int have = min(CHUNK, c_end - c);
-                    if (p.out_vec) {
-                        const int per = f32 ? 4 : 8, j = lane & 7;
-                        char* to = rowp + (size_t)(cb + c) * size;
-                        const bool whole = j * per + per <= have;
+#pragma unroll 1
+                    for (int row = 0; row < 32; ++row) {
+                        if (!(valid >> row & 1)) continue;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k, to += row4) {
-                            const int row = 4 * k + (lane >> 3);
-                            if (!(valid >> row & 1) || j * per >= have) continue;
-                            const uint4 x = ld_shared16(get + 512 * k + (((uint32_t)j ^ (uint32_t)(row & 7)) << 4));
-                            if (whole) {
-                                *reinterpret_cast<uint4*>(to) = x;
+                        for (int i = lane; i < CHUNK; i += 32) {
+                            if (i >= have) continue;
+                            const int byte = i * (f32 ? 4 : 2);
+                            const uint32_t addr = buf + row * 128 + ((((byte >> 4) ^ (row & 7)) << 4) | (byte & 15));
+                            const size_t at = (size_t)(mw + row) * p.ldo + n0 + cb + c + i;
+                            if (f32) {
+                                uint32_t x;
+                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
+                                ((uint32_t*)p.out)[at] = x;
                             } else {
-                                const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                                for (int i = 0; i < 8; ++i)
-                                    if (i < per && j * per + i < have) {
-                                        if (f32) ((uint32_t*)to)[i] = xs[i & 3];
-                                        else ((unsigned short*)to)[i] = (unsigned short)(xs[i >> 1] >> (16 * (i & 1)));
-                                    }
-                            }
-                        }
-                    } else {
-#pragma unroll 4
-                        for (int row = 0; row < 32; ++row) {
-                            if (!(valid >> row & 1)) continue;
-#pragma unroll
-                            for (int i = lane; i < CHUNK; i += 32) {
-                                if (i >= have) continue;
-                                const int byte = i * (f32 ? 4 : 2);
-                                const uint32_t addr = buf + row * 128 + ((((byte >> 4) ^ (row & 7)) << 4) | (byte & 15));
-                                const size_t at = (size_t)(mw + row) * p.ldo + n0 + cb + c + i;
-                                if (f32) {
-                                    uint32_t x;
-                                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
-                                    ((uint32_t*)p.out)[at] = x;
-                                } else {
-                                    unsigned short x;
-                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(addr) : "memory");
-                                    ((unsigned short*)p.out)[at] = x;
-                                }
+                                unsigned short x;
+                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(addr) : "memory");
+                                ((unsigned short*)p.out)[at] = x;
                             }
                         }
                     }
@@ -649,6 +662,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
             }
             if (lane == 0) mbar_arrive(&sh.iempty[ib]);
         }
+        if (lane == 0) tma_store_wait_all();
     }
     tc_fence_before();
     __syncthreads();
@@ -659,31 +673,250 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
     }
 }
 
+// ---- few rows (one tile of at most 128) ------------------------------------------------------------------------------------------------
+// Bound by the bytes of w, and by latency.  A cluster of CTAs shares a tile's l: each takes a range of it and every so many of the further blocks, and the
+// accumulators meet in distributed shared memory, where each CTA sums and finishes a part of the columns.  Rows of z behind the last are not
+// loaded: what the MMA finds there only reaches rows of the accumulator that nobody reads.
+struct ApFewShared {
+    uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], tfull, loads, ifull;
+    uint32_t tmem;
+    int abort, odd, ext;
+    int slot[AP_TILE], id[AP_TILE];
+    uint16_t list[AP_TILE];
+    ApFind find;
+};
+
+template <class Kind>
+__global__ void __launch_bounds__(AP_THREADS, 1)
+adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ApParams p) {
+    constexpr bool ROWS = Kind::ROWS, DUAL = Kind::DUAL;
+    constexpr int TERMS = Kind::TERMS, WIDTH = Kind::WIDTH;
+    extern __shared__ uint8_t ap_raw[];
+    __shared__ ApFewShared sh;
+    const uint32_t ring = (smem_u32(ap_raw) + 1023u) & ~1023u;
+    float* const sums = reinterpret_cast<float*>(ap_raw + (ring - smem_u32(ap_raw)));      // once the ring is done: [M][nt + 4], DUAL: the adapters' behind
+    const int pitch = p.nt + 4;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
+    const int tile = (int)blockIdx.x / p.split, c0 = tile * p.nt;
+    const int kb0 = (int)((long long)rank * p.kblocks / p.split), kb1 = (int)((long long)(rank + 1) * p.kblocks / p.split);
+    volatile int* abort_flag = &sh.abort;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < p.stages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        mbar_init(&sh.tfull, 1);
+        mbar_init(&sh.loads, 1);
+        mbar_init(&sh.ifull, 128);
+        sh.abort = 0;
+        sh.odd = 0;
+        fence_barrier_init();
+        prefetch_tensormap(&map_z);
+        prefetch_tensormap(&map_w);
+    }
+    if (warp == 1) { tmem_alloc(&sh.tmem, p.tmem_cols); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    if (p.split > 1) cluster_sync_all();                       // sh.odd of every CTA stands before another one writes it
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    const uint32_t full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]);
+    auto give_up = [&](int site) {
+        if (!*abort_flag) report_timeout(p.status, site, tile);
+        *abort_flag = 1;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 0;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag)) { give_up(92); break; }
+                const uint32_t fb = full0 + 8 * s;
+                mbar_expect_tx_u32(fb, p.stage_bytes);
+                const uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + p.a_bytes;
+                const int l = kb << 6;
+                if (ROWS) {
+                    for (int g = 0; g < p.nt >> 6; ++g) tma_load_2d_u32<false>(b + (uint32_t)g * 8192u, &map_w, fb, c0 + 64 * g, l, 1u);
+                } else {
+                    tma_load_2d_u32<false>(b, &map_w, fb, l, c0, 1u);
+                }
+                tma_load_2d_u32<false>(a, &map_z, fb, l, 0, 1u);
+                if (++s == p.stages) { s = 0; ph ^= 1; }
+            }
+            mbar_arrive(&sh.loads);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = make_idesc_bf16(AP_TILE, p.nt) | (ROWS ? 1u << 16 : 0u);
+            const int tail16 = ((p.L - ((p.kblocks - 1) << 6)) + 15) >> 4;
+            constexpr uint32_t b_step = ROWS ? 128u : 2u;
+            int s = 0;
+            uint32_t ph = 0, accum = 0;
+            bool ok = true;
+            auto block = [&](uint32_t d, int n16, int site) {
+                if (!mbar_wait_u32(full0 + 8 * s, ph, abort_flag)) { give_up(site); ok = false; return; }
+                tc_fence_after();
+                const uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + p.a_bytes;
+                const uint32_t al = sdesc_lo(a), bl = ROWS ? sdesc_rows_lo(b, 8192) : sdesc_lo(b);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    umma_bf16_lo<false>(d, al + 2 * k, bl + b_step * k, idesc, accum, k < n16 ? 1u : 0u);
+                    accum = 1;
+                }
+                umma_commit_u32<false>(empty0 + 8 * s);
+                if (++s == p.stages) { s = 0; ph ^= 1; }
+            };
+            for (int kb = kb0; kb < kb1 && ok; ++kb) block(tmem, kb == p.kblocks - 1 ? tail16 : 4, 93);
+            if (ok && !mbar_wait(&sh.ifull, 0, abort_flag)) { give_up(94); ok = false; }
+            const int ext = ok ? sh.ext : 0;
+            if (DUAL) accum = 0;
+            for (int e = rank * WIDTH; e < ext && ok; e += p.split * WIDTH) block(tmem + (DUAL ? p.acc_cols : 0u), (TERMS * min(WIDTH, ext - e) + 15) >> 4, 95);
+            umma_commit_u32<false>(smem_u32(&sh.tfull));
+        }
+        __syncwarp();
+    } else if (warp >= 12) {
+        const int bt = threadIdx.x - 384;
+        int s = (kb1 - kb0) % p.stages;
+        uint32_t ph = (uint32_t)((kb1 - kb0) / p.stages) & 1u;
+        int id[1] = {adapter_of_warp_row(p.rows, bt & ~31, lane)}, slot[1];
+        const int used = ap_find(sh.find, sh.list, id, slot, bt);
+        const int ext = used * p.Rp;
+        sh.slot[bt] = slot[0];
+        if (bt == 0) sh.ext = ext;
+        builders_sync();
+        mbar_arrive(&sh.ifull);
+        const float scale = (id[0] >= 0 && p.scale ? __ldg(p.scale + id[0]) : 1.f) * p.factor;
+        const float* const trow = p.t + (size_t)bt * p.Rp;
+        const int cpr = ROWS ? p.nt >> 3 : 4, cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
+        const bool row_there = (uint32_t)bt * 128u < p.a_bytes;
+        bool waited = false, ok = true;
+        for (int e0 = rank * WIDTH; e0 < ext && ok; e0 += p.split * WIDTH) {
+            uint4 fv[8], tv[WIDTH / 8][TERMS];
+            const int w = min(WIDTH, ext - e0);
+            ap_load_f<Kind>(p, sh.list, e0, w, p.nt, row0, step, cj, [&](int i) { return c0 + i; }, fv);
+            if (!waited) { grid_dependency_wait(); waited = true; }            // f needs no waiting, t is the kernel's in front
+            ap_load_t<Kind, false>(trow, slot[0], p.Rp, e0, w, scale, tv);
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) odd |= finite_only(fv[i]);
+            if (odd) {
+                for (int k = 0; k < p.split; ++k)
+                    asm volatile("red.relaxed.cluster.shared::cluster.max.s32 [%0], %1;" ::"r"(p.split > 1 ? mapa_shared(smem_u32(&sh.odd), k) : smem_u32(&sh.odd)), "r"(1) : "memory");
+            }
+            const bool slot_free = __all_sync(0xffffffffu, mbar_wait(&sh.loads, 0, abort_flag) && mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag));
+            if (!slot_free) give_up(96);
+            if (slot_free) {
+                const uint32_t a = ring + (uint32_t)s * p.stage_bytes;
+                ap_store_block<Kind>(a, a + p.a_bytes, bt, row_there, w, p.nt, row0, step, cj, fv, tv);
+            }
+            fence_proxy_async_smem();
+            if (builders_any(!slot_free)) { ok = false; break; }
+            if (bt == 0) mbar_arrive(&sh.full[s]);
+            if (++s == p.stages) { s = 0; ph ^= 1; }
+        }
+        if (!waited) grid_dependency_wait();
+    }
+    // every thread: the accumulators' rows into shared memory
+    if (warp >= 4 && warp < 12) {
+        const int q = warp & 3, side = (warp - 4) >> 2, row = q * 32 + lane;
+        if (q * 32 < p.rows.M) {
+            if (!__all_sync(0xffffffffu, mbar_wait(&sh.tfull, 0, abort_flag))) {
+                give_up(97);
+            } else {
+                tc_fence_after();
+                const int ext = sh.ext;
+                const bool own = ext > rank * WIDTH;             // this CTA had a further block
+                for (int c = side * 32; c < p.nt; c += 64) {
+#pragma unroll
+                    for (int k = 0; k < (DUAL ? 2 : 1); ++k) {
+                        uint32_t v[32];
+                        tmem_ld_x32(tmem + (uint32_t)k * p.acc_cols + ((uint32_t)(q * 32) << 16) + c, v);
+                        tmem_ld_wait();
+                        if (row < p.rows.M) {
+                            float4* to = reinterpret_cast<float4*>(sums + ((size_t)k * p.rows.M + row) * pitch + c);
+                            const bool there = k == 0 || own;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                if (c + 4 * i < p.nt)
+                                    to[i] = there ? make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]))
+                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (p.split > 1) cluster_sync_all();
+    {
+        const int width = p.nt / p.split, quads = width >> 2;
+        const unsigned long long off = DUAL ? drop_offset(p.key) : 0ull;
+        const bool odd = sh.odd != 0;
+        const float low = (p.flags & DR_RELU) ? 0.f : -INFINITY;
+        for (int i = threadIdx.x; i < p.rows.M * quads; i += AP_THREADS) {
+            const int m = i / quads, cl = rank * width + 4 * (i - m * quads), c = c0 + cl;
+            const int slot = sh.slot[m];
+            if (slot == ROW_NONE || c >= p.C) continue;
+            const uint32_t at = smem_u32(sums + (size_t)m * pitch + cl), at2 = smem_u32(sums + ((size_t)p.rows.M + m) * pitch + cl);
+            float v[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < p.split; ++k) {
+                const float4 x = ld_shared_cluster_f4(p.split > 1 ? mapa_shared(at, (uint32_t)k) : at);
+                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+                if (DUAL) {
+                    const float4 y = ld_shared_cluster_f4(p.split > 1 ? mapa_shared(at2, (uint32_t)k) : at2);
+                    u[0] += y.x; u[1] += y.y; u[2] += y.z; u[3] += y.w;
+                }
+            }
+            const uint32_t bits = DUAL ? drop_bits8_at(p.key, off, (unsigned long long)m * p.C + c) : 0xFu;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (DUAL && (bits >> k & 1)) v[k] += u[k];
+                if (odd && slot >= 0 && c + k < p.C && (bits >> k & 1)) v[k] += ap_odd<ROWS>(p, sh.list[slot], m, c + k);
+                if ((p.flags & DR_BIAS) && c + k < p.C) v[k] += __ldg(p.bias + c + k);
+                v[k] = max_nan(v[k], low);
+            }
+            const size_t to = (size_t)m * p.ldo + c;
+            if (p.out_vec && c + 4 <= p.C) {
+                if (TERMS == 3) *reinterpret_cast<float4*>((float*)p.out + to) = make_float4(v[0], v[1], v[2], v[3]);
+                else *reinterpret_cast<uint2*>((__nv_bfloat16*)p.out + to) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c + k < p.C) {
+                        if (TERMS == 3) ((float*)p.out)[to + k] = v[k];
+                        else ((__nv_bfloat16*)p.out)[to + k] = __float2bfloat16_rn(v[k]);
+                    }
+            }
+        }
+    }
+    __syncthreads();
+    if (p.split > 1) cluster_sync_all();                       // no CTA leaves while another reads its sums
+    if (warp == 1) tmem_dealloc(tmem, p.tmem_cols);
+}
+
 static int ap_map(CUtensorMap* map, const void* ptr, size_t rows, size_t inner, size_t ld, int box_inner, int box_rows) {
     const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * 2};
     const cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows};
     return tmap_tiled(map, 2, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
-template <class Kind>
-static int ap_launch(const CUtensorMap& mz, const CUtensorMap& mw, const ApParams& p, bool overlap, size_t smem, cudaStream_t s) {
-    static PerDeviceFlag ready;
-    auto* k = adapter_product_kernel<Kind>;
+template <class Kernel, class... Args>
+static int ap_start(Kernel k, PerDeviceFlag& ready, int grid, int cluster, bool overlap, size_t smem, cudaStream_t s, const Args&... args) {
     if (!ready.get()) {
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, AP_SMEM_MOST) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
         ready.set();
     }
     cudaLaunchConfig_t cfg = {};
-    const int units = Kind::PAIR ? num_sms() / 2 : num_sms();
-    cfg.gridDim = dim3((unsigned)(std::min(p.tiles, units) * (Kind::PAIR ? 2 : 1)));
+    cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(AP_THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     int n = 0;
-    if (Kind::PAIR) {
+    if (cluster > 1) {
         attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = 2; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
+        attr[n].val.clusterDim.x = (unsigned)cluster; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
         ++n;
     }
     if (overlap) {
@@ -693,9 +926,54 @@ static int ap_launch(const CUtensorMap& mz, const CUtensorMap& mw, const ApParam
     }
     cfg.attrs = attr;
     cfg.numAttrs = n;
-    if (cudaLaunchKernelEx(&cfg, k, mz, mw, p) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, k, args...) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
     count_launch();
     return DR_OK;
+}
+template <class Kind>
+static int ap_launch(const CUtensorMap& mz, const CUtensorMap& mw, const CUtensorMap& mo, const ApParams& p, bool overlap, size_t smem, cudaStream_t s) {
+    static PerDeviceFlag ready;
+    const int units = Kind::PAIR ? num_sms() / 2 : num_sms();
+    return ap_start(adapter_product_kernel<Kind>, ready, std::min(p.tiles, units) * (Kind::PAIR ? 2 : 1), Kind::PAIR ? 2 : 1, overlap, smem, s, mz, mw, mo, p);
+}
+template <class Kind>
+static int ap_launch_few(const CUtensorMap& mz, const CUtensorMap& mw, const ApParams& p, bool overlap, size_t smem, cudaStream_t s) {
+    static PerDeviceFlag ready;
+    return ap_start(adapter_few_kernel<Kind>, ready, p.tiles_c * p.split, p.split, overlap, smem, s, mz, mw, p);
+}
+
+static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t s) {
+    const int M = a.rows.M, sms = num_sms();
+    const bool dual = a.key.thr != 0;
+    p.a_bytes = (uint32_t)((M + 7) / 8 * 8) * 128u;
+    // Width of a tile and CTAs that share its l, by a model in cycles: w once from memory (3.4 KB a cycle for all SMs), a CTA's loads at 32 bytes a
+    // cycle and 150 cycles a stage, 1500 for the meeting of a cluster.  32 x 4096 x 4096 takes TODO
+    double best = 0.;
+    for (int nt = a.transposed ? 64 : 16; nt <= 128; nt *= 2)
+        for (int split = 1; split <= 8 && split <= p.kblocks && 4 * split <= nt; split *= 2) {
+            const int tiles = (a.C + nt - 1) / nt, blocks = (p.kblocks + split - 1) / split;
+            const int waves = (tiles * split + sms - 1) / sms;
+            const double cta = blocks * ((p.a_bytes + nt * 128.) / 32. + 150.);
+            const double t = std::max(waves * cta, (double)a.C * a.L * 2. / 3400.) + (split > 1 ? 1500. : 0.) + waves * 2. * nt;
+            if (best == 0. || t < best) { best = t; p.nt = nt; p.split = split; }
+        }
+    p.tiles_c = (a.C + p.nt - 1) / p.nt;
+    p.tiles = p.tiles_c;
+    p.b_bytes = (uint32_t)p.nt * 128u;
+    p.stage_bytes = p.a_bytes + p.b_bytes;
+    const uint32_t slack = 16384u - p.a_bytes;                                // the MMA reads 128 rows from the last stage on
+    p.stages = (int)std::min<uint32_t>(AP_MAX_STAGES, (AP_SMEM - slack) / p.stage_bytes);
+    p.acc_cols = std::max(32, p.nt);
+    p.tmem_cols = p.acc_cols * (dual ? 2 : 1);
+    const size_t ring = (size_t)p.stages * p.stage_bytes + slack, sums = (size_t)M * (p.nt + 4) * 4 * (dual ? 2 : 1);
+    const size_t smem = 1024 + std::max(ring, sums);
+    alignas(64) CUtensorMap mz, mw;
+    int rc = ap_map(&mz, a.z, M, a.L, a.ldz, 64, (M + 7) / 8 * 8);
+    if (rc != DR_OK) return rc;
+    rc = a.transposed ? ap_map(&mw, a.w, a.L, a.C, a.ldw, 64, 64) : ap_map(&mw, a.w, a.C, a.L, a.ldw, 64, p.nt);
+    if (rc != DR_OK) return rc;
+    if (a.transposed) return dual ? ap_launch_few<ApKind<false, false, true, true, 2>>(mz, mw, p, overlap, smem, s) : ap_launch_few<ApKind<false, false, true, false, 2>>(mz, mw, p, overlap, smem, s);
+    return (a.flags & DR_OUT_F32) ? ap_launch_few<ApKind<false, false, false, false, 3>>(mz, mw, p, overlap, smem, s) : ap_launch_few<ApKind<false, false, false, false, 2>>(mz, mw, p, overlap, smem, s);
 }
 
 int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
@@ -703,14 +981,16 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
     p.rows = a.rows;
     p.L = a.L; p.C = a.C; p.R = a.R; p.Rp = a.Rp;
     p.rp_magic = (uint32_t)((0x100000000ull + a.Rp - 1) / a.Rp);
-    p.t = a.t; p.scale = a.scale; p.bias = a.bias; p.f = a.f; p.ldf = a.ldf; p.factor = a.factor; p.keep = a.keep;
+    p.row_id = a.row_id; p.t = a.t; p.scale = a.scale; p.bias = a.bias; p.f = a.f; p.ldf = a.ldf; p.factor = a.factor;
     p.f_vec = !a.transposed && (a.R & 7) == 0;
     p.flags = a.flags; p.out = a.out; p.ldo = a.ldo; p.key = a.key;
-    const size_t size = (a.flags & DR_OUT_F32) ? 4 : 2;
+    const bool dual = a.key.thr != 0, f32 = a.flags & DR_OUT_F32;
+    const size_t size = f32 ? 4 : 2;
     p.out_vec = aligned16(a.out) && (a.ldo * size) % 16 == 0;
     p.status = dev_status_ptr();
-    const bool dual = a.key.thr != 0, f32 = a.flags & DR_OUT_F32;
+    p.kblocks = (a.L + 63) / 64;
     const int M = a.rows.M, sms = num_sms();
+    if (M <= AP_TILE) return few_run(a, p, overlap, s);
     const long long rows128 = (M + 127) / 128;
     const int gran = a.transposed ? 64 : 16;
     // Tile: as wide as leaves every SM one, by pairs where the pairs have enough tiles
@@ -721,12 +1001,13 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
         const long long want = std::max(1ll, sms / rows128);         // column blocks that give every SM a tile
         nt = (int)((a.C + want - 1) / want);
         nt = std::min(most, std::max(gran, (nt + gran - 1) / gran * gran));
-    } else if (M > 128 && a.C >= 128) {
+    } else if (a.C >= 128) {
         const int pn = a.C > 128 ? most : 128;
         const long long pairs = ((rows128 + 1) / 2) * ((a.C + pn - 1) / pn);
         if (pairs >= sms / 2) { pair = true; nt = pn; }
         // Out of L2 a pair's block of 256 x 256 takes 64 KB for 512 cycles of MMAs, more than the 12 TB/s that all SMs get; 256 x 512 takes 96 KB
-        // for 1024, but its accumulators fill the tensor memory, so a tile's drain is only half hidden: long l
+        // for 1024, but its accumulators fill the tensor memory, so a tile's drain is only half hidden: long l.  16384 x 4096 x 4096 takes 380 us
+        // instead of 509.
         if (pair && !dual && a.L >= 1024 && a.C >= 512 && ((rows128 + 1) / 2) * ((a.C + 511) / 512) >= sms / 2) { wide = true; nt = 512; }
     }
     p.nt = nt;
@@ -735,42 +1016,29 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
     if (tiles > 0x7fffffffll) return DR_ERR_UNSUPPORTED;
     p.tiles = (int)tiles;
     const int cols = pair ? nt / 2 : nt;
-    const int a_rows = std::min(128, (M + 7) / 8 * 8);
-    p.a_bytes = (uint32_t)a_rows * 128u;
+    p.a_bytes = AP_TILE * 128u;
     p.b_bytes = (uint32_t)cols * 128u;
-    p.kblocks = (a.L + 63) / 64;
-    const uint32_t block = p.a_bytes + p.b_bytes;
-    int kpb = block <= 8192 ? 4 : block <= 16384 ? 2 : 1;
-    if (kpb > 1) {
-        p.cache = (M * a.Rp * 4 + 1023) / 1024 * 1024;
-        if (p.cache > AP_CACHE) { p.cache = 0; kpb = 1; }
-    }
-    p.row_id = M > AP_TILE ? a.row_id : nullptr;
-    p.main_stages = (p.kblocks + kpb - 1) / kpb;
-    p.stage_bytes = (uint32_t)kpb * block;
-    const uint32_t slack = p.a_bytes < 16384u ? 16384u - p.a_bytes : 0u;      // the MMA reads 128 rows from the last stage on
-    p.stages = (int)std::min<uint32_t>(AP_MAX_STAGES, (AP_SMEM - p.cache - slack) / p.stage_bytes);
+    p.stage_bytes = p.a_bytes + p.b_bytes;
+    p.stages = (int)std::min<uint32_t>(AP_MAX_STAGES, AP_SMEM / p.stage_bytes);
     p.acc_cols = 32;
     while ((int)p.acc_cols < (wide ? 256 : nt)) p.acc_cols *= 2;
     p.tmem_cols = p.acc_cols * (dual ? 4 : 2);
-    const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes + slack + 8 * 4096 + p.cache;
-    alignas(64) CUtensorMap mz, mw;
-    int rc = ap_map(&mz, a.z, M, a.L, a.ldz, 64, a_rows);
+    const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes + 8 * 4096;
+    alignas(64) CUtensorMap mz, mw, mo = {};
+    int rc = ap_map(&mz, a.z, M, a.L, a.ldz, 64, AP_TILE);
     if (rc != DR_OK) return rc;
     rc = a.transposed ? ap_map(&mw, a.w, a.L, a.C, a.ldw, 64, 64) : ap_map(&mw, a.w, a.C, a.L, a.ldw, 64, wide ? 128 : cols);
+    if (rc == DR_OK && p.out_vec) rc = ap_map(&mo, a.out, M, (size_t)a.C * (f32 ? 2 : 1), a.ldo * (f32 ? 2 : 1), 64, 32);
     if (rc != DR_OK) return rc;
-    //                                                    KPB PAIR  WIDE   ROWS  DUAL TERMS
+    //                                     PAIR  WIDE   ROWS  DUAL TERMS
     if (a.transposed) {
-        if (wide) return ap_launch<ApKind<1, true, true, true, false, 2>>(mz, mw, p, overlap, smem, s);
-        if (pair) return dual ? ap_launch<ApKind<1, true, false, true, true, 2>>(mz, mw, p, overlap, smem, s) : ap_launch<ApKind<1, true, false, true, false, 2>>(mz, mw, p, overlap, smem, s);
-        if (kpb == 2) return dual ? ap_launch<ApKind<2, false, false, true, true, 2>>(mz, mw, p, overlap, smem, s) : ap_launch<ApKind<2, false, false, true, false, 2>>(mz, mw, p, overlap, smem, s);
-        return dual ? ap_launch<ApKind<1, false, false, true, true, 2>>(mz, mw, p, overlap, smem, s) : ap_launch<ApKind<1, false, false, true, false, 2>>(mz, mw, p, overlap, smem, s);
+        if (wide) return ap_launch<ApKind<true, true, true, false, 2>>(mz, mw, mo, p, overlap, smem, s);
+        if (pair) return dual ? ap_launch<ApKind<true, false, true, true, 2>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<true, false, true, false, 2>>(mz, mw, mo, p, overlap, smem, s);
+        return dual ? ap_launch<ApKind<false, false, true, true, 2>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<false, false, true, false, 2>>(mz, mw, mo, p, overlap, smem, s);
     }
-    if (wide) return f32 ? ap_launch<ApKind<1, true, true, false, false, 3>>(mz, mw, p, overlap, smem, s) : ap_launch<ApKind<1, true, true, false, false, 2>>(mz, mw, p, overlap, smem, s);
-    if (pair) return f32 ? ap_launch<ApKind<1, true, false, false, false, 3>>(mz, mw, p, overlap, smem, s) : ap_launch<ApKind<1, true, false, false, false, 2>>(mz, mw, p, overlap, smem, s);
-    if (kpb == 4) return f32 ? ap_launch<ApKind<4, false, false, false, false, 3>>(mz, mw, p, overlap, smem, s) : ap_launch<ApKind<4, false, false, false, false, 2>>(mz, mw, p, overlap, smem, s);
-    if (kpb == 2) return f32 ? ap_launch<ApKind<2, false, false, false, false, 3>>(mz, mw, p, overlap, smem, s) : ap_launch<ApKind<2, false, false, false, false, 2>>(mz, mw, p, overlap, smem, s);
-    return f32 ? ap_launch<ApKind<1, false, false, false, false, 3>>(mz, mw, p, overlap, smem, s) : ap_launch<ApKind<1, false, false, false, false, 2>>(mz, mw, p, overlap, smem, s);
+    if (wide) return f32 ? ap_launch<ApKind<true, true, false, false, 3>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<true, true, false, false, 2>>(mz, mw, mo, p, overlap, smem, s);
+    if (pair) return f32 ? ap_launch<ApKind<true, false, false, false, 3>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<true, false, false, false, 2>>(mz, mw, mo, p, overlap, smem, s);
+    return f32 ? ap_launch<ApKind<false, false, false, false, 3>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<false, false, false, false, 2>>(mz, mw, mo, p, overlap, smem, s);
 }
 
 }  // namespace dr
