@@ -30,7 +30,7 @@ static int up8(int n) { return (n + 7) & ~7; }
 
 struct ForwardPlan {
     DownPlan down;
-    int Kp, Rp;
+    int Kp, Rp, terms;
     bool copy_x, copy_k;        // x; w and a
     size_t ids, t, x, w, a, bytes;
 };
@@ -43,7 +43,8 @@ static ForwardPlan forward_plan(const dr_adapter_desc* d, int M, int ldx, int se
     f.copy_x = f.copy_k || (ldx & 7);
     Places at;
     f.ids = at.take((size_t)M * 4);
-    f.t = at.take((size_t)M * f.Rp * 4);
+    f.terms = (d->flags & DR_OUT_F32) ? 3 : 2;
+    f.t = at.take((size_t)M * f.terms * f.Rp * 2);
     f.x = at.take(f.copy_x ? (size_t)M * f.Kp * 2 : 0);
     f.w = at.take(f.copy_k ? (size_t)d->Cout * f.Kp * 2 : 0);
     f.a = at.take(f.copy_k ? (size_t)d->adapters * d->rank * f.Kp * 2 : 0);
@@ -71,7 +72,7 @@ static BackwardPlan backward_plan(const dr_adapter_desc* d, int M, int ldx, int 
     f.copy_dy = (d->Cout & 7) || (lddy & 7);
     Places at;
     f.ids = at.take((size_t)M * 4);
-    f.u = at.take((size_t)M * f.Rp * 4);
+    f.u = at.take((size_t)M * 3 * f.Rp * 2);
     f.x = at.take(f.copy_x ? (size_t)M * f.Kp * 2 : 0);
     f.w = at.take(f.copy_k ? (size_t)d->Cout * f.Kp * 2 : 0);
     f.a = at.take(f.copy_k ? (size_t)d->adapters * d->rank * f.Kp * 2 : 0);
@@ -136,11 +137,11 @@ extern "C" int dr_adapter(const dr_adapter_desc* d, int M, const void* x, int ld
     if ((rc = place(f.copy_x, M, K, f.Kp, x, ldx, ws, f.x, &xp, &ldxp, s)) != DR_OK) return rc;
     if ((rc = place(f.copy_k, N, K, f.Kp, w, K, ws, f.w, &wp, &ldwp, s)) != DR_OK) return rc;
     if ((rc = place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, ws, f.a, &ap, &ldap, s)) != DR_OK) return rc;
-    float* const tw = (float*)(ws + f.t);
+    __nv_bfloat16* const tw = (__nv_bfloat16*)(ws + f.t);
     int* const ids = (int*)(ws + f.ids);
-    rc = adapter_down_run(f.down, rows, K, R, f.Rp, xp, ldxp, ap, ldap, key, key.thr ? key.scale : 1.f, tw, t, ids, s);
+    rc = adapter_down_run(f.down, rows, K, R, f.Rp, xp, ldxp, ap, ldap, key, key.thr ? key.scale : 1.f, scale, 1.f, f.terms, tw, t, ids, s);
     if (rc != DR_OK) return rc;
-    const ProductArgs g = {rows, K, N, R, f.Rp, xp, wp, (const __nv_bfloat16*)b, ldxp, ldwp, 0, ids, tw, scale, bias, 1.f, d->flags, y, (size_t)ldy, false, none};
+    const ProductArgs g = {rows, K, N, R, f.Rp, xp, wp, (const __nv_bfloat16*)b, ldxp, ldwp, 0, ids, tw, f.terms, bias, d->flags, y, (size_t)ldy, false, none};
     return adapter_product_run(g, true, s);
 }
 
@@ -175,7 +176,7 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     if (da && (rc = place(f.copy_x, M, K, f.Kp, x, ldx, ws, f.x, &xp, &ldxp, s)) != DR_OK) return rc;
     if (dx && (rc = place(f.copy_k, N, K, f.Kp, w, K, ws, f.w, &wp, &ldwp, s)) != DR_OK) return rc;
     if (dx && (rc = place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, ws, f.a, &ap, &ldap, s)) != DR_OK) return rc;
-    float* const u = (float*)(ws + f.u);
+    __nv_bfloat16* const u = (__nv_bfloat16*)(ws + f.u);
     int* const ids = (int*)(ws + f.ids);
     if (da || db) {
         rc = adapter_sort_run(rows, (int*)(ws + f.g + f.grad.perm), (int*)(ws + f.g + f.grad.start), s);
@@ -184,14 +185,14 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     if (dx || da) {
         __nv_bfloat16* const bt = (__nv_bfloat16*)(ws + f.bt);
         if ((rc = adapter_transpose_run(d->adapters, N, R, (const __nv_bfloat16*)b, bt, f.Np, s)) != DR_OK) return rc;
-        if ((rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, u, nullptr, ids, s)) != DR_OK) return rc;
+        if ((rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, scale, kept, 3, u, nullptr, ids, s)) != DR_OK) return rc;
     }
     if (dx) {
-        const ProductArgs g = {rows, N, K, R, f.Rp, dyp, wp, ap, lddyp, ldwp, ldap, ids, u, scale, nullptr, kept, 0, dx, (size_t)lddx, true, key};
+        const ProductArgs g = {rows, N, K, R, f.Rp, dyp, wp, ap, lddyp, ldwp, ldap, ids, u, 3, nullptr, 0, dx, (size_t)lddx, true, key};
         if ((rc = adapter_product_run(g, true, s)) != DR_OK) return rc;
     }
     if (da || db) {
-        const GradJob jobs[2] = {{K, xp, ldxp, u, f.Rp, scale, kept, key, da, 0}, {N, dyp, lddyp, t, R, scale, 1.f, none, db, 1}};
+        const GradJob jobs[2] = {{K, xp, ldxp, nullptr, f.Rp, nullptr, u, key, da, 0}, {N, dyp, lddyp, t, R, scale, nullptr, none, db, 1}};
         if ((rc = adapter_grad_run(f.grad, rows, R, jobs, ws + f.g, s)) != DR_OK) return rc;
     }
     return DR_OK;

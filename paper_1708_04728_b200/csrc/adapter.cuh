@@ -62,10 +62,11 @@ __device__ __forceinline__ uint32_t drop_bits8(const DropKey& k, unsigned long l
     return b;
 }
 __device__ __forceinline__ uint32_t drop_bits8_at(const DropKey& k, unsigned long long off, unsigned long long e) {
-    uint32_t b = drop_bits8(k, off, e >> 3);
     const int sh = (int)(e & 7);
-    if (sh) b = (b | drop_bits8(k, off, (e >> 3) + 1) << 8) >> sh;
-    return b & 0xFFu;
+    uint32_t b = 0;
+#pragma unroll 1                                                 // one copy of the generator: the code has to stay in the instruction cache
+    for (int i = 0; i < (sh ? 2 : 1); ++i) b |= drop_bits8(k, off, (e >> 3) + i) << (8 * i);
+    return (b >> sh) & 0xFFu;
 }
 // 8 bfloat16 values, those whose bit is clear set to zero
 __device__ __forceinline__ uint4 drop_apply8(uint4 v, uint32_t bits) {
@@ -88,14 +89,15 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t&
 }
 
 // ---- launches (adapter_down.cu, adapter_product.cu, adapter_grad.cu) -------------------------------------------------------
-// out[m][r] = factor * sum_l D(z)[m][l] f_a[r][l] in rows of Rp, the same in rows of R in keep (may be nullptr; zeros where a row has no adapter, nothing
-// where it has no request), and each row's adapter; f [adapters * R][ldf], 16-byte aligned rows, zeros behind L
+// t[m][r] = factor * sum_l D(z)[m][l] f_a[r][l], f [adapters * R][ldf] with 16-byte aligned rows and zeros behind L.  Written: in keep t itself, in rows
+// of R (may be nullptr; zeros where a row has no adapter, nothing where it has no request); in out the bfloat16 terms of T = scale_a after t, [M][terms][Rp];
+// in row_id each row's adapter
 struct DownPlan { int mt, warps_k, rows_cta, ks, zsplit, rt, rchunks; };
 DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments);
 int adapter_down_run(const DownPlan& plan, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
-                     const DropKey& key, float factor, float* out, float* keep, int* row_id, cudaStream_t s);
+                     const DropKey& key, float factor, const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, cudaStream_t s);
 
-// out[m][c] = act(sum_l z[m][l] w + bias[c] + D(scale_a factor t[m] f_a)):   forward w [C][ldw] (rows of l), f [adapters][C][R];
+// out[m][c] = act(sum_l z[m][l] w + bias[c] + D(T[m] f_a)):   forward w [C][ldw] (rows of l), f [adapters][C][R];
 // transposed w [L][ldw] (rows of c), f [adapters][R][ldf]
 struct ProductArgs {
     AdRows rows;
@@ -103,8 +105,9 @@ struct ProductArgs {
     const __nv_bfloat16 *z, *w, *f;
     size_t ldz, ldw, ldf;
     const int* row_id;
-    const float *t, *scale, *bias;
-    float factor;
+    const __nv_bfloat16* t;     // [M][terms][Rp]; of the terms the result's type calls for are taken
+    int terms;
+    const float* bias;
     unsigned flags;
     void* out;
     size_t ldo;
@@ -118,10 +121,10 @@ struct GradJob {
     int C;
     const __nv_bfloat16* z;
     size_t ldz;
-    const float* p;             // [M][ldp]
+    const float* p;             // P as float32 [M][ldp], times scale_a (nullptr: 1), or
     int ldp;
-    const float* scale;         // scale_a on P, or nullptr
-    float factor;
+    const float* scale;
+    const __nv_bfloat16* terms; // as three bfloat16 values, [M][3][ldp]
     DropKey key;
     float* out;                 // [adapters][R][C], or [adapters][C][R] where swap
     int swap;

@@ -20,8 +20,11 @@ struct DownParams {
     const __nv_bfloat16 *z, *f;
     size_t ldz, ldf;
     DropKey key;
-    float factor;
-    float *out, *keep;
+    float factor, after;
+    const float* scale;
+    int terms;
+    __nv_bfloat16* out;
+    float* keep;
     int* row_id;
 };
 
@@ -34,8 +37,8 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 // MT tiles of 16 rows, RT tiles of 8 columns a warp; JOIN: the 8 warps of a CTA split l over the same rows, else each has rows of its own
 template <int MT, int RT, bool DROP, bool JOIN>
 __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
-    __shared__ float join[JOIN ? 8 : 1][JOIN ? 16 : 1][JOIN ? RT * 8 + 1 : 1];
-    __shared__ float range[JOIN ? 16 * RT * 8 : 1];              // this range's sums, read by the cluster
+    __shared__ float join[JOIN ? 8 : 1][JOIN ? 16 : 1][JOIN ? RT * 8 + 2 : 1];
+    __shared__ alignas(8) float range[JOIN ? 16 * RT * 8 : 1];              // this range's sums, read by the cluster
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int m0 = ((int)blockIdx.x * (JOIN ? 1 : 8) + (JOIN ? 0 : warp)) * MT * 16;
@@ -46,7 +49,6 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
     if (lane >= MT * 16) id = ROW_NONE;
     else if (p.row_id && blockIdx.y == 0 && blockIdx.z == 0 && (!JOIN || warp == 0) && m0 + lane < p.rows.M) p.row_id[m0 + lane] = id;
     const unsigned long long off = DROP ? drop_offset(p.key) : 0ull;
-    const bool whole = (p.L & 7) == 0;
 
     const __nv_bfloat16* zr[MT][2];
 #pragma unroll
@@ -54,9 +56,19 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) zr[t][h] = p.z + (size_t)min(m0 + 16 * t + 8 * h + g, p.rows.M - 1) * p.ldz;
 
-    auto put = [&](int row, int r, float v) {                    // row of this warp's, column of all
-        p.out[(size_t)(m0 + row) * p.Rp + r] = v;
-        if (p.keep && r < p.R) p.keep[(size_t)(m0 + row) * p.R + r] = v;
+    // t of a row of this warp's at two neighbouring columns (the first even)
+    auto put = [&](int row, int r, float x, float y, float scale) {
+        if (p.keep) {
+            float* to = p.keep + (size_t)(m0 + row) * p.R + r;
+            if (r < p.R) to[0] = x;
+            if (r + 1 < p.R) to[1] = y;
+        }
+        uint32_t u[3];
+        split3(x * scale, y * scale, u[0], u[1], u[2]);
+        uint32_t* to = reinterpret_cast<uint32_t*>(p.out + (size_t)(m0 + row) * p.terms * p.Rp + r);
+        to[0] = u[0];
+        to[p.Rp >> 1] = u[1];
+        if (p.terms == 3) to[p.Rp] = u[2];
     };
     if (p.keep && id == ROW_SHARED && blockIdx.y == 0 && zi == 0 && (!JOIN || warp == 0))
         for (int r = r0; r < min(p.R, r0 + RT * 8); ++r) p.keep[(size_t)(m0 + lane) * p.R + r] = 0.f;
@@ -66,6 +78,7 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
         const unsigned mine = __ballot_sync(0xffffffffu, id == a);
         rest &= ~mine;
         if (number++ % p.zsplit != zi) continue;
+        const float scale = (p.scale ? __ldg(p.scale + a) : 1.f) * p.after;
         float acc[MT][RT][4] = {};
         const __nv_bfloat16* f = p.f + ((size_t)a * p.R + r0 + g) * p.ldf;
 #pragma unroll 1
@@ -98,7 +111,7 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
                             const unsigned long long e = (unsigned long long)(m0 + 16 * t + 8 * h + g) * p.L + lq + 8 * k;
-                            const uint32_t bits = whole ? drop_bits8(p.key, off, e >> 3) : drop_bits8_at(p.key, off, e);
+                            const uint32_t bits = drop_bits8_at(p.key, off, e);
                             const uint4 v = drop_apply8(make_uint4(zw[t][h][4 * k], zw[t][h][4 * k + 1], zw[t][h][4 * k + 2], zw[t][h][4 * k + 3]), bits);
                             zw[t][h][4 * k] = v.x; zw[t][h][4 * k + 1] = v.y; zw[t][h][4 * k + 2] = v.z; zw[t][h][4 * k + 3] = v.w;
                         }
@@ -119,25 +132,28 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) join[warp][8 * (i >> 1) + g][8 * r + 2 * q + (i & 1)] = acc[t][r][i];
                 __syncthreads();
-                for (int i = threadIdx.x; i < 16 * RT * 8; i += 256) {
-                    const int row = i / (RT * 8), r = i - row * (RT * 8);
-                    float s = join[0][row][r];
+                const int row = threadIdx.x >> 4, col = 2 * (threadIdx.x & 15);        // 16 threads to a row, two columns each
+                const bool keeps = mine >> (16 * t + row) & 1;
+#pragma unroll 1
+                for (int r = col; r < RT * 8; r += 32) {
+                    float x = 0.f, y = 0.f;
 #pragma unroll
-                    for (int w = 1; w < 8; ++w) s += join[w][row][r];
-                    if (p.ks > 1) range[i] = s;
-                    else if ((mine >> (16 * t + row) & 1) && r0 + r < p.Rp) put(16 * t + row, r0 + r, s * p.factor);
+                    for (int w = 0; w < 8; ++w) { x += join[w][row][r]; y += join[w][row][r + 1]; }
+                    if (p.ks > 1) { range[row * RT * 8 + r] = x; range[row * RT * 8 + r + 1] = y; }
+                    else if (keeps && r0 + r < p.Rp) put(16 * t + row, r0 + r, x * p.factor, y * p.factor, scale);
                 }
                 if (p.ks > 1) {
                     ptx::cluster_sync_all();
-                    for (int i = 256 * ks + threadIdx.x; i < 16 * RT * 8; i += 256 * p.ks) {
-                        const int row = i / (RT * 8), r = i - row * (RT * 8);
-                        float s = 0.f;
+#pragma unroll 1
+                    for (int r = col; r < RT * 8; r += 32) {
+                        if (row % p.ks != ks) continue;          // the cluster's CTAs share the rows
+                        float x = 0.f, y = 0.f;
                         for (int k = 0; k < p.ks; ++k) {
-                            float v;
-                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ptx::mapa_shared(ptx::smem_u32(range + i), (uint32_t)k)) : "memory");
-                            s += v;
+                            float u, v;
+                            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(u), "=f"(v) : "r"(ptx::mapa_shared(ptx::smem_u32(range + row * RT * 8 + r), (uint32_t)k)) : "memory");
+                            x += u; y += v;
                         }
-                        if ((mine >> (16 * t + row) & 1) && r0 + r < p.Rp) put(16 * t + row, r0 + r, s * p.factor);
+                        if (keeps && r0 + r < p.Rp) put(16 * t + row, r0 + r, x * p.factor, y * p.factor, scale);
                     }
                     ptx::cluster_sync_all();                     // the sums are read: they may be overwritten, the CTA may leave
                 } else {
@@ -152,15 +168,7 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int row = 16 * t + 8 * h + g, c = r0 + 8 * r + 2 * q;
-                        if ((mine >> row & 1) && c < p.Rp) {
-                            const float2 v = make_float2(acc[t][r][2 * h] * p.factor, acc[t][r][2 * h + 1] * p.factor);
-                            *reinterpret_cast<float2*>(p.out + (size_t)(m0 + row) * p.Rp + c) = v;
-                            if (p.keep) {
-                                float* to = p.keep + (size_t)(m0 + row) * p.R + c;
-                                if (c < p.R) to[0] = v.x;
-                                if (c + 1 < p.R) to[1] = v.y;
-                            }
-                        }
+                        if ((mine >> row & 1) && c < p.Rp) put(row, c, acc[t][r][2 * h] * p.factor, acc[t][r][2 * h + 1] * p.factor, scale);
                     }
         }
     }
@@ -210,13 +218,13 @@ static int down_launch_rt(const DownPlan& d, const DownParams& p, cudaStream_t s
 }
 
 int adapter_down_run(const DownPlan& d, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
-                     const DropKey& key, float factor, float* out, float* keep, int* row_id, cudaStream_t s) {
+                     const DropKey& key, float factor, const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, cudaStream_t s) {
     DownParams p;
     p.rows = rows;
     p.L = L; p.L8 = (L + 7) / 8 * 8; p.R = R; p.Rp = Rp; p.ks = d.ks; p.zsplit = d.zsplit;
     p.l_range = (((L + d.ks - 1) / d.ks) + 63) / 64 * 64;
     p.z = z; p.f = f; p.ldz = ldz; p.ldf = ldf;
-    p.key = key; p.factor = factor; p.out = out; p.keep = keep; p.row_id = row_id;
+    p.key = key; p.factor = factor; p.scale = scale; p.after = after; p.terms = terms; p.out = out; p.keep = keep; p.row_id = row_id;
     if (d.rt == 1) return down_launch_rt<1>(d, p, s);
     if (d.rt == 2) return down_launch_rt<2>(d, p, s);
     return d.rt == 4 ? down_launch_rt<4>(d, p, s) : down_launch_rt<8>(d, p, s);

@@ -83,7 +83,7 @@ struct GradParams {
         const __nv_bfloat16* z;
         size_t ldz;
         const float *p, *scale;
-        float factor;
+        const __nv_bfloat16* terms;
         DropKey key;
         float *part, *out;
     } job[2];
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(256) adapter_grad_kernel(const GradParams p) {
         const int u = max(from, __ldg(p.start + a)), v = min(to, __ldg(p.start + a + 1));
         if (__ldg(p.start + a) >= to) break;
         if (u >= v) continue;
-        const float w = (j.scale ? __ldg(j.scale + a) : 1.f) * j.factor;
+        const float w = j.scale ? __ldg(j.scale + a) : 1.f;
         float acc[RT][8][4] = {};
         for (int i = u + 16 * warp; i < v; i += 128) {
             uint4 z[4];
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(256) adapter_grad_kernel(const GradParams p) {
                 z[k] = make_uint4(0, 0, 0, 0);
                 if (row[k] >= 0 && c < j.C) z[k] = __ldg(reinterpret_cast<const uint4*>(j.z + (size_t)row[k] * j.ldz + c));
             }
-            uint32_t ph[RT][4], pl[RT][4];
+            uint32_t ph[RT][4], pm[RT][4], pl[RT][4];
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 float x[2][4];
@@ -148,13 +148,20 @@ __global__ void __launch_bounds__(256) adapter_grad_kernel(const GradParams p) {
                         const int r = r0 + 16 * t + 8 * h + g;
                         float s = 0.f;
                         if (row[k] >= 0 && r < p.R)
-                            s = __ldg(j.p + (size_t)row[k] * j.ldp + r);
-                        x[h][k] = s * w;
+{
+                            if (j.terms) {
+                                const __nv_bfloat16* u = j.terms + (size_t)row[k] * 3 * j.ldp + r;
+                                s = (__bfloat162float(u[0]) + __bfloat162float(u[j.ldp])) + __bfloat162float(u[2 * j.ldp]);
+                            } else {
+                                s = __ldg(j.p + (size_t)row[k] * j.ldp + r) * w;
+                            }
+                        }
+                        x[h][k] = s;
                     }
-                split2(x[0][0], x[0][1], ph[t][0], pl[t][0]);
-                split2(x[1][0], x[1][1], ph[t][1], pl[t][1]);
-                split2(x[0][2], x[0][3], ph[t][2], pl[t][2]);
-                split2(x[1][2], x[1][3], ph[t][3], pl[t][3]);
+                split3(x[0][0], x[0][1], ph[t][0], pm[t][0], pl[t][0]);
+                split3(x[1][0], x[1][1], ph[t][1], pm[t][1], pl[t][1]);
+                split3(x[0][2], x[0][3], ph[t][2], pm[t][2], pl[t][2]);
+                split3(x[1][2], x[1][3], ph[t][3], pm[t][3], pl[t][3]);
             }
             if (j.key.thr) {
 #pragma unroll
@@ -171,6 +178,7 @@ __global__ void __launch_bounds__(256) adapter_grad_kernel(const GradParams p) {
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
                     mma_bf16_g(acc[t][n], ph[t], b0, b1);
+                    mma_bf16_g(acc[t][n], pm[t], b0, b1);
                     mma_bf16_g(acc[t][n], pl[t], b0, b1);
                 }
             }
@@ -255,7 +263,7 @@ int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const Grad
     int blocks[2], most = 0;
     for (int k = 0; k < 2; ++k) {
         const GradJob& g = jobs[k];
-        p.job[k] = {g.C, g.ldp, g.swap, g.z, g.ldz, g.p, g.scale, g.factor, g.key, (float*)(ws + plan.part[k]), g.out};
+        p.job[k] = {g.C, g.ldp, g.swap, g.z, g.ldz, g.p, g.scale, g.terms, g.key, (float*)(ws + plan.part[k]), g.out};
         blocks[k] = g.out ? (g.C + 63) / 64 : 0;
         if (g.out) most = std::max(most, g.C);
     }

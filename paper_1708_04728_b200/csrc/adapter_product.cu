@@ -41,11 +41,12 @@ struct ApParams {
     uint32_t acc_cols, tmem_cols;
     int split;                  // few rows: CTAs of a cluster that share a tile's l
     const int* row_id;
-    const float *t, *scale, *bias;
+    const __nv_bfloat16* t;     // [M][terms][Rp]
+    int t_terms;
+    const float* bias;
     const __nv_bfloat16* f;
     size_t ldf;
     int f_vec;
-    float factor;
     unsigned flags;
     void* out;
     size_t ldo;
@@ -90,29 +91,19 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
-// entries that are not finite become zero; true if there was one
-__device__ __forceinline__ bool finite_only(uint4& v) {
-    bool any = false;
-    uint32_t* u = reinterpret_cast<uint32_t*>(&v);
+// bits 15 and 31 of the result are set where a half of u has an exponent of all ones
+__device__ __forceinline__ uint32_t odd_halves(uint32_t u) { return (u & 0x7FFF7FFFu) + 0x00800080u; }
+template <int N>
+__device__ __forceinline__ bool any_odd(const uint4 (&v)[N]) {
+    uint32_t o = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t l = (u[i] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u, h = (u[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
-        any |= (l | h) != 0;
-        u[i] &= ~(l | h);
-    }
-    return any;
+    for (int i = 0; i < N; ++i) o |= odd_halves(v[i].x) | odd_halves(v[i].y) | odd_halves(v[i].z) | odd_halves(v[i].w);
+    return (o & 0x80008000u) != 0;
 }
-// eight T as bfloat16 values
-template <int TERMS>
-__device__ __forceinline__ void split8(const float* v, float c, uint4* o) {
-    uint32_t u[3][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (TERMS == 2) split2(v[2 * i] * c, v[2 * i + 1] * c, u[0][i], u[1][i]);
-        else split3(v[2 * i] * c, v[2 * i + 1] * c, u[0][i], u[1][i], u[2][i]);
-    }
-#pragma unroll
-    for (int k = 0; k < TERMS; ++k) o[k] = make_uint4(u[k][0], u[k][1], u[k][2], u[k][3]);
+// entries that are not finite become zero
+__device__ __forceinline__ uint32_t finite_halves(uint32_t u) {
+    const uint32_t o = odd_halves(u) & 0x80008000u;
+    return u & ~((o >> 15) * 0xFFFFu);
 }
 
 // What one kernel is compiled for.  PAIR: tiles of 256 rows by two CTAs.  WIDE (pairs): two accumulators of 256
@@ -175,6 +166,17 @@ __device__ __forceinline__ int ap_find(ApFind& f, uint16_t* list, const int (&id
     return f.sums[0] + f.sums[1] + f.sums[2] + f.sums[3];
 }
 
+// eight values of a row whose rank leaves them no alignment, zeros behind the last
+__device__ __noinline__ uint4 ap_odd_rank(const __nv_bfloat16* src, int n) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = 2 * i < n ? __ldg(reinterpret_cast<const unsigned short*>(src) + 2 * i) : 0u;
+        u[i] = lo | (2 * i + 1 < n ? (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(src) + 2 * i + 1) << 16 : 0u);
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
 // This thread's pieces of f in the block of `eb`: rows row0 + i * step of the block (ROWS: contraction rows, else columns of the output), 16 bytes at cj;
 // column(i): the output column that place i of the CTA's is.  Returns whether one was not finite (those are made zero).
 template <class Kind, class Column>
@@ -196,32 +198,20 @@ __device__ __forceinline__ void ap_load_f(const ApParams& p, const uint16_t* lis
             const int c = column(row);
             if (mine && row < cols && c < p.C) {
                 const __nv_bfloat16* src = fa + (size_t)c * p.R;
-                if (p.f_vec) {
-                    fv[i] = __ldg(reinterpret_cast<const uint4*>(src));
-                } else {
-                    unsigned short h[8];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) h[q] = rf + q < p.R ? __ldg(reinterpret_cast<const unsigned short*>(src) + q) : (unsigned short)0;
-                    fv[i] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
-                }
+                fv[i] = p.f_vec ? __ldg(reinterpret_cast<const uint4*>(src)) : ap_odd_rank(src, p.R - rf);
             }
         }
     }
 }
-// T of this thread's row in the block of `eb`: eight columns at a time, high and low values
-template <class Kind, bool SHARED>
-__device__ __forceinline__ void ap_load_t(const float* trow, int slot, int Rp, int eb, int w, float scale, uint4 (&tv)[Kind::WIDTH / 8][Kind::TERMS]) {
+// T of this thread's row in the block of `eb`, eight columns at a time
+template <class Kind>
+__device__ __forceinline__ void ap_load_t(const __nv_bfloat16* trow, int slot, int Rp, int eb, int w, uint4 (&tv)[Kind::WIDTH / 8][Kind::TERMS]) {
 #pragma unroll
     for (int j = 0; j < Kind::WIDTH / 8; ++j) {
-#pragma unroll
-        for (int k = 0; k < Kind::TERMS; ++k) tv[j][k] = make_uint4(0, 0, 0, 0);
         const int r = eb + 8 * j - slot * Rp;
-        if (slot >= 0 && (unsigned)r < (unsigned)Rp && 8 * j < w) {
-            const float4* src = reinterpret_cast<const float4*>(trow + r);
-            const float4 x = SHARED ? src[0] : __ldcg(src), y = SHARED ? src[1] : __ldcg(src + 1);
-            const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-            split8<Kind::TERMS>(v, scale, tv[j]);
-        }
+        const bool there = slot >= 0 && (unsigned)r < (unsigned)Rp && 8 * j < w;
+#pragma unroll
+        for (int k = 0; k < Kind::TERMS; ++k) tv[j][k] = there ? __ldcg(reinterpret_cast<const uint4*>(trow + k * Rp + r)) : make_uint4(0, 0, 0, 0);
     }
 }
 // both into the stage: z's part at a (rows of 128 bytes), w's at b
@@ -260,11 +250,12 @@ __device__ __forceinline__ void ap_store_block(uint32_t a, uint32_t b, int bt, b
 // what entries of f that are not finite add to out[m][c]: an infinity, NaN, or 0
 template <bool ROWS>
 __device__ __noinline__ float ap_odd(const ApParams& p, int a, int m, int c) {
-    const float w = (p.scale ? p.scale[a] : 1.f) * p.factor;
     float s = 0.f;
     for (int r = 0; r < p.R; ++r) {
         const float fr = __bfloat162float(ROWS ? p.f[((size_t)a * p.R + r) * p.ldf + c] : p.f[((size_t)a * p.C + c) * p.R + r]);
-        if (!(fabsf(fr) <= 3.4e38f)) s = fmaf(__ldcg(p.t + (size_t)m * p.Rp + r) * w, fr, s);
+        if (fabsf(fr) <= 3.4e38f) continue;
+        const __nv_bfloat16* t = p.t + (size_t)m * p.t_terms * p.Rp + r;
+        s = fmaf(__bfloat162float(__ldcg(t)) + __bfloat162float(__ldcg(t + p.Rp)), fr, s);
     }
     return s;
 }
@@ -476,23 +467,22 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 for (int c = bt; c < p.nt; c += 128) sh.bias[ib][c] = c0 + c < p.C ? __ldg(p.bias + c0 + c) : 0.f;
             int slots[H];
             const int used = ap_find(sh.find, sh.list[ib], id, slots, bt);
-            const int own = id[PAIR ? rank : 0], slot = slots[PAIR ? rank : 0], ext = used * p.Rp;
+            const int slot = slots[PAIR ? rank : 0], ext = used * p.Rp;
             sh.slot[ib][bt] = slot;
             if (bt == 0) sh.ext[ib] = ext;
-            const float scale = (own >= 0 && p.scale ? __ldg(p.scale + own) : 1.f) * p.factor;
             builders_sync();                            // the list stands; and no one still reads what the next tile's search clears
             mbar_arrive(&sh.ifull[ib]);
             if (it == 0) advance(p.kblocks);
-            const float* const trow = p.t + (size_t)m * p.Rp;
+            const __nv_bfloat16* const trow = p.t + (size_t)m * p.t_terms * p.Rp;
+#pragma unroll 1
             for (int e0 = 0; e0 < ext; e0 += WIDTH) {
                 uint4 fv[8], tv[WIDTH / 8][TERMS];
                 const int w = min(WIDTH, ext - e0);
                 ap_load_f<Kind>(p, sh.list[ib], e0, w, cols, row0, step, cj, [&](int i) { return c0 + column(i); }, fv);
-                ap_load_t<Kind, false>(trow, slot, p.Rp, e0, w, scale, tv);
-                bool odd = false;
+                ap_load_t<Kind>(trow, slot, p.Rp, e0, w, tv);
+                if (any_odd(fv)) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) odd |= finite_only(fv[i]);
-                if (odd) {
+                    for (int i = 0; i < 8; ++i) fv[i] = make_uint4(finite_halves(fv[i].x), finite_halves(fv[i].y), finite_halves(fv[i].z), finite_halves(fv[i].w));
                     // Both CTAs of a pair drain all columns: each is told.  The number only grows, so that a CTA that runs ahead hides nothing
                     // from one behind; a number ahead of a tile's costs that tile a search for entries it does not have.
                     if (PAIR) {
@@ -557,68 +547,65 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 const int c_end = WIDE ? min(256, n_here - 256 * part) : n_here, cb = WIDE ? 256 * part : 0;
 #pragma unroll 1
                 for (int c = side * CHUNK; c < c_end; c += 2 * CHUNK) {
-                    uint32_t v[CHUNK];
-#pragma unroll
-                    for (int h = 0; h < CHUNK; h += 32) tmem_ld_x32(acc + c + h, v + h);
-                    tmem_ld_wait();
-                    if (DUAL && ext) {
-#pragma unroll
-                        for (int h = 0; h < CHUNK; h += 8) {
-                            uint32_t u[8];
-                            tmem_ld_x8(acc + p.acc_cols + c + h, u);
-                            const uint32_t bits = drop_bits8_at(p.key, off, (unsigned long long)m * p.C + n0 + c + h);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                if (bits >> i & 1) v[h + i] = __float_as_uint(__uint_as_float(v[h + i]) + __uint_as_float(u[i]));
-                        }
-                    }
                     if (lane == 0) tma_store_wait_read();                      // the box in front has been read
                     __syncwarp();
-                    if (odd) {
 #pragma unroll 1
-                        for (int h = 0; h < CHUNK; h += 32) {
-                            for (int i = 0; i < 32; ++i) {                     // this row's 32 values, in its own place of the buffer
-                                const int col = n0 + cb + c + h + i;
-                                const bool mine = slot >= 0 && col < p.C && (!DUAL || drop_keep_at(p.key, off, (unsigned long long)m * p.C + col));
-                                const float x = mine ? ap_odd<ROWS>(p, sh.list[ib][slot], m, col) : 0.f;
-                                asm volatile("st.shared.f32 [%0], %1;" ::"r"(put + 4 * i), "f"(x) : "memory");
-                            }
+                    for (int h = 0; h < CHUNK; h += 32) {                      // rolled: what runs here has to stay in the instruction cache
+                        uint32_t v[32];
+                        tmem_ld_x32(acc + c + h, v);
+                        if (DUAL) {
+                            uint32_t bits = 0;
+                            const unsigned long long e = (unsigned long long)m * p.C + n0 + c + h;
+#pragma unroll 1
+                            for (int k = 0; k < 4; ++k) bits |= drop_bits8_at(p.key, off, e + 8 * k) << (8 * k);
+                            if (ext) {
+                                uint32_t u[32];
+                                tmem_ld_x32(acc + p.acc_cols + c + h, u);
+                                tmem_ld_wait();
 #pragma unroll
+                                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + (bits >> i & 1 ? __uint_as_float(u[i]) : 0.f));
+                            }
+                        }
+                        tmem_ld_wait();
+                        if (odd) {
+                            // what f that is not finite adds to this row's values
+#pragma unroll 1
                             for (int i = 0; i < 32; ++i) {
-                                float x;
-                                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(put + 4 * i) : "memory");
-                                if (h == 0) v[i] = __float_as_uint(__uint_as_float(v[i]) + x);
-                                else v[(32 + i) % CHUNK] = __float_as_uint(__uint_as_float(v[(32 + i) % CHUNK]) + x);
+                                const int col = n0 + cb + c + h + i;
+                                const bool mine = slot >= 0 && col < p.C && (!DUAL || drop_bits8_at(p.key, off, (unsigned long long)m * p.C + col) & 1);
+                                const float x = mine ? ap_odd<ROWS>(p, sh.list[ib][slot], m, col) : 0.f;
+#pragma unroll
+                                for (int k = 0; k < 32; ++k)
+                                    if (k == i && x != 0.f) v[k] = __float_as_uint(__uint_as_float(v[k]) + x);
                             }
                         }
-                        __syncwarp();
-                    }
-                    if (p.flags & DR_BIAS) {
-                        const float4* bias = reinterpret_cast<const float4*>(&sh.bias[ib][cb + c]);
+                        if (p.flags & DR_BIAS) {
+                            const float4* bias = reinterpret_cast<const float4*>(&sh.bias[ib][cb + c + h]);
 #pragma unroll
-                        for (int i = 0; i < CHUNK / 4; ++i) {
-                            const float4 x = bias[i];
-                            v[4 * i] = __float_as_uint(__uint_as_float(v[4 * i]) + x.x);
-                            v[4 * i + 1] = __float_as_uint(__uint_as_float(v[4 * i + 1]) + x.y);
-                            v[4 * i + 2] = __float_as_uint(__uint_as_float(v[4 * i + 2]) + x.z);
-                            v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + x.w);
+                            for (int i = 0; i < 8; ++i) {
+                                const float4 x = bias[i];
+                                v[4 * i] = __float_as_uint(__uint_as_float(v[4 * i]) + x.x);
+                                v[4 * i + 1] = __float_as_uint(__uint_as_float(v[4 * i + 1]) + x.y);
+                                v[4 * i + 2] = __float_as_uint(__uint_as_float(v[4 * i + 2]) + x.z);
+                                v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + x.w);
+                            }
                         }
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        uint4 x;
+                        // through shared memory, so that whole rows of 128 bytes are written
                         if (f32) {
-                            float y[4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) y[i] = max_nan(__uint_as_float(v[(4 * j + i) % CHUNK]), low);
-                            x = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+                            for (int j = 0; j < 8; ++j)
+                                st_shared16(put + (((uint32_t)j ^ px) << 4),
+                                            make_uint4(__float_as_uint(max_nan(__uint_as_float(v[4 * j]), low)), __float_as_uint(max_nan(__uint_as_float(v[4 * j + 1]), low)),
+                                                       __float_as_uint(max_nan(__uint_as_float(v[4 * j + 2]), low)), __float_as_uint(max_nan(__uint_as_float(v[4 * j + 3]), low))));
                         } else {
-                            const float* y = reinterpret_cast<const float*>(v + (8 * j) % CHUNK);
-                            x = make_uint4(max_nan_bf16x2(pack_bf16(y[0], y[1]), low2), max_nan_bf16x2(pack_bf16(y[2], y[3]), low2),
-                                           max_nan_bf16x2(pack_bf16(y[4], y[5]), low2), max_nan_bf16x2(pack_bf16(y[6], y[7]), low2));
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float* y = reinterpret_cast<const float*>(v + 8 * j);
+                                st_shared16(put + (((uint32_t)(j + (h >> 3)) ^ px) << 4),
+                                            make_uint4(max_nan_bf16x2(pack_bf16(y[0], y[1]), low2), max_nan_bf16x2(pack_bf16(y[2], y[3]), low2),
+                                                       max_nan_bf16x2(pack_bf16(y[4], y[5]), low2), max_nan_bf16x2(pack_bf16(y[6], y[7]), low2)));
+                            }
                         }
-                        st_shared16(put + (((uint32_t)j ^ px) << 4), x);
                     }
                     if (boxes && (c_end - c >= CHUNK || (n0 + cb + c_end == p.C && p.C * (f32 ? 4 : 2) % 16 == 0))) {
                         fence_proxy_async_smem();
@@ -785,21 +772,20 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         if (bt == 0) sh.ext = ext;
         builders_sync();
         mbar_arrive(&sh.ifull);
-        const float scale = (id[0] >= 0 && p.scale ? __ldg(p.scale + id[0]) : 1.f) * p.factor;
-        const float* const trow = p.t + (size_t)bt * p.Rp;
+        const __nv_bfloat16* const trow = p.t + (size_t)bt * p.t_terms * p.Rp;
         const int cpr = ROWS ? p.nt >> 3 : 4, cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
         const bool row_there = (uint32_t)bt * 128u < p.a_bytes;
         bool waited = false, ok = true;
+#pragma unroll 1
         for (int e0 = rank * WIDTH; e0 < ext && ok; e0 += p.split * WIDTH) {
             uint4 fv[8], tv[WIDTH / 8][TERMS];
             const int w = min(WIDTH, ext - e0);
             ap_load_f<Kind>(p, sh.list, e0, w, p.nt, row0, step, cj, [&](int i) { return c0 + i; }, fv);
             if (!waited) { grid_dependency_wait(); waited = true; }            // f needs no waiting, t is the kernel's in front
-            ap_load_t<Kind, false>(trow, slot[0], p.Rp, e0, w, scale, tv);
-            bool odd = false;
+            ap_load_t<Kind>(trow, slot[0], p.Rp, e0, w, tv);
+            if (any_odd(fv)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) odd |= finite_only(fv[i]);
-            if (odd) {
+                for (int i = 0; i < 8; ++i) fv[i] = make_uint4(finite_halves(fv[i].x), finite_halves(fv[i].y), finite_halves(fv[i].z), finite_halves(fv[i].w));
                 for (int k = 0; k < p.split; ++k)
                     asm volatile("red.relaxed.cluster.shared::cluster.max.s32 [%0], %1;" ::"r"(p.split > 1 ? mapa_shared(smem_u32(&sh.odd), k) : smem_u32(&sh.odd)), "r"(1) : "memory");
             }
@@ -981,7 +967,7 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
     p.rows = a.rows;
     p.L = a.L; p.C = a.C; p.R = a.R; p.Rp = a.Rp;
     p.rp_magic = (uint32_t)((0x100000000ull + a.Rp - 1) / a.Rp);
-    p.row_id = a.row_id; p.t = a.t; p.scale = a.scale; p.bias = a.bias; p.f = a.f; p.ldf = a.ldf; p.factor = a.factor;
+    p.row_id = a.row_id; p.t = a.t; p.t_terms = a.terms; p.bias = a.bias; p.f = a.f; p.ldf = a.ldf;
     p.f_vec = !a.transposed && (a.R & 7) == 0;
     p.flags = a.flags; p.out = a.out; p.ldo = a.ldo; p.key = a.key;
     const bool dual = a.key.thr != 0, f32 = a.flags & DR_OUT_F32;
