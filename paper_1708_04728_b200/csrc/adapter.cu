@@ -178,21 +178,19 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     if (dx && (rc = place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, ws, f.a, &ap, &ldap, s)) != DR_OK) return rc;
     __nv_bfloat16* const u = (__nv_bfloat16*)(ws + f.u);
     int* const ids = (int*)(ws + f.ids);
-    if (da || db) {
-        rc = adapter_sort_run(rows, (int*)(ws + f.g + f.grad.perm), (int*)(ws + f.g + f.grad.start), s);
-        if (rc != DR_OK) return rc;
-    }
-    if (dx || da) {
-        __nv_bfloat16* const bt = (__nv_bfloat16*)(ws + f.bt);
-        if ((rc = adapter_transpose_run(d->adapters, N, R, (const __nv_bfloat16*)b, bt, f.Np, s)) != DR_OK) return rc;
-        if ((rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, scale, kept, 3, u, nullptr, ids, s)) != DR_OK) return rc;
-    }
+    const bool grads = da || db, u_wanted = dx || da;
+    __nv_bfloat16* const bt = (__nv_bfloat16*)(ws + f.bt);
+    __nv_bfloat16* const terms = (__nv_bfloat16*)(ws + f.g + f.grad.terms);
+    rc = adapter_prep_run(rows, grads ? (int*)(ws + f.g + f.grad.perm) : nullptr, (int*)(ws + f.g + f.grad.start), N, R, f.Rp, (const __nv_bfloat16*)b,
+                          u_wanted ? bt : nullptr, f.Np, t, scale, db ? terms : nullptr, s);
+    if (rc != DR_OK) return rc;
+    if (u_wanted && (rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, scale, kept, 3, u, nullptr, ids, s)) != DR_OK) return rc;
     if (dx) {
         const ProductArgs g = {rows, N, K, R, f.Rp, dyp, wp, ap, lddyp, ldwp, ldap, ids, u, 3, nullptr, 0, dx, (size_t)lddx, true, key};
         if ((rc = adapter_product_run(g, true, s)) != DR_OK) return rc;
     }
     if (da || db) {
-        const GradJob jobs[2] = {{K, xp, ldxp, nullptr, f.Rp, nullptr, u, key, da, 0}, {N, dyp, lddyp, t, R, scale, nullptr, none, db, 1}};
+        const GradJob jobs[2] = {{K, xp, ldxp, u, key, da, 0}, {N, dyp, lddyp, terms, none, db, 1}};
         if ((rc = adapter_grad_run(f.grad, rows, R, jobs, ws + f.g, s)) != DR_OK) return rc;
     }
     return DR_OK;

@@ -121,22 +121,19 @@ struct GradJob {
     int C;
     const __nv_bfloat16* z;
     size_t ldz;
-    const float* p;             // P as float32 [M][ldp], times scale_a (nullptr: 1), or
-    int ldp;
-    const float* scale;
-    const __nv_bfloat16* terms; // as three bfloat16 values, [M][3][ldp]
+    const __nv_bfloat16* p;     // P as three bfloat16 values, [M][3][Rp]
     DropKey key;
     float* out;                 // [adapters][R][C], or [adapters][C][R] where swap
     int swap;
 };
-struct GradPlan { int splits, rt, rchunks; size_t perm, start, part[2], bytes; };
+struct GradPlan { int tiles, splits, rn, rchunks; size_t perm, start, terms, part[2], bytes; };
 GradPlan adapter_grad_plan(int M, int R, int adapters, const int C[2]);
-int adapter_sort_run(const AdRows& rows, int* perm, int* start, cudaStream_t s);
 int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const GradJob jobs[2], char* ws, cudaStream_t s);
+// in one launch, each where its result is wanted: the rows sorted by adapter (perm, start), b [adapters][N][R] turned to bt [adapters][R][ldb] with zeros
+// behind N, scale_a t as three bfloat16 values
+int adapter_prep_run(const AdRows& rows, int* perm, int* start, int N, int R, int Rp, const __nv_bfloat16* b, __nv_bfloat16* bt, size_t ldb, const float* t,
+                     const float* scale, __nv_bfloat16* terms, cudaStream_t s);
 
 // rows of `cols` elements, `ld` apart, as rows of ldd >= cols with zeros behind them
 int adapter_align_run(size_t rows, int cols, const __nv_bfloat16* src, size_t ld, __nv_bfloat16* dst, size_t ldd, cudaStream_t s);
-// [batch][rows][cols] -> [batch][cols][ldd], zeros behind rows
-int adapter_transpose_run(int batch, int rows, int cols, const __nv_bfloat16* src, __nv_bfloat16* dst, size_t ldd, cudaStream_t s);
-
 }  // namespace dr

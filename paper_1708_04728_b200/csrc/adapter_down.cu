@@ -247,25 +247,4 @@ int adapter_align_run(size_t rows, int cols, const __nv_bfloat16* src, size_t ld
     return launch_status();
 }
 
-__global__ void adapter_transpose_kernel(int rows, int cols, const __nv_bfloat16* __restrict__ src, __nv_bfloat16* __restrict__ dst, size_t ldd) {
-    __shared__ __nv_bfloat16 tile[32][33];
-    const int r0 = blockIdx.x * 32, c0 = blockIdx.y * 32;
-    const __nv_bfloat16* in = src + (size_t)blockIdx.z * rows * cols;
-    __nv_bfloat16* out = dst + (size_t)blockIdx.z * cols * ldd;
-    for (int i = threadIdx.y; i < 32; i += 8) {
-        const int r = r0 + i, c = c0 + (int)threadIdx.x;
-        tile[i][threadIdx.x] = r < rows && c < cols ? in[(size_t)r * cols + c] : __float2bfloat16_rn(0.f);
-    }
-    __syncthreads();
-    for (int i = threadIdx.y; i < 32; i += 8) {
-        const int c = c0 + i, r = r0 + (int)threadIdx.x;
-        if (c < cols && r < (int)ldd) out[(size_t)c * ldd + r] = tile[threadIdx.x][i];
-    }
-}
-int adapter_transpose_run(int batch, int rows, int cols, const __nv_bfloat16* src, __nv_bfloat16* dst, size_t ldd, cudaStream_t s) {
-    adapter_transpose_kernel<<<dim3((unsigned)((ldd + 31) / 32), (unsigned)((cols + 31) / 32), (unsigned)batch), dim3(32, 8), 0, s>>>(rows, cols, src, dst, ldd);
-    count_launch();
-    return launch_status();
-}
-
 }  // namespace dr

@@ -6,19 +6,38 @@
 // and adapter only grow along the list, so their sum numbers the partial results without gaps; they are added in order by a second
 // kernel: the same result on every run, and no share is larger than another however the requests are spread.
 //
-// Warps multiply fragments (mma.sync) of P^T (rows: r) and z (columns: c).  A thread loads 8 neighbouring columns of four rows: with
-// the columns of eight tiles interleaved (column 8 g + n is column g of tile n) and four neighbouring rows to a thread its loads are 16 bytes wide
-// and the transposition is a byte permutation in registers.  P enters as the sum of two bfloat16 values.
+// On the tensor cores (tcgen05): 128 columns of z are the rows of an accumulator in TMEM, P's columns its columns, so both operands have the contraction
+// index m as their rows and are brought as they lie in memory by TMA, 128 bytes wide, into tiles of 64 rows in the 128-byte swizzle: 64 or 16
+// rows that are neighbours in the tensor as one box, others gathered four at a time, with zeros for rows behind the last.  A thread takes about 100 cycles
+// to issue one of these, whatever it brings (16384 x 4096 x 4096 with 112 gathers a stage 319 us, with 28 boxes 129), hence the larger boxes
+// and three issuing warps.  P enters as three bfloat16 values, side by side, which the drain adds up.  With a
+// dropout further warps draw the mask again and clear the dropped values in place before the tile is multiplied.
 #include <algorithm>
 
 #include "adapter.cuh"
+#include "conv_common.cuh"
+#include "umma_ptx.cuh"
 
 namespace dr {
+using namespace ptx;
+
+// ---- what the backward pass lays out first, in one launch -------------------------------------------------------------------------------
+struct PrepParams {
+    AdRows rows;
+    int sort_blocks, turn_x, turn_y, turn_blocks, term_blocks;
+    int *perm, *start;
+    int N, R, Rp;
+    const __nv_bfloat16* b;     // [adapters][N][R], turned to bt [adapters][R][ldb]
+    __nv_bfloat16* bt;
+    size_t ldb;
+    const float *t, *scale;     // scale_a t as three bfloat16 values, [M][3][Rp]
+    __nv_bfloat16* terms;
+};
 
 // perm: rows sorted by adapter; start[a]: where adapter a's begin, start[adapters]: how many there are.  A block per adapter.
-__global__ void __launch_bounds__(256) adapter_sort_kernel(const AdRows r, int* __restrict__ perm, int* __restrict__ start) {
+__device__ __forceinline__ void prep_sort(const AdRows& r, int* __restrict__ perm, int* __restrict__ start, int a) {
     __shared__ int sum_own[8], sum_less[8];
-    const int a = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     auto length = [&](int s, int& id, int& first) {
         if (s >= r.segments) { id = ROW_NONE; first = 0; return 0; }
         first = min(max(__ldg(r.row_start + s), 0), r.M);
@@ -74,207 +93,461 @@ __global__ void __launch_bounds__(256) adapter_sort_kernel(const AdRows r, int* 
     }
 }
 
+// A 32 x 32 tile of an adapter's second factor, turned, with zeros behind its rows.
+__device__ __forceinline__ void prep_turn(const PrepParams& p, int block) {
+    __shared__ __nv_bfloat16 tile[32][33];
+    const int bx = block % p.turn_x, by = block / p.turn_x % p.turn_y, a = block / (p.turn_x * p.turn_y);
+    const int n0 = bx * 32, r0 = by * 32, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    for (int i = ty; i < 32; i += 8) {
+        const int n = n0 + i, r = r0 + tx;
+        tile[i][tx] = n < p.N && r < p.R ? p.b[((size_t)a * p.N + n) * p.R + r] : __float2bfloat16_rn(0.f);
+    }
+    __syncthreads();
+    for (int i = ty; i < 32; i += 8) {
+        const int r = r0 + i, n = n0 + tx;
+        if (r < p.R && n < (int)p.ldb) p.bt[((size_t)a * p.R + r) * p.ldb + n] = tile[tx][i];
+    }
+}
+// 32 rows of scale_a t as sums of three bfloat16 values.
+__device__ __forceinline__ void prep_terms(const PrepParams& p, int block) {
+    __shared__ float scales[32];
+    __shared__ int ids[32];
+    const int m0 = block * 32;
+    if (threadIdx.x < 32) {
+        const int id = adapter_of_warp_row(p.rows, m0, (int)threadIdx.x);
+        ids[threadIdx.x] = id;
+        scales[threadIdx.x] = id >= 0 && p.scale ? __ldg(p.scale + id) : 1.f;
+    }
+    __syncthreads();
+    const int pairs = p.Rp >> 1;
+    for (int i = threadIdx.x; i < 32 * pairs; i += 256) {
+        const int row = i / pairs, r = 2 * (i - row * pairs);
+        if (ids[row] < 0) continue;
+        const float* src = p.t + (size_t)(m0 + row) * p.R + r;
+        uint32_t* dst = reinterpret_cast<uint32_t*>(p.terms + (size_t)(m0 + row) * 3 * p.Rp + r);
+        uint32_t u[3];
+        split3(r < p.R ? src[0] * scales[row] : 0.f, r + 1 < p.R ? src[1] * scales[row] : 0.f, u[0], u[1], u[2]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) dst[(size_t)k * pairs] = u[k];
+    }
+}
+__global__ void __launch_bounds__(256) adapter_prep_kernel(const PrepParams p) {
+    const int b = blockIdx.x;
+    if (b < p.sort_blocks) prep_sort(p.rows, p.perm, p.start, b);
+    else if (b < p.sort_blocks + p.turn_blocks) prep_turn(p, b - p.sort_blocks);
+    else prep_terms(p, b - p.sort_blocks - p.turn_blocks);
+}
+int adapter_prep_run(const AdRows& rows, int* perm, int* start, int N, int R, int Rp, const __nv_bfloat16* b, __nv_bfloat16* bt, size_t ldb, const float* t,
+                     const float* scale, __nv_bfloat16* terms, cudaStream_t s) {
+    PrepParams p = {};
+    p.rows = rows;
+    p.perm = perm; p.start = start; p.N = N; p.R = R; p.Rp = Rp; p.b = b; p.bt = bt; p.ldb = ldb; p.t = t; p.scale = scale; p.terms = terms;
+    p.sort_blocks = perm ? rows.adapters : 0;
+    p.turn_x = (int)((ldb + 31) / 32);
+    p.turn_y = (R + 31) / 32;
+    const long long turn = bt ? (long long)p.turn_x * p.turn_y * rows.adapters : 0, term = terms ? (rows.M + 31) / 32 : 0;
+    if (p.sort_blocks + turn + term > 0x7fffffffll) return DR_ERR_UNSUPPORTED;
+    p.turn_blocks = (int)turn; p.term_blocks = (int)term;
+    adapter_prep_kernel<<<(unsigned)(p.sort_blocks + turn + term), 256, 0, s>>>(p);
+    count_launch();
+    return launch_status();
+}
+
+// ---- the products ---------------------------------------------------------------------------------------------------------------------
+constexpr int GR_THREADS = 384, GR_MASKERS = 256;      // warps 0, 2, 3 load, 1 issues MMAs, 4-11 drain; 12-19 mask, where there is a dropout
+constexpr int GR_ROWS = 64;                            // rows of a stage
+constexpr int GR_MAX_STAGES = 8;
+constexpr int GR_SMEM = 222 * 1024;
+constexpr int GR_BOX = GR_ROWS * 128;
+// Rows summed in TMEM at a time: the tensor cores cut their sums off instead of rounding them, so an error grows with the number of MMAs in a row;
+// longer sums are added up in float32 by the drain.  16384 rows of eight adapters: 7e-7 of the result with 512 rows at a time, over 1e-6 with all 2048.
+constexpr int GR_CHAIN = 512;
+
 struct GradParams {
-    int M, R, adapters, splits, rchunks;
+    int M, R, Rp, adapters, splits;
+    int tiles;                  // accumulators of 128 columns
+    int rn, N, acc_cols, tmem_cols;     // r of a chunk of ranks (a multiple of 8), accumulator columns (three terms of them), their place in TMEM
+    int rchunks, p_boxes, stages, stage_bytes;
     const int *perm, *start;
     int blocks0;                // column blocks of the first job
+    int* status;
     struct Job {
-        int C, ldp, swap;
-        const __nv_bfloat16* z;
-        size_t ldz;
-        const float *p, *scale;
-        const __nv_bfloat16* terms;
+        int C, swap, vec;           // vec: swapped rows of whole 16 bytes
         DropKey key;
         float *part, *out;
     } job[2];
 };
+struct GradShared {
+    uint64_t landed[GR_MAX_STAGES], full[GR_MAX_STAGES], empty[GR_MAX_STAGES], tfull, tempty;
+    uint32_t tmem;
+    int abort;
+    int rows[GR_MAX_STAGES][GR_ROWS];       // of the stage's tile, for the mask
+};
 
-__device__ __forceinline__ void mma_bf16_g(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// four rows of 64 columns from x on
+__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int r0, int r1, int r2, int r3) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+                 "l"(map), "r"(bar), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3)
+                 : "memory");
 }
+__device__ __forceinline__ uint32_t sdesc_mn(uint32_t smem_addr) { return ((smem_addr & 0x3FFFFu) >> 4) | ((uint32_t)(GR_BOX >> 4) << 16); }
 
-// A CTA: 64 columns, RT tiles of 16 r; its 8 warps take every eighth 16 rows.
-template <int RT>
-__global__ void __launch_bounds__(256) adapter_grad_kernel(const GradParams p) {
-    extern __shared__ float gr_join[];                           // [8 warps][RT * 16][65], half of them at a time
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int which = (int)blockIdx.x >= p.blocks0;
-    const GradParams::Job& j = p.job[which];
-    const int cb = (int)blockIdx.x - (which ? p.blocks0 : 0);
-    const int split = blockIdx.y, r0 = (int)blockIdx.z * RT * 16;
+struct GradMaps { CUtensorMap z[2][3], p[2][3]; };              // of both jobs: for gathers, boxes of 16 and of 64 rows
+
+// Shares and adapters of a CTA, in order: calls f(adapter, first sorted row, row behind the last, whole adapter?)
+template <class F>
+__device__ __forceinline__ void grad_ranges(const GradParams& p, int split, F f) {
     const int total = min(max(__ldg(p.start + p.adapters), 0), p.M);
     const int share = ((total + p.splits - 1) / p.splits + 15) & ~15;
     const int from = min(split * share, total), to = min(from + share, total);
     if (from >= to) return;
-    const int c = cb * 64 + 8 * g;
-    const unsigned long long off = j.key.thr ? drop_offset(j.key) : 0ull;
-    const bool whole = (j.C & 7) == 0;
-    // first adapter of the share: the last one that begins at or in front of it and is not empty
-    int lo = 0, hi = p.adapters;
+    int lo = 0, hi = p.adapters;                       // the first adapter whose rows reach beyond `from`
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (__ldg(p.start + mid + 1) <= from) lo = mid + 1;
         else hi = mid;
     }
     for (int a = lo; a < p.adapters; ++a) {
-        const int u = max(from, __ldg(p.start + a)), v = min(to, __ldg(p.start + a + 1));
-        if (__ldg(p.start + a) >= to) break;
-        if (u >= v) continue;
-        const float w = j.scale ? __ldg(j.scale + a) : 1.f;
-        float acc[RT][8][4] = {};
-        for (int i = u + 16 * warp; i < v; i += 128) {
-            uint4 z[4];
-            int row[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int at = i + 4 * q + k;
-                row[k] = at < v ? (int)min((unsigned)__ldg(p.perm + at), (unsigned)(p.M - 1)) : -1;
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                z[k] = make_uint4(0, 0, 0, 0);
-                if (row[k] >= 0 && c < j.C) z[k] = __ldg(reinterpret_cast<const uint4*>(j.z + (size_t)row[k] * j.ldz + c));
-            }
-            uint32_t ph[RT][4], pm[RT][4], pl[RT][4];
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                float x[2][4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int r = r0 + 16 * t + 8 * h + g;
-                        float s = 0.f;
-                        if (row[k] >= 0 && r < p.R)
-{
-                            if (j.terms) {
-                                const __nv_bfloat16* u = j.terms + (size_t)row[k] * 3 * j.ldp + r;
-                                s = (__bfloat162float(u[0]) + __bfloat162float(u[j.ldp])) + __bfloat162float(u[2 * j.ldp]);
-                            } else {
-                                s = __ldg(j.p + (size_t)row[k] * j.ldp + r) * w;
-                            }
-                        }
-                        x[h][k] = s;
-                    }
-                split3(x[0][0], x[0][1], ph[t][0], pm[t][0], pl[t][0]);
-                split3(x[1][0], x[1][1], ph[t][1], pm[t][1], pl[t][1]);
-                split3(x[0][2], x[0][3], ph[t][2], pm[t][2], pl[t][2]);
-                split3(x[1][2], x[1][3], ph[t][3], pm[t][3], pl[t][3]);
-            }
-            if (j.key.thr) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const unsigned long long e = (unsigned long long)max(row[k], 0) * j.C + c;
-                    z[k] = drop_apply8(z[k], whole ? drop_bits8(j.key, off, e >> 3) : drop_bits8_at(j.key, off, e));
-                }
-            }
-            const uint32_t* zu = reinterpret_cast<const uint32_t*>(z);
-#pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                const uint32_t sel = (n & 1) ? 0x7632u : 0x5410u;
-                const uint32_t b0 = __byte_perm(zu[n >> 1], zu[4 + (n >> 1)], sel), b1 = __byte_perm(zu[8 + (n >> 1)], zu[12 + (n >> 1)], sel);
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    mma_bf16_g(acc[t][n], ph[t], b0, b1);
-                    mma_bf16_g(acc[t][n], pm[t], b0, b1);
-                    mma_bf16_g(acc[t][n], pl[t], b0, b1);
-                }
-            }
-        }
-        // the warps' sums, in order: column 8 * (2 q + i) + n of tile n's column 2 q + i
-        float* mine = gr_join + (size_t)warp * (RT * 16) * 65;
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mine[(16 * t + 8 * (i >> 1) + g) * 65 + 8 * (2 * q + (i & 1)) + n] = acc[t][n][i];
-        __syncthreads();
-        float* part = j.part + (size_t)(split + a) * p.R * j.C;
-        for (int i = threadIdx.x; i < RT * 16 * 64; i += 256) {
-            const int r = i >> 6, cc = i & 63;
-            if (r0 + r >= p.R || cb * 64 + cc >= j.C) continue;
-            float s = 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) s += gr_join[((size_t)k * (RT * 16) + r) * 65 + cc];
-            part[(size_t)(r0 + r) * j.C + cb * 64 + cc] = s;
-        }
+        const int u0 = __ldg(p.start + a), v0 = min(__ldg(p.start + a + 1), total);
+        if (u0 >= to) break;
+        if (u0 < v0 && !f(a, max(from, u0), min(to, v0), u0 >= from && v0 <= to)) return;
     }
 }
 
-__global__ void __launch_bounds__(256) adapter_grad_join_kernel(const GradParams p, int from_job) {
-    const int which = from_job + (int)blockIdx.z;
+template <bool DROP>
+__global__ void __launch_bounds__(GR_THREADS + (DROP ? GR_MASKERS : 0), 1)
+adapter_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
+    extern __shared__ uint8_t gr_raw[];
+    __shared__ GradShared sh;
+    const uint32_t ring = (smem_u32(gr_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int which = (int)blockIdx.x >= p.blocks0;
     const GradParams::Job& j = p.job[which];
+    const bool drop = DROP && j.key.thr != 0;
+    const int split = blockIdx.y, r0 = (int)blockIdx.z * p.rn, rn = min(p.rn, p.Rp - r0);
+    const int c0 = ((int)blockIdx.x - (which ? p.blocks0 : 0)) * p.tiles * 128;
+    volatile int* abort_flag = &sh.abort;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < p.stages; ++i) { mbar_init(&sh.landed[i], 1); mbar_init(&sh.full[i], GR_MASKERS / 32); mbar_init(&sh.empty[i], 1); }
+        mbar_init(&sh.tfull, 1);
+        mbar_init(&sh.tempty, 8);
+        sh.abort = 0;
+        fence_barrier_init();
+        for (int k = 0; k < 3; ++k) { prefetch_tensormap(&maps.z[which][k]); prefetch_tensormap(&maps.p[which][k]); }
+    }
+    if (warp == 1) { tmem_alloc(&sh.tmem, (uint32_t)p.tmem_cols); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    const uint32_t landed0 = smem_u32(&sh.landed[0]), full0 = smem_u32(drop ? &sh.full[0] : &sh.landed[0]), empty0 = smem_u32(&sh.empty[0]);
+    auto give_up = [&](int site) {
+        if (!*abort_flag) report_timeout(p.status, site, split);
+        *abort_flag = 1;
+    };
+    auto rows_of = [&](int i, int v, int (&rows)[2]) {         // two of the 64 rows from sorted row i on to a lane; M: none
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = i + 32 * h + lane;
+            rows[h] = at < v ? (int)min((unsigned)__ldg(p.perm + at), (unsigned)(p.M - 1)) : p.M;
+        }
+    };
+
+    if (warp < 4 && warp != 1) {
+        // ---------------------------------------------------------------- loads: a lane has four rows, eight lanes sixteen; each warp every third box
+        const int w = warp ? warp - 1 : 0;
+        const int group = lane & 15, boxes = 2 * p.tiles + p.p_boxes;
+        int s = 0;
+        uint32_t ph = 0;
+        grad_ranges(p, split, [&](int, int u, int v, bool) {
+            int rows[2], next[2];
+            rows_of(u, v, rows);
+            for (int i = u; i < v; i += GR_ROWS) {
+                rows_of(i + GR_ROWS, v, next);                 // on their way during this tile
+                int r[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int from = 4 * (group & 7) + k;
+                    const int a = __shfl_sync(0xffffffffu, rows[0], from), b = __shfl_sync(0xffffffffu, rows[1], from);
+                    r[k] = group < 8 ? a : b;
+                }
+                if (!__all_sync(0xffffffffu, mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag))) { give_up(101); return false; }
+                if (drop && w == 0) { sh.rows[s][lane] = rows[0]; sh.rows[s][32 + lane] = rows[1]; }
+                __syncwarp();
+                if (lane == 0 && w == 0) mbar_expect_tx_u32(landed0 + 8 * s, (uint32_t)p.stage_bytes);
+                __syncwarp();
+                const int lead = __shfl_sync(0xffffffffu, r[0], lane & ~3);
+                const bool run = r[0] == lead + 4 * (lane & 3) && r[1] == r[0] + 1 && r[2] == r[0] + 2 && r[3] == r[0] + 3 && r[3] < p.M;
+                const unsigned runs = __ballot_sync(0xffffffffu, run);
+                const bool sixteen = (runs >> (lane & ~3) & 0xFu) == 0xFu;
+                const int zero = __shfl_sync(0xffffffffu, r[0], 0);
+                const bool all = runs == 0xffffffffu && __all_sync(0xffffffffu, lead == zero + 16 * (group >> 2));
+                auto from_x = [&](int b) { const int pb = b - 2 * p.tiles; return pb < 0 ? c0 + 64 * b : p.rchunks > 1 ? pb * p.Rp + r0 : 64 * pb; };
+                const uint32_t tile = ring + (uint32_t)s * p.stage_bytes, bar = landed0 + 8 * s;
+                if (all) {
+                    if (lane == 0)
+                        for (int b = w; b < boxes; b += 3)
+                            tma_load_2d_u32<false>(tile + (uint32_t)b * GR_BOX, b < 2 * p.tiles ? &maps.z[which][2] : &maps.p[which][2], bar, from_x(b), zero, 1u);
+                } else {
+                    // neighbours: the eight lanes of the sixteen rows take every eighth of the warp's boxes; others: each lane its own rows of every second
+                    const uint32_t dst = tile + (sixteen ? 2048u * (group >> 2) : 512u * group);
+                    const int first = sixteen ? (lane >> 4) * 4 + (lane & 3) : lane >> 4, step = sixteen ? 8 : 2;
+                    for (int b = w + 3 * first; b < boxes; b += 3 * step) {
+                        const int k = b < 2 * p.tiles;
+                        if (sixteen) tma_load_2d_u32<false>(dst + (uint32_t)b * GR_BOX, k ? &maps.z[which][1] : &maps.p[which][1], bar, from_x(b), lead, 1u);
+                        else tma_gather4(dst + (uint32_t)b * GR_BOX, k ? &maps.z[which][0] : &maps.p[which][0], bar, from_x(b), r[0], r[1], r[2], r[3]);
+                    }
+                }
+                __syncwarp();
+                if (++s == p.stages) { s = 0; ph ^= 1; }
+                rows[0] = next[0]; rows[1] = next[1];
+            }
+            return true;
+        });
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- MMAs
+        if (lane == 0) {
+            const uint32_t idesc = make_idesc_bf16(128, p.N) | (1u << 15) | (1u << 16);          // both with the contraction index as rows
+            int s = 0, n = 0;
+            uint32_t ph = 0;
+            grad_ranges(p, split, [&](int, int u, int v, bool) {
+                for (int chain = u; chain < v; chain += GR_CHAIN, ++n) {
+                    if (!mbar_wait(&sh.tempty, (uint32_t)(n & 1) ^ 1, abort_flag)) { give_up(102); return false; }
+                    tc_fence_after();
+                    uint32_t accum = 0;
+                    const int end = min(v, chain + GR_CHAIN);
+                    for (int i = chain; i < end; i += GR_ROWS) {
+                        if (!mbar_wait_u32(full0 + 8 * s, ph, abort_flag)) { give_up(103); return false; }
+                        tc_fence_after();
+                        const uint32_t z = ring + (uint32_t)s * p.stage_bytes, b = sdesc_mn(z + (uint32_t)(2 * p.tiles) * GR_BOX);
+                        const int n16 = (min(end - i, GR_ROWS) + 15) >> 4;
+                        for (int t = 0; t < p.tiles; ++t) {
+                            const uint32_t a = sdesc_mn(z + (uint32_t)(2 * t) * GR_BOX);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                umma_bf16_lo<false>(tmem + (uint32_t)(t * p.acc_cols), a + 128 * k, b + 128 * k, idesc, accum | (uint32_t)(k > 0), k < n16 ? 1u : 0u);
+                        }
+                        accum = 1;
+                        umma_commit_u32<false>(empty0 + 8 * s);
+                        if (++s == p.stages) { s = 0; ph ^= 1; }
+                    }
+                    umma_commit(&sh.tfull);
+                }
+                return true;
+            });
+        }
+        __syncwarp();
+    } else if (DROP && warp >= 12) {
+        // ---------------------------------------------------------------- mask: clears the dropped values of a tile
+        if (drop) {
+            const unsigned long long off = drop_offset(j.key);
+            const int t = threadIdx.x - GR_THREADS;
+            const int zc = p.tiles * 16, step = GR_MASKERS / zc;      // 16-byte pieces of a row; rows that all threads hold
+            const int col = t % zc, row0 = t / zc, c = c0 + 8 * col;
+            const uint32_t base = (uint32_t)(col >> 3) * GR_BOX, ch = (uint32_t)(col & 7);
+            int s = 0;
+            uint32_t ph = 0;
+            grad_ranges(p, split, [&](int, int u, int v, bool) {
+                for (int i = u; i < v; i += GR_ROWS) {
+                    if (!__all_sync(0xffffffffu, mbar_wait_u32(landed0 + 8 * s, ph, abort_flag))) { give_up(105); return false; }
+                    const uint32_t tile = ring + (uint32_t)s * p.stage_bytes + base;
+                    if (c < j.C) {
+#pragma unroll 2
+                        for (int r = row0; r < GR_ROWS; r += step) {
+                            const int row = sh.rows[s][r];
+                            const uint32_t at = tile + r * 128 + ((ch ^ (uint32_t)(r & 7)) << 4);
+                            uint4 x;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
+                            const unsigned long long e = (unsigned long long)row * j.C + c;
+                            const uint32_t bits = (j.C & 7) ? drop_bits8_at(j.key, off, e) : drop_bits8(j.key, off, e >> 3);
+                            x = drop_apply8(x, bits);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                        }
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.full[s]);
+                    if (++s == p.stages) { s = 0; ph ^= 1; }
+                }
+                return true;
+            });
+        }
+    } else if (warp >= 4) {
+        // ---------------------------------------------------------------- drain: lane = column of z, accumulator column = term and r
+        // Two warps to a quarter of the lanes: a tile each, or every other eight r of the only tile.  Sums over chains stay in registers.
+        constexpr int BLOCKS = 10;                              // of eight r: two tiles of 40 (four tiles of at most 128 columns), one of 64
+        const int q = warp & 3, side = (warp - 4) >> 2;
+        const int r8 = rn >> 3, mine = p.tiles > 1 ? (p.tiles >> 1) * r8 : (r8 + 1 - side) >> 1;
+        int n = 0;
+        auto tile_of = [&](int b) { return p.tiles > 1 ? side + 2 * (b >= r8 ? 1 : 0) : 0; };
+        auto r_of = [&](int b) { return p.tiles > 1 ? 8 * (b >= r8 ? b - r8 : b) : 8 * (2 * b + side); };
+        // eight r of a column: to [R][C] or, where swapped, [C][R]
+        auto put = [&](float* to, int c, int r, const float* x) {
+            float* at = to + (j.swap ? (size_t)c * p.R + r : (size_t)r * j.C + c);
+            if (j.vec) {
+                reinterpret_cast<float4*>(at)[0] = make_float4(x[0], x[1], x[2], x[3]);
+                if (r + 4 < p.R) reinterpret_cast<float4*>(at)[1] = make_float4(x[4], x[5], x[6], x[7]);
+                return;
+            }
+            const size_t step = j.swap ? 1 : j.C;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (r + i < p.R) at[i * step] = x[i];
+        };
+        grad_ranges(p, split, [&](int a, int u, int v, bool whole) {
+            float acc[BLOCKS][8];
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[b][i] = 0.f;
+            for (int chain = u; chain < v; chain += GR_CHAIN, ++n) {
+                if (!__all_sync(0xffffffffu, mbar_wait(&sh.tfull, (uint32_t)(n & 1), abort_flag))) { give_up(104); return false; }
+                tc_fence_after();
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    if (b >= mine) break;
+                    const uint32_t at = tmem + (uint32_t)(tile_of(b) * p.acc_cols + r_of(b)) + ((uint32_t)(q * 32) << 16);
+                    uint32_t x[8], y[8], z[8];
+                    tmem_ld_x8(at + 2 * p.rn, x);
+                    tmem_ld_x8(at + p.rn, y);
+                    tmem_ld_x8(at, z);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[b][i] += (__uint_as_float(x[i]) + __uint_as_float(y[i])) + __uint_as_float(z[i]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.tempty);
+            }
+            float* to = whole ? j.out + (size_t)a * p.R * j.C : j.part + (size_t)(split + a) * p.R * j.C;
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                const int c = c0 + 128 * tile_of(b) + 32 * q + lane;
+                if (b < mine && c < j.C) put(to, c, r0 + r_of(b), acc[b]);
+            }
+            return true;
+        });
+        // adapters without rows, shared out over the splits
+        const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int a = split; a < p.adapters; a += p.splits) {
+            if (__ldg(p.start + a) < __ldg(p.start + a + 1)) continue;
+            for (int b = 0; b < mine; ++b) {
+                const int c = c0 + 128 * tile_of(b) + 32 * q + lane;
+                if (c < j.C) put(j.out + (size_t)a * p.R * j.C, c, r0 + r_of(b), zero);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, (uint32_t)p.tmem_cols);
+}
+
+// Adapters whose rows lie in more than one share: their partial sums in order.
+__global__ void __launch_bounds__(256) adapter_grad_join_kernel(const __grid_constant__ GradParams p) {
+    const GradParams::Job& j = p.job[blockIdx.z];
     if (!j.out) return;
     const int a = blockIdx.y;
     const int total = min(max(__ldg(p.start + p.adapters), 0), p.M);
     const int share = ((total + p.splits - 1) / p.splits + 15) & ~15;
     const int u = __ldg(p.start + a), v = min(__ldg(p.start + a + 1), total);
-    const int n = p.R * j.C;
-    const int s0 = u < v ? u / share : 0, s1 = u < v ? (v - 1) / share : -1;
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+    if (u >= v) return;
+    const int s0 = u / share, s1 = (v - 1) / share;
+    if (s0 == s1) return;
+    const size_t n = (size_t)p.R * j.C, stride = (size_t)gridDim.x * 256;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
         float s = 0.f;
-        for (int k = s0; k <= s1; ++k) s += j.part[(size_t)(k + a) * n + i];
-        const int r = i / j.C, c = i - r * j.C;
-        j.out[(size_t)a * n + (j.swap ? (size_t)c * p.R + r : (size_t)i)] = s;
+        const float* part = j.part + (size_t)(s0 + a) * n + i;
+#pragma unroll 4
+        for (int k = s0; k <= s1; ++k, part += n) s += *part;
+        j.out[(size_t)a * n + i] = s;
     }
 }
 
 GradPlan adapter_grad_plan(int M, int R, int adapters, const int C[2]) {
     GradPlan g = {};
-    g.rt = R <= 16 ? 1 : R <= 32 ? 2 : 4;
-    g.rchunks = (R + 16 * g.rt - 1) / (16 * g.rt);
-    const int blocks = ((C[0] + 63) / 64 + (C[1] + 63) / 64) * g.rchunks;
-    g.splits = std::max(1, std::min((M + 127) / 128, (4 * num_sms() + blocks - 1) / blocks));
+    const int Rp = (R + 7) / 8 * 8, sms = num_sms();
+    g.rchunks = (Rp + 63) / 64;
+    g.rn = g.rchunks == 1 ? Rp : 64;
+    const int cols = (3 * g.rn + 31) / 32 * 32;               // of an accumulator
+    // Columns of a CTA: as many as tensor memory has room for, fewer where that leaves SMs without rows; shares of at least 256 rows
+    const int most = std::max(1, (M + 255) / 256);
+    for (g.tiles = 4; g.tiles > 1; g.tiles /= 2) {
+        const int blocks = ((C[0] + 128 * g.tiles - 1) / (128 * g.tiles) + (C[1] + 128 * g.tiles - 1) / (128 * g.tiles)) * g.rchunks;
+        if (g.tiles * cols <= 512 && (long long)blocks * most >= sms) break;
+    }
+    const int blocks = ((C[0] + 128 * g.tiles - 1) / (128 * g.tiles) + (C[1] + 128 * g.tiles - 1) / (128 * g.tiles)) * g.rchunks;
+    g.splits = std::max(1, std::min(most, sms / blocks));
     size_t at = 0;
     auto take = [&](size_t& where, size_t bytes) { where = at; at += (bytes + 255) / 256 * 256; };
     take(g.perm, (size_t)M * 4);
     take(g.start, (size_t)(adapters + 1) * 4);
-    for (int k = 0; k < 2; ++k) take(g.part[k], (size_t)(g.splits + adapters - 1) * R * C[k] * 4);
+    take(g.terms, (size_t)M * 3 * Rp * 2);
+    for (int k = 0; k < 2; ++k) take(g.part[k], g.splits > 1 ? (size_t)(g.splits + adapters - 1) * R * C[k] * 4 : 0);
     g.bytes = at;
     return g;
 }
 
-int adapter_sort_run(const AdRows& rows, int* perm, int* start, cudaStream_t s) {
-    adapter_sort_kernel<<<(unsigned)rows.adapters, 256, 0, s>>>(rows, perm, start);
-    count_launch();
-    return launch_status();
-}
-
-template <int RT>
-static int grad_launch(const dim3& grid, const GradParams& p, cudaStream_t s) {
-    constexpr int smem = 8 * RT * 16 * 65 * 4;
-    static PerDeviceFlag ready;
-    if (!ready.get()) {
-        if (cudaFuncSetAttribute(adapter_grad_kernel<RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
-        ready.set();
-    }
-    adapter_grad_kernel<RT><<<grid, 256, smem, s>>>(p);
-    return launch_status();
+// rows of `cols` elements, `ld` apart, 64 columns and box_rows rows at a time
+static int gr_map(CUtensorMap* map, const void* ptr, size_t rows, size_t cols, size_t ld, int box_rows) {
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    return tmap_tiled(map, 2, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const GradJob jobs[2], char* ws, cudaStream_t s) {
     GradParams p = {};
-    p.M = rows.M; p.R = R; p.adapters = rows.adapters; p.splits = plan.splits; p.rchunks = plan.rchunks;
+    p.M = rows.M; p.R = R; p.Rp = (R + 7) / 8 * 8; p.adapters = rows.adapters; p.splits = plan.splits;
+    p.tiles = plan.tiles; p.rn = plan.rn; p.rchunks = plan.rchunks;
+    p.N = (3 * plan.rn + 15) / 16 * 16;
+    p.acc_cols = (p.N + 31) / 32 * 32;
+    p.tmem_cols = 32;
+    while (p.tmem_cols < p.acc_cols * p.tiles) p.tmem_cols *= 2;
+    p.p_boxes = (3 * plan.rn + 63) / 64;
+    p.stage_bytes = (2 * p.tiles + p.p_boxes) * GR_BOX;
+    p.stages = std::min(GR_MAX_STAGES, GR_SMEM / p.stage_bytes);
     p.perm = (int*)(ws + plan.perm); p.start = (int*)(ws + plan.start);
-    int blocks[2], most = 0;
+    p.status = dev_status_ptr();
+    int blocks[2];
+    long long most = 0;
     for (int k = 0; k < 2; ++k) {
         const GradJob& g = jobs[k];
-        p.job[k] = {g.C, g.ldp, g.swap, g.z, g.ldz, g.p, g.scale, g.terms, g.key, (float*)(ws + plan.part[k]), g.out};
-        blocks[k] = g.out ? (g.C + 63) / 64 : 0;
-        if (g.out) most = std::max(most, g.C);
+        p.job[k] = {g.C, g.swap, g.swap && (R & 3) == 0 && aligned16(g.out), g.key, (float*)(ws + plan.part[k]), g.out};
+        blocks[k] = g.out ? (g.C + 128 * p.tiles - 1) / (128 * p.tiles) : 0;
+        if (g.out) most = std::max<long long>(most, (long long)R * g.C);
     }
     p.blocks0 = blocks[0];
-    const dim3 grid((unsigned)(blocks[0] + blocks[1]), (unsigned)plan.splits, (unsigned)plan.rchunks);
-    const int rc = plan.rt == 1 ? grad_launch<1>(grid, p, s) : plan.rt == 2 ? grad_launch<2>(grid, p, s) : grad_launch<4>(grid, p, s);
+    alignas(64) GradMaps maps = {};
+    int rc = DR_OK;
+    for (int k = 0; k < 2; ++k) {
+        const GradJob& g = jobs[k];
+        if (!g.out) continue;
+        const int box[3] = {1, 16, GR_ROWS};
+        for (int i = 0; i < 3 && rc == DR_OK; ++i) {
+            rc = gr_map(&maps.z[k][i], g.z, p.M, g.C, g.ldz, box[i]);
+            if (rc == DR_OK) rc = gr_map(&maps.p[k][i], g.p, p.M, 3 * (size_t)p.Rp, 3 * (size_t)p.Rp, box[i]);
+        }
+    }
     if (rc != DR_OK) return rc;
-    const long long n = ((long long)R * most + 255) / 256;
-    adapter_grad_join_kernel<<<dim3((unsigned)std::min(n, 1024ll), (unsigned)rows.adapters, 2), 256, 0, s>>>(p, 0);
-    count_launch(2);
-    return launch_status();
+    const bool drop = jobs[0].out && jobs[0].key.thr != 0;
+    static PerDeviceFlag ready[2];
+    if (!ready[drop].get()) {
+        const cudaError_t e = drop ? cudaFuncSetAttribute(adapter_grad_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, GR_SMEM + 1024)
+                                   : cudaFuncSetAttribute(adapter_grad_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, GR_SMEM + 1024);
+        if (e != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+        ready[drop].set();
+    }
+    const dim3 grid((unsigned)(blocks[0] + blocks[1]), (unsigned)plan.splits, (unsigned)plan.rchunks);
+    const int smem = 1024 + p.stages * p.stage_bytes;
+    if (drop) adapter_grad_kernel<true><<<grid, GR_THREADS + GR_MASKERS, smem, s>>>(maps, p);
+    else adapter_grad_kernel<false><<<grid, GR_THREADS, smem, s>>>(maps, p);
+    count_launch();
+    rc = launch_status();
+    if (rc == DR_OK && plan.splits > 1) {
+        adapter_grad_join_kernel<<<dim3((unsigned)std::min((most + 255) / 256, 512ll), (unsigned)rows.adapters, 2), 256, 0, s>>>(p);
+        count_launch();
+        rc = launch_status();
+    }
+    return rc;
 }
 
 }  // namespace dr
