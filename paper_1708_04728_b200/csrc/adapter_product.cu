@@ -16,6 +16,7 @@
 // stages.  A CTA's first tile takes them behind its blocks of l, so that w streams in while t is still being made; later tiles take them in front, so
 // that they are built while the tile before is multiplied.
 #include <algorithm>
+#include <atomic>
 
 #include "adapter.cuh"
 #include "conv_common.cuh"
@@ -663,7 +664,9 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
 // ---- few rows (one tile of at most 128) ------------------------------------------------------------------------------------------------
 // Bound by the bytes of w, and by latency.  A cluster of CTAs shares a tile's l: each takes a range of it and every so many of the further blocks, and the
 // accumulators meet in distributed shared memory, where each CTA sums and finishes a part of the columns.  Rows of z behind the last are not
-// loaded: what the MMA finds there only reaches rows of the accumulator that nobody reads.
+// loaded: what the MMA finds there only reaches rows of the accumulator that nobody reads.  8 warps of at most 128 registers (0 loads, 1 issues MMAs, 4-7
+// build the further blocks and then drain), so that a CTA fits beside the first product's and w streams in while t is still being made.
+constexpr int AP_FEW_THREADS = 256;
 struct ApFewShared {
     uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], tfull, loads, ifull;
     uint32_t tmem;
@@ -674,7 +677,7 @@ struct ApFewShared {
 };
 
 template <class Kind>
-__global__ void __launch_bounds__(AP_THREADS, 1)
+__global__ void __launch_bounds__(AP_FEW_THREADS, 2)
 adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ApParams p) {
     constexpr bool ROWS = Kind::ROWS, DUAL = Kind::DUAL;
     constexpr int TERMS = Kind::TERMS, WIDTH = Kind::WIDTH;
@@ -761,8 +764,8 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
             umma_commit_u32<false>(smem_u32(&sh.tfull));
         }
         __syncwarp();
-    } else if (warp >= 12) {
-        const int bt = threadIdx.x - 384;
+    } else if (warp >= 4) {
+        const int bt = threadIdx.x - 128;
         int s = (kb1 - kb0) % p.stages;
         uint32_t ph = (uint32_t)((kb1 - kb0) / p.stages) & 1u;
         int id[1] = {adapter_of_warp_row(p.rows, bt & ~31, lane)}, slot[1];
@@ -776,12 +779,14 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         const int cpr = ROWS ? p.nt >> 3 : 4, cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
         const bool row_there = (uint32_t)bt * 128u < p.a_bytes;
         bool waited = false, ok = true;
+        auto load_f = [&](int e0, uint4 (&fv)[8]) { ap_load_f<Kind>(p, sh.list, e0, min(WIDTH, ext - e0), p.nt, row0, step, cj, [&](int i) { return c0 + i; }, fv); };
+        uint4 fv[8];
+        if (rank * WIDTH < ext) load_f(rank * WIDTH, fv);                      // f needs no waiting, t is the kernel's in front
 #pragma unroll 1
         for (int e0 = rank * WIDTH; e0 < ext && ok; e0 += p.split * WIDTH) {
-            uint4 fv[8], tv[WIDTH / 8][TERMS];
+            uint4 fn[8], tv[WIDTH / 8][TERMS];
             const int w = min(WIDTH, ext - e0);
-            ap_load_f<Kind>(p, sh.list, e0, w, p.nt, row0, step, cj, [&](int i) { return c0 + i; }, fv);
-            if (!waited) { grid_dependency_wait(); waited = true; }            // f needs no waiting, t is the kernel's in front
+            if (!waited) { grid_dependency_wait(); waited = true; }
             ap_load_t<Kind>(trow, slot[0], p.Rp, e0, w, tv);
             if (any_odd(fv)) {
 #pragma unroll
@@ -789,6 +794,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
                 for (int k = 0; k < p.split; ++k)
                     asm volatile("red.relaxed.cluster.shared::cluster.max.s32 [%0], %1;" ::"r"(p.split > 1 ? mapa_shared(smem_u32(&sh.odd), k) : smem_u32(&sh.odd)), "r"(1) : "memory");
             }
+            if (e0 + p.split * WIDTH < ext) load_f(e0 + p.split * WIDTH, fn);  // the next block's on their way while this one is stored
             const bool slot_free = __all_sync(0xffffffffu, mbar_wait(&sh.loads, 0, abort_flag) && mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag));
             if (!slot_free) give_up(96);
             if (slot_free) {
@@ -799,12 +805,14 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
             if (builders_any(!slot_free)) { ok = false; break; }
             if (bt == 0) mbar_arrive(&sh.full[s]);
             if (++s == p.stages) { s = 0; ph ^= 1; }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) fv[i] = fn[i];
         }
         if (!waited) grid_dependency_wait();
     }
-    // every thread: the accumulators' rows into shared memory
-    if (warp >= 4 && warp < 12) {
-        const int q = warp & 3, side = (warp - 4) >> 2, row = q * 32 + lane;
+    // the accumulators' rows into shared memory
+    if (warp >= 4) {
+        const int q = warp & 3, row = q * 32 + lane;
         if (q * 32 < p.rows.M) {
             if (!__all_sync(0xffffffffu, mbar_wait(&sh.tfull, 0, abort_flag))) {
                 give_up(97);
@@ -812,8 +820,9 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
                 tc_fence_after();
                 const int ext = sh.ext;
                 const bool own = ext > rank * WIDTH;             // this CTA had a further block
-                for (int c = side * 32; c < p.nt; c += 64) {
-#pragma unroll
+#pragma unroll 1
+                for (int c = 0; c < p.nt; c += 32) {
+#pragma unroll 1
                     for (int k = 0; k < (DUAL ? 2 : 1); ++k) {
                         uint32_t v[32];
                         tmem_ld_x32(tmem + (uint32_t)k * p.acc_cols + ((uint32_t)(q * 32) << 16) + c, v);
@@ -840,7 +849,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         const unsigned long long off = DUAL ? drop_offset(p.key) : 0ull;
         const bool odd = sh.odd != 0;
         const float low = (p.flags & DR_RELU) ? 0.f : -INFINITY;
-        for (int i = threadIdx.x; i < p.rows.M * quads; i += AP_THREADS) {
+        for (int i = threadIdx.x; i < p.rows.M * quads; i += AP_FEW_THREADS) {
             const int m = i / quads, cl = rank * width + 4 * (i - m * quads), c = c0 + cl;
             const int slot = sh.slot[m];
             if (slot == ROW_NONE || c >= p.C) continue;
@@ -888,14 +897,14 @@ static int ap_map(CUtensorMap* map, const void* ptr, size_t rows, size_t inner, 
 }
 
 template <class Kernel, class... Args>
-static int ap_start(Kernel k, PerDeviceFlag& ready, int grid, int cluster, bool overlap, size_t smem, cudaStream_t s, const Args&... args) {
+static int ap_start(Kernel k, PerDeviceFlag& ready, int grid, int threads, int cluster, bool overlap, size_t smem, cudaStream_t s, const Args&... args) {
     if (!ready.get()) {
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, AP_SMEM_MOST) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
         ready.set();
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(AP_THREADS);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -920,12 +929,39 @@ template <class Kind>
 static int ap_launch(const CUtensorMap& mz, const CUtensorMap& mw, const CUtensorMap& mo, const ApParams& p, bool overlap, size_t smem, cudaStream_t s) {
     static PerDeviceFlag ready;
     const int units = Kind::PAIR ? num_sms() / 2 : num_sms();
-    return ap_start(adapter_product_kernel<Kind>, ready, std::min(p.tiles, units) * (Kind::PAIR ? 2 : 1), Kind::PAIR ? 2 : 1, overlap, smem, s, mz, mw, mo, p);
+    return ap_start(adapter_product_kernel<Kind>, ready, std::min(p.tiles, units) * (Kind::PAIR ? 2 : 1), AP_THREADS, Kind::PAIR ? 2 : 1, overlap, smem, s, mz, mw, mo, p);
 }
 template <class Kind>
 static int ap_launch_few(const CUtensorMap& mz, const CUtensorMap& mw, const ApParams& p, bool overlap, size_t smem, cudaStream_t s) {
     static PerDeviceFlag ready;
-    return ap_start(adapter_few_kernel<Kind>, ready, p.tiles_c * p.split, p.split, overlap, smem, s, mz, mw, p);
+    return ap_start(adapter_few_kernel<Kind>, ready, p.tiles_c * p.split, AP_FEW_THREADS, p.split, overlap, smem, s, mz, mw, p);
+}
+
+// Clusters of so many CTAs that the device holds at a time (a cluster lies within a group of SMs, so they are fewer than the SMs suggest).
+static int few_clusters(int ctas) {
+    static std::atomic<int> known[4][64];
+    const int d = PerDeviceFlag::dev(), i = ctas == 1 ? 0 : ctas == 2 ? 1 : ctas == 4 ? 2 : 3;
+    if (i == 0) return num_sms();
+    int n = known[i][d].load(std::memory_order_relaxed);
+    if (n == 0) {
+        auto* k = adapter_few_kernel<ApKind<false, false, false, false, 2>>;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(num_sms() / ctas * ctas));
+        cfg.blockDim = dim3(AP_FEW_THREADS);
+        cfg.dynamicSmemBytes = AP_SMEM;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, AP_SMEM_MOST) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, k, &cfg) != cudaSuccess || n < 1) {
+            (void)cudaGetLastError();
+            n = num_sms() / (2 * ctas);
+        }
+        known[i][d].store(n, std::memory_order_relaxed);
+    }
+    return n;
 }
 
 static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t s) {
@@ -938,7 +974,7 @@ static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t
     for (int nt = a.transposed ? 64 : 16; nt <= 128; nt *= 2)
         for (int split = 1; split <= 8 && split <= p.kblocks && 4 * split <= nt; split *= 2) {
             const int tiles = (a.C + nt - 1) / nt, blocks = (p.kblocks + split - 1) / split;
-            const int waves = (tiles * split + sms - 1) / sms;
+            const int waves = (tiles + few_clusters(split) - 1) / few_clusters(split);
             const double cta = blocks * ((p.a_bytes + nt * 128.) / 32. + 150.);
             const double t = std::max(waves * cta, (double)a.C * a.L * 2. / 3400.) + (split > 1 ? 1500. : 0.) + waves * 2. * nt;
             if (best == 0. || t < best) { best = t; p.nt = nt; p.split = split; }
