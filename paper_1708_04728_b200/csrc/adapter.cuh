@@ -29,9 +29,20 @@ __device__ __forceinline__ int adapter_of_count(const AdRows& r, int count) {   
     const int a = __ldg(r.adapter + count - 1);
     return a >= 0 && a < r.adapters ? a : ROW_SHARED;           // an adapter out of range is none
 }
-// The adapter of row m0 + lane, by a whole warp: 32 offsets are probed at a time (two dependent loads for a thousand requests instead of ten), for
-// the first and the last of the rows; rows between two requests search between these alone.
+// The adapter of row m0 + lane, by a whole warp, with few dependent loads: up to 32 offsets are loaded at once and counted out of registers; of more, 32 are
+// probed at a time (two loads for a thousand requests instead of ten) for the first and the last of the rows, and the ones between are counted.
+__device__ __forceinline__ int offsets_counted(const AdRows& r, int m, int lo, int n, int lane) {     // n <= 32 offsets from lo on
+    const int o = lane < n ? __ldg(r.row_start + lo + lane) : 0x7fffffff;
+    int count = lo;
+    for (int k = 0; k < n; ++k) count += __shfl_sync(0xffffffffu, o, k) <= m ? 1 : 0;
+    return count;
+}
 __device__ __forceinline__ int adapter_of_warp_row(const AdRows& r, int m0, int lane) {
+    const int m = m0 + lane;
+    if (r.segments < 32) {
+        const int count = offsets_counted(r, m, 0, r.segments + 1, lane);
+        return m >= r.M ? ROW_NONE : adapter_of_count(r, count);
+    }
     const int last = m0 + 31;
     int lo[2] = {0, 0}, n[2] = {r.segments + 1, r.segments + 1};
     while (n[0] > 0 || n[1] > 0) {
@@ -48,9 +59,9 @@ __device__ __forceinline__ int adapter_of_warp_row(const AdRows& r, int m0, int 
             n[k] = skip == n[k] ? 0 : min(step - 1, n[k] - skip - 1);   // the probed offset of the next piece is above the row
         }
     }
-    const int m = m0 + lane;
-    if (m >= r.M) return ROW_NONE;
-    return adapter_of_count(r, lo[0] >= lo[1] ? lo[0] : offsets_upto(r, m, lo[0], lo[1]));
+    const int between = lo[1] - lo[0];
+    const int count = between <= 0 ? lo[0] : between <= 32 ? offsets_counted(r, m, lo[0], between, lane) : offsets_upto(r, m, lo[0], lo[1]);
+    return m >= r.M ? ROW_NONE : adapter_of_count(r, count);
 }
 
 // Which of 8 consecutive elements, the first with number e, are kept: bit i for element e + i.

@@ -45,6 +45,11 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
     const int ks = blockIdx.y, zi = (int)blockIdx.z % p.zsplit, r0 = ((int)blockIdx.z / p.zsplit) * RT * 8;
     const int l0 = ks * p.l_range, l1 = min(p.L8, l0 + p.l_range);
     if (m0 >= p.rows.M) return;                                  // JOIN: the whole CTA
+    // z on its way to L2 while the rows' adapters are looked up: a line a thread
+    for (int i = JOIN ? (int)threadIdx.x : lane; i < MT * 16 * ((l1 - l0 + 63) >> 6); i += JOIN ? 256 : 32) {
+        const int row = i % (MT * 16), l = l0 + 64 * (i / (MT * 16));
+        if (m0 + row < p.rows.M && l < l1) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.z + (size_t)(m0 + row) * p.ldz + l));
+    }
     int id = adapter_of_warp_row(p.rows, m0, lane);
     if (lane >= MT * 16) id = ROW_NONE;
     else if (p.row_id && blockIdx.y == 0 && blockIdx.z == 0 && (!JOIN || warp == 0) && m0 + lane < p.rows.M) p.row_id[m0 + lane] = id;

@@ -671,9 +671,10 @@ struct ApFewShared {
     uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], tfull, loads, ifull;
     uint32_t tmem;
     int abort, odd, ext;
-    int slot[AP_TILE], id[AP_TILE];
+    int slot[AP_TILE];
     uint16_t list[AP_TILE];
     ApFind find;
+    float bias[AP_TILE];        // of the columns this CTA finishes
 };
 
 template <class Kind>
@@ -810,6 +811,10 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         }
         if (!waited) grid_dependency_wait();
     }
+    if (warp == 2 && (p.flags & DR_BIAS)) {
+        const int width = p.nt / p.split;
+        for (int i = lane; i < width; i += 32) sh.bias[i] = c0 + rank * width + i < p.C ? __ldg(p.bias + c0 + rank * width + i) : 0.f;
+    }
     // the accumulators' rows into shared memory
     if (warp >= 4) {
         const int q = warp & 3, row = q * 32 + lane;
@@ -868,7 +873,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
             for (int k = 0; k < 4; ++k) {
                 if (DUAL && (bits >> k & 1)) v[k] += u[k];
                 if (odd && slot >= 0 && c + k < p.C && (bits >> k & 1)) v[k] += ap_odd<ROWS>(p, sh.list[slot], m, c + k);
-                if ((p.flags & DR_BIAS) && c + k < p.C) v[k] += __ldg(p.bias + c + k);
+                if (p.flags & DR_BIAS) v[k] += sh.bias[cl - rank * width + k];
                 v[k] = max_nan(v[k], low);
             }
             const size_t to = (size_t)m * p.ldo + c;
