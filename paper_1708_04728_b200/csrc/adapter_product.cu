@@ -27,8 +27,8 @@ using namespace ptx;
 
 constexpr int AP_THREADS = 512;
 constexpr int AP_MAX_STAGES = 16;
-constexpr int AP_SMEM = 184 * 1024;     // the ring's; with 32 KB of the drain's and the barriers' all of an SM's
-constexpr int AP_SMEM_MOST = 217 * 1024;
+constexpr int AP_SMEM = 180 * 1024;     // the ring's; with 32 KB of the drain's and the barriers' all of an SM's
+constexpr int AP_SMEM_MOST = 213 * 1024;
 constexpr int AP_TILE = 128;
 
 struct ApParams {
@@ -63,15 +63,22 @@ struct ApFind {
     int sums[4];
 };
 struct ApShared {
-    uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], tfull[2], tempty[2], ifull[2], iempty[2], loads[2], built[2];
+    uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], tfull[2], tempty[2], ifull[3], iempty[3], loads[3], built[3];
     uint32_t tmem;
     int abort;
-    int ext[2];                 // columns of T of the tile
-    int odd[2];                 // number (from 1) of the latest tile that met an f that is not finite
-    int slot[2][AP_TILE];       // place of the row's adapter in list, ROW_SHARED or ROW_NONE
-    uint16_t list[2][2 * AP_TILE];
+    // what the builders find out about a tile: kept for three of them, one being drained, one multiplied, one looked at ahead
+    int ext[3];                 // columns of T of the tile
+    int odd[3];                 // number (from 1) of the latest tile that met an f that is not finite
+    int slot[3][AP_TILE];       // place of the row's adapter in list, ROW_SHARED or ROW_NONE
+    uint16_t list[3][2 * AP_TILE];
+    alignas(16) float bias[3][512];
     ApFind find;
-    alignas(16) float bias[2][512];
+};
+// a place in that ring of three and how often it was used
+struct ApInfo {
+    int at = 0;
+    uint32_t use = 0;
+    __device__ __forceinline__ void next() { if (++at == 3) { at = 0; use ^= 1; } }
 };
 
 __device__ __forceinline__ uint32_t sdesc_rows_lo(uint32_t smem_addr, uint32_t box) {    // contraction index = row of a 64-column box
@@ -115,7 +122,8 @@ struct ApKind {
     static constexpr int TERMS = TERMS_;
     static constexpr bool PAIR = PAIR_, WIDE = WIDE_, ROWS = ROWS_, DUAL = DUAL_;
     static constexpr int WIDTH = TERMS == 2 ? 32 : 16;         // columns of T in a further block of 64
-    static constexpr int EACH = 8;                              // 16-byte pieces of a block's f that a thread brings, at most
+    static constexpr int EACH = PAIR && !WIDE ? 4 : 8;          // 16-byte pieces of a block's f that a thread brings, at most
+    static constexpr bool AHEAD = EACH == 4;                    // registers for the next block's loads beside this one's
 };
 
 // ---- the builders' steps (128 threads, bt their number) --------------------------------------------------------------------
@@ -296,13 +304,15 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.tfull[i], 1);
             mbar_init(&sh.tempty[i], PAIR ? 16 : 8);
+        }
+        for (int i = 0; i < 3; ++i) {
             mbar_init(&sh.loads[i], 1);
             mbar_init(&sh.built[i], 1);
             mbar_init(&sh.ifull[i], 128);
             mbar_init(&sh.iempty[i], 9 + (rank == 0 ? (WIDE ? 2 : 1) : 0));
+            sh.odd[i] = 0;
         }
         sh.abort = 0;
-        sh.odd[0] = sh.odd[1] = 0;
         fence_barrier_init();
         prefetch_tensormap(&map_z);
         prefetch_tensormap(&map_w);
@@ -330,17 +340,19 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
             int s = 0, it = 0, gap = 0;
             uint32_t ph = 0;
             bool ok = true;
+            ApInfo info;
             // Passes over the further blocks of a tile.  The parity of a barrier tells two neighbouring phases apart and no more: who waits for a stage
-            // must know that the use before the last one is over.  The builders know it once the loads in front of theirs are all
+            // must know that the use before the last one is over, and no barrier here may run two phases ahead of one who waits for it (three of each are
+            // enough: no one is further ahead than the builders, who look at a tile while the one three in front of it is done).  The builders know it once the loads in front of theirs are all
             // issued (sh.loads); this thread where the further blocks since its last load are fewer than the stages, and otherwise once they are
             // built.
             auto pass = [&](int tile) {
-                const int ib = it & 1;
-                if (!mbar_wait(&sh.ifull[ib], (it >> 1) & 1, abort_flag)) { give_up(82, tile); return false; }
-                const int further = further_stages(sh.ext[ib]);
-                mbar_arrive(&sh.iempty[ib]);
+                if (!mbar_wait(&sh.ifull[info.at], info.use, abort_flag)) { give_up(82, tile); return false; }
+                const int further = further_stages(sh.ext[info.at]);
+                mbar_arrive(&sh.iempty[info.at]);
                 gap += further;
-                if (it > 0 && gap >= p.stages && !mbar_wait(&sh.built[ib], (it >> 1) & 1, abort_flag)) { give_up(91, tile); return false; }
+                if (it > 0 && gap >= p.stages && !mbar_wait(&sh.built[info.at], info.use, abort_flag)) { give_up(91, tile); return false; }
+                info.next();
                 s += further;
                 while (s >= p.stages) { s -= p.stages; ph ^= 1; }
                 return true;
@@ -367,7 +379,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 }
                 if (!ok) break;
                 gap = 0;
-                mbar_arrive(&sh.loads[it & 1]);
+                mbar_arrive(&sh.loads[it % 3]);
                 if (it == 0 && !pass(tile)) break;
             }
         }
@@ -381,11 +393,12 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
             constexpr uint32_t b_step = ROWS ? 128u : 2u;
             int s = 0, it = 0;
             uint32_t ph = 0, accum = 0, d = 0;
+            ApInfo info;
             auto further = [&](int tile) {
-                const int ib = it & 1;
-                if (!mbar_wait(&sh.ifull[ib], (it >> 1) & 1, abort_flag)) { give_up(85, tile); return false; }
-                const int ext = sh.ext[ib];
-                mbar_arrive(&sh.iempty[ib]);
+                if (!mbar_wait(&sh.ifull[info.at], info.use, abort_flag)) { give_up(85, tile); return false; }
+                const int ext = sh.ext[info.at];
+                mbar_arrive(&sh.iempty[info.at]);
+                info.next();
                 const uint32_t de = d + (DUAL ? p.acc_cols : 0u);
                 uint32_t acc = DUAL ? 0u : accum;
                 for (int e = 0; e < ext; e += WIDTH) {
@@ -435,84 +448,119 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
     } else if (warp >= 12) {
         // ---------------------------------------------------------------- the rows' adapters, and the further blocks
         const int bt = threadIdx.x - 384;
-        int s = 0, it = 0;
-        uint32_t ph = 0;
-        bool ok = true;
-        auto advance = [&](int n) {
-            s += n;
-            while (s >= p.stages) { s -= p.stages; ph ^= 1; }
-        };
         constexpr int H = PAIR ? 2 : 1;
-        int id[H], next[H];
-        auto ids = [&](int tile, int (&to)[H]) {
+        const int cpr = ROWS ? cols >> 3 : 4;                                  // 16-byte pieces of a row of a block
+        const int cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
+        struct Opened { int it, at, ext, slot, c0; const __nv_bfloat16* trow; };   // a tile that has been looked at
+        struct Block { uint4 f[Kind::EACH]; };
+        int id[H];
+        auto ids = [&](int tile) {
             const int mt = tile / p.tiles_c;
 #pragma unroll
             for (int h = 0; h < H; ++h) {
                 const int m = mt * tile_m + h * AP_TILE + bt;
-                to[h] = tile < p.tiles && m < p.rows.M ? __ldcg(p.row_id + m) : ROW_NONE;
+                id[h] = tile < p.tiles && m < p.rows.M ? __ldcg(p.row_id + m) : ROW_NONE;
             }
         };
-        grid_dependency_wait();                                                // the rows' adapters, and t, are the kernel's in front
-        ids(unit, id);
-        const int cpr = ROWS ? cols >> 3 : 4;                                  // 16-byte pieces of a row of a block
-        const int cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
-        for (int tile = unit; tile < p.tiles && ok; tile += units, ++it) {
-            const int ib = it & 1;
-            const int mt = tile / p.tiles_c, ct = tile - mt * p.tiles_c, c0 = ct * p.nt;
-            const int m = mt * tile_m + (int)rank * AP_TILE + bt;
-            ids(tile + units, next);                                           // on their way while this tile's blocks are built
-            const bool free_now = mbar_wait(&sh.iempty[ib], ((it >> 1) & 1) ^ 1, abort_flag);
+        ApInfo info;
+        // looks at a tile, whose rows' adapters are in id[], and tells the others; false: a wait ran out
+        auto open = [&](int tile, int it, Opened& o) {
+            const int mt = tile / p.tiles_c, ct = tile - mt * p.tiles_c;
+            o.it = it;
+            o.at = info.at;
+            o.c0 = ct * p.nt;
+            const bool free_now = mbar_wait(&sh.iempty[info.at], info.use ^ 1, abort_flag);
             if (!free_now) give_up(87, tile);
-            if (builders_any(!free_now)) break;
+            if (builders_any(!free_now)) return false;
             if (p.flags & DR_BIAS)
-                for (int c = bt; c < p.nt; c += 128) sh.bias[ib][c] = c0 + c < p.C ? __ldg(p.bias + c0 + c) : 0.f;
+                for (int c = bt; c < p.nt; c += 128) sh.bias[info.at][c] = o.c0 + c < p.C ? __ldg(p.bias + o.c0 + c) : 0.f;
             int slots[H];
-            const int used = ap_find(sh.find, sh.list[ib], id, slots, bt);
-            const int slot = slots[PAIR ? rank : 0], ext = used * p.Rp;
-            sh.slot[ib][bt] = slot;
-            if (bt == 0) sh.ext[ib] = ext;
-            builders_sync();                            // the list stands; and no one still reads what the next tile's search clears
-            mbar_arrive(&sh.ifull[ib]);
-            if (it == 0) advance(p.kblocks);
-            const __nv_bfloat16* const trow = p.t + (size_t)m * p.t_terms * p.Rp;
-#pragma unroll 1
-            for (int e0 = 0; e0 < ext; e0 += WIDTH) {
-                uint4 fv[8], tv[WIDTH / 8][TERMS];
-                const int w = min(WIDTH, ext - e0);
-                ap_load_f<Kind>(p, sh.list[ib], e0, w, cols, row0, step, cj, [&](int i) { return c0 + column(i); }, fv);
-                ap_load_t<Kind>(trow, slot, p.Rp, e0, w, tv);
-                if (any_odd(fv)) {
+            o.ext = ap_find(sh.find, sh.list[info.at], id, slots, bt) * p.Rp;
+            o.slot = slots[PAIR ? rank : 0];
+            o.trow = p.t + (size_t)(mt * tile_m + (int)rank * AP_TILE + bt) * p.t_terms * p.Rp;
+            sh.slot[info.at][bt] = o.slot;
+            if (bt == 0) sh.ext[info.at] = o.ext;
+            ids(tile + units);                          // the next tile's on their way
+            builders_sync();                            // the list stands; and no one still reads what the next search clears
+            mbar_arrive(&sh.ifull[info.at]);
+            info.next();
+            return true;
+        };
+        auto load = [&](const Opened& o, int e0, Block& k) {
+            const int w = min(WIDTH, o.ext - e0);
+            ap_load_f<Kind>(p, sh.list[o.at], e0, w, cols, row0, step, cj, [&](int i) { return o.c0 + column(i); }, k.f);
+        };
+        int s = 0;
+        uint32_t ph = 0;
+        auto advance = [&](int n) {
+            s += n;
+            while (s >= p.stages) { s -= p.stages; ph ^= 1; }
+        };
+        auto store = [&](const Opened& o, int e0, Block& k, const uint4 (&tv)[WIDTH / 8][TERMS]) {
+            if (any_odd(k.f)) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) fv[i] = make_uint4(finite_halves(fv[i].x), finite_halves(fv[i].y), finite_halves(fv[i].z), finite_halves(fv[i].w));
-                    // Both CTAs of a pair drain all columns: each is told.  The number only grows, so that a CTA that runs ahead hides nothing
-                    // from one behind; a number ahead of a tile's costs that tile a search for entries it does not have.
-                    if (PAIR) {
-                        for (uint32_t k = 0; k < 2; ++k)
-                            asm volatile("red.relaxed.cluster.shared::cluster.max.s32 [%0], %1;" ::"r"(mapa_shared(smem_u32(&sh.odd[ib]), k)), "r"(it + 1) : "memory");
-                    } else {
-                        atomicMax(&sh.odd[ib], it + 1);
-                    }
+                for (int i = 0; i < Kind::EACH; ++i) k.f[i] = make_uint4(finite_halves(k.f[i].x), finite_halves(k.f[i].y), finite_halves(k.f[i].z), finite_halves(k.f[i].w));
+                // Both CTAs of a pair drain all columns: each is told.  The number only grows, so that a CTA that runs ahead hides nothing
+                // from one behind; a number ahead of a tile's costs that tile a search for entries it does not have.
+                if (PAIR) {
+                    for (uint32_t c = 0; c < 2; ++c)
+                        asm volatile("red.relaxed.cluster.shared::cluster.max.s32 [%0], %1;" ::"r"(mapa_shared(smem_u32(&sh.odd[o.at]), c)), "r"(o.it + 1) : "memory");
+                } else {
+                    atomicMax(&sh.odd[o.at], o.it + 1);
                 }
-                const int before = it == 0 ? 0 : it - 1;        // the tile whose loads lie in front of this block
-                const bool slot_free = __all_sync(0xffffffffu, mbar_wait(&sh.loads[before & 1], (before >> 1) & 1, abort_flag) &&
-                                                                   mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag));
-                if (!slot_free) give_up(88, tile);
-                if (slot_free) {
-                    const uint32_t a = ring + (uint32_t)s * p.stage_bytes;
-                    ap_store_block<Kind>(a, a + p.a_bytes, bt, true, w, cols, row0, step, cj, fv, tv);
-                }
-                fence_proxy_async_smem();
-                if (builders_any(!slot_free)) { ok = false; break; }
-                if (bt == 0) {
-                    if (PAIR) mbar_arrive_leader(&sh.full[s]);
-                    else mbar_arrive(&sh.full[s]);
-                }
-                advance(1);
             }
-            if (bt == 0) mbar_arrive(&sh.built[ib]);
+            const int before = o.it == 0 ? 0 : o.it - 1;                       // the tile whose loads lie in front of this block
+            const bool slot_free = __all_sync(0xffffffffu, mbar_wait(&sh.loads[before % 3], (uint32_t)(before / 3) & 1, abort_flag) && mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag));
+            if (!slot_free) give_up(88, o.it);
+            if (slot_free) {
+                const uint32_t a = ring + (uint32_t)s * p.stage_bytes;
+                ap_store_block<Kind>(a, a + p.a_bytes, bt, true, min(WIDTH, o.ext - e0), cols, row0, step, cj, k.f, tv);
+            }
+            fence_proxy_async_smem();
+            if (builders_any(!slot_free)) return false;
+            if (bt == 0) {
+                if (PAIR) mbar_arrive_leader(&sh.full[s]);
+                else mbar_arrive(&sh.full[s]);
+            }
+            advance(1);
+            return true;
+        };
+        grid_dependency_wait();                                                // the rows' adapters, and t, are the kernel's in front
+        ids(unit);
+        Opened now, then;
+        Block block, ahead;
+        bool ok = unit < p.tiles && open(unit, 0, now);
+        if (ok && Kind::AHEAD && now.ext > 0) load(now, 0, block);
+        for (int tile = unit, it = 0; ok && tile < p.tiles; tile += units, ++it) {
+            if (it == 0) advance(p.kblocks);
+            // With AHEAD the next block's loads, of this tile or of the next, go out before this one is stored
+            const bool more = tile + units < p.tiles;
+            then.ext = 0;
+            bool opened = false;
+#pragma unroll 1
+            for (int e0 = 0; ok && e0 < now.ext; e0 += WIDTH) {
+                uint4 tv[WIDTH / 8][TERMS];
+                ap_load_t<Kind>(now.trow, now.slot, p.Rp, e0, min(WIDTH, now.ext - e0), tv);
+                if (!Kind::AHEAD) {
+                    load(now, e0, block);
+                } else if (e0 + WIDTH < now.ext) {
+                    load(now, e0 + WIDTH, ahead);
+                } else if (more) {
+                    ok = open(tile + units, it + 1, then);
+                    opened = true;
+                    if (ok && then.ext > 0) load(then, 0, ahead);
+                }
+                ok = ok && store(now, e0, block, tv);
+                if (Kind::AHEAD) block = ahead;
+            }
+            if (!ok) break;
+            if (bt == 0) mbar_arrive(&sh.built[now.at]);
             if (it > 0) advance(p.kblocks);
-#pragma unroll
-            for (int h = 0; h < H; ++h) id[h] = next[h];
+            if (more && !opened) {
+                ok = open(tile + units, it + 1, then);
+                if (ok && Kind::AHEAD && then.ext > 0) load(then, 0, block);
+            }
+            now = then;
         }
     } else if (warp >= 4) {
         // ---------------------------------------------------------------- drain: two warps to a quarter of the rows, every other 128 bytes of columns each
@@ -526,11 +574,12 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
         const unsigned long long off = DUAL ? drop_offset(p.key) : 0ull;
         int it = 0;
         bool ok = true;
-        for (int tile = unit; tile < p.tiles && ok; tile += units, ++it) {
-            const int ib = it & 1;
+        ApInfo info;
+        for (int tile = unit; tile < p.tiles && ok; tile += units, ++it, info.next()) {
+            const int ib = info.at;
             const int mt = tile / p.tiles_c, ct = tile - mt * p.tiles_c;
             const int n0 = ct * p.nt, n_here = min(p.nt, p.C - n0);
-            if (!__all_sync(0xffffffffu, mbar_wait(&sh.ifull[ib], (it >> 1) & 1, abort_flag))) { give_up(89, tile); break; }
+            if (!__all_sync(0xffffffffu, mbar_wait(&sh.ifull[ib], info.use, abort_flag))) { give_up(89, tile); break; }
             const int slot = sh.slot[ib][q * 32 + lane];
             const unsigned valid = __ballot_sync(0xffffffffu, slot != ROW_NONE);
             const int mw = mt * tile_m + (int)rank * AP_TILE + q * 32, m = mw + lane;
@@ -540,7 +589,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
             const uint32_t quarter = (uint32_t)(q * 32) << 16;
 #pragma unroll 1
             for (int part = 0; part < (WIDE ? 2 : 1); ++part) {
-                const int ab = WIDE ? part : ib, use = WIDE ? it : it >> 1;
+                const int ab = WIDE ? part : it & 1, use = WIDE ? it : it >> 1;
                 if (!__all_sync(0xffffffffu, mbar_wait(&sh.tfull[ab], use & 1, abort_flag))) { give_up(90, tile); ok = false; break; }
                 tc_fence_after();
                 const bool odd = *(volatile int*)&sh.odd[ib] > it;
