@@ -36,7 +36,7 @@ struct ForwardPlan {
 };
 static ForwardPlan forward_plan(const dr_adapter_desc* d, int M, int ldx, int segments) {
     ForwardPlan f;
-    f.down = adapter_down_plan(M, d->Cin, d->rank, d->adapters, segments);
+    f.down = adapter_down_plan(M, d->Cin, d->rank, d->adapters, segments, d->drop_p > 0.f);
     f.Kp = up8(d->Cin);
     f.Rp = up8(d->rank);
     f.copy_k = d->Cin & 7;
@@ -61,7 +61,7 @@ struct BackwardPlan {
 };
 static BackwardPlan backward_plan(const dr_adapter_desc* d, int M, int ldx, int lddy, int segments) {
     BackwardPlan f;
-    f.down = adapter_down_plan(M, d->Cout, d->rank, d->adapters, segments);
+    f.down = adapter_down_plan(M, d->Cout, d->rank, d->adapters, segments, false);
     const int C[2] = {d->Cin, d->Cout};
     f.grad = adapter_grad_plan(M, d->rank, d->adapters, C);
     f.Kp = up8(d->Cin);

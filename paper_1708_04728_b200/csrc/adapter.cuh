@@ -64,6 +64,68 @@ __device__ __forceinline__ int adapter_of_warp_row(const AdRows& r, int m0, int 
     return m >= r.M ? ROW_NONE : adapter_of_count(r, count);
 }
 
+// ---- the adapters of a tile of rows, by 128 threads (barrier 1; bt their number) ---------------------------------------------
+__device__ __forceinline__ void builders_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// the same, and whether any of them says so: they leave together or not at all, since this barrier has no limit
+__device__ __forceinline__ bool builders_any(bool v) {
+    uint32_t r;
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbar.red.or.pred p, 1, 128, q;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(r) : "r"((uint32_t)v) : "memory");
+    return r != 0;
+}
+struct ApFind {
+    int lowest[4], highest[4];
+    uint32_t bits[128];
+    int before[128];
+    int sums[4];
+};
+// The adapters in use among the rows whose adapters id[] are (N of them a thread): their list in ascending order, this thread's places in it (or id
+// itself where that is none), and how many there are.
+template <int N>
+__device__ __forceinline__ int ap_find(ApFind& f, uint16_t* list, const int (&id)[N], int (&slot)[N], int bt) {
+    const int lane = bt & 31, w = bt >> 5;
+    int lo = 0x7fffffff, hi = -1;
+#pragma unroll
+    for (int h = 0; h < N; ++h) {
+        lo = min(lo, id[h] >= 0 ? id[h] : 0x7fffffff);
+        hi = max(hi, id[h]);
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) { f.lowest[w] = lo; f.highest[w] = hi; }
+    f.bits[bt] = 0;
+    builders_sync();
+    lo = min(min(f.lowest[0], f.lowest[1]), min(f.lowest[2], f.lowest[3]));
+    hi = max(max(f.highest[0], f.highest[1]), max(f.highest[2], f.highest[3]));
+    if (hi < 0 || lo == hi) {                       // none, or one: most tiles
+        if (bt == 0) list[0] = (uint16_t)max(hi, 0);
+#pragma unroll
+        for (int h = 0; h < N; ++h) slot[h] = id[h] >= 0 ? 0 : id[h];
+        return hi < 0 ? 0 : 1;
+    }
+#pragma unroll
+    for (int h = 0; h < N; ++h)
+        if (id[h] >= 0) atomicOr(&f.bits[id[h] >> 5], 1u << (id[h] & 31));
+    builders_sync();
+    const uint32_t word = f.bits[bt];
+    const int n = __popc(word);
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) f.sums[w] = incl;
+    builders_sync();
+    int at = incl - n;
+    for (int k = 0; k < w; ++k) at += f.sums[k];
+    f.before[bt] = at;
+    for (uint32_t x = word; x; x &= x - 1) list[at++] = (uint16_t)(bt * 32 + __ffs(x) - 1);
+    builders_sync();
+#pragma unroll
+    for (int h = 0; h < N; ++h) slot[h] = id[h] >= 0 ? f.before[id[h] >> 5] + __popc(f.bits[id[h] >> 5] & ((1u << (id[h] & 31)) - 1u)) : id[h];
+    return f.sums[0] + f.sums[1] + f.sums[2] + f.sums[3];
+}
+
 // Which of 8 consecutive elements, the first with number e, are kept: bit i for element e + i.
 __device__ __forceinline__ uint32_t drop_bits8(const DropKey& k, unsigned long long off, unsigned long long counter) {
     const uint4 w = drop_words(k, off, counter);
@@ -103,8 +165,8 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t&
 // t[m][r] = factor * sum_l D(z)[m][l] f_a[r][l], f [adapters * R][ldf] with 16-byte aligned rows and zeros behind L.  Written: in keep t itself, in rows
 // of R (may be nullptr; zeros where a row has no adapter, nothing where it has no request); in out the bfloat16 terms of T = scale_a after t, [M][terms][Rp];
 // in row_id each row's adapter
-struct DownPlan { int mt, warps_k, rows_cta, ks, zsplit, rt, rchunks; };
-DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments);
+struct DownPlan { int mt, warps_k, rows_cta, ks, zsplit, rt, rchunks; bool tile; };
+DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments, bool dropped);
 int adapter_down_run(const DownPlan& plan, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
                      const DropKey& key, float factor, const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, cudaStream_t s);
 

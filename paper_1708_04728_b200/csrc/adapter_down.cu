@@ -9,6 +9,7 @@
 #include <algorithm>
 
 #include "adapter.cuh"
+#include "conv_common.cuh"
 #include "umma_ptx.cuh"
 
 namespace dr {
@@ -179,8 +180,202 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
     }
 }
 
-DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments) {
+// ---- many rows, long l, ranks over 16, requests of many rows --------------------------------------------------------------------------------
+// The same product on tcgen05: a CTA takes 128 rows, z and the adapter's rows come by TMA into a ring, the accumulator (128 x rank) lies in TMEM.  Rows
+// of several adapters: the product is run once for each.  The tensor cores cut their sums off instead of rounding them, so 512 l are summed at a time
+// and the drain adds those up in float32 (all 4096 at once: 5e-6 of a gradient built on them, so 7e-7).  16384 x 4096, rank 64: TODO us, with fragments
+// from memory 82 (every 32 rows read all of an adapter).
+constexpr int DT_THREADS = 192, DT_STAGES = 4;         // warp 0 loads, 1 issues MMAs, 2-5 find the adapters and drain; two CTAs to an SM
+constexpr int DT_CHAIN = 8;                            // blocks of 64 l
+
+struct DownTileParams {
+    AdRows rows;
+    int L, R, Rp, n, kblocks, terms;
+    float factor, after;
+    const float* scale;
+    __nv_bfloat16* out;
+    float* keep;
+    int* row_id;
+    int* status;
+};
+struct DownTileShared {
+    uint64_t full[DT_STAGES], empty[DT_STAGES], tfull[2], tempty[2], found;
+    uint32_t tmem;
+    int abort, used;
+    uint16_t list[128];
+    ApFind find;
+};
+
+__global__ void __launch_bounds__(DT_THREADS, 2)
+adapter_down_tile_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_f, const __grid_constant__ DownTileParams p) {
+    using namespace ptx;
+    extern __shared__ uint8_t dt_raw[];
+    __shared__ DownTileShared sh;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const uint32_t ring = (smem_u32(dt_raw) + 1023u) & ~1023u;
+    const uint32_t stage_bytes = 16384u + (uint32_t)p.n * 128u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m0 = (int)blockIdx.x * 128, r0 = (int)blockIdx.y * 64;
+    volatile int* abort_flag = &sh.abort;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < DT_STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 4); }
+        mbar_init(&sh.found, 128);
+        sh.abort = 0;
+        fence_barrier_init();
+        prefetch_tensormap(&map_z);
+        prefetch_tensormap(&map_f);
+    }
+    if (warp == 1) { tmem_alloc(&sh.tmem, 128); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem, full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]);
+    auto give_up = [&](int site) {
+        if (!*abort_flag) report_timeout(p.status, site, (int)blockIdx.x);
+        *abort_flag = 1;
+    };
+    if (warp == 0) {
+        if (lane == 0) {
+            if (!mbar_wait(&sh.found, 0, abort_flag)) {
+                give_up(111);
+            } else {
+                int s = 0;
+                uint32_t ph = 0;
+                bool ok = true;
+                for (int d = 0; d < sh.used && ok; ++d) {
+                    const int row = sh.list[d] * p.R + r0;
+                    for (int kb = 0; kb < p.kblocks; ++kb) {
+                        if (!mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag)) { give_up(112); ok = false; break; }
+                        const uint32_t a = ring + (uint32_t)s * stage_bytes, bar = full0 + 8 * s;
+                        mbar_expect_tx_u32(bar, stage_bytes);
+                        tma_load_2d_u32<false>(a, &map_z, bar, kb << 6, m0, 1u);
+                        tma_load_2d_u32<false>(a + 16384u, &map_f, bar, kb << 6, row, 1u);
+                        if (++s == DT_STAGES) { s = 0; ph ^= 1; }
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            if (!mbar_wait(&sh.found, 0, abort_flag)) {
+                give_up(113);
+            } else {
+                const uint32_t idesc = make_idesc_bf16(128, p.n);
+                const int tail16 = ((p.L - ((p.kblocks - 1) << 6)) + 15) >> 4;
+                int s = 0;
+                uint32_t ph = 0;
+                bool ok = true;
+                for (int d = 0, n = 0; d < sh.used && ok; ++d) {
+                    for (int k0 = 0; k0 < p.kblocks && ok; k0 += DT_CHAIN, ++n) {
+                        if (!mbar_wait(&sh.tempty[n & 1], (uint32_t)((n >> 1) & 1) ^ 1, abort_flag)) { give_up(114); ok = false; break; }
+                        tc_fence_after();
+                        for (int kb = k0; kb < min(p.kblocks, k0 + DT_CHAIN); ++kb) {
+                            if (!mbar_wait_u32(full0 + 8 * s, ph, abort_flag)) { give_up(115); ok = false; break; }
+                            tc_fence_after();
+                            const uint32_t a = sdesc_lo(ring + (uint32_t)s * stage_bytes), b = sdesc_lo(ring + (uint32_t)s * stage_bytes + 16384u);
+                            const int n16 = kb == p.kblocks - 1 ? tail16 : 4;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) umma_bf16_lo<false>(tmem + 64u * (n & 1), a + 2 * k, b + 2 * k, idesc, kb > k0 || k ? 1u : 0u, k < n16 ? 1u : 0u);
+                            umma_commit_u32<false>(empty0 + 8 * s);
+                            if (++s == DT_STAGES) { s = 0; ph ^= 1; }
+                        }
+                        umma_commit(&sh.tfull[n & 1]);
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------------- a thread to a row: TMEM lanes 32 (warp mod 4) + lane
+        const int q = warp & 3, row = 32 * q + lane, m = m0 + row;
+        int id[1] = {adapter_of_warp_row(p.rows, m0 + 32 * q, lane)}, slot[1];
+        if (m < p.rows.M && p.row_id && r0 == 0) p.row_id[m] = id[0];
+        const int used = ap_find(sh.find, sh.list, id, slot, (int)threadIdx.x - 64);
+        if (threadIdx.x == 64) sh.used = used;
+        builders_sync();
+        mbar_arrive(&sh.found);
+        const float scale = (id[0] >= 0 && p.scale ? __ldg(p.scale + id[0]) : 1.f) * p.after;
+        const int rn = min(64, p.Rp - r0);
+        if (p.keep && id[0] == ROW_SHARED)
+            for (int r = r0; r < min(p.R, r0 + 64); ++r) p.keep[(size_t)m * p.R + r] = 0.f;
+        float sum[8][8];
+        bool ok = true;
+        for (int d = 0, n = 0; d < used && ok; ++d) {
+#pragma unroll
+            for (int b = 0; b < 8; ++b)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[b][i] = 0.f;
+            for (int k0 = 0; k0 < p.kblocks; k0 += DT_CHAIN, ++n) {
+                if (!__all_sync(0xffffffffu, mbar_wait(&sh.tfull[n & 1], (uint32_t)(n >> 1) & 1, abort_flag))) { give_up(116); ok = false; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int b = 0; b < 8; ++b) {
+                    if (8 * b >= rn) break;
+                    uint32_t v[8];
+                    tmem_ld_x8(tmem + 64u * (n & 1) + 8 * b + ((uint32_t)(q * 32) << 16), v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[b][i] += __uint_as_float(v[i]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.tempty[n & 1]);
+            }
+            if (!ok || slot[0] != d) continue;
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                const int r = r0 + 8 * b;
+                if (8 * b >= rn) break;
+                float t[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[i] = r + i < p.R ? sum[b][i] * p.factor : 0.f;      // columns behind the rank are the next adapter's
+                if (p.keep) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) if (r + i < p.R) p.keep[(size_t)m * p.R + r + i] = t[i];
+                }
+                uint32_t u[3][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) split3(t[2 * i] * scale, t[2 * i + 1] * scale, u[0][i], u[1][i], u[2][i]);
+                __nv_bfloat16* to = p.out + (size_t)m * p.terms * p.Rp + r;
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    if (k < p.terms) *reinterpret_cast<uint4*>(to + (size_t)k * p.Rp) = make_uint4(u[k][0], u[k][1], u[k][2], u[k][3]);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, 128);
+}
+
+static int down_tile_run(const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf, float factor,
+                         const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, cudaStream_t s) {
+    DownTileParams p = {rows, L, R, Rp, R >= 64 ? 64 : (R + 15) / 16 * 16, (L + 63) / 64, terms, factor, after, scale, out, keep, row_id, dev_status_ptr()};
+    alignas(64) CUtensorMap mz, mf;
+    auto map = [](CUtensorMap* m, const void* ptr, size_t n, int cols, size_t ld, int box_rows) {
+        const cuuint64_t dims[2] = {(cuuint64_t)cols, n}, strides[1] = {ld * 2};
+        const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+        return tmap_tiled(m, 2, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+    };
+    int rc = map(&mz, z, rows.M, L, ldz, 128);
+    if (rc == DR_OK) rc = map(&mf, f, (size_t)rows.adapters * R, L, ldf, p.n);
+    if (rc != DR_OK) return rc;
+    const int smem = 1024 + DT_STAGES * (16384 + p.n * 128);
+    static PerDeviceFlag ready;
+    if (!ready.get()) {
+        if (cudaFuncSetAttribute(adapter_down_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 1024 + DT_STAGES * (16384 + 64 * 128)) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+        ready.set();
+    }
+    adapter_down_tile_kernel<<<dim3((unsigned)((rows.M + 127) / 128), (unsigned)((R + 63) / 64)), DT_THREADS, smem, s>>>(mz, mf, p);
+    count_launch();
+    return launch_status();
+}
+
+DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments, bool dropped) {
     DownPlan d = {};
+    // Tiles of 128 rows nearly for every SM, of mostly one adapter each, and enough l and columns that a tile's start does not show
+    d.tile = !dropped && M >= 96 * num_sms() && M >= 128ll * segments && L >= 512 && R > 16;
     d.rt = R <= 8 ? 1 : R <= 16 ? 2 : R <= 32 ? 4 : 8;
     d.rchunks = (R + 8 * d.rt - 1) / (8 * d.rt);
     const int sms = num_sms();
@@ -224,6 +419,7 @@ static int down_launch_rt(const DownPlan& d, const DownParams& p, cudaStream_t s
 
 int adapter_down_run(const DownPlan& d, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
                      const DropKey& key, float factor, const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, cudaStream_t s) {
+    if (d.tile) return down_tile_run(rows, L, R, Rp, z, ldz, f, ldf, factor, scale, after, terms, out, keep, row_id, s);
     DownParams p;
     p.rows = rows;
     p.L = L; p.L8 = (L + 7) / 8 * 8; p.R = R; p.Rp = Rp; p.ks = d.ks; p.zsplit = d.zsplit;

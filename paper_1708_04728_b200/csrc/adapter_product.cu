@@ -56,12 +56,6 @@ struct ApParams {
     int* status;
 };
 
-struct ApFind {
-    int lowest[4], highest[4];
-    uint32_t bits[128];
-    int before[128];
-    int sums[4];
-};
 struct ApShared {
     uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], tfull[2], tempty[2], ifull[3], iempty[3], loads[3], built[3];
     uint32_t tmem;
@@ -83,13 +77,6 @@ struct ApInfo {
 
 __device__ __forceinline__ uint32_t sdesc_rows_lo(uint32_t smem_addr, uint32_t box) {    // contraction index = row of a 64-column box
     return ((smem_addr & 0x3FFFFu) >> 4) | (((box >> 4) & 0x3FFFu) << 16);
-}
-__device__ __forceinline__ void builders_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-// the same, and whether any of them says so: they leave together or not at all, since this barrier has no limit
-__device__ __forceinline__ bool builders_any(bool v) {
-    uint32_t r;
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbar.red.or.pred p, 1, 128, q;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(r) : "r"((uint32_t)v) : "memory");
-    return r != 0;
 }
 __device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
@@ -127,54 +114,6 @@ struct ApKind {
 };
 
 // ---- the builders' steps (128 threads, bt their number) --------------------------------------------------------------------
-// The adapters in use among the rows whose adapters id[] are (N of them a thread): their list in ascending order, this thread's places in it (or id
-// itself where that is none), and how many there are.
-template <int N>
-__device__ __forceinline__ int ap_find(ApFind& f, uint16_t* list, const int (&id)[N], int (&slot)[N], int bt) {
-    const int lane = bt & 31, w = bt >> 5;
-    int lo = 0x7fffffff, hi = -1;
-#pragma unroll
-    for (int h = 0; h < N; ++h) {
-        lo = min(lo, id[h] >= 0 ? id[h] : 0x7fffffff);
-        hi = max(hi, id[h]);
-    }
-    lo = __reduce_min_sync(0xffffffffu, lo);
-    hi = __reduce_max_sync(0xffffffffu, hi);
-    if (lane == 0) { f.lowest[w] = lo; f.highest[w] = hi; }
-    f.bits[bt] = 0;
-    builders_sync();
-    lo = min(min(f.lowest[0], f.lowest[1]), min(f.lowest[2], f.lowest[3]));
-    hi = max(max(f.highest[0], f.highest[1]), max(f.highest[2], f.highest[3]));
-    if (hi < 0 || lo == hi) {                       // none, or one: most tiles
-        if (bt == 0) list[0] = (uint16_t)max(hi, 0);
-#pragma unroll
-        for (int h = 0; h < N; ++h) slot[h] = id[h] >= 0 ? 0 : id[h];
-        return hi < 0 ? 0 : 1;
-    }
-#pragma unroll
-    for (int h = 0; h < N; ++h)
-        if (id[h] >= 0) atomicOr(&f.bits[id[h] >> 5], 1u << (id[h] & 31));
-    builders_sync();
-    const uint32_t word = f.bits[bt];
-    const int n = __popc(word);
-    int incl = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
-    }
-    if (lane == 31) f.sums[w] = incl;
-    builders_sync();
-    int at = incl - n;
-    for (int k = 0; k < w; ++k) at += f.sums[k];
-    f.before[bt] = at;
-    for (uint32_t x = word; x; x &= x - 1) list[at++] = (uint16_t)(bt * 32 + __ffs(x) - 1);
-    builders_sync();
-#pragma unroll
-    for (int h = 0; h < N; ++h) slot[h] = id[h] >= 0 ? f.before[id[h] >> 5] + __popc(f.bits[id[h] >> 5] & ((1u << (id[h] & 31)) - 1u)) : id[h];
-    return f.sums[0] + f.sums[1] + f.sums[2] + f.sums[3];
-}
-
 // eight values of a row whose rank leaves them no alignment, zeros behind the last
 __device__ __noinline__ uint4 ap_odd_rank(const __nv_bfloat16* src, int n) {
     uint32_t u[4];
@@ -599,10 +538,15 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 for (int c = side * CHUNK; c < c_end; c += 2 * CHUNK) {
                     if (lane == 0) tma_store_wait_read();                      // the box in front has been read
                     __syncwarp();
-#pragma unroll 1
-                    for (int h = 0; h < CHUNK; h += 32) {                      // rolled: what runs here has to stay in the instruction cache
-                        uint32_t v[32];
-                        tmem_ld_x32(acc + c + h, v);
+                    uint32_t w[DUAL ? 1 : CHUNK / 32][32];
+                    if (!DUAL) {
+#pragma unroll
+                        for (int h = 0; h < CHUNK / 32; ++h) tmem_ld_x32(acc + c + 32 * h, w[h % (DUAL ? 1 : CHUNK / 32)]);
+                    }
+#pragma unroll(DUAL ? 1 : CHUNK / 32)
+                    for (int h = 0; h < CHUNK; h += 32) {                      // rolled with a generator in it: the code has to stay in the instruction cache
+                        uint32_t (&v)[32] = w[DUAL ? 0 : h / 32];
+                        if (DUAL) tmem_ld_x32(acc + c + h, v);
                         if (DUAL) {
                             uint32_t bits = 0;
                             const unsigned long long e = (unsigned long long)m * p.C + n0 + c + h;

@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(256) dropout_vec_kernel(const DropParams p) {
 // Any other rows: a warp takes 256 neighbouring elements.  Each lane draws a vector's mask, and gets the bits of the elements it moves (lane, lane + 32,
 // ...: whole lines of memory) from the lanes that drew them.
 template <typename TX, typename TY, bool RES>
-__global__ void __launch_bounds__(256) dropout_any_kernel(const DropParams p) {
+__global__ void __launch_bounds__(256, 6) dropout_any_kernel(const DropParams p) {
     const unsigned long long off = drop_offset(p.key);
     const int lane = threadIdx.x & 31;
     const unsigned long long stride = (unsigned long long)gridDim.x * 8 * 256;
@@ -115,18 +115,24 @@ __global__ void __launch_bounds__(256) dropout_any_kernel(const DropParams p) {
     size_t row = e / p.C;
     int col = (int)(e - row * p.C);
     for (; e < p.n; e += stride) {
+        // places are kept as the row's own pointer and 32 bits: few registers, and so many warps, hide the memory's latency here
+        const TX* const xr = (const TX*)p.x + row * p.ldx;
+        const TY* const rr = (const TY*)p.r + (RES ? row * p.ldr : 0);
+        TY* const yr = (TY*)p.y + row * p.ldy;
+        const int left = (int)min(p.n - e, 256ull);
+        auto split = [&](int k, uint32_t& over) {                              // column and rows passed of element 32 k + lane
+            const uint32_t c = (uint32_t)col + 32 * k + lane;
+            over = p.C >= 256 ? (c >= (uint32_t)p.C ? 1u : 0u) : p.C == 1 ? c : __umulhi(c, p.magic);
+            return c - over * (uint32_t)p.C;
+        };
         float x[8], r[8];
-        size_t at[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const uint32_t c = (uint32_t)col + 32 * k + lane;
-            const uint32_t over = p.C >= 256 ? (c >= (uint32_t)p.C ? 1u : 0u) : p.C == 1 ? c : __umulhi(c, p.magic);    // rows passed
-            const size_t m = row + over;
-            const uint32_t cc = c - over * (uint32_t)p.C;
-            at[k] = m * p.ldy + cc;
-            if (e + 32 * k + lane < p.n) {
-                x[k] = drop_ld<TX>(p.x, m * p.ldx + cc);
-                if (RES) r[k] = drop_ld<TY>(p.r, m * p.ldr + cc);
+            uint32_t over;
+            const uint32_t c = split(k, over);
+            if (32 * k + lane < left) {
+                x[k] = drop_ld<TX>(xr + (size_t)over * p.ldx, c);
+                if (RES) r[k] = drop_ld<TY>(rr + (size_t)over * p.ldr, c);
             }
         }
         const uint4 w = drop_words(p.key, off, (e >> 3) + lane);
@@ -135,9 +141,11 @@ __global__ void __launch_bounds__(256) dropout_any_kernel(const DropParams p) {
         for (int c = 0; c < 8; ++c) bits |= drop_keep(w, c, p.key.thr) ? 1u << c : 0u;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
+            uint32_t over;
+            const uint32_t c = split(k, over);
             const uint32_t b = __shfl_sync(0xffffffffu, bits, 4 * k + (lane >> 3)) >> (lane & 7);
             const float v = (b & 1) ? x[k] * p.key.scale : 0.f;
-            if (e + 32 * k + lane < p.n) drop_st((TY*)p.y + at[k], RES ? r[k] + v : v);
+            if (32 * k + lane < left) drop_st(yr + (size_t)over * p.ldy + c, RES ? r[k] + v : v);
         }
         row += p.step_row;
         col += p.step_col;

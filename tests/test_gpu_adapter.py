@@ -253,6 +253,17 @@ def test_what_is_not_finite_stays_with_its_request(dr, M, bad):
         assert np.allclose(gy[clean], y[clean], rtol=1e-4, atol=1e-3)
 
 
+@pytest.mark.parametrize("M,K,N,R,adapters,kind,p", [
+    (14300, 520, 72, 24, 3, "ragged", 0.0), (14299, 576, 40, 130, 2, "inner", 0.0), (14336, 512, 520, 64, 5, "even", 0.0), (19000, 64, 256, 8, 4, "even", 0.0),
+    (38100, 72, 24, 16, 3, "ragged", 0.1), (20000, 1024, 512, 8, 2, "one", 0.0), (9500, 136, 264, 16, 90, "ragged", 0.2)])
+def test_many_rows(dr, M, K, N, R, adapters, kind, p):
+    """The kernels for many rows: tiles on tensor cores for the first product, pairs of CTAs and pairs with two accumulators for the second, shares of rows that end
+    inside an adapter for the gradients."""
+    c = Case(M, K, N, R, adapters, kind)
+    check_forward(dr, c, p=p, relu=R == 24, f32=R == 64)
+    check_backward(dr, c, p=p)
+
+
 def test_same_on_every_run(dr):
     for M, kind in ((40, "rows"), (700, "ragged"), (3000, "one")):
         c = Case(M, 136, 200, 16, 5, kind)
