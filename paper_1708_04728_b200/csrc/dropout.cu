@@ -106,46 +106,44 @@ __global__ void __launch_bounds__(256) dropout_vec_kernel(const DropParams p) {
 
 // Any other rows: a warp takes 256 neighbouring elements.  Each lane draws a vector's mask, and gets the bits of the elements it moves (lane, lane + 32,
 // ...: whole lines of memory) from the lanes that drew them.
-template <typename TX, typename TY, bool RES>
-__global__ void __launch_bounds__(256, 6) dropout_any_kernel(const DropParams p) {
+// The issue slots bound it, so places are 32 bits from the row's start, and a row of 256 or more elements (NARROW false) ends at most once in them.
+template <typename TX, typename TY, bool RES, bool NARROW>
+__global__ void __launch_bounds__(256) dropout_any_kernel(const DropParams p) {
     const unsigned long long off = drop_offset(p.key);
     const int lane = threadIdx.x & 31;
     const unsigned long long stride = (unsigned long long)gridDim.x * 8 * 256;
     unsigned long long e = ((unsigned long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * 256;
     size_t row = e / p.C;
     int col = (int)(e - row * p.C);
+    const uint32_t C = (uint32_t)p.C, gap_x = (uint32_t)(p.ldx - p.C), gap_r = (uint32_t)(p.ldr - p.C), gap_y = (uint32_t)(p.ldy - p.C);
     for (; e < p.n; e += stride) {
-        // places are kept as the row's own pointer and 32 bits: few registers, and so many warps, hide the memory's latency here
-        const TX* const xr = (const TX*)p.x + row * p.ldx;
-        const TY* const rr = (const TY*)p.r + (RES ? row * p.ldr : 0);
-        TY* const yr = (TY*)p.y + row * p.ldy;
-        const int left = (int)min(p.n - e, 256ull);
-        auto split = [&](int k, uint32_t& over) {                              // column and rows passed of element 32 k + lane
-            const uint32_t c = (uint32_t)col + 32 * k + lane;
-            over = p.C >= 256 ? (c >= (uint32_t)p.C ? 1u : 0u) : p.C == 1 ? c : __umulhi(c, p.magic);
-            return c - over * (uint32_t)p.C;
-        };
+        const TX* const x0 = (const TX*)p.x + row * p.ldx;
+        const TY* const r0 = (const TY*)p.r + (RES ? row * p.ldr : 0);
+        TY* const y0 = (TY*)p.y + row * p.ldy;
+        const uint32_t left = (uint32_t)min(p.n - e, 256ull), first = (uint32_t)col + lane;
+        // rows passed by the element `i` of the row on: what the gaps between rows count for
+        auto passed = [&](uint32_t i) { return NARROW ? (C == 1 ? i : __umulhi(i, p.magic)) : (i >= C ? 1u : 0u); };
+        auto place = [](uint32_t i, uint32_t over, uint32_t gap) { return NARROW ? i + (size_t)over * gap : (size_t)(over ? i + gap : i); };
         float x[8], r[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            uint32_t over;
-            const uint32_t c = split(k, over);
+            const uint32_t i = first + 32 * k, over = passed(i);
             if (32 * k + lane < left) {
-                x[k] = drop_ld<TX>(xr + (size_t)over * p.ldx, c);
-                if (RES) r[k] = drop_ld<TY>(rr + (size_t)over * p.ldr, c);
+                x[k] = drop_ld<TX>(x0, place(i, over, gap_x));
+                if (RES) r[k] = drop_ld<TY>(r0, place(i, over, gap_r));
             }
         }
         const uint4 w = drop_words(p.key, off, (e >> 3) + lane);
         uint32_t bits = 0;
 #pragma unroll
         for (int c = 0; c < 8; ++c) bits |= drop_keep(w, c, p.key.thr) ? 1u << c : 0u;
+        const uint32_t mine = 1u << (lane & 7);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            uint32_t over;
-            const uint32_t c = split(k, over);
-            const uint32_t b = __shfl_sync(0xffffffffu, bits, 4 * k + (lane >> 3)) >> (lane & 7);
-            const float v = (b & 1) ? x[k] * p.key.scale : 0.f;
-            if (32 * k + lane < left) drop_st(yr + (size_t)over * p.ldy + c, RES ? r[k] + v : v);
+            const uint32_t i = first + 32 * k, over = passed(i);
+            const uint32_t b = __shfl_sync(0xffffffffu, bits, 4 * k + (lane >> 3)) & mine;
+            const float v = b ? x[k] * p.key.scale : 0.f;
+            if (32 * k + lane < left) drop_st(y0 + place(i, over, gap_y), RES ? r[k] + v : v);
         }
         row += p.step_row;
         col += p.step_col;
@@ -175,7 +173,8 @@ static void drop_launch(DropParams p, cudaStream_t s) {
         p.step_row = (int)(grid * 2048ull / p.C);
         p.step_col = (int)(grid * 2048ull % p.C);
         p.magic = p.C > 1 && p.C < 256 ? (uint32_t)((0x100000000ull + p.C - 1) / p.C) : 0u;
-        dropout_any_kernel<TX, TY, RES><<<grid, 256, 0, s>>>(p);
+        if (p.C < 256) dropout_any_kernel<TX, TY, RES, true><<<grid, 256, 0, s>>>(p);
+        else dropout_any_kernel<TX, TY, RES, false><<<grid, 256, 0, s>>>(p);
     }
 }
 template <typename TX, typename TY>
