@@ -139,7 +139,7 @@ extern "C" int dr_adapter(const dr_adapter_desc* d, int M, const void* x, int ld
     if ((rc = place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, ws, f.a, &ap, &ldap, s)) != DR_OK) return rc;
     __nv_bfloat16* const tw = (__nv_bfloat16*)(ws + f.t);
     int* const ids = (int*)(ws + f.ids);
-    rc = adapter_down_run(f.down, rows, K, R, f.Rp, xp, ldxp, ap, ldap, key, key.thr ? key.scale : 1.f, scale, 1.f, f.terms, tw, t, ids, s);
+    rc = adapter_down_run(f.down, rows, K, R, f.Rp, xp, ldxp, ap, ldap, key, key.thr ? key.scale : 1.f, scale, 1.f, f.terms, tw, t, ids, false, s);
     if (rc != DR_OK) return rc;
     const ProductArgs g = {rows, K, N, R, f.Rp, xp, wp, (const __nv_bfloat16*)b, ldxp, ldwp, 0, ids, tw, f.terms, bias, d->flags, y, (size_t)ldy, false, none};
     return adapter_product_run(g, true, s);
@@ -184,14 +184,14 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     rc = adapter_prep_run(rows, grads ? (int*)(ws + f.g + f.grad.perm) : nullptr, (int*)(ws + f.g + f.grad.start), N, R, f.Rp, (const __nv_bfloat16*)b,
                           u_wanted ? bt : nullptr, f.Np, t, scale, db ? terms : nullptr, s);
     if (rc != DR_OK) return rc;
-    if (u_wanted && (rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, scale, kept, 3, u, nullptr, ids, s)) != DR_OK) return rc;
+    if (u_wanted && (rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, scale, kept, 3, u, nullptr, ids, true, s)) != DR_OK) return rc;
     if (dx) {
         const ProductArgs g = {rows, N, K, R, f.Rp, dyp, wp, ap, lddyp, ldwp, ldap, ids, u, 3, nullptr, 0, dx, (size_t)lddx, true, key};
         if ((rc = adapter_product_run(g, true, s)) != DR_OK) return rc;
     }
     if (da || db) {
         const GradJob jobs[2] = {{K, xp, ldxp, u, key, da, 0}, {N, dyp, lddyp, terms, none, db, 1}};
-        if ((rc = adapter_grad_run(f.grad, rows, R, jobs, ws + f.g, s)) != DR_OK) return rc;
+        if ((rc = adapter_grad_run(f.grad, rows, R, jobs, ws + f.g, true, s)) != DR_OK) return rc;
     }
     return DR_OK;
 }

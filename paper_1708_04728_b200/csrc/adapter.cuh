@@ -161,6 +161,34 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t&
     lo = pack_bf16(ra - bf16_lo(mid), rb - bf16_hi(mid));
 }
 
+// A launch that may begin while the kernel in front of it ends (`overlap`): it then waits for that one before it reads what it wrote, in every CTA, so
+// that what follows sees all of them complete.
+template <class Kernel, class... Args>
+static int start_kernel(Kernel k, const dim3& grid, int threads, int cluster_y, bool overlap, size_t smem, cudaStream_t s, const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (cluster_y > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = 1; attr[n].val.clusterDim.y = (unsigned)cluster_y; attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (overlap) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    if (cudaLaunchKernelEx(&cfg, k, args...) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+    count_launch();
+    return DR_OK;
+}
+
 // ---- launches (adapter_down.cu, adapter_product.cu, adapter_grad.cu) -------------------------------------------------------
 // t[m][r] = factor * sum_l D(z)[m][l] f_a[r][l], f [adapters * R][ldf] with 16-byte aligned rows and zeros behind L.  Written: in keep t itself, in rows
 // of R (may be nullptr; zeros where a row has no adapter, nothing where it has no request); in out the bfloat16 terms of T = scale_a after t, [M][terms][Rp];
@@ -168,7 +196,7 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t&
 struct DownPlan { int mt, warps_k, rows_cta, ks, zsplit, rt, rchunks; bool tile; };
 DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments, bool dropped);
 int adapter_down_run(const DownPlan& plan, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
-                     const DropKey& key, float factor, const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, cudaStream_t s);
+                     const DropKey& key, float factor, const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, bool overlap, cudaStream_t s);
 
 // out[m][c] = act(sum_l z[m][l] w + bias[c] + D(T[m] f_a)):   forward w [C][ldw] (rows of l), f [adapters][C][R];
 // transposed w [L][ldw] (rows of c), f [adapters][R][ldf]
@@ -201,7 +229,7 @@ struct GradJob {
 };
 struct GradPlan { int tiles, splits, rn, rchunks; size_t perm, start, terms, part[2], bytes; };
 GradPlan adapter_grad_plan(int M, int R, int adapters, const int C[2]);
-int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const GradJob jobs[2], char* ws, cudaStream_t s);
+int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const GradJob jobs[2], char* ws, bool overlap, cudaStream_t s);
 // in one launch, each where its result is wanted: the rows sorted by adapter (perm, start), b [adapters][N][R] turned to bt [adapters][R][ldb] with zeros
 // behind N, scale_a t as three bfloat16 values
 int adapter_prep_run(const AdRows& rows, int* perm, int* start, int N, int R, int Rp, const __nv_bfloat16* b, __nv_bfloat16* bt, size_t ldb, const float* t,

@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
     if (lane >= MT * 16) id = ROW_NONE;
     else if (p.row_id && blockIdx.y == 0 && blockIdx.z == 0 && (!JOIN || warp == 0) && m0 + lane < p.rows.M) p.row_id[m0 + lane] = id;
     const unsigned long long off = DROP ? drop_offset(p.key) : 0ull;
+    ptx::grid_dependency_wait();                                 // f may be the work of the kernel in front
 
     const __nv_bfloat16* zr[MT][2];
 #pragma unroll
@@ -236,6 +237,7 @@ adapter_down_tile_kernel(const __grid_constant__ CUtensorMap map_z, const __grid
     };
     if (warp == 0) {
         if (lane == 0) {
+            grid_dependency_wait();                              // f may be the work of the kernel in front
             if (!mbar_wait(&sh.found, 0, abort_flag)) {
                 give_up(111);
             } else {
@@ -350,7 +352,7 @@ adapter_down_tile_kernel(const __grid_constant__ CUtensorMap map_z, const __grid
 }
 
 static int down_tile_run(const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf, float factor,
-                         const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, cudaStream_t s) {
+                         const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, bool overlap, cudaStream_t s) {
     DownTileParams p = {rows, L, R, Rp, R >= 64 ? 64 : (R + 15) / 16 * 16, (L + 63) / 64, terms, factor, after, scale, out, keep, row_id, dev_status_ptr()};
     alignas(64) CUtensorMap mz, mf;
     auto map = [](CUtensorMap* m, const void* ptr, size_t n, int cols, size_t ld, int box_rows) {
@@ -367,9 +369,7 @@ static int down_tile_run(const AdRows& rows, int L, int R, int Rp, const __nv_bf
         if (cudaFuncSetAttribute(adapter_down_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 1024 + DT_STAGES * (16384 + 64 * 128)) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
         ready.set();
     }
-    adapter_down_tile_kernel<<<dim3((unsigned)((rows.M + 127) / 128), (unsigned)((R + 63) / 64)), DT_THREADS, smem, s>>>(mz, mf, p);
-    count_launch();
-    return launch_status();
+    return start_kernel(adapter_down_tile_kernel, dim3((unsigned)((rows.M + 127) / 128), (unsigned)((R + 63) / 64)), DT_THREADS, 1, overlap, smem, s, mz, mf, p);
 }
 
 DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments, bool dropped) {
@@ -396,39 +396,29 @@ DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments, bool
 }
 
 template <int MT, int RT, bool JOIN>
-static int down_launch(const DownPlan& d, const DownParams& p, cudaStream_t s) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((p.rows.M + d.rows_cta - 1) / d.rows_cta), (unsigned)d.ks, (unsigned)(d.zsplit * d.rchunks));
-    cfg.blockDim = dim3(256);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = (unsigned)d.ks; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = d.ks > 1 ? 1 : 0;
-    const cudaError_t e = p.key.thr ? cudaLaunchKernelEx(&cfg, adapter_down_kernel<MT, RT, true, JOIN>, p) : cudaLaunchKernelEx(&cfg, adapter_down_kernel<MT, RT, false, JOIN>, p);
-    if (e != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
-    count_launch();
-    return DR_OK;
+static int down_launch(const DownPlan& d, const DownParams& p, bool overlap, cudaStream_t s) {
+    const dim3 grid((unsigned)((p.rows.M + d.rows_cta - 1) / d.rows_cta), (unsigned)d.ks, (unsigned)(d.zsplit * d.rchunks));
+    return p.key.thr ? start_kernel(adapter_down_kernel<MT, RT, true, JOIN>, grid, 256, d.ks, overlap, 0, s, p)
+                     : start_kernel(adapter_down_kernel<MT, RT, false, JOIN>, grid, 256, d.ks, overlap, 0, s, p);
 }
 template <int RT>
-static int down_launch_rt(const DownPlan& d, const DownParams& p, cudaStream_t s) {
-    if (d.warps_k == 1) return down_launch<2, RT, false>(d, p, s);
-    return d.mt == 2 ? down_launch<2, RT, true>(d, p, s) : down_launch<1, RT, true>(d, p, s);
+static int down_launch_rt(const DownPlan& d, const DownParams& p, bool overlap, cudaStream_t s) {
+    if (d.warps_k == 1) return down_launch<2, RT, false>(d, p, overlap, s);
+    return d.mt == 2 ? down_launch<2, RT, true>(d, p, overlap, s) : down_launch<1, RT, true>(d, p, overlap, s);
 }
 
 int adapter_down_run(const DownPlan& d, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
-                     const DropKey& key, float factor, const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, cudaStream_t s) {
-    if (d.tile) return down_tile_run(rows, L, R, Rp, z, ldz, f, ldf, factor, scale, after, terms, out, keep, row_id, s);
+                     const DropKey& key, float factor, const float* scale, float after, int terms, __nv_bfloat16* out, float* keep, int* row_id, bool overlap, cudaStream_t s) {
+    if (d.tile) return down_tile_run(rows, L, R, Rp, z, ldz, f, ldf, factor, scale, after, terms, out, keep, row_id, overlap, s);
     DownParams p;
     p.rows = rows;
     p.L = L; p.L8 = (L + 7) / 8 * 8; p.R = R; p.Rp = Rp; p.ks = d.ks; p.zsplit = d.zsplit;
     p.l_range = (((L + d.ks - 1) / d.ks) + 63) / 64 * 64;
     p.z = z; p.f = f; p.ldz = ldz; p.ldf = ldf;
     p.key = key; p.factor = factor; p.scale = scale; p.after = after; p.terms = terms; p.out = out; p.keep = keep; p.row_id = row_id;
-    if (d.rt == 1) return down_launch_rt<1>(d, p, s);
-    if (d.rt == 2) return down_launch_rt<2>(d, p, s);
-    return d.rt == 4 ? down_launch_rt<4>(d, p, s) : down_launch_rt<8>(d, p, s);
+    if (d.rt == 1) return down_launch_rt<1>(d, p, overlap, s);
+    if (d.rt == 2) return down_launch_rt<2>(d, p, overlap, s);
+    return d.rt == 4 ? down_launch_rt<4>(d, p, overlap, s) : down_launch_rt<8>(d, p, overlap, s);
 }
 
 // ---- layouts ------------------------------------------------------------------------------------------------------

@@ -133,6 +133,7 @@ __device__ __forceinline__ void prep_terms(const PrepParams& p, int block) {
 }
 __global__ void __launch_bounds__(256) adapter_prep_kernel(const PrepParams p) {
     const int b = blockIdx.x;
+    grid_launch_dependents();
     if (b < p.sort_blocks) prep_sort(p.rows, p.perm, p.start, b);
     else if (b < p.sort_blocks + p.turn_blocks) prep_turn(p, b - p.sort_blocks);
     else prep_terms(p, b - p.sort_blocks - p.turn_blocks);
@@ -194,11 +195,16 @@ __device__ __forceinline__ uint32_t sdesc_mn(uint32_t smem_addr) { return ((smem
 
 struct GradMaps { CUtensorMap z[2][3], p[2][3]; };              // of both jobs: for gathers, boxes of 16 and of 64 rows
 
+// rows of a share: whole groups of 16 where there are many
+__device__ __forceinline__ int grad_share(int total, int splits) {
+    const int n = (total + splits - 1) / splits;
+    return n >= 64 ? (n + 15) & ~15 : n;
+}
 // Shares and adapters of a CTA, in order: calls f(adapter, first sorted row, row behind the last, whole adapter?)
 template <class F>
 __device__ __forceinline__ void grad_ranges(const GradParams& p, int split, F f) {
     const int total = min(max(__ldg(p.start + p.adapters), 0), p.M);
-    const int share = ((total + p.splits - 1) / p.splits + 15) & ~15;
+    const int share = grad_share(total, p.splits);
     const int from = min(split * share, total), to = min(from + share, total);
     if (from >= to) return;
     int lo = 0, hi = p.adapters;                       // the first adapter whose rows reach beyond `from`
@@ -239,6 +245,8 @@ adapter_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    grid_launch_dependents();
+    grid_dependency_wait();                            // the lists, u and t's terms are the work of the kernels in front
     const uint32_t tmem = sh.tmem;
     const uint32_t landed0 = smem_u32(&sh.landed[0]), full0 = smem_u32(drop ? &sh.full[0] : &sh.landed[0]), empty0 = smem_u32(&sh.empty[0]);
     auto give_up = [&](int site) {
@@ -445,10 +453,11 @@ adapter_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
 // Adapters whose rows lie in more than one share: their partial sums in order.
 __global__ void __launch_bounds__(256) adapter_grad_join_kernel(const __grid_constant__ GradParams p) {
     const GradParams::Job& j = p.job[blockIdx.z];
+    grid_dependency_wait();
     if (!j.out) return;
     const int a = blockIdx.y;
     const int total = min(max(__ldg(p.start + p.adapters), 0), p.M);
-    const int share = ((total + p.splits - 1) / p.splits + 15) & ~15;
+    const int share = grad_share(total, p.splits);
     const int u = __ldg(p.start + a), v = min(__ldg(p.start + a + 1), total);
     if (u >= v) return;
     const int s0 = u / share, s1 = (v - 1) / share;
@@ -469,8 +478,9 @@ GradPlan adapter_grad_plan(int M, int R, int adapters, const int C[2]) {
     g.rchunks = (Rp + 63) / 64;
     g.rn = g.rchunks == 1 ? Rp : 64;
     const int cols = (3 * g.rn + 31) / 32 * 32;               // of an accumulator
-    // Columns of a CTA: as many as tensor memory has room for, fewer where that leaves SMs without rows; shares of at least 256 rows
-    const int most = std::max(1, (M + 255) / 256);
+    // Columns of a CTA: as many as tensor memory has room for, fewer where that leaves SMs without rows.  Shares of at least 256 rows, or an adapter each: a
+    // CTA takes 1.5 us for every adapter it meets
+    const int most = std::max(std::max(1, (M + 255) / 256), std::min(adapters, M));
     for (g.tiles = 4; g.tiles > 1; g.tiles /= 2) {
         const int blocks = ((C[0] + 128 * g.tiles - 1) / (128 * g.tiles) + (C[1] + 128 * g.tiles - 1) / (128 * g.tiles)) * g.rchunks;
         if (g.tiles * cols <= 512 && (long long)blocks * most >= sms) break;
@@ -494,7 +504,7 @@ static int gr_map(CUtensorMap* map, const void* ptr, size_t rows, size_t cols, s
     return tmap_tiled(map, 2, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
-int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const GradJob jobs[2], char* ws, cudaStream_t s) {
+int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const GradJob jobs[2], char* ws, bool overlap, cudaStream_t s) {
     GradParams p = {};
     p.M = rows.M; p.R = R; p.Rp = (R + 7) / 8 * 8; p.adapters = rows.adapters; p.splits = plan.splits;
     p.tiles = plan.tiles; p.rn = plan.rn; p.rchunks = plan.rchunks;
@@ -538,14 +548,10 @@ int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const Grad
     }
     const dim3 grid((unsigned)(blocks[0] + blocks[1]), (unsigned)plan.splits, (unsigned)plan.rchunks);
     const int smem = 1024 + p.stages * p.stage_bytes;
-    if (drop) adapter_grad_kernel<true><<<grid, GR_THREADS + GR_MASKERS, smem, s>>>(maps, p);
-    else adapter_grad_kernel<false><<<grid, GR_THREADS, smem, s>>>(maps, p);
-    count_launch();
-    rc = launch_status();
+    rc = drop ? start_kernel(adapter_grad_kernel<true>, grid, GR_THREADS + GR_MASKERS, 1, overlap, smem, s, maps, p)
+              : start_kernel(adapter_grad_kernel<false>, grid, GR_THREADS, 1, overlap, smem, s, maps, p);
     if (rc == DR_OK && plan.splits > 1) {
-        adapter_grad_join_kernel<<<dim3((unsigned)std::min((most + 255) / 256, 512ll), (unsigned)rows.adapters, 2), 256, 0, s>>>(p);
-        count_launch();
-        rc = launch_status();
+        rc = start_kernel(adapter_grad_join_kernel, dim3((unsigned)std::min((most + 255) / 256, 512ll), (unsigned)rows.adapters, 2), 256, 1, true, 0, s, p);
     }
     return rc;
 }

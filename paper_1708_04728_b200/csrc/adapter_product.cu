@@ -265,6 +265,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
     __syncthreads();
     if (PAIR) cluster_sync_all();
     tc_fence_after();
+    grid_launch_dependents();
     const uint32_t tmem = sh.tmem;
     const uint32_t full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]);
     const uint32_t full_mask = PAIR ? PEER_BIT_MASK : 0xFFFFFFFFu;
@@ -701,6 +702,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
     __syncthreads();
     if (p.split > 1) cluster_sync_all();                       // sh.odd of every CTA stands before another one writes it
     tc_fence_after();
+    grid_launch_dependents();
     const uint32_t tmem = sh.tmem;
     const uint32_t full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]);
     auto give_up = [&](int site) {
