@@ -36,8 +36,9 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 }
 
 // MT tiles of 16 rows, RT tiles of 8 columns a warp; JOIN: the 8 warps of a CTA split l over the same rows, else each has rows of its own
+// Few rows: 64 registers, so that the next kernel's CTAs (32768 registers each) find room beside two of these.
 template <int MT, int RT, bool DROP, bool JOIN>
-__global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
+__global__ void __launch_bounds__(256, MT == 1 && RT <= 2 && !DROP ? 4 : 1) adapter_down_kernel(const DownParams p) {
     __shared__ float join[JOIN ? 8 : 1][JOIN ? 16 : 1][JOIN ? RT * 8 + 2 : 1];
     __shared__ alignas(8) float range[JOIN ? 16 * RT * 8 : 1];              // this range's sums, read by the cluster
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -154,12 +155,14 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const DownParams p) {
 #pragma unroll 1
                     for (int r = col; r < RT * 8; r += 32) {
                         if (row % p.ks != ks) continue;          // the cluster's CTAs share the rows
-                        float x = 0.f, y = 0.f;
-                        for (int k = 0; k < p.ks; ++k) {
-                            float u, v;
-                            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(u), "=f"(v) : "r"(ptx::mapa_shared(ptx::smem_u32(range + row * RT * 8 + r), (uint32_t)k)) : "memory");
-                            x += u; y += v;
-                        }
+                        float x = 0.f, y = 0.f, u[8], v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)               // all on their way before the first is added
+                            if (k < p.ks)
+                                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(u[k]), "=f"(v[k]) : "r"(ptx::mapa_shared(ptx::smem_u32(range + row * RT * 8 + r), (uint32_t)k)) : "memory");
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (k < p.ks) { x += u[k]; y += v[k]; }
                         if (keeps && r0 + r < p.Rp) put(16 * t + row, r0 + r, x * p.factor, y * p.factor, scale);
                     }
                     ptx::cluster_sync_all();                     // the sums are read: they may be overwritten, the CTA may leave
@@ -398,8 +401,17 @@ DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments, bool
 template <int MT, int RT, bool JOIN>
 static int down_launch(const DownPlan& d, const DownParams& p, bool overlap, cudaStream_t s) {
     const dim3 grid((unsigned)((p.rows.M + d.rows_cta - 1) / d.rows_cta), (unsigned)d.ks, (unsigned)(d.zsplit * d.rchunks));
-    return p.key.thr ? start_kernel(adapter_down_kernel<MT, RT, true, JOIN>, grid, 256, d.ks, overlap, 0, s, p)
-                     : start_kernel(adapter_down_kernel<MT, RT, false, JOIN>, grid, 256, d.ks, overlap, 0, s, p);
+    auto* const k = p.key.thr ? adapter_down_kernel<MT, RT, true, JOIN> : adapter_down_kernel<MT, RT, false, JOIN>;
+    if (MT == 1) {
+        // An SM changes how it divides its memory only when it is empty: with the largest part shared the next kernel's CTAs can begin beside this one's
+        static PerDeviceFlag ready[2];
+        const int i = p.key.thr ? 1 : 0;
+        if (!ready[i].get()) {
+            if (cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+            ready[i].set();
+        }
+    }
+    return start_kernel(k, grid, 256, d.ks, overlap, 0, s, p);
 }
 template <int RT>
 static int down_launch_rt(const DownPlan& d, const DownParams& p, bool overlap, cudaStream_t s) {

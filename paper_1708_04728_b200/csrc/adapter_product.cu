@@ -41,6 +41,7 @@ struct ApParams {
     uint32_t a_bytes, b_bytes, stage_bytes;     // of a block of 64 l: z rows, w of this CTA; of a stage
     uint32_t acc_cols, tmem_cols;
     int split;                  // few rows: CTAs of a cluster that share a tile's l
+    int cache;                  // few rows: where T is kept in shared memory, 0: nowhere
     const int* row_id;
     const __nv_bfloat16* t;     // [M][terms][Rp]
     int t_terms;
@@ -151,7 +152,7 @@ __device__ __forceinline__ void ap_load_f(const ApParams& p, const uint16_t* lis
         }
     }
 }
-// T of this thread's row in the block of `eb`, eight columns at a time
+// T of this thread's row (in global or shared memory) in the block of `eb`, eight columns at a time
 template <class Kind>
 __device__ __forceinline__ void ap_load_t(const __nv_bfloat16* trow, int slot, int Rp, int eb, int w, uint4 (&tv)[Kind::WIDTH / 8][Kind::TERMS]) {
 #pragma unroll
@@ -159,7 +160,7 @@ __device__ __forceinline__ void ap_load_t(const __nv_bfloat16* trow, int slot, i
         const int r = eb + 8 * j - slot * Rp;
         const bool there = slot >= 0 && (unsigned)r < (unsigned)Rp && 8 * j < w;
 #pragma unroll
-        for (int k = 0; k < Kind::TERMS; ++k) tv[j][k] = there ? __ldcg(reinterpret_cast<const uint4*>(trow + k * Rp + r)) : make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < Kind::TERMS; ++k) tv[j][k] = there ? *reinterpret_cast<const uint4*>(trow + k * Rp + r) : make_uint4(0, 0, 0, 0);
     }
 }
 // both into the stage: z's part at a (rows of 128 bytes), w's at b
@@ -680,6 +681,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
     __shared__ ApFewShared sh;
     const uint32_t ring = (smem_u32(ap_raw) + 1023u) & ~1023u;
     float* const sums = reinterpret_cast<float*>(ap_raw + (ring - smem_u32(ap_raw)));      // once the ring is done: [M][nt + 4], DUAL: the adapters' behind
+    __nv_bfloat16* const cache = reinterpret_cast<__nv_bfloat16*>(ap_raw + (ring - smem_u32(ap_raw)) + p.cache);       // behind the ring
     const int pitch = p.nt + 4;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
@@ -771,7 +773,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         if (bt == 0) sh.ext = ext;
         builders_sync();
         mbar_arrive(&sh.ifull);
-        const __nv_bfloat16* const trow = p.t + (size_t)bt * p.t_terms * p.Rp;
+        const __nv_bfloat16* trow = p.t + (size_t)bt * p.t_terms * p.Rp;
         const int cpr = ROWS ? p.nt >> 3 : 4, cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
         const bool row_there = (uint32_t)bt * 128u < p.a_bytes;
         bool waited = false, ok = true;
@@ -782,7 +784,16 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         for (int e0 = rank * WIDTH; e0 < ext && ok; e0 += p.split * WIDTH) {
             uint4 fn[8], tv[WIDTH / 8][TERMS];
             const int w = min(WIDTH, ext - e0);
-            if (!waited) { grid_dependency_wait(); waited = true; }
+            if (!waited) {
+                grid_dependency_wait();
+                waited = true;
+                if (p.cache && row_there) {                    // the row's T at hand for all of its blocks
+                    uint4* const to = reinterpret_cast<uint4*>(cache + (size_t)bt * p.t_terms * p.Rp);
+                    if (slot[0] >= 0)
+                        for (int i = 0; i < p.t_terms * p.Rp / 8; ++i) to[i] = __ldcg(reinterpret_cast<const uint4*>(trow) + i);
+                    trow = cache + (size_t)bt * p.t_terms * p.Rp;
+                }
+            }
             ap_load_t<Kind>(trow, slot[0], p.Rp, e0, w, tv);
             if (any_odd(fv)) {
 #pragma unroll
@@ -855,14 +866,16 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
             if (slot == ROW_NONE || c >= p.C) continue;
             const uint32_t at = smem_u32(sums + (size_t)m * pitch + cl), at2 = smem_u32(sums + ((size_t)p.rows.M + m) * pitch + cl);
             float v[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int k = 0; k < p.split; ++k) {
-                const float4 x = ld_shared_cluster_f4(p.split > 1 ? mapa_shared(at, (uint32_t)k) : at);
-                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-                if (DUAL) {
-                    const float4 y = ld_shared_cluster_f4(p.split > 1 ? mapa_shared(at2, (uint32_t)k) : at2);
-                    u[0] += y.x; u[1] += y.y; u[2] += y.z; u[3] += y.w;
-                }
-            }
+            auto gather = [&](uint32_t from, float (&to)[4]) {
+                float4 x[8];                                   // all on their way before the first is added
+#pragma unroll
+                for (int k = 0; k < 8; ++k) if (k < p.split) x[k] = ld_shared_cluster_f4(p.split > 1 ? mapa_shared(from, (uint32_t)k) : from);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < p.split) { to[0] += x[k].x; to[1] += x[k].y; to[2] += x[k].z; to[3] += x[k].w; }
+            };
+            gather(at, v);
+            if (DUAL) gather(at2, u);
             const uint32_t bits = DUAL ? drop_bits8_at(p.key, off, (unsigned long long)m * p.C + c) : 0xFu;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -988,7 +1001,9 @@ static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t
     p.acc_cols = std::max(32, p.nt);
     p.tmem_cols = p.acc_cols * (dual ? 2 : 1);
     const size_t ring = (size_t)p.stages * p.stage_bytes + slack, sums = (size_t)M * (p.nt + 4) * 4 * (dual ? 2 : 1);
-    const size_t smem = 1024 + std::max(ring, sums);
+    const size_t rows_t = (size_t)(M + 7) / 8 * 8 * a.terms * a.Rp * 2, behind = std::max(ring, sums);
+    p.cache = behind + rows_t <= AP_SMEM_MOST - 1024 ? (int)behind : 0;
+    const size_t smem = 1024 + behind + (p.cache ? rows_t : 0);
     alignas(64) CUtensorMap mz, mw;
     int rc = ap_map(&mz, a.z, M, a.L, a.ldz, 64, (M + 7) / 8 * 8);
     if (rc != DR_OK) return rc;
