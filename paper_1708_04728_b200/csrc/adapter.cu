@@ -82,16 +82,18 @@ static BackwardPlan backward_plan(const dr_adapter_desc* d, int M, int ldx, int 
     f.bytes = at.bytes;
     return f;
 }
-// the tensor itself, or its aligned copy
-static int place(bool copy, size_t rows, int cols, int colsp, const void* src, size_t ld, char* ws, size_t at, const __nv_bfloat16** p, size_t* ldp, cudaStream_t s) {
-    *p = (const __nv_bfloat16*)src;
-    *ldp = ld;
-    if (!copy) return DR_OK;
-    __nv_bfloat16* dst = (__nv_bfloat16*)(ws + at);
-    *p = dst;
-    *ldp = colsp;
-    return adapter_align_run(rows, cols, (const __nv_bfloat16*)src, ld, dst, colsp, s);
-}
+// The tensors themselves, or their aligned copies, all made in one launch.
+struct Aligner {
+    AlignJob job[4];
+    int n = 0;
+    char* ws;
+    explicit Aligner(char* workspace) : ws(workspace) {}
+    void place(bool copy, size_t rows, int cols, int colsp, const void* src, size_t ld, size_t at, const __nv_bfloat16** p, size_t* ldp) {
+        *p = copy ? (const __nv_bfloat16*)(ws + at) : (const __nv_bfloat16*)src;
+        *ldp = copy ? (size_t)colsp : ld;
+        if (copy) job[n++] = {(const __nv_bfloat16*)src, ld, (__nv_bfloat16*)(ws + at), (size_t)colsp, rows, cols};
+    }
+};
 
 }  // namespace dr
 
@@ -134,9 +136,11 @@ extern "C" int dr_adapter(const dr_adapter_desc* d, int M, const void* x, int ld
     const DropKey key = drop_key(d->drop_p, d->drop_seed, d->drop_offset, step), none = drop_key(0., 0, 0, nullptr);
     const __nv_bfloat16 *xp, *wp, *ap;
     size_t ldxp, ldwp, ldap;
-    if ((rc = place(f.copy_x, M, K, f.Kp, x, ldx, ws, f.x, &xp, &ldxp, s)) != DR_OK) return rc;
-    if ((rc = place(f.copy_k, N, K, f.Kp, w, K, ws, f.w, &wp, &ldwp, s)) != DR_OK) return rc;
-    if ((rc = place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, ws, f.a, &ap, &ldap, s)) != DR_OK) return rc;
+    Aligner al(ws);
+    al.place(f.copy_x, M, K, f.Kp, x, ldx, f.x, &xp, &ldxp);
+    al.place(f.copy_k, N, K, f.Kp, w, K, f.w, &wp, &ldwp);
+    al.place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, f.a, &ap, &ldap);
+    if ((rc = adapter_align_run(al.job, al.n, s)) != DR_OK) return rc;
     __nv_bfloat16* const tw = (__nv_bfloat16*)(ws + f.t);
     int* const ids = (int*)(ws + f.ids);
     rc = adapter_down_run(f.down, rows, K, R, f.Rp, xp, ldxp, ap, ldap, key, key.thr ? key.scale : 1.f, scale, 1.f, f.terms, tw, t, ids, false, s);
@@ -172,10 +176,12 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     const float kept = key.thr ? key.scale : 1.f;
     const __nv_bfloat16 *dyp, *xp = nullptr, *wp = nullptr, *ap = nullptr;
     size_t lddyp, ldxp = 0, ldwp = 0, ldap = 0;
-    if ((rc = place(f.copy_dy, M, N, f.Np, dy, lddy, ws, f.dy, &dyp, &lddyp, s)) != DR_OK) return rc;
-    if (da && (rc = place(f.copy_x, M, K, f.Kp, x, ldx, ws, f.x, &xp, &ldxp, s)) != DR_OK) return rc;
-    if (dx && (rc = place(f.copy_k, N, K, f.Kp, w, K, ws, f.w, &wp, &ldwp, s)) != DR_OK) return rc;
-    if (dx && (rc = place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, ws, f.a, &ap, &ldap, s)) != DR_OK) return rc;
+    Aligner al(ws);
+    al.place(f.copy_dy, M, N, f.Np, dy, lddy, f.dy, &dyp, &lddyp);
+    if (da) al.place(f.copy_x, M, K, f.Kp, x, ldx, f.x, &xp, &ldxp);
+    if (dx) al.place(f.copy_k, N, K, f.Kp, w, K, f.w, &wp, &ldwp);
+    if (dx) al.place(f.copy_k, (size_t)d->adapters * R, K, f.Kp, a, K, f.a, &ap, &ldap);
+    if ((rc = adapter_align_run(al.job, al.n, s)) != DR_OK) return rc;
     __nv_bfloat16* const u = (__nv_bfloat16*)(ws + f.u);
     int* const ids = (int*)(ws + f.ids);
     const bool grads = da || db, u_wanted = dx || da;

@@ -235,6 +235,7 @@ int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const Grad
 int adapter_prep_run(const AdRows& rows, int* perm, int* start, int N, int R, int Rp, const __nv_bfloat16* b, __nv_bfloat16* bt, size_t ldb, const float* t,
                      const float* scale, __nv_bfloat16* terms, cudaStream_t s);
 
-// rows of `cols` elements, `ld` apart, as rows of ldd >= cols with zeros behind them
-int adapter_align_run(size_t rows, int cols, const __nv_bfloat16* src, size_t ld, __nv_bfloat16* dst, size_t ldd, cudaStream_t s);
+// rows of `cols` elements, `ld` apart, as rows of ldd >= cols (a multiple of 8) with zeros behind them; at most four tensors
+struct AlignJob { const __nv_bfloat16* src; size_t ld; __nv_bfloat16* dst; size_t ldd, rows; int cols; };
+int adapter_align_run(const AlignJob* jobs, int n, cudaStream_t s);
 }  // namespace dr

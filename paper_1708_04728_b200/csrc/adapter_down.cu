@@ -434,18 +434,30 @@ int adapter_down_run(const DownPlan& d, const AdRows& rows, int L, int R, int Rp
 }
 
 // ---- layouts ------------------------------------------------------------------------------------------------------
-__global__ void adapter_align_kernel(size_t rows, int cols, const __nv_bfloat16* __restrict__ src, size_t ld, __nv_bfloat16* __restrict__ dst, size_t ldd) {
-    const size_t row = (size_t)blockIdx.x * blockDim.y + threadIdx.y;
-    if (row >= rows) return;
-    for (int c = 2 * (int)threadIdx.x; c < (int)ldd; c += 64) {
-        __nv_bfloat162 v;
-        v.x = c < cols ? src[row * ld + c] : __float2bfloat16_rn(0.f);
-        v.y = c + 1 < cols ? src[row * ld + c + 1] : __float2bfloat16_rn(0.f);
-        *reinterpret_cast<__nv_bfloat162*>(dst + row * ldd + c) = v;
+// Up to four tensors in one launch; a thread writes 16 bytes.
+struct AlignJobs { AlignJob job[4]; };
+__global__ void __launch_bounds__(256) adapter_align_kernel(const AlignJobs jobs) {
+    const AlignJob& j = jobs.job[blockIdx.y];
+    const size_t per = j.ldd >> 3, n = j.rows * per, stride = (size_t)gridDim.x * 256;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
+        const size_t row = i / per;
+        const int c = 8 * (int)(i - row * per);
+        const unsigned short* src = reinterpret_cast<const unsigned short*>(j.src) + row * j.ld + c;
+        uint32_t u[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[k] = (c + 2 * k < j.cols ? (uint32_t)__ldg(src + 2 * k) : 0u) | (c + 2 * k + 1 < j.cols ? (uint32_t)__ldg(src + 2 * k + 1) << 16 : 0u);
+        *reinterpret_cast<uint4*>(j.dst + row * j.ldd + c) = make_uint4(u[0], u[1], u[2], u[3]);
     }
 }
-int adapter_align_run(size_t rows, int cols, const __nv_bfloat16* src, size_t ld, __nv_bfloat16* dst, size_t ldd, cudaStream_t s) {
-    adapter_align_kernel<<<(unsigned)((rows + 7) / 8), dim3(32, 8), 0, s>>>(rows, cols, src, ld, dst, ldd);
+int adapter_align_run(const AlignJob* jobs, int n, cudaStream_t s) {
+    if (n == 0) return DR_OK;
+    AlignJobs a = {};
+    size_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        a.job[i] = jobs[i];
+        most = std::max(most, (jobs[i].rows * (jobs[i].ldd >> 3) + 255) / 256);
+    }
+    adapter_align_kernel<<<dim3((unsigned)std::min(most, (size_t)num_sms() * 16), (unsigned)n), 256, 0, s>>>(a);
     count_launch();
     return launch_status();
 }
