@@ -349,28 +349,43 @@ adapter_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
         // ---------------------------------------------------------------- mask: clears the dropped values of a tile
         if (drop) {
             const unsigned long long off = drop_offset(j.key);
-            const int t = threadIdx.x - GR_THREADS;
-            const int zc = p.tiles * 16, step = GR_MASKERS / zc;      // 16-byte pieces of a row; rows that all threads hold
-            const int col = t % zc, row0 = t / zc, c = c0 + 8 * col;
-            const uint32_t base = (uint32_t)(col >> 3) * GR_BOX, ch = (uint32_t)(col & 7);
+            // the tile's 16-byte pieces that hold columns, dealt out to the threads; four at a time, for the generator's rounds depend on one another
+            const int per = min(p.tiles * 16, (j.C - c0 + 7) >> 3), pieces = GR_ROWS * per;
+            const int first = (int)threadIdx.x - GR_THREADS, row0 = first / per, col0 = first - row0 * per, dr = GR_MASKERS / per, dc = GR_MASKERS - dr * per;
             int s = 0;
             uint32_t ph = 0;
             grad_ranges(p, split, [&](int, int u, int v, bool) {
                 for (int i = u; i < v; i += GR_ROWS) {
                     if (!__all_sync(0xffffffffu, mbar_wait_u32(landed0 + 8 * s, ph, abort_flag))) { give_up(105); return false; }
-                    const uint32_t tile = ring + (uint32_t)s * p.stage_bytes + base;
-                    if (c < j.C) {
-#pragma unroll 2
-                        for (int r = row0; r < GR_ROWS; r += step) {
-                            const int row = sh.rows[s][r];
-                            const uint32_t at = tile + r * 128 + ((ch ^ (uint32_t)(r & 7)) << 4);
-                            uint4 x;
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
-                            const unsigned long long e = (unsigned long long)row * j.C + c;
-                            const uint32_t bits = (j.C & 7) ? drop_bits8_at(j.key, off, e) : drop_bits8(j.key, off, e >> 3);
-                            x = drop_apply8(x, bits);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                    uint8_t* const tile = gr_raw + (ring + (uint32_t)s * p.stage_bytes - smem_u32(gr_raw));
+                    int r = row0, col = col0;
+#pragma unroll 1
+                    for (int k0 = first; k0 < pieces; k0 += 4 * GR_MASKERS) {
+                        uint4* at[4];
+                        uint4 x[4];
+                        uint32_t bits[4];
+                        unsigned long long e[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            if (k0 + k * GR_MASKERS < pieces) {
+                                at[k] = reinterpret_cast<uint4*>(tile + (col >> 3) * GR_BOX + r * 128 + (((col ^ r) & 7) << 4));
+                                e[k] = (unsigned long long)sh.rows[s][r] * j.C + c0 + 8 * col;
+                                x[k] = *at[k];
+                            }
+                            r += dr;
+                            col += dc;
+                            if (col >= per) { col -= per; ++r; }
                         }
+                        if (j.C & 7) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) bits[k] = k0 + k * GR_MASKERS < pieces ? drop_bits8_at(j.key, off, e[k]) : 0u;
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) bits[k] = drop_bits8(j.key, off, e[k] >> 3);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (k0 + k * GR_MASKERS < pieces) *at[k] = drop_apply8(x[k], bits[k]);
                     }
                     fence_proxy_async_smem();
                     __syncwarp();

@@ -552,8 +552,13 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                         if (DUAL) {
                             uint32_t bits = 0;
                             const unsigned long long e = (unsigned long long)m * p.C + n0 + c + h;
+                            if (p.C & 7) {
 #pragma unroll 1
-                            for (int k = 0; k < 4; ++k) bits |= drop_bits8_at(p.key, off, e + 8 * k) << (8 * k);
+                                for (int k = 0; k < 4; ++k) bits |= drop_bits8_at(p.key, off, e + 8 * k) << (8 * k);
+                            } else {                                           // the rounds of a draw depend on one another: four draws at a time
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) bits |= drop_bits8(p.key, off, (e >> 3) + k) << (8 * k);
+                            }
                             if (ext) {
                                 uint32_t u[32];
                                 tmem_ld_x32(acc + p.acc_cols + c + h, u);
