@@ -365,9 +365,23 @@ def run_finetune(args):
         dgamma, dbeta, normed = torch.empty_like(gamma), torch.empty_like(beta), torch.empty_like(yt)      # its own: the step's buffers stay as they are
         norm = lambda: dr.dr_layernorm(npix, cout, y, 0, gamma, beta, 1e-5, normed, 0, mean, rstd)
         norm_bwd = lambda: dr.dr_layernorm_bwd(npix, cout, yt, 0, y, 0, gamma, mean, rstd, normed, 0, dgamma, dbeta, ln_ws, ln_ws.numel())
+        # a 1 x 1 layer of the same channels with rank-16 adapters of eight tasks, an image a request, dropout in front of them
+        npx, tasks, rank = B * hw * hw, 8, 16
+        ad = dr.dr_adapter_desc(Cin=cin, Cout=cout, rank=rank, adapters=tasks, flags=dr.DR_BIAS | dr.DR_RELU, drop_p=0.1, drop_seed=1, drop_offset=0)
+        ad_x = x[..., :cin].reshape(npx, cin)
+        ad_w, ad_a, ad_b = shadow.reshape(cout, -1)[:, :cin].contiguous(), shadow.new_ones((tasks, rank, cin)), shadow.new_ones((tasks, cout, rank))
+        ad_y, ad_dx, ad_t = x.new_empty((npx, cout)), x.new_empty((npx, cin)), torch.zeros((npx, rank), device="cuda")
+        ad_da, ad_db = torch.empty((tasks, rank, cin), device="cuda"), torch.empty((tasks, cout, rank), device="cuda")
+        ad_rows = torch.arange(B + 1, dtype=torch.int32, device="cuda") * (hw * hw)
+        ad_ids = (torch.arange(B, device="cuda") % tasks).to(torch.int32)
+        ad_n = max(dr.dr_adapter_workspace_bytes(ad, npx), dr.dr_adapter_bwd_workspace_bytes(ad, npx))
+        ad_ws = torch.empty(ad_n, dtype=torch.uint8, device="cuda")
+        drop = lambda: dr.dr_dropout(npx, cin, ad_x, 0, None, 0, ad_dx, 0, 0.1, 1, 0)
+        adapter = lambda: dr.dr_adapter(ad, npx, ad_x, 0, ad_w, b, ad_a, ad_b, None, B, ad_rows, ad_ids, ad_y, 0, ad_t, None, ad_ws, ad_n)
+        adapter_bwd = lambda: dr.dr_adapter_bwd(ad, npx, ad_y, 0, ad_x, 0, ad_w, ad_a, ad_b, None, B, ad_rows, ad_ids, ad_t, ad_dx, 0, ad_da, ad_db, None, ad_ws, ad_n)
         t = {}
         for what, fn in (("step", step), ("step_graph", graph.replay), ("wgrad", wgrad), ("forward", fwd), ("muon", muon), ("layernorm", norm),
-                         ("layernorm_bwd", norm_bwd)):
+                         ("layernorm_bwd", norm_bwd), ("dropout", drop), ("adapter", adapter), ("adapter_bwd", adapter_bwd)):
             ts = []
             for i in range(args.warmup + min(args.steps, 20)):
                 flush.zero_()
@@ -399,6 +413,7 @@ def run_finetune(args):
                 lib[what] = statistics.median(ts)
         rows.append({"layer": name, "step_us": t["step"], "step_graph_us": t["step_graph"], "forward_us": t["forward"], "wgrad_us": t["wgrad"],
                      "muon_update_us": t["muon"], "layernorm_us": t["layernorm"], "layernorm_bwd_us": t["layernorm_bwd"],
+                     "dropout_us": t["dropout"], "adapter_1x1_us": t["adapter"], "adapter_1x1_bwd_us": t["adapter_bwd"],
                      "images_per_s": B / t["step"] * 1e6, "wgrad_tflops": flops / t["wgrad"] * 1e-6,
                      "wgrad_frac": flops / t["wgrad"] * 1e-6 / pk["bf16_tflops"], "forward_tflops": flops / t["forward"] * 1e-6,
                      "loss": float(loss), **lib})
