@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(256, MT == 1 && RT <= 2 && !DROP ? 4 : 1) adap
 // ---- many rows, long l, ranks over 16, requests of many rows --------------------------------------------------------------------------------
 // The same product on tcgen05: a CTA takes 128 rows, z and the adapter's rows come by TMA into a ring, the accumulator (128 x rank) lies in TMEM.  Rows
 // of several adapters: the product is run once for each.  The tensor cores cut their sums off instead of rounding them, so 512 l are summed at a time
-// and the drain adds those up in float32 (all 4096 at once: 5e-6 of a gradient built on them, so 7e-7).  16384 x 4096, rank 64: TODO us, with fragments
+// and the drain adds those up in float32 (all 4096 at once: 5e-6 of a gradient built on them, so 7e-7).  16384 x 4096, rank 64: 35 us, with fragments
 // from memory 82 (every 32 rows read all of an adapter).
 constexpr int DT_THREADS = 192, DT_STAGES = 4;         // warp 0 loads, 1 issues MMAs, 2-5 find the adapters and drain; two CTAs to an SM
 constexpr int DT_CHAIN = 8;                            // blocks of 64 l

@@ -30,6 +30,9 @@ constexpr int AP_MAX_STAGES = 16;
 constexpr int AP_SMEM = 180 * 1024;     // the ring's; with 32 KB of the drain's and the barriers' all of an SM's
 constexpr int AP_SMEM_MOST = 213 * 1024;
 constexpr int AP_TILE = 128;
+// The tensor cores cut their sums off instead of rounding them: an error of about 2e-8 of the result for each MMA in a row, 5e-6 after 4096 l.  bfloat16
+// results do not show it; for float32 ones 512 l are summed in TMEM at a time and the drain adds those up.
+constexpr int AP_CHAIN = 8;             // blocks of 64 l
 
 struct ApParams {
     AdRows rows;
@@ -41,6 +44,7 @@ struct ApParams {
     uint32_t a_bytes, b_bytes, stage_bytes;     // of a block of 64 l: z rows, w of this CTA; of a stage
     uint32_t acc_cols, tmem_cols;
     int split;                  // few rows: CTAs of a cluster that share a tile's l
+    int accs;                   // few rows, float32 results: accumulators that share a CTA's l
     int cache;                  // few rows: where T is kept in shared memory, 0: nowhere
     const int* row_id;
     const __nv_bfloat16* t;     // [M][terms][Rp]
@@ -359,15 +363,25 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                 if (!DUAL) accum = acc;
                 return true;
             };
+            int n = 0;                                                          // accumulators begun
             for (int tile = unit; tile < p.tiles; tile += units, ++it) {
-                const int ab = WIDE ? half : it & 1, use = WIDE ? it : it >> 1;        // accumulator and how often it was used
-                if (!mbar_wait(&sh.tempty[ab], (use & 1) ^ 1, abort_flag)) { give_up(83, tile); break; }
-                tc_fence_after();
-                d = tmem + (uint32_t)ab * p.acc_cols * (DUAL ? 2u : 1u);
-                accum = 0;
+                auto begin = [&]() {                                            // the next accumulator, once it is drained
+                    const int ab = WIDE ? half : n & 1, use = WIDE ? n : n >> 1;
+                    if (!mbar_wait(&sh.tempty[ab], (use & 1) ^ 1, abort_flag)) { give_up(83, tile); return false; }
+                    tc_fence_after();
+                    d = tmem + (uint32_t)ab * p.acc_cols * (DUAL ? 2u : 1u);
+                    accum = 0;
+                    return true;
+                };
+                auto end = [&]() { umma_commit_u32<PAIR>(smem_u32(&sh.tfull[WIDE ? half : n & 1])); ++n; };
+                if (!begin()) break;
                 if (it > 0 && !further(tile)) break;
                 bool ok = true;
                 for (int kb = 0; kb < p.kblocks; ++kb) {
+                    if (TERMS == 3 && kb > 0 && kb % AP_CHAIN == 0) {
+                        end();
+                        if (!begin()) { ok = false; break; }
+                    }
                     if (!mbar_wait_u32(full0 + 8 * s, ph, abort_flag)) { give_up(84, tile); ok = false; break; }
                     tc_fence_after();
                     const uint32_t a = ring + (uint32_t)s * p.stage_bytes, b = a + p.a_bytes + (uint32_t)half * 16384u;
@@ -382,7 +396,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                     if (++s == p.stages) { s = 0; ph ^= 1; }
                 }
                 if (!ok || (it == 0 && !further(tile))) break;
-                umma_commit_u32<PAIR>(smem_u32(&sh.tfull[ab]));
+                end();
             }
         }
         __syncwarp();
@@ -513,7 +527,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
         const float low = (p.flags & DR_RELU) ? 0.f : -INFINITY;
         const uint32_t low2 = (p.flags & DR_RELU) ? 0u : 0xFF80FF80u;
         const unsigned long long off = DUAL ? drop_offset(p.key) : 0ull;
-        int it = 0;
+        int it = 0, n = 0;
         bool ok = true;
         ApInfo info;
         for (int tile = unit; tile < p.tiles && ok; tile += units, ++it, info.next()) {
@@ -530,14 +544,44 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
             const uint32_t quarter = (uint32_t)(q * 32) << 16;
 #pragma unroll 1
             for (int part = 0; part < (WIDE ? 2 : 1); ++part) {
-                const int ab = WIDE ? part : it & 1, use = WIDE ? it : it >> 1;
+                // float32 results: this warp's columns, at most two chunks (nt <= 128), added up over the chains in front of the last
+                float sum[TERMS == 3 ? 2 : 1][32];
+                if (TERMS == 3) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sum[TERMS == 3 ? j : 0][i] = 0.f;
+                    for (int kb = AP_CHAIN; kb < p.kblocks; kb += AP_CHAIN, ++n) {
+                        if (!__all_sync(0xffffffffu, mbar_wait(&sh.tfull[n & 1], (uint32_t)(n >> 1) & 1, abort_flag))) { give_up(90, tile); ok = false; break; }
+                        tc_fence_after();
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            if (side * 32 + 64 * j >= n_here) break;
+                            uint32_t v[32];
+                            tmem_ld_x32(tmem + (uint32_t)(n & 1) * p.acc_cols + quarter + side * 32 + 64 * j, v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) sum[TERMS == 3 ? j : 0][i] += __uint_as_float(v[i]);
+                        }
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (PAIR) mbar_arrive_leader(&sh.tempty[n & 1]);
+                            else mbar_arrive(&sh.tempty[n & 1]);
+                        }
+                    }
+                    if (!ok) break;
+                }
+                const int ab = WIDE ? part : n & 1, use = WIDE ? it : n >> 1;
                 if (!__all_sync(0xffffffffu, mbar_wait(&sh.tfull[ab], use & 1, abort_flag))) { give_up(90, tile); ok = false; break; }
                 tc_fence_after();
                 const bool odd = *(volatile int*)&sh.odd[ib] > it;
                 const uint32_t acc = tmem + (uint32_t)ab * p.acc_cols * (DUAL ? 2u : 1u) + quarter;
                 const int c_end = WIDE ? min(256, n_here - 256 * part) : n_here, cb = WIDE ? 256 * part : 0;
-#pragma unroll 1
-                for (int c = side * CHUNK; c < c_end; c += 2 * CHUNK) {
+#pragma unroll(TERMS == 3 ? 2 : 1)
+                for (int cj = 0; cj < (TERMS == 3 ? 2 : 1 << 30); ++cj) {
+                    const int c = (side + 2 * cj) * CHUNK;
+                    if (c >= c_end) break;
                     if (lane == 0) tma_store_wait_read();                      // the box in front has been read
                     __syncwarp();
                     uint32_t w[DUAL ? 1 : CHUNK / 32][32];
@@ -568,6 +612,10 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                             }
                         }
                         tmem_ld_wait();
+                        if (TERMS == 3) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + sum[TERMS == 3 ? cj & 1 : 0][i]);
+                        }
                         if (odd) {
                             // what f that is not finite adds to this row's values
 #pragma unroll 1
@@ -648,6 +696,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                     else mbar_arrive(&sh.tempty[ab]);
                 }
             }
+            ++n;
             if (lane == 0) mbar_arrive(&sh.iempty[ib]);
         }
         if (lane == 0) tma_store_wait_all();
@@ -746,6 +795,8 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
             int s = 0;
             uint32_t ph = 0, accum = 0;
             bool ok = true;
+            // float32 results: an accumulator for every so many blocks
+            const int chain = TERMS == 3 ? (kb1 - kb0 + p.accs - 1) / p.accs : 1 << 30;
             auto block = [&](uint32_t d, int n16, int site) {
                 if (!mbar_wait_u32(full0 + 8 * s, ph, abort_flag)) { give_up(site); ok = false; return; }
                 tc_fence_after();
@@ -759,11 +810,16 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
                 umma_commit_u32<false>(empty0 + 8 * s);
                 if (++s == p.stages) { s = 0; ph ^= 1; }
             };
-            for (int kb = kb0; kb < kb1 && ok; ++kb) block(tmem, kb == p.kblocks - 1 ? tail16 : 4, 93);
+            for (int kb = kb0, i = 0; kb < kb1 && ok; ++kb, ++i) {
+                const int acc = TERMS == 3 ? i / chain : 0;
+                if (TERMS == 3 && i - acc * chain == 0) accum = 0;
+                block(tmem + (uint32_t)acc * p.acc_cols, kb == p.kblocks - 1 ? tail16 : 4, 93);
+            }
             if (ok && !mbar_wait(&sh.ifull, 0, abort_flag)) { give_up(94); ok = false; }
             const int ext = ok ? sh.ext : 0;
             if (DUAL) accum = 0;
-            for (int e = rank * WIDTH; e < ext && ok; e += p.split * WIDTH) block(tmem + (DUAL ? p.acc_cols : 0u), (TERMS * min(WIDTH, ext - e) + 15) >> 4, 95);
+            const uint32_t last = TERMS == 3 ? (uint32_t)((kb1 - kb0 - 1) / chain) * p.acc_cols : 0u;
+            for (int e = rank * WIDTH; e < ext && ok; e += p.split * WIDTH) block(tmem + (DUAL ? p.acc_cols : last), (TERMS * min(WIDTH, ext - e) + 15) >> 4, 95);
             umma_commit_u32<false>(smem_u32(&sh.tfull));
         }
         __syncwarp();
@@ -843,6 +899,17 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
                         uint32_t v[32];
                         tmem_ld_x32(tmem + (uint32_t)k * p.acc_cols + ((uint32_t)(q * 32) << 16) + c, v);
                         tmem_ld_wait();
+                        if (TERMS == 3) {
+                            const int chain = (kb1 - kb0 + p.accs - 1) / p.accs, accs = (kb1 - kb0 + chain - 1) / chain;
+#pragma unroll 1
+                            for (int a = 1; a < accs; ++a) {
+                                uint32_t w[32];
+                                tmem_ld_x32(tmem + (uint32_t)a * p.acc_cols + ((uint32_t)(q * 32) << 16) + c, w);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
+                            }
+                        }
                         if (row < p.rows.M) {
                             float4* to = reinterpret_cast<float4*>(sums + ((size_t)k * p.rows.M + row) * pitch + c);
                             const bool there = k == 0 || own;
@@ -987,9 +1054,11 @@ static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t
     const bool dual = a.key.thr != 0;
     p.a_bytes = (uint32_t)((M + 7) / 8 * 8) * 128u;
     // Width of a tile and CTAs that share its l, by a model in cycles: w once from memory (3.4 KB a cycle for all SMs), a CTA's loads at 32 bytes a
-    // cycle and 150 cycles a stage, 1500 for the meeting of a cluster.  32 x 4096 x 4096 takes TODO
+    // cycle and 150 cycles a stage, 1500 for the meeting of a cluster.  For 32 x 4096 x 4096 it picks 128 columns and four CTAs, 27 us; 64 and two take 33,
+    // 32 alone 50, 128 alone 57.
     double best = 0.;
-    for (int nt = a.transposed ? 64 : 16; nt <= 128; nt *= 2)
+    const bool f32 = a.flags & DR_OUT_F32;
+    for (int nt = a.transposed ? 64 : 16; nt <= (f32 ? 64 : 128); nt *= 2)
         for (int split = 1; split <= 8 && split <= p.kblocks && 4 * split <= nt; split *= 2) {
             const int tiles = (a.C + nt - 1) / nt, blocks = (p.kblocks + split - 1) / split;
             const int waves = (tiles + few_clusters(split) - 1) / few_clusters(split);
@@ -1004,7 +1073,9 @@ static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t
     const uint32_t slack = 16384u - p.a_bytes;                                // the MMA reads 128 rows from the last stage on
     p.stages = (int)std::min<uint32_t>(AP_MAX_STAGES, (AP_SMEM - slack) / p.stage_bytes);
     p.acc_cols = std::max(32, p.nt);
+    p.accs = f32 ? std::min(256u / p.acc_cols, (uint32_t)std::max(1, (p.kblocks / p.split + AP_CHAIN) / AP_CHAIN)) : 1;
     p.tmem_cols = p.acc_cols * (dual ? 2 : 1);
+    while (p.tmem_cols < p.acc_cols * p.accs) p.tmem_cols *= 2;
     const size_t ring = (size_t)p.stages * p.stage_bytes + slack, sums = (size_t)M * (p.nt + 4) * 4 * (dual ? 2 : 1);
     const size_t rows_t = (size_t)(M + 7) / 8 * 8 * a.terms * a.Rp * 2, behind = std::max(ring, sums);
     p.cache = behind + rows_t <= AP_SMEM_MOST - 1024 ? (int)behind : 0;
@@ -1036,7 +1107,7 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
     const long long rows128 = (M + 127) / 128;
     const int gran = a.transposed ? 64 : 16;
     // Tile: as wide as leaves every SM one, by pairs where the pairs have enough tiles
-    const int most = dual ? 128 : 256;
+    const int most = dual || f32 ? 128 : 256;
     bool pair = false, wide = false;
     int nt = std::min(most, (a.C + gran - 1) / gran * gran);
     if (rows128 * ((a.C + nt - 1) / nt) < sms) {
@@ -1050,7 +1121,7 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
         // Out of L2 a pair's block of 256 x 256 takes 64 KB for 512 cycles of MMAs, more than the 12 TB/s that all SMs get; 256 x 512 takes 96 KB
         // for 1024, but its accumulators fill the tensor memory, so a tile's drain is only half hidden: long l.  16384 x 4096 x 4096 takes 380 us
         // instead of 509.
-        if (pair && !dual && a.L >= 1024 && a.C >= 512 && ((rows128 + 1) / 2) * ((a.C + 511) / 512) >= sms / 2) { wide = true; nt = 512; }
+        if (pair && !dual && !f32 && a.L >= 1024 && a.C >= 512 && ((rows128 + 1) / 2) * ((a.C + 511) / 512) >= sms / 2) { wide = true; nt = 512; }
     }
     p.nt = nt;
     p.tiles_c = (a.C + nt - 1) / nt;
@@ -1078,7 +1149,7 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
         if (pair) return dual ? ap_launch<ApKind<true, false, true, true, 2>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<true, false, true, false, 2>>(mz, mw, mo, p, overlap, smem, s);
         return dual ? ap_launch<ApKind<false, false, true, true, 2>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<false, false, true, false, 2>>(mz, mw, mo, p, overlap, smem, s);
     }
-    if (wide) return f32 ? ap_launch<ApKind<true, true, false, false, 3>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<true, true, false, false, 2>>(mz, mw, mo, p, overlap, smem, s);
+    if (wide) return ap_launch<ApKind<true, true, false, false, 2>>(mz, mw, mo, p, overlap, smem, s);
     if (pair) return f32 ? ap_launch<ApKind<true, false, false, false, 3>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<true, false, false, false, 2>>(mz, mw, mo, p, overlap, smem, s);
     return f32 ? ap_launch<ApKind<false, false, false, false, 3>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<false, false, false, false, 2>>(mz, mw, mo, p, overlap, smem, s);
 }
