@@ -38,7 +38,7 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 // MT tiles of 16 rows, RT tiles of 8 columns a warp; JOIN: the 8 warps of a CTA split l over the same rows, else each has rows of its own
 // Few rows: 64 registers, so that the next kernel's CTAs (32768 registers each) find room beside two of these.
 template <int MT, int RT, bool DROP, bool JOIN>
-__global__ void __launch_bounds__(256, MT == 1 && RT <= 2 && !DROP ? 4 : 1) adapter_down_kernel(const DownParams p) {
+__global__ void __launch_bounds__(256, MT == 1 && RT <= 2 && !DROP ? 4 : 0) adapter_down_kernel(const DownParams p) {
     __shared__ float join[JOIN ? 8 : 1][JOIN ? 16 : 1][JOIN ? RT * 8 + 2 : 1];
     __shared__ alignas(8) float range[JOIN ? 16 * RT * 8 : 1];              // this range's sums, read by the cluster
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
