@@ -480,9 +480,12 @@ int dr_dropout(size_t rows, int C, const void* x, int ldx, const void* residual,
  *  float32 with DR_OUT_F32; t: NULL, or float32 [M][rank], what a backward pass needs of the forward pass (0 in rows without a variant).
  *  x, w, a, b: 16-byte aligned; y: its type's alignment; any Cin, Cout, rank and pitches.  Where Cin or ldx is no multiple of 8 the call lays out
  *  aligned copies in the workspace first.  y may not overlap an input.
- *  Products are of bfloat16 values and sum in float32; t and u enter the second product as the sum of two bfloat16 values (16 to 17 bits).
- *  step: NULL or a counter in device memory, as in dr_dropout.  workspace: dr_adapter_workspace_bytes bytes, 256-byte aligned, contents
- *  irrelevant; calls that may overlap on the GPU need their own.
+ *  Products are of bfloat16 values and sum in float32.  t and u enter the second product as the sum of two bfloat16 values (16 to 17 bits), of three
+ *  (24) where y is float32 and in da and db; there sums longer than 512 to 2304 terms are added up from parts, because the tensor cores cut
+ *  theirs off instead of rounding them.  Relative error (2-norm): bfloat16 results their rounding, float32 ones up to 8e-7 with sums of 16384.
+ *  A variant that holds a NaN or an infinity, and a row of x that does, touch no other request's rows.
+ *  step: NULL or a counter in device memory, as in dr_dropout.  workspace: dr_adapter_workspace_bytes bytes (for the ldx of the call), 256-byte aligned,
+ *  contents irrelevant; calls that may overlap on the GPU need their own.  About 4 M + 6 M rank bytes, and the aligned copies.
  * Errors: INVALID_ARG, UNSUPPORTED (the limits below), ALIGNMENT, WORKSPACE, CUDA.                                    */
 #define DR_ADAPTER_MAX_RANK     256
 #define DR_ADAPTER_MAX_CHANNELS 65536
@@ -503,7 +506,9 @@ int dr_adapter(const dr_adapter_desc* desc, int M, const void* x, int ldx, const
  *  dy: [M][Cout] bfloat16, pitch lddy, 16-byte aligned; dx: [M][Cin] bfloat16, pitch lddx, or NULL; da: float32
  *  [adapters][rank][Cin], db: float32 [adapters][Cout][rank], overwritten (zeros for a variant without rows), or NULL.  x is read for da, t for db.  Sums over rows are
  *  taken in a fixed order: the same result on every run.  W itself and the bias take no gradient here (dr_conv_wgrad, dr_regress_grad).
- *  dx may not overlap an input.  With M = 0 or without segments da and db are zeros.  Workspace and errors as dr_adapter.                                  */
+ *  The drop_* fields and *step are those of the forward pass: the mask is drawn again.  dx may not overlap an input.  With M = 0 or without segments
+ *  da and db are zeros.  Workspace and errors as dr_adapter; about 16 M + 12 M rank bytes, b once more, the partial sums of da and db, and
+ *  the aligned copies (of dy too, where Cout or lddy is no multiple of 8).                                             */
 int dr_adapter_bwd_workspace_bytes(const dr_adapter_desc* desc, int M, int ldx, int lddy, size_t* bytes);
 int dr_adapter_bwd(const dr_adapter_desc* desc, int M, const void* dy, int lddy, const void* x, int ldx, const void* w,
                    const void* a, const void* b, const float* scale, int segments, const int* row_start, const int* adapter,
