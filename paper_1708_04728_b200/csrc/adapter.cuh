@@ -126,6 +126,16 @@ __device__ __forceinline__ int ap_find(ApFind& f, uint16_t* list, const int (&id
     return f.sums[0] + f.sums[1] + f.sums[2] + f.sums[3];
 }
 
+// The end of a CTA one of whose waits ran out, by all its threads: copies and MMAs in flight end within microseconds, then shared memory and TMEM may go.
+__device__ __forceinline__ void ap_settle(volatile int* abort_flag) {
+    __syncthreads();
+    if (*abort_flag) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 400000ll) {}
+        __syncthreads();
+    }
+}
+
 // Which of 8 consecutive elements, the first with number e, are kept: bit i for element e + i.
 __device__ __forceinline__ uint32_t drop_bits8(const DropKey& k, unsigned long long off, unsigned long long counter) {
     const uint4 w = drop_words(k, off, counter);

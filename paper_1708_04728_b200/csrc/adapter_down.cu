@@ -350,7 +350,7 @@ adapter_down_tile_kernel(const __grid_constant__ CUtensorMap map_z, const __grid
         }
     }
     tc_fence_before();
-    __syncthreads();
+    ap_settle(abort_flag);
     if (warp == 1) tmem_dealloc(tmem, 128);
 }
 

@@ -461,7 +461,7 @@ adapter_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
         }
     }
     tc_fence_before();
-    __syncthreads();
+    ap_settle(abort_flag);
     if (warp == 1) tmem_dealloc(tmem, (uint32_t)p.tmem_cols);
 }
 

@@ -702,7 +702,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
         if (lane == 0) tma_store_wait_all();
     }
     tc_fence_before();
-    __syncthreads();
+    ap_settle(abort_flag);
     if (PAIR) cluster_sync_all();
     if (warp == 1) {
         if (PAIR) tmem_dealloc_pair(tmem, p.tmem_cols);
@@ -925,7 +925,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         }
     }
     tc_fence_before();
-    __syncthreads();
+    ap_settle(abort_flag);
     if (p.split > 1) cluster_sync_all();
     {
         const int width = p.nt / p.split, quads = width >> 2;
@@ -1133,7 +1133,7 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
     p.b_bytes = (uint32_t)cols * 128u;
     p.stage_bytes = p.a_bytes + p.b_bytes;
     p.stages = (int)std::min<uint32_t>(AP_MAX_STAGES, AP_SMEM / p.stage_bytes);
-    p.acc_cols = 32;
+    p.acc_cols = f32 ? 32 : 64;             // the drain reads 128 bytes of results at a time, whatever the tile's width
     while ((int)p.acc_cols < (wide ? 256 : nt)) p.acc_cols *= 2;
     p.tmem_cols = p.acc_cols * (dual ? 4 : 2);
     const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes + 8 * 4096;

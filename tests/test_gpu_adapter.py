@@ -264,6 +264,44 @@ def test_many_rows(dr, M, K, N, R, adapters, kind, p):
     check_backward(dr, c, p=p)
 
 
+@pytest.mark.parametrize("M,K,N,R,adapters,kind,p", [
+    (60001, 40, 16, 8, 3, "ragged", 0.0), (40000, 72, 9, 5, 4, "inner", 0.1), (19003, 67, 131, 12, 6, "ragged", 0.1), (38001, 16, 72, 20, 3, "even", 0.0)])
+def test_many_rows_of_narrow_and_odd_layers(dr, M, K, N, R, adapters, kind, p):
+    """Several tiles to a CTA with the narrowest accumulators, and aligned copies of many rows."""
+    c = Case(M, K, N, R, adapters, kind)
+    check_forward(dr, c, p=p, relu=R == 8, f32=R == 5)
+    check_backward(dr, c, p=p)
+
+
+@pytest.mark.parametrize("M,K,N,p", [(19000, 264, 136, 0.0), (19000, 136, 264, 0.25), (19500, 1024, 1024, 0.0)])
+@pytest.mark.parametrize("f32", [False, True])
+def test_what_is_not_finite_stays_with_its_request_in_pairs(dr, M, K, N, p, f32):
+    """The same for the tiles of two CTAs, which both drain what either of them reads of a variant."""
+    c = Case(M, K, N, 16, 5, "ragged")
+    c.a[1, 3, 5], c.a[2, 15, K - 1] = np.inf, np.nan
+    c.b[2, 70, 4], c.b[0, N - 1, 15], c.b[3, 3, 0] = np.nan, -np.inf, np.inf
+    ids = np.full(M, -1)
+    for u, v, a in A.requests(c.row_start, c.ids, 5):
+        ids[u:v] = a
+    row = int(np.nonzero(ids == 4)[0][-1])
+    c.x[row, 9], c.dy[row, 11] = np.inf, np.nan
+    f = A.factors(M, K, p, 77, 5) if p else None
+    with np.errstate(invalid="ignore"):
+        y, t = A.forward(c.x, c.w, c.bias, c.a, c.b, c.scale, c.row_start, c.ids, False, f)
+        gy, gt, inside = forward(dr, c, p, f32=f32)
+        gy, y, gt, t = gy[inside], y[inside], gt[inside], t[inside]
+        assert np.array_equal(np.isfinite(gt), np.isfinite(t))
+        assert np.array_equal(np.isnan(gy), np.isnan(y)) and np.array_equal(np.isposinf(gy), np.isposinf(y)) and np.array_equal(np.isneginf(gy), np.isneginf(y))
+        clean = np.isfinite(y)
+        assert np.allclose(gy[clean], y[clean], rtol=2 * U16, atol=2 * U16)
+        tt = np.nan_to_num(A.forward(c.x, c.w, None, c.a, c.b, c.scale, c.row_start, c.ids, False, f)[1], nan=0.5, posinf=0.5, neginf=0.5)
+        tt = tt.astype(np.float32).astype(np.float64)
+        dx, da, db = A.backward(c.dy, c.x, c.w, c.a, c.b, c.scale, c.row_start, c.ids, tt, f)
+        gdx, gda, gdb, _ = backward(dr, c, tt, p)
+        for got, want in ((gdx[inside], dx[inside]), (gda, da), (gdb, db)):
+            assert np.array_equal(np.isfinite(got), np.isfinite(want))
+
+
 def test_same_on_every_run(dr):
     for M, kind in ((40, "rows"), (700, "ragged"), (3000, "one")):
         c = Case(M, 136, 200, 16, 5, kind)
