@@ -57,7 +57,8 @@ struct BackwardPlan {
     GradPlan grad;
     int Kp, Np, Rp;
     bool copy_x, copy_k, copy_dy;
-    size_t ids, u, x, w, a, dy, bt, g, bytes;
+    int ldm;                    // words of a row of the mask: whole 64 channels
+    size_t ids, u, x, w, a, dy, bt, mask, g, bytes;
 };
 static BackwardPlan backward_plan(const dr_adapter_desc* d, int M, int ldx, int lddy, int segments) {
     BackwardPlan f;
@@ -78,6 +79,8 @@ static BackwardPlan backward_plan(const dr_adapter_desc* d, int M, int ldx, int 
     f.a = at.take(f.copy_k ? (size_t)d->adapters * d->rank * f.Kp * 2 : 0);
     f.dy = at.take(f.copy_dy ? (size_t)M * f.Np * 2 : 0);
     f.bt = at.take((size_t)d->adapters * d->rank * f.Np * 2);
+    f.ldm = (d->Cin + 63) / 64 * 2;
+    f.mask = at.take(d->drop_p > 0.f ? (size_t)M * f.ldm * 4 : 0);
     f.g = at.take(f.grad.bytes);
     f.bytes = at.bytes;
     return f;
@@ -133,7 +136,7 @@ extern "C" int dr_adapter(const dr_adapter_desc* d, int M, const void* x, int ld
     char* const ws = (char*)workspace;
     const int K = d->Cin, N = d->Cout, R = d->rank;
     const AdRows rows = {M, segments, d->adapters, row_start, adapter};
-    const DropKey key = drop_key(d->drop_p, d->drop_seed, d->drop_offset, step), none = drop_key(0., 0, 0, nullptr);
+    const DropKey key = drop_key(d->drop_p, d->drop_seed, d->drop_offset, step);
     const __nv_bfloat16 *xp, *wp, *ap;
     size_t ldxp, ldwp, ldap;
     Aligner al(ws);
@@ -145,7 +148,7 @@ extern "C" int dr_adapter(const dr_adapter_desc* d, int M, const void* x, int ld
     int* const ids = (int*)(ws + f.ids);
     rc = adapter_down_run(f.down, rows, K, R, f.Rp, xp, ldxp, ap, ldap, key, key.thr ? key.scale : 1.f, scale, 1.f, f.terms, tw, t, ids, false, s);
     if (rc != DR_OK) return rc;
-    const ProductArgs g = {rows, K, N, R, f.Rp, xp, wp, (const __nv_bfloat16*)b, ldxp, ldwp, 0, ids, tw, f.terms, bias, d->flags, y, (size_t)ldy, false, none};
+    const ProductArgs g = {rows, K, N, R, f.Rp, xp, wp, (const __nv_bfloat16*)b, ldxp, ldwp, 0, ids, tw, f.terms, bias, d->flags, y, (size_t)ldy, false, nullptr, 0};
     return adapter_product_run(g, true, s);
 }
 
@@ -187,16 +190,17 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     const bool grads = da || db, u_wanted = dx || da;
     __nv_bfloat16* const bt = (__nv_bfloat16*)(ws + f.bt);
     __nv_bfloat16* const terms = (__nv_bfloat16*)(ws + f.g + f.grad.terms);
+    uint32_t* const mask = key.thr && u_wanted ? (uint32_t*)(ws + f.mask) : nullptr;
     rc = adapter_prep_run(rows, grads ? (int*)(ws + f.g + f.grad.perm) : nullptr, (int*)(ws + f.g + f.grad.start), N, R, f.Rp, (const __nv_bfloat16*)b,
-                          u_wanted ? bt : nullptr, f.Np, t, scale, db ? terms : nullptr, s);
+                          u_wanted ? bt : nullptr, f.Np, t, scale, db ? terms : nullptr, key, K, mask, f.ldm, s);
     if (rc != DR_OK) return rc;
     if (u_wanted && (rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, scale, kept, 3, u, nullptr, ids, true, s)) != DR_OK) return rc;
     if (dx) {
-        const ProductArgs g = {rows, N, K, R, f.Rp, dyp, wp, ap, lddyp, ldwp, ldap, ids, u, 3, nullptr, 0, dx, (size_t)lddx, true, key};
+        const ProductArgs g = {rows, N, K, R, f.Rp, dyp, wp, ap, lddyp, ldwp, ldap, ids, u, 3, nullptr, 0, dx, (size_t)lddx, true, mask, f.ldm};
         if ((rc = adapter_product_run(g, true, s)) != DR_OK) return rc;
     }
     if (da || db) {
-        const GradJob jobs[2] = {{K, xp, ldxp, u, key, da, 0}, {N, dyp, lddyp, terms, none, db, 1}};
+        const GradJob jobs[2] = {{K, xp, ldxp, u, mask, f.ldm, da, 0}, {N, dyp, lddyp, terms, nullptr, 0, db, 1}};
         if ((rc = adapter_grad_run(f.grad, rows, R, jobs, ws + f.g, true, s)) != DR_OK) return rc;
     }
     return DR_OK;

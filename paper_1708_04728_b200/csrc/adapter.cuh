@@ -223,7 +223,8 @@ struct ProductArgs {
     void* out;
     size_t ldo;
     bool transposed;
-    DropKey key;                // thr 0: D is the identity (the forward pass')
+    const uint32_t* mask;       // bits of what D keeps, rows of ldm words; nullptr: D is the identity (the forward pass')
+    int ldm;
 };
 int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s);
 
@@ -233,7 +234,8 @@ struct GradJob {
     const __nv_bfloat16* z;
     size_t ldz;
     const __nv_bfloat16* p;     // P as three bfloat16 values, [M][3][Rp]
-    DropKey key;
+    const uint32_t* mask;       // as in ProductArgs
+    int ldm;
     float* out;                 // [adapters][R][C], or [adapters][C][R] where swap
     int swap;
 };
@@ -241,9 +243,9 @@ struct GradPlan { int tiles, splits, rn, rchunks; size_t perm, start, terms, par
 GradPlan adapter_grad_plan(int M, int R, int adapters, const int C[2]);
 int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const GradJob jobs[2], char* ws, bool overlap, cudaStream_t s);
 // in one launch, each where its result is wanted: the rows sorted by adapter (perm, start), b [adapters][N][R] turned to bt [adapters][R][ldb] with zeros
-// behind N, scale_a t as three bfloat16 values
+// behind N, scale_a t as three bfloat16 values, the dropout's mask over [M][K] (a bit each: drawn once, and read by both products that want it)
 int adapter_prep_run(const AdRows& rows, int* perm, int* start, int N, int R, int Rp, const __nv_bfloat16* b, __nv_bfloat16* bt, size_t ldb, const float* t,
-                     const float* scale, __nv_bfloat16* terms, cudaStream_t s);
+                     const float* scale, __nv_bfloat16* terms, const DropKey& key, int K, uint32_t* mask, int ldm, cudaStream_t s);
 
 // rows of `cols` elements, `ld` apart, as rows of ldd >= cols (a multiple of 8) with zeros behind them; at most four tensors
 struct AlignJob { const __nv_bfloat16* src; size_t ld; __nv_bfloat16* dst; size_t ldd, rows; int cols; };

@@ -11,7 +11,8 @@
 // rows that are neighbours in the tensor as one box, others gathered four at a time, with zeros for rows behind the last.  A thread takes about 100 cycles
 // to issue one of these, whatever it brings (16384 x 4096 x 4096 with 112 gathers a stage 319 us, with 28 boxes 129), hence the larger boxes
 // and three issuing warps.  P enters as three bfloat16 values, side by side, which the drain adds up.  With a
-// dropout further warps draw the mask again and clear the dropped values in place before the tile is multiplied.
+// dropout further warps clear the dropped values in place before the tile is multiplied, by a mask that is drawn once for all products that want it
+// (12544 x 2048: the generator in this kernel cost 24 us and in that of dx 11, the one pass costs 13)
 #include <algorithm>
 
 #include "adapter.cuh"
@@ -32,6 +33,9 @@ struct PrepParams {
     size_t ldb;
     const float *t, *scale;     // scale_a t as three bfloat16 values, [M][3][Rp]
     __nv_bfloat16* terms;
+    int mask_blocks, K, ldm;
+    DropKey key;
+    uint32_t* mask;             // [M][ldm]
 };
 
 // perm: rows sorted by adapter; start[a]: where adapter a's begin, start[adapters]: how many there are.  A block per adapter.
@@ -131,31 +135,51 @@ __device__ __forceinline__ void prep_terms(const PrepParams& p, int block) {
         for (int k = 0; k < 3; ++k) dst[(size_t)k * pairs] = u[k];
     }
 }
+// What the dropout keeps, 64 channels of a row to a thread: the generator's rounds depend on one another, eight draws do not.
+__device__ __forceinline__ void prep_mask(const PrepParams& p, int block) {
+    const unsigned long long off = drop_offset(p.key);
+    const int per = p.ldm >> 1;
+    const size_t n = (size_t)p.rows.M * per, stride = (size_t)p.mask_blocks * 256;
+    for (size_t i = (size_t)block * 256 + threadIdx.x; i < n; i += stride) {
+        const size_t row = i / per;
+        const unsigned long long e = (unsigned long long)row * p.K + 64 * (i - row * per);
+        const int sh = (int)(e & 7);
+        unsigned long long v = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v |= (unsigned long long)drop_bits8(p.key, off, (e >> 3) + k) << (8 * k);
+        if (sh) v = v >> sh | (unsigned long long)drop_bits8(p.key, off, (e >> 3) + 8) << (64 - sh);
+        reinterpret_cast<unsigned long long*>(p.mask)[i] = v;
+    }
+}
 __global__ void __launch_bounds__(256) adapter_prep_kernel(const PrepParams p) {
     const int b = blockIdx.x;
     grid_launch_dependents();
     if (b < p.sort_blocks) prep_sort(p.rows, p.perm, p.start, b);
     else if (b < p.sort_blocks + p.turn_blocks) prep_turn(p, b - p.sort_blocks);
-    else prep_terms(p, b - p.sort_blocks - p.turn_blocks);
+    else if (b < p.sort_blocks + p.turn_blocks + p.term_blocks) prep_terms(p, b - p.sort_blocks - p.turn_blocks);
+    else prep_mask(p, b - p.sort_blocks - p.turn_blocks - p.term_blocks);
 }
 int adapter_prep_run(const AdRows& rows, int* perm, int* start, int N, int R, int Rp, const __nv_bfloat16* b, __nv_bfloat16* bt, size_t ldb, const float* t,
-                     const float* scale, __nv_bfloat16* terms, cudaStream_t s) {
+                     const float* scale, __nv_bfloat16* terms, const DropKey& key, int K, uint32_t* mask, int ldm, cudaStream_t s) {
     PrepParams p = {};
+    p.key = key; p.K = K; p.ldm = ldm; p.mask = mask;
+    p.mask_blocks = mask ? (int)std::min<size_t>(((size_t)rows.M * (ldm >> 1) + 255) / 256, (size_t)num_sms() * 32) : 0;
     p.rows = rows;
     p.perm = perm; p.start = start; p.N = N; p.R = R; p.Rp = Rp; p.b = b; p.bt = bt; p.ldb = ldb; p.t = t; p.scale = scale; p.terms = terms;
     p.sort_blocks = perm ? rows.adapters : 0;
     p.turn_x = (int)((ldb + 31) / 32);
     p.turn_y = (R + 31) / 32;
     const long long turn = bt ? (long long)p.turn_x * p.turn_y * rows.adapters : 0, term = terms ? (rows.M + 31) / 32 : 0;
-    if (p.sort_blocks + turn + term > 0x7fffffffll) return DR_ERR_UNSUPPORTED;
+    const long long blocks = p.sort_blocks + turn + term + p.mask_blocks;
+    if (blocks > 0x7fffffffll) return DR_ERR_UNSUPPORTED;
     p.turn_blocks = (int)turn; p.term_blocks = (int)term;
-    adapter_prep_kernel<<<(unsigned)(p.sort_blocks + turn + term), 256, 0, s>>>(p);
+    adapter_prep_kernel<<<(unsigned)blocks, 256, 0, s>>>(p);
     count_launch();
     return launch_status();
 }
 
 // ---- the products ---------------------------------------------------------------------------------------------------------------------
-constexpr int GR_THREADS = 384, GR_MASKERS = 256;      // warps 0, 2, 3 load, 1 issues MMAs, 4-11 drain; 12-19 mask, where there is a dropout
+constexpr int GR_THREADS = 384, GR_MASKERS = 128;      // warps 0, 2, 3 load, 1 issues MMAs, 4-11 drain; 12-15 mask, where there is a dropout
 constexpr int GR_ROWS = 64;                            // rows of a stage
 constexpr int GR_MAX_STAGES = 8;
 constexpr int GR_SMEM = 222 * 1024;
@@ -174,7 +198,8 @@ struct GradParams {
     int* status;
     struct Job {
         int C, swap, vec;           // vec: swapped rows of whole 16 bytes
-        DropKey key;
+        const uint32_t* mask;       // rows of ldm words
+        int ldm;
         float *part, *out;
     } job[2];
 };
@@ -182,7 +207,6 @@ struct GradShared {
     uint64_t landed[GR_MAX_STAGES], full[GR_MAX_STAGES], empty[GR_MAX_STAGES], tfull, tempty;
     uint32_t tmem;
     int abort;
-    int rows[GR_MAX_STAGES][GR_ROWS];       // of the stage's tile, for the mask
 };
 
 // four rows of 64 columns from x on
@@ -229,7 +253,7 @@ adapter_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int which = (int)blockIdx.x >= p.blocks0;
     const GradParams::Job& j = p.job[which];
-    const bool drop = DROP && j.key.thr != 0;
+    const bool drop = DROP && j.mask;
     const int split = blockIdx.y, r0 = (int)blockIdx.z * p.rn, rn = min(p.rn, p.Rp - r0);
     const int c0 = ((int)blockIdx.x - (which ? p.blocks0 : 0)) * p.tiles * 128;
     volatile int* abort_flag = &sh.abort;
@@ -280,8 +304,6 @@ adapter_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
                     r[k] = group < 8 ? a : b;
                 }
                 if (!__all_sync(0xffffffffu, mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag))) { give_up(101); return false; }
-                if (drop && w == 0) { sh.rows[s][lane] = rows[0]; sh.rows[s][32 + lane] = rows[1]; }
-                __syncwarp();
                 if (lane == 0 && w == 0) mbar_expect_tx_u32(landed0 + 8 * s, (uint32_t)p.stage_bytes);
                 __syncwarp();
                 const int lead = __shfl_sync(0xffffffffu, r[0], lane & ~3);
@@ -348,45 +370,40 @@ adapter_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant
     } else if (DROP && warp >= 12) {
         // ---------------------------------------------------------------- mask: clears the dropped values of a tile
         if (drop) {
-            const unsigned long long off = drop_offset(j.key);
-            // the tile's 16-byte pieces that hold columns, dealt out to the threads; four at a time, for the generator's rounds depend on one another
-            const int per = min(p.tiles * 16, (j.C - c0 + 7) >> 3), pieces = GR_ROWS * per;
-            const int first = (int)threadIdx.x - GR_THREADS, row0 = first / per, col0 = first - row0 * per, dr = GR_MASKERS / per, dc = GR_MASKERS - dr * per;
+            // A thread has one row's 64 columns of a box, of every second box; the next tile's bits are on their way during this one.
+            const int r = ((int)threadIdx.x - GR_THREADS) & 63, box0 = ((int)threadIdx.x - GR_THREADS) >> 6, boxes = min(2 * p.tiles, (j.C - c0 + 63) >> 6);
             int s = 0;
             uint32_t ph = 0;
+            auto row_of = [&](int i, int v) { return i + r < v ? (int)min((unsigned)__ldg(p.perm + i + r), (unsigned)(p.M - 1)) : -1; };
+            auto bits_of = [&](int row, uint2 (&bits)[4]) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int b = box0 + 2 * k;
+                    bits[k] = make_uint2(0, 0);
+                    if (row >= 0 && b < boxes) bits[k] = __ldcg(reinterpret_cast<const uint2*>(j.mask + (size_t)row * j.ldm + (c0 >> 5)) + b);
+                }
+            };
             grad_ranges(p, split, [&](int, int u, int v, bool) {
+                uint2 bits[4], next[4];
+                bits_of(row_of(u, v), bits);
+                int row = row_of(u + GR_ROWS, v);
                 for (int i = u; i < v; i += GR_ROWS) {
+                    bits_of(row, next);
+                    row = row_of(i + 2 * GR_ROWS, v);
                     if (!__all_sync(0xffffffffu, mbar_wait_u32(landed0 + 8 * s, ph, abort_flag))) { give_up(105); return false; }
-                    uint8_t* const tile = gr_raw + (ring + (uint32_t)s * p.stage_bytes - smem_u32(gr_raw));
-                    int r = row0, col = col0;
-#pragma unroll 1
-                    for (int k0 = first; k0 < pieces; k0 += 4 * GR_MASKERS) {
-                        uint4* at[4];
-                        uint4 x[4];
-                        uint32_t bits[4];
-                        unsigned long long e[4];
+                    uint8_t* const tile = gr_raw + (ring + (uint32_t)s * p.stage_bytes - smem_u32(gr_raw)) + r * 128;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            if (k0 + k * GR_MASKERS < pieces) {
-                                at[k] = reinterpret_cast<uint4*>(tile + (col >> 3) * GR_BOX + r * 128 + (((col ^ r) & 7) << 4));
-                                e[k] = (unsigned long long)sh.rows[s][r] * j.C + c0 + 8 * col;
-                                x[k] = *at[k];
-                            }
-                            r += dr;
-                            col += dc;
-                            if (col >= per) { col -= per; ++r; }
-                        }
-                        if (j.C & 7) {
+                    for (int k = 0; k < 4; ++k) {
+                        if (box0 + 2 * k >= boxes) break;
+                        uint4* const at = reinterpret_cast<uint4*>(tile + (box0 + 2 * k) * GR_BOX);
+                        uint4 x[8];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) bits[k] = k0 + k * GR_MASKERS < pieces ? drop_bits8_at(j.key, off, e[k]) : 0u;
-                        } else {
+                        for (int q = 0; q < 8; ++q) x[q] = at[q ^ (r & 7)];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) bits[k] = drop_bits8(j.key, off, e[k] >> 3);
-                        }
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (k0 + k * GR_MASKERS < pieces) *at[k] = drop_apply8(x[k], bits[k]);
+                        for (int q = 0; q < 8; ++q) at[q ^ (r & 7)] = drop_apply8(x[q], (q < 4 ? bits[k].x : bits[k].y) >> (8 * (q & 3)) & 0xFFu);
                     }
+                    #pragma unroll
+                    for (int k = 0; k < 4; ++k) bits[k] = next[k];
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.full[s]);
@@ -536,7 +553,7 @@ int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const Grad
     long long most = 0;
     for (int k = 0; k < 2; ++k) {
         const GradJob& g = jobs[k];
-        p.job[k] = {g.C, g.swap, g.swap && (R & 3) == 0 && aligned16(g.out), g.key, (float*)(ws + plan.part[k]), g.out};
+        p.job[k] = {g.C, g.swap, g.swap && (R & 3) == 0 && aligned16(g.out), g.mask, g.ldm, (float*)(ws + plan.part[k]), g.out};
         blocks[k] = g.out ? (g.C + 128 * p.tiles - 1) / (128 * p.tiles) : 0;
         if (g.out) most = std::max<long long>(most, (long long)R * g.C);
     }
@@ -553,7 +570,7 @@ int adapter_grad_run(const GradPlan& plan, const AdRows& rows, int R, const Grad
         }
     }
     if (rc != DR_OK) return rc;
-    const bool drop = jobs[0].out && jobs[0].key.thr != 0;
+    const bool drop = jobs[0].out && jobs[0].mask;
     static PerDeviceFlag ready[2];
     if (!ready[drop].get()) {
         const cudaError_t e = drop ? cudaFuncSetAttribute(adapter_grad_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, GR_SMEM + 1024)

@@ -7,7 +7,7 @@
 // enters as the sum of two bfloat16 values (its columns twice, high and low), because a single one would cost the adapter's part 2^-9; of three
 // where the result is float32.
 // Where a mask lies between the adapter's product and the sum (the gradient of the input behind a dropout), that product has an accumulator of its own
-// and the drain draws the mask again.
+// and the drain picks from it by the mask's bits.
 //
 // 0 * inf is NaN: entries of f that are not finite are left out of these blocks and added, for the rows of their own adapter only, in
 // the drain.
@@ -57,7 +57,8 @@ struct ApParams {
     void* out;
     size_t ldo;
     int out_vec;                // rows of the output on 16-byte boundaries
-    DropKey key;
+    const uint32_t* mask;       // DUAL: bits of what is kept, rows of ldm words
+    int ldm;
     int* status;
 };
 
@@ -526,7 +527,6 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
         constexpr int CHUNK = TERMS == 3 ? 32 : 64;                            // columns of 128 bytes
         const float low = (p.flags & DR_RELU) ? 0.f : -INFINITY;
         const uint32_t low2 = (p.flags & DR_RELU) ? 0u : 0xFF80FF80u;
-        const unsigned long long off = DUAL ? drop_offset(p.key) : 0ull;
         int it = 0, n = 0;
         bool ok = true;
         ApInfo info;
@@ -572,6 +572,8 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                     }
                     if (!ok) break;
                 }
+                uint2 kept = make_uint2(0, 0);                                 // of this warp's 64 columns: DUAL tiles have at most 128
+                if (DUAL && ext && m < p.rows.M && n0 + 64 * side < p.C) kept = __ldcg(reinterpret_cast<const uint2*>(p.mask + (size_t)m * p.ldm + (n0 >> 5)) + side);
                 const int ab = WIDE ? part : n & 1, use = WIDE ? it : n >> 1;
                 if (!__all_sync(0xffffffffu, mbar_wait(&sh.tfull[ab], use & 1, abort_flag))) { give_up(90, tile); ok = false; break; }
                 tc_fence_after();
@@ -590,26 +592,16 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
                         for (int h = 0; h < CHUNK / 32; ++h) tmem_ld_x32(acc + c + 32 * h, w[h % (DUAL ? 1 : CHUNK / 32)]);
                     }
 #pragma unroll(DUAL ? 1 : CHUNK / 32)
-                    for (int h = 0; h < CHUNK; h += 32) {                      // rolled with a generator in it: the code has to stay in the instruction cache
+                    for (int h = 0; h < CHUNK; h += 32) {                      // rolled where it is long: the code has to stay in the instruction cache
                         uint32_t (&v)[32] = w[DUAL ? 0 : h / 32];
                         if (DUAL) tmem_ld_x32(acc + c + h, v);
-                        if (DUAL) {
-                            uint32_t bits = 0;
-                            const unsigned long long e = (unsigned long long)m * p.C + n0 + c + h;
-                            if (p.C & 7) {
-#pragma unroll 1
-                                for (int k = 0; k < 4; ++k) bits |= drop_bits8_at(p.key, off, e + 8 * k) << (8 * k);
-                            } else {                                           // the rounds of a draw depend on one another: four draws at a time
+                        const uint32_t bits = h ? kept.y : kept.x;
+                        if (DUAL && ext) {
+                            uint32_t u[32];
+                            tmem_ld_x32(acc + p.acc_cols + c + h, u);
+                            tmem_ld_wait();
 #pragma unroll
-                                for (int k = 0; k < 4; ++k) bits |= drop_bits8(p.key, off, (e >> 3) + k) << (8 * k);
-                            }
-                            if (ext) {
-                                uint32_t u[32];
-                                tmem_ld_x32(acc + p.acc_cols + c + h, u);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + (bits >> i & 1 ? __uint_as_float(u[i]) : 0.f));
-                            }
+                            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + (bits >> i & 1 ? __uint_as_float(u[i]) : 0.f));
                         }
                         tmem_ld_wait();
                         if (TERMS == 3) {
@@ -621,7 +613,7 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
 #pragma unroll 1
                             for (int i = 0; i < 32; ++i) {
                                 const int col = n0 + cb + c + h + i;
-                                const bool mine = slot >= 0 && col < p.C && (!DUAL || drop_bits8_at(p.key, off, (unsigned long long)m * p.C + col) & 1);
+                                const bool mine = slot >= 0 && col < p.C && (!DUAL || (bits >> i & 1));
                                 const float x = mine ? ap_odd<ROWS>(p, sh.list[ib][slot], m, col) : 0.f;
 #pragma unroll
                                 for (int k = 0; k < 32; ++k)
@@ -929,7 +921,6 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
     if (p.split > 1) cluster_sync_all();
     {
         const int width = p.nt / p.split, quads = width >> 2;
-        const unsigned long long off = DUAL ? drop_offset(p.key) : 0ull;
         const bool odd = sh.odd != 0;
         const float low = (p.flags & DR_RELU) ? 0.f : -INFINITY;
         for (int i = threadIdx.x; i < p.rows.M * quads; i += AP_FEW_THREADS) {
@@ -948,7 +939,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
             };
             gather(at, v);
             if (DUAL) gather(at2, u);
-            const uint32_t bits = DUAL ? drop_bits8_at(p.key, off, (unsigned long long)m * p.C + c) : 0xFu;
+            const uint32_t bits = DUAL ? __ldcg(p.mask + (size_t)m * p.ldm + (c >> 5)) >> (c & 31) : 0xFu;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (DUAL && (bits >> k & 1)) v[k] += u[k];
@@ -1051,7 +1042,7 @@ static int few_clusters(int ctas) {
 
 static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t s) {
     const int M = a.rows.M, sms = num_sms();
-    const bool dual = a.key.thr != 0;
+    const bool dual = a.mask;
     p.a_bytes = (uint32_t)((M + 7) / 8 * 8) * 128u;
     // Width of a tile and CTAs that share its l, by a model in cycles: w once from memory (3.4 KB a cycle for all SMs), a CTA's loads at 32 bytes a
     // cycle and 150 cycles a stage, 1500 for the meeting of a cluster.  For 32 x 4096 x 4096 it picks 128 columns and four CTAs, 27 us; 64 and two take 33,
@@ -1096,8 +1087,8 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
     p.rp_magic = (uint32_t)((0x100000000ull + a.Rp - 1) / a.Rp);
     p.row_id = a.row_id; p.t = a.t; p.t_terms = a.terms; p.bias = a.bias; p.f = a.f; p.ldf = a.ldf;
     p.f_vec = !a.transposed && (a.R & 7) == 0;
-    p.flags = a.flags; p.out = a.out; p.ldo = a.ldo; p.key = a.key;
-    const bool dual = a.key.thr != 0, f32 = a.flags & DR_OUT_F32;
+    p.flags = a.flags; p.out = a.out; p.ldo = a.ldo; p.mask = a.mask; p.ldm = a.ldm;
+    const bool dual = a.mask, f32 = a.flags & DR_OUT_F32;
     const size_t size = f32 ? 4 : 2;
     p.out_vec = aligned16(a.out) && (a.ldo * size) % 16 == 0;
     p.status = dev_status_ptr();
