@@ -116,7 +116,6 @@ struct ApKind {
     static constexpr bool PAIR = PAIR_, WIDE = WIDE_, ROWS = ROWS_, DUAL = DUAL_;
     static constexpr int WIDTH = TERMS == 2 ? 32 : 16;         // columns of T in a further block of 64
     static constexpr int EACH = PAIR && !WIDE ? 4 : 8;          // 16-byte pieces of a block's f that a thread brings, at most
-    static constexpr bool AHEAD = EACH == 4;                    // registers for the next block's loads beside this one's
 };
 
 // ---- the builders' steps (128 threads, bt their number) --------------------------------------------------------------------
@@ -483,40 +482,24 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
         };
         grid_dependency_wait();                                                // the rows' adapters, and t, are the kernel's in front
         ids(unit);
-        Opened now, then;
-        Block block, ahead;
+        Opened now;
         bool ok = unit < p.tiles && open(unit, 0, now);
-        if (ok && Kind::AHEAD && now.ext > 0) load(now, 0, block);
         for (int tile = unit, it = 0; ok && tile < p.tiles; tile += units, ++it) {
             if (it == 0) advance(p.kblocks);
-            // With AHEAD the next block's loads, of this tile or of the next, go out before this one is stored
-            const bool more = tile + units < p.tiles;
-            then.ext = 0;
-            bool opened = false;
+            // A block's loads go out once the one in front of it is handed over: a fence waits for what is on its way, and the next block's loads in front of
+            // it cost more than they hid: 200704 x 64 x 256 69 us, so 65
 #pragma unroll 1
             for (int e0 = 0; ok && e0 < now.ext; e0 += WIDTH) {
+                Block block;
                 uint4 tv[WIDTH / 8][TERMS];
                 ap_load_t<Kind>(now.trow, now.slot, p.Rp, e0, min(WIDTH, now.ext - e0), tv);
-                if (!Kind::AHEAD) {
-                    load(now, e0, block);
-                } else if (e0 + WIDTH < now.ext) {
-                    load(now, e0 + WIDTH, ahead);
-                } else if (more) {
-                    ok = open(tile + units, it + 1, then);
-                    opened = true;
-                    if (ok && then.ext > 0) load(then, 0, ahead);
-                }
-                ok = ok && store(now, e0, block, tv);
-                if (Kind::AHEAD) block = ahead;
+                load(now, e0, block);
+                ok = store(now, e0, block, tv);
             }
             if (!ok) break;
             if (bt == 0) mbar_arrive(&sh.built[now.at]);
             if (it > 0) advance(p.kblocks);
-            if (more && !opened) {
-                ok = open(tile + units, it + 1, then);
-                if (ok && Kind::AHEAD && then.ext > 0) load(then, 0, block);
-            }
-            now = then;
+            if (tile + units < p.tiles) ok = open(tile + units, it + 1, now);
         }
     } else if (warp >= 4) {
         // ---------------------------------------------------------------- drain: two warps to a quarter of the rows, every other 128 bytes of columns each
