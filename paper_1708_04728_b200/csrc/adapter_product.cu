@@ -813,12 +813,12 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         const int cpr = ROWS ? p.nt >> 3 : 4, cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
         const bool row_there = (uint32_t)bt * 128u < p.a_bytes;
         bool waited = false, ok = true;
-        auto load_f = [&](int e0, uint4 (&fv)[8]) { ap_load_f<Kind>(p, sh.list, e0, min(WIDTH, ext - e0), p.nt, row0, step, cj, [&](int i) { return c0 + i; }, fv); };
         uint4 fv[8];
-        if (rank * WIDTH < ext) load_f(rank * WIDTH, fv);                      // f needs no waiting, t is the kernel's in front
+        auto load_f = [&](int e0) { ap_load_f<Kind>(p, sh.list, e0, min(WIDTH, ext - e0), p.nt, row0, step, cj, [&](int i) { return c0 + i; }, fv); };
+        if (rank * WIDTH < ext) load_f(rank * WIDTH);                          // f needs no waiting, t is the kernel's in front
 #pragma unroll 1
         for (int e0 = rank * WIDTH; e0 < ext && ok; e0 += p.split * WIDTH) {
-            uint4 fn[8], tv[WIDTH / 8][TERMS];
+            uint4 tv[WIDTH / 8][TERMS];
             const int w = min(WIDTH, ext - e0);
             if (!waited) {
                 grid_dependency_wait();
@@ -837,7 +837,6 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
                 for (int k = 0; k < p.split; ++k)
                     asm volatile("red.relaxed.cluster.shared::cluster.max.s32 [%0], %1;" ::"r"(p.split > 1 ? mapa_shared(smem_u32(&sh.odd), k) : smem_u32(&sh.odd)), "r"(1) : "memory");
             }
-            if (e0 + p.split * WIDTH < ext) load_f(e0 + p.split * WIDTH, fn);  // the next block's on their way while this one is stored
             const bool slot_free = __all_sync(0xffffffffu, mbar_wait(&sh.loads, 0, abort_flag) && mbar_wait_u32(empty0 + 8 * s, ph ^ 1, abort_flag));
             if (!slot_free) give_up(96);
             if (slot_free) {
@@ -848,14 +847,26 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
             if (builders_any(!slot_free)) { ok = false; break; }
             if (bt == 0) mbar_arrive(&sh.full[s]);
             if (++s == p.stages) { s = 0; ph ^= 1; }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) fv[i] = fn[i];
+            if (e0 + p.split * WIDTH < ext) load_f(e0 + p.split * WIDTH);
         }
         if (!waited) grid_dependency_wait();
     }
     if (warp == 2 && (p.flags & DR_BIAS)) {
         const int width = p.nt / p.split;
         for (int i = lane; i < width; i += 32) sh.bias[i] = c0 + rank * width + i < p.C ? __ldg(p.bias + c0 + rank * width + i) : 0.f;
+    }
+    // the adapters' f on its way to L2 while t is still being made: the cluster's CTAs share the list
+    if (warp == 3) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&sh.ifull, 0, abort_flag))) {
+            give_up(98);
+        } else {
+            const int used = sh.ext / p.Rp, cols = min(p.nt, p.C - c0), pieces = ROWS ? p.R * ((cols + 63) >> 6) : (cols * p.R + 63) >> 6;       // lines of 128 bytes
+            for (int d = rank; d < used; d += p.split)
+                for (int i = lane; i < pieces; i += 32) {
+                    const __nv_bfloat16* at = ROWS ? p.f + ((size_t)sh.list[d] * p.R + i % p.R) * p.ldf + c0 + 64 * (i / p.R) : p.f + ((size_t)sh.list[d] * p.C + c0) * p.R + 64 * i;
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+                }
+        }
     }
     // the accumulators' rows into shared memory
     if (warp >= 4) {
