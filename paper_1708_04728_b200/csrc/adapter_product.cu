@@ -1099,14 +1099,16 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
         const long long want = std::max(1ll, sms / rows128);         // column blocks that give every SM a tile
         nt = (int)((a.C + want - 1) / want);
         nt = std::min(most, std::max(gran, (nt + gran - 1) / gran * gran));
-    } else if (a.C >= 128) {
+    } else if (a.C >= 128 && a.L >= 512 && !dual) {
+        // A pair reads less of w, but its rows are of more adapters, and behind a mask its drains bound it: 12544 x 2048 x 64 alone 38 us, by pairs 42;
+        // x 512 54 and 52; x 2048 124 and 110; with images of 49 rows x 512 65 and 71; behind a mask x 512 91 and 107, x 2048 181 and 196
         const int pn = a.C > 128 ? most : 128;
         const long long pairs = ((rows128 + 1) / 2) * ((a.C + pn - 1) / pn);
         if (pairs >= sms / 2) { pair = true; nt = pn; }
         // Out of L2 a pair's block of 256 x 256 takes 64 KB for 512 cycles of MMAs, more than the 12 TB/s that all SMs get; 256 x 512 takes 96 KB
         // for 1024, but its accumulators fill the tensor memory, so a tile's drain is only half hidden: long l.  16384 x 4096 x 4096 takes 380 us
         // instead of 509.
-        if (pair && !dual && !f32 && a.L >= 1024 && a.C >= 512 && ((rows128 + 1) / 2) * ((a.C + 511) / 512) >= sms / 2) { wide = true; nt = 512; }
+        if (pair && !f32 && a.L >= 1024 && a.C >= 512 && ((rows128 + 1) / 2) * ((a.C + 511) / 512) >= sms / 2) { wide = true; nt = 512; }
     }
     p.nt = nt;
     p.tiles_c = (a.C + nt - 1) / nt;
@@ -1131,7 +1133,7 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
     //                                     PAIR  WIDE   ROWS  DUAL TERMS
     if (a.transposed) {
         if (wide) return ap_launch<ApKind<true, true, true, false, 2>>(mz, mw, mo, p, overlap, smem, s);
-        if (pair) return dual ? ap_launch<ApKind<true, false, true, true, 2>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<true, false, true, false, 2>>(mz, mw, mo, p, overlap, smem, s);
+        if (pair) return ap_launch<ApKind<true, false, true, false, 2>>(mz, mw, mo, p, overlap, smem, s);
         return dual ? ap_launch<ApKind<false, false, true, true, 2>>(mz, mw, mo, p, overlap, smem, s) : ap_launch<ApKind<false, false, true, false, 2>>(mz, mw, mo, p, overlap, smem, s);
     }
     if (wide) return ap_launch<ApKind<true, true, false, false, 2>>(mz, mw, mo, p, overlap, smem, s);

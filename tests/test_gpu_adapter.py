@@ -265,7 +265,8 @@ def test_many_rows(dr, M, K, N, R, adapters, kind, p):
 
 
 @pytest.mark.parametrize("M,K,N,R,adapters,kind,p", [
-    (60001, 40, 16, 8, 3, "ragged", 0.0), (40000, 72, 9, 5, 4, "inner", 0.1), (19003, 67, 131, 12, 6, "ragged", 0.1), (38001, 16, 72, 20, 3, "even", 0.0)])
+    (60001, 40, 16, 8, 3, "ragged", 0.0), (40000, 72, 9, 5, 4, "inner", 0.1), (19003, 67, 131, 12, 6, "ragged", 0.1), (38001, 16, 72, 20, 3, "even", 0.0),
+    (19003, 579, 131, 12, 6, "ragged", 0.1), (19003, 131, 579, 12, 6, "ragged", 0.0)])
 def test_many_rows_of_narrow_and_odd_layers(dr, M, K, N, R, adapters, kind, p):
     """Several tiles to a CTA with the narrowest accumulators, and aligned copies of many rows."""
     c = Case(M, K, N, R, adapters, kind)
@@ -273,7 +274,7 @@ def test_many_rows_of_narrow_and_odd_layers(dr, M, K, N, R, adapters, kind, p):
     check_backward(dr, c, p=p)
 
 
-@pytest.mark.parametrize("M,K,N,p", [(19000, 264, 136, 0.0), (19000, 136, 264, 0.25), (19500, 1024, 1024, 0.0)])
+@pytest.mark.parametrize("M,K,N,p", [(19000, 264, 136, 0.0), (19000, 136, 264, 0.25), (19500, 1024, 1024, 0.0), (19000, 520, 136, 0.0), (19000, 136, 520, 0.0)])
 @pytest.mark.parametrize("f32", [False, True])
 def test_what_is_not_finite_stays_with_its_request_in_pairs(dr, M, K, N, p, f32):
     """The same for the tiles of two CTAs, which both drain what either of them reads of a variant."""
