@@ -507,8 +507,9 @@ int dr_adapter(const dr_adapter_desc* desc, int M, const void* x, int ldx, const
  *  [adapters][rank][Cin], db: float32 [adapters][Cout][rank], overwritten (zeros for a variant without rows), or NULL.  x is read for da, t for db.  Sums over rows are
  *  taken in a fixed order: the same result on every run.  W itself and the bias take no gradient here (dr_conv_wgrad, dr_regress_grad).
  *  The drop_* fields and *step are those of the forward pass: the mask is drawn again.  dx may not overlap an input.  With M = 0 or without segments
- *  da and db are zeros.  Workspace and errors as dr_adapter; about 16 M + 12 M rank bytes, b once more, the partial sums of da and db, and
- *  the aligned copies (of dy too, where Cout or lddy is no multiple of 8).                                             */
+ *  da and db are zeros.  Workspace and errors as dr_adapter; about 16 M + 12 M rank bytes, b once more, with a dropout
+ *  M Cin / 8 for its mask, the partial sums of da and db, and the aligned copies (of dy too, where Cout or lddy is no
+ *  multiple of 8).                                                                                                     */
 int dr_adapter_bwd_workspace_bytes(const dr_adapter_desc* desc, int M, int ldx, int lddy, size_t* bytes);
 int dr_adapter_bwd(const dr_adapter_desc* desc, int M, const void* dy, int lddy, const void* x, int ldx, const void* w,
                    const void* a, const void* b, const float* scale, int segments, const int* row_start, const int* adapter,

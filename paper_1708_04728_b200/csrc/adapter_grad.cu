@@ -1,5 +1,6 @@
 // The adapters' gradients, g_a[r][c] = sum over the rows m of adapter a of P[m][r] D(z)[m][c]: with P = u and z = x the first factor's,
-// with P = t and z = dy the second's.  Bound by the bytes of z.
+// with P = t and z = dy the second's.  Bound by the bytes of z: 16384 x 4096 and 4096, rank 64, in 75 us, 3.8 TB/s; 12544 x 2048 behind a dropout and 512, images of 49
+// rows, in 28.
 //
 // The rows are sorted by adapter first (an index list; order within an adapter as in the tensor).  A CTA owns a column block and an even share of the
 // sorted rows, whatever their adapters; where its share passes from one adapter to the next it writes what it has and starts over.  Share

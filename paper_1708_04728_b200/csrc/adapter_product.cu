@@ -12,6 +12,9 @@
 // 0 * inf is NaN: entries of f that are not finite are left out of these blocks and added, for the rows of their own adapter only, in
 // the drain.
 //
+// Bound by the tensor cores where l and the output are long (16384 x 4096 x 4096, rank 64: 370 us, 1.53 PFLOP/s, 0.94 of cuBLAS' rate), by the latencies of a tile's
+// further blocks and drain where l is short (200704 x 64 x 256: 41 us, 3.5 a tile, of which memory 2).
+//
 // 16 warps: 0 loads (TMA), 1 (and 2) issue MMAs, 4-11 drain, 12-15 find the rows' adapters and build the further blocks in the ring's
 // stages.  A CTA's first tile takes them behind its blocks of l, so that w streams in while t is still being made; later tiles take them in front, so
 // that they are built while the tile before is multiplied.

@@ -1,5 +1,7 @@
 // Dropout: y = residual + keep * x / (1 - p), the mask drawn by a counter-based generator (dropout.cuh) and never stored; the backward
 // pass is the same call on the gradient.
+// Bound by memory where rows allow 16-byte accesses (200704 x 256 bfloat16 with residual 59 us, 5.2 TB/s, 0.79 of a plain copy's rate), by issue slots
+// elsewhere (50176 x 333 float32 in rows of 357 36 us, 70 % of the slots busy).
 #include <algorithm>
 #include <climits>
 

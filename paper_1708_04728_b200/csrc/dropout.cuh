@@ -1,4 +1,4 @@
-// The dropout's counter-based generator, shared by the kernels that draw, or draw again, a mask: nothing of a mask is stored.
+// The dropout's counter-based generator, shared by the kernels that draw a mask or draw it again.
 //
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011) under the key `seed`.  Elements e of a
 // row-major [rows][channels] tensor are numbered by e = row * channels + channel whatever the tensor's strides; counter (e / 8, offset)
