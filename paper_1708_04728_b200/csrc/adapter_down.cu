@@ -73,7 +73,8 @@ __global__ void __launch_bounds__(256, MT == 1 && RT <= 2 && !DROP ? 4 : 0) adap
             if (r + 1 < p.R) to[1] = y;
         }
         uint32_t u[3];
-        split3(x * scale, y * scale, u[0], u[1], u[2]);
+        // columns behind the rank are zeros whatever the row or the scale holds: 0 * inf would be NaN in the whole row of the second product
+        split3(r < p.R ? x * scale : 0.f, r + 1 < p.R ? y * scale : 0.f, u[0], u[1], u[2]);
         uint32_t* to = reinterpret_cast<uint32_t*>(p.out + (size_t)(m0 + row) * p.terms * p.Rp + r);
         to[0] = u[0];
         to[p.Rp >> 1] = u[1];
@@ -333,16 +334,19 @@ adapter_down_tile_kernel(const __grid_constant__ CUtensorMap map_z, const __grid
             for (int b = 0; b < 8; ++b) {
                 const int r = r0 + 8 * b;
                 if (8 * b >= rn) break;
-                float t[8];
+                float t[8], ts[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t[i] = r + i < p.R ? sum[b][i] * p.factor : 0.f;      // columns behind the rank are the next adapter's
+                for (int i = 0; i < 8; ++i) {
+                    t[i] = sum[b][i] * p.factor;
+                    ts[i] = r + i < p.R ? t[i] * scale : 0.f;                  // columns behind the rank are the next adapter's
+                }
                 if (p.keep) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) if (r + i < p.R) p.keep[(size_t)m * p.R + r + i] = t[i];
                 }
                 uint32_t u[3][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) split3(t[2 * i] * scale, t[2 * i + 1] * scale, u[0][i], u[1][i], u[2][i]);
+                for (int i = 0; i < 4; ++i) split3(ts[2 * i], ts[2 * i + 1], u[0][i], u[1][i], u[2][i]);
                 __nv_bfloat16* to = p.out + (size_t)m * p.terms * p.Rp + r;
 #pragma unroll
                 for (int k = 0; k < 3; ++k)
