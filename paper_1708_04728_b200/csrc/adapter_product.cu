@@ -9,8 +9,9 @@
 // Where a mask lies between the adapter's product and the sum (the gradient of the input behind a dropout), that product has an accumulator of its own
 // and the drain picks from it by the mask's bits.
 //
-// 0 * inf is NaN: entries of f that are not finite are left out of these blocks and added, for the rows of their own adapter only, in
-// the drain.
+// 0 * inf is NaN: entries of f that are not finite are 1 with their sign in these blocks, and what they add is added, for the rows of their own adapter
+// only, in the drain.  Not 0: where T is infinite too the MMA would make NaN of an infinity; and where T is finite that drain makes the result an infinity
+// or NaN, whatever the 1 has added.
 //
 // Bound by the tensor cores where l and the output are long (16384 x 4096 x 4096, rank 64: 370 us, 1.53 PFLOP/s, 0.94 of cuBLAS' rate), by the latencies of a tile's
 // further blocks and drain where l is short (200704 x 64 x 256: 41 us, 3.5 a tile, of which memory 2).
@@ -104,10 +105,10 @@ __device__ __forceinline__ bool any_odd(const uint4 (&v)[N]) {
     for (int i = 0; i < N; ++i) o |= odd_halves(v[i].x) | odd_halves(v[i].y) | odd_halves(v[i].z) | odd_halves(v[i].w);
     return (o & 0x80008000u) != 0;
 }
-// entries that are not finite become zero
+// entries that are not finite become 1 with their sign
 __device__ __forceinline__ uint32_t finite_halves(uint32_t u) {
-    const uint32_t o = odd_halves(u) & 0x80008000u;
-    return u & ~((o >> 15) * 0xFFFFu);
+    const uint32_t odd = ((odd_halves(u) & 0x80008000u) >> 15) * 0x7FFFu;
+    return (u & ~odd) | (odd & 0x3F803F80u);
 }
 
 // What one kernel is compiled for.  PAIR: tiles of 256 rows by two CTAs.  WIDE (pairs): two accumulators of 256
@@ -134,7 +135,7 @@ __device__ __noinline__ uint4 ap_odd_rank(const __nv_bfloat16* src, int n) {
 }
 
 // This thread's pieces of f in the block of `eb`: rows row0 + i * step of the block (ROWS: contraction rows, else columns of the output), 16 bytes at cj;
-// column(i): the output column that place i of the CTA's is.  Returns whether one was not finite (those are made zero).
+// column(i): the output column that place i of the CTA's is.  
 template <class Kind, class Column>
 __device__ __forceinline__ void ap_load_f(const ApParams& p, const uint16_t* list, int eb, int w, int cols, int row0, int step, int cj, Column column, uint4 (&fv)[Kind::EACH]) {
     const int ef = eb + 8 * cj, df = (int)__umulhi((uint32_t)ef, p.rp_magic), rf = ef - df * p.Rp;

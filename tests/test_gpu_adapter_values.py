@@ -65,3 +65,19 @@ def test_an_infinite_scale(dr, M, K, N, R, f32):
     c = positive(M, K, N, R)
     c.scale[1] = np.inf
     both(dr, c, f32)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("M,K,N,R", SHAPES + [(19000, 1024, 1024, 16)])            # the last: pairs of CTAs, with one accumulator or two
+def test_infinities_on_both_sides_of_a_product(dr, M, K, N, R, f32):
+    """A row whose t (u) is infinite and an infinite entry of its own variant's second factor: their product is an infinity."""
+    c = positive(M, K, N, R)
+    c.x[row_of(c, 1), 9] = c.b[1, 70, R // 2] = np.inf
+    c.dy[row_of(c, 1), 11] = c.a[1, R // 2, 5] = np.inf
+    both(dr, c, f32, want=(0,))
+    # the other sign: the shared part stays finite, t is infinite by its scale
+    c = positive(M, K, N, R)
+    c.scale[1] = np.inf
+    c.b[1, 70] *= -1
+    c.b[1, 70, R // 2] = -np.inf
+    both(dr, c, f32, want=())
