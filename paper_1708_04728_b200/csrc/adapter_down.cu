@@ -7,6 +7,11 @@
 //
 // Few rows: the warps of a CTA share 16 rows and split l, a cluster of CTAs takes ranges of l (their sums meet in distributed shared memory, in
 // order), and further clusters take adapters of their own.
+//
+// The tensor cores cut their sums off instead of rounding them, about 1.5e-8 of the result for each product of 16 l in a row, so 512 l are summed at a time
+// and those sums added up in float32.  Fragments (LONG, where a warp has more l than that): in shared memory, a place for each of a thread's sums, since
+// registers for them would halve the warps of an SM.  In one sum t of 40000 x 9216 was off by 1.0e-5, and is by 5e-7; 437 us, and 440 with the adding up,
+// up to 4 % more for other sizes.
 #include <algorithm>
 
 #include "adapter.cuh"
@@ -36,10 +41,13 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+constexpr int DOWN_CHAIN = 8;                          // blocks of 64 l
+
 // MT tiles of 16 rows, RT tiles of 8 columns a warp; JOIN: the 8 warps of a CTA split l over the same rows, else each has rows of its own
-// Few rows: 64 registers, so that the next kernel's CTAs (32768 registers each) find room beside two of these.
-template <int MT, int RT, bool DROP, bool JOIN>
-__global__ void __launch_bounds__(256, MT == 1 && RT <= 2 && !DROP ? 4 : 0) adapter_down_kernel(const DownParams p) {
+// Few rows: 64 registers, so that the next kernel's CTAs (32768 registers each) find room beside two of these.  LONG: what two CTAs an SM leave, where the
+// sums without a generator fit that (20000 x 9216, rank 32: 202 us, with 132 registers 262)
+template <int MT, int RT, bool DROP, bool JOIN, bool LONG>
+__global__ void __launch_bounds__(256, LONG ? (RT <= 4 && !DROP ? 2 : 0) : MT == 1 && RT <= 2 && !DROP ? 4 : 0) adapter_down_kernel(const DownParams p) {
     __shared__ float join[JOIN ? 8 : 1][JOIN ? 16 : 1][JOIN ? RT * 8 + 2 : 1];
     __shared__ alignas(8) float range[JOIN ? 16 * RT * 8 : 1];              // this range's sums, read by the cluster
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -91,6 +99,18 @@ __global__ void __launch_bounds__(256, MT == 1 && RT <= 2 && !DROP ? 4 : 0) adap
         const float scale = (p.scale ? __ldg(p.scale + a) : 1.f) * p.after;
         float acc[MT][RT][4] = {};
         const __nv_bfloat16* f = p.f + ((size_t)a * p.R + r0 + g) * p.ldf;
+        extern __shared__ float down_sums[];                     // LONG: [MT * RT * 4][256]
+        float* const sums = down_sums + threadIdx.x;
+        int left = DOWN_CHAIN;
+        bool summed = false;
+        auto add_sums = [&]() {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[t][r][i] += sums[((t * RT + r) * 4 + i) * 256];
+        };
 #pragma unroll 1
         for (int l = l0 + (JOIN ? warp * 64 : 0); l < l1; l += JOIN ? 512 : 64) {
             uint32_t zw[MT][2][8], fw[RT][8];
@@ -133,7 +153,22 @@ __global__ void __launch_bounds__(256, MT == 1 && RT <= 2 && !DROP ? 4 : 0) adap
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
                         mma_bf16(acc[t][r], zw[t][0][2 * s], zw[t][1][2 * s], zw[t][0][2 * s + 1], zw[t][1][2 * s + 1], fw[r][2 * s], fw[r][2 * s + 1]);
+            if (LONG && --left == 0) {
+                if (summed) add_sums();
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sums[((t * RT + r) * 4 + i) * 256] = acc[t][r][i];
+                            acc[t][r][i] = 0.f;
+                        }
+                summed = true;
+                left = DOWN_CHAIN;
+            }
         }
+        if (LONG && summed) add_sums();
         if (JOIN) {
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
@@ -188,8 +223,8 @@ __global__ void __launch_bounds__(256, MT == 1 && RT <= 2 && !DROP ? 4 : 0) adap
 
 // ---- many rows, long l, ranks over 16, requests of many rows --------------------------------------------------------------------------------
 // The same product on tcgen05: a CTA takes 128 rows, z and the adapter's rows come by TMA into a ring, the accumulator (128 x rank) lies in TMEM.  Rows
-// of several adapters: the product is run once for each.  The tensor cores cut their sums off instead of rounding them, so 512 l are summed at a time
-// and the drain adds those up in float32 (all 4096 at once: 5e-6 of a gradient built on them, so 7e-7).  16384 x 4096, rank 64: 35 us, with fragments
+// of several adapters: the product is run once for each.  512 l are summed at a time and the drain adds those up in float32 (all 4096 at once: 5e-6 of a
+// gradient built on them, so 9e-7).  16384 x 4096, rank 64: 35 us, with fragments
 // from memory 82 (every 32 rows read all of an adapter).
 constexpr int DT_THREADS = 192, DT_STAGES = 4;         // warp 0 loads, 1 issues MMAs, 2-5 find the adapters and drain; two CTAs to an SM
 constexpr int DT_CHAIN = 8;                            // blocks of 64 l
@@ -403,25 +438,27 @@ DownPlan adapter_down_plan(int M, int L, int R, int adapters, int segments, bool
     return d;
 }
 
-template <int MT, int RT, bool JOIN>
+template <int MT, int RT, bool JOIN, bool LONG>
 static int down_launch(const DownPlan& d, const DownParams& p, bool overlap, cudaStream_t s) {
     const dim3 grid((unsigned)((p.rows.M + d.rows_cta - 1) / d.rows_cta), (unsigned)d.ks, (unsigned)(d.zsplit * d.rchunks));
-    auto* const k = p.key.thr ? adapter_down_kernel<MT, RT, true, JOIN> : adapter_down_kernel<MT, RT, false, JOIN>;
-    if (MT == 1) {
+    auto* const k = p.key.thr ? adapter_down_kernel<MT, RT, true, JOIN, LONG> : adapter_down_kernel<MT, RT, false, JOIN, LONG>;
+    const int smem = LONG ? MT * RT * 4 * 256 * (int)sizeof(float) : 0;
+    static PerDeviceFlag ready[2];
+    const int i = p.key.thr ? 1 : 0;
+    if ((MT == 1 || LONG) && !ready[i].get()) {
         // An SM changes how it divides its memory only when it is empty: with the largest part shared the next kernel's CTAs can begin beside this one's
-        static PerDeviceFlag ready[2];
-        const int i = p.key.thr ? 1 : 0;
-        if (!ready[i].get()) {
-            if (cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
-            ready[i].set();
-        }
+        if (MT == 1 && cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+        if (LONG && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { (void)cudaGetLastError(); return DR_ERR_CUDA; }
+        ready[i].set();
     }
-    return start_kernel(k, grid, 256, d.ks, overlap, 0, s, p);
+    return start_kernel(k, grid, 256, d.ks, overlap, smem, s, p);
 }
 template <int RT>
 static int down_launch_rt(const DownPlan& d, const DownParams& p, bool overlap, cudaStream_t s) {
-    if (d.warps_k == 1) return down_launch<2, RT, false>(d, p, overlap, s);
-    return d.mt == 2 ? down_launch<2, RT, true>(d, p, overlap, s) : down_launch<1, RT, true>(d, p, overlap, s);
+    const bool more = p.l_range > 64 * DOWN_CHAIN * d.warps_k;
+    if (d.warps_k == 1) return more ? down_launch<2, RT, false, true>(d, p, overlap, s) : down_launch<2, RT, false, false>(d, p, overlap, s);
+    if (d.mt == 2) return more ? down_launch<2, RT, true, true>(d, p, overlap, s) : down_launch<2, RT, true, false>(d, p, overlap, s);
+    return more ? down_launch<1, RT, true, true>(d, p, overlap, s) : down_launch<1, RT, true, false>(d, p, overlap, s);
 }
 
 int adapter_down_run(const DownPlan& d, const AdRows& rows, int L, int R, int Rp, const __nv_bfloat16* z, size_t ldz, const __nv_bfloat16* f, size_t ldf,
