@@ -34,8 +34,8 @@ constexpr int AP_MAX_STAGES = 16;
 constexpr int AP_SMEM = 180 * 1024;     // the ring's; with 32 KB of the drain's and the barriers' all of an SM's
 constexpr int AP_SMEM_MOST = 213 * 1024;
 constexpr int AP_TILE = 128;
-// The tensor cores cut their sums off instead of rounding them: an error of about 2e-8 of the result for each MMA in a row, 5e-6 after 4096 l.  bfloat16
-// results do not show it; for float32 ones 512 l are summed in TMEM at a time and the drain adds those up.
+// The tensor cores cut their sums off instead of rounding them: an error of about 1.5e-8 of the result for each MMA in a row, 4e-6 after 4096 l.  bfloat16
+// results do not show it; for float32 ones 512 l (in the last or first sum the adapter's 3 rank columns too) are summed in TMEM at a time and the drain adds those up.
 constexpr int AP_CHAIN = 8;             // blocks of 64 l
 
 struct ApParams {
@@ -49,6 +49,7 @@ struct ApParams {
     uint32_t acc_cols, tmem_cols;
     int split;                  // few rows: CTAs of a cluster that share a tile's l
     int accs;                   // few rows, float32 results: accumulators that share a CTA's l
+    int early;                  // where in shared memory what they held before is added up
     int cache;                  // few rows: where T is kept in shared memory, 0: nowhere
     const int* row_id;
     const __nv_bfloat16* t;     // [M][terms][Rp]
@@ -135,7 +136,7 @@ __device__ __noinline__ uint4 ap_odd_rank(const __nv_bfloat16* src, int n) {
 }
 
 // This thread's pieces of f in the block of `eb`: rows row0 + i * step of the block (ROWS: contraction rows, else columns of the output), 16 bytes at cj;
-// column(i): the output column that place i of the CTA's is.  
+// column(i): the output column that place i of the CTA's is.
 template <class Kind, class Column>
 __device__ __forceinline__ void ap_load_f(const ApParams& p, const uint16_t* list, int eb, int w, int cols, int row0, int step, int cj, Column column, uint4 (&fv)[Kind::EACH]) {
     const int ef = eb + 8 * cj, df = (int)__umulhi((uint32_t)ef, p.rp_magic), rf = ef - df * p.Rp;
@@ -694,9 +695,14 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
 // accumulators meet in distributed shared memory, where each CTA sums and finishes a part of the columns.  Rows of z behind the last are not
 // loaded: what the MMA finds there only reaches rows of the accumulator that nobody reads.  8 warps of at most 128 registers (0 loads, 1 issues MMAs, 4-7
 // build the further blocks and then drain), so that a CTA fits beside the first product's and w streams in while t is still being made.
+//
+// float32 results: sums of at most 512 l, each in the next accumulator.  Where a CTA has more of them than accumulators, the builders first add the ones in front
+// up in shared memory: the further blocks are multiplied last, so nobody waits for one who waits for them.  128 x 32768 x 9472 (rank 16) in sums
+// of 8192 was off by 2.3e-6, and is by 5.7e-7; 206 us, and 208 so.
 constexpr int AP_FEW_THREADS = 256;
+constexpr int AP_FEW_ACCS = 8;          // 256 columns: two CTAs fit an SM whatever they hold
 struct ApFewShared {
-    uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], tfull, loads, ifull;
+    uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], cfull[AP_FEW_ACCS], cempty[AP_FEW_ACCS], tfull, loads, ifull;
     uint32_t tmem;
     int abort, odd, ext;
     int slot[AP_TILE];
@@ -723,6 +729,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
     volatile int* abort_flag = &sh.abort;
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < AP_FEW_ACCS; ++i) { mbar_init(&sh.cfull[i], 1); mbar_init(&sh.cempty[i], 4); }
         mbar_init(&sh.tfull, 1);
         mbar_init(&sh.loads, 1);
         mbar_init(&sh.ifull, 128);
@@ -744,6 +751,10 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         if (!*abort_flag) report_timeout(p.status, site, tile);
         *abort_flag = 1;
     };
+
+    // float32 results: sums of `chain` blocks, each in the next accumulator; of more of them than there are accumulators, the ones in front are drained early
+    const int chain = TERMS == 3 ? min(AP_CHAIN, (kb1 - kb0 + p.accs - 1) / p.accs) : 1 << 30;
+    const int chains = TERMS == 3 ? (kb1 - kb0 + chain - 1) / chain : 1, early = chains - p.accs;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -774,8 +785,6 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
             int s = 0;
             uint32_t ph = 0, accum = 0;
             bool ok = true;
-            // float32 results: an accumulator for every so many blocks
-            const int chain = TERMS == 3 ? (kb1 - kb0 + p.accs - 1) / p.accs : 1 << 30;
             auto block = [&](uint32_t d, int n16, int site) {
                 if (!mbar_wait_u32(full0 + 8 * s, ph, abort_flag)) { give_up(site); ok = false; return; }
                 tc_fence_after();
@@ -789,15 +798,27 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
                 umma_commit_u32<false>(empty0 + 8 * s);
                 if (++s == p.stages) { s = 0; ph ^= 1; }
             };
-            for (int kb = kb0, i = 0; kb < kb1 && ok; ++kb, ++i) {
-                const int acc = TERMS == 3 ? i / chain : 0;
-                if (TERMS == 3 && i - acc * chain == 0) accum = 0;
-                block(tmem + (uint32_t)acc * p.acc_cols, kb == p.kblocks - 1 ? tail16 : 4, 93);
+            int acc = 0, use = 0;                                               // the chain's accumulator, and how often that was used
+            for (int kb = kb0, c = 0; ok; ++c) {
+                const int end = TERMS == 3 ? min(kb1, kb + chain) : kb1;
+                if (TERMS == 3 && use > 0) {
+                    if (!mbar_wait(&sh.cempty[acc], (uint32_t)(use - 1) & 1, abort_flag)) { give_up(99); ok = false; break; }
+                    tc_fence_after();
+                }
+                accum = 0;
+                const uint32_t d = tmem + (TERMS == 3 ? (uint32_t)acc * p.acc_cols : 0u);
+#pragma unroll 1
+                for (; kb < end && ok; ++kb) block(d, kb == p.kblocks - 1 ? tail16 : 4, 93);
+                if (kb >= kb1) break;
+                if (TERMS == 3) {
+                    if (c < early) umma_commit_u32<false>(smem_u32(&sh.cfull[acc]));
+                    if (++acc == p.accs) { acc = 0; ++use; }
+                }
             }
             if (ok && !mbar_wait(&sh.ifull, 0, abort_flag)) { give_up(94); ok = false; }
             const int ext = ok ? sh.ext : 0;
             if (DUAL) accum = 0;
-            const uint32_t last = TERMS == 3 ? (uint32_t)((kb1 - kb0 - 1) / chain) * p.acc_cols : 0u;
+            const uint32_t last = TERMS == 3 ? (uint32_t)acc * p.acc_cols : 0u;
             for (int e = rank * WIDTH; e < ext && ok; e += p.split * WIDTH) block(tmem + (DUAL ? p.acc_cols : last), (TERMS * min(WIDTH, ext - e) + 15) >> 4, 95);
             umma_commit_u32<false>(smem_u32(&sh.tfull));
         }
@@ -817,9 +838,39 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
         const int cpr = ROWS ? p.nt >> 3 : 4, cj = bt % cpr, row0 = bt / cpr, step = 128 / cpr;
         const bool row_there = (uint32_t)bt * 128u < p.a_bytes;
         bool waited = false, ok = true;
+        if (TERMS == 3 && early > 0) {
+            const int q = warp & 3, row = q * 32 + lane;
+            float4* const to = reinterpret_cast<float4*>(ap_raw + (ring - smem_u32(ap_raw)) + p.early + (size_t)row * pitch * 4);
+#pragma unroll 1
+            for (int c = 0, acc = 0, use = 0; c < early; ++c) {
+                if (!__all_sync(0xffffffffu, mbar_wait(&sh.cfull[acc], (uint32_t)use & 1, abort_flag))) { give_up(100); ok = false; break; }
+                tc_fence_after();
+                if (q * 32 < p.rows.M) {
+#pragma unroll 1
+                    for (int col = 0; col < p.nt; col += 16) {
+                        uint32_t v[16];
+                        tmem_ld_x16(tmem + (uint32_t)acc * p.acc_cols + ((uint32_t)(q * 32) << 16) + col, v);
+                        tmem_ld_wait();
+                        if (row < p.rows.M) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                float4 x = c ? to[col / 4 + i] : make_float4(0.f, 0.f, 0.f, 0.f);
+                                x.x += __uint_as_float(v[4 * i]); x.y += __uint_as_float(v[4 * i + 1]); x.z += __uint_as_float(v[4 * i + 2]); x.w += __uint_as_float(v[4 * i + 3]);
+                                to[col / 4 + i] = x;
+                            }
+                        }
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.cempty[acc]);
+                if (++acc == p.accs) { acc = 0; ++use; }
+            }
+            ok = !builders_any(!ok);
+        }
         uint4 fv[8];
         auto load_f = [&](int e0) { ap_load_f<Kind>(p, sh.list, e0, min(WIDTH, ext - e0), p.nt, row0, step, cj, [&](int i) { return c0 + i; }, fv); };
-        if (rank * WIDTH < ext) load_f(rank * WIDTH);                          // f needs no waiting, t is the kernel's in front
+        if (ok && rank * WIDTH < ext) load_f(rank * WIDTH);                    // f needs no waiting, t is the kernel's in front
 #pragma unroll 1
         for (int e0 = rank * WIDTH; e0 < ext && ok; e0 += p.split * WIDTH) {
             uint4 tv[WIDTH / 8][TERMS];
@@ -890,14 +941,25 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_const
                         tmem_ld_x32(tmem + (uint32_t)k * p.acc_cols + ((uint32_t)(q * 32) << 16) + c, v);
                         tmem_ld_wait();
                         if (TERMS == 3) {
-                            const int chain = (kb1 - kb0 + p.accs - 1) / p.accs, accs = (kb1 - kb0 + chain - 1) / chain;
 #pragma unroll 1
-                            for (int a = 1; a < accs; ++a) {
+                            for (int a = 1; a < min(chains, p.accs); ++a) {
                                 uint32_t w[32];
                                 tmem_ld_x32(tmem + (uint32_t)a * p.acc_cols + ((uint32_t)(q * 32) << 16) + c, w);
                                 tmem_ld_wait();
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
+                            }
+                            if (early > 0 && row < p.rows.M) {
+                                const float4* from = reinterpret_cast<const float4*>(ap_raw + (ring - smem_u32(ap_raw)) + p.early + (size_t)row * pitch * 4 + c * 4);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    if (c + 4 * i >= p.nt) break;
+                                    const float4 x = from[i];
+                                    v[4 * i] = __float_as_uint(__uint_as_float(v[4 * i]) + x.x);
+                                    v[4 * i + 1] = __float_as_uint(__uint_as_float(v[4 * i + 1]) + x.y);
+                                    v[4 * i + 2] = __float_as_uint(__uint_as_float(v[4 * i + 2]) + x.z);
+                                    v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + x.w);
+                                }
                             }
                         }
                         if (row < p.rows.M) {
@@ -1059,14 +1121,17 @@ static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t
     p.tiles = p.tiles_c;
     p.b_bytes = (uint32_t)p.nt * 128u;
     p.stage_bytes = p.a_bytes + p.b_bytes;
-    const uint32_t slack = 16384u - p.a_bytes;                                // the MMA reads 128 rows from the last stage on
-    p.stages = (int)std::min<uint32_t>(AP_MAX_STAGES, (AP_SMEM - slack) / p.stage_bytes);
     p.acc_cols = std::max(32, p.nt);
-    p.accs = f32 ? std::min(256u / p.acc_cols, (uint32_t)std::max(1, (p.kblocks / p.split + AP_CHAIN) / AP_CHAIN)) : 1;
+    const int blocks = (p.kblocks + p.split - 1) / p.split;                   // of a CTA, at most
+    p.accs = f32 ? std::min(256 / (int)p.acc_cols, blocks / AP_CHAIN + 1) : 1;
     p.tmem_cols = p.acc_cols * (dual ? 2 : 1);
     while (p.tmem_cols < p.acc_cols * p.accs) p.tmem_cols *= 2;
-    const size_t ring = (size_t)p.stages * p.stage_bytes + slack, sums = (size_t)M * (p.nt + 4) * 4 * (dual ? 2 : 1);
-    const size_t rows_t = (size_t)(M + 7) / 8 * 8 * a.terms * a.Rp * 2, behind = std::max(ring, sums);
+    const size_t sums = (size_t)M * (p.nt + 4) * 4 * (dual ? 2 : 1), early = f32 && blocks > p.accs * AP_CHAIN ? sums : 0;
+    const uint32_t slack = 16384u - p.a_bytes;                                // the MMA reads 128 rows from the last stage on
+    p.stages = (int)std::min<uint32_t>(AP_MAX_STAGES, (std::min<uint32_t>(AP_SMEM, AP_SMEM_MOST - 1024 - (uint32_t)early) - slack) / p.stage_bytes);
+    const size_t ring = (size_t)p.stages * p.stage_bytes + slack;
+    const size_t rows_t = (size_t)(M + 7) / 8 * 8 * a.terms * a.Rp * 2, behind = std::max(ring, sums) + early;
+    p.early = (int)(behind - early);
     p.cache = behind + rows_t <= AP_SMEM_MOST - 1024 ? (int)behind : 0;
     const size_t smem = 1024 + behind + (p.cache ? rows_t : 0);
     alignas(64) CUtensorMap mz, mw;

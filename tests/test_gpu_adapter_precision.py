@@ -105,3 +105,25 @@ def test_gradients_of_a_wide_layer(dr, M, N, R, segments):
     """u's precision is da's: a sum of up to 512 l in a row, then one of up to 512 rows."""
     da, db = Layer(dr, M, 64, N, R, segments, 0.0, 1.0).backward(dr)
     assert da <= cut(CHAIN) + cut(CHAIN) and db <= cut(CHAIN), (da, db)
+
+
+# up to 128 rows (with more sums than accumulators, too), tiles of one CTA, pairs with several tiles to each
+Y = [(1, 16384, 8192, 16, 1), (32, 9216, 4096, 8, 3), (128, 32768, 9472, 16, 1), (128, 32768, 1000, 8, 5), (40, 65536, 520, 8, 4), (7, 4096, 24, 16, 2), (300, 4096, 200, 8, 2),
+     (5000, 9216, 256, 24, 4), (19000, 4096, 1024, 64, 1), (19000, 1024, 1024, 16, 5)]
+
+
+@pytest.mark.parametrize("shared", [2.0 ** 6, 2.0 ** -6])
+@pytest.mark.parametrize("M,K,N,R,segments", Y)
+def test_float32_results(dr, M, K, N, R, segments, shared):
+    """Nearly all of y the shared part's, or the adapters' (which t's precision is part of); their 3 R columns end or begin one of the sums."""
+    y, t = Layer(dr, M, K, N, R, segments, 0.0, shared).forward(dr)
+    assert y <= cut(CHAIN + (3 * R + 15) // 16) + (2.0 ** -5 if shared > 1 else 1) * cut(CHAIN), y
+
+
+@pytest.mark.parametrize("M", [32, 200])
+def test_three_terms(dr, M):
+    """Sums so short that a factor of 16 bits instead of 24 (2.5e-6 of the result for normal numbers) shows."""
+    y, t = Layer(dr, M, 64, 96, 16, 2, 0.0, 2.0 ** -6).forward(dr)
+    assert y <= cut(4 + 3) + cut(4) < 1e-6, y
+    da, db = Layer(dr, M, 64, 96, 16, 2, 0.0, 1.0).backward(dr)
+    assert da <= cut(7) + cut(6) < 1e-6 and db <= cut(7) < 1e-6, (da, db)
