@@ -41,7 +41,8 @@ struct PrepParams {
 
 // perm: rows sorted by adapter; start[a]: where adapter a's begin, start[adapters]: how many there are.  A block per adapter.
 __device__ __forceinline__ void prep_sort(const AdRows& r, int* __restrict__ perm, int* __restrict__ start, int a) {
-    __shared__ int sum_own[8], sum_less[8];
+    __shared__ long long sum_own[8];
+    __shared__ int sum_less[8];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     auto length = [&](int s, int& id, int& first) {
         if (s >= r.segments) { id = ROW_NONE; first = 0; return 0; }
@@ -60,7 +61,7 @@ __device__ __forceinline__ void prep_sort(const AdRows& r, int* __restrict__ per
         if (id == a) own += n;
     }
     for (int o = 16; o; o >>= 1) { less += __shfl_xor_sync(0xffffffffu, less, o); own += __shfl_xor_sync(0xffffffffu, own, o); }
-    if (lane == 0) { sum_less[warp] = (int)min(less, (long long)r.M); sum_own[warp] = (int)min(own, (long long)r.M); }
+    if (lane == 0) { sum_less[warp] = (int)min(less, (long long)r.M); sum_own[warp] = own; }
     __syncthreads();
     long long base = 0, count = 0;
     for (int w = 0; w < 8; ++w) { base += sum_less[w]; count += sum_own[w]; }
@@ -75,24 +76,24 @@ __device__ __forceinline__ void prep_sort(const AdRows& r, int* __restrict__ per
         int id, first;
         int n = length(s0 + (int)threadIdx.x, id, first);
         if (id != a) n = 0;
-        int incl = n;
+        long long incl = n;                                      // of offsets that decrease every request may have all M rows: 32 bits would not hold the sum
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            const long long v = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += v;
         }
         __syncthreads();
         if (lane == 31) sum_own[warp] = incl;
         __syncthreads();
-        int at = incl - n, total = 0;
+        long long at = incl - n, total = 0;
         for (int w = 0; w < 8; ++w) { if (w < warp) at += sum_own[w]; total += sum_own[w]; }
         // a warp writes the rows of its own segments one after the other
         for (unsigned some = __ballot_sync(0xffffffffu, n > 0); some; some &= some - 1) {
             const int k = __ffs(some) - 1;
-            const int len = __shfl_sync(0xffffffffu, n, k), f = __shfl_sync(0xffffffffu, first, k);
+            const int f = __shfl_sync(0xffffffffu, first, k);
             const long long to = base + __shfl_sync(0xffffffffu, at, k);
-            for (int i = lane; i < len; i += 32)
-                if (to + i < r.M) perm[to + i] = f + i;
+            const long long len = min((long long)__shfl_sync(0xffffffffu, n, k), r.M - to);        // 0 or less behind the end of the list
+            for (int i = lane; i < len; i += 32) perm[to + i] = f + i;
         }
         base += total;
     }
