@@ -490,7 +490,7 @@ int dr_dropout(size_t rows, int C, const void* x, int ldx, const void* residual,
 #define DR_ADAPTER_MAX_RANK     256
 #define DR_ADAPTER_MAX_CHANNELS 65536
 #define DR_ADAPTER_MAX_ADAPTERS 4096
-#define DR_ADAPTER_MAX_ROWS     (1 << 30)
+#define DR_ADAPTER_MAX_ROWS     (1 << 30)  /* and requests */
 typedef struct dr_adapter_desc {
     int Cin, Cout, rank, adapters;
     unsigned flags;                        /* DR_BIAS | DR_RELU | DR_OUT_F32; the backward pass does not look at them */

@@ -124,6 +124,7 @@ extern "C" int dr_adapter(const dr_adapter_desc* d, int M, const void* x, int ld
     int rc = desc_check(d, M);
     if (rc != DR_OK) return rc;
     if (ld_check(&ldx, d->Cin) != DR_OK || ld_check(&ldy, d->Cout) != DR_OK || segments < 0) return DR_ERR_INVALID_ARG;
+    if (segments > DR_ADAPTER_MAX_ROWS) return DR_ERR_UNSUPPORTED;
     if (M == 0 || segments == 0) return DR_OK;
     if (!x || !w || !a || !b || !y || !row_start || !adapter || !workspace || ((d->flags & DR_BIAS) && !bias)) return DR_ERR_INVALID_ARG;
     if (!aligned16(x) || !aligned16(w) || !aligned16(a) || !aligned16(b) || ((uintptr_t)y & ((d->flags & DR_OUT_F32) ? 3 : 1)) || ((uintptr_t)bias & 3) ||
@@ -158,6 +159,7 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     int rc = desc_check(d, M);
     if (rc != DR_OK) return rc;
     if (ld_check(&ldx, d->Cin) != DR_OK || ld_check(&lddx, d->Cin) != DR_OK || ld_check(&lddy, d->Cout) != DR_OK || segments < 0) return DR_ERR_INVALID_ARG;
+    if (segments > DR_ADAPTER_MAX_ROWS) return DR_ERR_UNSUPPORTED;              // numbers of requests are counted in 32 bits, 256 ahead
     if (((uintptr_t)da & 3) || ((uintptr_t)db & 3)) return DR_ERR_ALIGNMENT;
     const cudaStream_t s = (cudaStream_t)stream;
     const int K = d->Cin, N = d->Cout, R = d->rank;

@@ -18,7 +18,7 @@ struct AdRows {
 // Number of offsets row_start[lo .. hi) that are <= m, plus lo, by binary search.  Whatever the offsets hold, the search stays inside them.
 __device__ __forceinline__ int offsets_upto(const AdRows& r, int m, int lo, int hi) {
     while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
+        const int mid = lo + ((hi - lo) >> 1);
         if (__ldg(r.row_start + mid) <= m) lo = mid + 1;
         else hi = mid;
     }
