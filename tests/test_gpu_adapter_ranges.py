@@ -30,3 +30,46 @@ def test_offsets_that_decrease_over_many_rows(dr):
     assert dr.dr_device_status()[0] == 0
     # the first request has every row already: the list is that of a single request
     assert torch.equal(out[0][1], out[1][1]) and not out[0][0][0].any() and bool(torch.isfinite(out[0][0]).all())
+
+
+@pytest.mark.parametrize("M", [90, 300, 2500])
+def test_many_empty_requests_among_neighbouring_rows(dr, M):
+    """More offsets between the first and the last row of a warp than it counts out of registers."""
+    rng = np.random.default_rng(M)
+    c = Case(M, 72, 40, 8, 5)
+    cuts = np.concatenate([[0] * 3, [10] * 100, [11] * 40, [12, 30], np.sort(rng.integers(30, M - 3, 70)), [M // 2] * 200, [M - 3] * 33])
+    c.row_start = np.sort(cuts).tolist()
+    c.ids = rng.integers(-1, 5, len(cuts) - 1).tolist()
+    check_forward(dr, c)
+    check_backward(dr, c)
+
+
+@pytest.mark.parametrize("K", [8200, 8203])
+def test_elements_beyond_32_bits(dr, K):
+    """x of more than 2^32 elements behind a dropout: the first rows and the last ones, which are a variant's own, forward and backward."""
+    import torch
+    M, N, R, own, p, seed, offset = 530000, 16, 8, 5, 0.25, 31, 32
+    g = torch.Generator(device="cuda")
+    g.manual_seed(K)
+    normal = lambda s, *shape: (s * torch.randn(shape, generator=g, device="cuda")).to(torch.bfloat16)
+    x, dy = torch.empty((M, K), dtype=torch.bfloat16, device="cuda").normal_(generator=g), normal(1, M, N)
+    w, a, b = normal(K ** -0.5, N, K), normal(K ** -0.5, 2, R, K), normal(R ** -0.5, 2, N, R)
+    row_start, ids = ints([0, M - own, M]), ints([0, 1])
+    d = dr.dr_adapter_desc(Cin=K, Cout=N, rank=R, adapters=2, flags=dr.DR_OUT_F32, drop_p=p, drop_seed=seed, drop_offset=offset)
+    ws = torch.empty(max(dr.dr_adapter_workspace_bytes(d, M), dr.dr_adapter_bwd_workspace_bytes(d, M)), dtype=torch.uint8, device="cuda")
+    y, t = torch.empty((M, N), device="cuda"), torch.empty((M, R), device="cuda")
+    dr.dr_adapter(d, M, x, 0, w, None, a, b, None, 2, row_start, ids, y, 0, t, None, ws, ws.numel())
+    dx, da, db = torch.empty_like(x), torch.empty((2, R, K), device="cuda"), torch.empty((2, N, R), device="cuda")
+    dr.dr_adapter_bwd(d, M, dy, 0, x, 0, w, a, b, None, 2, row_start, ids, t, dx, 0, da, db, None, ws, ws.numel())
+    host = lambda v: v.double().cpu().numpy()
+    hw, ha, hb = host(w), host(a), host(b)
+    for first, rows, variant in ((0, 3, 0), (M - own, own, 1)):
+        part = slice(first, first + rows)
+        f = A.factors(rows, K, p, seed, offset, first=first * K)
+        hx, hdy, ht = host(x[part]), host(dy[part]), host(t[part])
+        ry, rt = A.forward(hx, hw, None, ha, hb, None, [0, rows], [variant], False, f)
+        # float32 sums of K products of numbers of both signs: their size is about that of the result, their rounding far below 1e-5 of it
+        assert np.linalg.norm(ht - rt) <= 1e-5 * np.linalg.norm(rt) and np.linalg.norm(host(y[part]) - ry) <= 1e-5 * np.linalg.norm(ry)
+        rdx, rda, rdb = A.backward(hdy, hx, hw, ha, hb, None, [0, rows], [variant], ht, f)
+        assert np.linalg.norm(host(dx[part]) - rdx) <= 2.0 ** -8 * np.linalg.norm(rdx)          # bfloat16: half a unit in the last place
+    assert np.linalg.norm(host(da[1]) - rda[1]) <= 1e-5 * np.linalg.norm(rda[1]) and np.linalg.norm(host(db[1]) - rdb[1]) <= 1e-5 * np.linalg.norm(rdb[1])
