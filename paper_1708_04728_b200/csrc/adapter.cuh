@@ -157,15 +157,10 @@ __device__ __forceinline__ uint4 drop_apply8(uint4 v, uint32_t bits) {
     return make_uint4(two(v.x, bits), two(v.y, bits >> 2), two(v.z, bits >> 4), two(v.w, bits >> 6));
 }
 
-// Two float32 values as sums of two bfloat16 values each (16 to 17 significant bits), or of three (all 24): packed in pairs.
-__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
-    hi = pack_bf16(a, b);
-    // an infinity (or what rounds to one) has no remainder: inf - inf would be NaN
-    const float ra = a - bf16_lo(hi), rb = b - bf16_hi(hi);
-    lo = pack_bf16(fabsf(bf16_lo(hi)) <= 3.4e38f ? ra : 0.f, fabsf(bf16_hi(hi)) <= 3.4e38f ? rb : 0.f);
-}
+// Two float32 values as sums of three bfloat16 values each (all 24 bits; the first two of them alone 16 to 17), packed in pairs.
 __device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
     hi = pack_bf16(a, b);
+    // an infinity (or what rounds to one) has no remainder: inf - inf would be NaN
     const float ra = fabsf(bf16_lo(hi)) <= 3.4e38f ? a - bf16_lo(hi) : 0.f, rb = fabsf(bf16_hi(hi)) <= 3.4e38f ? b - bf16_hi(hi) : 0.f;
     mid = pack_bf16(ra, rb);
     lo = pack_bf16(ra - bf16_lo(mid), rb - bf16_hi(mid));
