@@ -187,7 +187,8 @@ constexpr int GR_MAX_STAGES = 8;
 constexpr int GR_SMEM = 222 * 1024;
 constexpr int GR_BOX = GR_ROWS * 128;
 // Rows summed in TMEM at a time: the tensor cores cut their sums off instead of rounding them, so an error grows with the number of MMAs in a row;
-// longer sums are added up in float32 by the drain.  16384 rows of eight adapters: 7e-7 of the result with 512 rows at a time, over 1e-6 with all 2048.
+// longer sums are added up in float32 by the drain.  Sums of 16384 rows and more are off by 5e-7 so, da
+// (whose u is such a sum too) by 9e-7; with all 2048 rows of an adapter in one it was over 1e-6.
 constexpr int GR_CHAIN = 512;
 
 struct GradParams {

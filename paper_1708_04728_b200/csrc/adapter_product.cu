@@ -14,7 +14,7 @@
 // or NaN, whatever the 1 has added.
 //
 // Bound by the tensor cores where l and the output are long (16384 x 4096 x 4096, rank 64: 370 us, 1.53 PFLOP/s, 0.94 of cuBLAS' rate), by the latencies of a tile's
-// further blocks and drain where l is short (200704 x 64 x 256: 41 us, 3.5 a tile, of which memory 2).
+// further blocks and drain where l is short (200704 x 64 x 256: 41 us, 3.5 a tile, of which memory 2).  The kernels of two accumulators spill 56 bytes a thread, transposed 88.
 //
 // 16 warps: 0 loads (TMA), 1 (and 2) issue MMAs, 4-11 drain, 12-15 find the rows' adapters and build the further blocks in the ring's
 // stages.  A CTA's first tile takes them behind its blocks of l, so that w streams in while t is still being made; later tiles take them in front, so
@@ -1105,8 +1105,8 @@ static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t
     const bool dual = a.mask;
     p.a_bytes = (uint32_t)((M + 7) / 8 * 8) * 128u;
     // Width of a tile and CTAs that share its l, by a model in cycles: w once from memory (3.4 KB a cycle for all SMs), a CTA's loads at 32 bytes a
-    // cycle and 150 cycles a stage, 1500 for the meeting of a cluster.  For 32 x 4096 x 4096 it picks 128 columns and four CTAs, 27 us; 64 and two take 33,
-    // 32 alone 50, 128 alone 57.
+    // cycle and 150 cycles a stage, 1500 for the meeting of a cluster.  For 32 x 4096 x 4096 it picks 128 columns and four CTAs, 24.6 us; measured when
+    // that took 27, 64 and two took 33, 32 alone 50, 128 alone 57.
     double best = 0.;
     const bool f32 = a.flags & DR_OUT_F32;
     for (int nt = a.transposed ? 64 : 16; nt <= (f32 ? 64 : 128); nt *= 2)
@@ -1170,12 +1170,13 @@ int adapter_product_run(const ProductArgs& a, bool overlap, cudaStream_t s) {
         nt = std::min(most, std::max(gran, (nt + gran - 1) / gran * gran));
     } else if (a.C >= 128 && a.L >= 512 && !dual) {
         // A pair reads less of w, but its rows are of more adapters, and behind a mask its drains bound it: 12544 x 2048 x 64 alone 38 us, by pairs 42;
-        // x 512 54 and 52; x 2048 124 and 110; with images of 49 rows x 512 65 and 71; behind a mask x 512 91 and 107, x 2048 181 and 196
+        // x 512 54 and 52; x 2048 124 and 110; with images of 49 rows x 512 65 and 71 (l alone
+        // does not tell, and the rule takes the pair there); behind a mask x 512 91 and 107, x 2048 181 and 196
         const int pn = a.C > 128 ? most : 128;
         const long long pairs = ((rows128 + 1) / 2) * ((a.C + pn - 1) / pn);
         if (pairs >= sms / 2) { pair = true; nt = pn; }
         // Out of L2 a pair's block of 256 x 256 takes 64 KB for 512 cycles of MMAs, more than the 12 TB/s that all SMs get; 256 x 512 takes 96 KB
-        // for 1024, but its accumulators fill the tensor memory, so a tile's drain is only half hidden: long l.  16384 x 4096 x 4096 takes 380 us
+        // for 1024, but its accumulators fill the tensor memory, so a tile's drain is only half hidden: long l.  16384 x 4096 x 4096 takes 370 us
         // instead of 509.
         if (pair && !f32 && a.L >= 1024 && a.C >= 512 && ((rows128 + 1) / 2) * ((a.C + 511) / 512) >= sms / 2) { wide = true; nt = 512; }
     }
