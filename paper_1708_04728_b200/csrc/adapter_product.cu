@@ -700,7 +700,10 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap map_z, const __grid_c
 // up in shared memory: the further blocks are multiplied last, so nobody waits for one who waits for them.  128 x 32768 x 9472 (rank 16) in sums
 // of 8192 was off by 2.3e-6, and is by 5.7e-7; 206 us, and 208 so.
 constexpr int AP_FEW_THREADS = 256;
-constexpr int AP_FEW_ACCS = 8;          // 256 columns: two CTAs fit an SM whatever they hold
+// Two CTAs fit an SM whatever they hold of its tensor memory: 256 columns each, registers for no third, and shared memory for none either however few
+// registers a compiler takes.  A third would wait for tensor memory while its cluster's others hold theirs, and clusters might wait for one another.
+constexpr int AP_FEW_ACCS = 8;
+constexpr int AP_FEW_SMEM = 80 * 1024;
 struct ApFewShared {
     uint64_t full[AP_MAX_STAGES], empty[AP_MAX_STAGES], cfull[AP_FEW_ACCS], cempty[AP_FEW_ACCS], tfull, loads, ifull;
     uint32_t tmem;
@@ -1133,7 +1136,7 @@ static int few_run(const ProductArgs& a, ApParams& p, bool overlap, cudaStream_t
     const size_t rows_t = (size_t)(M + 7) / 8 * 8 * a.terms * a.Rp * 2, behind = std::max(ring, sums) + early;
     p.early = (int)(behind - early);
     p.cache = behind + rows_t <= AP_SMEM_MOST - 1024 ? (int)behind : 0;
-    const size_t smem = 1024 + behind + (p.cache ? rows_t : 0);
+    const size_t smem = std::max<size_t>(AP_FEW_SMEM, 1024 + behind + (p.cache ? rows_t : 0));
     alignas(64) CUtensorMap mz, mw;
     int rc = ap_map(&mz, a.z, M, a.L, a.ldz, 64, (M + 7) / 8 * 8);
     if (rc != DR_OK) return rc;

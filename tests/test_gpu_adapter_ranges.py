@@ -73,3 +73,28 @@ def test_elements_beyond_32_bits(dr, K):
         rdx, rda, rdb = A.backward(hdy, hx, hw, ha, hb, None, [0, rows], [variant], ht, f)
         assert np.linalg.norm(host(dx[part]) - rdx) <= 2.0 ** -8 * np.linalg.norm(rdx)          # bfloat16: half a unit in the last place
     assert np.linalg.norm(host(da[1]) - rda[1]) <= 1e-5 * np.linalg.norm(rda[1]) and np.linalg.norm(host(db[1]) - rdb[1]) <= 1e-5 * np.linalg.norm(rdb[1])
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 65536, 512), (20, 16384, 24), (5, 64, 20000)])
+def test_few_rows_on_three_streams(dr, M, K, N):
+    """Clusters of several calls at once share the SMs' tensor memory: all end, with the bits of a call alone."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N)
+    normal = lambda s, *shape: (s * torch.randn(shape, generator=g, device="cuda")).to(torch.bfloat16)
+    x, w, a, b = normal(1, M, K), normal(K ** -0.5, N, K), normal(K ** -0.5, 1, 16, K), normal(0.25, 1, N, 16)
+    row_start, ids = ints([0, M]), ints([0])
+    d = dr.dr_adapter_desc(Cin=K, Cout=N, rank=16, adapters=1, flags=dr.DR_OUT_F32)
+    n = dr.dr_adapter_workspace_bytes(d, M)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in streams]
+    call = lambda y, k, s: dr.dr_adapter(d, M, x, 0, w, None, a, b, None, 1, row_start, ids, y, 0, None, None, ws[k], n, s)
+    alone = torch.empty((M, N), device="cuda")
+    call(alone, 0, torch.cuda.current_stream())
+    outs = [[torch.zeros_like(alone) for _ in range(12)] for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(12):
+        for k, s in enumerate(streams):
+            call(outs[k][i], k, s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, alone) for side in outs for y in side) and dr.dr_device_status()[0] == 0
