@@ -471,8 +471,8 @@ int dr_dropout(size_t rows, int C, const void* x, int ldx, const void* residual,
  *   t = D(x) A_a^T,    y = act(x W^T + bias + scale[a] * t B_a^T),
  * D the dropout of dr_dropout (drop_p = 0: none) over the M x Cin elements of x, act ReLU with DR_RELU.
  *  Request s covers the rows row_start[s] <= m < row_start[s+1] and uses variant adapter[s]; any other number than 0 .. adapters-1 (say
- *  -1) is the shared layer alone.  row_start: `segments` + 1 non-decreasing int32 in DEVICE memory (offsets that decrease put rows into some
- *  request, and nothing is read or written out of range); adapter: int32 [segments] in device memory.  Both are read when the kernels run: a captured
+ *  -1) is the shared layer alone.  row_start: `segments` + 1 non-decreasing int32 in DEVICE memory (of offsets that decrease
+ *  the results are unspecified, and nothing is read or written out of range); adapter: int32 [segments] in device memory.  Both are read when the kernels run: a captured
  *  call serves other requests when they have changed.  Requests may be empty and share variants.  Rows of no request (in front of
  *  row_start[0], from row_start[segments] on) are left as they were in y, t and dx, and count in no gradient.
  *  x: [M][Cin] bfloat16, row pitch ldx elements (0: Cin); w: [Cout][Cin] bfloat16; bias: float32 [Cout] (with DR_BIAS); a: [adapters][rank][Cin]
