@@ -196,7 +196,10 @@ extern "C" int dr_adapter_bwd(const dr_adapter_desc* d, int M, const void* dy, i
     rc = adapter_prep_run(rows, grads ? (int*)(ws + f.g + f.grad.perm) : nullptr, (int*)(ws + f.g + f.grad.start), N, R, f.Rp, (const __nv_bfloat16*)b,
                           u_wanted ? bt : nullptr, f.Np, t, scale, db ? terms : nullptr, key, K, mask, f.ldm, s);
     if (rc != DR_OK) return rc;
-    if (u_wanted && (rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, scale, kept, 3, u, nullptr, ids, true, s)) != DR_OK) return rc;
+    // The lists are made by one block for each adapter, 4 ns for each request of the call: where they are many the first product begins once that is done, and
+    // with it the second, whose waits have a limit of two seconds.
+    const bool overlap = segments <= 1 << 22;
+    if (u_wanted && (rc = adapter_down_run(f.down, rows, N, R, f.Rp, dyp, lddyp, bt, f.Np, none, 1.f, scale, kept, 3, u, nullptr, ids, overlap, s)) != DR_OK) return rc;
     if (dx) {
         const ProductArgs g = {rows, N, K, R, f.Rp, dyp, wp, ap, lddyp, ldwp, ldap, ids, u, 3, nullptr, 0, dx, (size_t)lddx, true, mask, f.ldm};
         if ((rc = adapter_product_run(g, true, s)) != DR_OK) return rc;

@@ -98,3 +98,36 @@ def test_few_rows_on_three_streams(dr, M, K, N):
             call(outs[k][i], k, s)
     torch.cuda.synchronize()
     assert all(torch.equal(y, alone) for side in outs for y in side) and dr.dr_device_status()[0] == 0
+
+
+def test_as_many_requests_as_there_may_be(dr):
+    """2^30 requests, all but three of them empty: the backward pass' lists take seconds, longer than any wait of the kernels behind them may last."""
+    import torch
+    M, n = 300, dr.DR_ADAPTER_MAX_ROWS
+    c = Case(M, 72, 40, 8, 1)
+    bf, flat = torch.bfloat16, lambda v, t: torch.from_numpy(np.ascontiguousarray(v)).cuda().to(t).contiguous()
+    row_start, ids = torch.zeros(n + 1, dtype=torch.int32, device="cuda"), torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    row_start[n // 3 + 1:] = 100                    # request n / 3 has the rows 0 .. 99, 2 n / 3 the rows 100 .. 249, the last one 250 .. 289
+    row_start[2 * (n // 3) + 1:] = 250
+    row_start[n:] = 290
+    ids[n // 3] = ids[n - 1] = 0
+    few = ([0, 100, 250, 290], [0, -1, 0])
+    x, w, a, b, dy = (flat(v, bf) for v in (c.x, c.w, c.a, c.b, c.dy))
+    d = dr.dr_adapter_desc(Cin=72, Cout=40, rank=8, adapters=1, flags=dr.DR_OUT_F32)
+    ws = torch.empty(max(dr.dr_adapter_workspace_bytes(d, M), dr.dr_adapter_bwd_workspace_bytes(d, M)), dtype=torch.uint8, device="cuda")
+    out = []
+    for starts, variants, segments in ((row_start, ids, n), (ints(few[0]), ints(few[1]), 3)):
+        y, t, dx = (torch.full((M, k), 7.0, dtype=ty, device="cuda") for k, ty in ((40, torch.float32), (8, torch.float32), (72, bf)))
+        da, db = torch.full((1, 8, 72), 7.0, device="cuda"), torch.full((1, 40, 8), 7.0, device="cuda")
+        dr.dr_adapter(d, M, x, 0, w, None, a, b, None, segments, starts, variants, y, 0, t, None, ws, ws.numel())
+        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        begin.record()
+        dr.dr_adapter_bwd(d, M, dy, 0, x, 0, w, a, b, None, segments, starts, variants, t, dx, 0, da, db, None, ws, ws.numel())
+        end.record()
+        torch.cuda.synchronize()
+        print(f"{segments} requests: {begin.elapsed_time(end):.1f} ms")
+        assert dr.dr_device_status()[0] == 0
+        out.append((y, t, dx, da, db))
+    assert all(torch.equal(p, q) for p, q in zip(*out))
+    ry, _ = A.forward(c.x, c.w, None, c.a, c.b, None, *few, False)
+    assert np.allclose(out[0][0].double().cpu().numpy()[:290], ry[:290], rtol=1e-4, atol=1e-4)
