@@ -483,7 +483,7 @@ int dr_dropout(size_t rows, int C, const void* x, int ldx, const void* residual,
  *  Products are of bfloat16 values and sum in float32.  t and u enter the second product as the sum of two bfloat16 values (16 to 17 bits), of three
  *  (24) where y is float32 and in da and db; for float32 results (and t, u) sums longer than 512 terms are added up from parts, because the tensor cores cut
  *  theirs off instead of rounding them.  Relative error (2-norm): t and db up to 6e-7, da 1e-6, float32 y 1.2e-6 (2.2e-6 where adapters of rank 256 make
- *  most of it), whatever the lengths; bfloat16 results their rounding, behind sums that are off by 1e-9 for each of their terms.
+ *  most of it), da and db twice that of 1e8 rows of a variant; bfloat16 results their rounding, behind sums that are off by 1e-9 for each of their terms.
  *  A variant that holds a NaN or an infinity, and a row of x that does, touch no other request's rows.  y, t and dx are the infinity or NaN that the formula
  *  gives; da and db of a variant with an infinity in its rows of x or dy may be NaN where the sum is an infinity.
  *  step: NULL or a counter in device memory, as in dr_dropout.  workspace: dr_adapter_workspace_bytes bytes (for the ldx of the call), 256-byte aligned,
